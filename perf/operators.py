@@ -213,6 +213,7 @@ def _run_own(s):
 
 
 def _plain_quantize(w, group, zeros, dtype):
+    """Divisions are by tensors: a division by a Python number may be computed as a product with its reciprocal."""
     N, K = w.shape
     Kp = (K + 127) // 128 * 128
     v = torch.zeros(N, Kp, device=w.device)
@@ -220,12 +221,13 @@ def _plain_quantize(w, group, zeros, dtype):
     v = v.view(N, Kp // group, group)
     if zeros:
         lo, hi = v.amin(2).clamp(max=0.0), v.amax(2).clamp(min=0.0)
-        s16 = ((hi - lo) / 15.0).to(dtype)
+        s16 = ((hi - lo) / torch.full_like(lo, 15.0)).to(dtype)
         s = torch.where(s16 > 0, s16.float(), 1.0)
         z = torch.where(s16 > 0, torch.round(-lo / s).clamp(0, 15), 8.0)
         q = (torch.round(v / s[:, :, None]) + z[:, :, None]).clamp(0, 15)
     else:
-        s16 = (v.abs().amax(2) / 7.0).to(dtype)
+        top = v.abs().amax(2)
+        s16 = (top / torch.full_like(top, 7.0)).to(dtype)
         s = torch.where(s16 > 0, s16.float(), 1.0)
         z = torch.full_like(s, 8.0)
         q = torch.round(v / s[:, :, None]).clamp(-8, 7) + 8.0
@@ -300,12 +302,12 @@ def exact(case, seed):
                 part = torch.zeros_like(w[:, :1])
             if c["zeros"]:
                 a, b = part.min(1, keepdim=True)[0].clamp(max=0), part.max(1, keepdim=True)[0].clamp(min=0)
-                sc = ((b - a).float() / 15).to(dt).double()
+                sc = ((b - a) / 15).float().to(dt).double()
                 d = torch.where(sc > 0, sc, torch.ones_like(sc))
                 z = torch.where(sc > 0, (-a / d).round().clamp(0, 15), torch.full_like(sc, 8))
                 q = ((part / d).round() + z).clamp(0, 15) - z
             else:
-                sc = (part.abs().max(1, keepdim=True)[0].float() / 7).to(dt).double()
+                sc = (part.abs().max(1, keepdim=True)[0] / 7).float().to(dt).double()
                 d = torch.where(sc > 0, sc, torch.ones_like(sc))
                 z = torch.full_like(sc, 8)
                 q = (part / d).round().clamp(-8, 7)
