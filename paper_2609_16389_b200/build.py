@@ -15,9 +15,10 @@ LIB = os.path.join(HERE, "libexo_gemm.so")
 SHARE_DIR = os.path.join(CSRC, "cluster4")
 SHARE_LIB = os.path.join(HERE, "libexo_gemm_cluster4.so")
 SHARE_DEPS = [os.path.join("cluster4", "share_pairs.cuh")]
-SOURCES = ["api.cu", "gemv.cu"]
+SOURCES = ["api.cu", "gemv.cu", "q4.cu", "moe.cu"]
 DEPS = ["api.cu", "gemv.cu", "gemm_kernel.cuh", "gemm_params.h", "plan.h", "ptx.cuh", "tile_scheduler.h",
-        os.path.join("..", "..", "include", "exo_gemm.h")]
+        "q4.cu", "moe.cu", "decode_core.cuh", "decode_host.h",
+        os.path.join("..", "..", "include", "exo_gemm.h"), os.path.join("..", "..", "include", "exo_decode.h")]
 
 
 def nvcc_path() -> str:
@@ -35,15 +36,25 @@ def is_stale(lib: str = LIB, deps=DEPS) -> bool:
 
 
 def _compile(lib: str, defines, verbose: bool) -> str:
-    tmp = lib + f".tmp{os.getpid()}"
-    cmd = [nvcc_path(), "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-           "-shared", "-Xcompiler", "-fPIC", "-Xcompiler", "-fno-gnu-unique", "-cudart", "static", "-o", tmp]
-    cmd += [f"-D{d}" for d in defines]
+    """Compiles the sources side by side and links them."""
+    from concurrent.futures import ThreadPoolExecutor
+    nvcc, tmp = nvcc_path(), lib + f".tmp{os.getpid()}"
+    arch = ["-gencode", "arch=compute_100a,code=sm_100a"]
+    flags = arch + ["-lineinfo", "-O3", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcompiler", "-fno-gnu-unique"]
+    flags += [f"-D{d}" for d in defines]
     if verbose:
-        cmd += ["-Xptxas", "-v"]
-    cmd += [os.path.join(CSRC, s) for s in SOURCES]
-    subprocess.run(cmd, check=True)
-    os.replace(tmp, lib)
+        flags += ["-Xptxas", "-v"]
+    objects = [f"{tmp}.{s}.o" for s in SOURCES]
+    try:
+        with ThreadPoolExecutor(len(SOURCES)) as ex:
+            list(ex.map(lambda so: subprocess.run([nvcc, *flags, "-c", os.path.join(CSRC, so[0]), "-o", so[1]], check=True),
+                        zip(SOURCES, objects)))
+        subprocess.run([nvcc, *arch, "-shared", "-cudart", "static", "-o", tmp, *objects], check=True)
+        os.replace(tmp, lib)
+    finally:
+        for o in objects:
+            if os.path.exists(o):
+                os.remove(o)
     return lib
 
 

@@ -121,6 +121,7 @@ static int smem_of(const TileConfig& cfg, int c_dtype) {
 }
 
 static thread_local int g_last_cuda_error = 0;
+void note_cuda_error(int e) { g_last_cuda_error = e; }   // for the other translation units
 
 // K (in 16-bit-element units) from which a run that may store C straight from registers does so, for a
 // 32-bit and for a 16-bit C.

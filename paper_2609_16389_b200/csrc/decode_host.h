@@ -1,0 +1,74 @@
+// Host side of the few-token operators: device check and launch.
+#pragma once
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include <atomic>
+
+#include "../../include/exo_gemm.h"
+
+namespace exo {
+void note_cuda_error(int e);   // what exo_gemm_last_cuda_error reports (api.cu)
+
+namespace decode {
+
+constexpr int kMostSmem = 200 * 1024;   // dynamic shared memory a launch may ask for
+
+inline exo_gemm_status_t cuda_failed(cudaError_t e) {
+  note_cuda_error((int)e);
+  cudaGetLastError();   // clear the runtime's error state
+  return EXO_GEMM_ERR_CUDA;
+}
+
+// The current device has to be compute capability 10.x; *sms is its SM count.  Looked up once per device.
+inline exo_gemm_status_t device_check(int* sms) {
+  static std::atomic<int> seen[64];   // 0: not yet; else SM count, negative where the architecture is another
+  int device = 0;
+  cudaError_t e = cudaGetDevice(&device);
+  if (e != cudaSuccess) return cuda_failed(e);
+  int v = device < 64 ? seen[device].load(std::memory_order_relaxed) : 0;
+  if (v == 0) {
+    int major = 0, n = 0;
+    if ((e = cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, device)) != cudaSuccess) return cuda_failed(e);
+    if ((e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, device)) != cudaSuccess) return cuda_failed(e);
+    v = major == 10 ? n : -n;
+    if (device < 64) seen[device].store(v, std::memory_order_relaxed);
+  }
+  if (v < 0) return EXO_GEMM_ERR_ARCH;
+  *sms = v;
+  return EXO_GEMM_OK;
+}
+
+// Alignment of a 4-bit matrix's parts: a lane reads 16 bytes of codes, and the scales and zero points of 128 weights at once.
+inline bool q4_aligned(const void* codes, const void* scales, const void* zeros, int group) {
+  return ((uintptr_t)codes & 15u) == 0 && (uintptr_t)scales % (unsigned)(256 / group) == 0 && (uintptr_t)zeros % (unsigned)(128 / group) == 0;
+}
+
+// One launch with programmatic dependent launch and, for cluster > 1, clusters of that many CTAs along x.
+inline exo_gemm_status_t launch(void* fn, unsigned grid_x, unsigned grid_y, unsigned threads, size_t smem, unsigned cluster,
+                                cudaStream_t stream, void* params) {
+  cudaError_t e;
+  // always the same opt-in, so that threads which launch one kernel at different sizes cannot take it from each other
+  if (smem > 48 * 1024 && (e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostSmem)) != cudaSuccess)
+    return cuda_failed(e);
+  cudaLaunchConfig_t lc{};
+  lc.gridDim = dim3(grid_x, grid_y, 1);
+  lc.blockDim = dim3(threads, 1, 1);
+  lc.dynamicSmemBytes = smem;
+  lc.stream = stream;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = cluster;
+  at[1].val.clusterDim.y = 1;
+  at[1].val.clusterDim.z = 1;
+  lc.attrs = at;
+  lc.numAttrs = cluster > 1 ? 2 : 1;
+  void* args[1] = {params};
+  e = cudaLaunchKernelExC(&lc, fn, args);
+  return e == cudaSuccess ? EXO_GEMM_OK : cuda_failed(e);
+}
+
+}  // namespace decode
+}  // namespace exo

@@ -1,0 +1,509 @@
+"""The few-token operators against their definitions in 64 bits.
+
+Bounds, derived from the arithmetic and not from what the kernels give: a sum of n products that are exact in fp32,
+accumulated in fp32 in some order with at most n / 8 + 32 roundings or truncations on the way of any term, is off by
+at most (n / 8 + 32) * 2^-23 * sum |terms|; rounding to 16 bits adds u = 2^-8 (bf16) or 2^-11 (fp16) of the value, or
+half the smallest subnormal number (2^-134, 2^-25).
+"""
+import numpy as np
+import pytest
+
+from paper_2609_16389_b200 import binding as B
+from paper_2609_16389_b200 import decode as D
+
+pytestmark = pytest.mark.gpu
+U = {D.BF16: 2.0 ** -8, D.FP16: 2.0 ** -11, D.FP32: 2.0 ** -24}
+TINY = {D.BF16: 2.0 ** -134, D.FP16: 2.0 ** -25, D.FP32: 0.0}
+
+
+def torch():
+    import torch as t
+    return t
+
+
+def tt(dtype):
+    t = torch()
+    return {D.BF16: t.bfloat16, D.FP16: t.float16, D.FP32: t.float32}[dtype]
+
+
+def stream():
+    return torch().cuda.current_stream().cuda_stream
+
+
+def sum_bound(n):
+    return (n / 8 + 32) * 2.0 ** -23
+
+
+def groups(K, group):
+    return D.padded_k(K) // group
+
+
+class Matrix:
+    """A 4-bit matrix on the device with its codes on the host; padding codes and all-padding groups hold junk."""
+
+    def __init__(self, rows, K, group, dtype, zeros, seed, spread=0.02):
+        t = torch()
+        rng = np.random.default_rng(seed)
+        self.rows, self.K, self.group, self.dtype = rows, K, group, dtype
+        codes = rng.integers(0, 16, (rows, D.padded_k(K)), dtype=np.uint8)
+        self.codes = t.from_numpy(D.pack_codes(codes)).cuda()
+        G = groups(K, group)
+        s = t.from_numpy(rng.uniform(0.2, 1.0, (rows, G)) * spread * rng.choice([-1, 1], (rows, G), p=[0.1, 0.9]))
+        s[:, (K + group - 1) // group:] = float("nan")
+        self.scales = s.to(tt(dtype)).cuda()
+        self.zeros = t.from_numpy(rng.integers(0, 16, (rows, G), dtype=np.uint8)).cuda() if zeros else None
+        z = self.zeros.cpu().numpy().astype(np.float64) if zeros else np.full((rows, G), 8.0)
+        at = np.arange(K) // group
+        self.values = (codes[:, :K].astype(np.float64) - z[:, at]) * self.scales.double().cpu().numpy()[:, at]
+
+    def q4(self):
+        return D.Q4(self.rows, self.K, self.group, self.dtype, self.codes.data_ptr(), self.scales.data_ptr(),
+                    0 if self.zeros is None else self.zeros.data_ptr())
+
+
+# ------------------------------------------------------------------ quantisation
+QUANT = [(1, 1, 32, False), (3, 7, 32, True), (5, 127, 64, False), (2, 128, 128, True), (33, 260, 32, True),
+         (4, 300, 128, False), (7, 4097, 64, True), (2, 9000, 128, False), (130, 512, 64, False)]
+
+
+@pytest.mark.parametrize("rows,K,group,zeros", QUANT)
+@pytest.mark.parametrize("dtype,src", [(D.BF16, D.BF16), (D.FP16, D.FP16), (D.BF16, D.FP32), (D.FP16, D.FP32), (D.FP16, D.BF16)])
+def test_quantize_follows_its_formula_code_by_code(rows, K, group, zeros, dtype, src):
+    t = torch()
+    gen = t.Generator().manual_seed(rows * 1000 + K)
+    ldw = K + 3
+    w = t.full((rows, ldw), float("nan"))
+    w[:, :K] = t.randn(rows, K, generator=gen) * t.exp(t.randn(rows, 1, generator=gen))
+    if rows > 2:
+        w[1, :K] = 0.0                       # a row of zeros: scale 0, code = zero
+        w[2, :K] = w[2, :K].abs()            # one sign only
+    w = w.to(tt(src))
+    G, Kp = groups(K, group), D.padded_k(K)
+    codes = t.full((rows + 1, Kp // 2), 0xa5, dtype=t.uint8, device="cuda")      # one row more than is written
+    scales = t.full((rows + 1, G), 7.0, dtype=tt(dtype), device="cuda")
+    z = t.full((rows + 1, G), 99, dtype=t.uint8, device="cuda") if zeros else None
+    q = D.Q4(rows, K, group, dtype, codes.data_ptr(), scales.data_ptr(), z.data_ptr() if zeros else 0)
+    wd = w.cuda()
+    q.quantize(wd.data_ptr(), ldw, src, stream())
+    back = t.full((rows, K + 5), 3.0, dtype=tt(dtype), device="cuda")
+    q.dequantize(back.data_ptr(), K + 5, dtype, stream())
+    back32 = t.full((rows, K), 3.0, device="cuda")
+    q.dequantize(back32.data_ptr(), K, D.FP32, stream())
+    t.cuda.synchronize()
+    # the formula in numpy fp32, whose divisions are correctly rounded
+    v = np.zeros((rows, Kp), np.float32)
+    v[:, :K] = w[:, :K].float().numpy()
+    v = v.reshape(rows, G, group)
+    if zeros:
+        lo, hi = np.minimum(v.min(2), np.float32(0)), np.maximum(v.max(2), np.float32(0))
+        raw = (hi - lo) / np.float32(15)
+    else:
+        lo, raw = None, np.abs(v).max(2) / np.float32(7)
+    s16 = t.from_numpy(raw).to(tt(dtype))
+    s = s16.float().numpy()
+    safe = np.where(s > 0, s, np.float32(1))
+    zr = np.clip(np.rint(-lo / safe), 0, 15) if zeros else np.full_like(s, 8)
+    zr = np.where(s > 0, zr, 8).astype(np.float32)
+    qv = np.clip(np.rint(v / safe[:, :, None]) + zr[:, :, None], 0, 15)
+    qv = np.where((s > 0)[:, :, None], qv, zr[:, :, None])
+    want = D.pack_codes(qv.reshape(rows, Kp).astype(np.uint8))
+    assert np.array_equal(codes[:rows].cpu().numpy(), want)
+    assert t.equal(scales[:rows].cpu(), s16)
+    if zeros:
+        assert np.array_equal(z[:rows].cpu().numpy(), zr.astype(np.uint8))
+        assert (z[rows] == 99).all()
+    assert (codes[rows] == 0xa5).all() and (scales[rows] == 7).all()             # nothing beyond the rows
+    values = ((qv - zr[:, :, None]) * s[:, :, None]).reshape(rows, Kp)[:, :K].astype(np.float32)   # exact in fp32
+    assert np.array_equal(back32.cpu().numpy(), values)
+    assert t.equal(back[:, :K].cpu(), t.from_numpy(values).to(tt(dtype)))
+    assert (back[:, K:] == 3).all()
+
+
+def test_quantize_saturates_a_scale_that_its_type_cannot_hold():
+    t = torch()
+    w = t.full((1, 128), 3.0e38, device="cuda")
+    codes, scales = t.zeros(1, 64, dtype=t.uint8, device="cuda"), t.zeros(1, 1, dtype=t.float16, device="cuda")
+    D.Q4(1, 128, 128, D.FP16, codes.data_ptr(), scales.data_ptr()).quantize(w.data_ptr(), 128, D.FP32, stream())
+    assert scales.item() == 65504.0 and (codes == 0xff).all()
+
+
+# ------------------------------------------------------------------ gemv
+GEMV = [  # tokens, rows, K, group, zeros
+    (1, 1, 1, 32, False), (1, 16, 128, 128, False), (1, 17, 129, 64, True), (2, 100, 1000, 32, True), (1, 4096, 512, 128, True),
+    (1, 40, 16384, 128, False), (3, 333, 2052, 64, False), (8, 64, 4096, 128, False), (9, 70, 777, 32, True),
+    (16, 130, 1024, 64, True), (17, 200, 640, 128, False), (33, 65, 1536, 32, False), (64, 257, 2048, 128, True),
+    (64, 40, 9001, 64, True), (31, 1000, 384, 128, True),
+]
+
+
+@pytest.mark.parametrize("tokens,rows,K,group,zeros", GEMV)
+@pytest.mark.parametrize("dtype,out", [(D.BF16, D.BF16), (D.FP16, D.FP32), (D.FP16, D.FP16), (D.BF16, D.FP32)])
+def test_gemv_against_its_definition(tokens, rows, K, group, zeros, dtype, out):
+    t = torch()
+    m = Matrix(rows, K, group, dtype, zeros, seed=tokens * 7 + rows)
+    gen = t.Generator().manual_seed(K)
+    odd = rows % 2 == 1                                  # rows of x and y off any alignment, or padded ones
+    ldx, ldy = K + (1 if odd else 8 - K % 8), rows + 3
+    x = t.full((tokens, ldx), float("nan"), dtype=tt(dtype))
+    x[:, :K] = t.randn(tokens, K, generator=gen)
+    y0 = t.randn(tokens, ldy, generator=gen).to(tt(out))
+    xd = x.cuda()
+    ref = x[:, :K].double().numpy() @ m.values.T
+    mag = np.abs(x[:, :K].double().numpy()) @ np.abs(m.values).T
+    for alpha, beta in ((1.0, 0.0), (-0.5, 0.75)):
+        y = y0.clone()
+        if beta == 0.0:
+            y[:, :rows] = float("nan")                   # not read
+        yd = y.cuda()
+        m.q4().gemv(tokens, xd.data_ptr(), ldx, yd.data_ptr(), ldy, out, alpha, beta, stream())
+        got = yd.cpu()
+        want = alpha * ref + (beta * y0[:, :rows].double().numpy() if beta else 0.0)
+        bound = abs(alpha) * sum_bound(K) * mag + 4 * 2.0 ** -24 * np.abs(want) + U[out] * 1.01 * np.abs(want) + TINY[out]
+        err = np.abs(got[:, :rows].double().numpy() - want)
+        assert (err <= bound).all(), (err / bound).max()
+        assert t.equal(got[:, rows:], y0[:, rows:])      # nothing beside the matrix
+
+
+def test_gemv_without_products():
+    t = torch()
+    m = Matrix(70, 256, 64, D.BF16, False, seed=1)
+    m.codes.fill_(0)
+    for K, alpha in ((256, 0.0), (0, 1.0)):
+        for beta in (0.0, 2.0):
+            y = t.full((3, 70), float("nan") if beta == 0 else 1.5, device="cuda")
+            q = D.Q4(70, K, 64, D.BF16, m.codes.data_ptr(), m.scales.data_ptr())
+            q.gemv(3, 0, max(K, 1), y.data_ptr(), 70, D.FP32, alpha, beta, stream())
+            assert (y == 1.5 * beta).all()
+
+
+def test_gemv_keeps_infinities_to_their_token_and_row():
+    t = torch()
+    m = Matrix(50, 384, 128, D.FP16, True, seed=5)
+    x = t.randn(4, 384, generator=t.Generator().manual_seed(1)).half().cuda()
+    clean = t.empty(4, 50, device="cuda")
+    m.q4().gemv(4, x.data_ptr(), 384, clean.data_ptr(), 50, D.FP32, stream=stream())
+    x[1, 100] = float("nan")
+    m.scales[7, 1] = float("inf")
+    y = t.empty(4, 50, device="cuda")
+    m.q4().gemv(4, x.data_ptr(), 384, y.data_ptr(), 50, D.FP32, stream=stream())
+    assert t.isnan(y[1]).all()
+    rest = [r for r in range(50) if r != 7]
+    for token in (0, 2, 3):
+        assert t.equal(y[token, rest], clean[token, rest]) and not t.isfinite(y[token, 7])
+
+
+def test_gemv_on_a_side_stream_and_in_a_graph_gives_the_same_bits():
+    t = torch()
+    m = Matrix(1000, 2048, 64, D.BF16, True, seed=9)
+    x = t.randn(5, 2048, generator=t.Generator().manual_seed(3)).bfloat16().cuda()
+    y = [t.empty(5, 1000, dtype=t.bfloat16, device="cuda") for _ in range(3)]
+    q = m.q4()
+    run = lambda out: q.gemv(5, x.data_ptr(), 2048, out.data_ptr(), 1000, D.BF16, stream=stream())  # noqa: E731
+    run(y[0])
+    t.cuda.synchronize()
+    side = t.cuda.Stream()
+    with t.cuda.stream(side):
+        run(y[1])
+    side.synchronize()
+    graph = t.cuda.CUDAGraph()
+    with t.cuda.graph(graph):
+        run(y[2])
+    for _ in range(3):
+        y[2].zero_()
+        graph.replay()
+    t.cuda.synchronize()
+    assert t.equal(y[0], y[1]) and t.equal(y[0], y[2])
+
+
+def test_quantize_then_gemv_then_dequantize_in_one_stream():
+    """Each kernel may start while its predecessor drains: what a predecessor wrote has to be seen all the same."""
+    t = torch()
+    rows, K = 2048, 2048
+    q_codes, q_scales = t.empty(rows, K // 2, dtype=t.uint8, device="cuda"), t.empty(rows, K // 128, dtype=t.bfloat16, device="cuda")
+    q = D.Q4(rows, K, 128, D.BF16, q_codes.data_ptr(), q_scales.data_ptr())
+    gen = t.Generator(device="cuda").manual_seed(2)
+    x = t.randn(2, K, device="cuda", generator=gen).bfloat16()
+    ws = [t.randn(rows, K, device="cuda", generator=gen).bfloat16() for _ in range(6)]
+    ys = [t.empty(2, rows, device="cuda") for _ in ws]
+    back = [t.empty(rows, K, device="cuda") for _ in ws]
+    t.cuda.synchronize()
+    for w, y, b in zip(ws, ys, back):
+        q.quantize(w.data_ptr(), K, D.BF16, stream())
+        q.gemv(2, x.data_ptr(), K, y.data_ptr(), rows, D.FP32, stream=stream())
+        q.dequantize(b.data_ptr(), K, D.FP32, stream())
+    for y, b in zip(ys, back):
+        ref, mag = x.double() @ b.double().t(), x.double().abs() @ b.double().abs().t()
+        assert ((y.double() - ref).abs() <= sum_bound(K) * mag).all()
+
+
+# ------------------------------------------------------------------ mixture of experts
+class Layer:
+    def __init__(self, H, F, E, shared, k, dtype, group=0, zeros=False, renormalize=1, scale=1.0, seed=0, pad=0, merged=False,
+                 max_tokens=64):
+        t = torch()
+        self.H, self.F, self.E, self.shared, self.k, self.dtype = H, F, E, shared, k, dtype
+        self.renormalize, self.scale = renormalize, scale
+        gen = t.Generator().manual_seed(seed)
+        n = E + shared
+        self.ldr = H + pad
+        self.router = t.full((E, self.ldr), float("nan")).to(tt(dtype))
+        self.router[:, :H] = (t.randn(E, H, generator=gen) * 1.5 * H ** -0.5).to(tt(dtype))
+        self.mats, self.vals = {}, {}
+        if merged:   # rows of gate and up in turn, expert by expert
+            both = self._stack(n * 2 * F, H, group, zeros, pad, gen, seed + 1)
+            per = 2 * F
+            self.vals["gate"] = both["values"].reshape(n, per, H)[:, :F]
+            self.vals["up"] = both["values"].reshape(n, per, H)[:, F:]
+            self.mats["gate"] = self._matrix(both, per, 0)
+            self.mats["up"] = self._matrix(both, per, F)
+            self.keep = [both]
+        else:
+            self.keep = []
+            for i, name in enumerate(("gate", "up")):
+                extra = 3 if pad else 0
+                m = self._stack(n * (F + extra), H, group, zeros, pad, gen, seed + 1 + i)
+                self.vals[name] = m["values"].reshape(n, F + extra, H)[:, :F]
+                self.mats[name] = self._matrix(m, F + extra, 0)
+                self.keep.append(m)
+        m = self._stack(n * H, F, group, zeros, pad, gen, seed + 5)
+        self.vals["down"] = m["values"].reshape(n, H, F)
+        self.mats["down"] = self._matrix(m, H, 0)
+        self.keep.append(m)
+        self.router_d = self.router.cuda()
+        self.weights = D.MoeWeights(self.router_d.data_ptr(), self.ldr, self.mats["gate"], self.mats["up"], self.mats["down"])
+        self.plan = D.MoePlan(D.MoeDesc(H, F, E, shared, k, max_tokens, dtype, group, renormalize, scale))
+
+    def _stack(self, rows, K, group, zeros, pad, gen, seed):
+        t = torch()
+        if group:
+            m = Matrix(rows, K, group, self.dtype, zeros, seed, spread=0.5 * K ** -0.5)
+            return {"q4": m, "values": m.values}
+        w = t.full((rows, K + pad), float("nan")).to(tt(self.dtype))
+        w[:, :K] = (t.randn(rows, K, generator=gen) * K ** -0.5).to(tt(self.dtype))
+        return {"w": w.cuda(), "ld": K + pad, "values": w[:, :K].double().numpy()}
+
+    def _matrix(self, m, expert_rows, first):
+        if "q4" in m:
+            q = m["q4"]
+            return D.MoeMatrix(q.codes[first:].data_ptr(), 0, expert_rows, q.scales[first:].data_ptr(),
+                               0 if q.zeros is None else q.zeros[first:].data_ptr())
+        return D.MoeMatrix(m["w"][first:].data_ptr(), m["ld"], expert_rows, 0, 0)
+
+    def run(self, x, ldx, ldy=None, y=None):
+        t = torch()
+        T = x.shape[0]
+        ldy = ldy or self.H
+        y = t.full((T, ldy), 5.0, dtype=tt(self.dtype), device="cuda") if y is None else y
+        index = t.full((T, self.k), -7, dtype=t.int32, device="cuda")
+        weight = t.full((T, self.k), -7.0, device="cuda")
+        self.plan.run(self.weights, T, x.data_ptr(), ldx, y.data_ptr(), ldy, index.data_ptr(), weight.data_ptr(), stream())
+        return y, index, weight
+
+    def check(self, x, y, index, weight):
+        """x: T x H on the host.  The taken experts have to be a right choice up to the logits' own error."""
+        x = x.double().numpy()
+        y, index, weight = y.double().cpu().numpy()[:, :self.H], index.cpu().numpy(), weight.double().cpu().numpy()
+        r = self.router[:, :self.H].double().numpy()
+        logits, lb = x @ r.T, sum_bound(self.H) * (np.abs(x) @ np.abs(r).T)
+        for tok in range(len(x)):
+            e, took = index[tok], np.zeros(self.E, bool)
+            assert ((e >= 0) & (e < self.E)).all() and len(set(e)) == self.k
+            took[e] = True
+            if not took.all():
+                low, high = np.where(took, logits[tok] + lb[tok], np.inf).min(), np.where(took, -np.inf, logits[tok] - lb[tok]).max()
+                assert low >= high
+            p = np.exp(logits[tok] - logits[tok].max())
+            w = p[e] / (p[e].sum() if self.renormalize else p.sum()) * self.scale
+            # a logit off by b changes exp by a factor e^b; sums and quotients of at most 520 terms add 2^-14 at most
+            assert (np.abs(weight[tok] - w) <= w * (np.expm1(2 * lb[tok].max()) + 2.0 ** -14)).all()
+            assert (np.diff(weight[tok]) <= 0).all()
+            ref, bound = np.zeros(self.H), np.zeros(self.H)
+            for ex, we in list(zip(e, weight[tok])) + [(self.E + s, 1.0) for s in range(self.shared)]:
+                g, u = self.vals["gate"][ex] @ x[tok], self.vals["up"][ex] @ x[tok]
+                bg = sum_bound(self.H) * (np.abs(self.vals["gate"][ex]) @ np.abs(x[tok]))
+                bu = sum_bound(self.H) * (np.abs(self.vals["up"][ex]) @ np.abs(x[tok]))
+                silu = g / (1 + np.exp(-g))
+                h = we * silu * u
+                # |silu'| < 1.1; a few fp32 roundings and expf's; then one rounding to 16 bits
+                bh = we * (1.1 * bg * (np.abs(u) + bu) + np.abs(silu) * bu) + np.abs(h) * (16 * 2.0 ** -24 + U[self.dtype]) * 1.01 + TINY[self.dtype]
+                d = self.vals["down"][ex]
+                ref += d @ h
+                bound += np.abs(d) @ bh + sum_bound(self.F) * (np.abs(d) @ np.abs(h))
+            n = self.k + self.shared
+            bound += np.abs(ref) * U[self.dtype] * 1.01 + TINY[self.dtype] + n * 2.0 ** -20 * np.abs(ref)
+            err = np.abs(y[tok] - ref)
+            assert (err <= bound).all(), (tok, (err / bound).max())
+
+
+def tokens(T, H, dtype, seed, pad=0):
+    t = torch()
+    x = t.full((T, H + pad), float("nan")).to(tt(dtype))
+    x[:, :H] = t.randn(T, H, generator=t.Generator().manual_seed(seed)).to(tt(dtype))
+    return x
+
+
+MOE = [  # T, H, F, E, shared, k, group, zeros, pad, merged
+    (1, 64, 32, 4, 0, 2, 0, False, 0, False),
+    (1, 1, 1, 1, 0, 1, 0, False, 0, False),
+    (1, 520, 136, 8, 1, 3, 0, False, 8, False),
+    (3, 133, 77, 5, 0, 2, 0, False, 0, False),        # rows off any alignment
+    (8, 256, 200, 16, 2, 4, 0, False, 0, True),
+    (9, 300, 96, 7, 0, 7, 0, False, 4, True),         # every expert taken; unaligned rows
+    (17, 512, 64, 33, 0, 5, 0, False, 0, False),
+    (64, 264, 128, 6, 1, 2, 0, False, 0, False),      # many tokens to an expert
+    (64, 128, 40, 512, 0, 16, 0, False, 0, False),
+    (1, 256, 128, 4, 0, 2, 128, False, 0, False),
+    (2, 300, 200, 8, 1, 3, 64, True, 0, False),
+    (5, 1000, 130, 6, 0, 2, 32, True, 0, True),
+    (12, 384, 256, 20, 0, 4, 128, True, 0, False),
+    (64, 160, 96, 5, 1, 2, 32, False, 0, False),
+    (33, 2048, 64, 3, 0, 1, 64, False, 0, True),
+    (4, 100, 33, 6, 0, 2, 128, True, 0, True),        # one group to a row: rows' scales lie 2 bytes apart
+]
+
+
+@pytest.mark.parametrize("T,H,F,E,shared,k,group,zeros,pad,merged", MOE)
+@pytest.mark.parametrize("dtype", [D.BF16, D.FP16])
+def test_moe_against_its_definition(T, H, F, E, shared, k, group, zeros, pad, merged, dtype):
+    t = torch()
+    for renormalize, scale in ((1, 1.0), (0, 2.5)):
+        L = Layer(H, F, E, shared, k, dtype, group, zeros, renormalize, scale, seed=T + H, pad=pad, merged=merged, max_tokens=max(T, 2))
+        x = tokens(T, H, dtype, T * 31 + H, pad=3 if pad else 0)
+        xd = x.cuda()
+        y, index, weight = L.run(xd, xd.shape[1], ldy=H + 5)
+        assert (y[:, H:] == 5).all()
+        L.check(x[:, :H], y, index, weight)
+        y2, index2, weight2 = L.run(xd, xd.shape[1], ldy=H + 5)      # the workspace is left as it was found
+        assert t.equal(y, y2) and t.equal(index, index2) and t.equal(weight, weight2)
+
+
+def test_moe_ties_go_to_the_lowest_index():
+    t = torch()
+    L = Layer(64, 32, 40, 0, 4, D.BF16, seed=3)
+    L.router_d.zero_()
+    L.router.zero_()
+    x = tokens(3, 64, D.BF16, 1)
+    xd = x.cuda()
+    y, index, weight = L.run(xd, 64)
+    assert (index.cpu() == t.arange(4, dtype=t.int32)).all() and (weight == 0.25).all()
+    L.check(x, y, index, weight)
+    L.router_d[35] = L.router_d[3] = 1.0                 # two equal ones, the largest or the smallest by the token's sign
+    _, index, _ = L.run(xd, 64)
+    up = x.float().sum(1) > 0
+    for tok in range(3):
+        assert index[tok].tolist() == ([3, 35, 0, 1] if up[tok] else [0, 1, 2, 4])
+
+
+def test_moe_all_tokens_to_one_expert():
+    t = torch()
+    L = Layer(96, 48, 8, 0, 1, D.FP16, seed=4)
+    x = tokens(50, 96, D.FP16, 2).abs()
+    L.router_d[5] = L.router[5] = 4.0
+    xd = x.cuda()
+    y, index, weight = L.run(xd, 96)
+    assert (index == 5).all() and (weight == 1).all()
+    L.check(x, y, index, weight)
+
+
+def test_moe_fewer_tokens_than_the_plan_and_none():
+    t = torch()
+    L = Layer(128, 64, 12, 1, 3, D.BF16, seed=6, max_tokens=64)
+    for T in (64, 1, 20, 7):
+        x = tokens(T, 128, D.BF16, T)
+        xd = x.cuda()
+        L.check(x, *L.run(xd, 128))
+    y = t.full((1, 128), 5.0, dtype=t.bfloat16, device="cuda")
+    L.plan.run(L.weights, 0, 0, 128, 0, 128)
+    L.plan.run(L.weights, 1, tokens(1, 128, D.BF16, 1).cuda().data_ptr(), 128, y.data_ptr(), 128, stream=stream())   # no index, no weight
+    assert not (y == 5).all()
+
+
+def test_moe_keeps_nan_to_its_token_and_an_untaken_expert_out():
+    t = torch()
+    L = Layer(128, 64, 6, 0, 2, D.BF16, seed=8)
+    x = tokens(5, 128, D.BF16, 3)
+    xd = x.cuda()
+    y, index, _ = L.run(xd, 128)
+    xd[2, 17] = float("nan")
+    used = set(index[[0, 1, 3, 4]].flatten().tolist())
+    y2, index2, weight2 = L.run(xd, 128)
+    assert t.isnan(y2[2]).all() and t.isnan(weight2[2]).all()
+    assert ((index2 >= 0) & (index2 < 6)).all()
+    keep = [0, 1, 3, 4]
+    assert t.equal(index[keep], index2[keep]) and t.equal(y[keep], y2[keep])
+    L2 = Layer(128, 64, 6, 0, 2, D.BF16, seed=8)
+    for e in set(range(6)) - set(index.flatten().tolist()):
+        L2.keep[0]["w"][e * 64:(e + 1) * 64] = float("nan")
+    xd = x.cuda()
+    assert t.equal(L2.run(xd, 128)[0], y) and used
+
+
+def test_moe_captured_in_a_graph_and_on_a_side_stream():
+    t = torch()
+    L = Layer(512, 256, 16, 1, 4, D.FP16, group=64, zeros=True, seed=10)
+    x = tokens(6, 512, D.FP16, 9).cuda()
+    want, index, weight = L.run(x, 512)
+    t.cuda.synchronize()
+    side = t.cuda.Stream()
+    with t.cuda.stream(side):
+        got, _, _ = L.run(x, 512)
+    side.synchronize()
+    assert t.equal(want, got)
+    y = t.zeros(6, 512, dtype=t.float16, device="cuda")
+    graph = t.cuda.CUDAGraph()
+    with t.cuda.graph(graph):
+        L.plan.run(L.weights, 6, x.data_ptr(), 512, y.data_ptr(), 512, stream=stream())
+        L.plan.run(L.weights, 6, x.data_ptr(), 512, y.data_ptr(), 512, stream=stream())
+    for _ in range(3):
+        y.zero_()
+        graph.replay()
+    t.cuda.synchronize()
+    assert t.equal(want, y)
+
+
+def test_moe_runs_in_a_row_with_changing_inputs():
+    """Each run's first kernel may start while the last one drains; they share the workspace."""
+    t = torch()
+    L = Layer(256, 128, 32, 0, 6, D.BF16, seed=12)
+    xs = [tokens(T, 256, D.BF16, T).cuda() for T in (1, 40, 3, 64, 2, 9)]
+    first = [L.run(x, 256) for x in xs]
+    again = [L.run(x, 256) for x in xs for _ in range(1)]
+    alone = []
+    for x in xs:
+        alone.append(L.run(x, 256))
+        t.cuda.synchronize()
+    for a, b, c in zip(first, again, alone):
+        for u, v, w in zip(a, b, c):
+            assert t.equal(u, v) and t.equal(u, w)
+
+
+def test_moe_refuses_bad_arguments():
+    t = torch()
+    L = Layer(64, 32, 4, 0, 2, D.BF16, seed=1, max_tokens=4)
+    buf = t.zeros(1 << 16, dtype=t.uint8, device="cuda").data_ptr()
+    run = lambda w=L.weights, T=1, x=buf, ldx=64, y=buf + 8192, ldy=64, i=0, wt=0: D.exo_moe_run(L.plan.handle, w, T, x, ldx, y, ldy, i, wt)  # noqa: E731
+    assert run(w=None) == B.ERR_NULL and run(x=0) == B.ERR_NULL and run(y=0) == B.ERR_NULL
+    assert run(T=5) == B.ERR_INVALID_ARG and run(T=-1) == B.ERR_INVALID_ARG
+    assert run(ldx=63) == B.ERR_INVALID_ARG and run(ldy=63) == B.ERR_INVALID_ARG
+    assert run(x=buf + 1) == B.ERR_ALIGNMENT and run(i=buf + 2) == B.ERR_ALIGNMENT and run(wt=buf + 2) == B.ERR_ALIGNMENT
+
+    def changed(which, **kw):
+        mats = {n: D.MoeMatrix(*[getattr(L.mats[n], f) for f, _ in D.MoeMatrix._fields_]) for n in L.mats}
+        for name, value in kw.items():
+            setattr(mats[which], name, value)
+        return D.MoeWeights(L.router_d.data_ptr(), 64, mats["gate"], mats["up"], mats["down"])
+    for which, K, rows in (("gate", 64, 32), ("up", 64, 32), ("down", 32, 64)):
+        assert run(w=changed(which, w=0)) == B.ERR_NULL
+        assert run(w=changed(which, ld=K - 1)) == B.ERR_INVALID_ARG
+        assert run(w=changed(which, expert_rows=rows - 1)) == B.ERR_INVALID_ARG
+        assert run(w=changed(which, scales=buf)) == B.ERR_INVALID_ARG
+        assert run(w=changed(which, w=buf + 1)) == B.ERR_ALIGNMENT
+    assert run(w=D.MoeWeights(0, 64, L.mats["gate"], L.mats["up"], L.mats["down"])) == B.ERR_NULL
+    assert run(w=D.MoeWeights(buf, 63, L.mats["gate"], L.mats["up"], L.mats["down"])) == B.ERR_INVALID_ARG
+    Q = Layer(64, 32, 4, 0, 2, D.BF16, group=32, seed=1, max_tokens=4)
+    bad = D.MoeWeights(Q.router_d.data_ptr(), 64, D.MoeMatrix(Q.mats["gate"].w, 0, 32, 0, 0), Q.mats["up"], Q.mats["down"])
+    assert D.exo_moe_run(Q.plan.handle, bad, 1, buf, 64, buf + 8192, 64) == B.ERR_NULL
+    bad = D.MoeWeights(Q.router_d.data_ptr(), 64, D.MoeMatrix(Q.mats["gate"].w + 8, 0, 32, Q.mats["gate"].scales, 0), Q.mats["up"], Q.mats["down"])
+    assert D.exo_moe_run(Q.plan.handle, bad, 1, buf, 64, buf + 8192, 64) == B.ERR_ALIGNMENT
+    assert Q.plan.workspace_bytes() >= 4 * 2 * 32 * 2
+    t.cuda.synchronize()
