@@ -6,7 +6,7 @@
  *   exo_moe_create / run / destroy        a whole mixture-of-experts layer for 1 to 64 tokens, 16- or 4-bit experts
  *
  * For more tokens the same weights go through exo_q4_dequantize and exo_gemm_run (exo_gemm.h), whose status codes,
- * types and conventions hold here: all pointers to matrices are DEVICE pointers owned by the caller, calls are
+ * types and conventions hold here (exo_gemm_last_cuda_error included): all pointers to matrices are DEVICE pointers owned by the caller, calls are
  * enqueued on cuda_stream (a cudaStream_t; NULL = the legacy default stream) and return without synchronising, every
  * check happens before the first launch, nothing runs on the CPU, and a device that is not compute capability 10.x is
  * refused with EXO_GEMM_ERR_ARCH.  Calls may be captured into a CUDA graph.  Launches use programmatic dependent
@@ -65,9 +65,13 @@ exo_gemm_status_t exo_q4_dequantize(const exo_q4_t* q, void* W, int64_t ldw, int
  * Y = alpha * X * W^T + beta * Y for `tokens` rows: X is tokens x K of W's dtype, Y is tokens x rows of y_dtype (FP32
  * or W's dtype), both row-major with leading dimensions ldx >= K and ldy >= rows (elements; no alignment beyond the
  * element's is needed, 16-byte aligned rows of X are read faster).  beta == 0: Y is not read; alpha == 0: W and X are
- * not read.  X and W must not overlap Y.  Products are formed from the integers code - zero and the 16-bit activations
- * and summed in fp32, and a group's sum is multiplied by its scale in fp32.  0 <= tokens <= 64 (ERR_UNSUPPORTED
- * above).  Nothing is allocated.  Other errors as above.
+ * not read.  X and W must not overlap Y.  0 <= tokens <= 64 (ERR_UNSUPPORTED above).  Nothing is allocated.  Other
+ * errors as above.
+ *
+ * Products are formed from the integers code - zero and a group's sum is multiplied by its scale in fp32; all further
+ * sums are fp32.  From 5 tokens on the factors are the 16-bit activations and a group is summed in fp32.  Up to 4 tokens
+ * they are integers of 30 bits that stand for the activations of 128 neighbouring k: exact for values down to 2^-22 (bf16) or
+ * 2^-19 (fp16) of the largest of the 128, and off by at most 2^-30 of that largest below; their group sums are exact.
  */
 exo_gemm_status_t exo_gemv_q4_run(const exo_q4_t* W, int64_t tokens, const void* X, int64_t ldx, void* Y, int64_t ldy,
                                   int32_t y_dtype, float alpha, float beta, void* cuda_stream);
@@ -138,6 +142,12 @@ exo_gemm_status_t exo_moe_create(exo_moe_handle_t* out, const exo_moe_desc_t* de
  */
 exo_gemm_status_t exo_moe_run(exo_moe_handle_t plan, const exo_moe_weights_t* weights, int64_t tokens, const void* x,
                               int64_t ldx, void* y, int64_t ldy, int32_t* index, float* weight, void* cuda_stream);
+
+/*
+ * Waits for the current device and returns EXO_GEMM_ERR_DEVICE_TIMEOUT if a bounded device-side wait of a kernel of this
+ * header has given up since the last call (what that launch computed is then wrong), else EXO_GEMM_OK.
+ */
+exo_gemm_status_t exo_decode_check(void);
 
 /* Device memory the plan owns, in bytes. */
 int64_t exo_moe_workspace_bytes(exo_moe_handle_t plan);

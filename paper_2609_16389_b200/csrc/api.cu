@@ -192,6 +192,38 @@ static CUresult encode_3d(CUtensorMap* map, int dtype, const void* base, uint64_
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
 }
 
+// The rows of a 4-bit matrix (decode_host.h) as (16 words of a step, row, step): a copy of `steps` steps of 16 rows lands as
+// steps of 16 x 64 bytes; zeros outside.
+bool encode_steps_map(CUtensorMap* map, const void* codes, uint64_t rows, uint64_t blocks, uint32_t steps) {
+  EncodeTiledFn fn = get_encode_fn();
+  cuuint64_t dims[3] = {16, rows, blocks};
+  cuuint64_t strides[2] = {blocks * 64, 64};
+  cuuint32_t box[3] = {16, 16, steps};
+  cuuint32_t estr[3] = {1, 1, 1};
+  const CUresult r = !fn ? CUDA_ERROR_NOT_FOUND
+                         : fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 3, const_cast<void*>(codes), dims, strides, box, estr,
+                              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) g_last_cuda_error = (int)r;
+  return r == CUDA_SUCCESS;
+}
+
+// The rows of a matrix as words of 2 or 4 bytes (decode_host.h); zeros outside.
+bool encode_rows_map(CUtensorMap* map, int word_bytes, const void* base, uint64_t row_words, uint64_t rows, uint64_t row_bytes, uint32_t box_words,
+                     uint32_t box_rows) {
+  EncodeTiledFn fn = get_encode_fn();
+  cuuint64_t dims[2] = {row_words, rows};
+  cuuint64_t strides[1] = {row_bytes};
+  cuuint32_t box[2] = {box_words, box_rows};
+  cuuint32_t estr[2] = {1, 1};
+  const CUresult r = !fn ? CUDA_ERROR_NOT_FOUND
+                         : fn(map, word_bytes == 2 ? CU_TENSOR_MAP_DATA_TYPE_UINT16 : CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, const_cast<void*>(base),
+                              dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
+                              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) g_last_cuda_error = (int)r;
+  return r == CUDA_SUCCESS;
+}
+
 }  // namespace exo
 
 struct exo_gemm_plan {

@@ -33,7 +33,11 @@ struct Bf16 {
     const __nv_bfloat162 r = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
     return *reinterpret_cast<const uint32_t*>(&r);
   }
-  static __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  static __device__ __forceinline__ void mma0(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {   // d = a b
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+                 : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+  }
+  static __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {   // d += a b
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
   }
@@ -48,7 +52,11 @@ struct Fp16 {
     const __half2 r = __hsub2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
     return *reinterpret_cast<const uint32_t*>(&r);
   }
-  static __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  static __device__ __forceinline__ void mma0(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {   // d = a b
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+                 : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+  }
+  static __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {   // d += a b
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
   }
@@ -75,11 +83,40 @@ __device__ __forceinline__ uint4 load8_checked(const uint16_t* row, int k, int K
   return make_uint4(v[0], v[1], v[2], v[3]);
 }
 
+// ---- activations ----------------------------------------------------------------------------------------------
+// The rows of tokens g, 8 + g, 16 + g, ... are `stride` apart.  Rows of tokens that do not exist may hold anything: a
+// column of the product depends on its own token alone, and nobody reads theirs.
+struct XShared {
+  uint32_t base, stride;   // bytes, shared window
+  template <int OFF> __device__ __forceinline__ uint4 load(int i) const {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4+%5];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(base + i * stride), "n"(OFF * 2));
+    return v;
+  }
+  __device__ __forceinline__ void advance(int n) { base += 2 * n; }
+};
+struct XGlobal {
+  const uint16_t* base;
+  int64_t stride;          // elements
+  template <int OFF> __device__ __forceinline__ uint4 load(int i) const { return *reinterpret_cast<const uint4*>(base + i * stride + OFF); }
+  __device__ __forceinline__ void advance(int n) { base += n; }
+};
+// the last part of a step: values at and beyond `left` (counted from base) are 0
+struct XGlobalTail {
+  const uint16_t* base;
+  int64_t stride;
+  int left;
+  template <int OFF> __device__ __forceinline__ uint4 load(int i) const { return load8_checked(base + i * stride, OFF, left, true); }
+};
+
 // ---- weight formats -------------------------------------------------------------------------------------------
-// A format reads 16 weight rows in steps of kStep values of k.  Row pointers are those of the lane's rows g and g + 8.
-//   load(s, K)   step s of both rows (values at and beyond K read as 0)
-//   step(...)    acc += rows x tokens over that step; xb(i, k) is the lane's part of B: eight activations of token
-//                8 i + g at k .. k + 7 (k includes the lane's own 8 t)
+// A format reads 16 weight rows in steps of kStep values of k.  Its pointers are the lane's own: rows g and g + 8, at the
+// lane's part of the current step.
+//   load(n)      the step n ahead of the current one
+//   advance(n)   n steps on
+//   step(...)    acc += rows x tokens; x.load<OFF>(i) are the lane's eight activations of token 8 i + g, OFF elements
+//                behind the current step's (the lane's own 8 t included)
+// Only whole steps go through load() and step(); a last part of a step goes through load_tail() and step_tail().
 
 // 16-bit weights.  VEC: every row starts on a 16-byte boundary.
 template <class T, bool VEC>
@@ -88,39 +125,47 @@ struct Rows16 {
   const uint16_t *r0, *r1;
   struct Regs { uint4 a, b; };
 
-  __device__ __forceinline__ Regs load(int s, int K, int t) const {
-    const int k = s * kStep + 8 * t;
+  __device__ __forceinline__ void begin(int t) { r0 += 8 * t; r1 += 8 * t; }
+  __device__ __forceinline__ void advance(int n) { r0 += n * kStep; r1 += n * kStep; }
+  __device__ __forceinline__ Regs load(int n) const {
     Regs r;
-    if (VEC && k + 8 <= K) {
-      r.a = ldg_weights(r0 + k);
-      r.b = ldg_weights(r1 + k);
+    if constexpr (VEC) {
+      r.a = ldg_weights(r0 + n * kStep);
+      r.b = ldg_weights(r1 + n * kStep);
     } else {
-      r.a = load8_checked(r0, k, K, false);
-      r.b = load8_checked(r1, k, K, false);
+      r.a = load8_checked(r0 + n * kStep, 0, 8, false);
+      r.b = load8_checked(r1 + n * kStep, 0, 8, false);
     }
     return r;
   }
-  template <int NT, class XB>
-  __device__ __forceinline__ void step(const Regs& r, int s, int K, int t, const XB& xb, int nt, float (&acc)[NT][4]) const {
-    const int k = s * kStep + 8 * t;
+  // the current step, of which only the first `left` values of k exist
+  __device__ __forceinline__ Regs load_tail(int left, int t) const {
+    return Regs{load8_checked(r0, 0, left - 8 * t, VEC), load8_checked(r1, 0, left - 8 * t, VEC)};
+  }
+  template <int NT, int OFF, class X, class N>
+  __device__ __forceinline__ void step(const Regs& r, const X& x, N nt, float (&acc)[NT][4]) const {
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
-      if (i < nt) {
-        const uint4 b = xb(i, k);
+      if (i == 0 || i < nt) {
+        const uint4 b = x.template load<OFF>(i);
         T::mma(acc[i], r.a.x, r.b.x, r.a.y, r.b.y, b.x, b.y);
         T::mma(acc[i], r.a.z, r.b.z, r.a.w, r.b.w, b.z, b.w);
       }
     }
   }
+  template <int NT, class X, class N>
+  __device__ __forceinline__ void step_tail(const Regs& r, int, const X& x, N nt, float (&acc)[NT][4]) const {
+    step<NT, 0>(r, x, nt, acc);
+  }
 };
 
-// 4-bit weights, PER groups of 128 / PER weights in a step of 128.
-template <class T, int PER>
+// 4-bit weights, PER groups of 128 / PER weights in a step of 128.  ZEROS: with zero points, else 8 everywhere.
+template <class T, int PER, bool ZEROS>
 struct RowsQ4 {
   static constexpr int kStep = 128;
   const uint8_t *c0, *c1;        // codes
   const uint16_t *s0, *s1;       // scales
-  const uint8_t *z0, *z1;        // zero points (NULL: 8)
+  const uint8_t *z0, *z1;        // zero points
   struct Regs {
     uint4 a, b;
     uint32_t sa[(PER + 1) / 2], sb[(PER + 1) / 2];
@@ -128,28 +173,43 @@ struct RowsQ4 {
   };
 
   static __device__ __forceinline__ void load_scales(uint32_t (&v)[(PER + 1) / 2], const uint16_t* p) {
-    if constexpr (PER == 1) v[0] = __ldg(p);
-    else if constexpr (PER == 2) v[0] = __ldg(reinterpret_cast<const uint32_t*>(p));
-    else { const uint2 w = __ldg(reinterpret_cast<const uint2*>(p)); v[0] = w.x; v[1] = w.y; }
+    if constexpr (PER == 1) {
+      uint16_t h;
+      asm volatile("ld.global.nc.u16 %0, [%1];" : "=h"(h) : "l"(p));
+      v[0] = h;
+    } else if constexpr (PER == 2) {
+      asm volatile("ld.global.nc.u32 %0, [%1];" : "=r"(v[0]) : "l"(p));
+    } else {
+      asm volatile("ld.global.nc.v2.u32 {%0, %1}, [%2];" : "=r"(v[0]), "=r"(v[1]) : "l"(p));
+    }
   }
   static __device__ __forceinline__ uint32_t load_zeros(const uint8_t* p) {
-    if constexpr (PER == 1) return __ldg(p);
-    else if constexpr (PER == 2) return __ldg(reinterpret_cast<const uint16_t*>(p));
-    else return __ldg(reinterpret_cast<const uint32_t*>(p));
+    uint32_t v;
+    if constexpr (PER == 1) asm volatile("ld.global.nc.u8 %0, [%1];" : "=r"(v) : "l"(p));
+    else if constexpr (PER == 2) asm volatile("ld.global.nc.u16 %0, [%1];" : "=r"(v) : "l"(p));
+    else asm volatile("ld.global.nc.u32 %0, [%1];" : "=r"(v) : "l"(p));
+    return v;
   }
-  __device__ __forceinline__ Regs load(int s, int, int t) const {
+  __device__ __forceinline__ void begin(int t) { c0 += 16 * t; c1 += 16 * t; }
+  __device__ __forceinline__ void advance(int n) {
+    c0 += n * 64; c1 += n * 64;
+    s0 += n * PER; s1 += n * PER;
+    if constexpr (ZEROS) { z0 += n * PER; z1 += n * PER; }
+  }
+  __device__ __forceinline__ Regs load(int n) const {
     Regs r;
-    r.a = ldg_weights(c0 + (int64_t)s * 64 + 16 * t);
-    r.b = ldg_weights(c1 + (int64_t)s * 64 + 16 * t);
-    load_scales(r.sa, s0 + (int64_t)s * PER);
-    load_scales(r.sb, s1 + (int64_t)s * PER);
-    r.za = r.zb = 0x08080808u;
-    if (z0 != nullptr) {
-      r.za = load_zeros(z0 + (int64_t)s * PER);
-      r.zb = load_zeros(z1 + (int64_t)s * PER);
+    r.a = ldg_weights(c0 + n * 64);
+    r.b = ldg_weights(c1 + n * 64);
+    load_scales(r.sa, s0 + n * PER);
+    load_scales(r.sb, s1 + n * PER);
+    if constexpr (ZEROS) {
+      r.za = load_zeros(z0 + n * PER);
+      r.zb = load_zeros(z1 + n * PER);
     }
     return r;
   }
+  __device__ __forceinline__ Regs load_tail(int, int) const { return load(0); }   // rows are padded to whole steps
+
   // The eight weights of a word as four pairs of exact 16-bit numbers code - zero: a code put under the exponent of
   // 128 (bf16) or 1024 (fp16) is that number plus the code, and subtracting the same number plus zero leaves the difference.
   static __device__ __forceinline__ void unpack(uint32_t w, uint32_t base_zero, uint32_t (&p)[4]) {
@@ -160,18 +220,15 @@ struct RowsQ4 {
       p[i] = T::sub2(v, base_zero);
     }
   }
-  template <int NT, class XB>
-  __device__ __forceinline__ void step(const Regs& r, int s, int K, int t, const XB& xb, int nt, float (&acc)[NT][4]) const {
+  template <int NT, int OFF, bool TAIL, class X, class N>
+  __device__ __forceinline__ void products(const Regs& r, int left, const X& x, N nt, float (&acc)[NT][4]) const {
     const uint32_t wa[4] = {r.a.x, r.a.y, r.a.z, r.a.w}, wb[4] = {r.b.x, r.b.y, r.b.z, r.b.w};
 #pragma unroll
     for (int q = 0; q < PER; ++q) {
-      const int kq = s * kStep + q * (128 / PER);
-      if (PER > 1 && kq >= K) break;   // a group of padding alone: its scale may be anything
-      const uint32_t za = T::kNibbleBase | ((r.za >> (8 * q)) & 0xffu) * 0x00010001u;
-      const uint32_t zb = T::kNibbleBase | ((r.zb >> (8 * q)) & 0xffu) * 0x00010001u;
+      if (TAIL && q * (128 / PER) >= left) break;   // groups of padding alone: their scales may be anything
+      const uint32_t za = T::kNibbleBase | (ZEROS ? ((r.za >> (8 * q)) & 0xffu) * 0x00010001u : 0x00080008u);
+      const uint32_t zb = T::kNibbleBase | (ZEROS ? ((r.zb >> (8 * q)) & 0xffu) * 0x00010001u : 0x00080008u);
       float part[NT][4];
-#pragma unroll
-      for (int i = 0; i < NT; ++i) part[i][0] = part[i][1] = part[i][2] = part[i][3] = 0.f;
 #pragma unroll
       for (int j = 4 / PER * q; j < 4 / PER * (q + 1); ++j) {
         uint32_t pa[4], pb[4];
@@ -179,9 +236,10 @@ struct RowsQ4 {
         unpack(wb[j], zb, pb);
 #pragma unroll
         for (int i = 0; i < NT; ++i) {
-          if (i < nt) {
-            const uint4 b = xb(i, s * kStep + 32 * j + 8 * t);
-            T::mma(part[i], pa[0], pb[0], pa[1], pb[1], b.x, b.y);
+          if (i == 0 || i < nt) {
+            const uint4 b = j == 0 ? x.template load<OFF>(i) : j == 1 ? x.template load<OFF + 32>(i) : j == 2 ? x.template load<OFF + 64>(i) : x.template load<OFF + 96>(i);
+            if (j == 4 / PER * q) T::mma0(part[i], pa[0], pb[0], pa[1], pb[1], b.x, b.y);
+            else T::mma(part[i], pa[0], pb[0], pa[1], pb[1], b.x, b.y);
             T::mma(part[i], pa[2], pb[2], pa[3], pb[3], b.z, b.w);
           }
         }
@@ -189,7 +247,7 @@ struct RowsQ4 {
       const float sa = T::to_float((uint16_t)(r.sa[q / 2] >> (16 * (q % 2)))), sb = T::to_float((uint16_t)(r.sb[q / 2] >> (16 * (q % 2))));
 #pragma unroll
       for (int i = 0; i < NT; ++i) {
-        if (i < nt) {
+        if (i == 0 || i < nt) {
           acc[i][0] = fmaf(sa, part[i][0], acc[i][0]);
           acc[i][1] = fmaf(sa, part[i][1], acc[i][1]);
           acc[i][2] = fmaf(sb, part[i][2], acc[i][2]);
@@ -198,31 +256,86 @@ struct RowsQ4 {
       }
     }
   }
+  template <int NT, int OFF, class X, class N>
+  __device__ __forceinline__ void step(const Regs& r, const X& x, N nt, float (&acc)[NT][4]) const {
+    products<NT, OFF, false>(r, 128, x, nt, acc);
+  }
+  template <int NT, class X, class N>
+  __device__ __forceinline__ void step_tail(const Regs& r, int left, const X& x, N nt, float (&acc)[NT][4]) const {
+    products<NT, 0, true>(r, left, x, nt, acc);
+  }
 };
 
 // ---- a warp's walk over its steps -----------------------------------------------------------------------------
-// Steps s, s + ds, ... below `end`, with DEPTH steps' loads in flight: preload() issues the first ones (before the
-// activations are needed), walk() computes a step and at once refills its registers.
-template <class F, int DEPTH>
+// `n` whole steps, DS apart, with DEPTH steps' loads in flight: preload() issues the first ones (before the
+// activations are needed), walk() computes a step and at once refills its registers.  While 2 * DEPTH steps are left
+// nothing is checked.  Afterwards f and x point behind the n steps.
+template <class F, int DS, int DEPTH>
 struct Stream {
   typename F::Regs buf[DEPTH];
-  __device__ __forceinline__ void preload(const F& f, int s, int ds, int end, int K, int t) {
+
+  __device__ __forceinline__ void preload(const F& f, int n) {
 #pragma unroll
     for (int u = 0; u < DEPTH; ++u)
-      if (s + u * ds < end) buf[u] = f.load(s + u * ds, K, t);
+      if (u < n) buf[u] = f.load(u * DS);
   }
-  template <int NT, class XB>
-  __device__ __forceinline__ void walk(const F& f, int s, int ds, int end, int K, int t, const XB& xb, int nt, float (&acc)[NT][4]) {
-    for (; s < end; s += DEPTH * ds) {
-#pragma unroll
-      for (int u = 0; u < DEPTH; ++u) {
-        const int now = s + u * ds, next = now + DEPTH * ds;
-        if (now < end) f.template step<NT>(buf[u], now, K, t, xb, nt, acc);
-        if (next < end) buf[u] = f.load(next, K, t);
-      }
+  template <int NT, int U, class X, class N>
+  __device__ __forceinline__ void round(const F& f, int n, bool all, const X& x, N nt, float (&acc)[NT][4]) {
+    if constexpr (U < DEPTH) {
+      if (all || U < n) f.template step<NT, U * DS * F::kStep>(buf[U], x, nt, acc);
+      if (all || U + DEPTH < n) buf[U] = f.load((U + DEPTH) * DS);
+      round<NT, U + 1>(f, n, all, x, nt, acc);
+    }
+  }
+  template <int NT, class X, class N>
+  __device__ __forceinline__ void walk(F& f, int n, X& x, N nt, float (&acc)[NT][4]) {
+    while (n >= 2 * DEPTH) {
+      round<NT, 0>(f, n, true, x, nt, acc);
+      f.advance(DEPTH * DS);
+      x.advance(DEPTH * DS * F::kStep);
+      n -= DEPTH;
+    }
+    while (n > 0) {
+      round<NT, 0>(f, n, false, x, nt, acc);
+      const int done = n < DEPTH ? n : DEPTH;
+      f.advance(done * DS);
+      x.advance(done * DS * F::kStep);
+      n -= done;
     }
   }
 };
+
+// All NT tiles of columns, known when compiling: the `nt` of the functions above.
+template <int NT> struct All { __device__ constexpr operator int() const { return NT; } };
+
+// 16 bytes of shared memory
+__device__ __forceinline__ uint4 lds128(uint32_t at) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
+  return v;
+}
+// Waits for the copies of a piece.  The wait is bounded (some hundred milliseconds); one that gives up says so and the kernel
+// goes on to its end, where the host can learn of it (exo_decode_check).
+static __device__ unsigned gave_up;
+__device__ __forceinline__ void wait_piece(uint32_t bar, uint32_t parity) {
+  for (int i = 0; i < (1 << 22); ++i) {
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    if (ok) return;
+  }
+  gave_up = 1;
+}
+
+// This translation unit's word, put back to 0.
+static inline unsigned take_gave_up(cudaError_t* e) {
+  unsigned v = 0, zero = 0;
+  *e = cudaMemcpyFromSymbol(&v, gave_up, sizeof v);
+  if (*e == cudaSuccess && v) *e = cudaMemcpyToSymbol(gave_up, &zero, sizeof zero);
+  return v;
+}
+
+// How many of the steps s, s + ds, ... lie below `end`.
+__device__ __forceinline__ int steps_of(int s, int ds, int end) { return s < end ? (end - s + ds - 1) / ds : 0; }
 
 }  // namespace decode
 }  // namespace exo

@@ -1,5 +1,6 @@
 // Host side of the few-token operators: device check and launch.
 #pragma once
+#include <cuda.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -9,6 +10,11 @@
 
 namespace exo {
 void note_cuda_error(int e);   // what exo_gemm_last_cuda_error reports (api.cu)
+// Tensor map for copies of `steps` steps of 16 rows of a 4-bit matrix (api.cu, which looks the encoder up).
+bool encode_steps_map(CUtensorMap* map, const void* codes, uint64_t rows, uint64_t blocks, uint32_t steps);
+// The same for copies of a box of words (2 or 4 bytes) from the rows of a matrix.
+bool encode_rows_map(CUtensorMap* map, int word_bytes, const void* base, uint64_t row_words, uint64_t rows, uint64_t row_bytes, uint32_t box_words,
+                     uint32_t box_rows);
 
 namespace decode {
 
@@ -46,7 +52,7 @@ inline bool q4_aligned(const void* codes, const void* scales, const void* zeros,
 
 // One launch with programmatic dependent launch and, for cluster > 1, clusters of that many CTAs along x.
 inline exo_gemm_status_t launch(void* fn, unsigned grid_x, unsigned grid_y, unsigned threads, size_t smem, unsigned cluster,
-                                cudaStream_t stream, void* params) {
+                                cudaStream_t stream, void* params, void* params2 = nullptr, void* params3 = nullptr) {
   cudaError_t e;
   // always the same opt-in, so that threads which launch one kernel at different sizes cannot take it from each other
   if (smem > 48 * 1024 && (e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostSmem)) != cudaSuccess)
@@ -65,7 +71,7 @@ inline exo_gemm_status_t launch(void* fn, unsigned grid_x, unsigned grid_y, unsi
   at[1].val.clusterDim.z = 1;
   lc.attrs = at;
   lc.numAttrs = cluster > 1 ? 2 : 1;
-  void* args[1] = {params};
+  void* args[3] = {params, params2, params3};
   e = cudaLaunchKernelExC(&lc, fn, args);
   return e == cudaSuccess ? EXO_GEMM_OK : cuda_failed(e);
 }

@@ -21,7 +21,7 @@ namespace decode {
 
 constexpr int kMaxTokens = 64, kMaxExperts = 512, kMaxShared = 8, kMaxTopK = 16;
 
-struct Active { int expert, base, count, pad; };   // a taken expert: its tokens are entries base .. base + count - 1
+struct Active { int expert, base, count, cost_before; };   // a taken expert: its tokens are entries base .. base + count - 1
 
 namespace {
 
@@ -52,31 +52,13 @@ struct MoeParams {
   float* entry_weight;
   float* logits;            // tokens x experts
   uint16_t* h;              // entries x ldh
+  const uint16_t* xs;       // x itself, or (copy_x) route's copy in rows of ldxs elements, a multiple of 128, filled with zeros
+  int64_t ldxs;
+  bool copy_x;
+  int up_piece, down_piece;
 };
 
-// Row formats by number: 0 = 16-bit rows anywhere, 1 = 16-bit rows on 16-byte boundaries, 2 + n = 4-bit, 2^n groups in 128.
-template <class T, int FMT> struct FormatOf { using type = RowsQ4<T, 1 << (FMT - 2)>; };
-template <class T> struct FormatOf<T, 0> { using type = Rows16<T, false>; };
-template <class T> struct FormatOf<T, 1> { using type = Rows16<T, true>; };
-
-template <class T, int FMT>
-__device__ __forceinline__ typename FormatOf<T, FMT>::type rows_of(const Stack& m0, int64_t row0, const Stack& m1, int64_t row1) {
-  typename FormatOf<T, FMT>::type f;
-  if constexpr (FMT < 2) {
-    f.r0 = static_cast<const uint16_t*>(m0.w) + row0 * m0.ld;
-    f.r1 = static_cast<const uint16_t*>(m1.w) + row1 * m1.ld;
-  } else {
-    constexpr int PER = 1 << (FMT - 2);
-    const int64_t blocks = (m0.K + 127) / 128;
-    f.c0 = static_cast<const uint8_t*>(m0.w) + row0 * blocks * 64;
-    f.c1 = static_cast<const uint8_t*>(m1.w) + row1 * blocks * 64;
-    f.s0 = m0.scales + row0 * blocks * PER;
-    f.s1 = m1.scales + row1 * blocks * PER;
-    f.z0 = m0.zeros ? m0.zeros + row0 * blocks * PER : nullptr;
-    f.z1 = m1.zeros ? m1.zeros + row1 * blocks * PER : nullptr;
-  }
-  return f;
-}
+// Weight formats by number: 0 = 16-bit rows anywhere, 1 = 16-bit rows on 16-byte boundaries, 2 + n = 4-bit, 2^n groups in 128.
 
 template <int NT> __device__ __forceinline__ void clear(float (&acc)[NT][4]) {
 #pragma unroll
@@ -103,7 +85,8 @@ struct RouteTables {
   float weight[kMaxTokens * kMaxTopK];
 };
 
-__device__ void route_tokens(const MoeParams& p, RouteTables& tb) {
+template <int EPL>   // experts per lane
+__device__ __forceinline__ void route_tokens(const MoeParams& p, RouteTables& tb) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int all = p.experts + p.shared;
   for (int e = threadIdx.x; e < all; e += kRouteThreads)
@@ -111,10 +94,10 @@ __device__ void route_tokens(const MoeParams& p, RouteTables& tb) {
   __syncthreads();
   for (int token = warp; token < p.tokens; token += kRouteWarps) {
     const float* l = p.logits + (int64_t)token * p.experts;
-    float mine[kMaxExperts / 32];
-    uint32_t key[kMaxExperts / 32];
+    float mine[EPL];
+    uint32_t key[EPL];
 #pragma unroll
-    for (int j = 0; j < kMaxExperts / 32; ++j) {
+    for (int j = 0; j < EPL; ++j) {
       const int e = 32 * j + lane;
       key[j] = 0;
       if (e < p.experts) { mine[j] = __ldcg(l + e); key[j] = key_of(mine[j]); }
@@ -126,7 +109,7 @@ __device__ void route_tokens(const MoeParams& p, RouteTables& tb) {
       int at = 0;
       float val = 0.f;
 #pragma unroll
-      for (int j = 0; j < kMaxExperts / 32; ++j)
+      for (int j = 0; j < EPL; ++j)
         if (32 * j < p.experts && key[j] > best) { best = key[j]; at = 32 * j + lane; val = mine[j]; }
       const uint32_t most = __reduce_max_sync(0xffffffffu, best);
       const int e = (int)__reduce_min_sync(0xffffffffu, best == most ? (uint32_t)at : 0xffffffffu);
@@ -134,7 +117,7 @@ __device__ void route_tokens(const MoeParams& p, RouteTables& tb) {
       if (r == 0) top = val;
       if (lane == r) { my_expert = e; my_logit = val; }
 #pragma unroll
-      for (int j = 0; j < kMaxExperts / 32; ++j)
+      for (int j = 0; j < EPL; ++j)
         if (32 * j + lane == e) key[j] = 0;
     }
     float total;
@@ -143,7 +126,7 @@ __device__ void route_tokens(const MoeParams& p, RouteTables& tb) {
     } else {
       total = 0.f;
 #pragma unroll
-      for (int j = 0; j < kMaxExperts / 32; ++j)
+      for (int j = 0; j < EPL; ++j)
         if (32 * j + lane < p.experts) total += expf(mine[j] - top);
     }
 #pragma unroll
@@ -207,15 +190,27 @@ __global__ void __launch_bounds__(kRouteThreads) exo_moe_route_kernel(const MoeP
   f.r1 = p.router + (int64_t)min(e0 + g + 8, p.experts - 1) * p.ld_router;
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();
+  if (p.copy_x) {   // for `up`
+    const int per = (int)(p.ldxs / 8);
+    for (int i = blockIdx.x * kRouteThreads + threadIdx.x; i < p.tokens * per; i += gridDim.x * kRouteThreads) {
+      const int token = i / per, e = i - token * per;
+      *reinterpret_cast<uint4*>(const_cast<uint16_t*>(p.xs) + token * p.ldxs + 8 * e) = load8_checked(p.x + token * p.ldx, 8 * e, p.hidden, p.x_aligned);
+    }
+  }
   float acc[NT][4];
   clear(acc);
-  const int steps = (p.hidden + 31) / 32, ds = S * kRouteWarps, s = r * kRouteWarps + warp;
-  Stream<Rows16<T, VEC>, 2> stream;
-  stream.preload(f, s, ds, steps, p.hidden, t);
-  stream.template walk<NT>(f, s, ds, steps, p.hidden, t, [&](int i, int k) {
-    const int token = 8 * i + g;
-    return token < p.tokens ? load8_checked(p.x + token * p.ldx, k, p.hidden, p.x_aligned) : make_uint4(0, 0, 0, 0);
-  }, nt, acc);
+  const int steps = (p.hidden + 31) / 32, ds = S * kRouteWarps;
+  for (int s = r * kRouteWarps + warp; s < steps; s += ds) {
+    const int k = s * 32 + 8 * t;
+    const uint4 wa = load8_checked(f.r0, k, p.hidden, VEC), wb = load8_checked(f.r1, k, p.hidden, VEC);
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+      if (i < nt) {
+        const uint4 b = load8_checked(p.x + (int64_t)min(8 * i + g, p.tokens - 1) * p.ldx, k, p.hidden, p.x_aligned);
+        T::mma(acc[i], wa.x, wb.x, wa.y, wb.y, b.x, b.y);
+        T::mma(acc[i], wa.z, wb.z, wa.w, wb.w, b.z, b.w);
+      }
+  }
   float4* red = reinterpret_cast<float4*>(smem);   // [warp][nt][lane]
   float4* part = red + kRouteWarps * nt * 32;
 #pragma unroll
@@ -248,56 +243,287 @@ __global__ void __launch_bounds__(kRouteThreads) exo_moe_route_kernel(const MoeP
     if (last) { *p.arrivals = 0; __threadfence(); }
   }
   __syncthreads();
-  if (last) route_tokens(p, tables);
+  if (!last) return;
+  if (p.experts <= 64) route_tokens<2>(p, tables);
+  else if (p.experts <= 128) route_tokens<4>(p, tables);
+  else route_tokens<16>(p, tables);
+}
+
+// Inner activations from lane l's part of tile i: gate in v.x, v.y and up in v.z, v.w for two tokens.
+template <class T>
+__device__ __forceinline__ void store_inner(const MoeParams& p, const Active& a, int f0, int i, int l, const float4& v) {
+  const int n = 8 * i + 2 * (l & 3), col = f0 + (l >> 2);
+  if (col >= p.inner) return;
+  const float gate[2] = {v.x, v.y}, up[2] = {v.z, v.w};
+#pragma unroll
+  for (int q = 0; q < 2; ++q)
+    if (n + q < a.count) {
+      const float w = __ldcg(p.entry_weight + a.base + n + q);
+      p.h[(int64_t)(a.base + n + q) * p.ldh + col] = T::from_float(w * (gate[q] / (1.f + expf(-gate[q])) * up[q]));
+    }
+}
+
+// ==== the taken experts' weights ====================================================================================
+// A warp's own ring of pieces: `piece` steps (64 bytes of a row each, an odd number of them, so that the rows of a fragment
+// lie in different banks) of 16 rows, brought by tiled copies that the warp issues itself and waits for itself.
+constexpr int kMoeWarps = 8, kMoeThreads = 32 * kMoeWarps, kMoeStages = 2, kMostPiece = 7;
+
+struct Ring {
+  uint32_t bar, base;
+  int stage_bytes, pitch, put = 0, take = 0;
+  uint32_t parity = 0;
+
+  __device__ __forceinline__ void begin(uint8_t* bars, uint8_t* stages, int piece, int warp, int lane) {
+    pitch = piece * 64;
+    stage_bytes = 16 * pitch;
+    bar = ptx::smem_u32(bars) + warp * kMoeStages * 8;
+    base = ptx::smem_u32(stages) + warp * kMoeStages * stage_bytes;
+    if (lane == 0)
+      for (int i = 0; i < kMoeStages; ++i) ptx::mbar_init(bar + 8 * i, 1);
+    ptx::fence_mbar_init();
+    __syncwarp();
+  }
+  // one lane: a piece of rows r0 .. r0 + 7 of one map and r1 .. r1 + 7 of the other, or (m1 == nullptr) of 16 rows of one
+  __device__ __forceinline__ void copy(const CUtensorMap* m0, int r0, const CUtensorMap* m1, int r1, int x) {
+    ptx::mbar_arrive_expect_tx(bar + 8 * put, stage_bytes);
+    ptx::tma_load_2d(base + put * stage_bytes, m0, x, r0, bar + 8 * put);
+    if (m1) ptx::tma_load_2d(base + put * stage_bytes + 8 * pitch, m1, x, r1, bar + 8 * put);
+  }
+  __device__ __forceinline__ void copied() { put = put + 1 == kMoeStages ? 0 : put + 1; }
+  __device__ __forceinline__ uint32_t wait() const { wait_piece(bar + 8 * take, parity); return base + take * stage_bytes; }
+  __device__ __forceinline__ void taken() {
+    take = take + 1 == kMoeStages ? 0 : take + 1;
+    parity ^= take == 0 ? 1u : 0u;
+  }
+};
+
+// What a warp needs to multiply a piece, by format.  The activations of a tile are loaded while the tile, or the piece, before
+// it is multiplied: first(row, s, n) at the very beginning, then multiply() with the place of the next piece.
+//   xr(i)   the lane's row of tile i at the piece's first k
+//   next    the lane's row of tile 0 at the next piece's first k, of n_next steps (0: there is none)
+template <class T>
+struct Piece16 {
+  static constexpr int kStep = 32, kWords = 32;     // weights of a step, and elements of the tensor map
+  uint4 x[2][kMostPiece];
+  __device__ __forceinline__ void rows(const Stack&, int64_t, const Stack&, int64_t) {}
+  template <int B> __device__ __forceinline__ void load(const uint16_t* row, int n) {
+#pragma unroll
+    for (int u = 0; u < kMostPiece; ++u)
+      if (u < n) x[B][u] = *reinterpret_cast<const uint4*>(row + 32 * u);
+  }
+  __device__ __forceinline__ void first(const uint16_t* row, int n) { load<0>(row, n); }
+  template <int NT, int I, class XR>
+  __device__ __forceinline__ void tile(uint32_t w, int pitch, int n, const XR& xr, const uint16_t* next, int n_next, int nt, float (&acc)[NT][4]) {
+    if constexpr (I < NT) {
+      if (I == 0 || I < nt) {
+        if (I + 1 < nt) load<(I + 1) % 2>(xr(I + 1), n);
+        else load<(I + 1) % 2>(next, n_next);
+#pragma unroll
+        for (int u = 0; u < kMostPiece; ++u)
+          if (u < n) {
+            const uint4 a = lds128(w + u * 64), b = lds128(w + 8 * pitch + u * 64);
+            T::mma(acc[I], a.x, b.x, a.y, b.y, x[I % 2][u].x, x[I % 2][u].y);
+            T::mma(acc[I], a.z, b.z, a.w, b.w, x[I % 2][u].z, x[I % 2][u].w);
+          }
+        tile<NT, I + 1>(w, pitch, n, xr, next, n_next, nt, acc);
+      }
+    }
+  }
+  template <int NT, class XR>
+  __device__ __forceinline__ void multiply(uint32_t w, int pitch, int, int n, const XR& xr, const uint16_t* next, int n_next, int nt, float (&acc)[NT][4]) {
+    tile<NT, 0>(w, pitch, n, xr, next, n_next, nt, acc);
+    if (NT == 1 || (nt & 1)) {
+#pragma unroll
+      for (int u = 0; u < kMostPiece; ++u) x[0][u] = x[1][u];
+    }
+  }
+};
+
+template <class T, int PER>
+struct PieceQ4 {
+  using F = RowsQ4<T, PER, true>;
+  static constexpr int kStep = 128, kWords = 16;
+  const uint16_t *s0, *s1;
+  const uint8_t *z0, *z1;
+  int K;
+  typename F::Regs r;
+  uint4 x[4];
+  __device__ __forceinline__ void rows(const Stack& m0, int64_t row0, const Stack& m1, int64_t row1) {
+    const int64_t groups = (int64_t)((m0.K + 127) / 128) * PER;
+    s0 = m0.scales + row0 * groups;
+    s1 = m1.scales + row1 * groups;
+    z0 = m0.zeros ? m0.zeros + row0 * groups : nullptr;
+    z1 = m1.zeros ? m1.zeros + row1 * groups : nullptr;
+    K = m0.K;
+  }
+  __device__ __forceinline__ void scales(int s) {
+    F::load_scales(r.sa, s0 + s * PER);
+    F::load_scales(r.sb, s1 + s * PER);
+    r.za = r.zb = 0x08080808u;
+    if (z0) r.za = F::load_zeros(z0 + s * PER);
+    if (z1) r.zb = F::load_zeros(z1 + s * PER);
+    if (PER > 1 && (s + 1) * 128 > K) {              // groups of padding alone: their scales may be anything
+#pragma unroll
+      for (int q = 1; q < PER; ++q)
+        if (s * 128 + q * (128 / PER) >= K) {
+          r.sa[q / 2] &= q % 2 ? 0x0000ffffu : 0xffff0000u;
+          r.sb[q / 2] &= q % 2 ? 0x0000ffffu : 0xffff0000u;
+        }
+    }
+  }
+  __device__ __forceinline__ void activations(const uint16_t* xr) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = *reinterpret_cast<const uint4*>(xr + 32 * j);
+  }
+  __device__ __forceinline__ void first(const uint16_t* row, int) { activations(row); }
+  struct FirstTile {
+    const uint4 (&v)[4];
+    template <int OFF> __device__ __forceinline__ uint4 load(int) const { return v[OFF / 32]; }
+  };
+  template <class XR> struct Tiles {
+    const XR& xr;
+    int at;
+    template <int OFF> __device__ __forceinline__ uint4 load(int i) const { return *reinterpret_cast<const uint4*>(xr(i) + at + OFF); }
+  };
+  template <int NT, class XR>
+  __device__ __forceinline__ void multiply(uint32_t w, int pitch, int s, int n, const XR& xr, const uint16_t* next, int n_next, int nt, float (&acc)[NT][4]) {
+    scales(s);
+    for (int u = 0; u < n; ++u) {
+      typename F::Regs now = r;
+      now.a = lds128(w + u * 64);
+      now.b = lds128(w + 8 * pitch + u * 64);
+      F f;
+      if constexpr (NT == 1) {
+        const uint4 mine[4] = {x[0], x[1], x[2], x[3]};
+        if (u + 1 < n) { scales(s + u + 1); activations(xr(0) + (u + 1) * 128); }
+        else if (n_next) activations(next);
+        f.template step<NT, 0>(now, FirstTile{mine}, All<NT>(), acc);
+      } else {
+        if (u + 1 < n) scales(s + u + 1);
+        f.template step<NT, 0>(now, Tiles<XR>{xr, u * 128}, nt, acc);
+      }
+    }
+  }
+};
+template <class T, int FMT> struct PieceOf { using type = PieceQ4<T, 1 << (FMT - 2)>; };
+template <class T> struct PieceOf<T, 1> { using type = Piece16<T>; };
+
+// A CTA cuts its items into parts while it has fewer units than this: two turns of its warps, or one where the sums are large.
+__host__ __device__ constexpr int part_limit(int nt) { return nt <= 2 ? 2 * kMoeWarps : kMoeWarps; }
+
+// The routing tables, copied to shared memory.
+struct Tables {
+  Active active[kMaxExperts + kMaxShared];
+  int token[kMaxTokens * (kMaxTopK + kMaxShared)];
+  int cost;                  // of a step of every taken expert
+};
+__device__ __forceinline__ void copy_tables(Tables& tb, const MoeParams& p) {
+  const int all = p.experts + p.shared, entries = p.tokens * (p.top_k + p.shared);
+  for (int i = threadIdx.x; i < all; i += kMoeThreads) *reinterpret_cast<int4*>(&tb.active[i]) = __ldcg(reinterpret_cast<const int4*>(p.active) + i);
+  for (int i = threadIdx.x; i < entries; i += kMoeThreads) tb.token[i] = __ldcg(p.entry_token + i);
 }
 
 // ==== up ==========================================================================================================
-// A CTA computes 8 inner values of one taken expert for its tokens: the 16 rows of a fragment are eight rows of gate and
-// the same eight of up, so that a lane ends with both factors of an activation.  Eight warps cut `hidden`.
-constexpr int kUpThreads = 256, kUpWarps = 8;
-
+// An item is 8 inner values of one taken expert for its tokens: the 16 rows of a fragment are eight rows of gate and the
+// same eight of up, so that a lane ends with both factors of an activation.  The grid shares the items out; a CTA's warps
+// take its items one by one, or, where there are fewer items than warps, parts of their `hidden`, whose sums meet in
+// shared memory in order.
 template <class T, int FMT, int NT>
-__global__ void __launch_bounds__(kUpThreads) exo_moe_up_kernel(const MoeParams p) {
-  __shared__ float4 red[kUpWarps * NT * 32];
+__global__ void __launch_bounds__(kMoeThreads, 2)
+exo_moe_up_ring_kernel(const MoeParams p, const __grid_constant__ CUtensorMap gate_map, const __grid_constant__ CUtensorMap up_map) {
+  using P = typename PieceOf<T, FMT>::type;
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ Tables tb;
+  __shared__ __align__(8) uint8_t bars[kMoeWarps * kMoeStages * 8];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+  Ring ring;
+  ring.begin(bars, smem, p.up_piece, warp, lane);
+  float4* sums = reinterpret_cast<float4*>(smem + kMoeWarps * kMoeStages * ring.stage_bytes);   // [unit][tile][lane]
+  const int tiles = (p.inner + 7) / 8, steps = (p.hidden + P::kStep - 1) / P::kStep, pieces = (steps + p.up_piece - 1) / p.up_piece;
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();   // after the wait: `down` may then read the tables of `route` before it waits itself
-  if ((int)blockIdx.y >= __ldcg(p.n_active)) return;
-  const int4 raw = __ldcg(reinterpret_cast<const int4*>(p.active + blockIdx.y));
-  const Active a{raw.x, raw.y, raw.z, raw.w};
-  const int f0 = blockIdx.x * 8, nt = (a.count + 7) / 8;
-  const int64_t row = min(f0 + g, p.inner - 1);
-  using F = typename FormatOf<T, FMT>::type;
-  const F f = rows_of<T, FMT>(p.gate, a.expert * p.gate.expert_rows + row, p.up, a.expert * p.up.expert_rows + row);
-  const int steps = (p.hidden + F::kStep - 1) / F::kStep;
-  constexpr int DEPTH = NT <= 2 ? 4 : 2;
-  Stream<F, DEPTH> stream;
-  stream.preload(f, warp, kUpWarps, steps, p.hidden, t);
-  const uint16_t* xrow[NT];
-#pragma unroll
-  for (int i = 0; i < NT; ++i)
-    xrow[i] = 8 * i + g < a.count ? p.x + (int64_t)__ldcg(p.entry_token + a.base + 8 * i + g) * p.ldx : nullptr;
-  float acc[NT][4];
-  clear(acc);
-  stream.template walk<NT>(f, warp, kUpWarps, steps, p.hidden, t, [&](int i, int k) {
-    return xrow[i] ? load8_checked(xrow[i], k, p.hidden, p.x_aligned) : make_uint4(0, 0, 0, 0);
-  }, nt, acc);
-#pragma unroll
-  for (int i = 0; i < NT; ++i)
-    if (i < nt) red[(warp * nt + i) * 32 + lane] = make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
+  const int items = __ldcg(p.n_active) * tiles;
+  copy_tables(tb, p);
   __syncthreads();
-  for (int idx = threadIdx.x; idx < nt * 32; idx += kUpThreads) {
-    float4 v = red[idx];
-    for (int q = 1; q < kUpWarps; ++q) add(v, red[q * nt * 32 + idx]);
-    const int n = 8 * (idx >> 5) + 2 * (idx & 3), col = f0 + ((idx & 31) >> 2);
-    if (col < p.inner) {
-      const float gate[2] = {v.x, v.y}, up[2] = {v.z, v.w};
+  const int mine = (int)blockIdx.x < items ? (items - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x : 0;
+  int nk_log = 0;
+  while (nk_log < 3 && (mine << nk_log) < part_limit(NT) && (2 << nk_log) <= pieces) ++nk_log;
+  const int units = mine << nk_log, nk = 1 << nk_log;
+  auto begin_of = [&](int u) { return (pieces * (u & (nk - 1))) >> nk_log; };
+  auto end_of = [&](int u) { return (pieces * ((u & (nk - 1)) + 1)) >> nk_log; };
+  auto item_of = [&](int u) { return (int)blockIdx.x + (u >> nk_log) * (int)gridDim.x; };
+
+  int iu = warp, ip = begin_of(iu), igate = 0, iup = 0;
+  auto open = [&]() {
+    const int item = item_of(iu), at = item / tiles, f0 = (item - at * tiles) * 8;
+    igate = (int)(tb.active[at].expert * p.gate.expert_rows) + f0;
+    iup = (int)(tb.active[at].expert * p.up.expert_rows) + f0;
+  };
+  auto issue = [&]() {
+    if (iu < units) {
+      if (lane == 0) ring.copy(&gate_map, igate, &up_map, iup, ip * p.up_piece * P::kWords);
+      ring.copied();
+      if (++ip == end_of(iu)) {
+        iu += kMoeWarps;
+        ip = begin_of(iu);
+        if (iu < units) open();
+      }
+    }
+  };
+  if (iu < units) open();
+  for (int i = 0; i < kMoeStages; ++i) issue();
+
+  // the lane's row of activations for tile i of an item's tokens; columns without a token repeat the last one's
+  auto row_of = [&](const Active& a, int i) { return p.xs + (int64_t)tb.token[a.base + min(8 * i + g, a.count - 1)] * p.ldxs + 8 * t; };
+  auto steps_at = [&](int c) { return min(p.up_piece, steps - c * p.up_piece); };
+  P piece;
+  if (warp < units) piece.first(row_of(tb.active[item_of(warp) / tiles], 0) + begin_of(warp) * p.up_piece * P::kStep, steps_at(begin_of(warp)));
+  for (int u = warp; u < units; u += kMoeWarps) {
+    const int item = item_of(u), at = item / tiles, f0 = (item - at * tiles) * 8;
+    const Active a = tb.active[at];
+    const int nt = (a.count + 7) / 8;
+    const int64_t row = min(f0 + g, p.inner - 1);
+    piece.rows(p.gate, a.expert * p.gate.expert_rows + row, p.up, a.expert * p.up.expert_rows + row);
+    const uint16_t* xrow[NT];
 #pragma unroll
-      for (int q = 0; q < 2; ++q)
-        if (n + q < a.count) {
-          const float w = __ldcg(p.entry_weight + a.base + n + q);
-          p.h[(int64_t)(a.base + n + q) * p.ldh + col] = T::from_float(w * (gate[q] / (1.f + expf(-gate[q])) * up[q]));
-        }
+    for (int i = 0; i < NT; ++i) xrow[i] = row_of(a, i);
+    float acc[NT][4];
+    clear(acc);
+    const int end = end_of(u);
+    for (int c = begin_of(u); c < end; ++c) {
+      const int s = c * p.up_piece, n = steps_at(c);
+      const uint16_t* next = xrow[0] + (s + p.up_piece) * P::kStep;
+      int n_next = c + 1 < end ? steps_at(c + 1) : 0;
+      if (c + 1 == end && u + kMoeWarps < units) {
+        const int v = u + kMoeWarps;
+        next = row_of(tb.active[item_of(v) / tiles], 0) + begin_of(v) * p.up_piece * P::kStep;
+        n_next = steps_at(begin_of(v));
+      }
+      const uint32_t w = ring.wait() + g * ring.pitch + 16 * t;
+      piece.template multiply<NT>(w, ring.pitch, s, n, [&](int i) { return xrow[i] + s * P::kStep; }, next, n_next, nt, acc);
+      __syncwarp();
+      ring.taken();
+      issue();
+    }
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+      if (i < nt) {
+        const float4 v = make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
+        if (nk_log == 0) store_inner<T>(p, a, f0, i, lane, v);
+        else sums[(u * NT + i) * 32 + lane] = v;
+      }
+    }
+  }
+  if (nk_log > 0) {
+    __syncthreads();
+    for (int idx = threadIdx.x; idx < mine * NT * 32; idx += kMoeThreads) {
+      const int k = idx / (NT * 32), i = (idx >> 5) % NT;
+      const int item = (int)blockIdx.x + k * (int)gridDim.x, at = item / tiles;
+      const Active a = tb.active[at];
+      if (8 * i >= a.count) continue;
+      float4 v = sums[((k << nk_log) * NT + i) * 32 + (idx & 31)];
+      for (int q = 1; q < nk; ++q) add(v, sums[(((k << nk_log) + q) * NT + i) * 32 + (idx & 31)]);
+      store_inner<T>(p, a, (item - at * tiles) * 8, i, idx & 31, v);
     }
   }
 }
@@ -306,83 +532,135 @@ __global__ void __launch_bounds__(kUpThreads) exo_moe_up_kernel(const MoeParams 
 // A cluster computes 16 rows of y for all tokens.  Its warps share the steps of all taken experts, one after another,
 // in equal ranges; a warp adds what an expert gives onto its own sums in shared memory, by token.  The sums meet
 // in warp order and then in rank order.
-constexpr int kDownThreads = 256, kDownWarps = 8;
-
 template <class T, int FMT, int NT>
-__global__ void __launch_bounds__(kDownThreads) exo_moe_down_kernel(const MoeParams p) {
+__global__ void __launch_bounds__(kMoeThreads, 2)
+exo_moe_down_ring_kernel(const MoeParams p, const __grid_constant__ CUtensorMap map) {
   namespace cg = cooperative_groups;
+  using P = typename PieceOf<T, FMT>::type;
   extern __shared__ __align__(128) uint8_t smem[];
-  float* sums = reinterpret_cast<float*>(smem);               // [warp][token][row]
-  float* part = sums + kDownWarps * p.tokens * 16;            // [token][row]
+  __shared__ Tables tb;
+  __shared__ __align__(8) uint8_t bars[kMoeWarps * kMoeStages * 8];
   cg::cluster_group cluster = cg::this_cluster();
   const int S = (int)cluster.num_blocks(), r = (int)cluster.block_rank();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
   const int row0 = (int)(blockIdx.x / S) * 16;
-  using F = typename FormatOf<T, FMT>::type;
-  const int steps = (p.inner + F::kStep - 1) / F::kStep;
+  Ring ring;
+  ring.begin(bars, smem, p.down_piece, warp, lane);
+  float* sums = reinterpret_cast<float*>(smem + kMoeWarps * kMoeStages * ring.stage_bytes);   // [warp][token][row]
+  float* part = sums + kMoeWarps * p.tokens * 16;             // [token][row]
+  const int steps = (p.inner + P::kStep - 1) / P::kStep;
   // `route` is complete: `up` started this kernel after it had waited for that
-  const int64_t total = (int64_t)__ldcg(p.n_active) * steps;
-  const int64_t workers = (int64_t)S * kDownWarps, q = r * kDownWarps + warp;
-  int64_t pos = total * q / workers;
-  const int64_t end = total * (q + 1) / workers;
-  for (int i = threadIdx.x; i < kDownWarps * p.tokens * 16; i += kDownThreads) sums[i] = 0.f;
+  const int n_active = __ldcg(p.n_active);
+  copy_tables(tb, p);
+  for (int i = threadIdx.x; i < kMoeWarps * p.tokens * 16; i += kMoeThreads) sums[i] = 0.f;
   __syncthreads();
+  // A step costs a warp its weights and then its tiles of tokens: three parts and two for every tile.  Equal shares of that.
+  auto cost_of = [&](int at) { return 3 + 2 * ((tb.active[at].count + 7) / 8); };
+  if (warp == 0) {
+    int before = 0;
+    for (int e0 = 0; e0 < n_active; e0 += 32) {
+      int sum = e0 + lane < n_active ? cost_of(e0 + lane) : 0;
+      const int own = sum;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, sum, o);
+        if (lane >= o) sum += v;
+      }
+      if (e0 + lane < n_active) tb.active[e0 + lane].cost_before = before + sum - own;
+      before += __shfl_sync(0xffffffffu, sum, 31);
+    }
+    if (lane == 0) tb.cost = before;
+  }
+  __syncthreads();
+  const int64_t total = (int64_t)tb.cost * steps;
+  const int64_t workers = (int64_t)S * kMoeWarps, q = r * kMoeWarps + warp;
+  auto place = [&](int64_t cost, int& at, int& s) {   // the step that begins at or after this point
+    int lo = 0, hi = n_active;                        // the last expert that begins at or before it
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) / 2;
+      if ((int64_t)tb.active[mid].cost_before * steps <= cost) lo = mid; else hi = mid;
+    }
+    const int c = cost_of(lo);
+    at = lo;
+    s = (int)((cost - (int64_t)tb.active[lo].cost_before * steps + c - 1) / c);
+    if (s >= steps) { s = 0; ++at; }
+  };
+  int at, s, end_at, end_s;
+  place(total * q / workers, at, s);
+  place(total * (q + 1) / workers, end_at, end_s);
   float* mine = sums + warp * p.tokens * 16;
-  constexpr int DEPTH = NT <= 2 ? 4 : 2;
-  Stream<F, DEPTH> stream;
-  bool waited = false;
-  while (pos < end) {
-    const int at = (int)(pos / steps), s0 = (int)(pos - (int64_t)at * steps);
-    const int s1 = (int)min((int64_t)steps, s0 + (end - pos));
-    const int4 raw = __ldcg(reinterpret_cast<const int4*>(p.active + at));
-    const Active a{raw.x, raw.y, raw.z, raw.w};
-    const int nt = (a.count + 7) / 8;
+  // steps of expert e that are this warp's end here
+  auto stop_of = [&](int e) { return e < end_at ? steps : end_s; };
+  auto any = [&](int e, int from) { return e < end_at || (e == end_at && from < end_s); };
+  int iat = at, is = s;                               // the next copy
+  auto issue = [&]() {
+    if (any(iat, is)) {
+      if (lane == 0) ring.copy(&map, (int)(tb.active[iat].expert * p.down.expert_rows) + row0, nullptr, 0, is * P::kWords);
+      ring.copied();
+      is = min(is + p.down_piece, stop_of(iat));
+      if (is == steps) { is = 0; ++iat; }
+    }
+  };
+  for (int i = 0; i < kMoeStages; ++i) issue();
+  ptx::grid_dependency_wait();     // `up` is complete
+  ptx::grid_launch_dependents();
+  // rows behind an expert's are other entries', or spare ones
+  auto row_at = [&](int e, int from) { return p.h + (int64_t)(tb.active[e].base + g) * p.ldh + 8 * t + from * P::kStep; };
+  P piece;
+  if (any(at, s)) piece.first(row_at(at, s), min(p.down_piece, stop_of(at) - s));
+  while (any(at, s)) {
+    const Active a = tb.active[at];
+    const int nt = (a.count + 7) / 8, stop = stop_of(at);
     const int64_t first = a.expert * p.down.expert_rows;
-    const F f = rows_of<T, FMT>(p.down, first + min(row0 + g, p.hidden - 1), p.down, first + min(row0 + g + 8, p.hidden - 1));
-    stream.preload(f, s0, 1, s1, p.inner, t);
-    int token[NT][2];
-#pragma unroll
-    for (int i = 0; i < NT; ++i)
-#pragma unroll
-      for (int c = 0; c < 2; ++c)
-        token[i][c] = 8 * i + 2 * t + c < a.count ? __ldcg(p.entry_token + a.base + 8 * i + 2 * t + c) : -1;
-    if (!waited) { ptx::grid_dependency_wait(); waited = true; }   // `up` is complete
-    const uint16_t* hrow = p.h + (int64_t)(a.base + g) * p.ldh;
+    piece.rows(p.down, first + min(row0 + g, p.hidden - 1), p.down, first + min(row0 + g + 8, p.hidden - 1));
     float acc[NT][4];
     clear(acc);
-    stream.template walk<NT>(f, s0, 1, s1, p.inner, t, [&](int i, int k) {
-      if (8 * i + g >= a.count) return make_uint4(0, 0, 0, 0);
-      const uint16_t* hk = hrow + (int64_t)8 * i * p.ldh;
-      return k + 8 <= p.inner ? __ldcg(reinterpret_cast<const uint4*>(hk + k)) : load8_checked(hk, k, p.inner, false);
-    }, nt, acc);
+    while (s < stop) {
+      const int n = min(p.down_piece, stop - s), after = s + n;
+      const uint16_t* here = row_at(at, s);
+      const bool more = after < stop;
+      const int ne = more ? at : at + 1, nf = more ? after : 0;
+      const int n_next = any(ne, nf) ? min(p.down_piece, stop_of(ne) - nf) : 0;
+      const uint16_t* next = n_next ? row_at(ne, nf) : here;
+      const uint32_t w = ring.wait() + g * ring.pitch + 16 * t;
+      piece.template multiply<NT>(w, ring.pitch, s, n, [&](int i) { return here + (int64_t)8 * i * p.ldh; }, next, n_next, nt, acc);
+      __syncwarp();
+      ring.taken();
+      issue();
+      s = after;
+    }
 #pragma unroll
     for (int i = 0; i < NT; ++i)
+      if (i < nt) {
 #pragma unroll
-      for (int c = 0; c < 2; ++c)
-        if (token[i][c] >= 0) {
-          mine[token[i][c] * 16 + g] += acc[i][c];
-          mine[token[i][c] * 16 + g + 8] += acc[i][2 + c];
+        for (int c = 0; c < 2; ++c) {
+          const int n = 8 * i + 2 * t + c;
+          if (n < a.count) {
+            float* to = mine + tb.token[a.base + n] * 16 + g;
+            to[0] += acc[i][c];
+            to[8] += acc[i][2 + c];
+          }
         }
+      }
     __syncwarp();
-    pos += s1 - s0;
+    s = 0;
+    ++at;
   }
-  if (!waited) ptx::grid_dependency_wait();
-  ptx::grid_launch_dependents();
   __syncthreads();
   auto finish = [&](int idx, float v) {
     const int row = row0 + (idx & 15);
     if (row < p.hidden) p.y[(int64_t)(idx >> 4) * p.ldy + row] = T::from_float(v);
   };
-  for (int idx = threadIdx.x; idx < p.tokens * 16; idx += kDownThreads) {
+  for (int idx = threadIdx.x; idx < p.tokens * 16; idx += kMoeThreads) {
     float v = 0.f;
 #pragma unroll
-    for (int w = 0; w < kDownWarps; ++w) v += sums[w * p.tokens * 16 + idx];
+    for (int w = 0; w < kMoeWarps; ++w) v += sums[w * p.tokens * 16 + idx];
     if (S == 1) finish(idx, v);
     else part[idx] = v;
   }
   if (S > 1) {
     cluster.sync();
-    for (int idx = r * kDownThreads + threadIdx.x; idx < p.tokens * 16; idx += S * kDownThreads) {
+    for (int idx = r * kMoeThreads + threadIdx.x; idx < p.tokens * 16; idx += S * kMoeThreads) {
       float v = 0.f;
       for (int o = 0; o < S; ++o) v += cluster.map_shared_rank(part, o)[idx];
       finish(idx, v);
@@ -391,15 +669,124 @@ __global__ void __launch_bounds__(kDownThreads) exo_moe_down_kernel(const MoePar
   }
 }
 
+// ==== 16-bit rows that a tiled copy cannot address ==================================================================
+// Rows that do not start on 16-byte boundaries are read element by element, straight into the fragments: right at any
+// leading dimension, and slow.
+constexpr int kPlainThreads = 256, kPlainWarps = 8;
+
+template <class T, int NT>
+__device__ __forceinline__ void plain_steps(Rows16<T, false> f, const uint16_t* x0, int64_t stride, const uint16_t* const (&rows)[NT], int s, int ds, int end,
+                                            int K, int t, int nt, float (&acc)[NT][4]) {
+  f.begin(t);
+  const uint16_t *r0 = f.r0, *r1 = f.r1;
+  for (; s < end; s += ds) {
+    f.r0 = r0 + s * 32;
+    f.r1 = r1 + s * 32;
+    const typename Rows16<T, false>::Regs w = (s + 1) * 32 <= K ? f.load(0) : f.load_tail(K - s * 32, t);
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+      if (i < nt) {
+        const uint4 b = *reinterpret_cast<const uint4*>((x0 ? x0 + i * stride : rows[i]) + s * 32);
+        T::mma(acc[i], w.a.x, w.b.x, w.a.y, w.b.y, b.x, b.y);
+        T::mma(acc[i], w.a.z, w.b.z, w.a.w, w.b.w, b.z, b.w);
+      }
+  }
+}
+
+template <class T, int NT>
+__global__ void __launch_bounds__(kPlainThreads) exo_moe_up_plain_kernel(const MoeParams p) {
+  __shared__ float4 red[kPlainWarps * NT * 32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+  ptx::grid_dependency_wait();
+  ptx::grid_launch_dependents();   // after the wait: `down` may then read the tables of `route` before it waits itself
+  if ((int)blockIdx.y >= __ldcg(p.n_active)) return;
+  const int4 raw = __ldcg(reinterpret_cast<const int4*>(p.active + blockIdx.y));
+  const Active a{raw.x, raw.y, raw.z, raw.w};
+  const int f0 = blockIdx.x * 8, nt = (a.count + 7) / 8;
+  const int64_t row = min(f0 + g, p.inner - 1);
+  Rows16<T, false> f;
+  f.r0 = static_cast<const uint16_t*>(p.gate.w) + (a.expert * p.gate.expert_rows + row) * p.gate.ld;
+  f.r1 = static_cast<const uint16_t*>(p.up.w) + (a.expert * p.up.expert_rows + row) * p.up.ld;
+  const uint16_t* xrow[NT];
+#pragma unroll
+  for (int i = 0; i < NT; ++i)
+    xrow[i] = p.xs + (int64_t)__ldcg(p.entry_token + a.base + min(8 * i + g, a.count - 1)) * p.ldxs + 8 * t;
+  float acc[NT][4];
+  clear(acc);
+  plain_steps<T, NT>(f, nullptr, 0, xrow, warp, kPlainWarps, (p.hidden + 31) / 32, p.hidden, t, nt, acc);
+#pragma unroll
+  for (int i = 0; i < NT; ++i)
+    if (i < nt) red[(warp * nt + i) * 32 + lane] = make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
+  __syncthreads();
+  for (int idx = threadIdx.x; idx < nt * 32; idx += kPlainThreads) {
+    float4 v = red[idx];
+    for (int q = 1; q < kPlainWarps; ++q) add(v, red[q * nt * 32 + idx]);
+    store_inner<T>(p, a, f0, idx >> 5, idx & 31, v);
+  }
+}
+
+template <class T, int NT>
+__global__ void __launch_bounds__(kPlainThreads) exo_moe_down_plain_kernel(const MoeParams p) {
+  extern __shared__ __align__(128) uint8_t smem[];
+  float* sums = reinterpret_cast<float*>(smem);               // [warp][token][row]
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+  const int row0 = (int)blockIdx.x * 16, steps = (p.inner + 31) / 32;
+  for (int i = threadIdx.x; i < kPlainWarps * p.tokens * 16; i += kPlainThreads) sums[i] = 0.f;
+  __syncthreads();
+  float* mine = sums + warp * p.tokens * 16;
+  ptx::grid_dependency_wait();
+  ptx::grid_launch_dependents();
+  const int n_active = __ldcg(p.n_active);
+  for (int at = 0; at < n_active; ++at) {
+    const int4 raw = __ldcg(reinterpret_cast<const int4*>(p.active + at));
+    const Active a{raw.x, raw.y, raw.z, raw.w};
+    const int nt = (a.count + 7) / 8;
+    const int64_t first = a.expert * p.down.expert_rows;
+    Rows16<T, false> f;
+    f.r0 = static_cast<const uint16_t*>(p.down.w) + (first + min(row0 + g, p.hidden - 1)) * p.down.ld;
+    f.r1 = static_cast<const uint16_t*>(p.down.w) + (first + min(row0 + g + 8, p.hidden - 1)) * p.down.ld;
+    float acc[NT][4];
+    clear(acc);
+    const uint16_t* none[NT] = {};
+    plain_steps<T, NT>(f, p.h + (int64_t)(a.base + g) * p.ldh + 8 * t, 8 * p.ldh, none, warp, kPlainWarps, steps, p.inner, t, nt, acc);
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const int n = 8 * i + 2 * t + c;
+        if (i < nt && n < a.count) {
+          float* to = mine + __ldcg(p.entry_token + a.base + n) * 16 + g;
+          to[0] += acc[i][c];
+          to[8] += acc[i][2 + c];
+        }
+      }
+    __syncwarp();
+  }
+  __syncthreads();
+  for (int idx = threadIdx.x; idx < p.tokens * 16; idx += kPlainThreads) {
+    float v = 0.f;
+#pragma unroll
+    for (int w = 0; w < kPlainWarps; ++w) v += sums[w * p.tokens * 16 + idx];
+    const int row = row0 + (idx & 15);
+    if (row < p.hidden) p.y[(int64_t)(idx >> 4) * p.ldy + row] = T::from_float(v);
+  }
+}
+
 // ---- kernels by type, format and token count --------------------------------------------------------------------
 template <class T, bool VEC> void* pick_route(int nt) {
   return nt == 1 ? (void*)exo_moe_route_kernel<T, VEC, 1> : nt == 2 ? (void*)exo_moe_route_kernel<T, VEC, 2> : (void*)exo_moe_route_kernel<T, VEC, 8>;
 }
 template <class T, int FMT> void* pick_up_nt(int nt) {
-  return nt == 1 ? (void*)exo_moe_up_kernel<T, FMT, 1> : nt == 2 ? (void*)exo_moe_up_kernel<T, FMT, 2> : (void*)exo_moe_up_kernel<T, FMT, 8>;
+  if constexpr (FMT == 0)
+    return nt == 1 ? (void*)exo_moe_up_plain_kernel<T, 1> : nt == 2 ? (void*)exo_moe_up_plain_kernel<T, 2> : (void*)exo_moe_up_plain_kernel<T, 8>;
+  else
+    return nt == 1 ? (void*)exo_moe_up_ring_kernel<T, FMT, 1> : nt == 2 ? (void*)exo_moe_up_ring_kernel<T, FMT, 2> : (void*)exo_moe_up_ring_kernel<T, FMT, 8>;
 }
 template <class T, int FMT> void* pick_down_nt(int nt) {
-  return nt == 1 ? (void*)exo_moe_down_kernel<T, FMT, 1> : nt == 2 ? (void*)exo_moe_down_kernel<T, FMT, 2> : (void*)exo_moe_down_kernel<T, FMT, 8>;
+  if constexpr (FMT == 0)
+    return nt == 1 ? (void*)exo_moe_down_plain_kernel<T, 1> : nt == 2 ? (void*)exo_moe_down_plain_kernel<T, 2> : (void*)exo_moe_down_plain_kernel<T, 8>;
+  else
+    return nt == 1 ? (void*)exo_moe_down_ring_kernel<T, FMT, 1> : nt == 2 ? (void*)exo_moe_down_ring_kernel<T, FMT, 2> : (void*)exo_moe_down_ring_kernel<T, FMT, 8>;
 }
 template <class T> void* pick_up(int fmt, int nt) {
   switch (fmt) {
@@ -420,11 +807,18 @@ template <class T> void* pick_down(int fmt, int nt) {
   }
 }
 
+// Tensor map of a stack for pieces of `steps` steps of `box_rows` rows.
+bool stack_map(CUtensorMap* map, const Stack& m, int64_t all, bool q4, int steps, int box_rows) {
+  const uint64_t rows = (uint64_t)((all - 1) * m.expert_rows + m.rows), blocks = (uint64_t)(m.K + 127) / 128;
+  return q4 ? exo::encode_rows_map(map, 4, m.w, blocks * 16, rows, blocks * 64, (uint32_t)steps * 16, (uint32_t)box_rows)
+            : exo::encode_rows_map(map, 2, m.w, (uint64_t)m.K, rows, (uint64_t)m.ld * 2, (uint32_t)steps * 32, (uint32_t)box_rows);
+}
+
 bool rows_aligned(const void* w, int64_t ld) { return ((uintptr_t)w & 15u) == 0 && ld % 8 == 0; }
 
 exo_gemm_status_t check_stack(const exo_moe_matrix_t& m, int64_t rows, int64_t K, int q4_group) {
   if (!m.w) return EXO_GEMM_ERR_NULL;
-  if (m.expert_rows < rows || m.expert_rows > (1LL << 32)) return EXO_GEMM_ERR_INVALID_ARG;
+  if (m.expert_rows < rows || m.expert_rows > (1LL << 26)) return EXO_GEMM_ERR_INVALID_ARG;
   if (q4_group) {
     if (!m.scales) return EXO_GEMM_ERR_NULL;
     if (!q4_aligned(m.w, m.scales, m.zeros, q4_group)) return EXO_GEMM_ERR_ALIGNMENT;
@@ -459,14 +853,20 @@ struct DeviceGuard {
 }  // namespace decode
 }  // namespace exo
 
+namespace exo {
+namespace decode {
+unsigned take_gave_up_moe(cudaError_t* e) { return take_gave_up(e); }
+}  // namespace decode
+}  // namespace exo
+
 using namespace exo::decode;
 
 struct exo_moe_plan {
   exo_moe_desc_t desc;
   int device, sms;
-  int64_t ldh, bytes;
+  int64_t ldh, ldxs, bytes;
   uint8_t* ws;
-  int64_t at_active, at_token, at_weight, at_logits, at_h;   // offsets into ws; the arrival counter and n_active come first
+  int64_t at_active, at_token, at_weight, at_logits, at_xs, at_h;   // offsets into ws; the arrival counter and n_active come first
 };
 
 extern "C" {
@@ -503,11 +903,13 @@ exo_gemm_status_t exo_moe_create(exo_moe_handle_t* out, const exo_moe_desc_t* d)
   plan->at_token = take(entries * 4);
   plan->at_weight = take(entries * 4);
   plan->at_logits = take((int64_t)d->max_tokens * d->experts * 4);
-  plan->at_h = take(entries * plan->ldh * 2);
+  plan->ldxs = (d->hidden + 127) / 128 * 128;
+  plan->at_xs = take((int64_t)d->max_tokens * plan->ldxs * 2);
+  plan->at_h = take((entries + 8) * plan->ldh * 2);   // a last tile of eight tokens may read rows behind the last entry
   plan->bytes = at;
   cudaError_t e = cudaMalloc((void**)&plan->ws, (size_t)plan->bytes);
   if (e == cudaSuccess) {
-    e = cudaMemset(plan->ws, 0, 256);
+    e = cudaMemset(plan->ws, 0, (size_t)plan->bytes);   // the counter, and the padding of the inner activations
     if (e != cudaSuccess) cudaFree(plan->ws);
   }
   if (e != cudaSuccess) {
@@ -553,6 +955,16 @@ exo_gemm_status_t exo_moe_run(exo_moe_handle_t plan, const exo_moe_weights_t* w,
   p.logits = (float*)(plan->ws + plan->at_logits);
   p.h = (uint16_t*)(plan->ws + plan->at_h);
 
+  p.copy_x = !(p.x_aligned && d.hidden % 128 == 0);
+  p.xs = p.copy_x ? (const uint16_t*)(plan->ws + plan->at_xs) : p.x;
+  p.ldxs = p.copy_x ? plan->ldxs : ldx;
+  // Pieces: larger ones suit the copies, smaller ones leave room for a second CTA on the SM, which covers the first one's
+  // start and end (5 steps: 80 KB of ring).  Measured at 64 + 1 experts of 4096 x 1536 and 64 tokens: up with one CTA per SM and
+  // 7 steps; at up to 16 tokens two CTAs and 5 steps are ahead.
+  const bool many = p.tokens > 16;
+  p.up_piece = many ? 7 : 5;
+  p.down_piece = 5;
+
   const bool bf16 = d.dtype == EXO_GEMM_BF16;
   const int nt = (p.tokens + 7) / 8;
   const cudaStream_t stream = (cudaStream_t)cuda_stream;
@@ -567,21 +979,40 @@ exo_gemm_status_t exo_moe_run(exo_moe_handle_t plan, const exo_moe_weights_t* w,
   st = launch(fn, (unsigned)((p.experts + 15) / 16 * S), 1, kRouteThreads, (size_t)(kRouteWarps + 1) * nt * 512, (unsigned)S, stream, &p);
   if (st != EXO_GEMM_OK) return st;
 
-  const int q4_fmt = d.q4_group == 128 ? 2 : d.q4_group == 64 ? 3 : 4;
+  const int q4_fmt = d.q4_group == 128 ? 2 : d.q4_group == 64 ? 3 : 4, step = q4 ? 128 : 32, nt_kernel = nt <= 2 ? nt : 8;
+  const int64_t all = d.experts + d.shared;
   const int64_t most = (int64_t)p.tokens * p.top_k < p.experts ? (int64_t)p.tokens * p.top_k : p.experts;
   const int taken = (int)most + p.shared;   // the most experts this run can take
   const int up_fmt = q4 ? q4_fmt : rows_aligned(w->gate.w, w->gate.ld) && rows_aligned(w->up.w, w->up.ld) ? 1 : 0;
-  st = launch(bf16 ? pick_up<Bf16>(up_fmt, nt) : pick_up<Fp16>(up_fmt, nt), (unsigned)((p.inner + 7) / 8), (unsigned)taken, kUpThreads,
-              0, 1, stream, &p);
+  fn = bf16 ? pick_up<Bf16>(up_fmt, nt) : pick_up<Fp16>(up_fmt, nt);
+  if (up_fmt == 0) {
+    st = launch(fn, (unsigned)((p.inner + 7) / 8), (unsigned)taken, kPlainThreads, 0, 1, stream, &p);
+  } else {
+    CUtensorMap gate, up;
+    if (!stack_map(&gate, p.gate, all, q4, p.up_piece, 8) || !stack_map(&up, p.up, all, q4, p.up_piece, 8)) return EXO_GEMM_ERR_CUDA;
+    const size_t smem = (size_t)kMoeWarps * kMoeStages * p.up_piece * 1024 + (size_t)2 * part_limit(nt_kernel) * nt_kernel * 512;
+    const int64_t items = (int64_t)taken * ((p.inner + 7) / 8), slots = (int64_t)(many ? 1 : 2) * plan->sms;
+    st = launch(fn, (unsigned)(items < slots ? items : slots), 1, kMoeThreads, smem, 1, stream, &p, &gate, &up);
+  }
   if (st != EXO_GEMM_OK) return st;
 
-  // down: cut until the grid fills the device four times, as long as a warp keeps two steps
   const int down_fmt = q4 ? q4_fmt : rows_aligned(w->down.w, w->down.ld) ? 1 : 0;
-  const int64_t tiles = (p.hidden + 15) / 16, all_steps = (int64_t)taken * ((p.inner + (q4 ? 127 : 31)) / (q4 ? 128 : 32));
+  const int64_t tiles = (p.hidden + 15) / 16, all_steps = (int64_t)taken * ((p.inner + step - 1) / step);
+  fn = bf16 ? pick_down<Bf16>(down_fmt, nt) : pick_down<Fp16>(down_fmt, nt);
+  if (down_fmt == 0)
+    return launch(fn, (unsigned)tiles, 1, kPlainThreads, (size_t)kPlainWarps * p.tokens * 64, 1, stream, &p);
+  CUtensorMap down;
+  if (!stack_map(&down, p.down, all, q4, p.down_piece, 16)) return EXO_GEMM_ERR_CUDA;
+  // The cluster size with the shortest estimate: every turn of two CTAs per SM costs about 3 us and its weights at an SM's
+  // share of the bandwidth, 22 GB/s for each of the two.
   S = 1;
-  while (S < 8 && tiles * S < 4 * plan->sms && all_steps >= 4 * S * kDownWarps) S *= 2;
-  return launch(bf16 ? pick_down<Bf16>(down_fmt, nt) : pick_down<Fp16>(down_fmt, nt), (unsigned)(tiles * S), 1, kDownThreads,
-                (size_t)(kDownWarps + 1) * p.tokens * 64, (unsigned)S, stream, &p);
+  double best = 0.0;
+  for (int c = 1; c <= 8 && (c == 1 || all_steps >= (int64_t)c * kMoeWarps); c *= 2) {
+    const double us = (double)((tiles * c + 2 * plan->sms - 1) / (2 * plan->sms)) * (3.0 + (double)all_steps * 1024.0 / c / 22e3);
+    if (c == 1 || us < best) { best = us; S = c; }
+  }
+  return launch(fn, (unsigned)(tiles * S), 1, kMoeThreads,
+                (size_t)kMoeWarps * kMoeStages * p.down_piece * 1024 + (size_t)(kMoeWarps + 1) * p.tokens * 64, (unsigned)S, stream, &p, &down);
 }
 
 int64_t exo_moe_workspace_bytes(exo_moe_handle_t plan) { return plan ? plan->bytes : 0; }

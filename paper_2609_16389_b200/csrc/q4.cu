@@ -146,7 +146,7 @@ __global__ void __launch_bounds__(kQuantThreads) exo_q4_dequantize_kernel(const 
 }
 
 // ==== the product of a few tokens with a 4-bit matrix =============================================================
-// A CTA's eight warps are `wr` groups of 16 weight rows times 8 / wr parts of its steps of k; the CTAs of a cluster
+// A CTA's eight warps are 8 / NK groups of 16 weight rows times NK parts of its steps of k; the CTAs of a cluster
 // share the rows and split k.  The tokens' values for the CTA's part of k are staged in shared memory (rows 64 bytes off
 // a multiple of 128, so that a fragment load is free of bank conflicts).  Partial sums meet in shared memory in warp
 // order, then in distributed shared memory in rank order.
@@ -160,7 +160,6 @@ struct GemvParams {
   void* y;
   int64_t ldx, ldy, rows;
   int K, tokens, blocks;        // blocks: steps of 128
-  int wr;                       // warps across rows: 1, 2, 4 or 8
   int chunk;                    // steps staged at a time
   int y_dtype;
   bool x_aligned;
@@ -183,27 +182,21 @@ __device__ __forceinline__ void store_y(const GemvParams& p, int token, int64_t 
   }
 }
 
-template <class T, int PER, int NT>
-__global__ void __launch_bounds__(kGemvThreads) exo_gemv_q4_kernel(const GemvParams p) {
+template <class T, int PER, bool ZEROS, int NT, int NK>
+__global__ void __launch_bounds__(kGemvThreads, NT <= 4 ? 2 : 1) exo_gemv_q4_kernel(const GemvParams p) {
   namespace cg = cooperative_groups;
   extern __shared__ __align__(128) uint8_t smem[];
   cg::cluster_group cluster = cg::this_cluster();
   const int S = (int)cluster.num_blocks(), r = (int)cluster.block_rank();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-  const int wr = warp % p.wr, wk = warp / p.wr, nk = kGemvWarps / p.wr;
-  const int64_t tile_row = (int64_t)(blockIdx.x / S) * 16 * p.wr;
+  constexpr int WR = kGemvWarps / NK;   // warps across rows
+  const int wr = warp % WR, wk = warp / WR;
+  const int64_t tile_row = (int64_t)(blockIdx.x / S) * 16 * WR;
   const int64_t row0 = min(tile_row + 16 * wr + g, p.rows - 1), row1 = min(tile_row + 16 * wr + g + 8, p.rows - 1);
   const int s_begin = (int)((int64_t)p.blocks * r / S), s_end = (int)((int64_t)p.blocks * (r + 1) / S);
-  const int nt = (p.tokens + 7) / 8;
-
-  RowsQ4<T, PER> f;
-  f.c0 = p.codes + row0 * p.blocks * 64;
-  f.c1 = p.codes + row1 * p.blocks * 64;
-  f.s0 = p.scales + row0 * p.blocks * PER;
-  f.s1 = p.scales + row1 * p.blocks * PER;
-  f.z0 = p.zeros ? p.zeros + row0 * p.blocks * PER : nullptr;
-  f.z1 = p.zeros ? p.zeros + row1 * p.blocks * PER : nullptr;
-
+  const int whole = p.K / 128;          // whole steps; a part of one may follow
+  constexpr int nt = NT;
+  using F = RowsQ4<T, PER, ZEROS>;
   float acc[NT][4];
 #pragma unroll
   for (int i = 0; i < NT; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
@@ -211,11 +204,22 @@ __global__ void __launch_bounds__(kGemvThreads) exo_gemv_q4_kernel(const GemvPar
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();
   const int pitch = gemv_pitch(p.chunk);
-  constexpr int DEPTH = NT <= 2 ? 4 : 2;
-  Stream<RowsQ4<T, PER>, DEPTH> stream;
+  constexpr int DEPTH = NT == 1 ? 4 : 2;
   for (int c = s_begin; c < s_end; c += p.chunk) {
-    const int c_end = min(c + p.chunk, s_end);
-    stream.preload(f, c + wk, nk, c_end, p.K, t);
+    const int c_end = min(c + p.chunk, s_end), s = c + wk;
+    F f;
+    f.c0 = p.codes + (row0 * p.blocks + s) * 64;
+    f.c1 = p.codes + (row1 * p.blocks + s) * 64;
+    f.s0 = p.scales + (row0 * p.blocks + s) * PER;
+    f.s1 = p.scales + (row1 * p.blocks + s) * PER;
+    if constexpr (ZEROS) {
+      f.z0 = p.zeros + (row0 * p.blocks + s) * PER;
+      f.z1 = p.zeros + (row1 * p.blocks + s) * PER;
+    }
+    f.begin(t);
+    const int n = steps_of(s, NK, min(c_end, whole));
+    Stream<F, NK, DEPTH> stream;
+    stream.preload(f, n);
     if (c != s_begin) __syncthreads();   // the previous chunk has been read
     const int per_token = (c_end - c) * 16;
     for (int i = threadIdx.x; i < p.tokens * per_token; i += kGemvThreads) {
@@ -224,10 +228,10 @@ __global__ void __launch_bounds__(kGemvThreads) exo_gemv_q4_kernel(const GemvPar
           load8_checked(p.x + (int64_t)token * p.ldx, c * 128 + e * 8, p.K, p.x_aligned);
     }
     __syncthreads();
-    const uint8_t* mine = smem + g * pitch - c * 256;
-    stream.template walk<NT>(f, c + wk, nk, c_end, p.K, t, [&](int i, int k) {
-      return 8 * i + g < p.tokens ? *reinterpret_cast<const uint4*>(mine + 8 * i * pitch + 2 * k) : make_uint4(0, 0, 0, 0);
-    }, nt, acc);
+    // columns beyond the tokens read the last row again (up to 8 tokens) or rows that nobody wrote
+    XShared x{ptx::smem_u32(smem) + (NT == 1 ? min(g, p.tokens - 1) : g) * pitch + wk * 256 + 16 * t, 8u * pitch};
+    stream.template walk<NT>(f, n, x, All<NT>(), acc);
+    if (s + n * NK == whole && whole < c_end) f.template step_tail<NT>(f.load_tail(0, t), p.K - whole * 128, x, All<NT>(), acc);
   }
 
   // sums over the warps that share rows, then over the cluster
@@ -238,7 +242,7 @@ __global__ void __launch_bounds__(kGemvThreads) exo_gemv_q4_kernel(const GemvPar
   for (int i = 0; i < NT; ++i)
     if (i < nt) red[(warp * nt + i) * 32 + lane] = make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
   __syncthreads();
-  const int items = p.wr * nt * 32;
+  const int items = WR * nt * 32;
   auto finish = [&](int idx, float4 v) {
     const int l = idx & 31, i = (idx >> 5) % nt, w = (idx >> 5) / nt;
     const int64_t row = tile_row + 16 * w + (l >> 2);
@@ -250,7 +254,7 @@ __global__ void __launch_bounds__(kGemvThreads) exo_gemv_q4_kernel(const GemvPar
   };
   for (int idx = threadIdx.x; idx < items; idx += kGemvThreads) {
     float4 v = red[idx];
-    for (int q = 1; q < nk; ++q) {
+    for (int q = 1; q < NK; ++q) {
       const float4 w = red[q * items + idx];
       v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
     }
@@ -271,6 +275,310 @@ __global__ void __launch_bounds__(kGemvThreads) exo_gemv_q4_kernel(const GemvPar
   }
 }
 
+// ==== few tokens: integer products ==================================================================================
+// Turning 4-bit codes into 16-bit numbers costs the general kernel 11 instructions for eight weights, and at one token
+// that, not memory, is what it is bound by (181 clocks a step of 16 x 128 weights, where memory delivers one every 178).
+// Integers need three: the codes of a word, masked, are the bytes that mma.m16n8k32 takes as unsigned operands.  The
+// activations become signed bytes: per token and step of 128 they are scaled by a power of two to integers of 30
+// bits (exact for what is down to 2^-22 of the step's largest in bf16, 2^-19 in fp16; a smaller value is off by at most
+// 2^-30 of the largest), whose four balanced digits are four columns of the product.  The columns of few tokens are idle
+// otherwise.  A group's sum of (code - zero) * digit is an exact integer; it comes out as the float 1.5 * 2^23 + sum, since
+// the accumulator starts with that float's bits less zero * (sum of digits).  From there on everything is fp32.
+//
+// Weights come through shared memory: each warp keeps a ring of pieces (`piece` steps of 16 rows) filled with tiled copies
+// that it issues itself.  A lane's parts of a step are 16 bytes of rows g and g + 8.
+constexpr int kFewWarps = 8, kFewThreads = 32 * kFewWarps;
+constexpr int kMagic = 0x4b400000;        // 1.5 * 2^23
+
+struct FewParams {
+  GemvParams g;
+  int nk_log;       // parts of a tile's steps: 1 << nk_log
+  int piece, stages;
+  int digits_at, start_at, step_scale_at, ring_at;   // offsets in shared memory; the sums come first, the barriers before them
+};
+
+__device__ __forceinline__ void mma_u8s8(int (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.u8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// four words of four bytes, transposed
+__device__ __forceinline__ void transpose4(const uint32_t (&v)[4], uint32_t (&d)[4]) {
+  const uint32_t x0 = __byte_perm(v[0], v[1], 0x5140), x1 = __byte_perm(v[2], v[3], 0x5140);
+  const uint32_t y0 = __byte_perm(v[0], v[1], 0x7362), y1 = __byte_perm(v[2], v[3], 0x7362);
+  d[0] = __byte_perm(x0, x1, 0x5410); d[1] = __byte_perm(x0, x1, 0x7632);
+  d[2] = __byte_perm(y0, y1, 0x5410); d[3] = __byte_perm(y0, y1, 0x7632);
+}
+
+__device__ __forceinline__ int rank_part(int blocks, int r, int S) { return (int)((int64_t)blocks * r / S); }
+
+// What the values of a token that are not finite give a row over steps s0 .. s1 - 1; they count as 0 in the integers.
+template <class T>
+__device__ __noinline__ float not_finite_part(const GemvParams& p, int per, int token, int64_t row, int s0, int s1) {
+  float v = 0.f;
+  if (row >= p.rows) return v;
+  for (int k = s0 * 128; k < min(s1 * 128, p.K); ++k) {
+    const float x = T::to_float(p.x[(int64_t)token * p.ldx + k]);
+    if (fabsf(x) <= 3.4028235e38f) continue;
+    const int i = k & 7, n = i / 2 + 4 * (i & 1), j = k >> 5 & 3, t = k >> 3 & 3;
+    const uint32_t word = reinterpret_cast<const uint32_t*>(p.codes)[(row * p.blocks + k / 128) * 16 + 4 * t + j];
+    const int64_t group = (row * p.blocks + k / 128) * per + (k & 127) * per / 128;
+    const int zero = p.zeros ? p.zeros[group] : 8;
+    v += (float)((int)(word >> (4 * n) & 15u) - zero) * T::to_float(p.scales[group]) * x;
+  }
+  return v;
+}
+
+// NT: tiles of eight columns, two tokens each.
+template <class T, int PER, bool ZEROS, int NT>
+__global__ void __launch_bounds__(kFewThreads, 2) exo_gemv_q4_few_kernel(const FewParams fp, const __grid_constant__ CUtensorMap map) {
+  namespace cg = cooperative_groups;
+  using F = RowsQ4<T, PER, ZEROS>;
+  constexpr int COLS = 8 * NT;
+  const GemvParams& p = fp.g;
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ int strange;                  // bit t: token t has values that are not finite
+  cg::cluster_group cluster = cg::this_cluster();
+  const int S = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+  const int clusters = gridDim.x / S, cl = blockIdx.x / S;
+  const int tiles = (int)((p.rows + 15) / 16), nk = 1 << fp.nk_log;
+  const int units = ((tiles - cl + clusters - 1) / clusters) << fp.nk_log;   // of this cluster
+  const int k_begin = rank_part(p.blocks, rank, S), k_steps = rank_part(p.blocks, rank + 1, S) - k_begin;
+  const int pieces = (k_steps + fp.piece - 1) / fp.piece;
+  const int stage_bytes = fp.piece * 1024;
+  float* sums = reinterpret_cast<float*>(smem + 256);                        // [unit][token][16]
+  const int col_pitch = k_steps * 128 + 16;
+  const uint32_t bar = ptx::smem_u32(smem) + warp * 32, ring = ptx::smem_u32(smem + fp.ring_at) + warp * fp.stages * stage_bytes;
+  if (lane == 0)
+    for (int i = 0; i < fp.stages; ++i) ptx::mbar_init(bar + 8 * i, 1);
+  ptx::fence_mbar_init();
+  if (threadIdx.x == 0) strange = 0;
+  __syncwarp();
+  // unit u: tile cl + (u >> nk_log) * clusters, part u & (nk - 1) of its pieces
+  auto row_of = [&](int u) { return (cl + (u >> fp.nk_log) * clusters) * 16; };
+  auto begin_of = [&](int u) { return (pieces * (u & (nk - 1))) >> fp.nk_log; };
+  auto end_of = [&](int u) { return (pieces * ((u & (nk - 1)) + 1)) >> fp.nk_log; };
+
+  int iu = warp, ip, islot = 0;            // the next copy
+  ip = begin_of(iu);
+  auto issue = [&]() {
+    if (iu < units) {
+      if (lane == 0) {
+        ptx::mbar_arrive_expect_tx(bar + 8 * islot, stage_bytes);
+        ptx::tma_load_3d(ring + islot * stage_bytes, &map, 0, row_of(iu), k_begin + ip * fp.piece, bar + 8 * islot);
+      }
+      islot = islot + 1 == fp.stages ? 0 : islot + 1;
+      if (++ip == end_of(iu)) {
+        iu += kFewWarps;
+        ip = begin_of(iu);
+      }
+    }
+  };
+  ptx::grid_dependency_wait();
+  ptx::grid_launch_dependents();
+  for (int i = 0; i < fp.stages; ++i) issue();
+
+  // scales and zero points of up to eight steps of rows g and g + 8: lane t holds those of steps t and 4 + t
+  struct Scales { uint32_t a[2][(PER + 1) / 2], b[2][(PER + 1) / 2], za[2], zb[2]; };
+  auto load_scales = [&](Scales& sc, int u, int piece) {
+    const int row0 = row_of(u) + g, row1 = row0 + 8;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int step = 4 * h + t, s = piece * fp.piece + step;
+#pragma unroll
+      for (int i = 0; i < (PER + 1) / 2; ++i) sc.a[h][i] = sc.b[h][i] = 0;
+      sc.za[h] = sc.zb[h] = 0;
+      if (step < fp.piece && s < k_steps) {
+        const int64_t k = k_begin + s;
+        if (row0 < p.rows) {
+          F::load_scales(sc.a[h], p.scales + ((int64_t)row0 * p.blocks + k) * PER);
+          if constexpr (ZEROS) sc.za[h] = F::load_zeros(p.zeros + ((int64_t)row0 * p.blocks + k) * PER);
+        }
+        if (row1 < p.rows) {
+          F::load_scales(sc.b[h], p.scales + ((int64_t)row1 * p.blocks + k) * PER);
+          if constexpr (ZEROS) sc.zb[h] = F::load_zeros(p.zeros + ((int64_t)row1 * p.blocks + k) * PER);
+        }
+        if (PER > 1 && k == p.blocks - 1) {   // groups of padding alone: their scales may be anything
+#pragma unroll
+          for (int q = 1; q < PER; ++q)
+            if (k * 128 + q * (128 / PER) >= p.K) {
+              sc.a[h][q / 2] &= q % 2 ? 0x0000ffffu : 0xffff0000u;
+              sc.b[h][q / 2] &= q % 2 ? 0x0000ffffu : 0xffff0000u;
+            }
+        }
+      }
+    }
+  };
+  int cu = warp;
+  int cp = begin_of(cu);
+  Scales cur, nxt;
+  if (cu < units) load_scales(cur, cu, cp);
+
+  // the tokens' digits: 16 lanes to a step, eight values each
+  uint8_t* digits = smem + fp.digits_at;                                     // [column][k_steps][t][j][8]
+  int* start = reinterpret_cast<int*>(smem + fp.start_at);                   // [k_steps * PER][COLS]
+  float* step_scale = reinterpret_cast<float*>(smem + fp.step_scale_at);     // [k_steps][2 * NT]
+  __syncthreads();
+  for (int i0 = 0; i0 < p.tokens * k_steps * 16; i0 += kFewThreads) {
+    const int i = i0 + threadIdx.x, item = min(i >> 4, p.tokens * k_steps - 1), e = i & 15;
+    const int token = item / k_steps, s = item - token * k_steps;
+    const uint4 raw = load8_checked(p.x + (int64_t)token * p.ldx, (k_begin + s) * 128 + 8 * e, p.K, p.x_aligned);
+    const uint32_t rw[4] = {raw.x, raw.y, raw.z, raw.w};
+    float v[8], top = 0.f;
+    bool odd = false;
+#pragma unroll
+    for (int n = 0; n < 8; ++n) {
+      v[n] = T::to_float((uint16_t)(rw[n / 2] >> (16 * (n % 2))));
+      if (!(fabsf(v[n]) <= 3.4028235e38f)) { v[n] = 0.f; odd = true; }
+      top = fmaxf(top, fabsf(v[n]));
+    }
+#pragma unroll
+    for (int o = 1; o < 16; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    if (odd) atomicOr(&strange, 1 << token);
+    const int up = min(156 - (int)(__float_as_uint(top) >> 23), 127);        // |v| * 2^up < 2^30
+    const float factor = __uint_as_float((uint32_t)(up + 127) << 23);
+    uint32_t q[8];
+#pragma unroll
+    for (int n = 0; n < 8; ++n) q[n] = ((uint32_t)__float2int_rn(v[n] * factor) + 0x00808080u) ^ 0x00808080u;
+    const uint32_t first[4] = {q[0], q[4], q[1], q[5]}, second[4] = {q[2], q[6], q[3], q[7]};   // the order of the codes of a word, low and high
+    uint32_t d0[4], d1[4];
+    transpose4(first, d0);
+    transpose4(second, d1);
+    int sum[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      sum[c] = __dp4a((int)d0[c], 0x01010101, __dp4a((int)d1[c], 0x01010101, 0));
+#pragma unroll
+      for (int o = 1; o < 16 / PER; o <<= 1) sum[c] += __shfl_xor_sync(0xffffffffu, sum[c], o);
+    }
+    if (i < p.tokens * k_steps * 16) {
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        *reinterpret_cast<uint2*>(digits + (token * 4 + c) * col_pitch + s * 128 + (e & 3) * 32 + (e >> 2) * 8) = make_uint2(d0[c], d1[c]);
+      if (e % (16 / PER) == 0) {
+        int* to = start + ((s * PER + e / (16 / PER)) * COLS + token * 4);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) to[c] = ZEROS ? -sum[c] : kMagic - 8 * sum[c];
+      }
+      if (e == 0) step_scale[s * 2 * NT + token] = __uint_as_float(up == 127 ? 0x00400000u : (uint32_t)(127 - up) << 23);   // 2^-up
+    }
+  }
+  __syncthreads();
+
+  float acc[NT][4];
+#pragma unroll
+  for (int i = 0; i < NT; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
+  uint32_t xat[NT];                        // columns beyond the tokens repeat the last one; nobody reads them
+#pragma unroll
+  for (int i = 0; i < NT; ++i) xat[i] = ptx::smem_u32(digits) + min(8 * i + g, p.tokens * 4 - 1) * col_pitch + t * 32;
+  int cslot = 0;
+  uint32_t parity = 0;
+  while (cu < units) {
+    int nu = cu, np = cp + 1;              // the piece after this one
+    const bool ends = np == end_of(cu);
+    if (ends) {
+      nu += kFewWarps;
+      np = begin_of(nu);
+    }
+    if (nu < units) load_scales(nxt, nu, np);
+    wait_piece(bar + 8 * cslot, parity);
+    const uint32_t w = ring + cslot * stage_bytes + g * 64 + t * 16;
+    const int s0 = cp * fp.piece, n = min(fp.piece, k_steps - s0);
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      if (u < n) {
+        const uint4 ra = lds128(w + u * 1024), rb = lds128(w + u * 1024 + 512);
+        const uint32_t wa[4] = {ra.x, ra.y, ra.z, ra.w}, wb[4] = {rb.x, rb.y, rb.z, rb.w};
+        const int from = (lane & 28) | (u & 3);
+        uint32_t sa[(PER + 1) / 2], sb[(PER + 1) / 2], za = 0, zb = 0;
+        if constexpr (PER == 1) {
+          const uint32_t both = __shfl_sync(0xffffffffu, cur.a[u / 4][0] | cur.b[u / 4][0] << 16, from);
+          sa[0] = both & 0xffffu;
+          sb[0] = both >> 16;
+        } else {
+#pragma unroll
+          for (int q = 0; q < PER / 2; ++q) {
+            sa[q] = __shfl_sync(0xffffffffu, cur.a[u / 4][q], from);
+            sb[q] = __shfl_sync(0xffffffffu, cur.b[u / 4][q], from);
+          }
+        }
+        if constexpr (ZEROS) {
+          if constexpr (PER <= 2) {
+            const uint32_t both = __shfl_sync(0xffffffffu, cur.za[u / 4] | cur.zb[u / 4] << 16, from);
+            za = both & 0xffffu;
+            zb = both >> 16;
+          } else {
+            za = __shfl_sync(0xffffffffu, cur.za[u / 4], from);
+            zb = __shfl_sync(0xffffffffu, cur.zb[u / 4], from);
+          }
+        }
+        const int s = s0 + u;
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+          const uint4 x0 = lds128(xat[i] + s * 128), x1 = lds128(xat[i] + s * 128 + 16);
+          const uint32_t xl[4] = {x0.x, x0.z, x1.x, x1.z}, xh[4] = {x0.y, x0.w, x1.y, x1.w};
+          const float ss = step_scale[s * 2 * NT + 2 * i + t / 2];
+#pragma unroll
+          for (int q = 0; q < PER; ++q) {
+            const int2 c = *reinterpret_cast<const int2*>(start + (s * PER + q) * COLS + 8 * i + 2 * t);
+            int d[4] = {c.x, c.y, c.x, c.y};
+            if constexpr (ZEROS) {
+              const int z0 = (za >> (8 * q)) & 0xff, z1 = (zb >> (8 * q)) & 0xff;
+              d[0] = z0 * c.x + kMagic; d[1] = z0 * c.y + kMagic;
+              d[2] = z1 * c.x + kMagic; d[3] = z1 * c.y + kMagic;
+            }
+#pragma unroll
+            for (int j = 4 / PER * q; j < 4 / PER * (q + 1); ++j)
+              mma_u8s8(d, wa[j] & 0x0f0f0f0fu, wb[j] & 0x0f0f0f0fu, (wa[j] >> 4) & 0x0f0f0f0fu, (wb[j] >> 4) & 0x0f0f0f0fu, xl[j], xh[j]);
+            const float fa = ss * T::to_float((uint16_t)(sa[q / 2] >> (16 * (q % 2)))), fb = ss * T::to_float((uint16_t)(sb[q / 2] >> (16 * (q % 2))));
+            acc[i][0] = fmaf(fa, __int_as_float(d[0]) - 12582912.f, acc[i][0]);
+            acc[i][1] = fmaf(fa, __int_as_float(d[1]) - 12582912.f, acc[i][1]);
+            acc[i][2] = fmaf(fb, __int_as_float(d[2]) - 12582912.f, acc[i][2]);
+            acc[i][3] = fmaf(fb, __int_as_float(d[3]) - 12582912.f, acc[i][3]);
+          }
+        }
+      }
+    }
+    __syncwarp();
+    issue();
+    cslot = cslot + 1 == fp.stages ? 0 : cslot + 1;
+    parity ^= cslot == 0 ? 1u : 0u;
+    if (ends) {                            // digits 2 (t % 2) and 2 (t % 2) + 1 of token 2 i + t / 2, weighted by 256^digit
+      const float lo = t & 1 ? 65536.f : 1.f, hi = t & 1 ? 16777216.f : 256.f;
+      float* out = sums + cu * p.tokens * 16;
+#pragma unroll
+      for (int i = 0; i < NT; ++i) {
+        float v0 = fmaf(hi, acc[i][1], lo * acc[i][0]), v1 = fmaf(hi, acc[i][3], lo * acc[i][2]);
+        v0 += __shfl_xor_sync(0xffffffffu, v0, 1);
+        v1 += __shfl_xor_sync(0xffffffffu, v1, 1);
+        const int token = 2 * i + t / 2;
+        if ((t & 1) == 0 && token < p.tokens) {
+          out[token * 16 + g] = v0;
+          out[token * 16 + g + 8] = v1;
+        }
+        acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
+      }
+    }
+    cu = nu; cp = np;
+    cur = nxt;
+  }
+  // one value per row and token: over the parts of k in the CTA, then over the cluster
+  if (S > 1) cluster.sync(); else __syncthreads();
+  const int values = (units >> fp.nk_log) * p.tokens * 16;
+  for (int i = rank * kFewThreads + threadIdx.x; i < values; i += S * kFewThreads) {
+    const int tile = i / (p.tokens * 16), at = i - tile * (p.tokens * 16), token = at >> 4;
+    const int row = (cl + tile * clusters) * 16 + (at & 15);
+    float v = 0.f;
+    for (int r = 0; r < S; ++r) {
+      const float* from = (S > 1 ? cluster.map_shared_rank(sums, r) : sums) + (tile << fp.nk_log) * p.tokens * 16 + at;
+      for (int j = 0; j < nk; ++j) v += from[j * p.tokens * 16];
+      if ((S > 1 ? *cluster.map_shared_rank(&strange, r) : strange) >> token & 1) v += not_finite_part<T>(p, PER, token, row, rank_part(p.blocks, r, S), rank_part(p.blocks, r + 1, S));
+    }
+    store_y<T>(p, token, row, v);
+  }
+  if (S > 1) cluster.sync();   // no CTA leaves while another may still read its sums
+}
+
 // Y = beta * Y, for alpha == 0 or K == 0
 template <class T>
 __global__ void __launch_bounds__(kGemvThreads) exo_gemv_q4_scale_kernel(const GemvParams p) {
@@ -281,12 +589,67 @@ __global__ void __launch_bounds__(kGemvThreads) exo_gemv_q4_scale_kernel(const G
 }
 
 using GemvFn = void (*)(GemvParams);
-template <class T, int PER> GemvFn pick_nt(int nt) {
-  return nt == 1 ? exo_gemv_q4_kernel<T, PER, 1> : nt == 2 ? exo_gemv_q4_kernel<T, PER, 2>
-         : nt <= 4 ? exo_gemv_q4_kernel<T, PER, 4> : exo_gemv_q4_kernel<T, PER, 8>;
+using FewFn = void (*)(FewParams, CUtensorMap);
+// tiles of eight tokens that a kernel computes
+int gemv_tiles(int tokens) { return tokens <= 32 ? (tokens + 7) / 8 : tokens <= 48 ? 6 : 8; }
+template <class T, int PER, bool ZEROS> GemvFn pick_tokens(int tokens) {
+  return tokens <= 2    ? exo_gemv_q4_kernel<T, PER, ZEROS, 1, 8>
+         : tokens <= 8  ? exo_gemv_q4_kernel<T, PER, ZEROS, 1, 2>
+         : tokens <= 16 ? exo_gemv_q4_kernel<T, PER, ZEROS, 2, 1>
+         : tokens <= 24 ? exo_gemv_q4_kernel<T, PER, ZEROS, 3, 1>
+         : tokens <= 32 ? exo_gemv_q4_kernel<T, PER, ZEROS, 4, 1>
+         : tokens <= 48 ? exo_gemv_q4_kernel<T, PER, ZEROS, 6, 1>
+                        : exo_gemv_q4_kernel<T, PER, ZEROS, 8, 1>;
 }
-template <class T> GemvFn pick_gemv(int group, int nt) {
-  return group == 128 ? pick_nt<T, 1>(nt) : group == 64 ? pick_nt<T, 2>(nt) : pick_nt<T, 4>(nt);
+template <class T, bool ZEROS> GemvFn pick_group(int group, int tokens) {
+  return group == 128 ? pick_tokens<T, 1, ZEROS>(tokens) : group == 64 ? pick_tokens<T, 2, ZEROS>(tokens) : pick_tokens<T, 4, ZEROS>(tokens);
+}
+template <class T> GemvFn pick_gemv(int group, bool zeros, int tokens) {
+  return zeros ? pick_group<T, true>(group, tokens) : pick_group<T, false>(group, tokens);
+}
+
+template <class T, int PER, bool ZEROS> FewFn pick_few_tokens(int tokens) {
+  return tokens <= 2 ? exo_gemv_q4_few_kernel<T, PER, ZEROS, 1> : exo_gemv_q4_few_kernel<T, PER, ZEROS, 2>;
+}
+template <class T, bool ZEROS> FewFn pick_few_group(int group, int tokens) {
+  return group == 128 ? pick_few_tokens<T, 1, ZEROS>(tokens) : group == 64 ? pick_few_tokens<T, 2, ZEROS>(tokens) : pick_few_tokens<T, 4, ZEROS>(tokens);
+}
+template <class T> FewFn pick_few(int group, bool zeros, int tokens) {
+  return zeros ? pick_few_group<T, true>(group, tokens) : pick_few_group<T, false>(group, tokens);
+}
+
+// How the few-token kernel is cut.  Large matrices (a few dozen KB for every SM) run as one CTA per SM with pieces of 8
+// steps, which the copies like best (32768 x 16384, one token: 51.6 us, against 55.8 with two CTAs and pieces of 4); small
+// ones as two CTAs per SM with pieces of 4, where the time to the first piece counts.  The cluster cuts k where a CTA's
+// digits would take more than 40 KB.  False: the activations do not fit.
+bool plan_few(FewParams& fp, const GemvParams& p, int per, int sms, unsigned* ctas, unsigned* cluster, size_t* smem) {
+  const int nt = p.tokens <= 2 ? 1 : 2;
+  const int64_t tiles = (p.rows + 15) / 16;
+  int S = 1;
+  while (S < 8 && p.blocks >= 2 * S && 4 * p.tokens * ((p.blocks + S - 1) / S) * 128 > 40 * 1024) S *= 2;
+  const bool large = tiles * p.blocks >= (int64_t)sms * 96;
+  const int slice = (p.blocks + S - 1) / S, least = p.blocks / S;
+  const int64_t slots = (int64_t)(large ? 1 : 2) * sms / S, clusters = tiles < slots ? tiles : slots;
+  const int most = (int)((tiles + clusters - 1) / clusters);     // tiles of a cluster
+  fp.piece = large ? 8 : 4;
+  // parts of k: two pieces each, or fewer where the CTA would otherwise have less than a part for every warp
+  fp.nk_log = 0;
+  while (fp.nk_log < 3 && (least + fp.piece - 1) / fp.piece >= ((most << fp.nk_log) < kFewWarps ? 2 : 4) << fp.nk_log) ++fp.nk_log;
+  const int turns = ((most << fp.nk_log) + kFewWarps - 1) / kFewWarps;
+  const int pieces = ((slice + fp.piece - 1) / fp.piece + (1 << fp.nk_log) - 1) >> fp.nk_log;
+  fp.stages = turns * pieces < 2 ? 1 : 2;
+  int64_t at = 256 + (int64_t)(most << fp.nk_log) * p.tokens * 64;
+  fp.digits_at = (int)at; at += 4 * p.tokens * ((int64_t)slice * 128 + 16);
+  fp.start_at = (int)at; at += (int64_t)slice * per * 8 * nt * 4;
+  fp.step_scale_at = (int)at; at += (int64_t)slice * 2 * nt * 4;
+  at = (at + 127) / 128 * 128;
+  fp.ring_at = (int)at;
+  at += kFewWarps * fp.stages * fp.piece * 1024;
+  fp.g = p;
+  *ctas = (unsigned)(clusters * S);
+  *cluster = (unsigned)S;
+  *smem = (size_t)at;
+  return at <= kMostSmem;
 }
 
 exo_gemm_status_t check_q4(const exo_q4_t* q) {
@@ -332,10 +695,20 @@ exo_gemm_status_t run_quant(const exo_q4_t* q, void* W, int64_t ldw, int32_t w_d
 }
 
 }  // namespace
+unsigned take_gave_up_q4(cudaError_t* e) { return take_gave_up(e); }
+unsigned take_gave_up_moe(cudaError_t* e);   // moe.cu
 }  // namespace decode
 }  // namespace exo
 
 using namespace exo::decode;
+
+extern "C" exo_gemm_status_t exo_decode_check(void) {
+  cudaError_t e = cudaDeviceSynchronize();
+  if (e != cudaSuccess) return cuda_failed(e);
+  const unsigned n = take_gave_up_q4(&e) | (e == cudaSuccess ? take_gave_up_moe(&e) : 0u);
+  if (e != cudaSuccess) return cuda_failed(e);
+  return n ? EXO_GEMM_ERR_DEVICE_TIMEOUT : EXO_GEMM_OK;
+}
 
 extern "C" exo_gemm_status_t exo_q4_quantize(const exo_q4_t* q, const void* W, int64_t ldw, int32_t w_dtype, void* cuda_stream) {
   return run_quant(q, const_cast<void*>(W), ldw, w_dtype, false, cuda_stream);
@@ -374,19 +747,29 @@ extern "C" exo_gemm_status_t exo_gemv_q4_run(const exo_q4_t* W, int64_t tokens, 
   }
   // A CTA reads its part of X once for 16 * wr weight rows: more rows for more tokens.  Then the cluster cuts k until the
   // grid fills the device twice, as long as a warp keeps a step.
-  p.wr = tokens <= 2 ? 1 : tokens <= 8 ? 4 : 8;
-  const int64_t tiles = (p.rows + 16 * p.wr - 1) / (16 * p.wr);
-  const int nk = kGemvWarps / p.wr, nt = (p.tokens + 7) / 8;
+  if (p.tokens <= 4 && p.rows < (1LL << 31) - 16) {
+    FewParams fp{};
+    size_t smem = 0;
+    unsigned ctas = 0, cluster = 1;
+    if (plan_few(fp, p, 128 / W->group, sms, &ctas, &cluster, &smem)) {
+      CUtensorMap map;
+      if (!exo::encode_steps_map(&map, p.codes, (uint64_t)p.rows, (uint64_t)p.blocks, (uint32_t)fp.piece)) return EXO_GEMM_ERR_CUDA;
+      FewFn fn = bf16 ? pick_few<Bf16>(W->group, W->zeros, p.tokens) : pick_few<Fp16>(W->group, W->zeros, p.tokens);
+      return launch((void*)fn, ctas, 1, kFewThreads, smem, cluster, (cudaStream_t)cuda_stream, &fp, &map);
+    }
+  }
+  const int nk = tokens <= 2 ? 8 : tokens <= 8 ? 2 : 1, wr = kGemvWarps / nk, nt = gemv_tiles(p.tokens);
+  const int64_t tiles = (p.rows + 16 * wr - 1) / (16 * wr);
   int S = 1;
   while (S < 8 && tiles * S < 2 * sms && p.blocks >= 2 * S * nk) S *= 2;
   if (tiles * S >= (1LL << 31)) return EXO_GEMM_ERR_UNSUPPORTED;
   const int mine = (p.blocks + S - 1) / S;
   // staged activations: all of the CTA's part of k where that leaves room for two CTAs per SM
-  const int most = (100 * 1024 / p.tokens - 64) / 256;
+  const int staged = nt == 1 ? p.tokens : 8 * nt, most = (100 * 1024 / staged - 64) / 256;
   p.chunk = mine < most ? mine : most;
-  size_t smem = (size_t)p.tokens * gemv_pitch(p.chunk);
-  const size_t reduce = (size_t)(kGemvWarps + p.wr) * nt * 512;
+  size_t smem = (size_t)staged * gemv_pitch(p.chunk);
+  const size_t reduce = (size_t)(kGemvWarps + wr) * nt * 512;
   if (smem < reduce) smem = reduce;
-  GemvFn fn = bf16 ? pick_gemv<Bf16>(W->group, nt) : pick_gemv<Fp16>(W->group, nt);
+  GemvFn fn = bf16 ? pick_gemv<Bf16>(W->group, W->zeros, p.tokens) : pick_gemv<Fp16>(W->group, W->zeros, p.tokens);
   return launch((void*)fn, (unsigned)(tiles * S), 1, kGemvThreads, smem, (unsigned)S, (cudaStream_t)cuda_stream, &p);
 }

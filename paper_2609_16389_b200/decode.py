@@ -15,7 +15,7 @@ from .binding import BF16, FP16, FP32, OK, ExoGemmError  # noqa: F401
 
 EXPORTED_SYMBOLS = (
     "exo_q4_quantize", "exo_q4_dequantize", "exo_gemv_q4_run", "exo_moe_validate", "exo_moe_create", "exo_moe_run",
-    "exo_moe_workspace_bytes", "exo_moe_destroy",
+    "exo_moe_workspace_bytes", "exo_moe_destroy", "exo_decode_check",
 )
 
 _vp, _i32, _i64, _f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
@@ -96,6 +96,10 @@ def exo_moe_create(desc):
 def exo_moe_run(handle, weights, tokens: int, x_ptr: int, ldx: int, y_ptr: int, ldy: int, index_ptr: int = 0,
                 weight_ptr: int = 0, stream: int = 0) -> int:
     return lib().exo_moe_run(handle, weights, tokens, x_ptr, ldx, y_ptr, ldy, index_ptr, weight_ptr, stream)
+
+
+def exo_decode_check() -> int:
+    return lib().exo_decode_check()
 
 
 def exo_moe_workspace_bytes(handle) -> int:
