@@ -28,6 +28,10 @@ struct Bf16 {
   static constexpr uint32_t kNibbleBase = 0x43004300u;   // a pair of 128.0: one unit in the last place is 1
   static __device__ __forceinline__ float to_float(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
   static __device__ __forceinline__ uint16_t from_float(float v) { return __bfloat16_as_ushort(__float2bfloat16_rn(v)); }
+  static __device__ __forceinline__ uint32_t pair(float lo, float hi) {
+    const __nv_bfloat162 r = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&r);
+  }
   static __device__ __forceinline__ float max_finite() { return __uint_as_float(0x7f7f0000u); }
   static __device__ __forceinline__ uint32_t sub2(uint32_t a, uint32_t b) {
     const __nv_bfloat162 r = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
@@ -47,6 +51,10 @@ struct Fp16 {
   static constexpr uint32_t kNibbleBase = 0x64006400u;   // a pair of 1024.0: one unit in the last place is 1
   static __device__ __forceinline__ float to_float(uint16_t v) { return __half2float(__ushort_as_half(v)); }
   static __device__ __forceinline__ uint16_t from_float(float v) { return __half_as_ushort(__float2half_rn(v)); }
+  static __device__ __forceinline__ uint32_t pair(float lo, float hi) {
+    const __half2 r = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&r);
+  }
   static __device__ __forceinline__ float max_finite() { return 65504.f; }
   static __device__ __forceinline__ uint32_t sub2(uint32_t a, uint32_t b) {
     const __half2 r = __hsub2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));

@@ -1,6 +1,8 @@
 // 4-bit weights: quantisation, its inverse, and the product of a few tokens with a 4-bit matrix (exo_decode.h).
 #include <cooperative_groups.h>
 
+#include <type_traits>
+
 #include "../../include/exo_decode.h"
 #include "decode_core.cuh"
 #include "decode_host.h"
@@ -12,53 +14,89 @@ namespace {
 
 // ==== quantisation ===============================================================================================
 // A lane holds eight consecutive weights, so a group is 16, 8 or 4 neighbouring lanes and its extremes are a shuffle
-// tree; a warp walks along a row, 256 weights at a time.  Bound by memory: 2 (4) bytes in and 1/2 out per weight,
-// and the division by the scale (IEEE, so that codes are the formula's) hides behind it.
+// tree; a warp walks along a row, 256 weights at a time.  Memory is the bound (2 or 4 bytes in and 1/2 out per weight) only
+// if a weight costs about a dozen instructions: a division takes that many alone.  So w / scale is w times the rounded
+// reciprocal, off by less than 2^-18 for quotients up to 16, which rounds to the same integer unless it lies that near the
+// middle of two; lanes that see such a weight divide.
 constexpr int kQuantThreads = 256;
 constexpr int kQuantSegment = 4096;   // weights of a row per warp
 
-template <class T, class W> struct Source;   // eight weights as floats, and back
-template <class T> struct Source<T, uint16_t> {
-  static __device__ __forceinline__ void load(const uint16_t* row, int k, int K, bool aligned, float (&v)[8]) {
-    const uint4 r = load8_checked(row, k, K, aligned);
-    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+// Eight elements at k .. k + 7 of a row (those at and beyond K are 0, and not written).  ALIGN: bytes that every row's start
+// is a multiple of.
+template <int BYTES, int ALIGN>
+__device__ __forceinline__ void load_eight(const void* row, int k, int K, uint32_t (&w)[2 * BYTES]) {
+  const char* p = static_cast<const char*>(row) + (int64_t)k * BYTES;
+  if (k + 8 <= K) {
+    if constexpr (ALIGN == 16) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = T::to_float((uint16_t)(w[i / 2] >> (16 * (i % 2))));
-  }
-  static __device__ __forceinline__ void store(uint16_t* row, int k, int K, bool aligned, const float (&v)[8]) {
-    if (aligned && k + 8 <= K) {
-      uint32_t w[4];
+      for (int i = 0; i < BYTES / 2; ++i) {
+        const uint4 v = __ldcs(reinterpret_cast<const uint4*>(p) + i);
+        w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
+      }
+    } else if constexpr (ALIGN == 8) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = (uint32_t)T::from_float(v[2 * i]) | (uint32_t)T::from_float(v[2 * i + 1]) << 16;
-      *reinterpret_cast<uint4*>(row + k) = make_uint4(w[0], w[1], w[2], w[3]);
+      for (int i = 0; i < BYTES; ++i) {
+        const uint2 v = __ldcs(reinterpret_cast<const uint2*>(p) + i);
+        w[2 * i] = v.x; w[2 * i + 1] = v.y;
+      }
+    } else if constexpr (ALIGN == 4) {
+#pragma unroll
+      for (int i = 0; i < 2 * BYTES; ++i) w[i] = __ldcs(reinterpret_cast<const uint32_t*>(p) + i);
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (k + i < K) row[k + i] = T::from_float(v[i]);
+      for (int i = 0; i < 4; ++i) {
+        const uint16_t* h = reinterpret_cast<const uint16_t*>(p) + 2 * i;
+        w[i] = (uint32_t)h[0] | (uint32_t)h[1] << 16;
+      }
     }
+    return;
   }
-};
-template <class T> struct Source<T, float> {
-  static __device__ __forceinline__ void load(const float* row, int k, int K, bool aligned, float (&v)[8]) {
-    if (aligned && k + 8 <= K) {
-      const float4 a = *reinterpret_cast<const float4*>(row + k), b = *reinterpret_cast<const float4*>(row + k + 4);
-      v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+#pragma unroll
+  for (int i = 0; i < 2 * BYTES; ++i) w[i] = 0;
+  for (int i = 0; i < 8; ++i)
+    if (k + i < K) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (j == i) {
+          if constexpr (BYTES == 4) w[j] = reinterpret_cast<const uint32_t*>(p)[j];
+          else w[j / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[j] << (16 * (j % 2));
+        }
+    }
+}
+template <int BYTES, int ALIGN>
+__device__ __forceinline__ void store_eight(void* row, int k, int K, const uint32_t (&w)[2 * BYTES]) {
+  char* p = static_cast<char*>(row) + (int64_t)k * BYTES;
+  if (k + 8 <= K) {
+    if constexpr (ALIGN == 16) {
+#pragma unroll
+      for (int i = 0; i < BYTES / 2; ++i) __stcs(reinterpret_cast<uint4*>(p) + i, make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]));
+    } else if constexpr (ALIGN == 8) {
+#pragma unroll
+      for (int i = 0; i < BYTES; ++i) reinterpret_cast<uint2*>(p)[i] = make_uint2(w[2 * i], w[2 * i + 1]);
+    } else if constexpr (ALIGN == 4) {
+#pragma unroll
+      for (int i = 0; i < 2 * BYTES; ++i) reinterpret_cast<uint32_t*>(p)[i] = w[i];
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = k + i < K ? row[k + i] : 0.f;
+      for (int i = 0; i < 8; ++i) reinterpret_cast<uint16_t*>(p)[i] = (uint16_t)(w[i / 2] >> (16 * (i % 2)));
     }
+    return;
   }
-  static __device__ __forceinline__ void store(float* row, int k, int K, bool aligned, const float (&v)[8]) {
-    if (aligned && k + 8 <= K) {
-      *reinterpret_cast<float4*>(row + k) = make_float4(v[0], v[1], v[2], v[3]);
-      *reinterpret_cast<float4*>(row + k + 4) = make_float4(v[4], v[5], v[6], v[7]);
-    } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (k + i < K) row[k + i] = v[i];
+  for (int i = 0; i < 8; ++i)
+    if (k + i < K) {
+      if constexpr (BYTES == 4) reinterpret_cast<uint32_t*>(p)[i] = w[i];
+      else reinterpret_cast<uint16_t*>(p)[i] = (uint16_t)(w[i / 2] >> (16 * (i % 2)));
     }
-  }
-};
+}
+
+// a / N, correctly rounded (P. Markstein: the product with the rounded reciprocal, corrected by its exact remainder).
+template <int N>
+__device__ __forceinline__ float divided(float a) {
+  if (!(a > 1.0e-30f && a < 1.0e38f)) return __fdiv_rn(a, (float)N);   // where the remainder may underflow, or not be finite
+  const float q = a * (1.f / N);
+  return fmaf(fmaf(-q, (float)N, a), 1.f / N, q);
+}
 
 struct QuantParams {
   int64_t rows, ldw;
@@ -67,12 +105,13 @@ struct QuantParams {
   uint32_t* codes;
   uint16_t* scales;
   uint8_t* zeros;
-  bool aligned;
 };
 
-// T: type of the scales.  WT/W: type of the weights (a 16-bit type with its format, or float).
-template <class T, class WT, class W>
+// T: type of the scales; WT: type of the weights (float: 32 bits).
+template <class T, class WT, int ALIGN>
 __global__ void __launch_bounds__(kQuantThreads) exo_q4_quantize_kernel(const QuantParams p) {
+  constexpr bool WIDE = std::is_same<WT, float>::value;
+  constexpr int BYTES = WIDE ? 4 : 2;
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();
   const int lane = threadIdx.x & 31;
@@ -81,44 +120,75 @@ __global__ void __launch_bounds__(kQuantThreads) exo_q4_quantize_kernel(const Qu
   if (row >= p.rows) return;
   const int seg = (int)(item - row * p.segments);
   const int k_end = min((seg + 1) * (kQuantSegment / 128), p.blocks) * 128;
-  const W* src = static_cast<const W*>(p.w) + row * p.ldw;
-  const int lanes = p.group / 8, per_row = p.blocks * 128 / p.group;
-#pragma unroll 2
+  const char* src = static_cast<const char*>(p.w) + row * p.ldw * BYTES;
+  const int lanes = p.group / 8, per_row = p.blocks * 128 / p.group, group_log = 31 - __clz(p.group);
+  auto weights = [&](const uint32_t (&w)[2 * BYTES], float (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if constexpr (WIDE) v[i] = __uint_as_float(w[i]);
+      else v[i] = WT::to_float((uint16_t)(w[i / 2] >> (16 * (i % 2))));
+    }
+  };
+  uint32_t ahead[2 * BYTES];
+  load_eight<BYTES, ALIGN>(src, seg * kQuantSegment + 8 * lane, p.K, ahead);
   for (int k0 = seg * kQuantSegment; k0 < k_end; k0 += 256) {
     const int k = k0 + 8 * lane;
     float v[8];
-    Source<WT, W>::load(src, k, p.K, p.aligned, v);
+    weights(ahead, v);
+    if (k0 + 256 < k_end) load_eight<BYTES, ALIGN>(src, k + 256, p.K, ahead);
     float lo = 0.f, hi = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) { lo = fminf(lo, v[i]); hi = fmaxf(hi, v[i]); }
+    if (!p.zeros) hi = fmaxf(hi, -lo);
     for (int o = 1; o < lanes; o <<= 1) {
-      lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
       hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+      if (p.zeros) lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
     }
-    const float raw = p.zeros ? __fdiv_rn(hi - lo, 15.f) : __fdiv_rn(fmaxf(hi, -lo), 7.f);
+    const float raw = p.zeros ? divided<15>(hi - lo) : divided<7>(hi);
     const uint16_t s16 = T::from_float(fminf(raw, T::max_finite()));
     const float s = T::to_float(s16);
+    float inverse;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inverse) : "f"(s));
+    if (s == 0.f) inverse = 0.f;
+    bool near = !(inverse <= 3.0e38f) || raw > T::max_finite();   // no reciprocal, or quotients beyond 16
     float zero = 8.f;
-    if (p.zeros && s > 0.f) zero = fminf(fmaxf(rintf(__fdiv_rn(-lo, s)), 0.f), 15.f);
+    if (p.zeros && s > 0.f) {
+      const float y = -lo * inverse;
+      zero = rintf(y);
+      if (near || fabsf(y - zero) > 0.49998f) zero = rintf(__fdiv_rn(-lo, s));
+      zero = fminf(fmaxf(zero, 0.f), 15.f);
+    }
     uint32_t word = 0;
+    const float magic = 12582912.f + zero;      // 1.5 * 2^23: the sum's last bits are the rounded quotient plus zero
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float q = s > 0.f ? rintf(__fdiv_rn(v[i], s)) + zero : zero;   // symmetric: -8 .. 7 plus 8
-      word |= (uint32_t)fminf(fmaxf(q, 0.f), 15.f) << (4 * (i / 2 + 4 * (i % 2)));
+      const float y = v[i] * inverse, m = y + magic;
+      near |= fabsf(y - (m - magic)) > 0.49998f;
+      word += (uint32_t)__vimin_s32_relu(__float_as_int(m) - 0x4b400000, 15) << (4 * (i / 2 + 4 * (i % 2)));
+    }
+    if (near) {
+      word = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float q = rintf(__fdiv_rn(v[i], s)) + zero;   // without zero points: -8 .. 7 plus 8
+        word |= (uint32_t)fminf(fmaxf(q, 0.f), 15.f) << (4 * (i / 2 + 4 * (i % 2)));
+      }
     }
     if (k < k_end) {   // the last pass may hold one block of 128 only
       const int l = lane & 15;
       p.codes[(row * p.blocks + k / 128) * 16 + 4 * (l & 3) + (l >> 2)] = word;
       if ((lane & (lanes - 1)) == 0) {
-        p.scales[row * per_row + k / p.group] = s16;
-        if (p.zeros) p.zeros[row * per_row + k / p.group] = (uint8_t)zero;
+        p.scales[row * per_row + (k >> group_log)] = s16;
+        if (p.zeros) p.zeros[row * per_row + (k >> group_log)] = (uint8_t)zero;
       }
     }
   }
 }
 
-template <class T, class WT, class W>
+template <class T, class WT, int ALIGN>
 __global__ void __launch_bounds__(kQuantThreads) exo_q4_dequantize_kernel(const QuantParams p) {
+  constexpr bool WIDE = std::is_same<WT, float>::value;
+  constexpr int BYTES = WIDE ? 4 : 2;
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();
   const int lane = threadIdx.x & 31;
@@ -127,20 +197,39 @@ __global__ void __launch_bounds__(kQuantThreads) exo_q4_dequantize_kernel(const 
   if (row >= p.rows) return;
   const int seg = (int)(item - row * p.segments);
   const int k_end = min((seg + 1) * (kQuantSegment / 128), p.blocks) * 128;
-  W* dst = static_cast<W*>(p.w) + row * p.ldw;
-  const int per_row = p.blocks * 128 / p.group;
-#pragma unroll 4
-  for (int k0 = seg * kQuantSegment; k0 < k_end; k0 += 256) {
-    const int k = k0 + 8 * lane;
-    if (k < k_end) {
-      const int l = lane & 15;
-      const uint32_t word = p.codes[(row * p.blocks + k / 128) * 16 + 4 * (l & 3) + (l >> 2)];
-      const float s = T::to_float(p.scales[row * per_row + k / p.group]);
-      const int zero = p.zeros ? (int)p.zeros[row * per_row + k / p.group] : 8;
-      float v[8];
+  char* dst = static_cast<char*>(p.w) + row * p.ldw * BYTES;
+  const int group_log = 31 - __clz(p.group);
+  const int64_t groups = row * (p.blocks * 128 / p.group);
+  const uint32_t* codes = p.codes + row * p.blocks * 16 + 4 * (lane & 3) + ((lane & 15) >> 2);
+  constexpr int N = 4;   // passes whose loads are in flight together
+  for (int k0 = seg * kQuantSegment + 8 * lane; k0 < k_end; k0 += N * 256) {
+    uint32_t word[N];
+    float s[N], zero[N];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = (float)((int)(word >> (4 * (i / 2 + 4 * (i % 2))) & 15u) - zero) * s;
-      Source<WT, W>::store(dst, k, p.K, p.aligned, v);
+    for (int u = 0; u < N; ++u) {
+      const int k = k0 + 256 * u;
+      if (k < k_end) {
+        word[u] = __ldcs(codes + k / 128 * 16);
+        s[u] = T::to_float(__ldg(p.scales + groups + (k >> group_log)));
+        zero[u] = 8388608.f + (p.zeros ? (float)__ldg(p.zeros + groups + (k >> group_log)) : 8.f);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      const int k = k0 + 256 * u;
+      if (k < k_end) {
+        float v[8];
+        uint32_t out[2 * BYTES];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)   // 2^23 + code, less 2^23 + zero: exact, as is the product with the scale
+          v[i] = (__uint_as_float((word[u] >> (4 * (i / 2 + 4 * (i % 2))) & 15u) | 0x4b000000u) - zero[u]) * s[u];
+#pragma unroll
+        for (int i = 0; i < 2 * BYTES; ++i) {
+          if constexpr (WIDE) out[i] = __float_as_uint(v[i]);
+          else out[i] = WT::pair(v[2 * i], v[2 * i + 1]);
+        }
+        store_eight<BYTES, ALIGN>(dst, k, p.K, out);
+      }
     }
   }
 }
@@ -665,11 +754,18 @@ exo_gemm_status_t check_q4_pointers(const exo_q4_t* q) {
 }
 int blocks_of(int64_t K) { return (int)((K + 127) / 128); }
 
-template <class T>
-void* quant_fn(int w_dtype, bool back) {
-  if (w_dtype == EXO_GEMM_FP32) return back ? (void*)exo_q4_dequantize_kernel<T, T, float> : (void*)exo_q4_quantize_kernel<T, T, float>;
-  if (w_dtype == EXO_GEMM_BF16) return back ? (void*)exo_q4_dequantize_kernel<T, Bf16, uint16_t> : (void*)exo_q4_quantize_kernel<T, Bf16, uint16_t>;
-  return back ? (void*)exo_q4_dequantize_kernel<T, Fp16, uint16_t> : (void*)exo_q4_quantize_kernel<T, Fp16, uint16_t>;
+template <class T, class WT, int ALIGN> void* quant_dir(bool back) {
+  return back ? (void*)exo_q4_dequantize_kernel<T, WT, ALIGN> : (void*)exo_q4_quantize_kernel<T, WT, ALIGN>;
+}
+template <class T, class WT> void* quant_align(int align, bool back) {
+  if (align == 16) return quant_dir<T, WT, 16>(back);
+  if (align == 8) return quant_dir<T, WT, 8>(back);
+  if constexpr (std::is_same<WT, float>::value) return quant_dir<T, WT, 4>(back);
+  else return align == 4 ? quant_dir<T, WT, 4>(back) : quant_dir<T, WT, 2>(back);
+}
+template <class T> void* quant_fn(int w_dtype, int align, bool back) {
+  return w_dtype == EXO_GEMM_FP32 ? quant_align<T, float>(align, back)
+         : w_dtype == EXO_GEMM_BF16 ? quant_align<T, Bf16>(align, back) : quant_align<T, Fp16>(align, back);
 }
 
 exo_gemm_status_t run_quant(const exo_q4_t* q, void* W, int64_t ldw, int32_t w_dtype, bool back, void* cuda_stream) {
@@ -687,10 +783,11 @@ exo_gemm_status_t run_quant(const exo_q4_t* q, void* W, int64_t ldw, int32_t w_d
   p.rows = q->rows; p.ldw = ldw; p.K = (int)q->K; p.blocks = blocks_of(q->K); p.group = q->group;
   p.segments = (p.blocks * 128 + kQuantSegment - 1) / kQuantSegment;
   p.w = W; p.codes = (uint32_t*)q->codes; p.scales = (uint16_t*)q->scales; p.zeros = q->zeros;
-  p.aligned = ((uintptr_t)W & 15u) == 0 && (ldw * bytes) % 16 == 0;
+  const uintptr_t at = (uintptr_t)W | (uintptr_t)(ldw * bytes);   // what every row's start is a multiple of
+  const int align = at % 16 == 0 ? 16 : at % 8 == 0 ? 8 : at % 4 == 0 ? 4 : 2;
   const int64_t ctas = (p.rows * p.segments + kQuantThreads / 32 - 1) / (kQuantThreads / 32);
   if (ctas >= (1LL << 31)) return EXO_GEMM_ERR_UNSUPPORTED;
-  void* fn = q->dtype == EXO_GEMM_BF16 ? quant_fn<Bf16>(w_dtype, back) : quant_fn<Fp16>(w_dtype, back);
+  void* fn = q->dtype == EXO_GEMM_BF16 ? quant_fn<Bf16>(w_dtype, align, back) : quant_fn<Fp16>(w_dtype, align, back);
   return launch(fn, (unsigned)ctas, 1, kQuantThreads, 0, 1, (cudaStream_t)cuda_stream, &p);
 }
 

@@ -119,6 +119,64 @@ def test_quantize_follows_its_formula_code_by_code(rows, K, group, zeros, dtype,
     assert (back[:, K:] == 3).all()
 
 
+def quantized(w, group, dtype, zeros):
+    """codes (as numbers), scales and zero points of a host matrix, from the kernel"""
+    t = torch()
+    rows, K = w.shape
+    G = groups(K, group)
+    codes = t.zeros(rows, D.padded_k(K) // 2, dtype=t.uint8, device="cuda")
+    scales = t.zeros(rows, G, dtype=tt(dtype), device="cuda")
+    z = t.zeros(rows, G, dtype=t.uint8, device="cuda") if zeros else None
+    wd = w.cuda()
+    D.Q4(rows, K, group, dtype, codes.data_ptr(), scales.data_ptr(), z.data_ptr() if zeros else 0).quantize(
+        wd.data_ptr(), K, {t.bfloat16: D.BF16, t.float16: D.FP16, t.float32: D.FP32}[w.dtype], stream())
+    return codes.cpu().numpy(), scales.cpu(), None if z is None else z.cpu().numpy()
+
+
+@pytest.mark.parametrize("src", [D.BF16, D.FP32])
+@pytest.mark.parametrize("zeros", [False, True])
+def test_quantize_many_ties_and_neighbours_of_ties(src, zeros):
+    """Weights at, one step below and one step above the middle of two codes, at scales over the whole range."""
+    t = torch()
+    rows, K = 240, 128
+    w = np.zeros((rows, K), np.float32)
+    for r in range(rows):
+        s = np.float32(2.0 ** (r - 120)) * np.float32(1 + (r % 7) / 8)
+        w[r, 0], w[r, 1] = 7 * s, -7 * s
+        mid = (np.arange(2, K) % 14 - 6.5).astype(np.float32) * s
+        step = np.arange(2, K) % 3 - 1
+        w[r, 2:] = np.where(step < 0, np.nextafter(mid, np.float32(-1e38)), np.where(step > 0, np.nextafter(mid, np.float32(1e38)), mid))
+    w = t.from_numpy(w).to(tt(src))
+    codes, scales, z = quantized(w, 128, D.BF16, zeros)
+    v, s = w.float().numpy(), scales.float().numpy()
+    if zeros:
+        raw = (np.maximum(v.max(1), np.float32(0)) - np.minimum(v.min(1), np.float32(0))) / np.float32(15)
+        zr = np.clip(np.rint(-np.minimum(v.min(1), np.float32(0)) / s[:, 0]), 0, 15).astype(np.float32)
+        assert np.array_equal(z[:, 0], zr)
+    else:
+        raw, zr = np.abs(v).max(1) / np.float32(7), np.full(rows, 8, np.float32)
+    assert t.equal(t.from_numpy(raw).bfloat16(), scales[:, 0])
+    q = np.clip(np.rint(v / s) + zr[:, None], 0, 15).astype(np.uint8)
+    assert np.array_equal(codes, D.pack_codes(q))
+
+
+def test_quantize_extremes():
+    """Scales that are subnormal, beyond their type's range or zero, and quotients far beyond the codes."""
+    t = torch()
+    w = t.zeros(6, 128)
+    w[0, :4] = t.tensor([1e-7, -1e-7, 5e-8, 3e-8])          # fp16: a scale of a few units in the last place
+    w[1, :2] = t.tensor([1e-9, -1e-9])                      # rounds to 0
+    w[2, :4] = t.tensor([3e38, -3e38, 8e11, -8e11])         # saturates; quotients of 1e33 and 1e7
+    w[3, :2] = t.tensor([1e-40, -1e-40])                    # subnormal weights
+    w[4, :2] = t.tensor([5e5, -4.6e5])
+    codes, scales, _ = quantized(w, 128, D.FP16, False)
+    s = np.minimum(np.abs(w.numpy()).max(1) / np.float32(7), np.float32(65504)).astype(np.float16)
+    assert np.array_equal(scales[:, 0].numpy(), s)
+    with np.errstate(divide="ignore", invalid="ignore"):
+        q = np.where(s[:, None] > 0, np.clip(np.rint(w.numpy() / s[:, None].astype(np.float32)), -8, 7) + 8, 8).astype(np.uint8)
+    assert np.array_equal(codes, D.pack_codes(q))
+
+
 def test_quantize_saturates_a_scale_that_its_type_cannot_hold():
     t = torch()
     w = t.full((1, 128), 3.0e38, device="cuda")
@@ -190,6 +248,61 @@ def test_gemv_keeps_infinities_to_their_token_and_row():
     rest = [r for r in range(50) if r != 7]
     for token in (0, 2, 3):
         assert t.equal(y[token, rest], clean[token, rest]) and not t.isfinite(y[token, 7])
+
+
+@pytest.mark.parametrize("dtype", [D.BF16, D.FP16])
+def test_gemv_of_infinities_gives_infinities(dtype):
+    """inf * 0 is NaN, inf times another weight is inf, and both stay in their token."""
+    t = torch()
+    m = Matrix(40, 300, 32, dtype, True, seed=15)
+    x = t.randn(3, 300, generator=t.Generator().manual_seed(1)).to(tt(dtype))
+    x[1, 3], x[2, 290], x[2, 17] = float("inf"), float("-inf"), float("nan")
+    y = t.empty(3, 40, device="cuda")
+    xd = x.cuda()
+    m.q4().gemv(3, xd.data_ptr(), 300, y.data_ptr(), 40, D.FP32, stream=stream())
+    y = y.cpu().numpy()
+    w = m.values[:, 3]
+    assert np.array_equal(np.isnan(y[1]), w == 0) and (y[1][w > 0] == np.inf).all() and (y[1][w < 0] == -np.inf).all()
+    assert np.isfinite(y[0]).all() and np.isnan(y[2]).all()
+
+
+@pytest.mark.parametrize("tokens", [1, 2, 3, 4, 5])
+def test_gemv_at_the_ends_of_the_activations_range(tokens):
+    """Tiny, huge and mixed magnitudes within one group of 128, against the bound that the header states."""
+    t = torch()
+    rows, K = 64, 640
+    m = Matrix(rows, K, 128, D.BF16, False, seed=21, spread=1.0)
+    gen = t.Generator().manual_seed(tokens)
+    x = t.randn(tokens, K, generator=gen) * 2.0 ** t.randint(-30, 30, (tokens, K), generator=gen).float()
+    x[:, 128:256] *= 2.0 ** -100
+    x[:, 256:384] = 0
+    x[:, 384:512] *= 2.0 ** 60
+    x = x.bfloat16()
+    y = t.empty(tokens, rows, device="cuda")
+    xd = x.cuda()
+    m.q4().gemv(tokens, xd.data_ptr(), K, y.data_ptr(), rows, D.FP32, stream=stream())
+    xs = x.double().numpy()
+    top = np.abs(xs).reshape(tokens, -1, 128).max(2).repeat(128, 1)
+    ref, mag = xs @ m.values.T, np.abs(xs) @ np.abs(m.values).T
+    bound = sum_bound(K) * mag + (top * 2.0 ** -30) @ np.abs(m.values).T
+    assert (np.abs(y.cpu().double().numpy() - ref) <= bound).all()
+
+
+def test_a_row_of_zero_weights_gives_zero():
+    t = torch()
+    m = Matrix(48, 1024, 64, D.BF16, False, seed=2)
+    codes = np.full((48, 1024), 8, np.uint8)
+    codes[5, 77] = 9
+    m.codes = t.from_numpy(D.pack_codes(codes)).cuda()
+    for tokens in (1, 4, 7):
+        x = (t.randn(tokens, 1024, generator=t.Generator().manual_seed(3)) + 3).bfloat16().cuda()
+        y = t.empty(tokens, 48, device="cuda")
+        m.q4().gemv(tokens, x.data_ptr(), 1024, y.data_ptr(), 48, D.FP32, stream=stream())
+        assert (y[:, [r for r in range(48) if r != 5]] == 0).all() and (y[:, 5] != 0).all()
+
+
+def test_check_reports_no_wait_that_gave_up():
+    assert D.exo_decode_check() == B.OK
 
 
 def test_gemv_on_a_side_stream_and_in_a_graph_gives_the_same_bits():
