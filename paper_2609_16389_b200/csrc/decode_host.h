@@ -50,13 +50,33 @@ inline bool q4_aligned(const void* codes, const void* scales, const void* zeros,
   return ((uintptr_t)codes & 15u) == 0 && (uintptr_t)scales % (unsigned)(256 / group) == 0 && (uintptr_t)zeros % (unsigned)(128 / group) == 0;
 }
 
+// Opts a kernel in to kMostSmem, once per device: always to the same size, so that threads which launch one kernel at different
+// sizes cannot take it from each other.
+inline cudaError_t allow_smem(void* fn) {
+  constexpr int kSlots = 512;
+  static std::atomic<void*> done[8][kSlots];   // the kernels that have it, by hash of their address
+  int device = 0;
+  cudaError_t e = cudaGetDevice(&device);
+  if (e != cudaSuccess) return e;
+  std::atomic<void*>* slot = nullptr;
+  if (device < 8) {
+    for (int i = 0; i < 4; ++i) {
+      std::atomic<void*>& s = done[device][(((uintptr_t)fn >> 4) * 0x9e3779b1u + (unsigned)i) % kSlots];
+      void* have = s.load(std::memory_order_relaxed);
+      if (have == fn) return cudaSuccess;
+      if (!have && !slot) slot = &s;
+    }
+  }
+  e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostSmem);
+  if (e == cudaSuccess && slot) slot->store(fn, std::memory_order_relaxed);
+  return e;
+}
+
 // One launch with programmatic dependent launch and, for cluster > 1, clusters of that many CTAs along x.
 inline exo_gemm_status_t launch(void* fn, unsigned grid_x, unsigned grid_y, unsigned threads, size_t smem, unsigned cluster,
                                 cudaStream_t stream, void* params, void* params2 = nullptr, void* params3 = nullptr) {
   cudaError_t e;
-  // always the same opt-in, so that threads which launch one kernel at different sizes cannot take it from each other
-  if (smem > 48 * 1024 && (e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostSmem)) != cudaSuccess)
-    return cuda_failed(e);
+  if (smem > 48 * 1024 && (e = allow_smem(fn)) != cudaSuccess) return cuda_failed(e);
   cudaLaunchConfig_t lc{};
   lc.gridDim = dim3(grid_x, grid_y, 1);
   lc.blockDim = dim3(threads, 1, 1);

@@ -15,9 +15,10 @@ namespace {
 // ==== quantisation ===============================================================================================
 // A lane holds eight consecutive weights, so a group is 16, 8 or 4 neighbouring lanes and its extremes are a shuffle
 // tree; a warp walks along a row, 256 weights at a time.  Memory is the bound (2 or 4 bytes in and 1/2 out per weight) only
-// if a weight costs about a dozen instructions: a division takes that many alone.  So w / scale is w times the rounded
-// reciprocal, off by less than 2^-18 for quotients up to 16, which rounds to the same integer unless it lies that near the
-// middle of two; lanes that see such a weight divide.
+// if a weight costs about a dozen instructions: a division takes that many alone.  A group divides by one scale, so the
+// quotient is the product with the scale's reciprocal, corrected once by its remainder: with fused operations and a
+// correctly rounded reciprocal that is the correctly rounded quotient (P. Markstein, 1990), as the formula has it, wherever
+// nothing under- or overflows.
 constexpr int kQuantThreads = 256;
 constexpr int kQuantSegment = 4096;   // weights of a row per warp
 
@@ -122,6 +123,9 @@ __global__ void __launch_bounds__(kQuantThreads) exo_q4_quantize_kernel(const Qu
   const int k_end = min((seg + 1) * (kQuantSegment / 128), p.blocks) * 128;
   const char* src = static_cast<const char*>(p.w) + row * p.ldw * BYTES;
   const int lanes = p.group / 8, per_row = p.blocks * 128 / p.group, group_log = 31 - __clz(p.group);
+  uint32_t* codes = p.codes + row * p.blocks * 16;
+  uint16_t* scales = p.scales + row * per_row;
+  uint8_t* zeros = p.zeros ? p.zeros + row * per_row : nullptr;
   auto weights = [&](const uint32_t (&w)[2 * BYTES], float (&v)[8]) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -140,46 +144,44 @@ __global__ void __launch_bounds__(kQuantThreads) exo_q4_quantize_kernel(const Qu
 #pragma unroll
     for (int i = 0; i < 8; ++i) { lo = fminf(lo, v[i]); hi = fmaxf(hi, v[i]); }
     if (!p.zeros) hi = fmaxf(hi, -lo);
-    for (int o = 1; o < lanes; o <<= 1) {
-      hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-      if (p.zeros) lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+#pragma unroll
+    for (int o = 1; o < 16; o <<= 1) {
+      if (o < lanes) {
+        hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+        if (p.zeros) lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+      }
     }
     const float raw = p.zeros ? divided<15>(hi - lo) : divided<7>(hi);
     const uint16_t s16 = T::from_float(fminf(raw, T::max_finite()));
     const float s = T::to_float(s16);
-    float inverse;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inverse) : "f"(s));
-    if (s == 0.f) inverse = 0.f;
-    bool near = !(inverse <= 3.0e38f) || raw > T::max_finite();   // no reciprocal, or quotients beyond 16
-    float zero = 8.f;
-    if (p.zeros && s > 0.f) {
-      const float y = -lo * inverse;
-      zero = rintf(y);
-      if (near || fabsf(y - zero) > 0.49998f) zero = rintf(__fdiv_rn(-lo, s));
-      zero = fminf(fmaxf(zero, 0.f), 15.f);
-    }
+    // scales whose quotients are beyond 16, or whose remainders may underflow, or none at all
+    const bool plain = s > 1.0e-30f && raw <= T::max_finite();
+    const float inverse = __frcp_rn(plain ? s : 1.f);
+    auto quotient = [&](float v) {
+      const float y = v * inverse;
+      return fmaf(fmaf(-y, s, v), inverse, y);
+    };
+    int zero = 8;
+    if (p.zeros && s > 0.f) zero = (int)fminf(fmaxf(rintf(plain ? quotient(-lo) : __fdiv_rn(-lo, s)), 0.f), 15.f);
     uint32_t word = 0;
-    const float magic = 12582912.f + zero;      // 1.5 * 2^23: the sum's last bits are the rounded quotient plus zero
+    if (plain) {
+      const int base = 0x4b400000 - zero;       // 1.5 * 2^23 + v has the rounded v in its last bits
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float y = v[i] * inverse, m = y + magic;
-      near |= fabsf(y - (m - magic)) > 0.49998f;
-      word += (uint32_t)__vimin_s32_relu(__float_as_int(m) - 0x4b400000, 15) << (4 * (i / 2 + 4 * (i % 2)));
-    }
-    if (near) {
-      word = 0;
+      for (int i = 0; i < 8; ++i)
+        word += (uint32_t)__vimin_s32_relu(__float_as_int(quotient(v[i]) + 12582912.f) - base, 15) << (4 * (i / 2 + 4 * (i % 2)));
+    } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float q = rintf(__fdiv_rn(v[i], s)) + zero;   // without zero points: -8 .. 7 plus 8
+        const float q = s > 0.f ? rintf(__fdiv_rn(v[i], s)) + (float)zero : (float)zero;   // without zero points: -8 .. 7 plus 8
         word |= (uint32_t)fminf(fmaxf(q, 0.f), 15.f) << (4 * (i / 2 + 4 * (i % 2)));
       }
     }
     if (k < k_end) {   // the last pass may hold one block of 128 only
       const int l = lane & 15;
-      p.codes[(row * p.blocks + k / 128) * 16 + 4 * (l & 3) + (l >> 2)] = word;
+      codes[k / 128 * 16 + 4 * (l & 3) + (l >> 2)] = word;
       if ((lane & (lanes - 1)) == 0) {
-        p.scales[row * per_row + (k >> group_log)] = s16;
-        if (p.zeros) p.zeros[row * per_row + (k >> group_log)] = (uint8_t)zero;
+        scales[k >> group_log] = s16;
+        if (p.zeros) zeros[k >> group_log] = (uint8_t)zero;
       }
     }
   }
@@ -374,8 +376,9 @@ __global__ void __launch_bounds__(kGemvThreads, NT <= 4 ? 2 : 1) exo_gemv_q4_ker
 // otherwise.  A group's sum of (code - zero) * digit is an exact integer; it comes out as the float 1.5 * 2^23 + sum, since
 // the accumulator starts with that float's bits less zero * (sum of digits).  From there on everything is fp32.
 //
-// Weights come through shared memory: each warp keeps a ring of pieces (`piece` steps of 16 rows) filled with tiled copies
-// that it issues itself.  A lane's parts of a step are 16 bytes of rows g and g + 8.
+// Weights come through shared memory: each warp keeps a ring of pieces (`piece` steps of 16 rows) that it fills itself, large
+// matrices by tiled copies, small ones by 16-byte copies of every lane, which need no tensor map: making one takes the host
+// about 2 us, and a small product is over in 4.  A lane's parts of a step are 16 bytes of rows g and g + 8.
 constexpr int kFewWarps = 8, kFewThreads = 32 * kFewWarps;
 constexpr int kMagic = 0x4b400000;        // 1.5 * 2^23
 
@@ -383,6 +386,7 @@ struct FewParams {
   GemvParams g;
   int nk_log;       // parts of a tile's steps: 1 << nk_log
   int piece, stages;
+  bool tiled;       // pieces by tiled copies
   int digits_at, start_at, step_scale_at, ring_at;   // offsets in shared memory; the sums come first, the barriers before them
 };
 
@@ -398,21 +402,25 @@ __device__ __forceinline__ void transpose4(const uint32_t (&v)[4], uint32_t (&d)
   d[2] = __byte_perm(y0, y1, 0x5410); d[3] = __byte_perm(y0, y1, 0x7632);
 }
 
+// 16 bytes to shared memory, asynchronously; zeros where there is nothing to read.
+__device__ __forceinline__ void copy16(uint32_t to, const void* from, bool there) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(there ? 16 : 0) : "memory");
+}
 __device__ __forceinline__ int rank_part(int blocks, int r, int S) { return (int)((int64_t)blocks * r / S); }
 
-// What the values of a token that are not finite give a row over steps s0 .. s1 - 1; they count as 0 in the integers.
+// What the values of a token that are not finite give a row over steps s0 .. s1 - 1 (they count as 0 in the integers).  codes,
+// scales and zeros are the row's, x the token's.
 template <class T>
-__device__ __noinline__ float not_finite_part(const GemvParams& p, int per, int token, int64_t row, int s0, int s1) {
+__device__ __noinline__ float not_finite_part(const uint32_t* codes, const uint16_t* scales, const uint8_t* zeros, const uint16_t* x, int per, int K, int s0, int s1) {
   float v = 0.f;
-  if (row >= p.rows) return v;
-  for (int k = s0 * 128; k < min(s1 * 128, p.K); ++k) {
-    const float x = T::to_float(p.x[(int64_t)token * p.ldx + k]);
-    if (fabsf(x) <= 3.4028235e38f) continue;
+  for (int k = s0 * 128; k < min(s1 * 128, K); ++k) {
+    const float xk = T::to_float(x[k]);
+    if (fabsf(xk) <= 3.4028235e38f) continue;
     const int i = k & 7, n = i / 2 + 4 * (i & 1), j = k >> 5 & 3, t = k >> 3 & 3;
-    const uint32_t word = reinterpret_cast<const uint32_t*>(p.codes)[(row * p.blocks + k / 128) * 16 + 4 * t + j];
-    const int64_t group = (row * p.blocks + k / 128) * per + (k & 127) * per / 128;
-    const int zero = p.zeros ? p.zeros[group] : 8;
-    v += (float)((int)(word >> (4 * n) & 15u) - zero) * T::to_float(p.scales[group]) * x;
+    const uint32_t word = codes[k / 128 * 16 + 4 * t + j];
+    const int group = k / 128 * per + (k & 127) * per / 128;
+    const int zero = zeros ? zeros[group] : 8;
+    v += (float)((int)(word >> (4 * n) & 15u) - zero) * T::to_float(scales[group]) * xk;
   }
   return v;
 }
@@ -439,7 +447,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) exo_gemv_q4_few_kernel(const F
   const int col_pitch = k_steps * 128 + 16;
   const uint32_t bar = ptx::smem_u32(smem) + warp * 32, ring = ptx::smem_u32(smem + fp.ring_at) + warp * fp.stages * stage_bytes;
   if (lane == 0)
-    for (int i = 0; i < fp.stages; ++i) ptx::mbar_init(bar + 8 * i, 1);
+    for (int i = 0; i < fp.stages; ++i) ptx::mbar_init(bar + 8 * i, fp.tiled ? 1 : 32);
   ptx::fence_mbar_init();
   if (threadIdx.x == 0) strange = 0;
   __syncwarp();
@@ -452,9 +460,21 @@ __global__ void __launch_bounds__(kFewThreads, 2) exo_gemv_q4_few_kernel(const F
   ip = begin_of(iu);
   auto issue = [&]() {
     if (iu < units) {
-      if (lane == 0) {
+      const int row = row_of(iu), step = k_begin + ip * fp.piece;
+      if (!fp.tiled) {
+        const uint32_t to = ring + islot * stage_bytes + g * 64 + t * 16;
+        const int left = min(fp.piece, k_begin + k_steps - step);
+        const bool has0 = row + g < p.rows, has1 = row + g + 8 < p.rows;
+        const uint8_t* from0 = p.codes + ((has0 ? (int64_t)row + g : 0) * p.blocks + step) * 64 + 16 * t;
+        const uint8_t* from1 = p.codes + ((has1 ? (int64_t)row + g + 8 : 0) * p.blocks + step) * 64 + 16 * t;
+        for (int u = 0; u < left; ++u) {
+          copy16(to + u * 1024, from0 + u * 64, has0);
+          copy16(to + u * 1024 + 512, from1 + u * 64, has1);
+        }
+        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar + 8 * islot) : "memory");
+      } else if (lane == 0) {
         ptx::mbar_arrive_expect_tx(bar + 8 * islot, stage_bytes);
-        ptx::tma_load_3d(ring + islot * stage_bytes, &map, 0, row_of(iu), k_begin + ip * fp.piece, bar + 8 * islot);
+        ptx::tma_load_3d(ring + islot * stage_bytes, &map, 0, row, step, bar + 8 * islot);
       }
       islot = islot + 1 == fp.stages ? 0 : islot + 1;
       if (++ip == end_of(iu)) {
@@ -661,7 +681,11 @@ __global__ void __launch_bounds__(kFewThreads, 2) exo_gemv_q4_few_kernel(const F
     for (int r = 0; r < S; ++r) {
       const float* from = (S > 1 ? cluster.map_shared_rank(sums, r) : sums) + (tile << fp.nk_log) * p.tokens * 16 + at;
       for (int j = 0; j < nk; ++j) v += from[j * p.tokens * 16];
-      if ((S > 1 ? *cluster.map_shared_rank(&strange, r) : strange) >> token & 1) v += not_finite_part<T>(p, PER, token, row, rank_part(p.blocks, r, S), rank_part(p.blocks, r + 1, S));
+      if (((S > 1 ? *cluster.map_shared_rank(&strange, r) : strange) >> token & 1) && row < p.rows) {
+        const int64_t at = (int64_t)row * p.blocks;
+        v += not_finite_part<T>(reinterpret_cast<const uint32_t*>(p.codes) + at * 16, p.scales + at * PER, ZEROS ? p.zeros + at * PER : nullptr,
+                                p.x + (int64_t)token * p.ldx, PER, p.K, rank_part(p.blocks, r, S), rank_part(p.blocks, r + 1, S));
+      }
     }
     store_y<T>(p, token, row, v);
   }
@@ -720,6 +744,7 @@ bool plan_few(FewParams& fp, const GemvParams& p, int per, int sms, unsigned* ct
   const int slice = (p.blocks + S - 1) / S, least = p.blocks / S;
   const int64_t slots = (int64_t)(large ? 1 : 2) * sms / S, clusters = tiles < slots ? tiles : slots;
   const int most = (int)((tiles + clusters - 1) / clusters);     // tiles of a cluster
+  fp.tiled = large;
   fp.piece = large ? 8 : 4;
   // parts of k: two pieces each, or fewer where the CTA would otherwise have less than a part for every warp
   fp.nk_log = 0;
@@ -850,7 +875,7 @@ extern "C" exo_gemm_status_t exo_gemv_q4_run(const exo_q4_t* W, int64_t tokens, 
     unsigned ctas = 0, cluster = 1;
     if (plan_few(fp, p, 128 / W->group, sms, &ctas, &cluster, &smem)) {
       CUtensorMap map;
-      if (!exo::encode_steps_map(&map, p.codes, (uint64_t)p.rows, (uint64_t)p.blocks, (uint32_t)fp.piece)) return EXO_GEMM_ERR_CUDA;
+      if (fp.tiled && !exo::encode_steps_map(&map, p.codes, (uint64_t)p.rows, (uint64_t)p.blocks, (uint32_t)fp.piece)) return EXO_GEMM_ERR_CUDA;
       FewFn fn = bf16 ? pick_few<Bf16>(W->group, W->zeros, p.tokens) : pick_few<Fp16>(W->group, W->zeros, p.tokens);
       return launch((void*)fn, ctas, 1, kFewThreads, smem, cluster, (cudaStream_t)cuda_stream, &fp, &map);
     }

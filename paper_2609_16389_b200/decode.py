@@ -133,21 +133,24 @@ class Q4:
 
     def __init__(self, rows: int, K: int, group: int, dtype: int, codes: int, scales: int, zeros: int = 0):
         self.struct = Q4Struct(rows, K, group, dtype, codes, scales, zeros)
+        # the methods are what a decode loop calls: entry points and the struct's address are looked up once
+        L = lib()
+        self._calls, self._at = (L.exo_q4_quantize, L.exo_q4_dequantize, L.exo_gemv_q4_run), ctypes.byref(self.struct)
 
     def quantize(self, w_ptr: int, ldw: int, w_dtype: int, stream: int = 0):
-        st = exo_q4_quantize(self.struct, w_ptr, ldw, w_dtype, stream)
-        if st != OK:
+        st = self._calls[0](self._at, w_ptr, ldw, w_dtype, stream)
+        if st:
             raise ExoGemmError(st, "exo_q4_quantize")
 
     def dequantize(self, w_ptr: int, ldw: int, w_dtype: int, stream: int = 0):
-        st = exo_q4_dequantize(self.struct, w_ptr, ldw, w_dtype, stream)
-        if st != OK:
+        st = self._calls[1](self._at, w_ptr, ldw, w_dtype, stream)
+        if st:
             raise ExoGemmError(st, "exo_q4_dequantize")
 
     def gemv(self, tokens: int, x_ptr: int, ldx: int, y_ptr: int, ldy: int, y_dtype: int, alpha: float = 1.0,
              beta: float = 0.0, stream: int = 0):
-        st = exo_gemv_q4_run(self.struct, tokens, x_ptr, ldx, y_ptr, ldy, y_dtype, alpha, beta, stream)
-        if st != OK:
+        st = self._calls[2](self._at, tokens, x_ptr, ldx, y_ptr, ldy, y_dtype, alpha, beta, stream)
+        if st:
             raise ExoGemmError(st, "exo_gemv_q4_run")
 
 
@@ -159,12 +162,12 @@ class MoePlan:
         st, h = exo_moe_create(desc)
         if st != OK:
             raise ExoGemmError(st, "exo_moe_create")
-        self.handle, self.desc = h, desc
+        self.handle, self.desc, self._run = h, desc, lib().exo_moe_run
 
     def run(self, weights: MoeWeights, tokens: int, x_ptr: int, ldx: int, y_ptr: int, ldy: int, index_ptr: int = 0,
             weight_ptr: int = 0, stream: int = 0):
-        st = exo_moe_run(self.handle, weights, tokens, x_ptr, ldx, y_ptr, ldy, index_ptr, weight_ptr, stream)
-        if st != OK:
+        st = self._run(self.handle, weights, tokens, x_ptr, ldx, y_ptr, ldy, index_ptr, weight_ptr, stream)
+        if st:
             raise ExoGemmError(st, "exo_moe_run")
 
     def workspace_bytes(self) -> int:
