@@ -42,6 +42,7 @@ struct MoeParams {
   float* weight;            // may be NULL
   Stack gate, up, down;
   int tokens, hidden, inner, experts, shared, top_k;
+  int taken;                // the most experts this run can take
   bool renormalize, x_aligned;
   float routed_scale;
   // workspace
@@ -86,21 +87,21 @@ struct RouteTables {
 };
 
 template <int EPL>   // experts per lane
-__device__ __forceinline__ void route_tokens(const MoeParams& p, RouteTables& tb) {
+__device__ __forceinline__ void route_tokens(const MoeParams& p, const float* logits, RouteTables& tb) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int all = p.experts + p.shared;
   for (int e = threadIdx.x; e < all; e += kRouteThreads)
     tb.tokens_of[e] = e < p.experts ? 0ull : ~0ull >> (64 - p.tokens);
   __syncthreads();
   for (int token = warp; token < p.tokens; token += kRouteWarps) {
-    const float* l = p.logits + (int64_t)token * p.experts;
+    const float* l = logits + (int64_t)token * p.experts;
     float mine[EPL];
     uint32_t key[EPL];
 #pragma unroll
     for (int j = 0; j < EPL; ++j) {
       const int e = 32 * j + lane;
       key[j] = 0;
-      if (e < p.experts) { mine[j] = __ldcg(l + e); key[j] = key_of(mine[j]); }
+      if (e < p.experts) { mine[j] = l[e]; key[j] = key_of(mine[j]); }
     }
     int my_expert = 0;        // lane r keeps the r-th taken one
     float my_logit = 0.f, top = 0.f;
@@ -174,6 +175,87 @@ __device__ __forceinline__ void route_tokens(const MoeParams& p, RouteTables& tb
   }
 }
 
+__device__ __forceinline__ void route_all(const MoeParams& p, const float* logits, RouteTables& tb) {
+  if (p.experts <= 64) route_tokens<2>(p, logits, tb);
+  else if (p.experts <= 128) route_tokens<4>(p, logits, tb);
+  else route_tokens<16>(p, logits, tb);
+}
+
+// x in rows that start on 16-byte boundaries and end in zeros, for `up`
+__device__ __forceinline__ void copy_rows(const MoeParams& p) {
+  const int per = (int)(p.ldxs / 8);
+  for (int i = blockIdx.x * kRouteThreads + threadIdx.x; i < p.tokens * per; i += gridDim.x * kRouteThreads) {
+    const int token = i / per, e = i - token * per;
+    *reinterpret_cast<uint4*>(const_cast<uint16_t*>(p.xs) + token * p.ldxs + 8 * e) = load8_checked(p.x + token * p.ldx, 8 * e, p.hidden, p.x_aligned);
+  }
+}
+
+// The same for up to 8 tokens and 128 experts as one cluster of eight CTAs: a CTA has up to 16 of the experts, its warps cut k, and
+// the logits go straight into the first CTA's shared memory.  No memory fence, counter or second reading: 4.5 us
+// where the general form takes 7.7 (64 experts of 2048, one token).
+constexpr int kOneCtas = 8, kOneTokens = 8, kOneExperts = 16 * kOneCtas;
+
+template <class T, bool VEC>
+__global__ void __launch_bounds__(kRouteThreads) exo_moe_route_one_kernel(const MoeParams p) {
+  namespace cg = cooperative_groups;
+  __shared__ float4 red[kRouteWarps * 32];
+  __shared__ float logits[kOneTokens * kOneExperts];     // [token][expert], of the first CTA
+  __shared__ RouteTables tables;
+  cg::cluster_group cluster = cg::this_cluster();
+  const int r = (int)cluster.block_rank(), lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+  const int e0 = p.experts * r / kOneCtas, mine = p.experts * (r + 1) / kOneCtas - e0;
+  const uint16_t* r0 = p.router + (int64_t)min(e0 + min(g, mine - 1), p.experts - 1) * p.ld_router;
+  const uint16_t* r1 = p.router + (int64_t)min(e0 + min(g + 8, mine - 1), p.experts - 1) * p.ld_router;
+  ptx::grid_dependency_wait();
+  ptx::grid_launch_dependents();
+  if (mine > 0) {
+    if (mine <= 8) r1 = r0;
+    const uint16_t* x = p.x + (int64_t)min(g, p.tokens - 1) * p.ldx;
+    float acc[1][4];
+    clear(acc);
+    const int steps = (p.hidden + 31) / 32;
+    constexpr int N = 4;           // steps whose loads are in flight together
+    for (int s0 = warp; s0 < steps; s0 += N * kRouteWarps) {
+      uint4 wa[N], wb[N], b[N];
+#pragma unroll
+      for (int u = 0; u < N; ++u) {
+        const int k = (s0 + u * kRouteWarps) * 32 + 8 * t;
+        if (VEC && p.x_aligned && k + 8 <= p.hidden) {
+          wa[u] = ldg_weights(r0 + k);
+          wb[u] = ldg_weights(r1 + k);
+          b[u] = *reinterpret_cast<const uint4*>(x + k);
+        } else {
+          wa[u] = load8_checked(r0, k, p.hidden, VEC);
+          wb[u] = load8_checked(r1, k, p.hidden, VEC);
+          b[u] = load8_checked(x, k, p.hidden, p.x_aligned);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < N; ++u) {
+        T::mma(acc[0], wa[u].x, wb[u].x, wa[u].y, wb[u].y, b[u].x, b[u].y);
+        T::mma(acc[0], wa[u].z, wb[u].z, wa[u].w, wb[u].w, b[u].z, b[u].w);
+      }
+    }
+    red[warp * 32 + lane] = make_float4(acc[0][0], acc[0][1], acc[0][2], acc[0][3]);
+  }
+  if (p.copy_x) copy_rows(p);
+  cluster.sync();      // this CTA's sums are there, and the first CTA runs
+  if (warp == 0 && mine > 0) {
+    float4 v = red[lane];
+#pragma unroll
+    for (int q = 1; q < kRouteWarps; ++q) add(v, red[q * 32 + lane]);
+    float* to = cluster.map_shared_rank(logits, 0);
+    const float vals[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int token = 2 * t + (q & 1), e = g + 8 * (q >> 1);
+      if (token < p.tokens && e < mine) to[token * p.experts + e0 + e] = vals[q];
+    }
+  }
+  cluster.sync();
+  if (r == 0) route_all(p, logits, tables);
+}
+
 template <class T, bool VEC, int NT>
 __global__ void __launch_bounds__(kRouteThreads) exo_moe_route_kernel(const MoeParams p) {
   namespace cg = cooperative_groups;
@@ -190,13 +272,7 @@ __global__ void __launch_bounds__(kRouteThreads) exo_moe_route_kernel(const MoeP
   f.r1 = p.router + (int64_t)min(e0 + g + 8, p.experts - 1) * p.ld_router;
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();
-  if (p.copy_x) {   // for `up`
-    const int per = (int)(p.ldxs / 8);
-    for (int i = blockIdx.x * kRouteThreads + threadIdx.x; i < p.tokens * per; i += gridDim.x * kRouteThreads) {
-      const int token = i / per, e = i - token * per;
-      *reinterpret_cast<uint4*>(const_cast<uint16_t*>(p.xs) + token * p.ldxs + 8 * e) = load8_checked(p.x + token * p.ldx, 8 * e, p.hidden, p.x_aligned);
-    }
-  }
+  if (p.copy_x) copy_rows(p);
   float acc[NT][4];
   clear(acc);
   const int steps = (p.hidden + 31) / 32, ds = S * kRouteWarps;
@@ -244,21 +320,19 @@ __global__ void __launch_bounds__(kRouteThreads) exo_moe_route_kernel(const MoeP
   }
   __syncthreads();
   if (!last) return;
-  if (p.experts <= 64) route_tokens<2>(p, tables);
-  else if (p.experts <= 128) route_tokens<4>(p, tables);
-  else route_tokens<16>(p, tables);
+  route_all(p, p.logits, tables);
 }
 
 // Inner activations from lane l's part of tile i: gate in v.x, v.y and up in v.z, v.w for two tokens.
 template <class T>
-__device__ __forceinline__ void store_inner(const MoeParams& p, const Active& a, int f0, int i, int l, const float4& v) {
+__device__ __forceinline__ void store_inner(const MoeParams& p, const float* weight, const Active& a, int f0, int i, int l, const float4& v) {
   const int n = 8 * i + 2 * (l & 3), col = f0 + (l >> 2);
   if (col >= p.inner) return;
   const float gate[2] = {v.x, v.y}, up[2] = {v.z, v.w};
 #pragma unroll
   for (int q = 0; q < 2; ++q)
     if (n + q < a.count) {
-      const float w = __ldcg(p.entry_weight + a.base + n + q);
+      const float w = weight[a.base + n + q];
       p.h[(int64_t)(a.base + n + q) * p.ldh + col] = T::from_float(w * (gate[q] / (1.f + expf(-gate[q])) * up[q]));
     }
 }
@@ -411,16 +485,32 @@ template <class T> struct PieceOf<T, 1> { using type = Piece16<T>; };
 // A CTA cuts its items into parts while it has fewer units than this: two turns of its warps, or one where the sums are large.
 __host__ __device__ constexpr int part_limit(int nt) { return nt <= 2 ? 2 * kMoeWarps : kMoeWarps; }
 
-// The routing tables, copied to shared memory.
+constexpr int kUnitsAhead = 4;
+
+// The routing tables, copied to shared memory (table_bytes() of it).  Every CTA reads the same few lines at the same time, so it
+// reads each of them once and no more than a run of this size can fill.
 struct Tables {
-  Active active[kMaxExperts + kMaxShared];
-  int token[kMaxTokens * (kMaxTopK + kMaxShared)];
-  int cost;                  // of a step of every taken expert
+  Active* active;
+  int* token;
+  float* weight;
 };
-__device__ __forceinline__ void copy_tables(Tables& tb, const MoeParams& p) {
-  const int all = p.experts + p.shared, entries = p.tokens * (p.top_k + p.shared);
-  for (int i = threadIdx.x; i < all; i += kMoeThreads) *reinterpret_cast<int4*>(&tb.active[i]) = __ldcg(reinterpret_cast<const int4*>(p.active) + i);
-  for (int i = threadIdx.x; i < entries; i += kMoeThreads) tb.token[i] = __ldcg(p.entry_token + i);
+__host__ __device__ inline int table_bytes(const MoeParams& p) {
+  return p.taken * (int)sizeof(Active) + p.tokens * (p.top_k + p.shared) * 8;
+}
+__device__ __forceinline__ Tables copy_tables(uint8_t* at, int& n_active, const MoeParams& p) {
+  const int entries = p.tokens * (p.top_k + p.shared);
+  Tables tb;
+  tb.active = reinterpret_cast<Active*>(at);
+  tb.token = reinterpret_cast<int*>(at + p.taken * sizeof(Active));
+  tb.weight = reinterpret_cast<float*>(tb.token + entries);
+  for (int i = threadIdx.x; i < p.taken; i += kMoeThreads) *reinterpret_cast<int4*>(&tb.active[i]) = __ldcg(reinterpret_cast<const int4*>(p.active) + i);
+  for (int i = (int)threadIdx.x - 32; i < entries; i += kMoeThreads)
+    if (i >= 0) tb.token[i] = __ldcg(p.entry_token + i);
+  for (int i = (int)threadIdx.x - 64; i < entries; i += kMoeThreads)
+    if (i >= 0) tb.weight[i] = __ldcg(p.entry_weight + i);
+  if (threadIdx.x == kMoeThreads - 1) n_active = __ldcg(p.n_active);
+  __syncthreads();
+  return tb;
 }
 
 // ==== up ==========================================================================================================
@@ -433,54 +523,69 @@ __global__ void __launch_bounds__(kMoeThreads, 2)
 exo_moe_up_ring_kernel(const MoeParams p, const __grid_constant__ CUtensorMap gate_map, const __grid_constant__ CUtensorMap up_map) {
   using P = typename PieceOf<T, FMT>::type;
   extern __shared__ __align__(128) uint8_t smem[];
-  __shared__ Tables tb;
+  __shared__ int active_shared, next_unit, ahead_of[kMoeWarps][kUnitsAhead];
   __shared__ __align__(8) uint8_t bars[kMoeWarps * kMoeStages * 8];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
   Ring ring;
   ring.begin(bars, smem, p.up_piece, warp, lane);
   float4* sums = reinterpret_cast<float4*>(smem + kMoeWarps * kMoeStages * ring.stage_bytes);   // [unit][tile][lane]
   const int tiles = (p.inner + 7) / 8, steps = (p.hidden + P::kStep - 1) / P::kStep, pieces = (steps + p.up_piece - 1) / p.up_piece;
+  if (threadIdx.x == 0) next_unit = kMoeWarps;
+  if (lane == 0) { ptx::prefetch_tensormap(&gate_map); ptx::prefetch_tensormap(&up_map); }
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();   // after the wait: `down` may then read the tables of `route` before it waits itself
-  const int items = __ldcg(p.n_active) * tiles;
-  copy_tables(tb, p);
-  __syncthreads();
+  const Tables tb = copy_tables(reinterpret_cast<uint8_t*>(sums + 2 * part_limit(NT) * NT * 32), active_shared, p);
+  const int n_active = active_shared;
+  const int items = n_active * tiles;
   const int mine = (int)blockIdx.x < items ? (items - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x : 0;
   int nk_log = 0;
   while (nk_log < 3 && (mine << nk_log) < part_limit(NT) && (2 << nk_log) <= pieces) ++nk_log;
   const int units = mine << nk_log, nk = 1 << nk_log;
   auto begin_of = [&](int u) { return (pieces * (u & (nk - 1))) >> nk_log; };
   auto end_of = [&](int u) { return (pieces * ((u & (nk - 1)) + 1)) >> nk_log; };
+  // items by expert, the last first: the shared experts, who have all tokens, are last
   auto item_of = [&](int u) { return (int)blockIdx.x + (u >> nk_log) * (int)gridDim.x; };
-
-  int iu = warp, ip = begin_of(iu), igate = 0, iup = 0;
+  auto expert_of = [&](int item) { return n_active - 1 - item / tiles; };
+  // A warp takes its first unit by its number and any other when its copies get there; the numbers of the units between the
+  // copies and the products (at most one per stage, the one that is open, and the end) wait in shared memory.
+  int* ahead = ahead_of[warp];
+  int iu = warp, ip = begin_of(warp), igate = 0, iup = 0, put = 1;
+  if (lane == 0) ahead[0] = warp;
   auto open = [&]() {
-    const int item = item_of(iu), at = item / tiles, f0 = (item - at * tiles) * 8;
-    igate = (int)(tb.active[at].expert * p.gate.expert_rows) + f0;
-    iup = (int)(tb.active[at].expert * p.up.expert_rows) + f0;
+    const int item = item_of(iu), f0 = item % tiles * 8, expert = tb.active[expert_of(item)].expert;
+    igate = (int)(expert * p.gate.expert_rows) + f0;
+    iup = (int)(expert * p.up.expert_rows) + f0;
   };
   auto issue = [&]() {
     if (iu < units) {
       if (lane == 0) ring.copy(&gate_map, igate, &up_map, iup, ip * p.up_piece * P::kWords);
       ring.copied();
       if (++ip == end_of(iu)) {
-        iu += kMoeWarps;
-        ip = begin_of(iu);
-        if (iu < units) open();
+        if (lane == 0) {
+          iu = atomicAdd(&next_unit, 1);
+          ahead[put % kUnitsAhead] = iu;
+        }
+        iu = __shfl_sync(0xffffffffu, iu, 0);
+        ++put;
+        if (iu < units) {
+          ip = begin_of(iu);
+          open();
+        }
       }
     }
   };
   if (iu < units) open();
   for (int i = 0; i < kMoeStages; ++i) issue();
+  __syncwarp();
 
   // the lane's row of activations for tile i of an item's tokens; columns without a token repeat the last one's
   auto row_of = [&](const Active& a, int i) { return p.xs + (int64_t)tb.token[a.base + min(8 * i + g, a.count - 1)] * p.ldxs + 8 * t; };
   auto steps_at = [&](int c) { return min(p.up_piece, steps - c * p.up_piece); };
   P piece;
-  if (warp < units) piece.first(row_of(tb.active[item_of(warp) / tiles], 0) + begin_of(warp) * p.up_piece * P::kStep, steps_at(begin_of(warp)));
-  for (int u = warp; u < units; u += kMoeWarps) {
-    const int item = item_of(u), at = item / tiles, f0 = (item - at * tiles) * 8;
-    const Active a = tb.active[at];
+  if (warp < units) piece.first(row_of(tb.active[expert_of(item_of(warp))], 0) + begin_of(warp) * p.up_piece * P::kStep, steps_at(begin_of(warp)));
+  for (int u = warp, took = 1; u < units; ++took) {
+    const int item = item_of(u), f0 = item % tiles * 8;
+    const Active a = tb.active[expert_of(item)];
     const int nt = (a.count + 7) / 8;
     const int64_t row = min(f0 + g, p.inner - 1);
     piece.rows(p.gate, a.expert * p.gate.expert_rows + row, p.up, a.expert * p.up.expert_rows + row);
@@ -490,40 +595,45 @@ exo_moe_up_ring_kernel(const MoeParams p, const __grid_constant__ CUtensorMap ga
     float acc[NT][4];
     clear(acc);
     const int end = end_of(u);
+    int after = units;                 // the unit after this one
     for (int c = begin_of(u); c < end; ++c) {
       const int s = c * p.up_piece, n = steps_at(c);
       const uint16_t* next = xrow[0] + (s + p.up_piece) * P::kStep;
       int n_next = c + 1 < end ? steps_at(c + 1) : 0;
-      if (c + 1 == end && u + kMoeWarps < units) {
-        const int v = u + kMoeWarps;
-        next = row_of(tb.active[item_of(v) / tiles], 0) + begin_of(v) * p.up_piece * P::kStep;
-        n_next = steps_at(begin_of(v));
+      if (c + 1 == end) {
+        after = ahead[took % kUnitsAhead];   // its copies have begun, or there is none
+        if (after < units) {
+          next = row_of(tb.active[expert_of(item_of(after))], 0) + begin_of(after) * p.up_piece * P::kStep;
+          n_next = steps_at(begin_of(after));
+        }
       }
       const uint32_t w = ring.wait() + g * ring.pitch + 16 * t;
       piece.template multiply<NT>(w, ring.pitch, s, n, [&](int i) { return xrow[i] + s * P::kStep; }, next, n_next, nt, acc);
       __syncwarp();
       ring.taken();
       issue();
+      __syncwarp();
     }
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
       if (i < nt) {
         const float4 v = make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
-        if (nk_log == 0) store_inner<T>(p, a, f0, i, lane, v);
+        if (nk_log == 0) store_inner<T>(p, tb.weight, a, f0, i, lane, v);
         else sums[(u * NT + i) * 32 + lane] = v;
       }
     }
+    u = after;
   }
   if (nk_log > 0) {
     __syncthreads();
     for (int idx = threadIdx.x; idx < mine * NT * 32; idx += kMoeThreads) {
       const int k = idx / (NT * 32), i = (idx >> 5) % NT;
-      const int item = (int)blockIdx.x + k * (int)gridDim.x, at = item / tiles;
-      const Active a = tb.active[at];
+      const int item = (int)blockIdx.x + k * (int)gridDim.x;
+      const Active a = tb.active[expert_of(item)];
       if (8 * i >= a.count) continue;
       float4 v = sums[((k << nk_log) * NT + i) * 32 + (idx & 31)];
       for (int q = 1; q < nk; ++q) add(v, sums[(((k << nk_log) + q) * NT + i) * 32 + (idx & 31)]);
-      store_inner<T>(p, a, (item - at * tiles) * 8, i, idx & 31, v);
+      store_inner<T>(p, tb.weight, a, (item % tiles) * 8, i, idx & 31, v);
     }
   }
 }
@@ -538,7 +648,7 @@ exo_moe_down_ring_kernel(const MoeParams p, const __grid_constant__ CUtensorMap 
   namespace cg = cooperative_groups;
   using P = typename PieceOf<T, FMT>::type;
   extern __shared__ __align__(128) uint8_t smem[];
-  __shared__ Tables tb;
+  __shared__ int all_costs, active_shared;
   __shared__ __align__(8) uint8_t bars[kMoeWarps * kMoeStages * 8];
   cg::cluster_group cluster = cg::this_cluster();
   const int S = (int)cluster.num_blocks(), r = (int)cluster.block_rank();
@@ -549,11 +659,11 @@ exo_moe_down_ring_kernel(const MoeParams p, const __grid_constant__ CUtensorMap 
   float* sums = reinterpret_cast<float*>(smem + kMoeWarps * kMoeStages * ring.stage_bytes);   // [warp][token][row]
   float* part = sums + kMoeWarps * p.tokens * 16;             // [token][row]
   const int steps = (p.inner + P::kStep - 1) / P::kStep;
+  if (lane == 0) ptx::prefetch_tensormap(&map);
   // `route` is complete: `up` started this kernel after it had waited for that
-  const int n_active = __ldcg(p.n_active);
-  copy_tables(tb, p);
   for (int i = threadIdx.x; i < kMoeWarps * p.tokens * 16; i += kMoeThreads) sums[i] = 0.f;
-  __syncthreads();
+  const Tables tb = copy_tables(reinterpret_cast<uint8_t*>(part + p.tokens * 16), active_shared, p);
+  const int n_active = active_shared;
   // A step costs a warp its weights and then its tiles of tokens: three parts and two for every tile.  Equal shares of that.
   auto cost_of = [&](int at) { return 3 + 2 * ((tb.active[at].count + 7) / 8); };
   if (warp == 0) {
@@ -569,10 +679,10 @@ exo_moe_down_ring_kernel(const MoeParams p, const __grid_constant__ CUtensorMap 
       if (e0 + lane < n_active) tb.active[e0 + lane].cost_before = before + sum - own;
       before += __shfl_sync(0xffffffffu, sum, 31);
     }
-    if (lane == 0) tb.cost = before;
+    if (lane == 0) all_costs = before;
   }
   __syncthreads();
-  const int64_t total = (int64_t)tb.cost * steps;
+  const int64_t total = (int64_t)all_costs * steps;
   const int64_t workers = (int64_t)S * kMoeWarps, q = r * kMoeWarps + warp;
   auto place = [&](int64_t cost, int& at, int& s) {   // the step that begins at or after this point
     int lo = 0, hi = n_active;                        // the last expert that begins at or before it
@@ -721,7 +831,7 @@ __global__ void __launch_bounds__(kPlainThreads) exo_moe_up_plain_kernel(const M
   for (int idx = threadIdx.x; idx < nt * 32; idx += kPlainThreads) {
     float4 v = red[idx];
     for (int q = 1; q < kPlainWarps; ++q) add(v, red[q * nt * 32 + idx]);
-    store_inner<T>(p, a, f0, idx >> 5, idx & 31, v);
+    store_inner<T>(p, p.entry_weight, a, f0, idx >> 5, idx & 31, v);
   }
 }
 
@@ -945,6 +1055,7 @@ exo_gemm_status_t exo_moe_run(exo_moe_handle_t plan, const exo_moe_weights_t* w,
   p.down = stack_of(w->down, d.hidden, d.inner);
   p.tokens = (int)tokens; p.hidden = (int)d.hidden; p.inner = (int)d.inner;
   p.experts = d.experts; p.shared = d.shared; p.top_k = d.top_k;
+  p.taken = (int)((int64_t)p.tokens * p.top_k < p.experts ? (int64_t)p.tokens * p.top_k : p.experts) + p.shared;
   p.renormalize = d.renormalize != 0; p.routed_scale = d.routed_scale;
   p.x_aligned = rows_aligned(x, ldx);
   p.arrivals = (unsigned*)plan->ws;
@@ -969,50 +1080,55 @@ exo_gemm_status_t exo_moe_run(exo_moe_handle_t plan, const exo_moe_weights_t* w,
   const int nt = (p.tokens + 7) / 8;
   const cudaStream_t stream = (cudaStream_t)cuda_stream;
 
-  // route: 16 experts per cluster; a warp keeps a step of 32
-  int S = 1;
-  const int steps = (p.hidden + 31) / 32;
-  while (S < 8 && steps >= 2 * S * kRouteWarps) S *= 2;
   const bool router_aligned = rows_aligned(w->router, w->ld_router);
-  void* fn = bf16 ? (router_aligned ? pick_route<Bf16, true>(nt) : pick_route<Bf16, false>(nt))
-                  : (router_aligned ? pick_route<Fp16, true>(nt) : pick_route<Fp16, false>(nt));
-  st = launch(fn, (unsigned)((p.experts + 15) / 16 * S), 1, kRouteThreads, (size_t)(kRouteWarps + 1) * nt * 512, (unsigned)S, stream, &p);
+  int S = 1;
+  void* fn;
+  if (p.tokens <= kOneTokens && p.experts <= kOneExperts && (int64_t)p.experts * p.hidden <= 1 << 20) {   // at most 256 KB of the router to a CTA
+    fn = bf16 ? (router_aligned ? (void*)exo_moe_route_one_kernel<Bf16, true> : (void*)exo_moe_route_one_kernel<Bf16, false>)
+              : (router_aligned ? (void*)exo_moe_route_one_kernel<Fp16, true> : (void*)exo_moe_route_one_kernel<Fp16, false>);
+    st = launch(fn, kOneCtas, 1, kRouteThreads, 0, kOneCtas, stream, &p);
+  } else {   // 16 experts per cluster; a warp keeps a step of 32
+    const int steps = (p.hidden + 31) / 32;
+    while (S < 8 && steps >= 2 * S * kRouteWarps) S *= 2;
+    fn = bf16 ? (router_aligned ? pick_route<Bf16, true>(nt) : pick_route<Bf16, false>(nt))
+              : (router_aligned ? pick_route<Fp16, true>(nt) : pick_route<Fp16, false>(nt));
+    st = launch(fn, (unsigned)((p.experts + 15) / 16 * S), 1, kRouteThreads, (size_t)(kRouteWarps + 1) * nt * 512, (unsigned)S, stream, &p);
+  }
   if (st != EXO_GEMM_OK) return st;
 
   const int q4_fmt = d.q4_group == 128 ? 2 : d.q4_group == 64 ? 3 : 4, step = q4 ? 128 : 32, nt_kernel = nt <= 2 ? nt : 8;
   const int64_t all = d.experts + d.shared;
-  const int64_t most = (int64_t)p.tokens * p.top_k < p.experts ? (int64_t)p.tokens * p.top_k : p.experts;
-  const int taken = (int)most + p.shared;   // the most experts this run can take
   const int up_fmt = q4 ? q4_fmt : rows_aligned(w->gate.w, w->gate.ld) && rows_aligned(w->up.w, w->up.ld) ? 1 : 0;
   fn = bf16 ? pick_up<Bf16>(up_fmt, nt) : pick_up<Fp16>(up_fmt, nt);
   if (up_fmt == 0) {
-    st = launch(fn, (unsigned)((p.inner + 7) / 8), (unsigned)taken, kPlainThreads, 0, 1, stream, &p);
+    st = launch(fn, (unsigned)((p.inner + 7) / 8), (unsigned)p.taken, kPlainThreads, 0, 1, stream, &p);
   } else {
     CUtensorMap gate, up;
     if (!stack_map(&gate, p.gate, all, q4, p.up_piece, 8) || !stack_map(&up, p.up, all, q4, p.up_piece, 8)) return EXO_GEMM_ERR_CUDA;
-    const size_t smem = (size_t)kMoeWarps * kMoeStages * p.up_piece * 1024 + (size_t)2 * part_limit(nt_kernel) * nt_kernel * 512;
-    const int64_t items = (int64_t)taken * ((p.inner + 7) / 8), slots = (int64_t)(many ? 1 : 2) * plan->sms;
+    const size_t smem = (size_t)kMoeWarps * kMoeStages * p.up_piece * 1024 + (size_t)2 * part_limit(nt_kernel) * nt_kernel * 512 + table_bytes(p);
+    const int64_t items = (int64_t)p.taken * ((p.inner + 7) / 8), slots = (int64_t)(many ? 1 : 2) * plan->sms;
     st = launch(fn, (unsigned)(items < slots ? items : slots), 1, kMoeThreads, smem, 1, stream, &p, &gate, &up);
   }
   if (st != EXO_GEMM_OK) return st;
 
   const int down_fmt = q4 ? q4_fmt : rows_aligned(w->down.w, w->down.ld) ? 1 : 0;
-  const int64_t tiles = (p.hidden + 15) / 16, all_steps = (int64_t)taken * ((p.inner + step - 1) / step);
+  const int64_t tiles = (p.hidden + 15) / 16, all_steps = (int64_t)p.taken * ((p.inner + step - 1) / step);
   fn = bf16 ? pick_down<Bf16>(down_fmt, nt) : pick_down<Fp16>(down_fmt, nt);
   if (down_fmt == 0)
     return launch(fn, (unsigned)tiles, 1, kPlainThreads, (size_t)kPlainWarps * p.tokens * 64, 1, stream, &p);
   CUtensorMap down;
   if (!stack_map(&down, p.down, all, q4, p.down_piece, 16)) return EXO_GEMM_ERR_CUDA;
-  // The cluster size with the shortest estimate: every turn of two CTAs per SM costs about 3 us and its weights at an SM's
-  // share of the bandwidth, 22 GB/s for each of the two.
+  // The cluster size with the shortest estimate: a turn of the CTAs that fit costs their start and end (4 us, and more for
+  // the sums of many tokens) and the weights at an SM's share of the bandwidth, 44 GB/s.
+  const size_t smem = (size_t)kMoeWarps * kMoeStages * p.down_piece * 1024 + (size_t)(kMoeWarps + 1) * p.tokens * 64 + table_bytes(p);
+  const int fit = smem <= 110 * 1024 ? 2 : 1;
   S = 1;
   double best = 0.0;
   for (int c = 1; c <= 8 && (c == 1 || all_steps >= (int64_t)c * kMoeWarps); c *= 2) {
-    const double us = (double)((tiles * c + 2 * plan->sms - 1) / (2 * plan->sms)) * (3.0 + (double)all_steps * 1024.0 / c / 22e3);
+    const double us = (double)((tiles * c + fit * plan->sms - 1) / (fit * plan->sms)) * (4.0 + 0.1 * p.tokens + (double)all_steps * 1024.0 / c / (44e3 / fit));
     if (c == 1 || us < best) { best = us; S = c; }
   }
-  return launch(fn, (unsigned)(tiles * S), 1, kMoeThreads,
-                (size_t)kMoeWarps * kMoeStages * p.down_piece * 1024 + (size_t)(kMoeWarps + 1) * p.tokens * 64, (unsigned)S, stream, &p, &down);
+  return launch(fn, (unsigned)(tiles * S), 1, kMoeThreads, smem, (unsigned)S, stream, &p, &down);
 }
 
 int64_t exo_moe_workspace_bytes(exo_moe_handle_t plan) { return plan ? plan->bytes : 0; }
