@@ -18,7 +18,7 @@ bool encode_rows_map(CUtensorMap* map, int word_bytes, const void* base, uint64_
 
 namespace decode {
 
-constexpr int kMostSmem = 200 * 1024;   // dynamic shared memory a launch may ask for
+constexpr int kMostSmem = 220 * 1024;   // dynamic shared memory a launch may ask for
 
 inline exo_gemm_status_t cuda_failed(cudaError_t e) {
   note_cuda_error((int)e);
@@ -70,6 +70,35 @@ inline cudaError_t allow_smem(void* fn) {
   e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostSmem);
   if (e == cudaSuccess && slot) slot->store(fn, std::memory_order_relaxed);
   return e;
+}
+
+// How many clusters of `cluster` CTAs of this kernel the current device holds at once: fewer than its SMs divided by the cluster where
+// a GPC's SMs do not divide.  Asked once per device for each kind (an index below 32 that the caller gives to kernel, cluster size
+// and shared memory).
+inline int resident_clusters(int kind, void* fn, unsigned threads, size_t smem, unsigned cluster, int sms, int ctas_per_sm) {
+  static std::atomic<int> known[8][32];
+  const int otherwise = ctas_per_sm * sms / (int)cluster;
+  if (cluster == 1) return otherwise;
+  int device = 0, n = 0;
+  if (cudaGetDevice(&device) != cudaSuccess || device >= 8) return otherwise;
+  if ((n = known[device][kind].load(std::memory_order_relaxed)) > 0) return n;
+  cudaLaunchConfig_t lc{};
+  lc.gridDim = dim3(cluster, 1, 1);
+  lc.blockDim = dim3(threads, 1, 1);
+  lc.dynamicSmemBytes = smem;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = cluster;
+  at[0].val.clusterDim.y = 1;
+  at[0].val.clusterDim.z = 1;
+  lc.attrs = at;
+  lc.numAttrs = 1;
+  if (allow_smem(fn) != cudaSuccess || cudaOccupancyMaxActiveClusters(&n, fn, &lc) != cudaSuccess || n < 1) {
+    cudaGetLastError();
+    n = otherwise;
+  }
+  known[device][kind].store(n, std::memory_order_relaxed);
+  return n;
 }
 
 // One launch with programmatic dependent launch and, for cluster > 1, clusters of that many CTAs along x.

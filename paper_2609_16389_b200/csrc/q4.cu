@@ -237,10 +237,10 @@ __global__ void __launch_bounds__(kQuantThreads) exo_q4_dequantize_kernel(const 
 }
 
 // ==== the product of a few tokens with a 4-bit matrix =============================================================
-// A CTA's eight warps are 8 / NK groups of 16 weight rows times NK parts of its steps of k; the CTAs of a cluster
-// share the rows and split k.  The tokens' values for the CTA's part of k are staged in shared memory (rows 64 bytes off
-// a multiple of 128, so that a fragment load is free of bank conflicts).  Partial sums meet in shared memory in warp
-// order, then in distributed shared memory in rank order.
+// The general form, for activations that fit no shared memory (rows of tens of thousands of weights): 16 weight rows and up to
+// eight tokens to a CTA, whose eight warps split k; the CTAs of a cluster split it once more.  The activations are staged
+// in shared memory a chunk of k at a time (rows 64 bytes off a multiple of 128, so that a fragment load is free of bank
+// conflicts).  Partial sums meet in shared memory in warp order, then in distributed shared memory in rank order.
 constexpr int kGemvThreads = 256, kGemvWarps = 8;
 
 struct GemvParams {
@@ -273,31 +273,26 @@ __device__ __forceinline__ void store_y(const GemvParams& p, int token, int64_t 
   }
 }
 
-template <class T, int PER, bool ZEROS, int NT, int NK>
-__global__ void __launch_bounds__(kGemvThreads, NT <= 4 ? 2 : 1) exo_gemv_q4_kernel(const GemvParams p) {
+template <class T, int PER, bool ZEROS>
+__global__ void __launch_bounds__(kGemvThreads, 2) exo_gemv_q4_kernel(const GemvParams p) {
   namespace cg = cooperative_groups;
   extern __shared__ __align__(128) uint8_t smem[];
   cg::cluster_group cluster = cg::this_cluster();
   const int S = (int)cluster.num_blocks(), r = (int)cluster.block_rank();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-  constexpr int WR = kGemvWarps / NK;   // warps across rows
-  const int wr = warp % WR, wk = warp / WR;
-  const int64_t tile_row = (int64_t)(blockIdx.x / S) * 16 * WR;
-  const int64_t row0 = min(tile_row + 16 * wr + g, p.rows - 1), row1 = min(tile_row + 16 * wr + g + 8, p.rows - 1);
+  const int64_t tile_row = (int64_t)(blockIdx.x / S) * 16;
+  const int64_t row0 = min(tile_row + g, p.rows - 1), row1 = min(tile_row + g + 8, p.rows - 1);
+  const int first = blockIdx.y * 8, tokens = min(p.tokens - first, 8);   // this CTA's tokens
   const int s_begin = (int)((int64_t)p.blocks * r / S), s_end = (int)((int64_t)p.blocks * (r + 1) / S);
   const int whole = p.K / 128;          // whole steps; a part of one may follow
-  constexpr int nt = NT;
   using F = RowsQ4<T, PER, ZEROS>;
-  float acc[NT][4];
-#pragma unroll
-  for (int i = 0; i < NT; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
+  float acc[1][4] = {{0.f, 0.f, 0.f, 0.f}};
 
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();
   const int pitch = gemv_pitch(p.chunk);
-  constexpr int DEPTH = NT == 1 ? 4 : 2;
   for (int c = s_begin; c < s_end; c += p.chunk) {
-    const int c_end = min(c + p.chunk, s_end), s = c + wk;
+    const int c_end = min(c + p.chunk, s_end), s = c + warp;
     F f;
     f.c0 = p.codes + (row0 * p.blocks + s) * 64;
     f.c1 = p.codes + (row1 * p.blocks + s) * 64;
@@ -308,59 +303,51 @@ __global__ void __launch_bounds__(kGemvThreads, NT <= 4 ? 2 : 1) exo_gemv_q4_ker
       f.z1 = p.zeros + (row1 * p.blocks + s) * PER;
     }
     f.begin(t);
-    const int n = steps_of(s, NK, min(c_end, whole));
-    Stream<F, NK, DEPTH> stream;
+    const int n = steps_of(s, kGemvWarps, min(c_end, whole));
+    Stream<F, kGemvWarps, 4> stream;
     stream.preload(f, n);
     if (c != s_begin) __syncthreads();   // the previous chunk has been read
     const int per_token = (c_end - c) * 16;
-    for (int i = threadIdx.x; i < p.tokens * per_token; i += kGemvThreads) {
+    for (int i = threadIdx.x; i < tokens * per_token; i += kGemvThreads) {
       const int token = i / per_token, e = i - token * per_token;
       *reinterpret_cast<uint4*>(smem + token * pitch + e * 16) =
-          load8_checked(p.x + (int64_t)token * p.ldx, c * 128 + e * 8, p.K, p.x_aligned);
+          load8_checked(p.x + (int64_t)(first + token) * p.ldx, c * 128 + e * 8, p.K, p.x_aligned);
     }
     __syncthreads();
-    // columns beyond the tokens read the last row again (up to 8 tokens) or rows that nobody wrote
-    XShared x{ptx::smem_u32(smem) + (NT == 1 ? min(g, p.tokens - 1) : g) * pitch + wk * 256 + 16 * t, 8u * pitch};
-    stream.template walk<NT>(f, n, x, All<NT>(), acc);
-    if (s + n * NK == whole && whole < c_end) f.template step_tail<NT>(f.load_tail(0, t), p.K - whole * 128, x, All<NT>(), acc);
+    // columns beyond the tokens read the last row again
+    XShared x{ptx::smem_u32(smem) + min(g, tokens - 1) * pitch + warp * 256 + 16 * t, 0};
+    stream.template walk<1>(f, n, x, All<1>(), acc);
+    if (s + n * kGemvWarps == whole && whole < c_end) f.template step_tail<1>(f.load_tail(0, t), p.K - whole * 128, x, All<1>(), acc);
   }
 
-  // sums over the warps that share rows, then over the cluster
+  // sums over the warps, then over the cluster
   __syncthreads();
-  float4* red = reinterpret_cast<float4*>(smem);                        // [warp][nt][lane]
-  float4* part = red + kGemvWarps * nt * 32;                            // [wr][nt][lane]
-#pragma unroll
-  for (int i = 0; i < NT; ++i)
-    if (i < nt) red[(warp * nt + i) * 32 + lane] = make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
+  float4* red = reinterpret_cast<float4*>(smem);                        // [warp][lane]
+  float4* part = red + kGemvWarps * 32;                                 // [lane]
+  red[warp * 32 + lane] = make_float4(acc[0][0], acc[0][1], acc[0][2], acc[0][3]);
   __syncthreads();
-  const int items = WR * nt * 32;
-  auto finish = [&](int idx, float4 v) {
-    const int l = idx & 31, i = (idx >> 5) % nt, w = (idx >> 5) / nt;
-    const int64_t row = tile_row + 16 * w + (l >> 2);
-    const int token = 8 * i + 2 * (l & 3);
+  auto finish = [&](float4 v) {
+    const int token = first + 2 * t;
+    const int64_t row = tile_row + g;
     store_y<T>(p, token, row, v.x);
     store_y<T>(p, token + 1, row, v.y);
     store_y<T>(p, token, row + 8, v.z);
     store_y<T>(p, token + 1, row + 8, v.w);
   };
-  for (int idx = threadIdx.x; idx < items; idx += kGemvThreads) {
-    float4 v = red[idx];
-    for (int q = 1; q < NK; ++q) {
-      const float4 w = red[q * items + idx];
-      v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
-    }
-    if (S == 1) finish(idx, v);
-    else part[idx] = v;
+  auto add = [](float4& v, const float4& w) { v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w; };
+  if (warp == 0) {
+    float4 v = red[lane];
+#pragma unroll
+    for (int q = 1; q < kGemvWarps; ++q) add(v, red[q * 32 + lane]);
+    if (S == 1) finish(v);
+    else part[lane] = v;
   }
   if (S > 1) {
     cluster.sync();
-    for (int idx = r * kGemvThreads + threadIdx.x; idx < items; idx += S * kGemvThreads) {
-      float4 v = cluster.map_shared_rank(part, 0)[idx];
-      for (int q = 1; q < S; ++q) {
-        const float4 w = cluster.map_shared_rank(part, q)[idx];
-        v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
-      }
-      finish(idx, v);
+    if (r == 0 && warp == 0) {
+      float4 v = part[lane];
+      for (int q = 1; q < S; ++q) add(v, cluster.map_shared_rank(part, q)[lane]);
+      finish(v);
     }
     cluster.sync();   // no CTA leaves while another may still read its sums
   }
@@ -425,6 +412,72 @@ __device__ __noinline__ float not_finite_part(const uint32_t* codes, const uint1
   return v;
 }
 
+// Scales and zero points of up to eight steps of a lane's rows g and g + 8, loaded together: lane t of four holds those of steps t
+// and 4 + t, and hands them out.  Rows that do not exist, and groups of padding alone (whose scales may be anything), get 0.
+template <class T, int PER, bool ZEROS>
+struct StepScales {
+  using F = RowsQ4<T, PER, ZEROS>;
+  static constexpr int N = (PER + 1) / 2;
+  uint32_t a[2][N], b[2][N], za[2], zb[2];
+
+  // steps k .. k + n - 1 of the matrix
+  __device__ __forceinline__ void load(const GemvParams& p, int row, int k, int n) {
+    const int lane = threadIdx.x & 31, row0 = row + (lane >> 2), row1 = row0 + 8;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int step = 4 * h + (lane & 3);
+#pragma unroll
+      for (int i = 0; i < N; ++i) a[h][i] = b[h][i] = 0;
+      za[h] = zb[h] = 0;
+      if (step < n) {
+        const int64_t at0 = ((int64_t)row0 * p.blocks + k + step) * PER, at1 = ((int64_t)row1 * p.blocks + k + step) * PER;
+        if (row0 < p.rows) {
+          F::load_scales(a[h], p.scales + at0);
+          if constexpr (ZEROS) za[h] = F::load_zeros(p.zeros + at0);
+        }
+        if (row1 < p.rows) {
+          F::load_scales(b[h], p.scales + at1);
+          if constexpr (ZEROS) zb[h] = F::load_zeros(p.zeros + at1);
+        }
+        if (PER > 1 && k + step == p.blocks - 1) {
+#pragma unroll
+          for (int q = 1; q < PER; ++q)
+            if ((k + step) * 128 + q * (128 / PER) >= p.K) {
+              a[h][q / 2] &= q % 2 ? 0x0000ffffu : 0xffff0000u;
+              b[h][q / 2] &= q % 2 ? 0x0000ffffu : 0xffff0000u;
+            }
+        }
+      }
+    }
+  }
+  // step u (the same for all lanes; known when compiling where it matters)
+  __device__ __forceinline__ void get(int u, uint32_t (&sa)[N], uint32_t (&sb)[N], uint32_t& z0, uint32_t& z1) const {
+    const int from = ((threadIdx.x & 31) & 28) | (u & 3), h = u / 4;
+    if constexpr (PER == 1) {
+      const uint32_t both = __shfl_sync(0xffffffffu, a[h][0] | b[h][0] << 16, from);
+      sa[0] = both & 0xffffu;
+      sb[0] = both >> 16;
+    } else {
+#pragma unroll
+      for (int q = 0; q < N; ++q) {
+        sa[q] = __shfl_sync(0xffffffffu, a[h][q], from);
+        sb[q] = __shfl_sync(0xffffffffu, b[h][q], from);
+      }
+    }
+    z0 = z1 = 0;
+    if constexpr (ZEROS) {
+      if constexpr (PER <= 2) {
+        const uint32_t both = __shfl_sync(0xffffffffu, za[h] | zb[h] << 16, from);
+        z0 = both & 0xffffu;
+        z1 = both >> 16;
+      } else {
+        z0 = __shfl_sync(0xffffffffu, za[h], from);
+        z1 = __shfl_sync(0xffffffffu, zb[h], from);
+      }
+    }
+  }
+};
+
 // NT: tiles of eight columns, two tokens each.
 template <class T, int PER, bool ZEROS, int NT>
 __global__ void __launch_bounds__(kFewThreads, 2) exo_gemv_q4_few_kernel(const FewParams fp, const __grid_constant__ CUtensorMap map) {
@@ -487,40 +540,12 @@ __global__ void __launch_bounds__(kFewThreads, 2) exo_gemv_q4_few_kernel(const F
   ptx::grid_launch_dependents();
   for (int i = 0; i < fp.stages; ++i) issue();
 
-  // scales and zero points of up to eight steps of rows g and g + 8: lane t holds those of steps t and 4 + t
-  struct Scales { uint32_t a[2][(PER + 1) / 2], b[2][(PER + 1) / 2], za[2], zb[2]; };
-  auto load_scales = [&](Scales& sc, int u, int piece) {
-    const int row0 = row_of(u) + g, row1 = row0 + 8;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int step = 4 * h + t, s = piece * fp.piece + step;
-#pragma unroll
-      for (int i = 0; i < (PER + 1) / 2; ++i) sc.a[h][i] = sc.b[h][i] = 0;
-      sc.za[h] = sc.zb[h] = 0;
-      if (step < fp.piece && s < k_steps) {
-        const int64_t k = k_begin + s;
-        if (row0 < p.rows) {
-          F::load_scales(sc.a[h], p.scales + ((int64_t)row0 * p.blocks + k) * PER);
-          if constexpr (ZEROS) sc.za[h] = F::load_zeros(p.zeros + ((int64_t)row0 * p.blocks + k) * PER);
-        }
-        if (row1 < p.rows) {
-          F::load_scales(sc.b[h], p.scales + ((int64_t)row1 * p.blocks + k) * PER);
-          if constexpr (ZEROS) sc.zb[h] = F::load_zeros(p.zeros + ((int64_t)row1 * p.blocks + k) * PER);
-        }
-        if (PER > 1 && k == p.blocks - 1) {   // groups of padding alone: their scales may be anything
-#pragma unroll
-          for (int q = 1; q < PER; ++q)
-            if (k * 128 + q * (128 / PER) >= p.K) {
-              sc.a[h][q / 2] &= q % 2 ? 0x0000ffffu : 0xffff0000u;
-              sc.b[h][q / 2] &= q % 2 ? 0x0000ffffu : 0xffff0000u;
-            }
-        }
-      }
-    }
+  auto load_scales = [&](StepScales<T, PER, ZEROS>& sc, int u, int piece) {
+    sc.load(p, row_of(u), k_begin + piece * fp.piece, min(fp.piece, k_steps - piece * fp.piece));
   };
   int cu = warp;
   int cp = begin_of(cu);
-  Scales cur, nxt;
+  StepScales<T, PER, ZEROS> cur, nxt;
   if (cu < units) load_scales(cur, cu, cp);
 
   // the tokens' digits: 16 lanes to a step, eight values each
@@ -598,29 +623,8 @@ __global__ void __launch_bounds__(kFewThreads, 2) exo_gemv_q4_few_kernel(const F
       if (u < n) {
         const uint4 ra = lds128(w + u * 1024), rb = lds128(w + u * 1024 + 512);
         const uint32_t wa[4] = {ra.x, ra.y, ra.z, ra.w}, wb[4] = {rb.x, rb.y, rb.z, rb.w};
-        const int from = (lane & 28) | (u & 3);
-        uint32_t sa[(PER + 1) / 2], sb[(PER + 1) / 2], za = 0, zb = 0;
-        if constexpr (PER == 1) {
-          const uint32_t both = __shfl_sync(0xffffffffu, cur.a[u / 4][0] | cur.b[u / 4][0] << 16, from);
-          sa[0] = both & 0xffffu;
-          sb[0] = both >> 16;
-        } else {
-#pragma unroll
-          for (int q = 0; q < PER / 2; ++q) {
-            sa[q] = __shfl_sync(0xffffffffu, cur.a[u / 4][q], from);
-            sb[q] = __shfl_sync(0xffffffffu, cur.b[u / 4][q], from);
-          }
-        }
-        if constexpr (ZEROS) {
-          if constexpr (PER <= 2) {
-            const uint32_t both = __shfl_sync(0xffffffffu, cur.za[u / 4] | cur.zb[u / 4] << 16, from);
-            za = both & 0xffffu;
-            zb = both >> 16;
-          } else {
-            za = __shfl_sync(0xffffffffu, cur.za[u / 4], from);
-            zb = __shfl_sync(0xffffffffu, cur.zb[u / 4], from);
-          }
-        }
+        uint32_t sa[(PER + 1) / 2], sb[(PER + 1) / 2], za, zb;
+        cur.get(u, sa, sb, za, zb);
         const int s = s0 + u;
 #pragma unroll
         for (int i = 0; i < NT; ++i) {
@@ -692,6 +696,127 @@ __global__ void __launch_bounds__(kFewThreads, 2) exo_gemv_q4_few_kernel(const F
   if (S > 1) cluster.sync();   // no CTA leaves while another may still read its sums
 }
 
+// ==== five to 64 tokens ==============================================================================================
+// The same cut as for few tokens, with 16-bit products: a step's codes become exact 16-bit integers once for NT tiles of
+// eight tokens, whose values for the CTA's part of k lie in shared memory for the whole run (rows 64 bytes off a
+// multiple of 128, so that a fragment load is free of bank conflicts).  Eight more tokens cost a step 8 matrix instructions and
+// four 512-byte loads of activations; at 24 tokens the tensor pipe is the bound (mma.sync, 8 clocks each).
+constexpr int kBatchWarps = 16, kBatchThreads = 32 * kBatchWarps, kBatchPiece = 2;
+
+template <class T, int PER, bool ZEROS, int NT>
+__global__ void __launch_bounds__(kBatchThreads, 1) exo_gemv_q4_batch_kernel(const FewParams fp, const __grid_constant__ CUtensorMap map) {
+  namespace cg = cooperative_groups;
+  using F = RowsQ4<T, PER, ZEROS>;
+  const GemvParams& p = fp.g;
+  extern __shared__ __align__(128) uint8_t smem[];
+  cg::cluster_group cluster = cg::this_cluster();
+  const int S = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+  const int clusters = gridDim.x / S, cl = blockIdx.x / S;
+  const int first = blockIdx.y * 8 * NT, tokens = min(p.tokens - first, 8 * NT);   // this CTA's tokens
+  const int tiles = (int)((p.rows + 15) / 16), nk = 1 << fp.nk_log;
+  const int units = ((tiles - cl + clusters - 1) / clusters) << fp.nk_log;         // of this cluster
+  const int k_begin = rank_part(p.blocks, rank, S), k_steps = rank_part(p.blocks, rank + 1, S) - k_begin;
+  const int pieces = (k_steps + fp.piece - 1) / fp.piece, stage_bytes = fp.piece * 1024;
+  float* sums = reinterpret_cast<float*>(smem + 512);                              // [unit][token][16]
+  uint8_t* xs = smem + fp.digits_at;                                               // [token][pitch]
+  const int pitch = k_steps * 256 + 64;
+  const uint32_t bar = ptx::smem_u32(smem) + warp * 32, ring = ptx::smem_u32(smem + fp.ring_at) + warp * fp.stages * stage_bytes;
+  if (lane == 0) {
+    for (int i = 0; i < fp.stages; ++i) ptx::mbar_init(bar + 8 * i, 1);
+    ptx::prefetch_tensormap(&map);
+  }
+  ptx::fence_mbar_init();
+  __syncwarp();
+  auto row_of = [&](int u) { return (cl + (u >> fp.nk_log) * clusters) * 16; };
+  auto begin_of = [&](int u) { return (pieces * (u & (nk - 1))) >> fp.nk_log; };
+  auto end_of = [&](int u) { return (pieces * ((u & (nk - 1)) + 1)) >> fp.nk_log; };
+  int iu = warp, ip = begin_of(iu), islot = 0;            // the next copy
+  auto issue = [&]() {
+    if (iu < units) {
+      if (lane == 0) {
+        ptx::mbar_arrive_expect_tx(bar + 8 * islot, stage_bytes);
+        ptx::tma_load_3d(ring + islot * stage_bytes, &map, 0, row_of(iu), k_begin + ip * fp.piece, bar + 8 * islot);
+      }
+      islot = islot + 1 == fp.stages ? 0 : islot + 1;
+      if (++ip == end_of(iu)) {
+        iu += kBatchWarps;
+        ip = begin_of(iu);
+      }
+    }
+  };
+  ptx::grid_dependency_wait();
+  ptx::grid_launch_dependents();
+  for (int i = 0; i < fp.stages; ++i) issue();
+
+  F f;
+  auto load_scales = [&](StepScales<T, PER, ZEROS>& sc, int u, int piece) {
+    sc.load(p, row_of(u), k_begin + piece * fp.piece, min(fp.piece, k_steps - piece * fp.piece));
+  };
+  StepScales<T, PER, ZEROS> cur, nxt;
+  if (warp < units) load_scales(cur, warp, begin_of(warp));
+
+  const int per_token = k_steps * 16;
+  for (int i = threadIdx.x; i < tokens * per_token; i += kBatchThreads) {
+    const int token = i / per_token, e = i - token * per_token;
+    *reinterpret_cast<uint4*>(xs + token * pitch + e * 16) =
+        load8_checked(p.x + (int64_t)(first + token) * p.ldx, (k_begin * 16 + e) * 8, p.K, p.x_aligned);
+  }
+  __syncthreads();
+  // columns beyond the tokens repeat the last one (one tile) or hold what happens to be there; nobody reads them
+  const XShared x0{ptx::smem_u32(xs) + (NT == 1 ? min(g, tokens - 1) : g) * pitch + 16 * t, 8u * pitch};
+  int cslot = 0;
+  uint32_t parity = 0;
+  for (int u = warp; u < units; u += kBatchWarps) {
+    float acc[NT][4];
+#pragma unroll
+    for (int i = 0; i < NT; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
+    const int end = end_of(u);
+    for (int c = begin_of(u); c < end; ++c) {
+      wait_piece(bar + 8 * cslot, parity);
+      const uint32_t w = ring + cslot * stage_bytes + g * 64 + t * 16;
+      const int s0 = c * fp.piece, n = min(fp.piece, k_steps - s0);
+      if (c + 1 < end) load_scales(nxt, u, c + 1);
+      else if (u + kBatchWarps < units) load_scales(nxt, u + kBatchWarps, begin_of(u + kBatchWarps));
+#pragma unroll
+      for (int v = 0; v < kBatchPiece; ++v) {
+        if (v < n) {
+          typename F::Regs now;
+          cur.get(v, now.sa, now.sb, now.za, now.zb);
+          now.a = lds128(w + v * 1024);
+          now.b = lds128(w + v * 1024 + 512);
+          f.template step<NT, 0>(now, XShared{x0.base + (s0 + v) * 256, x0.stride}, All<NT>(), acc);
+        }
+      }
+      cur = nxt;
+      __syncwarp();
+      issue();
+      cslot = cslot + 1 == fp.stages ? 0 : cslot + 1;
+      parity ^= cslot == 0 ? 1u : 0u;
+    }
+    float* out = sums + u * tokens * 16;
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const int token = 8 * i + 2 * t + (c & 1);
+        if (token < tokens) out[token * 16 + g + 8 * (c >> 1)] = acc[i][c];
+      }
+  }
+  if (S > 1) cluster.sync(); else __syncthreads();
+  const int values = (units >> fp.nk_log) * tokens * 16;
+  for (int i = rank * kBatchThreads + threadIdx.x; i < values; i += S * kBatchThreads) {
+    const int tile = i / (tokens * 16), at = i - tile * (tokens * 16);
+    float v = 0.f;
+    for (int r = 0; r < S; ++r) {
+      const float* from = (S > 1 ? cluster.map_shared_rank(sums, r) : sums) + (tile << fp.nk_log) * tokens * 16 + at;
+      for (int j = 0; j < nk; ++j) v += from[j * tokens * 16];
+    }
+    store_y<T>(p, first + at / 16, (cl + tile * clusters) * 16 + (at & 15), v);
+  }
+  if (S > 1) cluster.sync();   // no CTA leaves while another may still read its sums
+}
+
 // Y = beta * Y, for alpha == 0 or K == 0
 template <class T>
 __global__ void __launch_bounds__(kGemvThreads) exo_gemv_q4_scale_kernel(const GemvParams p) {
@@ -703,32 +828,22 @@ __global__ void __launch_bounds__(kGemvThreads) exo_gemv_q4_scale_kernel(const G
 
 using GemvFn = void (*)(GemvParams);
 using FewFn = void (*)(FewParams, CUtensorMap);
-// tiles of eight tokens that a kernel computes
-int gemv_tiles(int tokens) { return tokens <= 32 ? (tokens + 7) / 8 : tokens <= 48 ? 6 : 8; }
-template <class T, int PER, bool ZEROS> GemvFn pick_tokens(int tokens) {
-  return tokens <= 2    ? exo_gemv_q4_kernel<T, PER, ZEROS, 1, 8>
-         : tokens <= 8  ? exo_gemv_q4_kernel<T, PER, ZEROS, 1, 2>
-         : tokens <= 16 ? exo_gemv_q4_kernel<T, PER, ZEROS, 2, 1>
-         : tokens <= 24 ? exo_gemv_q4_kernel<T, PER, ZEROS, 3, 1>
-         : tokens <= 32 ? exo_gemv_q4_kernel<T, PER, ZEROS, 4, 1>
-         : tokens <= 48 ? exo_gemv_q4_kernel<T, PER, ZEROS, 6, 1>
-                        : exo_gemv_q4_kernel<T, PER, ZEROS, 8, 1>;
+template <class T, bool ZEROS> GemvFn pick_group(int group) {
+  return group == 128 ? exo_gemv_q4_kernel<T, 1, ZEROS> : group == 64 ? exo_gemv_q4_kernel<T, 2, ZEROS> : exo_gemv_q4_kernel<T, 4, ZEROS>;
 }
-template <class T, bool ZEROS> GemvFn pick_group(int group, int tokens) {
-  return group == 128 ? pick_tokens<T, 1, ZEROS>(tokens) : group == 64 ? pick_tokens<T, 2, ZEROS>(tokens) : pick_tokens<T, 4, ZEROS>(tokens);
-}
-template <class T> GemvFn pick_gemv(int group, bool zeros, int tokens) {
-  return zeros ? pick_group<T, true>(group, tokens) : pick_group<T, false>(group, tokens);
-}
+template <class T> GemvFn pick_gemv(int group, bool zeros) { return zeros ? pick_group<T, true>(group) : pick_group<T, false>(group); }
 
-template <class T, int PER, bool ZEROS> FewFn pick_few_tokens(int tokens) {
-  return tokens <= 2 ? exo_gemv_q4_few_kernel<T, PER, ZEROS, 1> : exo_gemv_q4_few_kernel<T, PER, ZEROS, 2>;
+// few: the integer kernel, nt tiles of two tokens; else nt tiles of eight
+template <class T, int PER, bool ZEROS> FewFn pick_few_tiles(bool few, int nt) {
+  if (few) return nt == 1 ? exo_gemv_q4_few_kernel<T, PER, ZEROS, 1> : exo_gemv_q4_few_kernel<T, PER, ZEROS, 2>;
+  return nt == 1 ? exo_gemv_q4_batch_kernel<T, PER, ZEROS, 1> : nt == 2 ? exo_gemv_q4_batch_kernel<T, PER, ZEROS, 2>
+         : nt == 3 ? exo_gemv_q4_batch_kernel<T, PER, ZEROS, 3> : exo_gemv_q4_batch_kernel<T, PER, ZEROS, 4>;
 }
-template <class T, bool ZEROS> FewFn pick_few_group(int group, int tokens) {
-  return group == 128 ? pick_few_tokens<T, 1, ZEROS>(tokens) : group == 64 ? pick_few_tokens<T, 2, ZEROS>(tokens) : pick_few_tokens<T, 4, ZEROS>(tokens);
+template <class T, bool ZEROS> FewFn pick_few_group(int group, bool few, int nt) {
+  return group == 128 ? pick_few_tiles<T, 1, ZEROS>(few, nt) : group == 64 ? pick_few_tiles<T, 2, ZEROS>(few, nt) : pick_few_tiles<T, 4, ZEROS>(few, nt);
 }
-template <class T> FewFn pick_few(int group, bool zeros, int tokens) {
-  return zeros ? pick_few_group<T, true>(group, tokens) : pick_few_group<T, false>(group, tokens);
+template <class T> FewFn pick_few(int group, bool zeros, bool few, int nt) {
+  return zeros ? pick_few_group<T, true>(group, few, nt) : pick_few_group<T, false>(group, few, nt);
 }
 
 // How the few-token kernel is cut.  Large matrices (a few dozen KB for every SM) run as one CTA per SM with pieces of 8
@@ -742,7 +857,9 @@ bool plan_few(FewParams& fp, const GemvParams& p, int per, int sms, unsigned* ct
   while (S < 8 && p.blocks >= 2 * S && 4 * p.tokens * ((p.blocks + S - 1) / S) * 128 > 40 * 1024) S *= 2;
   const bool large = tiles * p.blocks >= (int64_t)sms * 96;
   const int slice = (p.blocks + S - 1) / S, least = p.blocks / S;
-  const int64_t slots = (int64_t)(large ? 1 : 2) * sms / S, clusters = tiles < slots ? tiles : slots;
+  const int64_t slots = S == 1 ? (int64_t)(large ? 1 : 2) * sms
+                               : resident_clusters(8 + 2 * S + large, (void*)exo_gemv_q4_few_kernel<Bf16, 1, false, 1>, kFewThreads, large ? 200 * 1024 : 100 * 1024, (unsigned)S, sms, large ? 1 : 2);
+  const int64_t clusters = tiles < slots ? tiles : slots;
   const int most = (int)((tiles + clusters - 1) / clusters);     // tiles of a cluster
   fp.tiled = large;
   fp.piece = large ? 8 : 4;
@@ -764,6 +881,44 @@ bool plan_few(FewParams& fp, const GemvParams& p, int per, int sms, unsigned* ct
   *cluster = (unsigned)S;
   *smem = (size_t)at;
   return at <= kMostSmem;
+}
+
+// How the kernel for more tokens is cut, one CTA to an SM; nt is the number of tiles of eight tokens that a CTA keeps.  The
+// smallest cluster whose CTAs hold their part of the activations and of the sums.  False: they do not fit.
+bool plan_batch(FewParams& fp, const GemvParams& p, int sms, int nt, unsigned* ctas, unsigned* cluster, size_t* smem) {
+  const int64_t tiles = (p.rows + 15) / 16, staged = nt == 1 && p.tokens < 8 ? p.tokens : 8 * nt, tokens = p.tokens < 8 * nt ? p.tokens : 8 * nt;
+  fp.tiled = true;
+  fp.piece = kBatchPiece;
+  for (int S = 1; S <= 8 && (S == 1 || p.blocks >= S); S *= 2) {
+    const int slice = (p.blocks + S - 1) / S, least = p.blocks / S;
+    const int64_t x_bytes = staged * ((int64_t)slice * 256 + 64);
+    const bool enough = tiles * S >= sms || S == 8 || p.blocks < 2 * S * kBatchWarps;   // a cluster also spreads few rows over the SMs
+    if (x_bytes > 110 * 1024 || !enough) continue;
+    int64_t clusters = resident_clusters(S, (void*)exo_gemv_q4_batch_kernel<Bf16, 1, false, 1>, kBatchThreads, kMostSmem, (unsigned)S, sms, 1);
+    if (tiles < clusters) clusters = tiles;
+    for (;; clusters = 2 * clusters < tiles ? 2 * clusters : tiles) {   // more turns where the sums would not fit
+      const int most = (int)((tiles + clusters - 1) / clusters);
+      fp.nk_log = 0;
+      while (fp.nk_log < 4 && (most << fp.nk_log) < kBatchWarps && (least + fp.piece - 1) / fp.piece >= 2 << fp.nk_log) ++fp.nk_log;
+      const int turns = ((most << fp.nk_log) + kBatchWarps - 1) / kBatchWarps;
+      const int pieces = ((slice + fp.piece - 1) / fp.piece + (1 << fp.nk_log) - 1) >> fp.nk_log;
+      fp.stages = turns * pieces < 2 ? turns * pieces : 2;
+      int64_t at = 512 + (int64_t)(most << fp.nk_log) * tokens * 64;
+      fp.digits_at = (int)at; at += x_bytes;
+      at = (at + 127) / 128 * 128;
+      fp.ring_at = (int)at;
+      at += kBatchWarps * fp.stages * fp.piece * 1024;
+      if (at <= kMostSmem) {
+        *ctas = (unsigned)(clusters * S);
+        *cluster = (unsigned)S;
+        *smem = (size_t)at;
+        fp.g = p;
+        return true;
+      }
+      if (most <= 1) break;
+    }
+  }
+  return false;
 }
 
 exo_gemm_status_t check_q4(const exo_q4_t* q) {
@@ -869,29 +1024,32 @@ extern "C" exo_gemm_status_t exo_gemv_q4_run(const exo_q4_t* W, int64_t tokens, 
   }
   // A CTA reads its part of X once for 16 * wr weight rows: more rows for more tokens.  Then the cluster cuts k until the
   // grid fills the device twice, as long as a warp keeps a step.
-  if (p.tokens <= 4 && p.rows < (1LL << 31) - 16) {
+  if (p.rows < (1LL << 31) - 16) {
     FewParams fp{};
     size_t smem = 0;
-    unsigned ctas = 0, cluster = 1;
-    if (plan_few(fp, p, 128 / W->group, sms, &ctas, &cluster, &smem)) {
+    unsigned ctas = 0, cluster = 1, groups = 1;
+    const bool few = p.tokens <= 4;
+    int nt = few ? (p.tokens + 1) / 2 : p.tokens < 32 ? (p.tokens + 7) / 8 : 4;
+    bool fits = few && plan_few(fp, p, 128 / W->group, sms, &ctas, &cluster, &smem);
+    if (!few)
+      while (!(fits = plan_batch(fp, p, sms, nt, &ctas, &cluster, &smem)) && nt > 1) --nt;
+    if (fits) {
+      if (!few) groups = (unsigned)((p.tokens + 8 * nt - 1) / (8 * nt));
       CUtensorMap map;
       if (fp.tiled && !exo::encode_steps_map(&map, p.codes, (uint64_t)p.rows, (uint64_t)p.blocks, (uint32_t)fp.piece)) return EXO_GEMM_ERR_CUDA;
-      FewFn fn = bf16 ? pick_few<Bf16>(W->group, W->zeros, p.tokens) : pick_few<Fp16>(W->group, W->zeros, p.tokens);
-      return launch((void*)fn, ctas, 1, kFewThreads, smem, cluster, (cudaStream_t)cuda_stream, &fp, &map);
+      FewFn fn = bf16 ? pick_few<Bf16>(W->group, W->zeros, few, nt) : pick_few<Fp16>(W->group, W->zeros, few, nt);
+      return launch((void*)fn, ctas, groups, few ? kFewThreads : kBatchThreads, smem, cluster, (cudaStream_t)cuda_stream, &fp, &map);
     }
   }
-  const int nk = tokens <= 2 ? 8 : tokens <= 8 ? 2 : 1, wr = kGemvWarps / nk, nt = gemv_tiles(p.tokens);
-  const int64_t tiles = (p.rows + 16 * wr - 1) / (16 * wr);
+  const int64_t tiles = (p.rows + 15) / 16;
   int S = 1;
-  while (S < 8 && tiles * S < 2 * sms && p.blocks >= 2 * S * nk) S *= 2;
+  while (S < 8 && tiles * S < 2 * sms && p.blocks >= 2 * S * kGemvWarps) S *= 2;
   if (tiles * S >= (1LL << 31)) return EXO_GEMM_ERR_UNSUPPORTED;
-  const int mine = (p.blocks + S - 1) / S;
   // staged activations: all of the CTA's part of k where that leaves room for two CTAs per SM
-  const int staged = nt == 1 ? p.tokens : 8 * nt, most = (100 * 1024 / staged - 64) / 256;
+  const int mine = (p.blocks + S - 1) / S, staged = p.tokens < 8 ? p.tokens : 8, most = (100 * 1024 / staged - 64) / 256;
   p.chunk = mine < most ? mine : most;
   size_t smem = (size_t)staged * gemv_pitch(p.chunk);
-  const size_t reduce = (size_t)(kGemvWarps + wr) * nt * 512;
-  if (smem < reduce) smem = reduce;
-  GemvFn fn = bf16 ? pick_gemv<Bf16>(W->group, W->zeros, p.tokens) : pick_gemv<Fp16>(W->group, W->zeros, p.tokens);
-  return launch((void*)fn, (unsigned)(tiles * S), 1, kGemvThreads, smem, (unsigned)S, (cudaStream_t)cuda_stream, &p);
+  if (smem < (kGemvWarps + 1) * 512) smem = (kGemvWarps + 1) * 512;
+  GemvFn fn = bf16 ? pick_gemv<Bf16>(W->group, W->zeros) : pick_gemv<Fp16>(W->group, W->zeros);
+  return launch((void*)fn, (unsigned)(tiles * S), (unsigned)((p.tokens + 7) / 8), kGemvThreads, smem, (unsigned)S, (cudaStream_t)cuda_stream, &p);
 }
