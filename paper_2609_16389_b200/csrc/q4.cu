@@ -253,7 +253,8 @@ struct GemvParams {
   int K, tokens, blocks;        // blocks: steps of 128
   int chunk;                    // steps staged at a time
   int y_dtype;
-  bool x_aligned;
+  int x_align;                  // bytes that every row of x starts on a multiple of, 16 at most
+  bool x_aligned;               // 16 of them
   float alpha, beta;
 };
 
@@ -393,6 +394,18 @@ __device__ __forceinline__ void transpose4(const uint32_t (&v)[4], uint32_t (&d)
 __device__ __forceinline__ void copy16(uint32_t to, const void* from, bool there) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(there ? 16 : 0) : "memory");
 }
+// eight 16-bit values, by copies of `align` bytes (4, 8 or 16 at least)
+__device__ __forceinline__ void copy_eight(uint32_t to, const uint16_t* from, int align) {
+  if (align >= 16) {
+    copy16(to, from, true);
+  } else if (align == 8) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to + 8 * i), "l"(from + 4 * i) : "memory");
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to + 4 * i), "l"(from + 2 * i) : "memory");
+  }
+}
 __device__ __forceinline__ int rank_part(int blocks, int r, int S) { return (int)((int64_t)blocks * r / S); }
 
 // What the values of a token that are not finite give a row over steps s0 .. s1 - 1 (they count as 0 in the integers).  codes,
@@ -412,37 +425,45 @@ __device__ __noinline__ float not_finite_part(const uint32_t* codes, const uint1
   return v;
 }
 
-// Scales and zero points of up to eight steps of a lane's rows g and g + 8, loaded together: lane t of four holds those of steps t
-// and 4 + t, and hands them out.  Rows that do not exist, and groups of padding alone (whose scales may be anything), get 0.
-template <class T, int PER, bool ZEROS>
+// Scales and zero points of up to STEPS (4 or 8) steps of a lane's rows g and g + 8, loaded together: lane t of four holds those of
+// steps t and 4 + t, and hands them out.  Groups of padding alone (whose scales may be anything) get 0.
+template <class T, int PER, bool ZEROS, int STEPS>
 struct StepScales {
   using F = RowsQ4<T, PER, ZEROS>;
-  static constexpr int N = (PER + 1) / 2;
-  uint32_t a[2][N], b[2][N], za[2], zb[2];
+  static constexpr int N = (PER + 1) / 2, H = STEPS / 4;
+  uint32_t a[H][N], b[H][N], za[H], zb[H];
 
-  // steps k .. k + n - 1 of the matrix
-  __device__ __forceinline__ void load(const GemvParams& p, int row, int k, int n) {
-    const int lane = threadIdx.x & 31, row0 = row + (lane >> 2), row1 = row0 + 8;
+  struct Rows {                  // this lane's places in the rows of one tile
+    const uint16_t *s0, *s1;
+    const uint8_t *z0, *z1;
+  };
+  // rows row + g and row + g + 8 from step k_begin on; rows that do not exist repeat the last one, nobody stores theirs
+  static __device__ __forceinline__ Rows rows(const GemvParams& p, int row, int k_begin) {
+    const int lane = threadIdx.x & 31;
+    const int64_t r0 = min((int64_t)row + (lane >> 2), p.rows - 1), r1 = min((int64_t)row + (lane >> 2) + 8, p.rows - 1);
+    const int64_t at0 = (r0 * p.blocks + k_begin + (lane & 3)) * PER, at1 = (r1 * p.blocks + k_begin + (lane & 3)) * PER;
+    return Rows{p.scales + at0, p.scales + at1, ZEROS ? p.zeros + at0 : nullptr, ZEROS ? p.zeros + at1 : nullptr};
+  }
+  // steps s .. s + n - 1 of the CTA's; left: values of k from step s on
+  __device__ __forceinline__ void load(const Rows& r, int s, int n, int left) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int step = 4 * h + (lane & 3);
+    for (int h = 0; h < H; ++h) {
+      const int step = 4 * h + (threadIdx.x & 3);
 #pragma unroll
       for (int i = 0; i < N; ++i) a[h][i] = b[h][i] = 0;
       za[h] = zb[h] = 0;
       if (step < n) {
-        const int64_t at0 = ((int64_t)row0 * p.blocks + k + step) * PER, at1 = ((int64_t)row1 * p.blocks + k + step) * PER;
-        if (row0 < p.rows) {
-          F::load_scales(a[h], p.scales + at0);
-          if constexpr (ZEROS) za[h] = F::load_zeros(p.zeros + at0);
+        const int at = (s + 4 * h) * PER;
+        F::load_scales(a[h], r.s0 + at);
+        F::load_scales(b[h], r.s1 + at);
+        if constexpr (ZEROS) {
+          za[h] = F::load_zeros(r.z0 + at);
+          zb[h] = F::load_zeros(r.z1 + at);
         }
-        if (row1 < p.rows) {
-          F::load_scales(b[h], p.scales + at1);
-          if constexpr (ZEROS) zb[h] = F::load_zeros(p.zeros + at1);
-        }
-        if (PER > 1 && k + step == p.blocks - 1) {
+        if (PER > 1 && (step + 1) * 128 > left) {
 #pragma unroll
           for (int q = 1; q < PER; ++q)
-            if ((k + step) * 128 + q * (128 / PER) >= p.K) {
+            if (step * 128 + q * (128 / PER) >= left) {
               a[h][q / 2] &= q % 2 ? 0x0000ffffu : 0xffff0000u;
               b[h][q / 2] &= q % 2 ? 0x0000ffffu : 0xffff0000u;
             }
@@ -540,23 +561,36 @@ __global__ void __launch_bounds__(kFewThreads, 2) exo_gemv_q4_few_kernel(const F
   ptx::grid_launch_dependents();
   for (int i = 0; i < fp.stages; ++i) issue();
 
-  auto load_scales = [&](StepScales<T, PER, ZEROS>& sc, int u, int piece) {
-    sc.load(p, row_of(u), k_begin + piece * fp.piece, min(fp.piece, k_steps - piece * fp.piece));
+  using SC = StepScales<T, PER, ZEROS, 8>;
+  typename SC::Rows srows;
+  auto load_scales = [&](SC& sc, int piece) {
+    const int s = piece * fp.piece;
+    sc.load(srows, s, min(fp.piece, k_steps - s), p.K - (k_begin + s) * 128);
   };
   int cu = warp;
   int cp = begin_of(cu);
-  StepScales<T, PER, ZEROS> cur, nxt;
-  if (cu < units) load_scales(cur, cu, cp);
+  SC cur, nxt;
+  if (cu < units) {
+    srows = SC::rows(p, row_of(cu), k_begin);
+    load_scales(cur, cp);
+  }
 
   // the tokens' digits: 16 lanes to a step, eight values each
   uint8_t* digits = smem + fp.digits_at;                                     // [column][k_steps][t][j][8]
   int* start = reinterpret_cast<int*>(smem + fp.start_at);                   // [k_steps * PER][COLS]
   float* step_scale = reinterpret_cast<float*>(smem + fp.step_scale_at);     // [k_steps][2 * NT]
   __syncthreads();
-  for (int i0 = 0; i0 < p.tokens * k_steps * 16; i0 += kFewThreads) {
+  const int all_parts = p.tokens * k_steps * 16;
+  auto raw_part = [&](int i) {             // clamped, so that all lanes take part in the shuffles below
+    const int item = min(i >> 4, p.tokens * k_steps - 1), token = item / k_steps, s = item - token * k_steps;
+    return load8_checked(p.x + (int64_t)token * p.ldx, (k_begin + s) * 128 + 8 * (i & 15), p.K, p.x_aligned);
+  };
+  uint4 raw_next = raw_part(threadIdx.x);
+  for (int i0 = 0; i0 < all_parts; i0 += kFewThreads) {
     const int i = i0 + threadIdx.x, item = min(i >> 4, p.tokens * k_steps - 1), e = i & 15;
     const int token = item / k_steps, s = item - token * k_steps;
-    const uint4 raw = load8_checked(p.x + (int64_t)token * p.ldx, (k_begin + s) * 128 + 8 * e, p.K, p.x_aligned);
+    const uint4 raw = raw_next;
+    if (i0 + kFewThreads < all_parts) raw_next = raw_part(i + kFewThreads);
     const uint32_t rw[4] = {raw.x, raw.y, raw.z, raw.w};
     float v[8], top = 0.f;
     bool odd = false;
@@ -585,7 +619,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) exo_gemv_q4_few_kernel(const F
 #pragma unroll
       for (int o = 1; o < 16 / PER; o <<= 1) sum[c] += __shfl_xor_sync(0xffffffffu, sum[c], o);
     }
-    if (i < p.tokens * k_steps * 16) {
+    if (i < all_parts) {
 #pragma unroll
       for (int c = 0; c < 4; ++c)
         *reinterpret_cast<uint2*>(digits + (token * 4 + c) * col_pitch + s * 128 + (e & 3) * 32 + (e >> 2) * 8) = make_uint2(d0[c], d1[c]);
@@ -613,8 +647,9 @@ __global__ void __launch_bounds__(kFewThreads, 2) exo_gemv_q4_few_kernel(const F
     if (ends) {
       nu += kFewWarps;
       np = begin_of(nu);
+      if (nu < units) srows = SC::rows(p, row_of(nu), k_begin);
     }
-    if (nu < units) load_scales(nxt, nu, np);
+    if (nu < units) load_scales(nxt, np);
     wait_piece(bar + 8 * cslot, parity);
     const uint32_t w = ring + cslot * stage_bytes + g * 64 + t * 16;
     const int s0 = cp * fp.piece, n = min(fp.piece, k_steps - s0);
@@ -717,7 +752,7 @@ __global__ void __launch_bounds__(kBatchThreads, 1) exo_gemv_q4_batch_kernel(con
   const int tiles = (int)((p.rows + 15) / 16), nk = 1 << fp.nk_log;
   const int units = ((tiles - cl + clusters - 1) / clusters) << fp.nk_log;         // of this cluster
   const int k_begin = rank_part(p.blocks, rank, S), k_steps = rank_part(p.blocks, rank + 1, S) - k_begin;
-  const int pieces = (k_steps + fp.piece - 1) / fp.piece, stage_bytes = fp.piece * 1024;
+  const int pieces = (k_steps + kBatchPiece - 1) / kBatchPiece, stage_bytes = kBatchPiece * 1024;
   float* sums = reinterpret_cast<float*>(smem + 512);                              // [unit][token][16]
   uint8_t* xs = smem + fp.digits_at;                                               // [token][pitch]
   const int pitch = k_steps * 256 + 64;
@@ -736,7 +771,7 @@ __global__ void __launch_bounds__(kBatchThreads, 1) exo_gemv_q4_batch_kernel(con
     if (iu < units) {
       if (lane == 0) {
         ptx::mbar_arrive_expect_tx(bar + 8 * islot, stage_bytes);
-        ptx::tma_load_3d(ring + islot * stage_bytes, &map, 0, row_of(iu), k_begin + ip * fp.piece, bar + 8 * islot);
+        ptx::tma_load_3d(ring + islot * stage_bytes, &map, 0, row_of(iu), k_begin + ip * kBatchPiece, bar + 8 * islot);
       }
       islot = islot + 1 == fp.stages ? 0 : islot + 1;
       if (++ip == end_of(iu)) {
@@ -750,18 +785,30 @@ __global__ void __launch_bounds__(kBatchThreads, 1) exo_gemv_q4_batch_kernel(con
   for (int i = 0; i < fp.stages; ++i) issue();
 
   F f;
-  auto load_scales = [&](StepScales<T, PER, ZEROS>& sc, int u, int piece) {
-    sc.load(p, row_of(u), k_begin + piece * fp.piece, min(fp.piece, k_steps - piece * fp.piece));
+  using SC = StepScales<T, PER, ZEROS, 4>;
+  typename SC::Rows srows;
+  auto load_scales = [&](SC& sc, int piece) {
+    const int s = piece * kBatchPiece;
+    sc.load(srows, s, min(kBatchPiece, k_steps - s), p.K - (k_begin + s) * 128);
   };
-  StepScales<T, PER, ZEROS> cur, nxt;
-  if (warp < units) load_scales(cur, warp, begin_of(warp));
-
-  const int per_token = k_steps * 16;
-  for (int i = threadIdx.x; i < tokens * per_token; i += kBatchThreads) {
-    const int token = i / per_token, e = i - token * per_token;
-    *reinterpret_cast<uint4*>(xs + token * pitch + e * 16) =
-        load8_checked(p.x + (int64_t)(first + token) * p.ldx, (k_begin * 16 + e) * 8, p.K, p.x_aligned);
+  SC cur, nxt;
+  if (warp < units) {
+    srows = SC::rows(p, row_of(warp), k_begin);
+    load_scales(cur, begin_of(warp));
   }
+
+  // all of the activations' loads in flight at once, as wide as their rows' alignment lets them be
+  const int per_token = k_steps * 16, segments = (per_token + 31) / 32;
+  for (int i = warp; i < tokens * segments; i += kBatchWarps) {
+    const int token = i / segments, e = (i - token * segments) * 32 + lane, left = p.K - k_begin * 128;
+    if (e < per_token) {
+      const uint16_t* from = p.x + (int64_t)(first + token) * p.ldx + k_begin * 128;
+      uint8_t* to = xs + token * pitch + e * 16;
+      if (p.x_align >= 4 && e * 8 + 8 <= left) copy_eight(ptx::smem_u32(to), from + e * 8, p.x_align);
+      else *reinterpret_cast<uint4*>(to) = load8_checked(from, e * 8, left, p.x_aligned);
+    }
+  }
+  asm volatile("cp.async.wait_all;" ::: "memory");
   __syncthreads();
   // columns beyond the tokens repeat the last one (one tile) or hold what happens to be there; nobody reads them
   const XShared x0{ptx::smem_u32(xs) + (NT == 1 ? min(g, tokens - 1) : g) * pitch + 16 * t, 8u * pitch};
@@ -775,9 +822,13 @@ __global__ void __launch_bounds__(kBatchThreads, 1) exo_gemv_q4_batch_kernel(con
     for (int c = begin_of(u); c < end; ++c) {
       wait_piece(bar + 8 * cslot, parity);
       const uint32_t w = ring + cslot * stage_bytes + g * 64 + t * 16;
-      const int s0 = c * fp.piece, n = min(fp.piece, k_steps - s0);
-      if (c + 1 < end) load_scales(nxt, u, c + 1);
-      else if (u + kBatchWarps < units) load_scales(nxt, u + kBatchWarps, begin_of(u + kBatchWarps));
+      const int s0 = c * kBatchPiece, n = min(kBatchPiece, k_steps - s0);
+      if (c + 1 < end) {
+        load_scales(nxt, c + 1);
+      } else if (u + kBatchWarps < units) {
+        srows = SC::rows(p, row_of(u + kBatchWarps), k_begin);
+        load_scales(nxt, begin_of(u + kBatchWarps));
+      }
 #pragma unroll
       for (int v = 0; v < kBatchPiece; ++v) {
         if (v < n) {
@@ -1014,7 +1065,9 @@ extern "C" exo_gemm_status_t exo_gemv_q4_run(const exo_q4_t* W, int64_t tokens, 
   p.x = (const uint16_t*)X; p.y = Y; p.ldx = ldx; p.ldy = ldy; p.rows = W->rows;
   p.K = (int)W->K; p.tokens = (int)tokens; p.blocks = blocks_of(W->K);
   p.y_dtype = y_dtype; p.alpha = alpha; p.beta = beta;
-  p.x_aligned = ((uintptr_t)X & 15u) == 0 && ldx % 8 == 0;
+  const uintptr_t x_at = (uintptr_t)X | (uintptr_t)(ldx * 2);
+  p.x_align = x_at % 16 == 0 ? 16 : x_at % 8 == 0 ? 8 : x_at % 4 == 0 ? 4 : 2;
+  p.x_aligned = p.x_align == 16;
   const bool bf16 = W->dtype == EXO_GEMM_BF16;
   if (!read) {
     const int64_t ctas = (p.rows + kGemvThreads - 1) / kGemvThreads;
