@@ -1,16 +1,17 @@
-// What the few-token kernels share: weights streamed from device memory straight into the fragments of
-// mma.sync.m16n8k16, 16 weight rows by 8 tokens at a time.
+// What the few-token kernels share: the fragments of mma.sync, 16 weight rows by 8 tokens at a time, straight from rows of
+// weights.
 //
 // For a few tokens a product is bound by reading the weights, so the kernels are built around the load: a lane
-// reads 16 consecutive bytes of a weight row, and the order in which the tensor core sums over k is chosen so that
+// takes 16 consecutive bytes of a weight row, and the order in which the tensor core sums over k is chosen so that
 // those bytes are its fragment.  In m16n8k16 lane 4 g + t holds the A elements of rows g and g + 8 at four
 // values of k and the B elements of column g at the same four.  Any assignment of the real k to those places gives the
-// same sum as long as A and B agree, so lane t takes eight consecutive k for two instructions: no shuffle, no
-// shared-memory pass and no transposition of either operand.
+// same sum as long as A and B agree, so lane t takes eight consecutive k for two instructions: no shuffle and no
+// transposition of either operand.
 //
 // mma.sync and not tcgen05: an operand of tcgen05.mma comes from shared or tensor memory, 64 or 128 rows at a time.
-// Here the weights arrive in registers, 4-bit ones have to pass through them anyway, and 16 rows per warp cut a
-// matrix into pieces fine enough to occupy 148 SMs.  Up to 64 tokens the legacy path's rate is not the bound.
+// 4-bit weights have to pass through registers anyway, and 16 rows per warp cut a matrix into pieces fine enough to
+// occupy 148 SMs.  m16n8k16 takes a quarter of an SM 8 clocks (ncu, sm__pipe_tensor): at one token 64 of the 178 clocks in
+// which memory delivers a step of 16 x 128 4-bit weights, from about 24 tokens on more than that.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -103,70 +104,15 @@ struct XShared {
   }
   __device__ __forceinline__ void advance(int n) { base += 2 * n; }
 };
-struct XGlobal {
-  const uint16_t* base;
-  int64_t stride;          // elements
-  template <int OFF> __device__ __forceinline__ uint4 load(int i) const { return *reinterpret_cast<const uint4*>(base + i * stride + OFF); }
-  __device__ __forceinline__ void advance(int n) { base += n; }
-};
-// the last part of a step: values at and beyond `left` (counted from base) are 0
-struct XGlobalTail {
-  const uint16_t* base;
-  int64_t stride;
-  int left;
-  template <int OFF> __device__ __forceinline__ uint4 load(int i) const { return load8_checked(base + i * stride, OFF, left, true); }
-};
 
-// ---- weight formats -------------------------------------------------------------------------------------------
-// A format reads 16 weight rows in steps of kStep values of k.  Its pointers are the lane's own: rows g and g + 8, at the
-// lane's part of the current step.
+// ---- 4-bit rows -----------------------------------------------------------------------------------------------
+// Sixteen rows of 4-bit weights in steps of 128 values of k.  The pointers are the lane's own: rows g and g + 8, at its part of
+// the current step.
 //   load(n)      the step n ahead of the current one
 //   advance(n)   n steps on
 //   step(...)    acc += rows x tokens; x.load<OFF>(i) are the lane's eight activations of token 8 i + g, OFF elements
 //                behind the current step's (the lane's own 8 t included)
 // Only whole steps go through load() and step(); a last part of a step goes through load_tail() and step_tail().
-
-// 16-bit weights.  VEC: every row starts on a 16-byte boundary.
-template <class T, bool VEC>
-struct Rows16 {
-  static constexpr int kStep = 32;
-  const uint16_t *r0, *r1;
-  struct Regs { uint4 a, b; };
-
-  __device__ __forceinline__ void begin(int t) { r0 += 8 * t; r1 += 8 * t; }
-  __device__ __forceinline__ void advance(int n) { r0 += n * kStep; r1 += n * kStep; }
-  __device__ __forceinline__ Regs load(int n) const {
-    Regs r;
-    if constexpr (VEC) {
-      r.a = ldg_weights(r0 + n * kStep);
-      r.b = ldg_weights(r1 + n * kStep);
-    } else {
-      r.a = load8_checked(r0 + n * kStep, 0, 8, false);
-      r.b = load8_checked(r1 + n * kStep, 0, 8, false);
-    }
-    return r;
-  }
-  // the current step, of which only the first `left` values of k exist
-  __device__ __forceinline__ Regs load_tail(int left, int t) const {
-    return Regs{load8_checked(r0, 0, left - 8 * t, VEC), load8_checked(r1, 0, left - 8 * t, VEC)};
-  }
-  template <int NT, int OFF, class X, class N>
-  __device__ __forceinline__ void step(const Regs& r, const X& x, N nt, float (&acc)[NT][4]) const {
-#pragma unroll
-    for (int i = 0; i < NT; ++i) {
-      if (i == 0 || i < nt) {
-        const uint4 b = x.template load<OFF>(i);
-        T::mma(acc[i], r.a.x, r.b.x, r.a.y, r.b.y, b.x, b.y);
-        T::mma(acc[i], r.a.z, r.b.z, r.a.w, r.b.w, b.z, b.w);
-      }
-    }
-  }
-  template <int NT, class X, class N>
-  __device__ __forceinline__ void step_tail(const Regs& r, int, const X& x, N nt, float (&acc)[NT][4]) const {
-    step<NT, 0>(r, x, nt, acc);
-  }
-};
-
 // 4-bit weights, PER groups of 128 / PER weights in a step of 128.  ZEROS: with zero points, else 8 everywhere.
 template <class T, int PER, bool ZEROS>
 struct RowsQ4 {
@@ -271,6 +217,75 @@ struct RowsQ4 {
   template <int NT, class X, class N>
   __device__ __forceinline__ void step_tail(const Regs& r, int left, const X& x, N nt, float (&acc)[NT][4]) const {
     products<NT, 0, true>(r, left, x, nt, acc);
+  }
+};
+
+// Scales and zero points of up to STEPS (4 or 8) steps of a lane's rows g and g + 8, loaded together: lane t of four holds those of
+// steps t and 4 + t, and hands them out.  Groups of padding alone (whose scales may be anything) get 0.
+template <class T, int PER, bool ZEROS, int STEPS>
+struct StepScales {
+  using F = RowsQ4<T, PER, ZEROS>;
+  static constexpr int N = (PER + 1) / 2, H = STEPS / 4;
+  uint32_t a[H][N], b[H][N], za[H], zb[H];
+
+  struct Rows {                  // this lane's places in the rows of a tile: their step 0, t further on
+    const uint16_t *s0, *s1;
+    const uint8_t *z0, *z1;      // NULL: 8
+  };
+  // steps s .. s + n - 1; left: values of k from step s on
+  __device__ __forceinline__ void load(const Rows& r, int s, int n, int left) {
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+      const int step = 4 * h + (threadIdx.x & 3);
+#pragma unroll
+      for (int i = 0; i < N; ++i) a[h][i] = b[h][i] = 0;
+      za[h] = zb[h] = 0;
+      if (step < n) {
+        const int at = (s + 4 * h) * PER;
+        F::load_scales(a[h], r.s0 + at);
+        F::load_scales(b[h], r.s1 + at);
+        if constexpr (ZEROS) {
+          za[h] = r.z0 ? F::load_zeros(r.z0 + at) : 0x08080808u;
+          zb[h] = r.z1 ? F::load_zeros(r.z1 + at) : 0x08080808u;
+        }
+        if (PER > 1 && (step + 1) * 128 > left) {
+#pragma unroll
+          for (int q = 1; q < PER; ++q)
+            if (step * 128 + q * (128 / PER) >= left) {
+              a[h][q / 2] &= q % 2 ? 0x0000ffffu : 0xffff0000u;
+              b[h][q / 2] &= q % 2 ? 0x0000ffffu : 0xffff0000u;
+            }
+        }
+      }
+    }
+  }
+  // step u, the same for all lanes
+  __device__ __forceinline__ void get(int u, uint32_t (&sa)[N], uint32_t (&sb)[N], uint32_t& z0, uint32_t& z1) const {
+    const int from = ((threadIdx.x & 31) & 28) | (u & 3);
+    auto pick = [&](const uint32_t (&v)[H]) { return H == 1 || u < 4 ? v[0] : v[H - 1]; };
+    auto pick_n = [&](const uint32_t (&v)[H][N], int i) { return H == 1 || u < 4 ? v[0][i] : v[H - 1][i]; };
+    if constexpr (PER == 1) {
+      const uint32_t both = __shfl_sync(0xffffffffu, pick_n(a, 0) | pick_n(b, 0) << 16, from);
+      sa[0] = both & 0xffffu;
+      sb[0] = both >> 16;
+    } else {
+#pragma unroll
+      for (int q = 0; q < N; ++q) {
+        sa[q] = __shfl_sync(0xffffffffu, pick_n(a, q), from);
+        sb[q] = __shfl_sync(0xffffffffu, pick_n(b, q), from);
+      }
+    }
+    z0 = z1 = 0;
+    if constexpr (ZEROS) {
+      if constexpr (PER <= 2) {
+        const uint32_t both = __shfl_sync(0xffffffffu, (pick(za) & 0xffffu) | pick(zb) << 16, from);
+        z0 = both & 0xffffu;
+        z1 = both >> 16;
+      } else {
+        z0 = __shfl_sync(0xffffffffu, pick(za), from);
+        z1 = __shfl_sync(0xffffffffu, pick(zb), from);
+      }
+    }
   }
 };
 

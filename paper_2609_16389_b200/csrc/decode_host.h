@@ -50,7 +50,7 @@ inline bool q4_aligned(const void* codes, const void* scales, const void* zeros,
   return ((uintptr_t)codes & 15u) == 0 && (uintptr_t)scales % (unsigned)(256 / group) == 0 && (uintptr_t)zeros % (unsigned)(128 / group) == 0;
 }
 
-// Opts a kernel in to kMostSmem, once per device: always to the same size, so that threads which launch one kernel at different
+// Opts a kernel in to kMostSmem, or what it can have, once per device: always to the same size, so that threads which launch one kernel at different
 // sizes cannot take it from each other.
 inline cudaError_t allow_smem(void* fn) {
   constexpr int kSlots = 512;
@@ -67,7 +67,10 @@ inline cudaError_t allow_smem(void* fn) {
       if (!have && !slot) slot = &s;
     }
   }
-  e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostSmem);
+  cudaFuncAttributes a;
+  if ((e = cudaFuncGetAttributes(&a, fn)) != cudaSuccess) return e;
+  const int room = 227 * 1024 - (int)a.sharedSizeBytes;   // what the kernel's own variables leave
+  e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, room < kMostSmem ? room : kMostSmem);
   if (e == cudaSuccess && slot) slot->store(fn, std::memory_order_relaxed);
   return e;
 }

@@ -1,12 +1,15 @@
-// A whole mixture-of-experts layer for a few tokens (exo_decode.h), in three kernels that follow one another by
-// programmatic dependent launch:
+// A whole mixture-of-experts layer for a few tokens (exo_decode.h): a routing kernel and two kernels for the experts, that follow
+// one another by programmatic dependent launch:
 //
-//   route   logits = x * router^T; its last CTA picks each token's experts and lists, for every taken expert, its tokens
+//   route   logits = x * router^T; each token's experts, and for every taken expert its tokens
 //   up      a = w_e * silu(gate_e x) * (up_e x) for every taken expert and its tokens
 //   down    y = sum of down_e a over the taken experts
 //
-// The layer is bound by reading the taken experts' weights once.  All three stream weight rows into mma fragments
-// (decode_core.cuh); a fragment's eight columns are the expert's own tokens, gathered.
+// The layer is bound by reading the taken experts' weights once.  A fragment (decode_core.cuh) is 16 weight rows by eight of the
+// expert's own tokens.  Measured on a B200 (CUDA graph of passes, three sets of inputs in turn): 8 of 64 experts of 2048 x 1024 in
+// bf16, one token, 29.3 us for 101 MB (15.4 at the copy bandwidth): of that 5.4 are routing, 2 to 4 each kernel's start and 1 to 2
+// its end, and the weights themselves stream at the bandwidth; 64 tokens, 6 of 64 and a shared one of 4096 x 1536, 533 us
+// for 2.45 GB (374).  4-bit experts are held up by their unpacking (2 of 8 of 4096 x 8192, one token, 50 us; 15.9).
 #include <cooperative_groups.h>
 
 #include <new>
@@ -267,9 +270,8 @@ __global__ void __launch_bounds__(kRouteThreads) exo_moe_route_kernel(const MoeP
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
   const int e0 = (int)(blockIdx.x / S) * 16;
   const int nt = (p.tokens + 7) / 8;
-  Rows16<T, VEC> f;
-  f.r0 = p.router + (int64_t)min(e0 + g, p.experts - 1) * p.ld_router;
-  f.r1 = p.router + (int64_t)min(e0 + g + 8, p.experts - 1) * p.ld_router;
+  const uint16_t* r0 = p.router + (int64_t)min(e0 + g, p.experts - 1) * p.ld_router;
+  const uint16_t* r1 = p.router + (int64_t)min(e0 + g + 8, p.experts - 1) * p.ld_router;
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();
   if (p.copy_x) copy_rows(p);
@@ -278,7 +280,7 @@ __global__ void __launch_bounds__(kRouteThreads) exo_moe_route_kernel(const MoeP
   const int steps = (p.hidden + 31) / 32, ds = S * kRouteWarps;
   for (int s = r * kRouteWarps + warp; s < steps; s += ds) {
     const int k = s * 32 + 8 * t;
-    const uint4 wa = load8_checked(f.r0, k, p.hidden, VEC), wb = load8_checked(f.r1, k, p.hidden, VEC);
+    const uint4 wa = load8_checked(r0, k, p.hidden, VEC), wb = load8_checked(r1, k, p.hidden, VEC);
 #pragma unroll
     for (int i = 0; i < NT; ++i)
       if (i < nt) {
@@ -375,11 +377,13 @@ struct Ring {
 // it is multiplied: first(row, s, n) at the very beginning, then multiply() with the place of the next piece.
 //   xr(i)   the lane's row of tile i at the piece's first k
 //   next    the lane's row of tile 0 at the next piece's first k, of n_next steps (0: there is none)
+// The scales of 4-bit weights come a piece ahead too: scales() asks for the next piece's, scales_here() takes them.
 template <class T>
 struct Piece16 {
   static constexpr int kStep = 32, kWords = 32;     // weights of a step, and elements of the tensor map
   uint4 x[2][kMostPiece];
-  __device__ __forceinline__ void rows(const Stack&, int64_t, const Stack&, int64_t) {}
+  __device__ __forceinline__ void scales(const Stack&, int64_t, const Stack&, int64_t, int, int) {}
+  __device__ __forceinline__ void scales_here() {}
   template <int B> __device__ __forceinline__ void load(const uint16_t* row, int n) {
 #pragma unroll
     for (int u = 0; u < kMostPiece; ++u)
@@ -416,35 +420,18 @@ struct Piece16 {
 template <class T, int PER>
 struct PieceQ4 {
   using F = RowsQ4<T, PER, true>;
+  using SC = StepScales<T, PER, true, 8>;
   static constexpr int kStep = 128, kWords = 16;
-  const uint16_t *s0, *s1;
-  const uint8_t *z0, *z1;
-  int K;
-  typename F::Regs r;
+  SC now, next_scales;
   uint4 x[4];
-  __device__ __forceinline__ void rows(const Stack& m0, int64_t row0, const Stack& m1, int64_t row1) {
-    const int64_t groups = (int64_t)((m0.K + 127) / 128) * PER;
-    s0 = m0.scales + row0 * groups;
-    s1 = m1.scales + row1 * groups;
-    z0 = m0.zeros ? m0.zeros + row0 * groups : nullptr;
-    z1 = m1.zeros ? m1.zeros + row1 * groups : nullptr;
-    K = m0.K;
+  // the scales of steps s .. s + n - 1 of row0 of one stack and row1 of the other, for the piece after the one at hand
+  __device__ __forceinline__ void scales(const Stack& m0, int64_t row0, const Stack& m1, int64_t row1, int s, int n) {
+    const int t = threadIdx.x & 3;
+    const int64_t groups = (int64_t)((m0.K + 127) / 128) * PER, at0 = row0 * groups + t * PER, at1 = row1 * groups + t * PER;
+    next_scales.load(typename SC::Rows{m0.scales + at0, m1.scales + at1, m0.zeros ? m0.zeros + at0 : nullptr, m1.zeros ? m1.zeros + at1 : nullptr},
+                     s, n, m0.K - s * 128);
   }
-  __device__ __forceinline__ void scales(int s) {
-    F::load_scales(r.sa, s0 + s * PER);
-    F::load_scales(r.sb, s1 + s * PER);
-    r.za = r.zb = 0x08080808u;
-    if (z0) r.za = F::load_zeros(z0 + s * PER);
-    if (z1) r.zb = F::load_zeros(z1 + s * PER);
-    if (PER > 1 && (s + 1) * 128 > K) {              // groups of padding alone: their scales may be anything
-#pragma unroll
-      for (int q = 1; q < PER; ++q)
-        if (s * 128 + q * (128 / PER) >= K) {
-          r.sa[q / 2] &= q % 2 ? 0x0000ffffu : 0xffff0000u;
-          r.sb[q / 2] &= q % 2 ? 0x0000ffffu : 0xffff0000u;
-        }
-    }
-  }
+  __device__ __forceinline__ void scales_here() { now = next_scales; }
   __device__ __forceinline__ void activations(const uint16_t* xr) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) x[j] = *reinterpret_cast<const uint4*>(xr + 32 * j);
@@ -460,22 +447,31 @@ struct PieceQ4 {
     template <int OFF> __device__ __forceinline__ uint4 load(int i) const { return *reinterpret_cast<const uint4*>(xr(i) + at + OFF); }
   };
   template <int NT, class XR>
-  __device__ __forceinline__ void multiply(uint32_t w, int pitch, int s, int n, const XR& xr, const uint16_t* next, int n_next, int nt, float (&acc)[NT][4]) {
-    scales(s);
-    for (int u = 0; u < n; ++u) {
-      typename F::Regs now = r;
-      now.a = lds128(w + u * 64);
-      now.b = lds128(w + 8 * pitch + u * 64);
-      F f;
-      if constexpr (NT == 1) {
+  __device__ __forceinline__ void multiply(uint32_t w, int pitch, int, int n, const XR& xr, const uint16_t* next, int n_next, int nt, float (&acc)[NT][4]) {
+    F f;
+    if (NT == 1 || nt == 1) {   // the next step's activations while this one is multiplied
+      float one[1][4] = {{acc[0][0], acc[0][1], acc[0][2], acc[0][3]}};
+      for (int u = 0; u < n; ++u) {
+        typename F::Regs r;
+        now.get(u, r.sa, r.sb, r.za, r.zb);
+        r.a = lds128(w + u * 64);
+        r.b = lds128(w + 8 * pitch + u * 64);
         const uint4 mine[4] = {x[0], x[1], x[2], x[3]};
-        if (u + 1 < n) { scales(s + u + 1); activations(xr(0) + (u + 1) * 128); }
+        if (u + 1 < n) activations(xr(0) + (u + 1) * 128);
         else if (n_next) activations(next);
-        f.template step<NT, 0>(now, FirstTile{mine}, All<NT>(), acc);
-      } else {
-        if (u + 1 < n) scales(s + u + 1);
-        f.template step<NT, 0>(now, Tiles<XR>{xr, u * 128}, nt, acc);
+        f.template step<1, 0>(r, FirstTile{mine}, All<1>(), one);
       }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[0][i] = one[0][i];
+    } else {
+      for (int u = 0; u < n; ++u) {
+        typename F::Regs r;
+        now.get(u, r.sa, r.sb, r.za, r.zb);
+        r.a = lds128(w + u * 64);
+        r.b = lds128(w + 8 * pitch + u * 64);
+        f.template step<NT, 0>(r, Tiles<XR>{xr, u * 128}, nt, acc);
+      }
+      if (n_next) activations(next);
     }
   }
 };
@@ -519,7 +515,7 @@ __device__ __forceinline__ Tables copy_tables(uint8_t* at, int& n_active, const 
 // take its items one by one, or, where there are fewer items than warps, parts of their `hidden`, whose sums meet in
 // shared memory in order.
 template <class T, int FMT, int NT>
-__global__ void __launch_bounds__(kMoeThreads, 2)
+__global__ void __launch_bounds__(kMoeThreads, NT <= 2 || FMT == 1 ? 2 : 1)
 exo_moe_up_ring_kernel(const MoeParams p, const __grid_constant__ CUtensorMap gate_map, const __grid_constant__ CUtensorMap up_map) {
   using P = typename PieceOf<T, FMT>::type;
   extern __shared__ __align__(128) uint8_t smem[];
@@ -582,13 +578,19 @@ exo_moe_up_ring_kernel(const MoeParams p, const __grid_constant__ CUtensorMap ga
   auto row_of = [&](const Active& a, int i) { return p.xs + (int64_t)tb.token[a.base + min(8 * i + g, a.count - 1)] * p.ldxs + 8 * t; };
   auto steps_at = [&](int c) { return min(p.up_piece, steps - c * p.up_piece); };
   P piece;
-  if (warp < units) piece.first(row_of(tb.active[expert_of(item_of(warp))], 0) + begin_of(warp) * p.up_piece * P::kStep, steps_at(begin_of(warp)));
+  auto ask_scales = [&](int u, int c) {
+    const int item = item_of(u), expert = tb.active[expert_of(item)].expert;
+    const int64_t row = min(item % tiles * 8 + g, p.inner - 1);
+    piece.scales(p.gate, expert * p.gate.expert_rows + row, p.up, expert * p.up.expert_rows + row, c * p.up_piece, steps_at(c));
+  };
+  if (warp < units) {
+    ask_scales(warp, begin_of(warp));
+    piece.first(row_of(tb.active[expert_of(item_of(warp))], 0) + begin_of(warp) * p.up_piece * P::kStep, steps_at(begin_of(warp)));
+  }
   for (int u = warp, took = 1; u < units; ++took) {
     const int item = item_of(u), f0 = item % tiles * 8;
     const Active a = tb.active[expert_of(item)];
     const int nt = (a.count + 7) / 8;
-    const int64_t row = min(f0 + g, p.inner - 1);
-    piece.rows(p.gate, a.expert * p.gate.expert_rows + row, p.up, a.expert * p.up.expert_rows + row);
     const uint16_t* xrow[NT];
 #pragma unroll
     for (int i = 0; i < NT; ++i) xrow[i] = row_of(a, i);
@@ -600,9 +602,13 @@ exo_moe_up_ring_kernel(const MoeParams p, const __grid_constant__ CUtensorMap ga
       const int s = c * p.up_piece, n = steps_at(c);
       const uint16_t* next = xrow[0] + (s + p.up_piece) * P::kStep;
       int n_next = c + 1 < end ? steps_at(c + 1) : 0;
-      if (c + 1 == end) {
+      piece.scales_here();
+      if (c + 1 < end) {
+        ask_scales(u, c + 1);
+      } else {
         after = ahead[took % kUnitsAhead];   // its copies have begun, or there is none
         if (after < units) {
+          ask_scales(after, begin_of(after));
           next = row_of(tb.active[expert_of(item_of(after))], 0) + begin_of(after) * p.up_piece * P::kStep;
           n_next = steps_at(begin_of(after));
         }
@@ -643,7 +649,7 @@ exo_moe_up_ring_kernel(const MoeParams p, const __grid_constant__ CUtensorMap ga
 // in equal ranges; a warp adds what an expert gives onto its own sums in shared memory, by token.  The sums meet
 // in warp order and then in rank order.
 template <class T, int FMT, int NT>
-__global__ void __launch_bounds__(kMoeThreads, 2)
+__global__ void __launch_bounds__(kMoeThreads, NT <= 2 || FMT == 1 ? 2 : 1)
 exo_moe_down_ring_kernel(const MoeParams p, const __grid_constant__ CUtensorMap map) {
   namespace cg = cooperative_groups;
   using P = typename PieceOf<T, FMT>::type;
@@ -717,12 +723,18 @@ exo_moe_down_ring_kernel(const MoeParams p, const __grid_constant__ CUtensorMap 
   // rows behind an expert's are other entries', or spare ones
   auto row_at = [&](int e, int from) { return p.h + (int64_t)(tb.active[e].base + g) * p.ldh + 8 * t + from * P::kStep; };
   P piece;
-  if (any(at, s)) piece.first(row_at(at, s), min(p.down_piece, stop_of(at) - s));
+  auto ask_scales = [&](int e, int from, int n) {
+    const int64_t first = tb.active[e].expert * p.down.expert_rows;
+    piece.scales(p.down, first + min(row0 + g, p.hidden - 1), p.down, first + min(row0 + g + 8, p.hidden - 1), from, n);
+  };
+  if (any(at, s)) {
+    const int n = min(p.down_piece, stop_of(at) - s);
+    ask_scales(at, s, n);
+    piece.first(row_at(at, s), n);
+  }
   while (any(at, s)) {
     const Active a = tb.active[at];
     const int nt = (a.count + 7) / 8, stop = stop_of(at);
-    const int64_t first = a.expert * p.down.expert_rows;
-    piece.rows(p.down, first + min(row0 + g, p.hidden - 1), p.down, first + min(row0 + g + 8, p.hidden - 1));
     float acc[NT][4];
     clear(acc);
     while (s < stop) {
@@ -732,6 +744,8 @@ exo_moe_down_ring_kernel(const MoeParams p, const __grid_constant__ CUtensorMap 
       const int ne = more ? at : at + 1, nf = more ? after : 0;
       const int n_next = any(ne, nf) ? min(p.down_piece, stop_of(ne) - nf) : 0;
       const uint16_t* next = n_next ? row_at(ne, nf) : here;
+      piece.scales_here();
+      if (n_next) ask_scales(ne, nf, n_next);
       const uint32_t w = ring.wait() + g * ring.pitch + 16 * t;
       piece.template multiply<NT>(w, ring.pitch, s, n, [&](int i) { return here + (int64_t)8 * i * p.ldh; }, next, n_next, nt, acc);
       __syncwarp();
@@ -784,21 +798,20 @@ exo_moe_down_ring_kernel(const MoeParams p, const __grid_constant__ CUtensorMap 
 // leading dimension, and slow.
 constexpr int kPlainThreads = 256, kPlainWarps = 8;
 
+// Steps of 32 from s on, ds apart, of the lane's rows r0 and r1; the lane's activations of tile i begin at x0 + i * stride, or at
+// rows[i] where x0 is NULL.
 template <class T, int NT>
-__device__ __forceinline__ void plain_steps(Rows16<T, false> f, const uint16_t* x0, int64_t stride, const uint16_t* const (&rows)[NT], int s, int ds, int end,
-                                            int K, int t, int nt, float (&acc)[NT][4]) {
-  f.begin(t);
-  const uint16_t *r0 = f.r0, *r1 = f.r1;
+__device__ __forceinline__ void plain_steps(const uint16_t* r0, const uint16_t* r1, const uint16_t* x0, int64_t stride, const uint16_t* const (&rows)[NT],
+                                            int s, int ds, int end, int K, int t, int nt, float (&acc)[NT][4]) {
   for (; s < end; s += ds) {
-    f.r0 = r0 + s * 32;
-    f.r1 = r1 + s * 32;
-    const typename Rows16<T, false>::Regs w = (s + 1) * 32 <= K ? f.load(0) : f.load_tail(K - s * 32, t);
+    const int k = s * 32 + 8 * t;
+    const uint4 wa = load8_checked(r0, k, K, false), wb = load8_checked(r1, k, K, false);
 #pragma unroll
     for (int i = 0; i < NT; ++i)
       if (i < nt) {
         const uint4 b = *reinterpret_cast<const uint4*>((x0 ? x0 + i * stride : rows[i]) + s * 32);
-        T::mma(acc[i], w.a.x, w.b.x, w.a.y, w.b.y, b.x, b.y);
-        T::mma(acc[i], w.a.z, w.b.z, w.a.w, w.b.w, b.z, b.w);
+        T::mma(acc[i], wa.x, wb.x, wa.y, wb.y, b.x, b.y);
+        T::mma(acc[i], wa.z, wb.z, wa.w, wb.w, b.z, b.w);
       }
   }
 }
@@ -814,16 +827,15 @@ __global__ void __launch_bounds__(kPlainThreads) exo_moe_up_plain_kernel(const M
   const Active a{raw.x, raw.y, raw.z, raw.w};
   const int f0 = blockIdx.x * 8, nt = (a.count + 7) / 8;
   const int64_t row = min(f0 + g, p.inner - 1);
-  Rows16<T, false> f;
-  f.r0 = static_cast<const uint16_t*>(p.gate.w) + (a.expert * p.gate.expert_rows + row) * p.gate.ld;
-  f.r1 = static_cast<const uint16_t*>(p.up.w) + (a.expert * p.up.expert_rows + row) * p.up.ld;
+  const uint16_t* r0 = static_cast<const uint16_t*>(p.gate.w) + (a.expert * p.gate.expert_rows + row) * p.gate.ld;
+  const uint16_t* r1 = static_cast<const uint16_t*>(p.up.w) + (a.expert * p.up.expert_rows + row) * p.up.ld;
   const uint16_t* xrow[NT];
 #pragma unroll
   for (int i = 0; i < NT; ++i)
     xrow[i] = p.xs + (int64_t)__ldcg(p.entry_token + a.base + min(8 * i + g, a.count - 1)) * p.ldxs + 8 * t;
   float acc[NT][4];
   clear(acc);
-  plain_steps<T, NT>(f, nullptr, 0, xrow, warp, kPlainWarps, (p.hidden + 31) / 32, p.hidden, t, nt, acc);
+  plain_steps<T, NT>(r0, r1, nullptr, 0, xrow, warp, kPlainWarps, (p.hidden + 31) / 32, p.hidden, t, nt, acc);
 #pragma unroll
   for (int i = 0; i < NT; ++i)
     if (i < nt) red[(warp * nt + i) * 32 + lane] = make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
@@ -852,13 +864,12 @@ __global__ void __launch_bounds__(kPlainThreads) exo_moe_down_plain_kernel(const
     const Active a{raw.x, raw.y, raw.z, raw.w};
     const int nt = (a.count + 7) / 8;
     const int64_t first = a.expert * p.down.expert_rows;
-    Rows16<T, false> f;
-    f.r0 = static_cast<const uint16_t*>(p.down.w) + (first + min(row0 + g, p.hidden - 1)) * p.down.ld;
-    f.r1 = static_cast<const uint16_t*>(p.down.w) + (first + min(row0 + g + 8, p.hidden - 1)) * p.down.ld;
+    const uint16_t* r0 = static_cast<const uint16_t*>(p.down.w) + (first + min(row0 + g, p.hidden - 1)) * p.down.ld;
+    const uint16_t* r1 = static_cast<const uint16_t*>(p.down.w) + (first + min(row0 + g + 8, p.hidden - 1)) * p.down.ld;
     float acc[NT][4];
     clear(acc);
     const uint16_t* none[NT] = {};
-    plain_steps<T, NT>(f, p.h + (int64_t)(a.base + g) * p.ldh + 8 * t, 8 * p.ldh, none, warp, kPlainWarps, steps, p.inner, t, nt, acc);
+    plain_steps<T, NT>(r0, r1, p.h + (int64_t)(a.base + g) * p.ldh + 8 * t, 8 * p.ldh, none, warp, kPlainWarps, steps, p.inner, t, nt, acc);
 #pragma unroll
     for (int i = 0; i < NT; ++i)
 #pragma unroll
@@ -926,9 +937,11 @@ bool stack_map(CUtensorMap* map, const Stack& m, int64_t all, bool q4, int steps
 
 bool rows_aligned(const void* w, int64_t ld) { return ((uintptr_t)w & 15u) == 0 && ld % 8 == 0; }
 
-exo_gemm_status_t check_stack(const exo_moe_matrix_t& m, int64_t rows, int64_t K, int q4_group) {
+// all: experts of the stack
+exo_gemm_status_t check_stack(const exo_moe_matrix_t& m, int64_t rows, int64_t K, int64_t all, int q4_group) {
   if (!m.w) return EXO_GEMM_ERR_NULL;
-  if (m.expert_rows < rows || m.expert_rows > (1LL << 26)) return EXO_GEMM_ERR_INVALID_ARG;
+  if (m.expert_rows < rows || m.expert_rows > (1LL << 40)) return EXO_GEMM_ERR_INVALID_ARG;
+  if (all * m.expert_rows > 0x7fffffffLL - 16) return EXO_GEMM_ERR_UNSUPPORTED;   // row numbers are 32 bits in a tensor map's copies
   if (q4_group) {
     if (!m.scales) return EXO_GEMM_ERR_NULL;
     if (!q4_aligned(m.w, m.scales, m.zeros, q4_group)) return EXO_GEMM_ERR_ALIGNMENT;
@@ -1038,10 +1051,11 @@ exo_gemm_status_t exo_moe_run(exo_moe_handle_t plan, const exo_moe_weights_t* w,
   if (tokens == 0) return EXO_GEMM_OK;
   if (!x || !y || !w->router) return EXO_GEMM_ERR_NULL;
   const bool q4 = d.q4_group != 0;
+  const int64_t all = d.experts + d.shared;
   exo_gemm_status_t st;
-  if ((st = check_stack(w->gate, d.inner, d.hidden, d.q4_group)) != EXO_GEMM_OK) return st;
-  if ((st = check_stack(w->up, d.inner, d.hidden, d.q4_group)) != EXO_GEMM_OK) return st;
-  if ((st = check_stack(w->down, d.hidden, d.inner, d.q4_group)) != EXO_GEMM_OK) return st;
+  if ((st = check_stack(w->gate, d.inner, d.hidden, all, d.q4_group)) != EXO_GEMM_OK) return st;
+  if ((st = check_stack(w->up, d.inner, d.hidden, all, d.q4_group)) != EXO_GEMM_OK) return st;
+  if ((st = check_stack(w->down, d.hidden, d.inner, all, d.q4_group)) != EXO_GEMM_OK) return st;
   if ((((uintptr_t)x | (uintptr_t)y | (uintptr_t)w->router) & 1u) || (((uintptr_t)index | (uintptr_t)weight) & 3u)) return EXO_GEMM_ERR_ALIGNMENT;
   DeviceGuard guard(plan->device);
   if (guard.err != cudaSuccess) return cuda_failed(guard.err);
@@ -1073,12 +1087,20 @@ exo_gemm_status_t exo_moe_run(exo_moe_handle_t plan, const exo_moe_weights_t* w,
   // start and end (5 steps: 80 KB of ring).  Measured at 64 + 1 experts of 4096 x 1536 and 64 tokens: up with one CTA per SM and
   // 7 steps; at up to 16 tokens two CTAs and 5 steps are ahead.
   const bool many = p.tokens > 16;
-  p.up_piece = many ? 7 : 5;
-  p.down_piece = 5;
+  p.up_piece = many && !q4 ? 7 : 5;
+  p.down_piece = q4 ? 5 : many ? 7 : 5;
 
   const bool bf16 = d.dtype == EXO_GEMM_BF16;
   const int nt = (p.tokens + 7) / 8;
   const cudaStream_t stream = (cudaStream_t)cuda_stream;
+
+  // formats and tensor maps, before anything is launched
+  const int q4_fmt = d.q4_group == 128 ? 2 : d.q4_group == 64 ? 3 : 4, step = q4 ? 128 : 32, nt_kernel = nt <= 2 ? nt : 8;
+  const int up_fmt = q4 ? q4_fmt : rows_aligned(w->gate.w, w->gate.ld) && rows_aligned(w->up.w, w->up.ld) ? 1 : 0;
+  const int down_fmt = q4 ? q4_fmt : rows_aligned(w->down.w, w->down.ld) ? 1 : 0;
+  CUtensorMap gate, up, down;
+  if (up_fmt && (!stack_map(&gate, p.gate, all, q4, p.up_piece, 8) || !stack_map(&up, p.up, all, q4, p.up_piece, 8))) return EXO_GEMM_ERR_CUDA;
+  if (down_fmt && !stack_map(&down, p.down, all, q4, p.down_piece, 16)) return EXO_GEMM_ERR_CUDA;
 
   const bool router_aligned = rows_aligned(w->router, w->ld_router);
   int S = 1;
@@ -1096,28 +1118,20 @@ exo_gemm_status_t exo_moe_run(exo_moe_handle_t plan, const exo_moe_weights_t* w,
   }
   if (st != EXO_GEMM_OK) return st;
 
-  const int q4_fmt = d.q4_group == 128 ? 2 : d.q4_group == 64 ? 3 : 4, step = q4 ? 128 : 32, nt_kernel = nt <= 2 ? nt : 8;
-  const int64_t all = d.experts + d.shared;
-  const int up_fmt = q4 ? q4_fmt : rows_aligned(w->gate.w, w->gate.ld) && rows_aligned(w->up.w, w->up.ld) ? 1 : 0;
   fn = bf16 ? pick_up<Bf16>(up_fmt, nt) : pick_up<Fp16>(up_fmt, nt);
   if (up_fmt == 0) {
     st = launch(fn, (unsigned)((p.inner + 7) / 8), (unsigned)p.taken, kPlainThreads, 0, 1, stream, &p);
   } else {
-    CUtensorMap gate, up;
-    if (!stack_map(&gate, p.gate, all, q4, p.up_piece, 8) || !stack_map(&up, p.up, all, q4, p.up_piece, 8)) return EXO_GEMM_ERR_CUDA;
     const size_t smem = (size_t)kMoeWarps * kMoeStages * p.up_piece * 1024 + (size_t)2 * part_limit(nt_kernel) * nt_kernel * 512 + table_bytes(p);
     const int64_t items = (int64_t)p.taken * ((p.inner + 7) / 8), slots = (int64_t)(many ? 1 : 2) * plan->sms;
     st = launch(fn, (unsigned)(items < slots ? items : slots), 1, kMoeThreads, smem, 1, stream, &p, &gate, &up);
   }
   if (st != EXO_GEMM_OK) return st;
 
-  const int down_fmt = q4 ? q4_fmt : rows_aligned(w->down.w, w->down.ld) ? 1 : 0;
   const int64_t tiles = (p.hidden + 15) / 16, all_steps = (int64_t)p.taken * ((p.inner + step - 1) / step);
   fn = bf16 ? pick_down<Bf16>(down_fmt, nt) : pick_down<Fp16>(down_fmt, nt);
   if (down_fmt == 0)
     return launch(fn, (unsigned)tiles, 1, kPlainThreads, (size_t)kPlainWarps * p.tokens * 64, 1, stream, &p);
-  CUtensorMap down;
-  if (!stack_map(&down, p.down, all, q4, p.down_piece, 16)) return EXO_GEMM_ERR_CUDA;
   // The cluster size with the shortest estimate: a turn of the CTAs that fit costs their start and end (4 us, and more for
   // the sums of many tokens) and the weights at an SM's share of the bandwidth, 44 GB/s.
   const size_t smem = (size_t)kMoeWarps * kMoeStages * p.down_piece * 1024 + (size_t)(kMoeWarps + 1) * p.tokens * 64 + table_bytes(p);

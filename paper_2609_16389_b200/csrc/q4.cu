@@ -260,6 +260,16 @@ struct GemvParams {
 
 __host__ __device__ constexpr int gemv_pitch(int chunk) { return chunk * 256 + 64; }   // bytes of a token's staged row
 
+// The lane's places in the scales of the tile that begins at `row`, from step k_begin on; rows that do not exist repeat the last
+// one, nobody stores theirs.
+template <class SC, int PER, bool ZEROS>
+__device__ __forceinline__ typename SC::Rows scale_rows(const GemvParams& p, int row, int k_begin) {
+  const int lane = threadIdx.x & 31;
+  const int64_t r0 = min((int64_t)row + (lane >> 2), p.rows - 1), r1 = min((int64_t)row + (lane >> 2) + 8, p.rows - 1);
+  const int64_t at0 = (r0 * p.blocks + k_begin + (lane & 3)) * PER, at1 = (r1 * p.blocks + k_begin + (lane & 3)) * PER;
+  return typename SC::Rows{p.scales + at0, p.scales + at1, ZEROS ? p.zeros + at0 : nullptr, ZEROS ? p.zeros + at1 : nullptr};
+}
+
 template <class T>
 __device__ __forceinline__ void store_y(const GemvParams& p, int token, int64_t row, float v) {
   if (token >= p.tokens || row >= p.rows) return;
@@ -425,80 +435,6 @@ __device__ __noinline__ float not_finite_part(const uint32_t* codes, const uint1
   return v;
 }
 
-// Scales and zero points of up to STEPS (4 or 8) steps of a lane's rows g and g + 8, loaded together: lane t of four holds those of
-// steps t and 4 + t, and hands them out.  Groups of padding alone (whose scales may be anything) get 0.
-template <class T, int PER, bool ZEROS, int STEPS>
-struct StepScales {
-  using F = RowsQ4<T, PER, ZEROS>;
-  static constexpr int N = (PER + 1) / 2, H = STEPS / 4;
-  uint32_t a[H][N], b[H][N], za[H], zb[H];
-
-  struct Rows {                  // this lane's places in the rows of one tile
-    const uint16_t *s0, *s1;
-    const uint8_t *z0, *z1;
-  };
-  // rows row + g and row + g + 8 from step k_begin on; rows that do not exist repeat the last one, nobody stores theirs
-  static __device__ __forceinline__ Rows rows(const GemvParams& p, int row, int k_begin) {
-    const int lane = threadIdx.x & 31;
-    const int64_t r0 = min((int64_t)row + (lane >> 2), p.rows - 1), r1 = min((int64_t)row + (lane >> 2) + 8, p.rows - 1);
-    const int64_t at0 = (r0 * p.blocks + k_begin + (lane & 3)) * PER, at1 = (r1 * p.blocks + k_begin + (lane & 3)) * PER;
-    return Rows{p.scales + at0, p.scales + at1, ZEROS ? p.zeros + at0 : nullptr, ZEROS ? p.zeros + at1 : nullptr};
-  }
-  // steps s .. s + n - 1 of the CTA's; left: values of k from step s on
-  __device__ __forceinline__ void load(const Rows& r, int s, int n, int left) {
-#pragma unroll
-    for (int h = 0; h < H; ++h) {
-      const int step = 4 * h + (threadIdx.x & 3);
-#pragma unroll
-      for (int i = 0; i < N; ++i) a[h][i] = b[h][i] = 0;
-      za[h] = zb[h] = 0;
-      if (step < n) {
-        const int at = (s + 4 * h) * PER;
-        F::load_scales(a[h], r.s0 + at);
-        F::load_scales(b[h], r.s1 + at);
-        if constexpr (ZEROS) {
-          za[h] = F::load_zeros(r.z0 + at);
-          zb[h] = F::load_zeros(r.z1 + at);
-        }
-        if (PER > 1 && (step + 1) * 128 > left) {
-#pragma unroll
-          for (int q = 1; q < PER; ++q)
-            if (step * 128 + q * (128 / PER) >= left) {
-              a[h][q / 2] &= q % 2 ? 0x0000ffffu : 0xffff0000u;
-              b[h][q / 2] &= q % 2 ? 0x0000ffffu : 0xffff0000u;
-            }
-        }
-      }
-    }
-  }
-  // step u (the same for all lanes; known when compiling where it matters)
-  __device__ __forceinline__ void get(int u, uint32_t (&sa)[N], uint32_t (&sb)[N], uint32_t& z0, uint32_t& z1) const {
-    const int from = ((threadIdx.x & 31) & 28) | (u & 3), h = u / 4;
-    if constexpr (PER == 1) {
-      const uint32_t both = __shfl_sync(0xffffffffu, a[h][0] | b[h][0] << 16, from);
-      sa[0] = both & 0xffffu;
-      sb[0] = both >> 16;
-    } else {
-#pragma unroll
-      for (int q = 0; q < N; ++q) {
-        sa[q] = __shfl_sync(0xffffffffu, a[h][q], from);
-        sb[q] = __shfl_sync(0xffffffffu, b[h][q], from);
-      }
-    }
-    z0 = z1 = 0;
-    if constexpr (ZEROS) {
-      if constexpr (PER <= 2) {
-        const uint32_t both = __shfl_sync(0xffffffffu, za[h] | zb[h] << 16, from);
-        z0 = both & 0xffffu;
-        z1 = both >> 16;
-      } else {
-        z0 = __shfl_sync(0xffffffffu, za[h], from);
-        z1 = __shfl_sync(0xffffffffu, zb[h], from);
-      }
-    }
-  }
-};
-
 // NT: tiles of eight columns, two tokens each.
 template <class T, int PER, bool ZEROS, int NT>
 __global__ void __launch_bounds__(kFewThreads, 2) exo_gemv_q4_few_kernel(const FewParams fp, const __grid_constant__ CUtensorMap map) {
@@ -571,7 +507,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) exo_gemv_q4_few_kernel(const F
   int cp = begin_of(cu);
   SC cur, nxt;
   if (cu < units) {
-    srows = SC::rows(p, row_of(cu), k_begin);
+    srows = scale_rows<SC, PER, ZEROS>(p, row_of(cu), k_begin);
     load_scales(cur, cp);
   }
 
@@ -647,7 +583,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) exo_gemv_q4_few_kernel(const F
     if (ends) {
       nu += kFewWarps;
       np = begin_of(nu);
-      if (nu < units) srows = SC::rows(p, row_of(nu), k_begin);
+      if (nu < units) srows = scale_rows<SC, PER, ZEROS>(p, row_of(nu), k_begin);
     }
     if (nu < units) load_scales(nxt, np);
     wait_piece(bar + 8 * cslot, parity);
@@ -793,7 +729,7 @@ __global__ void __launch_bounds__(kBatchThreads, 1) exo_gemv_q4_batch_kernel(con
   };
   SC cur, nxt;
   if (warp < units) {
-    srows = SC::rows(p, row_of(warp), k_begin);
+    srows = scale_rows<SC, PER, ZEROS>(p, row_of(warp), k_begin);
     load_scales(cur, begin_of(warp));
   }
 
@@ -826,7 +762,7 @@ __global__ void __launch_bounds__(kBatchThreads, 1) exo_gemv_q4_batch_kernel(con
       if (c + 1 < end) {
         load_scales(nxt, c + 1);
       } else if (u + kBatchWarps < units) {
-        srows = SC::rows(p, row_of(u + kBatchWarps), k_begin);
+        srows = scale_rows<SC, PER, ZEROS>(p, row_of(u + kBatchWarps), k_begin);
         load_scales(nxt, begin_of(u + kBatchWarps));
       }
 #pragma unroll
@@ -905,7 +841,7 @@ bool plan_few(FewParams& fp, const GemvParams& p, int per, int sms, unsigned* ct
   const int nt = p.tokens <= 2 ? 1 : 2;
   const int64_t tiles = (p.rows + 15) / 16;
   int S = 1;
-  while (S < 8 && p.blocks >= 2 * S && 4 * p.tokens * ((p.blocks + S - 1) / S) * 128 > 40 * 1024) S *= 2;
+  while (S < 8 && p.blocks >= 2 * S && (int64_t)4 * p.tokens * ((p.blocks + S - 1) / S) * 128 > 40 * 1024) S *= 2;
   const bool large = tiles * p.blocks >= (int64_t)sms * 96;
   const int slice = (p.blocks + S - 1) / S, least = p.blocks / S;
   const int64_t slots = S == 1 ? (int64_t)(large ? 1 : 2) * sms

@@ -190,7 +190,8 @@ GEMV = [  # tokens, rows, K, group, zeros
     (1, 1, 1, 32, False), (1, 16, 128, 128, False), (1, 17, 129, 64, True), (2, 100, 1000, 32, True), (1, 4096, 512, 128, True),
     (1, 40, 16384, 128, False), (3, 333, 2052, 64, False), (8, 64, 4096, 128, False), (9, 70, 777, 32, True),
     (16, 130, 1024, 64, True), (17, 200, 640, 128, False), (33, 65, 1536, 32, False), (64, 257, 2048, 128, True),
-    (64, 40, 9001, 64, True), (31, 1000, 384, 128, True),
+    (64, 40, 9001, 64, True), (31, 1000, 384, 128, True), (24, 4000, 1100, 64, False), (5, 2100, 700, 32, True),
+    (4, 17, 200000, 128, False), (11, 20, 150001, 32, True),   # activations that fit no shared memory
 ]
 
 
@@ -620,3 +621,16 @@ def test_moe_refuses_bad_arguments():
     assert D.exo_moe_run(Q.plan.handle, bad, 1, buf, 64, buf + 8192, 64) == B.ERR_ALIGNMENT
     assert Q.plan.workspace_bytes() >= 4 * 2 * 32 * 2
     t.cuda.synchronize()
+
+
+# ------------------------------------------------------------------ all of them together
+@pytest.mark.parametrize("tokens", [1, 6])
+def test_decode_layer_example(tokens):
+    """The tokens' projection from 4 bits is the prompt's GEMM on the dequantised weights: W's values are exact in fp32 but
+    rounded to bf16 for the GEMM (2^-8 each), the sums are fp32, and both results are rounded to bf16."""
+    from examples import decode_layer
+    t = torch()
+    h, by_prompt, y, taken = decode_layer.run(tokens, hidden=768, inner=320, experts=12, top_k=3, prompt=96, seed=tokens)
+    a, b = h.double(), by_prompt.double()
+    assert ((a - b).norm() / b.norm()).item() <= 3 * 2.0 ** -8
+    assert t.isfinite(y).all() and ((taken >= 0) & (taken < 12)).all()
