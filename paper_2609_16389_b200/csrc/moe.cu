@@ -7,9 +7,9 @@
 //
 // The layer is bound by reading the taken experts' weights once.  A fragment (decode_core.cuh) is 16 weight rows by eight of the
 // expert's own tokens.  Measured on a B200 (CUDA graph of passes, three sets of inputs in turn): 8 of 64 experts of 2048 x 1024 in
-// bf16, one token, 29.3 us for 101 MB (15.4 at the copy bandwidth): of that 5.4 are routing, 2 to 4 each kernel's start and 1 to 2
-// its end, and the weights themselves stream at the bandwidth; 64 tokens, 6 of 64 and a shared one of 4096 x 1536, 533 us
-// for 2.45 GB (374).  4-bit experts are held up by their unpacking (2 of 8 of 4096 x 8192, one token, 50 us; 15.9).
+// bf16, one token, 30 us for 101 MB (15.4 at the copy bandwidth): of that 5.4 are routing, 2 to 4 each kernel's start and 1 to 2
+// its end, and the weights themselves stream at the bandwidth; 64 tokens, 6 of 64 and a shared one of 4096 x 1536, 537 us
+// for 2.45 GB (374).  4-bit experts are held up by their unpacking (2 of 8 of 4096 x 8192, one token, 51 us; 15.9).
 #include <cooperative_groups.h>
 
 #include <new>
@@ -196,8 +196,9 @@ __device__ __forceinline__ void copy_rows(const MoeParams& p) {
 }
 
 // The same for up to 8 tokens and 128 experts as one cluster of eight CTAs: a CTA has up to 16 of the experts, its warps cut k, and
-// the logits go straight into the first CTA's shared memory.  No memory fence, counter or second reading: 4.5 us
-// where the general form takes 7.7 (64 experts of 2048, one token).
+// the logits go straight into the first CTA's shared memory.  No memory fence, counter or second reading.
+// The layer with it and with the general form (us): 64 experts of 2048 x 1024, one token 30.1 / 31.2, 4 tokens 68.1 / 69.0; 60 of
+// 1416 x 1000, 6 tokens 44.7 / 46.4; 64 of 4096 x 1536, 4 tokens 142.4 / 143.0, 8 tokens 233 / 231.
 constexpr int kOneCtas = 8, kOneTokens = 8, kOneExperts = 16 * kOneCtas;
 
 template <class T, bool VEC>
@@ -1093,9 +1094,10 @@ exo_gemm_status_t exo_moe_run(exo_moe_handle_t plan, const exo_moe_weights_t* w,
   p.xs = p.copy_x ? (const uint16_t*)(plan->ws + plan->at_xs) : p.x;
   p.ldxs = p.copy_x ? plan->ldxs : ldx;
   // Pieces: larger ones suit the copies, smaller ones leave room for a second CTA on the SM, which covers the first one's
-  // start and end (5 steps: 80 KB of ring).  Measured at 64 + 1 experts of 4096 x 1536 and 64 tokens: up with one CTA per SM and
-  // 7 steps; at up to 16 tokens two CTAs and 5 steps are ahead.
-  const bool many = p.tokens > 16;
+  // start and end (5 steps: 80 KB of ring).  Measured, one CTA of 7 steps against two of 5 (us): 16 bits, 64 experts of 4096 x 1536 and
+  // a shared one, 8 tokens 236 / 233, 9 tokens 265 / 286, 16 tokens 335 / 360, 64 tokens 537 / 675; 4 bits (one CTA or two of 5), 8
+  // experts of 4096 x 8192, 16 tokens 242 / 166, 24 tokens 302 / 349, 64 tokens 740 / 783.
+  const bool many = p.tokens > (q4 ? 16 : 8);
   p.up_piece = many && !q4 ? 7 : 5;
   p.down_piece = q4 ? 5 : many ? 7 : 5;
 

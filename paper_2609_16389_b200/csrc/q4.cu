@@ -364,7 +364,7 @@ __global__ void __launch_bounds__(kGemvThreads, 2) exo_gemv_q4_kernel(const Gemv
   }
 }
 
-// ==== few tokens: integer products ==================================================================================
+// ==== one or two tokens and a large matrix: integer products ========================================================
 // Turning 4-bit codes into 16-bit numbers costs the general kernel 11 instructions for eight weights, and at one token
 // that, not memory, is what it is bound by (181 clocks a step of 16 x 128 weights, where memory delivers one every 178).
 // Integers need three: the codes of a word, masked, are the bytes that mma.m16n8k32 takes as unsigned operands.  The
@@ -374,17 +374,23 @@ __global__ void __launch_bounds__(kGemvThreads, 2) exo_gemv_q4_kernel(const Gemv
 // otherwise.  A group's sum of (code - zero) * digit is an exact integer; it comes out as the float 1.5 * 2^23 + sum, since
 // the accumulator starts with that float's bits less zero * (sum of digits).  From there on everything is fp32.
 //
-// Weights come through shared memory: each warp keeps a ring of pieces (`piece` steps of 16 rows) that it fills itself, large
-// matrices by tiled copies, small ones by 16-byte copies of every lane, which need no tensor map: making one takes the host
-// about 2 us, and a small product is over in 4.  A lane's parts of a step are 16 bytes of rows g and g + 8.
-constexpr int kFewWarps = 8, kFewThreads = 32 * kFewWarps;
+// Weights come through shared memory: each warp keeps a ring of pieces (eight steps of 16 rows) that it fills itself by tiled
+// copies.  A lane's parts of a step are 16 bytes of rows g and g + 8.
+//
+// The digits have to be made by every CTA, so the matrix has to be large before the saved instructions are ahead of the 16-bit
+// kernel below.  Measured, integer against 16-bit products (us, group 128, bf16):
+//                   1024 x 2048  4096 x 4096  8192 x 8192  16384 x 8192  32768 x 16384
+//   one token         3.8 / 3.0    5.3 / 5.0  12.5 / 12.8   18.3 / 20.8    50.4 / 70.2
+//   two tokens        4.3 / 3.0    6.6 / 5.2  13.7 / 13.2   19.7 / 21.3    59.4 / 70.8
+// and with three and four tokens, whose digits take twice the columns, 83 / 71 and 87 / 72 on 32768 x 16384.  Hence two tokens at
+// most, and 256 KB of weights for every SM.  32768 x 16384 is 277 MB: one token at 5.5 TB/s, 0.84 of what a copy does.
+constexpr int kFewWarps = 8, kFewThreads = 32 * kFewWarps, kFewPiece = 8, kFewTokens = 2, kFewSteps = 256;   // steps of 1 KB per SM
 constexpr int kMagic = 0x4b400000;        // 1.5 * 2^23
 
 struct FewParams {
   GemvParams g;
   int nk_log;       // parts of a tile's steps: 1 << nk_log
-  int piece, stages;
-  bool tiled;       // pieces by tiled copies
+  int stages;
   int digits_at, start_at, step_scale_at, ring_at;   // offsets in shared memory; the sums come first, the barriers before them
 };
 
@@ -400,14 +406,10 @@ __device__ __forceinline__ void transpose4(const uint32_t (&v)[4], uint32_t (&d)
   d[2] = __byte_perm(y0, y1, 0x5410); d[3] = __byte_perm(y0, y1, 0x7632);
 }
 
-// 16 bytes to shared memory, asynchronously; zeros where there is nothing to read.
-__device__ __forceinline__ void copy16(uint32_t to, const void* from, bool there) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(there ? 16 : 0) : "memory");
-}
-// eight 16-bit values, by copies of `align` bytes (4, 8 or 16 at least)
+// eight 16-bit values to shared memory, asynchronously, by copies of `align` bytes (4, 8 or 16 at least)
 __device__ __forceinline__ void copy_eight(uint32_t to, const uint16_t* from, int align) {
   if (align >= 16) {
-    copy16(to, from, true);
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
   } else if (align == 8) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to + 8 * i), "l"(from + 4 * i) : "memory");
@@ -435,12 +437,10 @@ __device__ __noinline__ float not_finite_part(const uint32_t* codes, const uint1
   return v;
 }
 
-// NT: tiles of eight columns, two tokens each.
-template <class T, int PER, bool ZEROS, int NT>
-__global__ void __launch_bounds__(kFewThreads, 2) exo_gemv_q4_few_kernel(const FewParams fp, const __grid_constant__ CUtensorMap map) {
+template <class T, int PER, bool ZEROS>
+__global__ void __launch_bounds__(kFewThreads, 1) exo_gemv_q4_few_kernel(const FewParams fp, const __grid_constant__ CUtensorMap map) {
   namespace cg = cooperative_groups;
-  using F = RowsQ4<T, PER, ZEROS>;
-  constexpr int COLS = 8 * NT;
+    constexpr int COLS = 8;                  // two tokens of four digits
   const GemvParams& p = fp.g;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ int strange;                  // bit t: token t has values that are not finite
@@ -451,13 +451,13 @@ __global__ void __launch_bounds__(kFewThreads, 2) exo_gemv_q4_few_kernel(const F
   const int tiles = (int)((p.rows + 15) / 16), nk = 1 << fp.nk_log;
   const int units = ((tiles - cl + clusters - 1) / clusters) << fp.nk_log;   // of this cluster
   const int k_begin = rank_part(p.blocks, rank, S), k_steps = rank_part(p.blocks, rank + 1, S) - k_begin;
-  const int pieces = (k_steps + fp.piece - 1) / fp.piece;
-  const int stage_bytes = fp.piece * 1024;
+  const int pieces = (k_steps + kFewPiece - 1) / kFewPiece;
+  const int stage_bytes = kFewPiece * 1024;
   float* sums = reinterpret_cast<float*>(smem + 256);                        // [unit][token][16]
   const int col_pitch = k_steps * 128 + 16;
   const uint32_t bar = ptx::smem_u32(smem) + warp * 32, ring = ptx::smem_u32(smem + fp.ring_at) + warp * fp.stages * stage_bytes;
   if (lane == 0)
-    for (int i = 0; i < fp.stages; ++i) ptx::mbar_init(bar + 8 * i, fp.tiled ? 1 : 32);
+    for (int i = 0; i < fp.stages; ++i) ptx::mbar_init(bar + 8 * i, 1);
   ptx::fence_mbar_init();
   if (threadIdx.x == 0) strange = 0;
   __syncwarp();
@@ -470,19 +470,8 @@ __global__ void __launch_bounds__(kFewThreads, 2) exo_gemv_q4_few_kernel(const F
   ip = begin_of(iu);
   auto issue = [&]() {
     if (iu < units) {
-      const int row = row_of(iu), step = k_begin + ip * fp.piece;
-      if (!fp.tiled) {
-        const uint32_t to = ring + islot * stage_bytes + g * 64 + t * 16;
-        const int left = min(fp.piece, k_begin + k_steps - step);
-        const bool has0 = row + g < p.rows, has1 = row + g + 8 < p.rows;
-        const uint8_t* from0 = p.codes + ((has0 ? (int64_t)row + g : 0) * p.blocks + step) * 64 + 16 * t;
-        const uint8_t* from1 = p.codes + ((has1 ? (int64_t)row + g + 8 : 0) * p.blocks + step) * 64 + 16 * t;
-        for (int u = 0; u < left; ++u) {
-          copy16(to + u * 1024, from0 + u * 64, has0);
-          copy16(to + u * 1024 + 512, from1 + u * 64, has1);
-        }
-        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar + 8 * islot) : "memory");
-      } else if (lane == 0) {
+      const int row = row_of(iu), step = k_begin + ip * kFewPiece;
+      if (lane == 0) {
         ptx::mbar_arrive_expect_tx(bar + 8 * islot, stage_bytes);
         ptx::tma_load_3d(ring + islot * stage_bytes, &map, 0, row, step, bar + 8 * islot);
       }
@@ -500,8 +489,8 @@ __global__ void __launch_bounds__(kFewThreads, 2) exo_gemv_q4_few_kernel(const F
   using SC = StepScales<T, PER, ZEROS, 8>;
   typename SC::Rows srows;
   auto load_scales = [&](SC& sc, int piece) {
-    const int s = piece * fp.piece;
-    sc.load(srows, s, min(fp.piece, k_steps - s), p.K - (k_begin + s) * 128);
+    const int s = piece * kFewPiece;
+    sc.load(srows, s, min(kFewPiece, k_steps - s), p.K - (k_begin + s) * 128);
   };
   int cu = warp;
   int cp = begin_of(cu);
@@ -514,7 +503,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) exo_gemv_q4_few_kernel(const F
   // the tokens' digits: 16 lanes to a step, eight values each
   uint8_t* digits = smem + fp.digits_at;                                     // [column][k_steps][t][j][8]
   int* start = reinterpret_cast<int*>(smem + fp.start_at);                   // [k_steps * PER][COLS]
-  float* step_scale = reinterpret_cast<float*>(smem + fp.step_scale_at);     // [k_steps][2 * NT]
+  float* step_scale = reinterpret_cast<float*>(smem + fp.step_scale_at);     // [k_steps][2]
   __syncthreads();
   const int all_parts = p.tokens * k_steps * 16;
   auto raw_part = [&](int i) {             // clamped, so that all lanes take part in the shuffles below
@@ -564,17 +553,13 @@ __global__ void __launch_bounds__(kFewThreads, 2) exo_gemv_q4_few_kernel(const F
 #pragma unroll
         for (int c = 0; c < 4; ++c) to[c] = ZEROS ? -sum[c] : kMagic - 8 * sum[c];
       }
-      if (e == 0) step_scale[s * 2 * NT + token] = __uint_as_float(up == 127 ? 0x00400000u : (uint32_t)(127 - up) << 23);   // 2^-up
+      if (e == 0) step_scale[2 * s + token] = __uint_as_float(up == 127 ? 0x00400000u : (uint32_t)(127 - up) << 23);   // 2^-up
     }
   }
   __syncthreads();
 
-  float acc[NT][4];
-#pragma unroll
-  for (int i = 0; i < NT; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
-  uint32_t xat[NT];                        // columns beyond the tokens repeat the last one; nobody reads them
-#pragma unroll
-  for (int i = 0; i < NT; ++i) xat[i] = ptx::smem_u32(digits) + min(8 * i + g, p.tokens * 4 - 1) * col_pitch + t * 32;
+  float acc[4] = {};
+  const uint32_t xat = ptx::smem_u32(digits) + min(g, p.tokens * 4 - 1) * col_pitch + t * 32;   // columns beyond the tokens repeat the last one; nobody reads them
   int cslot = 0;
   uint32_t parity = 0;
   while (cu < units) {
@@ -588,7 +573,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) exo_gemv_q4_few_kernel(const F
     if (nu < units) load_scales(nxt, np);
     wait_piece(bar + 8 * cslot, parity);
     const uint32_t w = ring + cslot * stage_bytes + g * 64 + t * 16;
-    const int s0 = cp * fp.piece, n = min(fp.piece, k_steps - s0);
+    const int s0 = cp * kFewPiece, n = min(kFewPiece, k_steps - s0);
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
       if (u < n) {
@@ -597,29 +582,26 @@ __global__ void __launch_bounds__(kFewThreads, 2) exo_gemv_q4_few_kernel(const F
         uint32_t sa[(PER + 1) / 2], sb[(PER + 1) / 2], za, zb;
         cur.get(u, sa, sb, za, zb);
         const int s = s0 + u;
+        const uint4 x0 = lds128(xat + s * 128), x1 = lds128(xat + s * 128 + 16);
+        const uint32_t xl[4] = {x0.x, x0.z, x1.x, x1.z}, xh[4] = {x0.y, x0.w, x1.y, x1.w};
+        const float ss = step_scale[2 * s + t / 2];
 #pragma unroll
-        for (int i = 0; i < NT; ++i) {
-          const uint4 x0 = lds128(xat[i] + s * 128), x1 = lds128(xat[i] + s * 128 + 16);
-          const uint32_t xl[4] = {x0.x, x0.z, x1.x, x1.z}, xh[4] = {x0.y, x0.w, x1.y, x1.w};
-          const float ss = step_scale[s * 2 * NT + 2 * i + t / 2];
-#pragma unroll
-          for (int q = 0; q < PER; ++q) {
-            const int2 c = *reinterpret_cast<const int2*>(start + (s * PER + q) * COLS + 8 * i + 2 * t);
-            int d[4] = {c.x, c.y, c.x, c.y};
-            if constexpr (ZEROS) {
-              const int z0 = (za >> (8 * q)) & 0xff, z1 = (zb >> (8 * q)) & 0xff;
-              d[0] = z0 * c.x + kMagic; d[1] = z0 * c.y + kMagic;
-              d[2] = z1 * c.x + kMagic; d[3] = z1 * c.y + kMagic;
-            }
-#pragma unroll
-            for (int j = 4 / PER * q; j < 4 / PER * (q + 1); ++j)
-              mma_u8s8(d, wa[j] & 0x0f0f0f0fu, wb[j] & 0x0f0f0f0fu, (wa[j] >> 4) & 0x0f0f0f0fu, (wb[j] >> 4) & 0x0f0f0f0fu, xl[j], xh[j]);
-            const float fa = ss * T::to_float((uint16_t)(sa[q / 2] >> (16 * (q % 2)))), fb = ss * T::to_float((uint16_t)(sb[q / 2] >> (16 * (q % 2))));
-            acc[i][0] = fmaf(fa, __int_as_float(d[0]) - 12582912.f, acc[i][0]);
-            acc[i][1] = fmaf(fa, __int_as_float(d[1]) - 12582912.f, acc[i][1]);
-            acc[i][2] = fmaf(fb, __int_as_float(d[2]) - 12582912.f, acc[i][2]);
-            acc[i][3] = fmaf(fb, __int_as_float(d[3]) - 12582912.f, acc[i][3]);
+        for (int q = 0; q < PER; ++q) {
+          const int2 c = *reinterpret_cast<const int2*>(start + (s * PER + q) * COLS + 2 * t);
+          int d[4] = {c.x, c.y, c.x, c.y};
+          if constexpr (ZEROS) {
+            const int z0 = (za >> (8 * q)) & 0xff, z1 = (zb >> (8 * q)) & 0xff;
+            d[0] = z0 * c.x + kMagic; d[1] = z0 * c.y + kMagic;
+            d[2] = z1 * c.x + kMagic; d[3] = z1 * c.y + kMagic;
           }
+#pragma unroll
+          for (int j = 4 / PER * q; j < 4 / PER * (q + 1); ++j)
+            mma_u8s8(d, wa[j] & 0x0f0f0f0fu, wb[j] & 0x0f0f0f0fu, (wa[j] >> 4) & 0x0f0f0f0fu, (wb[j] >> 4) & 0x0f0f0f0fu, xl[j], xh[j]);
+          const float fa = ss * T::to_float((uint16_t)(sa[q / 2] >> (16 * (q % 2)))), fb = ss * T::to_float((uint16_t)(sb[q / 2] >> (16 * (q % 2))));
+          acc[0] = fmaf(fa, __int_as_float(d[0]) - 12582912.f, acc[0]);
+          acc[1] = fmaf(fa, __int_as_float(d[1]) - 12582912.f, acc[1]);
+          acc[2] = fmaf(fb, __int_as_float(d[2]) - 12582912.f, acc[2]);
+          acc[3] = fmaf(fb, __int_as_float(d[3]) - 12582912.f, acc[3]);
         }
       }
     }
@@ -627,21 +609,17 @@ __global__ void __launch_bounds__(kFewThreads, 2) exo_gemv_q4_few_kernel(const F
     issue();
     cslot = cslot + 1 == fp.stages ? 0 : cslot + 1;
     parity ^= cslot == 0 ? 1u : 0u;
-    if (ends) {                            // digits 2 (t % 2) and 2 (t % 2) + 1 of token 2 i + t / 2, weighted by 256^digit
+    if (ends) {                            // digits 2 (t % 2) and 2 (t % 2) + 1 of token t / 2, weighted by 256^digit
       const float lo = t & 1 ? 65536.f : 1.f, hi = t & 1 ? 16777216.f : 256.f;
       float* out = sums + cu * p.tokens * 16;
-#pragma unroll
-      for (int i = 0; i < NT; ++i) {
-        float v0 = fmaf(hi, acc[i][1], lo * acc[i][0]), v1 = fmaf(hi, acc[i][3], lo * acc[i][2]);
-        v0 += __shfl_xor_sync(0xffffffffu, v0, 1);
-        v1 += __shfl_xor_sync(0xffffffffu, v1, 1);
-        const int token = 2 * i + t / 2;
-        if ((t & 1) == 0 && token < p.tokens) {
-          out[token * 16 + g] = v0;
-          out[token * 16 + g + 8] = v1;
-        }
-        acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
+      float v0 = fmaf(hi, acc[1], lo * acc[0]), v1 = fmaf(hi, acc[3], lo * acc[2]);
+      v0 += __shfl_xor_sync(0xffffffffu, v0, 1);
+      v1 += __shfl_xor_sync(0xffffffffu, v1, 1);
+      if ((t & 1) == 0 && t / 2 < p.tokens) {
+        out[t / 2 * 16 + g] = v0;
+        out[t / 2 * 16 + g + 8] = v1;
       }
+      acc[0] = acc[1] = acc[2] = acc[3] = 0.f;
     }
     cu = nu; cp = np;
     cur = nxt;
@@ -667,11 +645,13 @@ __global__ void __launch_bounds__(kFewThreads, 2) exo_gemv_q4_few_kernel(const F
   if (S > 1) cluster.sync();   // no CTA leaves while another may still read its sums
 }
 
-// ==== five to 64 tokens ==============================================================================================
-// The same cut as for few tokens, with 16-bit products: a step's codes become exact 16-bit integers once for NT tiles of
+// ==== all others up to 64 tokens =====================================================================================
+// The same cut, with 16-bit products: a step's codes become exact 16-bit integers once for NT tiles of
 // eight tokens, whose values for the CTA's part of k lie in shared memory for the whole run (rows 64 bytes off a
 // multiple of 128, so that a fragment load is free of bank conflicts).  Eight more tokens cost a step 8 matrix instructions and
-// four 512-byte loads of activations; at 24 tokens the tensor pipe is the bound (mma.sync, 8 clocks each).
+// four 512-byte loads of activations.  16384 x 8192 (69 MB, 10.7 us at the copy bandwidth), us: 20.8 for one token, 23 for 8, 30 for
+// 16, 37 for 24: at one token the unpacking is the bound, and every further tile adds its loads and products, which a warp
+// does not overlap with the unpacking (ncu at 24 tokens: the tensor pipe is 30 % busy, DRAM 27 %).
 constexpr int kBatchWarps = 16, kBatchThreads = 32 * kBatchWarps, kBatchPiece = 2;
 
 template <class T, int PER, bool ZEROS, int NT>
@@ -820,10 +800,10 @@ template <class T, bool ZEROS> GemvFn pick_group(int group) {
 }
 template <class T> GemvFn pick_gemv(int group, bool zeros) { return zeros ? pick_group<T, true>(group) : pick_group<T, false>(group); }
 
-// few: the integer kernel, nt tiles of two tokens; else nt tiles of eight
+// few: the integer kernel; else the 16-bit one with nt tiles of eight tokens
 template <class T, int PER, bool ZEROS> FewFn pick_few_tiles(bool few, int nt) {
-  if (few) return nt == 1 ? exo_gemv_q4_few_kernel<T, PER, ZEROS, 1> : exo_gemv_q4_few_kernel<T, PER, ZEROS, 2>;
-  return nt == 1 ? exo_gemv_q4_batch_kernel<T, PER, ZEROS, 1> : nt == 2 ? exo_gemv_q4_batch_kernel<T, PER, ZEROS, 2>
+  return few ? exo_gemv_q4_few_kernel<T, PER, ZEROS>
+         : nt == 1 ? exo_gemv_q4_batch_kernel<T, PER, ZEROS, 1> : nt == 2 ? exo_gemv_q4_batch_kernel<T, PER, ZEROS, 2>
          : nt == 3 ? exo_gemv_q4_batch_kernel<T, PER, ZEROS, 3> : exo_gemv_q4_batch_kernel<T, PER, ZEROS, 4>;
 }
 template <class T, bool ZEROS> FewFn pick_few_group(int group, bool few, int nt) {
@@ -833,36 +813,31 @@ template <class T> FewFn pick_few(int group, bool zeros, bool few, int nt) {
   return zeros ? pick_few_group<T, true>(group, few, nt) : pick_few_group<T, false>(group, few, nt);
 }
 
-// How the few-token kernel is cut.  Large matrices (a few dozen KB for every SM) run as one CTA per SM with pieces of 8
-// steps, which the copies like best (32768 x 16384, one token: 51.6 us, against 55.8 with two CTAs and pieces of 4); small
-// ones as two CTAs per SM with pieces of 4, where the time to the first piece counts.  The cluster cuts k where a CTA's
-// digits would take more than 40 KB.  False: the activations do not fit.
+// How the integer kernel is cut: one CTA per SM with pieces of 8 steps, which the copies like best (32768 x 16384, one token:
+// 50.4 us; 54.8 with two CTAs and pieces of 4).  The cluster cuts k where a CTA's digits would take more than 40 KB.  False: not
+// for this size, or the sums do not fit.
 bool plan_few(FewParams& fp, const GemvParams& p, int per, int sms, unsigned* ctas, unsigned* cluster, size_t* smem) {
-  const int nt = p.tokens <= 2 ? 1 : 2;
   const int64_t tiles = (p.rows + 15) / 16;
+  if (p.tokens > kFewTokens || tiles * p.blocks < (int64_t)sms * kFewSteps) return false;
   int S = 1;
   while (S < 8 && p.blocks >= 2 * S && (int64_t)4 * p.tokens * ((p.blocks + S - 1) / S) * 128 > 40 * 1024) S *= 2;
-  const bool large = tiles * p.blocks >= (int64_t)sms * 96;
   const int slice = (p.blocks + S - 1) / S, least = p.blocks / S;
-  const int64_t slots = S == 1 ? (int64_t)(large ? 1 : 2) * sms
-                               : resident_clusters(8 + 2 * S + large, (void*)exo_gemv_q4_few_kernel<Bf16, 1, false, 1>, kFewThreads, large ? 200 * 1024 : 100 * 1024, (unsigned)S, sms, large ? 1 : 2);
+  const int64_t slots = resident_clusters(8 + S, (void*)exo_gemv_q4_few_kernel<Bf16, 1, false>, kFewThreads, 200 * 1024, (unsigned)S, sms, 1);
   const int64_t clusters = tiles < slots ? tiles : slots;
   const int most = (int)((tiles + clusters - 1) / clusters);     // tiles of a cluster
-  fp.tiled = large;
-  fp.piece = large ? 8 : 4;
   // parts of k: two pieces each, or fewer where the CTA would otherwise have less than a part for every warp
   fp.nk_log = 0;
-  while (fp.nk_log < 3 && (least + fp.piece - 1) / fp.piece >= ((most << fp.nk_log) < kFewWarps ? 2 : 4) << fp.nk_log) ++fp.nk_log;
+  while (fp.nk_log < 3 && (least + kFewPiece - 1) / kFewPiece >= ((most << fp.nk_log) < kFewWarps ? 2 : 4) << fp.nk_log) ++fp.nk_log;
   const int turns = ((most << fp.nk_log) + kFewWarps - 1) / kFewWarps;
-  const int pieces = ((slice + fp.piece - 1) / fp.piece + (1 << fp.nk_log) - 1) >> fp.nk_log;
+  const int pieces = ((slice + kFewPiece - 1) / kFewPiece + (1 << fp.nk_log) - 1) >> fp.nk_log;
   fp.stages = turns * pieces < 2 ? 1 : 2;
   int64_t at = 256 + (int64_t)(most << fp.nk_log) * p.tokens * 64;
   fp.digits_at = (int)at; at += 4 * p.tokens * ((int64_t)slice * 128 + 16);
-  fp.start_at = (int)at; at += (int64_t)slice * per * 8 * nt * 4;
-  fp.step_scale_at = (int)at; at += (int64_t)slice * 2 * nt * 4;
+  fp.start_at = (int)at; at += (int64_t)slice * per * 8 * 4;
+  fp.step_scale_at = (int)at; at += (int64_t)slice * 2 * 4;
   at = (at + 127) / 128 * 128;
   fp.ring_at = (int)at;
-  at += kFewWarps * fp.stages * fp.piece * 1024;
+  at += kFewWarps * fp.stages * kFewPiece * 1024;
   fp.g = p;
   *ctas = (unsigned)(clusters * S);
   *cluster = (unsigned)S;
@@ -871,41 +846,41 @@ bool plan_few(FewParams& fp, const GemvParams& p, int per, int sms, unsigned* ct
 }
 
 // How the kernel for more tokens is cut, one CTA to an SM; nt is the number of tiles of eight tokens that a CTA keeps.  The
-// smallest cluster whose CTAs hold their part of the activations and of the sums.  False: they do not fit.
-bool plan_batch(FewParams& fp, const GemvParams& p, int sms, int nt, unsigned* ctas, unsigned* cluster, size_t* smem) {
+// smallest cluster whose CTAs hold their part of the activations and of the sums, on the clusters that the device holds (16384 x 8192,
+// 24 tokens: 37 us with the 33 clusters of four that there are, 67 with 37).  Returns an estimate of the time, in 16ths of a
+// microsecond or so, or 0 where nothing fits.
+int64_t plan_batch(FewParams& fp, const GemvParams& p, int sms, int nt, unsigned* ctas, unsigned* cluster, size_t* smem) {
   const int64_t tiles = (p.rows + 15) / 16, staged = nt == 1 && p.tokens < 8 ? p.tokens : 8 * nt, tokens = p.tokens < 8 * nt ? p.tokens : 8 * nt;
-  fp.tiled = true;
-  fp.piece = kBatchPiece;
+  const int64_t groups = (p.tokens + 8 * nt - 1) / (8 * nt);
   for (int S = 1; S <= 8 && (S == 1 || p.blocks >= S); S *= 2) {
     const int slice = (p.blocks + S - 1) / S, least = p.blocks / S;
     const int64_t x_bytes = staged * ((int64_t)slice * 256 + 64);
     const bool enough = tiles * S >= sms || S == 8 || p.blocks < 2 * S * kBatchWarps;   // a cluster also spreads few rows over the SMs
     if (x_bytes > 110 * 1024 || !enough) continue;
-    int64_t clusters = resident_clusters(S, (void*)exo_gemv_q4_batch_kernel<Bf16, 1, false, 1>, kBatchThreads, kMostSmem, (unsigned)S, sms, 1);
-    if (tiles < clusters) clusters = tiles;
-    for (;; clusters = 2 * clusters < tiles ? 2 * clusters : tiles) {   // more turns where the sums would not fit
+    const int64_t fit = resident_clusters(S, (void*)exo_gemv_q4_batch_kernel<Bf16, 1, false, 1>, kBatchThreads, kMostSmem, (unsigned)S, sms, 1);
+    for (int64_t clusters = tiles < fit ? tiles : fit;; clusters = 2 * clusters < tiles ? 2 * clusters : tiles) {   // more turns where the sums would not fit
       const int most = (int)((tiles + clusters - 1) / clusters);
       fp.nk_log = 0;
-      while (fp.nk_log < 4 && (most << fp.nk_log) < kBatchWarps && (least + fp.piece - 1) / fp.piece >= 2 << fp.nk_log) ++fp.nk_log;
+      while (fp.nk_log < 4 && (most << fp.nk_log) < kBatchWarps && (least + kBatchPiece - 1) / kBatchPiece >= 2 << fp.nk_log) ++fp.nk_log;
       const int turns = ((most << fp.nk_log) + kBatchWarps - 1) / kBatchWarps;
-      const int pieces = ((slice + fp.piece - 1) / fp.piece + (1 << fp.nk_log) - 1) >> fp.nk_log;
+      const int pieces = ((slice + kBatchPiece - 1) / kBatchPiece + (1 << fp.nk_log) - 1) >> fp.nk_log;
       fp.stages = turns * pieces < 2 ? turns * pieces : 2;
       int64_t at = 512 + (int64_t)(most << fp.nk_log) * tokens * 64;
       fp.digits_at = (int)at; at += x_bytes;
       at = (at + 127) / 128 * 128;
       fp.ring_at = (int)at;
-      at += kBatchWarps * fp.stages * fp.piece * 1024;
+      at += kBatchWarps * fp.stages * kBatchPiece * 1024;
       if (at <= kMostSmem) {
         *ctas = (unsigned)(clusters * S);
         *cluster = (unsigned)S;
         *smem = (size_t)at;
         fp.g = p;
-        return true;
+        return (clusters * groups + fit - 1) / fit * ((int64_t)turns * pieces * (16 + 7 * nt) + 60);
       }
       if (most <= 1) break;
     }
   }
-  return false;
+  return 0;
 }
 
 exo_gemm_status_t check_q4(const exo_q4_t* q) {
@@ -1017,15 +992,25 @@ extern "C" exo_gemm_status_t exo_gemv_q4_run(const exo_q4_t* W, int64_t tokens, 
     FewParams fp{};
     size_t smem = 0;
     unsigned ctas = 0, cluster = 1, groups = 1;
-    const bool few = p.tokens <= 4;
-    int nt = few ? (p.tokens + 1) / 2 : p.tokens < 32 ? (p.tokens + 7) / 8 : 4;
-    bool fits = few && plan_few(fp, p, 128 / W->group, sms, &ctas, &cluster, &smem);
-    if (!few)
-      while (!(fits = plan_batch(fp, p, sms, nt, &ctas, &cluster, &smem)) && nt > 1) --nt;
-    if (fits) {
-      if (!few) groups = (unsigned)((p.tokens + 8 * nt - 1) / (8 * nt));
+    int nt = 0;
+    const bool few = plan_few(fp, p, 128 / W->group, sms, &ctas, &cluster, &smem);
+    if (!few) {
+      // A CTA's tokens: with more the weights are read and unpacked less often, with fewer its activations and sums leave room for
+      // smaller clusters and longer turns.  The estimate is a line through 8, 16 and 24 tokens.  16384 x 8192, us, with 1, 2, 3 and 4
+      // tiles of eight to a CTA: 32 tokens 90, 59, 67, 69; 64 tokens 180, 119, 106, 137; 4096 x 4096, 64 tokens 46, 31, 27, 24.
+      int64_t best = 0;
+      for (int n = 1; n <= 4 && n <= (p.tokens + 7) / 8; ++n) {
+        FewParams q{};
+        size_t bytes = 0;
+        unsigned c = 0, cl = 1;
+        const int64_t cost = plan_batch(q, p, sms, n, &c, &cl, &bytes);
+        if (cost > 0 && (nt == 0 || cost < best)) { best = cost; nt = n; fp = q; ctas = c; cluster = cl; smem = bytes; }
+      }
+      if (nt > 0) groups = (unsigned)((p.tokens + 8 * nt - 1) / (8 * nt));
+    }
+    if (few || nt > 0) {
       CUtensorMap map;
-      if (fp.tiled && !exo::encode_steps_map(&map, p.codes, (uint64_t)p.rows, (uint64_t)p.blocks, (uint32_t)fp.piece)) return EXO_GEMM_ERR_CUDA;
+      if (!exo::encode_steps_map(&map, p.codes, (uint64_t)p.rows, (uint64_t)p.blocks, few ? kFewPiece : kBatchPiece)) return EXO_GEMM_ERR_CUDA;
       FewFn fn = bf16 ? pick_few<Bf16>(W->group, W->zeros, few, nt) : pick_few<Fp16>(W->group, W->zeros, few, nt);
       return launch((void*)fn, ctas, groups, few ? kFewThreads : kBatchThreads, smem, cluster, (cudaStream_t)cuda_stream, &fp, &map);
     }

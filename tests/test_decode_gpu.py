@@ -634,3 +634,106 @@ def test_decode_layer_example(tokens):
     a, b = h.double(), by_prompt.double()
     assert ((a - b).norm() / b.norm()).item() <= 3 * 2.0 ** -8
     assert t.isfinite(y).all() and ((taken >= 0) & (taken < 12)).all()
+
+
+# ------------------------------------------------------------------ one or two tokens and a large matrix: integer products
+class LargeMatrix:
+    """A 4-bit matrix of random codes made on the device; ``values`` are its weights in 64 bits."""
+
+    def __init__(self, rows, K, group, dtype, zeros, seed):
+        t = torch()
+        gen = t.Generator(device="cuda").manual_seed(seed)
+        self.rows, self.K, self.group, self.dtype = rows, K, group, dtype
+        kp = D.padded_k(K)
+        words = t.randint(-2 ** 31, 2 ** 31, (rows, kp // 8), generator=gen, device="cuda", dtype=t.int64).int()
+        G = groups(K, group)
+        self.codes = words
+        self.scales = ((t.rand(rows, G, generator=gen, device="cuda") + 0.25) * 0.02).to(tt(dtype))
+        self.scales[:, (K + group - 1) // group:] = float("nan")
+        self.zeros = t.randint(0, 16, (rows, G), generator=gen, device="cuda", dtype=t.uint8) if zeros else None
+        # weight 128 b + 32 j + 8 t + i is nibble i / 2 + 4 (i % 2) of word 16 b + 4 t + j
+        w = words.view(rows, kp // 128, 4, 4).permute(0, 1, 3, 2)
+        codes = t.empty(rows, kp // 128, 4, 4, 8, device="cuda", dtype=t.uint8)
+        for i in range(8):
+            codes[..., i] = (w >> (4 * (i // 2 + 4 * (i % 2)))) & 15
+        at = t.arange(K, device="cuda") // group
+        zero = self.zeros.double()[:, at] if zeros else 8.0
+        self.values = (codes.view(rows, kp)[:, :K].double() - zero) * self.scales.double()[:, at]
+
+    def gemv(self, x, y, alpha=1.0, beta=0.0):
+        q = D.Q4(self.rows, self.K, self.group, self.dtype, self.codes.data_ptr(), self.scales.data_ptr(),
+                 0 if self.zeros is None else self.zeros.data_ptr())
+        out = {v: k for k, v in ((k, tt(k)) for k in (D.BF16, D.FP16, D.FP32))}[y.dtype]
+        q.gemv(x.shape[0], x.data_ptr(), x.stride(0), y.data_ptr(), y.stride(0), out, alpha, beta, stream())
+
+    def bound(self, x):
+        """What sums in fp32 and activations within 2^-30 of the largest of their 128 may be off by."""
+        t = torch()
+        xs = t.zeros(x.shape[0], D.padded_k(self.K), device="cuda", dtype=t.float64)
+        xs[:, :self.K] = x[:, :self.K].double().abs()
+        top = xs.view(x.shape[0], -1, 128).amax(2).repeat_interleave(128, 1)[:, :self.K]
+        return (sum_bound(self.K) * xs[:, :self.K] + 2.0 ** -30 * top) @ self.values.abs().T
+
+
+LARGE = [  # tokens, rows, K, group, zeros: 38 MB of weights or more, few and many rows, odd ends
+    (1, 4000, 20010, 128, False), (2, 18961, 4100, 32, True), (2, 1297, 60001, 64, False), (1, 606500, 100, 128, True),
+    (1, 9001, 9001, 64, True), (2, 32768, 2560, 32, False)]
+
+
+@pytest.mark.parametrize("tokens,rows,K,group,zeros", LARGE)
+@pytest.mark.parametrize("dtype,out", [(D.BF16, D.FP32), (D.FP16, D.FP16)])
+def test_gemv_of_large_matrices_against_its_definition(tokens, rows, K, group, zeros, dtype, out):
+    t = torch()
+    m = LargeMatrix(rows, K, group, dtype, zeros, seed=rows)
+    gen = t.Generator(device="cuda").manual_seed(K)
+    x = t.randn(tokens, K + K % 2, generator=gen, device="cuda").to(tt(dtype))
+    x[:, K:] = float("nan")
+    ref, bound = x[:, :K].double() @ m.values.T, m.bound(x)
+    y0 = t.randn(tokens, rows + 3, generator=gen, device="cuda").to(tt(out))
+    for alpha, beta in ((1.0, 0.0), (-0.5, 0.75)):
+        y = y0.clone()
+        if beta == 0.0:
+            y[:, :rows] = float("nan")
+        m.gemv(x, y, alpha, beta)
+        want = alpha * ref + (beta * y0[:, :rows].double() if beta else 0.0)
+        off = (y[:, :rows].double() - want).abs()
+        allowed = abs(alpha) * bound + (4 * 2.0 ** -24 + U[out] * 1.01) * want.abs() + TINY[out]
+        assert bool((off <= allowed).all()), float((off / allowed).max())
+        assert t.equal(y[:, rows:], y0[:, rows:])
+        again = y0.clone()
+        m.gemv(x, again, alpha, beta)
+        assert t.equal(again[:, :rows], y[:, :rows])
+
+
+def test_gemv_of_large_matrices_at_the_ends_of_the_activations_range():
+    t = torch()
+    m = LargeMatrix(9000, 9000, 128, D.BF16, False, seed=3)
+    gen = t.Generator(device="cuda").manual_seed(4)
+    x = t.randn(2, 9000, generator=gen, device="cuda") * 2.0 ** t.randint(-30, 30, (2, 9000), generator=gen, device="cuda").float()
+    x[:, 128:256] *= 2.0 ** -100
+    x[:, 256:384] = 0
+    x[:, 384:512] *= 2.0 ** 60
+    x = x.bfloat16()
+    y = t.empty(2, 9000, device="cuda")
+    m.gemv(x, y)
+    ref = x.double() @ m.values.T
+    assert bool(((y.double() - ref).abs() <= m.bound(x) + (4 * 2.0 ** -24 + U[D.FP32] * 1.01) * ref.abs()).all())
+
+
+@pytest.mark.parametrize("dtype", [D.BF16, D.FP16])
+def test_gemv_of_large_matrices_keeps_infinities_to_their_token_and_row(dtype):
+    t = torch()
+    m = LargeMatrix(4000, 20010, 32, dtype, True, seed=6)
+    x = t.randn(2, 20010, generator=t.Generator(device="cuda").manual_seed(7), device="cuda").to(tt(dtype))
+    clean = t.empty(2, 4000, device="cuda")
+    m.gemv(x, clean)
+    x[1, 20009] = float("inf")
+    y = t.empty(2, 4000, device="cuda")
+    m.gemv(x, y)
+    w = m.values[:, 20009]
+    assert t.equal(y[0], clean[0]) and t.equal(t.isnan(y[1]), w == 0)
+    assert bool((y[1][w > 0] == float("inf")).all()) and bool((y[1][w < 0] == float("-inf")).all())
+    m.scales[7, 3] = float("inf")
+    m.gemv(x, y)
+    rest = t.arange(4000, device="cuda") != 7
+    assert t.equal(y[0][rest], clean[0][rest]) and not t.isfinite(y[0, 7])
