@@ -69,8 +69,8 @@ exo_gemm_status_t exo_q4_dequantize(const exo_q4_t* q, void* W, int64_t ldw, int
  * errors as above.
  *
  * Products are formed from the integers code - zero and a group's sum is multiplied by its scale in fp32; all further
- * sums are fp32.  From 5 tokens on the factors are the 16-bit activations and a group is summed in fp32.  Up to 4 tokens
- * they are integers of 30 bits that stand for the activations of 128 neighbouring k: exact for values down to 2^-22 (bf16) or
+ * sums are fp32.  The factors are the 16-bit activations and a group is summed in fp32; or, for one or two tokens and a large
+ * matrix, they are integers of 30 bits that stand for the activations of 128 neighbouring k: exact for values down to 2^-22 (bf16) or
  * 2^-19 (fp16) of the largest of the 128, and off by at most 2^-30 of that largest below; their group sums are exact.
  */
 exo_gemm_status_t exo_gemv_q4_run(const exo_q4_t* W, int64_t tokens, const void* X, int64_t ldx, void* Y, int64_t ldy,
