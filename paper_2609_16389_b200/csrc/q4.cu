@@ -74,12 +74,9 @@ __device__ __forceinline__ void store_eight(void* row, int k, int K, const uint3
     } else if constexpr (ALIGN == 8) {
 #pragma unroll
       for (int i = 0; i < BYTES; ++i) reinterpret_cast<uint2*>(p)[i] = make_uint2(w[2 * i], w[2 * i + 1]);
-    } else if constexpr (ALIGN == 4) {
-#pragma unroll
-      for (int i = 0; i < 2 * BYTES; ++i) reinterpret_cast<uint32_t*>(p)[i] = w[i];
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) reinterpret_cast<uint16_t*>(p)[i] = (uint16_t)(w[i / 2] >> (16 * (i % 2)));
+      for (int i = 0; i < 2 * BYTES; ++i) reinterpret_cast<uint32_t*>(p)[i] = w[i];
     }
     return;
   }
@@ -89,6 +86,20 @@ __device__ __forceinline__ void store_eight(void* row, int k, int K, const uint3
       if constexpr (BYTES == 4) reinterpret_cast<uint32_t*>(p)[i] = w[i];
       else reinterpret_cast<uint16_t*>(p)[i] = (uint16_t)(w[i / 2] >> (16 * (i % 2)));
     }
+}
+
+// Rows of 16-bit elements at odd addresses can be written by halves only, and a lane that wrote its own eight would touch a sector
+// for each: elements 0 .. 255 of a pass change their order in the warp's part of shared memory, so that neighbouring lanes write
+// neighbouring elements.  32768 x 4097, us: 98, against 359 without.  At multiples of 4 and 8 bytes the detour loses (111 / 78 and 92 /
+// 77), and so it does for reading, which finds the sector's rest in the L1 (164 / 171, 162 / 131 and 150 / 128).
+__device__ __forceinline__ void store_halves(uint4* mine, uint16_t* to, int left, const uint32_t (&w)[4]) {
+  const int lane = threadIdx.x & 31;
+  __syncwarp();                            // what was there has been read
+  mine[lane] = make_uint4(w[0], w[1], w[2], w[3]);
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (32 * i + lane < left) to[32 * i + lane] = reinterpret_cast<const uint16_t*>(mine)[32 * i + lane];
 }
 
 // a / N, correctly rounded (P. Markstein: the product with the rounded reciprocal, corrected by its exact remainder).
@@ -207,12 +218,18 @@ __global__ void __launch_bounds__(kQuantThreads) exo_q4_dequantize_kernel(const 
   const int64_t groups = row * (p.blocks * 128 / p.group);
   const uint32_t* codes = p.codes + row * p.blocks * 16 + 4 * (lane & 3) + ((lane & 15) >> 2);
   constexpr int N = 4;   // passes whose loads are in flight together
-  for (int k0 = seg * kQuantSegment + 8 * lane; k0 < k_end; k0 += N * 256) {
+  constexpr bool HALVES = ALIGN == 2;
+  __shared__ uint4 moved[HALVES ? kQuantThreads : 1];
+  for (int k0 = seg * kQuantSegment + 8 * lane; k0 - (HALVES ? 8 * lane : 0) < k_end; k0 += N * 256) {   // by halves all lanes take part
     uint32_t word[N];
     float s[N], zero[N];
 #pragma unroll
     for (int u = 0; u < N; ++u) {
       const int k = k0 + 256 * u;
+      if constexpr (HALVES) {
+        word[u] = 0;
+        s[u] = zero[u] = 0.f;
+      }
       if (k < k_end) {
         word[u] = __ldcs(codes + k / 128 * 16);
         s[u] = T::to_float(__ldg(p.scales + groups + (k >> group_log)));
@@ -222,7 +239,7 @@ __global__ void __launch_bounds__(kQuantThreads) exo_q4_dequantize_kernel(const 
 #pragma unroll
     for (int u = 0; u < N; ++u) {
       const int k = k0 + 256 * u;
-      if (k < k_end) {
+      if (k - (HALVES ? 8 * lane : 0) < k_end) {
         float v[8];
         uint32_t out[2 * BYTES];
 #pragma unroll
@@ -233,7 +250,8 @@ __global__ void __launch_bounds__(kQuantThreads) exo_q4_dequantize_kernel(const 
           if constexpr (WIDE) out[i] = __float_as_uint(v[i]);
           else out[i] = WT::pair(v[2 * i], v[2 * i + 1]);
         }
-        store_eight<BYTES, ALIGN>(dst, k, p.K, out);
+        if constexpr (HALVES) store_halves(moved + (threadIdx.x & ~31u), reinterpret_cast<uint16_t*>(dst) + (k - 8 * lane), min(p.K, k_end) - (k - 8 * lane), out);
+        else store_eight<BYTES, ALIGN>(dst, k, p.K, out);
       }
     }
   }
