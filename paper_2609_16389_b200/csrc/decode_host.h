@@ -108,7 +108,8 @@ inline int resident_clusters(int kind, void* fn, unsigned threads, size_t smem, 
 inline exo_gemm_status_t launch(void* fn, unsigned grid_x, unsigned grid_y, unsigned threads, size_t smem, unsigned cluster,
                                 cudaStream_t stream, void* params, void* params2 = nullptr, void* params3 = nullptr) {
   cudaError_t e;
-  if (smem > 48 * 1024 && (e = allow_smem(fn)) != cudaSuccess) return cuda_failed(e);
+  // without it a kernel has 48 KB, its own variables included: what it needs beyond `smem` is not known here
+  if (smem > 0 && (e = allow_smem(fn)) != cudaSuccess) return cuda_failed(e);
   cudaLaunchConfig_t lc{};
   lc.gridDim = dim3(grid_x, grid_y, 1);
   lc.blockDim = dim3(threads, 1, 1);

@@ -737,3 +737,28 @@ def test_gemv_of_large_matrices_keeps_infinities_to_their_token_and_row(dtype):
     m.gemv(x, y)
     rest = t.arange(4000, device="cuda") != 7
     assert t.equal(y[0][rest], clean[0][rest]) and not t.isfinite(y[0, 7])
+
+
+# ------------------------------------------------------------------ launches that no larger one has prepared
+FIRST = [  # T, H, F, E, shared, k, group: around the token counts at which the kernels' shared memory passes 48 KB
+    (20, 160, 96, 5, 0, 2, 0), (28, 160, 96, 5, 0, 2, 0), (36, 160, 96, 5, 1, 2, 0), (40, 160, 96, 5, 0, 2, 32), (48, 160, 96, 5, 0, 2, 0),
+    (64, 133, 77, 5, 0, 2, 0), (28, 4096, 64, 5, 0, 2, 0), (36, 4096, 64, 5, 1, 2, 0), (40, 1100, 64, 5, 0, 2, 0)]
+
+
+@pytest.mark.parametrize("T,H,F,E,shared,k,group", FIRST)
+def test_moe_of_any_token_count(T, H, F, E, shared, k, group):
+    L = Layer(H, F, E, shared, k, D.BF16, group, False, 1, 1.0, seed=T + H, max_tokens=T)
+    x = tokens(T, H, D.BF16, T)
+    y, index, weight = L.run(x.cuda(), H, ldy=H)
+    L.check(x, y, index, weight)
+
+
+@pytest.mark.parametrize("case", FIRST, ids=str)
+def test_moe_as_a_process_first_call(case):
+    import os
+    import subprocess
+    import sys
+    here = os.path.dirname(os.path.abspath(__file__))
+    code = "import sys; sys.path[:0] = %r; import test_decode_gpu as m; m.test_moe_of_any_token_count(*%r)" % ([here, os.path.dirname(here)], case)
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr[-2000:]
