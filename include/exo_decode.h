@@ -126,8 +126,8 @@ typedef struct {
 exo_gemm_status_t exo_moe_validate(const exo_moe_desc_t* desc);
 
 /*
- * Makes a plan: validates and allocates the workspace (routing tables and the taken experts' inner activations).
- * *out is written only on success.
+ * Makes a plan: validates, allocates the workspace (routing tables and the taken experts' inner activations) and clears it, which is
+ * done when the call returns: the plan may be run on any stream.  *out is written only on success.
  */
 exo_gemm_status_t exo_moe_create(exo_moe_handle_t* out, const exo_moe_desc_t* desc);
 

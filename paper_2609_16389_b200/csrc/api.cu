@@ -123,6 +123,18 @@ static int smem_of(const TileConfig& cfg, int c_dtype) {
 static thread_local int g_last_cuda_error = 0;
 void note_cuda_error(int e) { g_last_cuda_error = e; }   // for the other translation units
 
+// cudaMemset does not do here: it returns before the memory is clear, which it is in the order of the legacy default stream only, and
+// non-blocking streams do not wait for that one.
+cudaError_t clear_now(void* at, size_t bytes) {
+  cudaStream_t own;
+  cudaError_t e = cudaStreamCreateWithFlags(&own, cudaStreamNonBlocking);
+  if (e != cudaSuccess) return e;
+  e = cudaMemsetAsync(at, 0, bytes, own);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(own);
+  const cudaError_t gone = cudaStreamDestroy(own);
+  return e != cudaSuccess ? e : gone;
+}
+
 // K (in 16-bit-element units) from which a run that may store C straight from registers does so, for a
 // 32-bit and for a 16-bit C.
 constexpr int64_t kDirectMinK32 = 2048, kDirectMinK16 = 1024;

@@ -10,6 +10,8 @@
 
 namespace exo {
 void note_cuda_error(int e);   // what exo_gemm_last_cuda_error reports (api.cu)
+// Zeroes device memory and returns when that is done: a plan may be run on any stream at once (api.cu).
+cudaError_t clear_now(void* at, size_t bytes);
 // Tensor map for copies of `steps` steps of 16 rows of a 4-bit matrix (api.cu, which looks the encoder up).
 bool encode_steps_map(CUtensorMap* map, const void* codes, uint64_t rows, uint64_t blocks, uint32_t steps);
 // The same for copies of a box of words (2 or 4 bytes) from the rows of a matrix.

@@ -1041,7 +1041,7 @@ exo_gemm_status_t exo_moe_create(exo_moe_handle_t* out, const exo_moe_desc_t* d)
   plan->bytes = at;
   cudaError_t e = cudaMalloc((void**)&plan->ws, (size_t)plan->bytes);
   if (e == cudaSuccess) {
-    e = cudaMemset(plan->ws, 0, (size_t)plan->bytes);   // the counter, and the padding of the inner activations
+    e = exo::clear_now(plan->ws, (size_t)plan->bytes);   // the counter, and the padding of the inner activations
     if (e != cudaSuccess) cudaFree(plan->ws);
   }
   if (e != cudaSuccess) {

@@ -762,3 +762,31 @@ def test_moe_as_a_process_first_call(case):
     code = "import sys; sys.path[:0] = %r; import test_decode_gpu as m; m.test_moe_of_any_token_count(*%r)" % ([here, os.path.dirname(here)], case)
     r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300)
     assert r.returncode == 0, r.stderr[-2000:]
+
+
+# ------------------------------------------------------------------ a plan's first run
+def test_moe_plan_made_while_the_default_stream_is_busy_runs_on_another_one():
+    """A new plan's workspace is clear when it is returned, in whatever order streams get to their work."""
+    t = torch()
+    T, H, F, E, k = 20, 512, 100, 16, 4
+    L = Layer(H, F, E, 0, k, D.FP16, seed=30, max_tokens=T)
+    x = tokens(T, H, D.FP16, 31).cuda()
+    want, index, weight = L.run(x, H)
+    a = t.randn(8192, 8192, device="cuda", dtype=t.bfloat16)
+    got = t.zeros(T, H, dtype=t.float16, device="cuda")
+    side = t.cuda.Stream()
+    a @ a
+    t.cuda.synchronize()
+    for _ in range(3):
+        junk = t.full((L.plan.workspace_bytes(),), 0xff, dtype=t.uint8, device="cuda")   # what the new plan's memory may have held
+        t.cuda.synchronize()
+        del junk
+        t.cuda.empty_cache()
+        for _ in range(60):                              # some 40 ms of work
+            a @ a
+        with D.MoePlan(D.MoeDesc(H, F, E, 0, k, T, D.FP16)) as plan:
+            with t.cuda.stream(side):
+                plan.run(L.weights, T, x.data_ptr(), H, got.data_ptr(), H, stream=stream())
+            side.synchronize()
+        t.cuda.synchronize()
+        assert t.equal(got, want)
