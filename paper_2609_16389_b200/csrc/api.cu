@@ -541,7 +541,7 @@ exo_gemm_status_t exo_gemm_create_batched(exo_gemm_handle_t* out, const exo_gemm
   if (e != cudaSuccess) { delete p; return cuda_fail(e); }
   e = cudaMalloc((void**)&p->d_status, kStatusBytes);
   if (e != cudaSuccess) { delete p; return cuda_fail(e); }
-  e = cudaMemset(p->d_status, 0, kStatusBytes);
+  e = clear_now(p->d_status, kStatusBytes);
   for (int m = 0; m < 3 && e == cudaSuccess; ++m)   // aligned copies of the matrices whose rows TMA cannot address
     if (p->repack & (1 << m)) e = cudaMalloc(&p->d_pack[m], (size_t)pack_bytes(p->desc, m));
   if (e != cudaSuccess) {
@@ -557,7 +557,7 @@ exo_gemm_status_t exo_gemm_create_batched(exo_gemm_handle_t* out, const exo_gemm
     } else {
       e = cudaMalloc((void**)&p->d_split_ws, (size_t)p->cfg.workspace_bytes);
       if (e == cudaSuccess) e = cudaMalloc((void**)&p->d_split_flags, flag_bytes);
-      if (e == cudaSuccess) e = cudaMemset(p->d_split_flags, 0, flag_bytes);
+      if (e == cudaSuccess) e = clear_now(p->d_split_flags, flag_bytes);
     }
     const size_t table_entries = 4 * (size_t)p->cfg.workers;
     TailItem* table = new (std::nothrow) TailItem[table_entries];
@@ -843,10 +843,10 @@ exo_gemm_status_t exo_gemm_check(exo_gemm_handle_t plan, uint32_t* detail) {
   if (e != cudaSuccess) return cuda_fail(e);
   if (detail) memcpy(detail, h, 32);
   if (h[0] == kStatusOk) return EXO_GEMM_OK;
-  e = cudaMemset(plan->d_status, 0, 32);
+  e = clear_now(plan->d_status, 32);
   if (e != cudaSuccess) return cuda_fail(e);
   if (plan->d_split_flags) {  // an abandoned run may have left the counters of the tail tiles out of step
-    e = cudaMemset(plan->d_split_flags, 0, 2 * sizeof(uint32_t) * (size_t)plan->cfg.tail_tiles * (size_t)plan->cfg.pairs);
+    e = clear_now(plan->d_split_flags, 2 * sizeof(uint32_t) * (size_t)plan->cfg.tail_tiles * (size_t)plan->cfg.pairs);
     if (e != cudaSuccess) return cuda_fail(e);
   }
   return EXO_GEMM_ERR_DEVICE_TIMEOUT;

@@ -997,3 +997,35 @@ def test_seeded_random_problems_on_the_librarys_own_plans(case):
         if p.ldc > cols and r < rows - 1:
             a, b = flat_before[r * p.ldc + cols:(r + 1) * p.ldc], flat_after[r * p.ldc + cols:(r + 1) * p.ldc]
             assert np.array_equal(a.view(np.uint8), b.view(np.uint8)), (r, info)
+
+
+# ------------------------------------------------------------------ a plan's first run
+def test_plan_made_while_the_default_stream_is_busy_runs_on_another_one():
+    """A new plan's status words and arrival counters are clear when it is returned, in whatever order streams get to their work."""
+    import torch
+    M, N, K = 1280, 1280, 1024
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    a = torch.randn(M, K, device="cuda", generator=gen).bfloat16()
+    b = torch.randn(N, K, device="cuda", generator=gen).bfloat16()
+    busy = torch.randn(8192, 8192, device="cuda").bfloat16()
+    c = [torch.zeros(M, N, device="cuda") for _ in range(4)]
+    desc = B.make_desc(M, N, K, BF16, FP32, B.ROW_MAJOR, B.COL_MAJOR, B.ROW_MAJOR, flags=flags_for(2, 256, 16, split=2))
+    side = torch.cuda.Stream()
+    with B.Plan(desc) as plan:
+        assert plan.info()["split_k"] == 2
+        plan.run(a.data_ptr(), b.data_ptr(), c[0].data_ptr(), stream=torch.cuda.current_stream().cuda_stream)
+        busy @ busy
+        torch.cuda.synchronize()
+        plan.check()
+    for out in c[1:]:
+        junk = [torch.full((n,), 0xff, dtype=torch.uint8, device="cuda") for n in (1 << 21, 1 << 20)]   # what the new plan's memory may have held
+        torch.cuda.synchronize()
+        del junk
+        torch.cuda.empty_cache()
+        for _ in range(60):                              # some 40 ms of work
+            busy @ busy
+        with B.Plan(desc) as plan:
+            plan.run(a.data_ptr(), b.data_ptr(), out.data_ptr(), stream=side.cuda_stream)
+            side.synchronize()
+            plan.check()
+        assert torch.equal(out, c[0])
