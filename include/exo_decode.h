@@ -137,7 +137,8 @@ exo_gemm_status_t exo_moe_create(exo_moe_handle_t* out, const exo_moe_desc_t* de
  * their w_e; either may be NULL.  y, index and weight must not overlap the inputs or each other.  Runs of one plan
  * must not overlap on the GPU (they share its workspace).  silu(gate) * up * w_e is computed in fp32 and held in
  * `dtype` between the two products (up to 4 tokens as the sum of two values of it), as the activations of a 16-bit
- * matrix product are; all sums are fp32.
+ * matrix product are; all sums are fp32.  Beyond the largest finite value of `dtype` (twice that, where it is held as a
+ * sum) it is infinite.
  * Matrices of `dtype` need the alignment of their elements (16-byte aligned rows are read faster), the parts of 4-bit
  * ones that of exo_q4_t.
  */

@@ -340,10 +340,15 @@ __device__ __forceinline__ void store_inner(const MoeParams& p, const float* wei
   for (int q = 0; q < 2; ++q)
     if (n + q < a.count) {
       const float v = weight[a.base + n + q] * (gate[q] / (1.f + expf(-gate[q])) * up[q]);
-      const uint16_t hi = T::from_float(v);
       uint16_t* to = p.h + ((int64_t)(a.base + n + q) << p.halves) * p.ldh + col;
-      to[0] = hi;
-      if (p.halves) to[p.ldh] = T::from_float(v - T::to_float(hi));
+      if (p.halves && fabsf(v) <= 3.4028235e38f) {   // beyond the type's range the first part is its largest value, the second the rest
+        const uint16_t hi = T::from_float(fminf(fmaxf(v, -T::max_finite()), T::max_finite()));
+        to[0] = hi;
+        to[p.ldh] = T::from_float(v - T::to_float(hi));
+      } else {
+        to[0] = T::from_float(v);
+        if (p.halves) to[p.ldh] = 0;
+      }
     }
 }
 

@@ -790,3 +790,42 @@ def test_moe_plan_made_while_the_default_stream_is_busy_runs_on_another_one():
             side.synchronize()
         t.cuda.synchronize()
         assert t.equal(got, want)
+
+
+# ------------------------------------------------------------------ large inner activations
+def one_expert(H, F, dtype, gate, up, down):
+    """A layer of one expert with constant gate and up weights; its weight is 1."""
+    L = Layer(H, F, 1, 0, 1, dtype, seed=40, max_tokens=8)
+    L.keep[0]["w"].fill_(gate)
+    L.keep[1]["w"].fill_(up)
+    L.keep[2]["w"].copy_(down)
+    return L
+
+
+@pytest.mark.parametrize("T", [1, 4])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_moe_inner_activations_beyond_the_largest_fp16_number(T, sign):
+    """silu(256) * 273.5 = 70016 = 65504 + 4512: representable as two parts, so that only sums and y's rounding are left."""
+    t = torch()
+    H, F = 16, 40
+    d = (t.randn(H, F, generator=t.Generator().manual_seed(1)) * 0.01).half()
+    L = one_expert(H, F, D.FP16, 16.0, 17.09375 * sign, d.cuda())
+    x = t.ones(T, H, dtype=t.float16, device="cuda")
+    y, _, weight = L.run(x, H)
+    assert (weight == 1).all()
+    ref, mag = d.double().sum(1) * 70016 * sign, d.double().abs().sum(1) * 70016
+    bound = sum_bound(F) * mag + U[D.FP16] * 1.01 * ref.abs() + TINY[D.FP16]
+    assert bool(((y.cpu().double() - ref).abs() <= bound).all())
+
+
+@pytest.mark.parametrize("T", [1, 4, 5])
+@pytest.mark.parametrize("dtype,x,gate", [(D.FP16, 4.0, 1024.0), (D.BF16, 1.0e25, 1.0e8)])
+def test_moe_inner_activations_beyond_their_type_are_infinite(T, dtype, x, gate):
+    """(fp16: 2^16 squared; bf16: beyond fp32 as well.)  An infinity keeps its sign through positive and negative weights."""
+    t = torch()
+    H, F = 16, 40
+    d = t.full((H, F), 2.0 ** -20)
+    d[H // 2:] = -2.0 ** -20
+    L = one_expert(H, F, dtype, gate, gate, d.to(tt(dtype)).cuda())
+    y, _, _ = L.run(t.full((T, H), x, dtype=tt(dtype), device="cuda"), H)
+    assert (y[:, :H // 2] == float("inf")).all() and (y[:, H // 2:] == -float("inf")).all()
