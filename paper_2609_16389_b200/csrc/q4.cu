@@ -393,7 +393,9 @@ __global__ void __launch_bounds__(kGemvThreads, 2) exo_gemv_q4_kernel(const Gemv
 // bits (exact for what is down to 2^-22 of the step's largest in bf16, 2^-19 in fp16; a smaller value is off by at most
 // 2^-30 of the largest), whose four balanced digits are four columns of the product.  The columns of few tokens are idle
 // otherwise.  A group's sum of (code - zero) * digit is an exact integer; it comes out as the float 1.5 * 2^23 + sum, since
-// the accumulator starts with that float's bits less zero * (sum of digits).  From there on everything is fp32.
+// the accumulator starts with that float's bits less zero * (sum of digits).  From there on everything is fp32: an integer is multiplied by its
+// weights' scale, which cannot underflow, then by its activations' with the weight of the top digit in it, so that the top digits' sum is of
+// the result's own size.  The lower digits' sums may be four times that: a result that is not finite is summed again in floats.
 //
 // Weights come through shared memory: each warp keeps a ring of pieces (eight steps of 16 rows) that it fills itself by tiled
 // copies.  A lane's parts of a step are 16 bytes of rows g and g + 8.
@@ -441,19 +443,20 @@ __device__ __forceinline__ void copy_eight(uint32_t to, const uint16_t* from, in
 }
 __device__ __forceinline__ int rank_part(int blocks, int r, int S) { return (int)((int64_t)blocks * r / S); }
 
-// What the values of a token that are not finite give a row over steps s0 .. s1 - 1 (they count as 0 in the integers).  codes,
-// scales and zeros are the row's, x the token's.
+// A row's product with a token in 32-bit floats, value by value: for tokens that have infinities or NaN, which are no integers, and sums of
+// digits that overflow.  codes, scales and zeros are the row's, x the token's.
 template <class T>
-__device__ __noinline__ float not_finite_part(const uint32_t* codes, const uint16_t* scales, const uint8_t* zeros, const uint16_t* x, int per, int K, int s0, int s1) {
+__device__ __noinline__ float sum_in_floats(const uint32_t* codes, const uint16_t* scales, const uint8_t* zeros, const uint16_t* x, int per, int K) {
   float v = 0.f;
-  for (int k = s0 * 128; k < min(s1 * 128, K); ++k) {
-    const float xk = T::to_float(x[k]);
-    if (fabsf(xk) <= 3.4028235e38f) continue;
-    const int i = k & 7, n = i / 2 + 4 * (i & 1), j = k >> 5 & 3, t = k >> 3 & 3;
-    const uint32_t word = codes[k / 128 * 16 + 4 * t + j];
-    const int group = k / 128 * per + (k & 127) * per / 128;
-    const int zero = zeros ? zeros[group] : 8;
-    v += (float)((int)(word >> (4 * n) & 15u) - zero) * T::to_float(scales[group]) * xk;
+  for (int group = 0; group * (128 / per) < K; ++group) {
+    const int zero = zeros ? zeros[group] : 8, end = min((group + 1) * (128 / per), K);
+    float part = 0.f;
+    for (int k = group * (128 / per); k < end; ++k) {
+      const int i = k & 7, n = i / 2 + 4 * (i & 1), j = k >> 5 & 3, t = k >> 3 & 3;
+      const uint32_t word = codes[k / 128 * 16 + 4 * t + j];
+      part = fmaf((float)((int)(word >> (4 * n) & 15u) - zero), T::to_float(x[k]), part);
+    }
+    v = fmaf(T::to_float(scales[group]), part, v);
   }
   return v;
 }
@@ -461,7 +464,7 @@ __device__ __noinline__ float not_finite_part(const uint32_t* codes, const uint1
 template <class T, int PER, bool ZEROS>
 __global__ void __launch_bounds__(kFewThreads, 1) exo_gemv_q4_few_kernel(const FewParams fp, const __grid_constant__ CUtensorMap map) {
   namespace cg = cooperative_groups;
-    constexpr int COLS = 8;                  // two tokens of four digits
+  constexpr int COLS = 8;                  // two tokens of four digits
   const GemvParams& p = fp.g;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ int strange;                  // bit t: token t has values that are not finite
@@ -549,11 +552,11 @@ __global__ void __launch_bounds__(kFewThreads, 1) exo_gemv_q4_few_kernel(const F
 #pragma unroll
     for (int o = 1; o < 16; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
     if (odd) atomicOr(&strange, 1 << token);
-    const int up = min(156 - (int)(__float_as_uint(top) >> 23), 127);        // |v| * 2^up < 2^30
-    const float factor = __uint_as_float((uint32_t)(up + 127) << 23);
+    const int up = 156 - (int)(__float_as_uint(top) >> 23), half = up / 2;   // |v| * 2^up < 2^30; up is 156 at most
+    const float factor = __uint_as_float((uint32_t)(half + 127) << 23), factor2 = __uint_as_float((uint32_t)(up - half + 127) << 23);
     uint32_t q[8];
 #pragma unroll
-    for (int n = 0; n < 8; ++n) q[n] = ((uint32_t)__float2int_rn(v[n] * factor) + 0x00808080u) ^ 0x00808080u;
+    for (int n = 0; n < 8; ++n) q[n] = ((uint32_t)__float2int_rn(v[n] * factor * factor2) + 0x00808080u) ^ 0x00808080u;
     const uint32_t first[4] = {q[0], q[4], q[1], q[5]}, second[4] = {q[2], q[6], q[3], q[7]};   // the order of the codes of a word, low and high
     uint32_t d0[4], d1[4];
     transpose4(first, d0);
@@ -574,7 +577,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) exo_gemv_q4_few_kernel(const F
 #pragma unroll
         for (int c = 0; c < 4; ++c) to[c] = ZEROS ? -sum[c] : kMagic - 8 * sum[c];
       }
-      if (e == 0) step_scale[2 * s + token] = __uint_as_float(up == 127 ? 0x00400000u : (uint32_t)(127 - up) << 23);   // 2^-up
+      if (e == 0) step_scale[2 * s + token] = ldexpf(1.f, 24 - up);
     }
   }
   __syncthreads();
@@ -606,6 +609,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) exo_gemv_q4_few_kernel(const F
         const uint4 x0 = lds128(xat + s * 128), x1 = lds128(xat + s * 128 + 16);
         const uint32_t xl[4] = {x0.x, x0.z, x1.x, x1.z}, xh[4] = {x0.y, x0.w, x1.y, x1.w};
         const float ss = step_scale[2 * s + t / 2];
+        float part[4];
 #pragma unroll
         for (int q = 0; q < PER; ++q) {
           const int2 c = *reinterpret_cast<const int2*>(start + (s * PER + q) * COLS + 2 * t);
@@ -618,20 +622,23 @@ __global__ void __launch_bounds__(kFewThreads, 1) exo_gemv_q4_few_kernel(const F
 #pragma unroll
           for (int j = 4 / PER * q; j < 4 / PER * (q + 1); ++j)
             mma_u8s8(d, wa[j] & 0x0f0f0f0fu, wb[j] & 0x0f0f0f0fu, (wa[j] >> 4) & 0x0f0f0f0fu, (wb[j] >> 4) & 0x0f0f0f0fu, xl[j], xh[j]);
-          const float fa = ss * T::to_float((uint16_t)(sa[q / 2] >> (16 * (q % 2)))), fb = ss * T::to_float((uint16_t)(sb[q / 2] >> (16 * (q % 2))));
-          acc[0] = fmaf(fa, __int_as_float(d[0]) - 12582912.f, acc[0]);
-          acc[1] = fmaf(fa, __int_as_float(d[1]) - 12582912.f, acc[1]);
-          acc[2] = fmaf(fb, __int_as_float(d[2]) - 12582912.f, acc[2]);
-          acc[3] = fmaf(fb, __int_as_float(d[3]) - 12582912.f, acc[3]);
+          const float fa = T::to_float((uint16_t)(sa[q / 2] >> (16 * (q % 2)))), fb = T::to_float((uint16_t)(sb[q / 2] >> (16 * (q % 2))));
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            const float sum = __int_as_float(d[c]) - 12582912.f;
+            part[c] = q == 0 ? (c < 2 ? fa : fb) * sum : fmaf(c < 2 ? fa : fb, sum, part[c]);
+          }
         }
+#pragma unroll
+        for (int c = 0; c < 4; ++c) acc[c] = fmaf(ss, part[c], acc[c]);
       }
     }
     __syncwarp();
     issue();
     cslot = cslot + 1 == fp.stages ? 0 : cslot + 1;
     parity ^= cslot == 0 ? 1u : 0u;
-    if (ends) {                            // digits 2 (t % 2) and 2 (t % 2) + 1 of token t / 2, weighted by 256^digit
-      const float lo = t & 1 ? 65536.f : 1.f, hi = t & 1 ? 16777216.f : 256.f;
+    if (ends) {                            // digits 2 (t % 2) and 2 (t % 2) + 1 of token t / 2, weighted by 256^(digit - 3)
+      const float lo = t & 1 ? 0x1p-8f : 0x1p-24f, hi = t & 1 ? 1.f : 0x1p-16f;
       float* out = sums + cu * p.tokens * 16;
       float v0 = fmaf(hi, acc[1], lo * acc[0]), v1 = fmaf(hi, acc[3], lo * acc[2]);
       v0 += __shfl_xor_sync(0xffffffffu, v0, 1);
@@ -652,14 +659,16 @@ __global__ void __launch_bounds__(kFewThreads, 1) exo_gemv_q4_few_kernel(const F
     const int tile = i / (p.tokens * 16), at = i - tile * (p.tokens * 16), token = at >> 4;
     const int row = (cl + tile * clusters) * 16 + (at & 15);
     float v = 0.f;
+    bool floats = false;
     for (int r = 0; r < S; ++r) {
       const float* from = (S > 1 ? cluster.map_shared_rank(sums, r) : sums) + (tile << fp.nk_log) * p.tokens * 16 + at;
       for (int j = 0; j < nk; ++j) v += from[j * p.tokens * 16];
-      if (((S > 1 ? *cluster.map_shared_rank(&strange, r) : strange) >> token & 1) && row < p.rows) {
-        const int64_t at = (int64_t)row * p.blocks;
-        v += not_finite_part<T>(reinterpret_cast<const uint32_t*>(p.codes) + at * 16, p.scales + at * PER, ZEROS ? p.zeros + at * PER : nullptr,
-                                p.x + (int64_t)token * p.ldx, PER, p.K, rank_part(p.blocks, r, S), rank_part(p.blocks, r + 1, S));
-      }
+      floats = floats || ((S > 1 ? *cluster.map_shared_rank(&strange, r) : strange) >> token & 1);
+    }
+    if ((floats || !(fabsf(v) <= 3.4028235e38f)) && row < p.rows) {
+      const int64_t at = (int64_t)row * p.blocks;
+      v = sum_in_floats<T>(reinterpret_cast<const uint32_t*>(p.codes) + at * 16, p.scales + at * PER, ZEROS ? p.zeros + at * PER : nullptr,
+                           p.x + (int64_t)token * p.ldx, PER, p.K);
     }
     store_y<T>(p, token, row, v);
   }

@@ -829,3 +829,61 @@ def test_moe_inner_activations_beyond_their_type_are_infinite(T, dtype, x, gate)
     L = one_expert(H, F, dtype, gate, gate, d.to(tt(dtype)).cuda())
     y, _, _ = L.run(t.full((T, H), x, dtype=tt(dtype), device="cuda"), H)
     assert (y[:, :H // 2] == float("inf")).all() and (y[:, H // 2:] == -float("inf")).all()
+
+
+# ------------------------------------------------------------------ integer products over all of bf16's range
+def scaled(m, exponent):
+    """m with its scales (and so its values) times 2^exponent, a power that bf16 scales of 0.005 and more take exactly."""
+    m.scales = (m.scales.float() * 2.0 ** exponent).to(m.scales.dtype)
+    m.values = m.values * 2.0 ** exponent
+    return m
+
+
+# a result below the smallest normal number is off by half the last subnormal bit for each of an fp32 sum's roundings: four columns of
+# digits in steps of 128, and the sums of warps and CTAs
+def tiny_bound(K):
+    return (K / 32 + 64) * 2.0 ** -150
+
+
+@pytest.mark.parametrize("tokens", [1, 2, 3])
+@pytest.mark.parametrize("group,zeros", [(128, False), (32, True)])
+@pytest.mark.parametrize("x_exp,s_exp", [(-83, -43), (-60, -60), (-100, -20), (-123, 0), (-129, 20), (60, 50), (-20, 118), (110, -100)])
+def test_gemv_of_large_matrices_at_any_magnitude(tokens, group, zeros, x_exp, s_exp):
+    t = torch()
+    m = scaled(LargeMatrix(9000, 9000, group, D.BF16, zeros, seed=50), s_exp)
+    x = (t.randn(tokens, 9000, generator=t.Generator(device="cuda").manual_seed(51), device="cuda", dtype=t.float64) * 2.0 ** x_exp).bfloat16()
+    y = t.empty(tokens, 9000, device="cuda")
+    m.gemv(x, y)
+    ref = x.double() @ m.values.T
+    allowed = m.bound(x) + (4 * 2.0 ** -24 + U[D.FP32] * 1.01) * ref.abs() + tiny_bound(9000)
+    off = (y.double() - ref).abs()
+    assert bool(t.isfinite(y).all()) and bool((off <= allowed).all()), float((off / allowed).max())
+
+
+@pytest.mark.parametrize("tokens", [1, 2, 3])
+def test_gemv_of_large_matrices_up_to_the_largest_float(tokens):
+    """130 = 33 * 4 - 2: the second digit is -128 where the first is 33, and its sum overflows before the result does."""
+    t = torch()
+    m = LargeMatrix(9000, 9000, 64, D.BF16, True, seed=52)
+    m.codes.fill_(-1)
+    m.zeros.zero_()
+    m.scales[:, :] = m.scales[:, :1].float() * 2.0 ** 60
+    m.values = (15 * m.scales[:, :1].double()).expand(-1, 9000)
+    top = 0.8 * 3.4e38 / float(m.values[:, 0].max() * 9000)
+    x = t.full((tokens, 9000), 130 * 2.0 ** np.floor(np.log2(top / 130)), device="cuda").bfloat16()
+    y = t.empty(tokens, 9000, device="cuda")
+    m.gemv(x, y)
+    ref = x.double() @ m.values.T
+    assert float(ref.max()) > 1.0e38
+    assert bool(((y.double() - ref).abs() <= m.bound(x) + (4 * 2.0 ** -24 + U[D.FP32] * 1.01) * ref.abs()).all())
+
+
+@pytest.mark.parametrize("tokens", [1, 2, 3])
+def test_gemv_of_large_matrices_of_zero_weights_gives_zero(tokens):
+    t = torch()
+    m = scaled(LargeMatrix(9000, 9000, 128, D.BF16, False, seed=53), 100)
+    m.codes.fill_(-0x77777778)                           # 0x88888888
+    x = (t.randn(tokens, 9000, generator=t.Generator(device="cuda").manual_seed(54), device="cuda") * 2.0 ** 120).bfloat16()
+    y = t.empty(tokens, 9000, device="cuda")
+    m.gemv(x, y)
+    assert bool((y == 0).all())
