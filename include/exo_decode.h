@@ -136,7 +136,7 @@ exo_gemm_status_t exo_moe_create(exo_moe_handle_t* out, const exo_moe_desc_t* de
  * ldx, ldy >= hidden.  index (int32) and weight (fp32), tokens x top_k, receive the taken experts, largest first, and
  * their w_e; either may be NULL.  y, index and weight must not overlap the inputs or each other.  Runs of one plan
  * must not overlap on the GPU (they share its workspace).  silu(gate) * up * w_e is computed in fp32 and held in
- * `dtype` between the two products (up to 4 tokens as the sum of two values of it), as the activations of a 16-bit
+ * `dtype` between the two products (for an expert of up to 4 tokens as the sum of two values of it), as the activations of a 16-bit
  * matrix product are; all sums are fp32.  Beyond the largest finite value of `dtype` (twice that, where it is held as a
  * sum) it is infinite.
  * Matrices of `dtype` need the alignment of their elements (16-byte aligned rows are read faster), the parts of 4-bit

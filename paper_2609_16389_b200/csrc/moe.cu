@@ -22,7 +22,7 @@
 namespace exo {
 namespace decode {
 
-constexpr int kHalvesTokens = 4;   // up to this many tokens the inner activations are kept in two 16-bit parts
+constexpr int kHalvesTokens = 4;   // the inner activations of an expert of up to this many tokens are kept in two 16-bit parts
 constexpr int kMaxTokens = 64, kMaxExperts = 512, kMaxShared = 8, kMaxTopK = 16;
 
 struct Active { int expert, base, count, cost_before; };   // a taken expert: its tokens are entries base .. base + count - 1
@@ -56,8 +56,7 @@ struct MoeParams {
   int* entry_token;
   float* entry_weight;
   float* logits;            // tokens x experts
-  uint16_t* h;              // (entries << halves) x ldh
-  int halves;               // 1: an inner activation is the sum of two 16-bit values, in rows 2 n and 2 n + 1
+  uint16_t* h;              // inner activations, two rows of ldh for every entry (halves_of)
   const uint16_t* xs;       // x itself, or (copy_x) route's copy in rows of ldxs elements, a multiple of 128, filled with zeros
   int64_t ldxs;
   bool copy_x;
@@ -328,26 +327,30 @@ __global__ void __launch_bounds__(kRouteThreads) exo_moe_route_kernel(const MoeP
   route_all(p, p.logits, tables);
 }
 
+// Rows of h: an expert's begin at twice its first entry, and hold an entry each, or (1) its two parts.
+__device__ __forceinline__ int halves_of(int count) { return count <= kHalvesTokens ? 1 : 0; }
+
 // Inner activations from lane l's part of tile i: gate in x, y and up in z, w for two tokens.  Rounding them to 16 bits would cost
-// as much accuracy as rounding y does.  Up to four tokens the columns of a fragment have room for the rounding's remainder too, as
-// a token of its own, and `down` adds both; with more tokens one 16-bit value is kept, as for any 16-bit matrix product.
+// as much accuracy as rounding y does.  Where an expert has up to four tokens, the columns of their fragment have room for the rounding's
+// remainder too, as a token of its own, and `down` adds both; with more tokens one 16-bit value is kept, as for any 16-bit matrix product.
 template <class T>
 __device__ __forceinline__ void store_inner(const MoeParams& p, const float* weight, const Active& a, int f0, int i, int l, const float4& sums) {
   const int n = 8 * i + 2 * (l & 3), col = f0 + (l >> 2);
   if (col >= p.inner) return;
   const float gate[2] = {sums.x, sums.y}, up[2] = {sums.z, sums.w};
+  const int halves = halves_of(a.count);
 #pragma unroll
   for (int q = 0; q < 2; ++q)
     if (n + q < a.count) {
       const float v = weight[a.base + n + q] * (gate[q] / (1.f + expf(-gate[q])) * up[q]);
-      uint16_t* to = p.h + ((int64_t)(a.base + n + q) << p.halves) * p.ldh + col;
-      if (p.halves && fabsf(v) <= 3.4028235e38f) {   // beyond the type's range the first part is its largest value, the second the rest
+      uint16_t* to = p.h + (2 * (int64_t)a.base + ((n + q) << halves)) * p.ldh + col;
+      if (halves && fabsf(v) <= 3.4028235e38f) {   // beyond the type's range the first part is its largest value, the second the rest
         const uint16_t hi = T::from_float(fminf(fmaxf(v, -T::max_finite()), T::max_finite()));
         to[0] = hi;
         to[p.ldh] = T::from_float(v - T::to_float(hi));
       } else {
         to[0] = T::from_float(v);
-        if (p.halves) to[p.ldh] = 0;
+        if (halves) to[p.ldh] = 0;
       }
     }
 }
@@ -684,7 +687,7 @@ exo_moe_down_ring_kernel(const MoeParams p, const __grid_constant__ CUtensorMap 
   const Tables tb = copy_tables(reinterpret_cast<uint8_t*>(part + p.tokens * 16), active_shared, p);
   const int n_active = active_shared;
   // A step costs a warp its weights and then its tiles of tokens: three parts and two for every tile.  Equal shares of that.
-  auto cost_of = [&](int at) { return 3 + 2 * (((tb.active[at].count << p.halves) + 7) / 8); };
+  auto cost_of = [&](int at) { return 3 + 2 * (((tb.active[at].count << halves_of(tb.active[at].count)) + 7) / 8); };
   if (warp == 0) {
     int before = 0;
     for (int e0 = 0; e0 < n_active; e0 += 32) {
@@ -734,7 +737,7 @@ exo_moe_down_ring_kernel(const MoeParams p, const __grid_constant__ CUtensorMap 
   ptx::grid_dependency_wait();     // `up` is complete
   ptx::grid_launch_dependents();
   // rows behind an expert's are other entries', or spare ones
-  auto row_at = [&](int e, int from) { return p.h + ((int64_t)(tb.active[e].base << p.halves) + g) * p.ldh + 8 * t + from * P::kStep; };
+  auto row_at = [&](int e, int from) { return p.h + (2 * (int64_t)tb.active[e].base + g) * p.ldh + 8 * t + from * P::kStep; };
   P piece;
   auto ask_scales = [&](int e, int from, int n) {
     const int64_t first = tb.active[e].expert * p.down.expert_rows;
@@ -747,7 +750,7 @@ exo_moe_down_ring_kernel(const MoeParams p, const __grid_constant__ CUtensorMap 
   }
   while (any(at, s)) {
     const Active a = tb.active[at];
-    const int columns = a.count << p.halves, nt = (columns + 7) / 8, stop = stop_of(at);
+    const int halves = halves_of(a.count), columns = a.count << halves, nt = (columns + 7) / 8, stop = stop_of(at);
     float acc[NT][4];
     clear(acc);
     while (s < stop) {
@@ -773,7 +776,7 @@ exo_moe_down_ring_kernel(const MoeParams p, const __grid_constant__ CUtensorMap 
         for (int c = 0; c < 2; ++c) {
           const int n = 8 * i + 2 * t + c;
           if (n < columns) {   // both parts of an activation are the same lane's
-            float* to = mine + tb.token[a.base + (n >> p.halves)] * 16 + g;
+            float* to = mine + tb.token[a.base + (n >> halves)] * 16 + g;
             to[0] += acc[i][c];
             to[8] += acc[i][2 + c];
           }
@@ -875,21 +878,21 @@ __global__ void __launch_bounds__(kPlainThreads) exo_moe_down_plain_kernel(const
   for (int at = 0; at < n_active; ++at) {
     const int4 raw = __ldcg(reinterpret_cast<const int4*>(p.active + at));
     const Active a{raw.x, raw.y, raw.z, raw.w};
-    const int columns = a.count << p.halves, nt = (columns + 7) / 8;
+    const int halves = halves_of(a.count), columns = a.count << halves, nt = (columns + 7) / 8;
     const int64_t first = a.expert * p.down.expert_rows;
     const uint16_t* r0 = static_cast<const uint16_t*>(p.down.w) + (first + min(row0 + g, p.hidden - 1)) * p.down.ld;
     const uint16_t* r1 = static_cast<const uint16_t*>(p.down.w) + (first + min(row0 + g + 8, p.hidden - 1)) * p.down.ld;
     float acc[NT][4];
     clear(acc);
     const uint16_t* none[NT] = {};
-    plain_steps<T, NT>(r0, r1, p.h + ((int64_t)(a.base << p.halves) + g) * p.ldh + 8 * t, 8 * p.ldh, none, warp, kPlainWarps, steps, p.inner, t, nt, acc);
+    plain_steps<T, NT>(r0, r1, p.h + (2 * (int64_t)a.base + g) * p.ldh + 8 * t, 8 * p.ldh, none, warp, kPlainWarps, steps, p.inner, t, nt, acc);
 #pragma unroll
     for (int i = 0; i < NT; ++i)
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         const int n = 8 * i + 2 * t + c;
         if (i < nt && n < columns) {
-          float* to = mine + __ldcg(p.entry_token + a.base + (n >> p.halves)) * 16 + g;
+          float* to = mine + __ldcg(p.entry_token + a.base + (n >> halves)) * 16 + g;
           to[0] += acc[i][c];
           to[8] += acc[i][2 + c];
         }
@@ -1041,8 +1044,7 @@ exo_gemm_status_t exo_moe_create(exo_moe_handle_t* out, const exo_moe_desc_t* d)
   plan->at_logits = take((int64_t)d->max_tokens * d->experts * 4);
   plan->ldxs = (d->hidden + 127) / 128 * 128;
   plan->at_xs = take((int64_t)d->max_tokens * plan->ldxs * 2);
-  const int64_t halves = 2 * (int64_t)(d->max_tokens < kHalvesTokens ? d->max_tokens : kHalvesTokens) * (d->top_k + d->shared);
-  plan->at_h = take(((entries > halves ? entries : halves) + 8) * plan->ldh * 2);   // a last tile of eight may read rows behind the last one
+  plan->at_h = take((2 * entries + 8) * plan->ldh * 2);   // a last tile of eight may read rows behind the last one
   plan->bytes = at;
   cudaError_t e = cudaMalloc((void**)&plan->ws, (size_t)plan->bytes);
   if (e == cudaSuccess) {
@@ -1094,7 +1096,6 @@ exo_gemm_status_t exo_moe_run(exo_moe_handle_t plan, const exo_moe_weights_t* w,
   p.logits = (float*)(plan->ws + plan->at_logits);
   p.h = (uint16_t*)(plan->ws + plan->at_h);
 
-  p.halves = p.tokens <= kHalvesTokens ? 1 : 0;
   p.copy_x = !(p.x_aligned && d.hidden % 128 == 0);
   p.xs = p.copy_x ? (const uint16_t*)(plan->ws + plan->at_xs) : p.x;
   p.ldxs = p.copy_x ? plan->ldxs : ldx;

@@ -887,3 +887,68 @@ def test_gemv_of_large_matrices_of_zero_weights_gives_zero(tokens):
     y = t.empty(tokens, 9000, device="cuda")
     m.gemv(x, y)
     assert bool((y == 0).all())
+
+
+# ------------------------------------------------------------------ how inner activations are held
+def cancelling_layer(T, H, F, E, k, dtype, group, pad):
+    """Neighbouring inner values differ by one step of `dtype` and meet weights of opposite sign: y is small, and what rounds an
+    inner activation once to `dtype` shows."""
+    t = torch()
+    L = Layer(H, F, E, 0, k, dtype, group, False, seed=60, pad=pad, max_tokens=T)
+    step = 1 + 2 * U[dtype]
+    if group:
+        for name, m, factor in (("gate", L.keep[0]["q4"], 1.0), ("up", L.keep[1]["q4"], step)):
+            m.codes[1::2] = m.codes[0::2]
+            old = m.scales.clone()
+            m.scales[1::2] = (m.scales[0::2].float() * factor).to(m.scales.dtype)
+            at = np.arange(H) // group
+            codes = m.values[0::2] / old[0::2].double().cpu().numpy()[:, at]
+            m.values[1::2] = codes * m.scales[1::2].double().cpu().numpy()[:, at]
+            L.vals[name] = m.values.reshape(E, F, H)
+        m = L.keep[2]["q4"]
+        c = np.random.default_rng(61).integers(1, 16, (E * H, F), dtype=np.uint8)
+        c[:, 1::2] = 16 - c[:, 0::2]
+        m.codes.copy_(t.from_numpy(D.pack_codes(c)))
+        m.values = (c.astype(np.float64) - 8) * m.scales.double().cpu().numpy()[:, np.arange(F) // group]
+        L.vals["down"] = m.values.reshape(E, H, F)
+    else:
+        for name, keep, factor in (("gate", L.keep[0], 1.0), ("up", L.keep[1], step)):
+            w = keep["w"].view(E, -1, keep["ld"])
+            w[:, 1:F:2] = (w[:, 0:F:2].float() * factor).to(w.dtype)
+            L.vals[name] = w[:, :F, :H].double().cpu().numpy()
+        w = L.keep[2]["w"]
+        w[:, 1:F:2] = -w[:, 0:F:2]
+        L.vals["down"] = w[:, :F].double().cpu().numpy().reshape(E, H, F)
+    return L
+
+
+@pytest.mark.parametrize("dtype", [D.BF16, D.FP16])
+@pytest.mark.parametrize("group,pad", [(0, 0), (0, 1), (32, 0)])
+@pytest.mark.parametrize("T,E,k", [(1, 8, 2), (4, 8, 2), (6, 24, 2), (12, 40, 3), (20, 40, 2), (64, 256, 2)])
+def test_moe_holds_the_inner_activations_of_few_tokens_in_two_parts(T, E, k, group, pad, dtype):
+    """Each token has one channel, so that gate and up are exact.  An inner activation is then off by a few roundings of fp32 and, where its
+    expert has up to four tokens, by the rounding of the second part: U * U of it."""
+    t = torch()
+    H, F = 64, 64
+    L = cancelling_layer(T, H, F, E, k, dtype, group, pad)
+    x = t.zeros(T, H, dtype=tt(dtype))
+    x[t.arange(T), (t.arange(T) * 7) % H] = 4.0
+    y, index, weight = L.run(x.cuda(), H)
+    y, index, weight, xs = y.double().cpu().numpy(), index.cpu().numpy(), weight.double().cpu().numpy(), x.double().numpy()
+    count = np.bincount(index.reshape(-1), minlength=E)
+    seen = 0
+    for tok in range(T):
+        ref, once, bound = np.zeros(H), np.zeros(H), np.zeros(H)
+        for e, we in zip(index[tok], weight[tok]):
+            g, u, d = L.vals["gate"][e] @ xs[tok], L.vals["up"][e] @ xs[tok], L.vals["down"][e]
+            h = we * g / (1 + np.exp(-g)) * u
+            part = U[dtype] ** 2 if count[e] <= 4 else U[dtype]
+            ref += d @ h
+            once += d @ t.from_numpy(h).to(tt(dtype)).double().numpy()
+            bound += np.abs(d) @ (np.abs(h) * (16 * 2.0 ** -24 + part * 1.01) + TINY[dtype]) + sum_bound(F) * (np.abs(d) @ np.abs(h))
+        bound += np.abs(ref) * (U[dtype] * 1.01 + k * 2.0 ** -20) + TINY[dtype]
+        assert (np.abs(y[tok] - ref) <= bound).all(), (tok, (np.abs(y[tok] - ref) / bound).max())
+        if (count[index[tok]] <= 4).all():
+            seen += 1
+            assert (np.abs(once - ref) > bound).any()    # one part would show
+    assert seen > 0
