@@ -151,6 +151,14 @@ exo_gemm_status_t exo_moe_run(exo_moe_handle_t plan, const exo_moe_weights_t* we
  */
 exo_gemm_status_t exo_decode_check(void);
 
+/*
+ * Test hook for the bounded waits: in the next exo_gemv_q4_run or exo_moe_run of this process a wait for copies lasts `timeout_ms` (0 ..
+ * 10000; 0 stands for the usual bound of 4 s), and with skip_copies 1 (a product, an expert's gate and up) or 2 (an expert's down) the first
+ * CTA's first warp issues none, so that its wait runs out and the kernel reports that without trapping.  Products and layers that
+ * read their weights without copies ignore it.
+ */
+exo_gemm_status_t exo_decode_debug_set(int32_t timeout_ms, int32_t skip_copies);
+
 /* Device memory the plan owns, in bytes. */
 int64_t exo_moe_workspace_bytes(exo_moe_handle_t plan);
 

@@ -18,6 +18,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include "ptx.cuh"
+
 namespace exo {
 void note_cuda_error(int e);   // what exo_gemm_last_cuda_error reports (api.cu)
 
@@ -337,17 +339,36 @@ __device__ __forceinline__ uint4 lds128(uint32_t at) {
   asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
   return v;
 }
-// Waits for the copies of a piece.  The wait is bounded (some hundred milliseconds); one that gives up says so and the kernel
-// goes on to its end, where the host can learn of it (exo_decode_check).
+// A warp's waits for the copies of a piece, bounded by the SM's clock.  One that gives up says so and lets the copies in flight land; the
+// warp then neither issues nor awaits any more and goes on to the kernel's end, and the host can learn of it (exo_decode_check).
+struct WaitBound {
+  uint64_t clocks;
+  int skip;         // for tests: the first CTA's first warp issues no copies
+};
 static __device__ unsigned gave_up;
-__device__ __forceinline__ void wait_piece(uint32_t bar, uint32_t parity) {
-  for (int i = 0; i < (1 << 22); ++i) {
-    uint32_t ok;
-    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-    if (ok) return;
-  }
+__device__ __forceinline__ bool wait_on(uint32_t bar, uint32_t parity, uint64_t clocks) {
+  const long long begin = clock64();
+  do {
+#pragma unroll 1
+    for (int i = 0; i < 64; ++i)
+      if (ptx::mbar_try_wait(bar, parity)) return true;
+  } while ((uint64_t)(clock64() - begin) <= clocks);
   gave_up = 1;
+  for (int i = 0; i < 200; ++i) __nanosleep(1000);
+  return false;
 }
+static __device__ __noinline__ bool wait_on_call(uint32_t bar, uint32_t parity, uint64_t clocks) { return wait_on(bar, parity, clocks); }
+struct Copies {
+  bool issues, awaits = true;   // issues: this lane, lane 0
+  __device__ __forceinline__ explicit Copies(const WaitBound& b) : issues((threadIdx.x & 31) == 0 && !(b.skip && blockIdx.x == 0 && threadIdx.x < 32)) {}
+  // CALL: the longer part of the wait is a call.  It frees the integer products' loop (32768 x 16384: 49.9 us, 51.1 inline), and costs
+  // the others more than it gives (64 tokens of 64 experts of 4096 x 1536: 547 us, 539 inline).
+  template <bool CALL>
+  __device__ __forceinline__ void wait(uint32_t bar, uint32_t parity, const WaitBound& b) {
+    if (ptx::mbar_try_wait(bar, parity) || !awaits) return;
+    if (!(CALL ? wait_on_call(bar, parity, b.clocks) : wait_on(bar, parity, b.clocks))) issues = awaits = false;
+  }
+};
 
 // This translation unit's word, put back to 0.
 static inline unsigned take_gave_up(cudaError_t* e) {

@@ -22,6 +22,14 @@ namespace decode {
 
 constexpr int kMostSmem = 220 * 1024;   // dynamic shared memory a launch may ask for
 
+// What exo_decode_debug_set has set for this call (q4.cu): the bound of its waits for copies in SM clocks (at 2 GHz; 4 s if nothing is
+// set), and whose first warp issues none.
+struct WaitHook {
+  uint64_t clocks;
+  int skip;
+};
+WaitHook take_wait_hook();
+
 inline exo_gemm_status_t cuda_failed(cudaError_t e) {
   note_cuda_error((int)e);
   cudaGetLastError();   // clear the runtime's error state

@@ -61,6 +61,7 @@ struct MoeParams {
   int64_t ldxs;
   bool copy_x;
   int up_piece, down_piece;
+  WaitBound up_wait, down_wait;
 };
 
 // Weight formats by number: 0 = 16-bit rows anywhere, 1 = 16-bit rows on 16-byte boundaries, 2 + n = 4-bit, 2^n groups in 128.
@@ -364,7 +365,9 @@ struct Ring {
   uint32_t bar, base;
   int stage_bytes, pitch, put = 0, take = 0;
   uint32_t parity = 0;
+  Copies copies;
 
+  __device__ __forceinline__ explicit Ring(const WaitBound& b) : copies(b) {}
   __device__ __forceinline__ void begin(uint8_t* bars, uint8_t* stages, int piece, int warp, int lane) {
     pitch = piece * 64;
     stage_bytes = 16 * pitch;
@@ -375,14 +378,15 @@ struct Ring {
     ptx::fence_mbar_init();
     __syncwarp();
   }
-  // one lane: a piece of rows r0 .. r0 + 7 of one map and r1 .. r1 + 7 of the other, or (m1 == nullptr) of 16 rows of one
+  // a piece of rows r0 .. r0 + 7 of one map and r1 .. r1 + 7 of the other, or (m1 == nullptr) of 16 rows of one
   __device__ __forceinline__ void copy(const CUtensorMap* m0, int r0, const CUtensorMap* m1, int r1, int x) {
+    if (!copies.issues) return;
     ptx::mbar_arrive_expect_tx(bar + 8 * put, stage_bytes);
     ptx::tma_load_2d(base + put * stage_bytes, m0, x, r0, bar + 8 * put);
     if (m1) ptx::tma_load_2d(base + put * stage_bytes + 8 * pitch, m1, x, r1, bar + 8 * put);
   }
   __device__ __forceinline__ void copied() { put = put + 1 == kMoeStages ? 0 : put + 1; }
-  __device__ __forceinline__ uint32_t wait() const { wait_piece(bar + 8 * take, parity); return base + take * stage_bytes; }
+  __device__ __forceinline__ uint32_t wait(const WaitBound& b) { copies.wait<false>(bar + 8 * take, parity, b); return base + take * stage_bytes; }
   __device__ __forceinline__ void taken() {
     take = take + 1 == kMoeStages ? 0 : take + 1;
     parity ^= take == 0 ? 1u : 0u;
@@ -538,7 +542,7 @@ exo_moe_up_ring_kernel(const MoeParams p, const __grid_constant__ CUtensorMap ga
   __shared__ int active_shared, next_unit, ahead_of[kMoeWarps][kUnitsAhead];
   __shared__ __align__(8) uint8_t bars[kMoeWarps * kMoeStages * 8];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-  Ring ring;
+  Ring ring(p.up_wait);
   ring.begin(bars, smem, p.up_piece, warp, lane);
   float4* sums = reinterpret_cast<float4*>(smem + kMoeWarps * kMoeStages * ring.stage_bytes);   // [unit][tile][lane]
   const int tiles = (p.inner + 7) / 8, steps = (p.hidden + P::kStep - 1) / P::kStep, pieces = (steps + p.up_piece - 1) / p.up_piece;
@@ -570,7 +574,7 @@ exo_moe_up_ring_kernel(const MoeParams p, const __grid_constant__ CUtensorMap ga
   };
   auto issue = [&]() {
     if (iu < units) {
-      if (lane == 0) ring.copy(&gate_map, igate, &up_map, iup, ip * p.up_piece * P::kWords);
+      ring.copy(&gate_map, igate, &up_map, iup, ip * p.up_piece * P::kWords);
       ring.copied();
       if (++ip == end_of(iu)) {
         if (lane == 0) {
@@ -629,7 +633,7 @@ exo_moe_up_ring_kernel(const MoeParams p, const __grid_constant__ CUtensorMap ga
           n_next = steps_at(begin_of(after));
         }
       }
-      const uint32_t w = ring.wait() + g * ring.pitch + 16 * t;
+      const uint32_t w = ring.wait(p.up_wait) + g * ring.pitch + 16 * t;
       piece.template multiply<NT>(w, ring.pitch, s, n, [&](int i) { return xrow[i] + s * P::kStep; }, next, n_next, nt, acc);
       __syncwarp();
       ring.taken();
@@ -676,7 +680,7 @@ exo_moe_down_ring_kernel(const MoeParams p, const __grid_constant__ CUtensorMap 
   const int S = (int)cluster.num_blocks(), r = (int)cluster.block_rank();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
   const int row0 = (int)(blockIdx.x / S) * 16;
-  Ring ring;
+  Ring ring(p.down_wait);
   ring.begin(bars, smem, p.down_piece, warp, lane);
   float* sums = reinterpret_cast<float*>(smem + kMoeWarps * kMoeStages * ring.stage_bytes);   // [warp][token][row]
   float* part = sums + kMoeWarps * p.tokens * 16;             // [token][row]
@@ -727,7 +731,7 @@ exo_moe_down_ring_kernel(const MoeParams p, const __grid_constant__ CUtensorMap 
   int iat = at, is = s;                               // the next copy
   auto issue = [&]() {
     if (any(iat, is)) {
-      if (lane == 0) ring.copy(&map, (int)(tb.active[iat].expert * p.down.expert_rows) + row0, nullptr, 0, is * P::kWords);
+      ring.copy(&map, (int)(tb.active[iat].expert * p.down.expert_rows) + row0, nullptr, 0, is * P::kWords);
       ring.copied();
       is = min(is + p.down_piece, stop_of(iat));
       if (is == steps) { is = 0; ++iat; }
@@ -762,7 +766,7 @@ exo_moe_down_ring_kernel(const MoeParams p, const __grid_constant__ CUtensorMap 
       const uint16_t* next = n_next ? row_at(ne, nf) : here;
       piece.scales_here();
       if (n_next) ask_scales(ne, nf, n_next);
-      const uint32_t w = ring.wait() + g * ring.pitch + 16 * t;
+      const uint32_t w = ring.wait(p.down_wait) + g * ring.pitch + 16 * t;
       piece.template multiply<NT>(w, ring.pitch, s, n, [&](int i) { return here + (int64_t)8 * i * p.ldh; }, next, n_next, nt, acc);
       __syncwarp();
       ring.taken();
@@ -1106,6 +1110,10 @@ exo_gemm_status_t exo_moe_run(exo_moe_handle_t plan, const exo_moe_weights_t* w,
   const bool many = p.tokens > (q4 ? 16 : 8);
   p.up_piece = many && !q4 ? 7 : 5;
   p.down_piece = q4 ? 5 : many ? 7 : 5;
+
+  const WaitHook hook = take_wait_hook();
+  p.up_wait = WaitBound{hook.clocks, hook.skip == 1};
+  p.down_wait = WaitBound{hook.clocks, hook.skip == 2};
 
   const bool bf16 = d.dtype == EXO_GEMM_BF16;
   const int nt = (p.tokens + 7) / 8;

@@ -414,6 +414,7 @@ struct FewParams {
   GemvParams g;
   int nk_log;       // parts of a tile's steps: 1 << nk_log
   int stages;
+  WaitBound wait;
   int digits_at, start_at, step_scale_at, ring_at;   // offsets in shared memory; the sums come first, the barriers before them
 };
 
@@ -483,6 +484,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) exo_gemv_q4_few_kernel(const F
   if (lane == 0)
     for (int i = 0; i < fp.stages; ++i) ptx::mbar_init(bar + 8 * i, 1);
   ptx::fence_mbar_init();
+  Copies copies(fp.wait);
   if (threadIdx.x == 0) strange = 0;
   __syncwarp();
   // unit u: tile cl + (u >> nk_log) * clusters, part u & (nk - 1) of its pieces
@@ -495,7 +497,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) exo_gemv_q4_few_kernel(const F
   auto issue = [&]() {
     if (iu < units) {
       const int row = row_of(iu), step = k_begin + ip * kFewPiece;
-      if (lane == 0) {
+      if (copies.issues) {
         ptx::mbar_arrive_expect_tx(bar + 8 * islot, stage_bytes);
         ptx::tma_load_3d(ring + islot * stage_bytes, &map, 0, row, step, bar + 8 * islot);
       }
@@ -595,7 +597,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) exo_gemv_q4_few_kernel(const F
       if (nu < units) srows = scale_rows<SC, PER, ZEROS>(p, row_of(nu), k_begin);
     }
     if (nu < units) load_scales(nxt, np);
-    wait_piece(bar + 8 * cslot, parity);
+    copies.wait<true>(bar + 8 * cslot, parity, fp.wait);
     const uint32_t w = ring + cslot * stage_bytes + g * 64 + t * 16;
     const int s0 = cp * kFewPiece, n = min(kFewPiece, k_steps - s0);
 #pragma unroll
@@ -708,6 +710,7 @@ __global__ void __launch_bounds__(kBatchThreads, 1) exo_gemv_q4_batch_kernel(con
     ptx::prefetch_tensormap(&map);
   }
   ptx::fence_mbar_init();
+  Copies copies(fp.wait);
   __syncwarp();
   auto row_of = [&](int u) { return (cl + (u >> fp.nk_log) * clusters) * 16; };
   auto begin_of = [&](int u) { return (pieces * (u & (nk - 1))) >> fp.nk_log; };
@@ -715,7 +718,7 @@ __global__ void __launch_bounds__(kBatchThreads, 1) exo_gemv_q4_batch_kernel(con
   int iu = warp, ip = begin_of(iu), islot = 0;            // the next copy
   auto issue = [&]() {
     if (iu < units) {
-      if (lane == 0) {
+      if (copies.issues) {
         ptx::mbar_arrive_expect_tx(bar + 8 * islot, stage_bytes);
         ptx::tma_load_3d(ring + islot * stage_bytes, &map, 0, row_of(iu), k_begin + ip * kBatchPiece, bar + 8 * islot);
       }
@@ -766,7 +769,7 @@ __global__ void __launch_bounds__(kBatchThreads, 1) exo_gemv_q4_batch_kernel(con
     for (int i = 0; i < NT; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
     const int end = end_of(u);
     for (int c = begin_of(u); c < end; ++c) {
-      wait_piece(bar + 8 * cslot, parity);
+      copies.wait<false>(bar + 8 * cslot, parity, fp.wait);
       const uint32_t w = ring + cslot * stage_bytes + g * 64 + t * 16;
       const int s0 = c * kBatchPiece, n = min(kBatchPiece, k_steps - s0);
       if (c + 1 < end) {
@@ -966,6 +969,12 @@ exo_gemm_status_t run_quant(const exo_q4_t* q, void* W, int64_t ldw, int32_t w_d
 }  // namespace
 unsigned take_gave_up_q4(cudaError_t* e) { return take_gave_up(e); }
 unsigned take_gave_up_moe(cudaError_t* e);   // moe.cu
+
+static std::atomic<int64_t> wait_hook{0};   // milliseconds * 4 + skip
+WaitHook take_wait_hook() {
+  const int64_t v = wait_hook.load(std::memory_order_relaxed) ? wait_hook.exchange(0) : 0;
+  return WaitHook{(uint64_t)(v / 4 > 0 ? v / 4 : 4000) * 2000000ull, (int)(v % 4)};
+}
 }  // namespace decode
 }  // namespace exo
 
@@ -977,6 +986,12 @@ extern "C" exo_gemm_status_t exo_decode_check(void) {
   const unsigned n = take_gave_up_q4(&e) | (e == cudaSuccess ? take_gave_up_moe(&e) : 0u);
   if (e != cudaSuccess) return cuda_failed(e);
   return n ? EXO_GEMM_ERR_DEVICE_TIMEOUT : EXO_GEMM_OK;
+}
+
+extern "C" exo_gemm_status_t exo_decode_debug_set(int32_t timeout_ms, int32_t skip_copies) {
+  if (timeout_ms < 0 || timeout_ms > 10000 || skip_copies < 0 || skip_copies > 2) return EXO_GEMM_ERR_INVALID_ARG;
+  wait_hook.store((int64_t)timeout_ms * 4 + skip_copies);
+  return EXO_GEMM_OK;
 }
 
 extern "C" exo_gemm_status_t exo_q4_quantize(const exo_q4_t* q, const void* W, int64_t ldw, int32_t w_dtype, void* cuda_stream) {
@@ -1037,6 +1052,8 @@ extern "C" exo_gemm_status_t exo_gemv_q4_run(const exo_q4_t* W, int64_t tokens, 
       if (nt > 0) groups = (unsigned)((p.tokens + 8 * nt - 1) / (8 * nt));
     }
     if (few || nt > 0) {
+      const WaitHook hook = take_wait_hook();
+      fp.wait = WaitBound{hook.clocks, hook.skip == 1};
       CUtensorMap map;
       if (!exo::encode_steps_map(&map, p.codes, (uint64_t)p.rows, (uint64_t)p.blocks, few ? kFewPiece : kBatchPiece)) return EXO_GEMM_ERR_CUDA;
       FewFn fn = bf16 ? pick_few<Bf16>(W->group, W->zeros, few, nt) : pick_few<Fp16>(W->group, W->zeros, few, nt);

@@ -15,7 +15,7 @@ from .binding import BF16, FP16, FP32, OK, ExoGemmError  # noqa: F401
 
 EXPORTED_SYMBOLS = (
     "exo_q4_quantize", "exo_q4_dequantize", "exo_gemv_q4_run", "exo_moe_validate", "exo_moe_create", "exo_moe_run",
-    "exo_moe_workspace_bytes", "exo_moe_destroy", "exo_decode_check",
+    "exo_moe_workspace_bytes", "exo_moe_destroy", "exo_decode_check", "exo_decode_debug_set",
 )
 
 _vp, _i32, _i64, _f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
@@ -62,6 +62,7 @@ def lib():
         L.exo_moe_run.argtypes = [_vp, weights, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _vp]
         L.exo_moe_workspace_bytes.argtypes = [_vp]
         L.exo_moe_destroy.argtypes = [_vp]
+        L.exo_decode_debug_set.argtypes = [_i32, _i32]
         for name in EXPORTED_SYMBOLS:
             getattr(L, name).restype = ctypes.c_int
         L.exo_moe_workspace_bytes.restype = _i64
@@ -100,6 +101,10 @@ def exo_moe_run(handle, weights, tokens: int, x_ptr: int, ldx: int, y_ptr: int, 
 
 def exo_decode_check() -> int:
     return lib().exo_decode_check()
+
+
+def exo_decode_debug_set(timeout_ms: int, skip_copies: int) -> int:
+    return lib().exo_decode_debug_set(timeout_ms, skip_copies)
 
 
 def exo_moe_workspace_bytes(handle) -> int:

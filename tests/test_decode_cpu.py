@@ -103,3 +103,9 @@ def test_pack_codes_follows_the_layout(rows, K):
             b, j, t, i = k // 128, k % 128 // 32, k % 32 // 8, k % 8
             n = i // 2 + 4 * (i % 2)
             assert (int(words[r, 16 * b + 4 * t + j]) >> 4 * n) & 15 == codes[r, k]
+
+
+def test_debug_set_refuses_bad_arguments():
+    for bad in ((-1, 0), (10001, 0), (20, -1), (20, 3)):
+        assert D.exo_decode_debug_set(*bad) == B.ERR_INVALID_ARG
+    assert D.exo_decode_debug_set(20, 2) == B.OK and D.exo_decode_debug_set(0, 0) == B.OK

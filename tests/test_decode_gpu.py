@@ -952,3 +952,36 @@ def test_moe_holds_the_inner_activations_of_few_tokens_in_two_parts(T, E, k, gro
             seen += 1
             assert (np.abs(once - ref) > bound).any()    # one part would show
     assert seen > 0
+
+
+# ------------------------------------------------------------------ bounded waits
+@pytest.mark.parametrize("tokens,rows,K,group", [(1, 9000, 9000, 128), (5, 2100, 4100, 64), (24, 16384, 1024, 32)])
+def test_gemv_reports_a_wait_that_runs_out_and_recovers(tokens, rows, K, group):
+    """The first warp issues no copies and waits 20 ms for them: an error status, no trap, and the next call is a good one."""
+    t = torch()
+    m = LargeMatrix(rows, K, group, D.BF16, True, seed=70)
+    x = t.randn(tokens, K, generator=t.Generator(device="cuda").manual_seed(71), device="cuda").bfloat16()
+    good, y = t.empty(tokens, rows, device="cuda"), t.empty(tokens, rows, device="cuda")
+    m.gemv(x, good)
+    assert D.exo_decode_check() == B.OK
+    assert D.exo_decode_debug_set(20, 1) == B.OK
+    m.gemv(x, y)
+    assert D.exo_decode_check() == B.ERR_DEVICE_TIMEOUT
+    assert D.exo_decode_check() == B.OK                  # said once
+    m.gemv(x, y)
+    assert D.exo_decode_check() == B.OK and t.equal(y, good)
+
+
+@pytest.mark.parametrize("skip", [1, 2])
+@pytest.mark.parametrize("T,group", [(2, 0), (12, 0), (40, 0), (2, 128), (20, 32)])
+def test_moe_reports_a_wait_that_runs_out_and_recovers(T, group, skip):
+    t = torch()
+    L = Layer(512, 384, 16, 1, 4, D.BF16, group=group, seed=72, max_tokens=T)
+    x = tokens(T, 512, D.BF16, 73).cuda()
+    good = L.run(x, 512)
+    assert D.exo_decode_check() == B.OK
+    assert D.exo_decode_debug_set(20, skip) == B.OK
+    L.run(x, 512)
+    assert D.exo_decode_check() == B.ERR_DEVICE_TIMEOUT
+    again = L.run(x, 512)
+    assert D.exo_decode_check() == B.OK and all(t.equal(a, b) for a, b in zip(good, again))
