@@ -985,3 +985,106 @@ def test_moe_reports_a_wait_that_runs_out_and_recovers(T, group, skip):
     assert D.exo_decode_check() == B.ERR_DEVICE_TIMEOUT
     again = L.run(x, 512)
     assert D.exo_decode_check() == B.OK and all(t.equal(a, b) for a, b in zip(good, again))
+
+
+# ------------------------------------------------------------------ rings in use: units beyond the warps, pieces beyond the stages
+STEADY = [  # tokens, rows, K, group, zeros: 25000 x 4100 has more units than warps, 16384 x 8192 more pieces than stages as well
+    (3, 25000, 4100, 32, True), (3, 16384, 8192, 128, False), (8, 25000, 4100, 64, False), (8, 16384, 8192, 32, True), (9, 25000, 4100, 128, True),
+    (24, 16384, 8192, 128, False), (24, 25000, 4100, 64, True), (24, 16384, 8192, 32, False), (40, 16384, 8192, 64, True), (40, 25000, 4100, 32, False),
+    (64, 16384, 8192, 128, True), (64, 16384, 8192, 32, False), (64, 25000, 4100, 64, True),
+    (32, 4096, 4096, 128, False), (64, 4096, 4096, 64, False), (57, 4096, 4096, 32, True)]   # four tiles of eight tokens to a CTA
+
+
+@pytest.mark.parametrize("tokens,rows,K,group,zeros", STEADY)
+@pytest.mark.parametrize("dtype,out", [(D.BF16, D.FP32), (D.FP16, D.FP16)])
+def test_gemv_of_several_tokens_and_large_matrices_against_its_definition(tokens, rows, K, group, zeros, dtype, out):
+    t = torch()
+    m = LargeMatrix(rows, K, group, dtype, zeros, seed=tokens + rows)
+    x = t.randn(tokens, K, generator=t.Generator(device="cuda").manual_seed(K), device="cuda").to(tt(dtype))
+    y = t.full((tokens, rows + 1), 3.0, device="cuda").to(tt(out))
+    m.gemv(x, y[:, :rows])
+    ref = x.double() @ m.values.T
+    allowed = sum_bound(K) * (x.double().abs() @ m.values.abs().T) + U[out] * 1.01 * ref.abs() + TINY[out]
+    off = (y[:, :rows].double() - ref).abs()
+    assert bool((off <= allowed).all()), float((off / allowed).max())
+    assert bool((y[:, rows:] == 3).all())
+
+
+class LargeLayer:
+    """A layer whose weights are made, and whose definition is evaluated, on the device."""
+
+    def __init__(self, H, F, E, shared, k, dtype, group, zeros, T, seed):
+        t = torch()
+        self.H, self.F, self.E, self.shared, self.k, self.dtype = H, F, E, shared, k, dtype
+        gen = t.Generator(device="cuda").manual_seed(seed)
+        n = E + shared
+        self.router = (t.randn(E, H, generator=gen, device="cuda") * 1.5 * H ** -0.5).to(tt(dtype))
+        self.vals, self.keep, mats = {}, [], []
+        for i, (name, rows, K) in enumerate((("gate", F, H), ("up", F, H), ("down", H, F))):
+            if group:
+                m = scaled(LargeMatrix(n * rows, K, group, dtype, zeros, seed + 1 + i), -int(np.log2(K) / 2))   # weights of about K^-1/2 / 10
+                self.vals[name] = m.values.view(n, rows, K)
+                mats.append(D.MoeMatrix(m.codes.data_ptr(), 0, rows, m.scales.data_ptr(), 0 if m.zeros is None else m.zeros.data_ptr()))
+            else:
+                m = (t.randn(n * rows, K, generator=gen, device="cuda") * K ** -0.5).to(tt(dtype))
+                self.vals[name] = m.double().view(n, rows, K)
+                mats.append(D.MoeMatrix(m.data_ptr(), K, rows, 0, 0))
+            self.keep.append(m)
+        self.weights = D.MoeWeights(self.router.data_ptr(), H, *mats)
+        self.plan = D.MoePlan(D.MoeDesc(H, F, E, shared, k, T, dtype, group))
+
+    def run(self, x):
+        t = torch()
+        T = x.shape[0]
+        y = t.empty(T, self.H, dtype=tt(self.dtype), device="cuda")
+        index, weight = t.empty(T, self.k, dtype=t.int32, device="cuda"), t.empty(T, self.k, device="cuda")
+        self.plan.run(self.weights, T, x.data_ptr(), self.H, y.data_ptr(), self.H, index.data_ptr(), weight.data_ptr(), stream())
+        return y, index, weight
+
+    def check(self, x, y, index, weight):
+        """As Layer.check; the inner activations of experts of up to four tokens are held in two parts."""
+        t = torch()
+        T, x, at = x.shape[0], x.double(), index.long()
+        r = self.router.double()
+        logits, lb = x @ r.T, sum_bound(self.H) * (x.abs() @ r.abs().T)
+        took = t.zeros(T, self.E, dtype=t.bool, device="cuda").scatter_(1, at, True)
+        assert bool((took.sum(1) == self.k).all())
+        inf = float("inf")
+        assert bool((t.where(took, logits + lb, inf).amin(1) >= t.where(took, -inf, logits - lb).amax(1)).all())
+        p = t.exp(logits - logits.amax(1, keepdim=True)).gather(1, at)
+        w = p / p.sum(1, keepdim=True)
+        assert bool(((weight.double() - w).abs() <= w * (t.expm1(2 * lb.amax(1, keepdim=True)) + 2.0 ** -14)).all())
+        part = t.zeros(T, self.E + self.shared, device="cuda", dtype=t.float64)
+        part[:, self.E:] = 1
+        part[:, :self.E].scatter_(1, at, weight.double())
+        ref, bound = t.zeros(T, self.H, device="cuda", dtype=t.float64), t.zeros(T, self.H, device="cuda", dtype=t.float64)
+        for e in range(self.E + self.shared):
+            rows = part[:, e].nonzero()[:, 0]
+            if len(rows) == 0:
+                continue
+            a, we = x[rows], part[rows, e][:, None]
+            gate, up, down = (self.vals[name][e] for name in ("gate", "up", "down"))
+            g, u = a @ gate.T, a @ up.T
+            bg, bu = sum_bound(self.H) * (a.abs() @ gate.abs().T), sum_bound(self.H) * (a.abs() @ up.abs().T)
+            silu = g / (1 + t.exp(-g))
+            h = we * silu * u
+            held = U[self.dtype] ** 2 if len(rows) <= 4 else U[self.dtype]
+            bh = we * (1.1 * bg * (u.abs() + bu) + silu.abs() * bu) + h.abs() * (16 * 2.0 ** -24 + held) * 1.01 + TINY[self.dtype]
+            ref[rows] += h @ down.T
+            bound[rows] += bh @ down.abs().T + sum_bound(self.F) * (h.abs() @ down.abs().T)
+        bound += ref.abs() * (U[self.dtype] * 1.01 + (self.k + self.shared) * 2.0 ** -20) + TINY[self.dtype]
+        off = (y.double() - ref).abs()
+        assert bool((off <= bound).all()), float((off / bound).max())
+
+
+@pytest.mark.parametrize("T", [1, 4, 8, 16, 64])
+@pytest.mark.parametrize("group,zeros,dtype", [(0, False, D.BF16), (0, False, D.FP16), (128, False, D.BF16), (64, True, D.FP16), (32, True, D.BF16)])
+def test_moe_of_many_items_against_its_definition(T, group, zeros, dtype):
+    """32 experts of 2048 x 1536 and a shared one: from four tokens on more items than a CTA has warps, and several pieces to each."""
+    t = torch()
+    L = LargeLayer(2048, 1536, 32, 1, 4, dtype, group, zeros, T, seed=80)
+    x = t.randn(T, 2048, generator=t.Generator(device="cuda").manual_seed(T), device="cuda").to(tt(dtype))
+    got = L.run(x)
+    L.check(x, *got)
+    assert all(t.equal(a, b) for a, b in zip(got, L.run(x)))
+    assert D.exo_decode_check() == B.OK
