@@ -359,6 +359,7 @@ __device__ __forceinline__ void store_inner(const MoeParams& p, const float* wei
 // ==== the taken experts' weights ====================================================================================
 // A warp's own ring of pieces: `piece` steps (64 bytes of a row each, an odd number of them, so that the rows of a fragment
 // lie in different banks) of 16 rows, brought by tiled copies that the warp issues itself and waits for itself.
+constexpr int kPairSmem = 110 * 1024;   // dynamic shared memory with which two CTAs fit an SM
 constexpr int kMoeWarps = 8, kMoeThreads = 32 * kMoeWarps, kMoeStages = 2, kMostPiece = 7;
 
 struct Ring {
@@ -498,8 +499,10 @@ struct PieceQ4 {
 template <class T, int FMT> struct PieceOf { using type = PieceQ4<T, 1 << (FMT - 2)>; };
 template <class T> struct PieceOf<T, 1> { using type = Piece16<T>; };
 
-// A CTA cuts its items into parts while it has fewer units than this: two turns of its warps, or one where the sums are large.
-__host__ __device__ constexpr int part_limit(int nt) { return nt <= 2 ? 2 * kMoeWarps : kMoeWarps; }
+// A CTA cuts its items into parts while it has fewer units than this: two turns of its warps, or one where the sums are large.  With two
+// turns for two tiles of tokens the sums (32 KB) and the routing tables left no room for a second CTA of 4-bit experts: 16 tokens,
+// 8 of 64 of 4096 x 1536, 245 us; 203 with one turn.
+__host__ __device__ constexpr int part_limit(int nt) { return nt == 1 ? 2 * kMoeWarps : kMoeWarps; }
 
 constexpr int kUnitsAhead = 4;
 
@@ -1105,11 +1108,10 @@ exo_gemm_status_t exo_moe_run(exo_moe_handle_t plan, const exo_moe_weights_t* w,
   p.ldxs = p.copy_x ? plan->ldxs : ldx;
   // Pieces: larger ones suit the copies, smaller ones leave room for a second CTA on the SM, which covers the first one's
   // start and end (5 steps: 80 KB of ring).  Measured, one CTA of 7 steps against two of 5 (us): 16 bits, 64 experts of 4096 x 1536 and
-  // a shared one, 8 tokens 236 / 233, 9 tokens 265 / 286, 16 tokens 335 / 360, 64 tokens 537 / 675; 4 bits (one CTA or two of 5), 8
-  // experts of 4096 x 8192, 16 tokens 242 / 166, 24 tokens 302 / 349, 64 tokens 740 / 783.
-  const bool many = p.tokens > (q4 ? 16 : 8);
-  p.up_piece = many && !q4 ? 7 : 5;
-  p.down_piece = q4 ? 5 : many ? 7 : 5;
+  // a shared one, 8 tokens 236 / 233, 9 tokens 265 / 286, 16 tokens 335 / 360, 64 tokens 537 / 675.  4-bit experts keep 5: two CTAs up to 16
+  // tokens, beyond that one, for which eight tiles' sums leave room (8 experts of 4096 x 8192, one CTA or two: 16 tokens 242 / 166, 24 tokens
+  // 302 / 349, 64 tokens 740 / 783).
+  p.up_piece = p.down_piece = !q4 && p.tokens > 8 ? 7 : 5;
 
   const WaitHook hook = take_wait_hook();
   p.up_wait = WaitBound{hook.clocks, hook.skip == 1};
@@ -1148,7 +1150,7 @@ exo_gemm_status_t exo_moe_run(exo_moe_handle_t plan, const exo_moe_weights_t* w,
     st = launch(fn, (unsigned)((p.inner + 7) / 8), (unsigned)p.taken, kPlainThreads, 0, 1, stream, &p);
   } else {
     const size_t smem = (size_t)kMoeWarps * kMoeStages * p.up_piece * 1024 + (size_t)2 * part_limit(nt_kernel) * nt_kernel * 512 + table_bytes(p);
-    const int64_t items = (int64_t)p.taken * ((p.inner + 7) / 8), slots = (int64_t)(many ? 1 : 2) * plan->sms;
+    const int64_t items = (int64_t)p.taken * ((p.inner + 7) / 8), slots = (int64_t)(smem <= kPairSmem ? 2 : 1) * plan->sms;
     st = launch(fn, (unsigned)(items < slots ? items : slots), 1, kMoeThreads, smem, 1, stream, &p, &gate, &up);
   }
   if (st != EXO_GEMM_OK) return st;
@@ -1160,7 +1162,7 @@ exo_gemm_status_t exo_moe_run(exo_moe_handle_t plan, const exo_moe_weights_t* w,
   // The cluster size with the shortest estimate: a turn of the CTAs that fit costs their start and end (4 us, and more for
   // the sums of many tokens) and the weights at an SM's share of the bandwidth, 44 GB/s.
   const size_t smem = (size_t)kMoeWarps * kMoeStages * p.down_piece * 1024 + (size_t)(kMoeWarps + 1) * p.tokens * 64 + table_bytes(p);
-  const int fit = smem <= 110 * 1024 ? 2 : 1;
+  const int fit = smem <= kPairSmem ? 2 : 1;
   S = 1;
   double best = 0.0;
   for (int c = 1; c <= 8 && (c == 1 || all_steps >= (int64_t)c * kMoeWarps); c *= 2) {
