@@ -334,16 +334,18 @@ __device__ __forceinline__ int halves_of(int count) { return count <= kHalvesTok
 // Inner activations from lane l's part of tile i: gate in x, y and up in z, w for two tokens.  Rounding them to 16 bits would cost
 // as much accuracy as rounding y does.  Where an expert has up to four tokens, the columns of their fragment have room for the rounding's
 // remainder too, as a token of its own, and `down` adds both; with more tokens one 16-bit value is kept, as for any 16-bit matrix product.
+// (Two parts for every expert of up to 8 or 32 tokens take further tiles of `down`: 64 tokens of 64 experts of 4096 x 1536, 539 us,
+// 567 and 583.)
 template <class T>
 __device__ __forceinline__ void store_inner(const MoeParams& p, const float* weight, const Active& a, int f0, int i, int l, const float4& sums) {
   const int n = 8 * i + 2 * (l & 3), col = f0 + (l >> 2);
   if (col >= p.inner) return;
   const float gate[2] = {sums.x, sums.y}, up[2] = {sums.z, sums.w};
   const int halves = halves_of(a.count);
-#pragma unroll
+#pragma unroll 1   // the code of eight tiles twice over costs the 4-bit kernel registers (64 tokens of 8 experts of 4096 x 8192: 770 us, 733 so)
   for (int q = 0; q < 2; ++q)
     if (n + q < a.count) {
-      const float v = weight[a.base + n + q] * (gate[q] / (1.f + expf(-gate[q])) * up[q]);
+      const float gq = q ? gate[1] : gate[0], uq = q ? up[1] : up[0], v = weight[a.base + n + q] * (gq / (1.f + expf(-gq)) * uq);
       uint16_t* to = p.h + (2 * (int64_t)a.base + ((n + q) << halves)) * p.ldh + col;
       if (halves && fabsf(v) <= 3.4028235e38f) {   // beyond the type's range the first part is its largest value, the second the rest
         const uint16_t hi = T::from_float(fminf(fmaxf(v, -T::max_finite()), T::max_finite()));
@@ -359,8 +361,8 @@ __device__ __forceinline__ void store_inner(const MoeParams& p, const float* wei
 // ==== the taken experts' weights ====================================================================================
 // A warp's own ring of pieces: `piece` steps (64 bytes of a row each, an odd number of them, so that the rows of a fragment
 // lie in different banks) of 16 rows, brought by tiled copies that the warp issues itself and waits for itself.
-constexpr int kPairSmem = 110 * 1024;   // dynamic shared memory with which two CTAs fit an SM
 constexpr int kMoeWarps = 8, kMoeThreads = 32 * kMoeWarps, kMoeStages = 2, kMostPiece = 7;
+constexpr int kPairSmem = 110 * 1024;   // dynamic shared memory with which two CTAs fit an SM
 
 struct Ring {
   uint32_t bar, base;
