@@ -1013,7 +1013,7 @@ extern "C" exo_gemm_status_t exo_gemv_q4_run(const exo_q4_t* W, int64_t tokens, 
   const bool read = alpha != 0.f && W->K > 0;
   if (!Y || (read && !X)) return EXO_GEMM_ERR_NULL;
   if (read && (st = check_q4_pointers(W)) != EXO_GEMM_OK) return st;
-  if (((uintptr_t)X & 1u) || ((uintptr_t)Y & (y_dtype == EXO_GEMM_FP32 ? 3u : 1u))) return EXO_GEMM_ERR_ALIGNMENT;
+  if ((read && ((uintptr_t)X & 1u)) || ((uintptr_t)Y & (y_dtype == EXO_GEMM_FP32 ? 3u : 1u))) return EXO_GEMM_ERR_ALIGNMENT;
   int sms = 0;
   if ((st = device_check(&sms)) != EXO_GEMM_OK) return st;
   GemvParams p{};

@@ -1088,3 +1088,13 @@ def test_moe_of_many_items_against_its_definition(T, group, zeros, dtype):
     L.check(x, *got)
     assert all(t.equal(a, b) for a, b in zip(got, L.run(x)))
     assert D.exo_decode_check() == B.OK
+
+
+@pytest.mark.parametrize("K,alpha", [(256, 0.0), (0, 1.0)])
+def test_gemv_without_products_does_not_look_at_the_address_of_x(K, alpha):
+    t = torch()
+    m = Matrix(70, 256, 64, D.BF16, False, seed=1)
+    y = t.full((3, 70), 1.5, device="cuda")
+    q = D.Q4(70, K, 64, D.BF16, m.codes.data_ptr(), m.scales.data_ptr())
+    q.gemv(3, y.data_ptr() + 1, max(K, 1), y.data_ptr(), 70, D.FP32, alpha, 2.0, stream())
+    assert (y == 3).all()
