@@ -1109,11 +1109,11 @@ exo_gemm_status_t exo_moe_run(exo_moe_handle_t plan, const exo_moe_weights_t* w,
   p.xs = p.copy_x ? (const uint16_t*)(plan->ws + plan->at_xs) : p.x;
   p.ldxs = p.copy_x ? plan->ldxs : ldx;
   // Pieces: larger ones suit the copies, smaller ones leave room for a second CTA on the SM, which covers the first one's
-  // start and end (5 steps: 80 KB of ring).  Measured, one CTA of 7 steps against two of 5 (us): 16 bits, 64 experts of 4096 x 1536 and
-  // a shared one, 8 tokens 236 / 233, 9 tokens 265 / 286, 16 tokens 335 / 360, 64 tokens 537 / 675.  4-bit experts keep 5: two CTAs up to 16
-  // tokens, beyond that one, for which eight tiles' sums leave room (8 experts of 4096 x 8192, one CTA or two: 16 tokens 242 / 166, 24 tokens
-  // 302 / 349, 64 tokens 740 / 783).
-  p.up_piece = p.down_piece = !q4 && p.tokens > 8 ? 7 : 5;
+  // start and end (5 steps: 80 KB of ring), up to 16 tokens, whose sums leave room for it.  5 steps against 7 (us): 16 bits, 64 experts of
+  // 4096 x 1536 and a shared one, 8 tokens 234 / 243, 9 tokens 254 / 271, 16 tokens 319 / 343, 20 tokens 411 / 414, 64 tokens 645 / 538; 8 of 64 of
+  // 2048 x 1024, 16 tokens 136 / 141.  4 bits, 8 experts of 4096 x 8192, one token 50.6 / 55.8, 16 tokens 162 / 209, 24 tokens 311 / 302, 64 tokens
+  // 728 / 715: 5 for all.
+  p.up_piece = p.down_piece = !q4 && p.tokens > 16 ? 7 : 5;
 
   const WaitHook hook = take_wait_hook();
   p.up_wait = WaitBound{hook.clocks, hook.skip == 1};
