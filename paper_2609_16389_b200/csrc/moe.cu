@@ -1164,7 +1164,7 @@ exo_gemm_status_t exo_moe_run(exo_moe_handle_t plan, const exo_moe_weights_t* w,
   // The cluster size with the shortest estimate: a turn of the CTAs that fit costs their start and end (4 us, and more for
   // the sums of many tokens) and the weights at an SM's share of the bandwidth, 44 GB/s.
   const size_t smem = (size_t)kMoeWarps * kMoeStages * p.down_piece * 1024 + (size_t)(kMoeWarps + 1) * p.tokens * 64 + table_bytes(p);
-  const int fit = smem <= kPairSmem ? 2 : 1;
+  const int fit = smem <= kPairSmem && !(q4 && nt_kernel > 2) ? 2 : 1;   // (eight tiles of 4-bit experts take all registers)
   S = 1;
   double best = 0.0;
   for (int c = 1; c <= 8 && (c == 1 || all_steps >= (int64_t)c * kMoeWarps); c *= 2) {
