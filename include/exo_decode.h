@@ -5,13 +5,14 @@
  *   exo_gemv_q4_run                       Y = alpha * X * W^T + beta * Y, W in 4 bits, 1 to 64 tokens
  *   exo_moe_create / run / destroy        a whole mixture-of-experts layer for 1 to 64 tokens, 16- or 4-bit experts
  *
- * For more tokens the same weights go through exo_q4_dequantize and exo_gemm_run (exo_gemm.h), whose status codes,
- * types and conventions hold here (exo_gemm_last_cuda_error included): all pointers to matrices are DEVICE pointers owned by the caller, calls are
+ * For more tokens a 4-bit matrix goes through exo_q4_dequantize and exo_gemm_run (exo_gemm.h); a layer takes them 64 at a time.  The status codes,
+ * types and conventions of exo_gemm.h hold here (exo_gemm_last_cuda_error included): all pointers to matrices are DEVICE pointers owned by the caller, calls are
  * enqueued on cuda_stream (a cudaStream_t; NULL = the legacy default stream) and return without synchronising, every
  * check happens before the first launch, nothing runs on the CPU, and a device that is not compute capability 10.x is
  * refused with EXO_GEMM_ERR_ARCH.  Calls may be captured into a CUDA graph.  Launches use programmatic dependent
  * launch: a kernel may begin while its predecessor in the stream drains, and waits for it before it reads or writes
- * anything (it only asks the L2 cache for weights earlier).
+ * anything.  The last of a layer's three kernels reads the routing tables and its first weights before the second one has ended: what
+ * came before the layer, and the first kernel, have ended by then.
  *
  * Every result is bitwise reproducible from run to run on the same inputs: sums are taken in fixed orders.
  */
@@ -71,7 +72,8 @@ exo_gemm_status_t exo_q4_dequantize(const exo_q4_t* q, void* W, int64_t ldw, int
  * Products are formed from the integers code - zero and a group's sum is multiplied by its scale in fp32; all further
  * sums are fp32.  The factors are the 16-bit activations and a group is summed in fp32; or, for one or two tokens and a large
  * matrix, they are integers of 30 bits that stand for the activations of 128 neighbouring k: exact for values down to 2^-22 (bf16) or
- * 2^-19 (fp16) of the largest of the 128, and off by at most 2^-30 of that largest below; their group sums are exact.
+ * 2^-19 (fp16) of the largest of the 128, and off by at most 2^-30 of that largest below; their group sums are exact.  (Tokens with values
+ * that are not finite, and results that come out so, are summed in fp32.)
  */
 exo_gemm_status_t exo_gemv_q4_run(const exo_q4_t* W, int64_t tokens, const void* X, int64_t ldx, void* Y, int64_t ldy,
                                   int32_t y_dtype, float alpha, float beta, void* cuda_stream);

@@ -7,9 +7,10 @@
 //
 // The layer is bound by reading the taken experts' weights once.  A fragment (decode_core.cuh) is 16 weight rows by eight of the
 // expert's own tokens.  Measured on a B200 (CUDA graph of passes, three sets of inputs in turn): 8 of 64 experts of 2048 x 1024 in
-// bf16, one token, 30 us for 101 MB (15.4 at the copy bandwidth): of that 5.4 are routing, 2 to 4 each kernel's start and 1 to 2
-// its end, and the weights themselves stream at the bandwidth; 64 tokens, 6 of 64 and a shared one of 4096 x 1536, 537 us
-// for 2.45 GB (374).  4-bit experts are held up by their unpacking (2 of 8 of 4096 x 8192, one token, 51 us; 15.9).
+// bf16, one token, 29.5 us for 101 MB (15.4 at the copy bandwidth): 5.4 are routing, and `up` and `down` each have a start of 2 to 4 us and an end
+// of 1 to 2 in which memory is idle (alone, `up` draws 44 % of the nominal bandwidth and `down` 27 %); 64 tokens, 6 of 64 and a shared one of
+// 4096 x 1536, 538 us for 2.45 GB (374).  4-bit experts are held up by their unpacking (2 of 8 of 4096 x 8192, one token, 51 us; 15.9), from 17
+// tokens on by their activations from L2 too (24 tokens 309 us, 64 tokens 729; 63).
 #include <cooperative_groups.h>
 
 #include <new>
@@ -820,7 +821,8 @@ exo_moe_down_ring_kernel(const MoeParams p, const __grid_constant__ CUtensorMap 
 
 // ==== 16-bit rows that a tiled copy cannot address ==================================================================
 // Rows that do not start on 16-byte boundaries are read element by element, straight into the fragments: right at any
-// leading dimension, and slow.
+// leading dimension, and slow (us, 8 of 64 experts: one token 2048 x 1024 32, 2044 x 1020 92, 2047 x 1023 81; 16 tokens 143, 573 and 485; 6 of 64 and a
+// shared one, 64 tokens, 4096 x 1536 540, 4095 x 1535 1538).
 constexpr int kPlainThreads = 256, kPlainWarps = 8;
 
 // Steps of 32 from s on, ds apart, of the lane's rows r0 and r1; the lane's activations of tile i begin at x0 + i * stride, or at

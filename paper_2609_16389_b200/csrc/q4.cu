@@ -401,12 +401,13 @@ __global__ void __launch_bounds__(kGemvThreads, 2) exo_gemv_q4_kernel(const Gemv
 // copies.  A lane's parts of a step are 16 bytes of rows g and g + 8.
 //
 // The digits have to be made by every CTA, so the matrix has to be large before the saved instructions are ahead of the 16-bit
-// kernel below.  Measured, integer against 16-bit products (us, group 128, bf16):
+// kernel below.  Measured in a CUDA graph, integer against 16-bit products (us, group 128, bf16):
 //                   1024 x 2048  4096 x 4096  8192 x 8192  16384 x 8192  32768 x 16384
-//   one token         3.8 / 3.0    5.3 / 5.0  12.5 / 12.8   18.3 / 20.8    50.4 / 70.2
-//   two tokens        4.3 / 3.0    6.6 / 5.2  13.7 / 13.2   19.7 / 21.3    59.4 / 70.8
+//   one token         4.0 / 3.0    5.2 / 5.0  12.2 / 12.6   18.4 / 20.4    49.8 / 67.9
+//   two tokens        4.6 / 3.0    6.5 / 5.2  13.2 / 12.9   19.6 / 20.8    58.7 / 68.3
 // and with three and four tokens, whose digits take twice the columns, 83 / 71 and 87 / 72 on 32768 x 16384.  Hence two tokens at
-// most, and 256 KB of weights for every SM.  32768 x 16384 is 277 MB: one token at 5.5 TB/s, 0.84 of what a copy does.
+// most, and 256 KB of weights for every SM.  32768 x 16384 is 277 MB: one token at 5.6 TB/s, 0.85 of what a copy does (called
+// from Python one by one 53 us, 0.80).
 constexpr int kFewWarps = 8, kFewThreads = 32 * kFewWarps, kFewPiece = 8, kFewTokens = 2, kFewSteps = 256;   // steps of 1 KB per SM
 constexpr int kMagic = 0x4b400000;        // 1.5 * 2^23
 
@@ -681,7 +682,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) exo_gemv_q4_few_kernel(const F
 // The same cut, with 16-bit products: a step's codes become exact 16-bit integers once for NT tiles of
 // eight tokens, whose values for the CTA's part of k lie in shared memory for the whole run (rows 64 bytes off a
 // multiple of 128, so that a fragment load is free of bank conflicts).  Eight more tokens cost a step 8 matrix instructions and
-// four 512-byte loads of activations.  16384 x 8192 (69 MB, 10.7 us at the copy bandwidth), us: 20.8 for one token, 23 for 8, 30 for
+// four 512-byte loads of activations.  16384 x 8192 (69 MB, 10.7 us at the copy bandwidth), us: 20.4 for one token, 23 for 8, 30 for
 // 16, 37 for 24: at one token the unpacking is the bound, and every further tile adds its loads and products, which a warp
 // does not overlap with the unpacking (ncu at 24 tokens: issue slots 51 % used, the tensor pipe 35 %, DRAM 20 %).
 constexpr int kBatchWarps = 16, kBatchThreads = 32 * kBatchWarps, kBatchPiece = 2;
@@ -847,7 +848,7 @@ template <class T> FewFn pick_few(int group, bool zeros, bool few, int nt) {
 }
 
 // How the integer kernel is cut: one CTA per SM with pieces of 8 steps, which the copies like best (32768 x 16384, one token:
-// 50.4 us; 54.8 with two CTAs and pieces of 4).  The cluster cuts k where a CTA's digits would take more than 40 KB.  False: not
+// 50 us; 55 with two CTAs and pieces of 4).  The cluster cuts k where a CTA's digits would take more than 40 KB.  False: not
 // for this size, or the sums do not fit.
 bool plan_few(FewParams& fp, const GemvParams& p, int per, int sms, unsigned* ctas, unsigned* cluster, size_t* smem) {
   const int64_t tiles = (p.rows + 15) / 16;
