@@ -138,6 +138,7 @@ def prepare(case, seed):
             from paper_2609_16389_b200 import fused as E
             t = E.BF16 if c["dtype"] == "bf16" else E.FP16
             s["plan"] = E.CePlan(E.CeDesc(T, H, V, t, training=int(c["train"]), grad_dtype=t, label_smoothing=c["smoothing"]))
+            s["saved"] = torch.empty(s["plan"].saved_bytes(), device=DEV, dtype=torch.uint8)
     else:
         N, K = c["N"], c["K"]
         x = torch.randn(T, K, device=DEV, generator=g)
@@ -188,10 +189,11 @@ def _run_own(s):
         return {n: s[n] for n in ("y", "dx", "dgate_up", "ddown")}
     if c["op"] == "ce":
         plan = s["plan"]
-        plan.forward(p("x"), p("w"), p("target"), p("loss"), p("lse"), stream=stream)
         if not c["train"]:
+            plan.forward(p("x"), p("w"), p("target"), p("loss"), p("lse"), stream=stream)
             return {"loss": s["loss"], "lse": s["lse"]}
-        plan.backward(p("x"), p("w"), p("target"), p("lse"), p("dloss"), p("dx"), p("dw"), stream=stream)
+        plan.forward(p("x"), p("w"), p("target"), p("loss"), p("lse"), p("saved"), stream)
+        plan.backward(p("x"), p("w"), p("target"), p("lse"), p("dloss"), p("saved"), p("dx"), p("dw"), stream=stream)
         return {n: s[n] for n in ("loss", "lse", "dx", "dw")}
     s["qx"].quantize(p("x"), c["K"], E.BF16 if c["dtype"] == "bf16" else E.FP16, stream)
     s["qw"].gemm(s["qx"], p("y"), c["N"], {"bf16": E.BF16, "fp16": E.FP16, "fp32": E.FP32}[c["out"]], stream=stream)
