@@ -15,10 +15,11 @@ LIB = os.path.join(HERE, "libexo_gemm.so")
 SHARE_DIR = os.path.join(CSRC, "cluster4")
 SHARE_LIB = os.path.join(HERE, "libexo_gemm_cluster4.so")
 SHARE_DEPS = [os.path.join("cluster4", "share_pairs.cuh")]
-SOURCES = ["api.cu", "gemv.cu", "q4.cu", "moe.cu"]
+SOURCES = ["api.cu", "gemv.cu", "q4.cu", "moe.cu", "ffn.cu", "ce.cu", "i8.cu"]
 DEPS = ["api.cu", "gemv.cu", "gemm_kernel.cuh", "gemm_params.h", "plan.h", "ptx.cuh", "tile_scheduler.h",
-        "q4.cu", "moe.cu", "decode_core.cuh", "decode_host.h",
-        os.path.join("..", "..", "include", "exo_gemm.h"), os.path.join("..", "..", "include", "exo_decode.h")]
+        "q4.cu", "moe.cu", "decode_core.cuh", "decode_host.h", "ffn.cu", "ce.cu", "i8.cu", "fused_core.cuh", "fused_host.h",
+        os.path.join("..", "..", "include", "exo_gemm.h"), os.path.join("..", "..", "include", "exo_decode.h"),
+        os.path.join("..", "..", "include", "exo_fused.h")]
 
 
 def nvcc_path() -> str:

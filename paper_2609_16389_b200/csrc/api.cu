@@ -236,6 +236,23 @@ bool encode_rows_map(CUtensorMap* map, int word_bytes, const void* base, uint64_
   return r == CUDA_SUCCESS;
 }
 
+// The rows of a tensor-core operand (fused_host.h): boxes of 128 bytes of `box_rows` rows, 128-byte swizzle, zeros outside.
+bool encode_operand_map(CUtensorMap* map, int elem_bytes, bool bf16, const void* base, uint64_t inner, uint64_t rows, uint64_t row_bytes,
+                        uint32_t box_rows) {
+  EncodeTiledFn fn = get_encode_fn();
+  cuuint64_t dims[2] = {inner, rows};
+  cuuint64_t strides[1] = {row_bytes};
+  cuuint32_t box[2] = {128u / (uint32_t)elem_bytes, box_rows};
+  cuuint32_t estr[2] = {1, 1};
+  const CUtensorMapDataType dt = elem_bytes == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                                                                                       : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+  const CUresult r = !fn ? CUDA_ERROR_NOT_FOUND
+                         : fn(map, dt, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) g_last_cuda_error = (int)r;
+  return r == CUDA_SUCCESS;
+}
+
 }  // namespace exo
 
 struct exo_gemm_plan {
@@ -493,8 +510,11 @@ exo_gemm_status_t exo_gemm_create(exo_gemm_handle_t* out, const exo_gemm_desc_t*
   return exo_gemm_create_batched(out, desc, 1, 0, 0, 0);
 }
 
-exo_gemm_status_t exo_gemm_create_batched(exo_gemm_handle_t* out, const exo_gemm_desc_t* desc, int64_t batch_count,
-                                          int64_t stride_a, int64_t stride_b, int64_t stride_c) {
+}  // extern "C"
+
+// repack_more: matrices (4 = C) that go through an aligned copy although TMA could address them.
+static exo_gemm_status_t create_plan(exo_gemm_handle_t* out, const exo_gemm_desc_t* desc, int64_t batch_count, int64_t stride_a, int64_t stride_b,
+                                     int64_t stride_c, int repack_more) {
   if (!out) return EXO_GEMM_ERR_NULL;
   exo_gemm_status_t st = validate_batch(desc, batch_count, stride_a, stride_b, stride_c);
   if (st != EXO_GEMM_OK) return st;
@@ -518,7 +538,7 @@ exo_gemm_status_t exo_gemm_create_batched(exo_gemm_handle_t* out, const exo_gemm
   exo_gemm_plan* p = new (std::nothrow) exo_gemm_plan{};
   if (!p) return EXO_GEMM_ERR_CUDA;
   p->user_desc = *desc;
-  p->repack = repack_mask(*desc);
+  p->repack = repack_mask(*desc) | repack_more;
   p->desc = aligned_desc(*desc, p->repack);
   p->canon = canonicalize(p->desc, batch_count, stride_a, stride_b, stride_c);
   p->device = device;
@@ -584,6 +604,22 @@ exo_gemm_status_t exo_gemm_create_batched(exo_gemm_handle_t* out, const exo_gemm
   return EXO_GEMM_OK;
 }
 
+namespace exo {
+// A plan that writes nothing but the M x N values of a row-major C: a TMA store moves 16 bytes at a time, so where a row ends inside such
+// a piece the rest of it, which belongs to the caller's gap between rows, is written as well unless C goes through a copy (fused_host.h).
+exo_gemm_status_t gemm_create_exact(exo_gemm_handle_t* out, const exo_gemm_desc_t* desc) {
+  const bool gap = desc->M > 0 && desc->N > 0 && desc->ldc > desc->N && desc->N * elem_bytes(desc->c_dtype) % 16 != 0;
+  return create_plan(out, desc, 1, 0, 0, 0, gap ? 4 : 0);
+}
+}  // namespace exo
+
+extern "C" {
+
+exo_gemm_status_t exo_gemm_create_batched(exo_gemm_handle_t* out, const exo_gemm_desc_t* desc, int64_t batch_count,
+                                          int64_t stride_a, int64_t stride_b, int64_t stride_c) {
+  return create_plan(out, desc, batch_count, stride_a, stride_b, stride_c, 0);
+}
+
 exo_gemm_status_t exo_gemm_get_info(exo_gemm_handle_t plan, exo_gemm_info_t* info) {
   if (!plan || !info) return EXO_GEMM_ERR_NULL;
   fill_info(plan, info);
@@ -631,7 +667,7 @@ exo_gemm_status_t check_run_args(const exo_gemm_plan* plan, const void* A, const
 
 // Tensor maps and the launch, for arguments that passed check_run_args.
 exo_gemm_status_t launch_plan(exo_gemm_plan* plan, const void* A, const void* B, void* C, float alpha, float beta,
-                              void* cuda_stream) {
+                              void* cuda_stream, const float* alpha_dev = nullptr) {
   const Canonical& cn = plan->canon;
   const bool read_ab = alpha != 0.f && cn.K > 0;
   const exo_gemm_desc_t& d = plan->desc;
@@ -695,6 +731,7 @@ exo_gemm_status_t launch_plan(exo_gemm_plan* plan, const void* A, const void* B,
   prm.split_flags = plan->d_split_flags;
   prm.split_arrivals = (uint32_t)(kEpiWarps * cfg.cta_group * cfg.mrep);
   prm.alpha = read_ab ? alpha : 0.f;
+  prm.alpha_dev = read_ab ? alpha_dev : nullptr;
   prm.beta = beta;
   prm.idesc = make_idesc(d.ab_dtype, cn.a_mn_major, cn.b_mn_major, 128 * cfg.cta_group, cfg.tile_n);
   prm.a = make_staging(cn.a_mn_major, kBlockM * cfg.mrep, cfg.ksub, cn.ab_bytes);
@@ -806,15 +843,16 @@ exo_gemm_status_t copy_matrix(const exo_gemm_plan* plan, int m, void* dst, const
 
 }  // namespace
 
-extern "C" {
+namespace exo {
 
-exo_gemm_status_t exo_gemm_run(exo_gemm_handle_t plan, const void* A, const void* B, void* C, float alpha,
-                               float beta, void* cuda_stream) {
+// exo_gemm_run with a factor of alpha that is read on the device when the kernel runs (fused_host.h).
+exo_gemm_status_t gemm_run_scaled(exo_gemm_plan* plan, const void* A, const void* B, void* C, float alpha, const float* alpha_dev, float beta,
+                                  void* cuda_stream) {
   if (!plan) return EXO_GEMM_ERR_NULL;
   bool launch = false;
   exo_gemm_status_t st = check_run_args(plan, A, B, C, alpha, &launch);
   if (st != EXO_GEMM_OK || !launch) return st;
-  if (!plan->repack) return launch_plan(plan, A, B, C, alpha, beta, cuda_stream);
+  if (!plan->repack) return launch_plan(plan, A, B, C, alpha, beta, cuda_stream, alpha_dev);
   // Matrices whose rows TMA cannot address travel through the plan's aligned copies: operands in before the
   // GEMM, C in as well if it is read, C out after it (only its M x N elements: the caller's padding is untouched).
   DeviceGuard guard(plan->device);
@@ -829,9 +867,18 @@ exo_gemm_status_t exo_gemm_run(exo_gemm_handle_t plan, const void* A, const void
     st = copy_matrix(plan, m, plan->d_pack[m], user[m], /*into_aligned=*/true, cuda_stream);
     if (st != EXO_GEMM_OK) return st;
   }
-  st = launch_plan(plan, eff[0], eff[1], const_cast<void*>(eff[2]), alpha, beta, cuda_stream);
+  st = launch_plan(plan, eff[0], eff[1], const_cast<void*>(eff[2]), alpha, beta, cuda_stream, alpha_dev);
   if (st != EXO_GEMM_OK || !(plan->repack & 4)) return st;
   return copy_matrix(plan, 2, C, plan->d_pack[2], /*into_aligned=*/false, cuda_stream);
+}
+
+}  // namespace exo
+
+extern "C" {
+
+exo_gemm_status_t exo_gemm_run(exo_gemm_handle_t plan, const void* A, const void* B, void* C, float alpha,
+                               float beta, void* cuda_stream) {
+  return gemm_run_scaled(plan, A, B, C, alpha, nullptr, beta, cuda_stream);
 }
 
 exo_gemm_status_t exo_gemm_check(exo_gemm_handle_t plan, uint32_t* detail) {

@@ -1,0 +1,471 @@
+// Products whose epilogue is an operator: the two kernels behind exo_fused.h.
+//
+// exo_fused_pair_kernel   persistent, a pair of CTAs (tcgen05 cta_group::2) per tile of 256 rows x BN accumulator columns, two accumulators
+//                         in tensor memory, so that a tile's epilogue runs beside the next tile's main loop
+// exo_fused_thin_kernel   up to 128 rows (a few tokens): one tile per CTA, two CTAs per SM; what counts is the stream of B's rows
+//
+// The operator is a class `Op`: its epilogue takes a row's accumulator columns in units of U, and for a gated product (Op::kGated) two units
+// at once, the second from `gap` columns further on.  There the rows of B that a tile stages are `gap` rows of gate and `gap` rows of up:
+// CTA 0 of a pair stages the ones and CTA 1 the others, which is how a pair splits B anyway, so both projections are one product.
+//
+// Results go from registers to memory, a row per lane.  The main loops are long (K of a model's width), so that the 32 KB of staging are
+// better spent on a seventh stage of operands, as in the library's plain product.
+//
+// Every wait is bounded: one that gives up records that, all roles leave their loops, tensor memory is freed and the kernel returns.
+#pragma once
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <stdint.h>
+
+#include "gemm_params.h"
+#include "ptx.cuh"
+
+namespace exo {
+namespace fused {
+
+struct Bf16 {
+  using type = __nv_bfloat16;
+  static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
+    __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<uint32_t*>(&v);
+  }
+  static __device__ __forceinline__ float2 unpack(uint32_t w) { return __bfloat1622float2(*reinterpret_cast<__nv_bfloat162*>(&w)); }
+};
+struct Fp16 {
+  using type = __half;
+  static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
+    __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<uint32_t*>(&v);
+  }
+  static __device__ __forceinline__ float2 unpack(uint32_t w) { return __half22float2(*reinterpret_cast<__half2*>(&w)); }
+};
+
+struct CoreParams {
+  int32_t M, N;        // rows of A, and columns of the result (columns of gate, for a gated product)
+  int32_t nkb;         // k-blocks: 128 bytes of a row of A and of B
+  int32_t stages;
+  int32_t width;       // result columns of a tile
+  int32_t b_split;     // pair: how many rows of B lie between what CTA 0 and what CTA 1 stage; thin: between gate and up
+  int32_t a_rows;      // thin: rows of A staged, M rounded up to 8
+  uint32_t idesc;
+  OperandStaging a, b;
+  Raster raster;
+  uint64_t wait_clocks;   // bound of every wait, in SM clocks
+  int32_t skip_copies;    // test hook: CTA 0 leaves out the copies of its first k-block
+};
+
+constexpr int kPairBarrierBytes = 512;
+constexpr int kThinThreads = 320;    // producer, MMA issuer, eight epilogue warps
+constexpr int kThinMaxStages = 16;
+constexpr int kThinBarrierBytes = 512;
+
+EXO_CX int pair_stage_bytes(int bn) { return kATileBytes + bn / 2 * 128; }
+EXO_CX int pair_stages(int bn) {
+  const int n = (kSmemLimit - 1024 - kPairBarrierBytes) / pair_stage_bytes(bn);
+  return n > kMaxStages ? kMaxStages : n;
+}
+EXO_CX int pair_smem(int bn) { return pair_stages(bn) * pair_stage_bytes(bn) + kPairBarrierBytes + 1024; }
+// The MMAs read 128 rows of A whatever a stage holds of it: what follows the rows staged becomes accumulator rows that nobody reads, and
+// behind the last stage it is room that the ring keeps.
+EXO_CX int thin_smem(int stages, int b_rows, int a_rows) {
+  return 1024 + kThinBarrierBytes + 512 + stages * (b_rows + a_rows) * 128 + (128 - a_rows) * 128;
+}
+
+// ---------------------------------------------------------------- bounded waits
+static __device__ uint32_t fused_gave_up;   // one per translation unit: the number of waits that gave up
+
+static __device__ __noinline__ bool wait_slow(uint32_t bar, uint32_t parity, uint64_t clocks) {
+  const long long t0 = clock64();
+  uint32_t n = 0;
+  for (;;) {
+    if (ptx::mbar_try_wait(bar, parity)) return true;
+    if ((++n & 63u) == 0u) {
+      if (*(volatile uint32_t*)&fused_gave_up != 0u) return false;   // another role, or an earlier launch that nobody has asked about
+      if ((uint64_t)(clock64() - t0) > clocks) {
+        atomicAdd(&fused_gave_up, 1u);
+        return false;
+      }
+    }
+  }
+}
+__device__ __forceinline__ bool wait_on(uint32_t bar, uint32_t parity, uint64_t clocks) {
+#pragma unroll 1
+  for (int i = 0; i < 8; ++i)
+    if (ptx::mbar_try_wait(bar, parity)) return true;
+  return wait_slow(bar, parity, clocks);
+}
+// the same for a whole warp: true if no lane gave up
+__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, uint64_t clocks) {
+  return __all_sync(0xffffffffu, wait_on(bar, parity, clocks)) != 0;
+}
+
+__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, const OperandStaging& op) {
+  return ((uint64_t)op.desc_hi << 32) | (((addr & 0x3FFFFu) >> 4) | (op.lbo_enc << 16));
+}
+
+// ---------------------------------------------------------------- tensor-core instructions of exo_fused.h only
+template <int CTA_GROUP>
+__device__ __forceinline__ void umma_i8(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  if constexpr (CTA_GROUP == 1)
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+  else
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+}
+template <class Op, int CTA_GROUP>
+__device__ __forceinline__ void umma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  if constexpr (Op::kInt8) umma_i8<CTA_GROUP>(d, a, b, idesc, accumulate);
+  else ptx::umma_f16<CTA_GROUP>(d, a, b, idesc, accumulate);
+}
+
+__device__ __forceinline__ void tmem_ld(uint32_t taddr, uint32_t (&r)[32]) { ptx::tmem_ld_32x32(taddr, r); }
+__device__ __forceinline__ void tmem_ld(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+                 "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+               : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_ld(uint32_t taddr, uint32_t (&r)[8]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(taddr) : "memory");
+}
+
+// ---------------------------------------------------------------- a row's U values to memory
+// `align`: a power of two up to 32 that divides the address of every unit.  n <= U values exist; the others are not written.
+template <class T, int U>
+__device__ __forceinline__ void store16(void* at, const float (&v)[U], int n, int align) {
+  uint32_t w[U / 2];
+#pragma unroll
+  for (int k = 0; k < U / 2; ++k) w[k] = T::pack(v[2 * k], v[2 * k + 1]);
+  char* const c = static_cast<char*>(at);
+  if (n >= U && align >= 16) {
+    if (U >= 16 && align >= 32) {
+#pragma unroll
+      for (int j = 0; j < U / 16; ++j) ptx::st_global_v8(c + 32 * j, &w[8 * j]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < U / 8; ++j) ptx::st_global_v4(c + 16 * j, w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
+    }
+  } else if (align >= 8) {
+#pragma unroll
+    for (int j = 0; j < U / 4; ++j)
+      if (4 * j + 4 <= n) {
+        *reinterpret_cast<uint2*>(c + 8 * j) = make_uint2(w[2 * j], w[2 * j + 1]);
+      } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (4 * j + k < n) *reinterpret_cast<uint16_t*>(c + 8 * j + 2 * k) = (uint16_t)(w[2 * j + k / 2] >> (16 * (k & 1)));
+      }
+  } else {
+#pragma unroll
+    for (int k = 0; k < U / 2; ++k)
+      if (align >= 4 && 2 * k + 2 <= n) {
+        *reinterpret_cast<uint32_t*>(c + 4 * k) = w[k];
+      } else {
+        if (2 * k < n) *reinterpret_cast<uint16_t*>(c + 4 * k) = (uint16_t)w[k];
+        if (2 * k + 1 < n) *reinterpret_cast<uint16_t*>(c + 4 * k + 2) = (uint16_t)(w[k] >> 16);
+      }
+  }
+}
+template <int U>
+__device__ __forceinline__ void store32(void* at, const float (&v)[U], int n, int align) {
+  char* const c = static_cast<char*>(at);
+  if (n >= U && align >= 16) {
+    uint32_t w[U];
+#pragma unroll
+    for (int k = 0; k < U; ++k) w[k] = __float_as_uint(v[k]);
+    if (align >= 32) {
+#pragma unroll
+      for (int j = 0; j < U / 8; ++j) ptx::st_global_v8(c + 32 * j, &w[8 * j]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < U / 4; ++j) ptx::st_global_v4(c + 16 * j, w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < U; ++k)
+      if (k < n) reinterpret_cast<float*>(c)[k] = v[k];
+  }
+}
+
+// ---------------------------------------------------------------- the epilogue of one warp: 32 rows, `units` units of U columns
+// tacc: the warp's lanes of the accumulator, at its first unit's column; release() hands the accumulator back after the last read.
+template <class Op, int U, class Release>
+__device__ __forceinline__ void run_units(const typename Op::Params& o, uint32_t tacc, uint32_t gap, int row, bool row_ok, int col, int units, int N,
+                                          int part, const Release& release) {
+  const int left = N > col ? (N - col + U - 1) / U : 0;
+  if (units > left) units = left;
+  typename Op::State s;
+  Op::begin(o, s, row, row_ok);
+  if constexpr (Op::kTwice) {   // a first look at the columns
+#pragma unroll 1
+    for (int i = 0; i < units; ++i) {
+      uint32_t v[U];
+      tmem_ld(tacc + (uint32_t)(i * U), v);
+      ptx::tmem_ld_wait();
+      Op::template look<U>(o, s, v, N - col - i * U);
+    }
+    Op::looked(s);
+  }
+  if (units == 0) release();
+#pragma unroll 1
+  for (int i = 0; i < units; ++i) {
+    uint32_t v[U], v2[Op::kGated ? U : 1];
+    tmem_ld(tacc + (uint32_t)(i * U), v);
+    if constexpr (Op::kGated) tmem_ld(tacc + gap + (uint32_t)(i * U), v2);
+    ptx::tmem_ld_wait();
+    if (i + 1 == units) release();
+    const int n = N - col - i * U;
+    Op::template unit<U>(o, s, v, v2, row, row_ok, col + i * U, n < U ? n : U);
+  }
+  Op::end(o, s, row, row_ok, part);
+}
+
+// ---------------------------------------------------------------- pairs of CTAs, persistent
+// Roles as in the library's plain product: warps 0 and 10 copy A and B, warp 1 issues the MMAs (CTA 0) and owns tensor memory, warps 2 to 9
+// are the epilogue, two per lane quadrant, each of them half of the tile's columns.
+template <class Op, int BN, bool B_MN>
+__global__ void __launch_bounds__(kNumThreads, 1)
+exo_fused_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b, const __grid_constant__ CoreParams p,
+                      const __grid_constant__ typename Op::Params o) {
+  constexpr int B_ROWS = BN / 2, STAGE = pair_stage_bytes(BN), STAGES = pair_stages(BN);
+  constexpr int WIDTH = Op::kGated ? BN / 2 : BN;      // result columns of a tile
+  constexpr int SUB_K = Op::kInt8 ? 128 : 64;          // elements of a k-block
+  constexpr uint32_t TMEM_COLS = 2 * BN;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t stage0 = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u, bar0 = stage0 + STAGES * STAGE;
+  auto full_bar = [&](uint32_t s) { return bar0 + 8u * s; };
+  auto empty_bar = [&](uint32_t s) { return bar0 + 8u * (kMaxStages + s); };
+  auto tfull_bar = [&](uint32_t a) { return bar0 + 8u * (2 * kMaxStages + a); };
+  auto tempty_bar = [&](uint32_t a) { return bar0 + 8u * (2 * kMaxStages + 2 + a); };
+  const uint32_t tmem_slot = bar0 + 8u * (2 * kMaxStages + 4);
+  const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
+  const uint32_t rank = ptx::cluster_ctarank();
+  const int64_t worker = blockIdx.x / 2, workers = gridDim.x / 2, tiles = raster_total(p.raster);
+  const int32_t nkb = p.nkb;
+
+  if (warp == 2) {
+    if (lane == 0) {
+      ptx::prefetch_tensormap(&tm_a);
+      ptx::prefetch_tensormap(&tm_b);
+    }
+    for (uint32_t i = lane; i < 2u * kMaxStages + 4u; i += 32u) ptx::mbar_init(bar0 + 8u * i, i >= 2u * kMaxStages + 2u ? kEpiWarps * 2 : 1);
+    ptx::fence_mbar_init();
+  }
+  if (warp == 1) {
+    ptx::tmem_alloc<2>(tmem_slot, TMEM_COLS);
+    ptx::tmem_relinquish<2>();
+  }
+  ptx::cluster_arrive();
+  ptx::tc_fence_before_sync();
+  __syncthreads();
+  ptx::cluster_wait();   // the peer's barriers and tensor memory exist before anything remote touches them
+  ptx::tc_fence_after_sync();
+  uint32_t tmem_base;
+  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem_base) : "r"(tmem_slot) : "memory");
+  bool ok = true;
+
+  if (warp == 0 || warp == (uint32_t)kProducerBWarp) {
+    const bool do_a = warp == 0;
+    uint32_t s = 0, ph = 0;
+    const uint32_t full0 = ptx::map_to_cta(full_bar(0), 0u);   // both CTAs' copies are counted on CTA 0's barrier
+    ptx::grid_dependency_wait();
+    bool skip = p.skip_copies != 0 && blockIdx.x == 0;
+    for (int64_t t = worker; t < tiles && ok; t += workers) {
+      const TileCoord tc = raster_decode(p.raster, t);
+      const int32_t a0 = tc.m * 256 + (int32_t)rank * 128, b0 = tc.n * WIDTH + (int32_t)rank * p.b_split;
+      for (int32_t kb = 0; kb < nkb; ++kb) {
+        ok = wait_warp(empty_bar(s), ph ^ 1u, p.wait_clocks);
+        if (!ok) break;
+        if (ptx::elect_one()) {
+          if (rank == 0 && do_a) ptx::mbar_arrive_expect_tx(full_bar(s), STAGE * 2);
+          const uint32_t a_dst = stage0 + s * STAGE, b_dst = a_dst + kATileBytes, bar = full0 + 8u * s;
+          if (skip) {
+          } else if (do_a) {
+            ptx::tma_load_2d_pair(a_dst, &tm_a, kb * SUB_K, a0, bar);
+          } else if constexpr (!B_MN) {
+            ptx::tma_load_2d_pair(b_dst, &tm_b, kb * SUB_K, b0, bar);
+          } else {
+#pragma unroll
+            for (int b = 0; b < B_ROWS / 64; ++b) ptx::tma_load_2d_pair(b_dst + b * 8192u, &tm_b, b0 + 64 * b, kb * SUB_K, bar);
+          }
+        }
+        skip = false;
+        if (++s == STAGES) { s = 0; ph ^= 1u; }
+      }
+    }
+    for (uint32_t i = 0; i < STAGES && ok; ++i) {   // no stage release may still be on its way to this CTA
+      ok = wait_warp(empty_bar(s), ph ^ 1u, p.wait_clocks);
+      if (++s == STAGES) { s = 0; ph ^= 1u; }
+    }
+  } else if (warp == 1) {
+    if (rank == 0) {
+      ptx::grid_dependency_wait();
+      uint32_t s = 0, ph = 0, acc = 0, acc_ph = 0;
+      const uint32_t a_step = p.a.k_step_enc, b_step = p.b.k_step_enc, idesc = p.idesc;
+      for (int64_t t = worker; t < tiles && ok; t += workers) {
+        ok = wait_warp(tempty_bar(acc), acc_ph ^ 1u, p.wait_clocks);   // both CTAs' epilogues have read it
+        if (!ok) break;
+        ptx::tc_fence_after_sync();
+        const uint32_t d = tmem_base + acc * BN;
+        for (int32_t kb = 0; kb < nkb; ++kb) {
+          ok = wait_warp(full_bar(s), ph, p.wait_clocks);
+          if (!ok) break;
+          ptx::tc_fence_after_sync();
+          const uint64_t a_desc = smem_desc(stage0 + s * STAGE, p.a), b_desc = smem_desc(stage0 + s * STAGE + kATileBytes, p.b);
+          if (ptx::elect_one()) {
+#pragma unroll
+            for (uint32_t k = 0; k < 4; ++k)   // 32 bytes of K each
+              umma<Op, 2>(d, a_desc + k * a_step, b_desc + k * b_step, idesc, (kb > 0 || k > 0) ? 1u : 0u);
+            ptx::umma_commit<2>(empty_bar(s), 3);
+            if (kb == nkb - 1) ptx::umma_commit<2>(tfull_bar(acc), 3);
+          }
+          if (++s == STAGES) { s = 0; ph ^= 1u; }
+        }
+        if ((acc ^= 1u) == 0u) acc_ph ^= 1u;
+      }
+    }
+  } else {
+    if (warp == 2) ptx::grid_launch_dependents();
+    ptx::grid_dependency_wait();
+    const uint32_t quad = warp & 3u;
+    const int32_t half = (int32_t)((warp - 2u) >> 2);
+    const uint32_t tempty0 = ptx::map_to_cta(tempty_bar(0), 0u);
+    constexpr int U = Op::kUnit, UNITS = WIDTH / 2 / U;
+    static_assert(UNITS * U * 2 == WIDTH, "whole units per warp");
+    uint32_t acc = 0, acc_ph = 0;
+    for (int64_t t = worker; t < tiles; t += workers) {
+      const TileCoord tc = raster_decode(p.raster, t);
+      const int32_t row0 = tc.m * 256 + (int32_t)rank * 128 + (int32_t)quad * 32, row = row0 + (int32_t)lane;
+      ok = wait_warp(tfull_bar(acc), acc_ph, p.wait_clocks);
+      if (!ok) break;
+      ptx::tc_fence_after_sync();
+      auto release = [&]() {
+        ptx::tc_fence_before_sync();
+        __syncwarp();
+        if (ptx::elect_one()) ptx::mbar_arrive_cluster(tempty0 + 8u * acc);
+      };
+      if (row0 >= p.M) {
+        release();
+      } else {
+        const uint32_t tacc = tmem_base + ((quad * 32u) << 16) + acc * BN + (uint32_t)(half * (WIDTH / 2));
+        run_units<Op, U>(o, tacc, (uint32_t)WIDTH, row, row < p.M, tc.n * WIDTH + half * (WIDTH / 2), UNITS, p.N, tc.n * 2 + half, release);
+      }
+      if ((acc ^= 1u) == 0u) acc_ph ^= 1u;
+    }
+  }
+
+  if (!ok)
+    for (int i = 0; i < 200; ++i) __nanosleep(1000);   // a wait was abandoned: copies and MMAs in flight land first
+  ptx::tc_fence_before_sync();
+  __syncthreads();
+  ptx::cluster_arrive();   // the peer's shared and tensor memory stay valid until both CTAs are done
+  ptx::cluster_wait();
+  if (warp == 1) {
+    ptx::tc_fence_after_sync();
+    ptx::tmem_dealloc<2>(tmem_base, TMEM_COLS);
+  }
+}
+
+// ---------------------------------------------------------------- a few rows: one tile per CTA
+// A stage is the tile's rows of B (gate's and up's for a gated product) and the a_rows rows of A.  U: columns of an epilogue unit.
+template <class Op, int U>
+__global__ void __launch_bounds__(kThinThreads, 2)
+exo_fused_thin_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b, const __grid_constant__ CoreParams p,
+                      const __grid_constant__ typename Op::Params o) {
+  constexpr int SUB_K = Op::kInt8 ? 128 : 64;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t stage0 = (ptx::smem_u32(smem_raw) + kThinBarrierBytes + 1023u) & ~1023u, bar0 = stage0 - kThinBarrierBytes;
+  auto full_bar = [&](uint32_t s) { return bar0 + 8u * s; };
+  auto empty_bar = [&](uint32_t s) { return bar0 + 8u * (kThinMaxStages + s); };
+  const uint32_t tfull_bar = bar0 + 8u * (2 * kThinMaxStages), tmem_slot = tfull_bar + 8u;
+  const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
+  const uint32_t width = (uint32_t)p.width, bn = Op::kGated ? 2u * width : width;
+  const uint32_t b_bytes = bn * 128u, stage_bytes = b_bytes + (uint32_t)p.a_rows * 128u, stages = (uint32_t)p.stages;
+  uint32_t tmem_cols = 32;
+  while (tmem_cols < bn) tmem_cols *= 2;
+  const int32_t nkb = p.nkb, col0 = (int32_t)(blockIdx.x * width);
+
+  if (warp == 0) {
+    if (lane == 0) {
+      ptx::prefetch_tensormap(&tm_a);
+      ptx::prefetch_tensormap(&tm_b);
+    }
+    for (uint32_t i = lane; i < 2u * kThinMaxStages + 1u; i += 32u) ptx::mbar_init(bar0 + 8u * i, 1);
+    ptx::fence_mbar_init();
+  }
+  if (warp == 1) {
+    ptx::tmem_alloc<1>(tmem_slot, tmem_cols);
+    ptx::tmem_relinquish<1>();
+  }
+  ptx::tc_fence_before_sync();
+  __syncthreads();
+  ptx::tc_fence_after_sync();
+  uint32_t tmem_base;
+  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem_base) : "r"(tmem_slot) : "memory");
+  bool ok = true;
+
+  if (warp == 0) {
+    ptx::grid_launch_dependents();
+    ptx::grid_dependency_wait();
+    uint32_t s = 0, ph = 0;
+    bool skip = p.skip_copies != 0 && blockIdx.x == 0;
+    for (int32_t kb = 0; kb < nkb; ++kb) {
+      ok = wait_warp(empty_bar(s), ph ^ 1u, p.wait_clocks);
+      if (!ok) break;
+      if (ptx::elect_one()) {
+        const uint32_t dst = stage0 + s * stage_bytes;
+        ptx::mbar_arrive_expect_tx(full_bar(s), stage_bytes);
+        if (!skip) {
+          ptx::tma_load_2d(dst, &tm_b, kb * SUB_K, col0, full_bar(s));
+          if constexpr (Op::kGated) ptx::tma_load_2d(dst + width * 128u, &tm_b, kb * SUB_K, col0 + p.b_split, full_bar(s));
+          ptx::tma_load_2d(dst + b_bytes, &tm_a, kb * SUB_K, 0, full_bar(s));
+        }
+      }
+      skip = false;
+      if (++s == stages) { s = 0; ph ^= 1u; }
+    }
+  } else if (warp == 1) {
+    ptx::grid_dependency_wait();
+    uint32_t s = 0, ph = 0;
+    const uint32_t a_step = p.a.k_step_enc, b_step = p.b.k_step_enc, idesc = p.idesc;
+    for (int32_t kb = 0; kb < nkb; ++kb) {
+      ok = wait_warp(full_bar(s), ph, p.wait_clocks);
+      if (!ok) break;
+      ptx::tc_fence_after_sync();
+      const uint64_t b_desc = smem_desc(stage0 + s * stage_bytes, p.b), a_desc = smem_desc(stage0 + s * stage_bytes + b_bytes, p.a);
+      if (ptx::elect_one()) {
+#pragma unroll
+        for (uint32_t k = 0; k < 4; ++k) umma<Op, 1>(tmem_base, a_desc + k * a_step, b_desc + k * b_step, idesc, (kb > 0 || k > 0) ? 1u : 0u);
+        ptx::umma_commit<1>(empty_bar(s), 1);
+        if (kb == nkb - 1) ptx::umma_commit<1>(tfull_bar, 1);
+      }
+      if (++s == stages) { s = 0; ph ^= 1u; }
+    }
+  } else {
+    ptx::grid_dependency_wait();
+    const uint32_t quad = warp & 3u;
+    const int32_t half = (int32_t)((warp - 2u) >> 2), row0 = (int32_t)quad * 32, row = row0 + (int32_t)lane;
+    ok = wait_warp(tfull_bar, 0u, p.wait_clocks);
+    if (ok && row0 < p.M) {
+      ptx::tc_fence_after_sync();
+      const int32_t units = (int32_t)width / U, first = half ? (units + 1) / 2 : 0, mine = half ? units / 2 : (units + 1) / 2;
+      const uint32_t tacc = tmem_base + ((quad * 32u) << 16) + (uint32_t)(first * U);
+      run_units<Op, U>(o, tacc, width, row, row < p.M, col0 + first * U, mine, p.N, (int)blockIdx.x * 2 + half, [] {});
+    }
+  }
+  if (!ok)
+    for (int i = 0; i < 200; ++i) __nanosleep(1000);
+  ptx::tc_fence_before_sync();
+  __syncthreads();
+  if (warp == 1) {
+    ptx::tc_fence_after_sync();
+    ptx::tmem_dealloc<1>(tmem_base, tmem_cols);
+  }
+}
+
+}  // namespace fused
+}  // namespace exo

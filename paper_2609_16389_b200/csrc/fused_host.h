@@ -1,0 +1,255 @@
+// Host side of exo_fused.h: launches, tensor maps, tile shapes, aligned copies and device memory of plans.
+#pragma once
+#include <cuda.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include <atomic>
+#include <initializer_list>
+
+#include "../../include/exo_fused.h"
+#include "decode_host.h"
+#include "fused_core.cuh"
+#include "plan.h"
+
+namespace exo {
+bool encode_operand_map(CUtensorMap* map, int elem_bytes, bool bf16, const void* base, uint64_t inner, uint64_t rows, uint64_t row_bytes,
+                        uint32_t box_rows);   // api.cu
+exo_gemm_status_t gemm_create_exact(exo_gemm_handle_t* out, const exo_gemm_desc_t* desc);   // api.cu
+exo_gemm_status_t gemm_run_scaled(exo_gemm_plan* plan, const void* A, const void* B, void* C, float alpha, const float* alpha_dev, float beta,
+                                  void* cuda_stream);   // api.cu
+
+namespace fused {
+
+// What exo_fused_debug_set has set for the next kernel with products (i8.cu).
+struct WaitHook {
+  uint64_t clocks;
+  int skip;
+};
+WaitHook take_wait_hook();
+
+using decode::cuda_failed;
+using decode::device_check;
+
+struct OnDevice {   // makes `device` the current one while it lives
+  int before = -1;
+  cudaError_t err;
+  explicit OnDevice(int device) {
+    err = cudaGetDevice(&before);
+    if (err == cudaSuccess && before != device) err = cudaSetDevice(device);
+    else before = -1;
+  }
+  ~OnDevice() {
+    if (before >= 0) cudaSetDevice(before);
+  }
+};
+
+inline int64_t round_up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
+inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
+// the largest power of two up to 32 that divides an address and a row stride in bytes
+inline int align_of(const void* p, int64_t row_bytes) {
+  const uint64_t at = (uint64_t)(uintptr_t)p | (uint64_t)row_bytes | 32u;
+  return (int)(at & (~at + 1));
+}
+inline bool is16(int32_t t) { return t == EXO_GEMM_BF16 || t == EXO_GEMM_FP16; }
+
+// One launch with programmatic dependent launch.  args: the kernel's parameters, in order.
+inline exo_gemm_status_t launch_args(void* fn, dim3 grid, unsigned threads, size_t smem, unsigned cluster, cudaStream_t stream, void** args) {
+  cudaError_t e;
+  if (smem > 48 * 1024) {
+    // every kernel gets the whole of what a CTA may have, once per device: launches of other sizes cannot lower it for one another
+    constexpr int kSlots = 64;
+    static std::atomic<void*> done[8][kSlots];
+    int device = 0;
+    if ((e = cudaGetDevice(&device)) != cudaSuccess) return cuda_failed(e);
+    std::atomic<void*>* free_slot = nullptr;
+    bool known = false;
+    for (int i = 0; device < 8 && i < kSlots && !known && !free_slot; ++i) {
+      void* have = done[device][i].load(std::memory_order_relaxed);
+      known = have == fn;
+      if (!have) free_slot = &done[device][i];
+    }
+    if (!known) {
+      if ((e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit)) != cudaSuccess) return cuda_failed(e);
+      if (free_slot) free_slot->store(fn, std::memory_order_relaxed);
+    }
+  }
+  cudaLaunchConfig_t lc{};
+  lc.gridDim = grid;
+  lc.blockDim = dim3(threads, 1, 1);
+  lc.dynamicSmemBytes = smem;
+  lc.stream = stream;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = cluster;
+  at[1].val.clusterDim.y = 1;
+  at[1].val.clusterDim.z = 1;
+  lc.attrs = at;
+  lc.numAttrs = cluster > 1 ? 2 : 1;
+  e = cudaLaunchKernelExC(&lc, fn, args);
+  return e == cudaSuccess ? EXO_GEMM_OK : cuda_failed(e);
+}
+
+// How a product runs: thin (a few rows) or by pairs of CTAs, and how many result columns a tile has.
+struct Shape {
+  bool thin;
+  int width;      // result columns of a tile
+  int stages;     // thin
+  int b_rows;     // thin: rows of B per stage
+};
+
+constexpr int kThinRows = 128;   // what one tile's accumulator has
+
+// Thin tiles: the widest that spreads the columns evenly over the SMs.  quantum: what a width is a multiple of; most: the widest.
+inline int thin_width(int64_t N, int quantum, int most, int sms) {
+  int best = quantum;
+  int64_t cost = -1;
+  for (int w = quantum; w <= most; w += quantum) {
+    const int64_t tiles = (N + w - 1) / w, waves = (tiles + sms - 1) / sms, c = waves * w;
+    if (cost < 0 || c <= cost) { cost = c; best = w; }
+  }
+  return best;
+}
+// Stages of a thin tile: 100 KB of ring, so that two CTAs share an SM and one's start and end hide behind the other's copies, but four stages
+// at least.
+inline int thin_stages(int b_rows, int a_rows, int64_t nkb) {
+  const int stage = (b_rows + a_rows) * 128;
+  int n = 100 * 1024 / stage;
+  if (n < 4) n = 4;
+  while (n > 2 && thin_smem(n, b_rows, a_rows) > kSmemLimit) --n;
+  if (n > kThinMaxStages) n = kThinMaxStages;
+  if (n > nkb) n = (int)nkb;
+  return n < 1 ? 1 : n;
+}
+
+// Columns of a pair's tile: 256 accumulator columns, or 128 where that fills the waves better by more than it costs (a tile of 128 moves a half
+// more operand bytes per product).
+inline int pair_bn(int64_t M, int64_t N, bool gated, int sms) {
+  const int pairs = sms / 2;
+  auto cost = [&](int bn, double each) {
+    const int64_t w = gated ? bn / 2 : bn, tiles = ((M + 255) / 256) * ((N + w - 1) / w);
+    return (double)((tiles + pairs - 1) / pairs) * bn * each;
+  };
+  return cost(128, 1.15) < cost(256, 1.0) ? 128 : 256;
+}
+
+struct Operand {
+  const void* base;
+  int64_t rows, inner, ld;   // elements; ld * element size is a multiple of 16
+};
+
+// A product of A (M rows) and B with operator Op.  b_mn: B lies K x N (N contiguous) instead of N x K.
+template <class Op, bool B_MN>
+exo_gemm_status_t launch_pair(int bn, const Operand& A, const Operand& B, int64_t N, int64_t K, int64_t b_split, bool bf16, int sms,
+                              const typename Op::Params& op, cudaStream_t stream) {
+  constexpr int ES = Op::kInt8 ? 1 : 2, SUB_K = 128 / ES;
+  const int width = Op::kGated ? bn / 2 : bn;
+  CoreParams p{};
+  p.M = (int32_t)A.rows;
+  p.N = (int32_t)N;
+  p.nkb = (int32_t)((K + SUB_K - 1) / SUB_K);
+  p.width = width;
+  p.b_split = (int32_t)(Op::kGated ? b_split : bn / 2);
+  p.idesc = Op::kInt8 ? (2u << 4 | 1u << 7 | 1u << 10 | (uint32_t)(bn >> 3) << 17 | 16u << 24)   // signed bytes, 32-bit integer sums
+                      : make_idesc(bf16 ? EXO_GEMM_BF16 : EXO_GEMM_FP16, 0, B_MN ? 1 : 0, 256, bn);
+  p.a = make_staging(0, kBlockM, 1, 2);   // (128 bytes of K per row whatever the type)
+  p.b = make_staging(B_MN ? 1 : 0, bn / 2, 1, 2);
+  const int32_t tiles_m = (int32_t)((A.rows + 255) / 256), tiles_n = (int32_t)((N + width - 1) / width);
+  // Bands of 8 tile columns: the 74 tiles at work then cover about 9 x 8 tiles, whose rows of A and B L2 holds.
+  p.raster = make_raster(tiles_m, tiles_n, 8, 0);
+  const int64_t tiles = (int64_t)tiles_m * tiles_n;
+  if (tiles >= (1LL << 31)) return EXO_GEMM_ERR_UNSUPPORTED;
+  CUtensorMap ma, mb;
+  if (!encode_operand_map(&ma, ES, bf16, A.base, (uint64_t)A.inner, (uint64_t)A.rows, (uint64_t)(A.ld * ES), 128) ||
+      !encode_operand_map(&mb, ES, bf16, B.base, (uint64_t)B.inner, (uint64_t)B.rows, (uint64_t)(B.ld * ES), B_MN ? 64u : (uint32_t)bn / 2))
+    return EXO_GEMM_ERR_CUDA;
+  const WaitHook hook = take_wait_hook();
+  p.wait_clocks = hook.clocks;
+  p.skip_copies = hook.skip;
+  const int64_t pairs = tiles < sms / 2 ? tiles : sms / 2;
+  typename Op::Params o = op;
+  void* args[4] = {&ma, &mb, &p, &o};
+  void* fn = bn == 256 ? (void*)exo_fused_pair_kernel<Op, 256, B_MN> : (void*)exo_fused_pair_kernel<Op, 128, B_MN>;
+  return launch_args(fn, dim3((unsigned)(2 * pairs)), kNumThreads, (size_t)pair_smem(bn), 2, stream, args);
+}
+
+template <class Op, int U>
+exo_gemm_status_t launch_thin(int width, const Operand& A, const Operand& B, int64_t N, int64_t K, int64_t b_split, bool bf16,
+                              const typename Op::Params& op, cudaStream_t stream) {
+  constexpr int ES = Op::kInt8 ? 1 : 2, SUB_K = 128 / ES;
+  const int bn = Op::kGated ? 2 * width : width, a_rows = (int)round_up(A.rows, 8);
+  CoreParams p{};
+  p.M = (int32_t)A.rows;
+  p.N = (int32_t)N;
+  p.nkb = (int32_t)((K + SUB_K - 1) / SUB_K);
+  p.width = width;
+  p.b_split = (int32_t)b_split;
+  p.a_rows = a_rows;
+  p.stages = thin_stages(bn, a_rows, p.nkb);
+  p.idesc = Op::kInt8 ? (2u << 4 | 1u << 7 | 1u << 10 | (uint32_t)(bn >> 3) << 17 | 8u << 24)
+                      : make_idesc(bf16 ? EXO_GEMM_BF16 : EXO_GEMM_FP16, 0, 0, 128, bn);
+  p.a = make_staging(0, kBlockM, 1, 2);
+  p.b = make_staging(0, bn, 1, 2);
+  CUtensorMap ma, mb;
+  if (!encode_operand_map(&ma, ES, bf16, A.base, (uint64_t)A.inner, (uint64_t)A.rows, (uint64_t)(A.ld * ES), (uint32_t)a_rows) ||
+      !encode_operand_map(&mb, ES, bf16, B.base, (uint64_t)B.inner, (uint64_t)B.rows, (uint64_t)(B.ld * ES), (uint32_t)width))
+    return EXO_GEMM_ERR_CUDA;
+  const WaitHook hook = take_wait_hook();
+  p.wait_clocks = hook.clocks;
+  p.skip_copies = hook.skip;
+  typename Op::Params o = op;
+  void* args[4] = {&ma, &mb, &p, &o};
+  return launch_args((void*)exo_fused_thin_kernel<Op, U>, dim3((unsigned)((N + width - 1) / width)), kThinThreads,
+                     (size_t)thin_smem(p.stages, bn, a_rows), 1, stream, args);
+}
+
+// dst = src, `rows` rows of `inner` 16-bit values; dst's rows start on 16 bytes and have room for a multiple of 8 values.
+exo_gemm_status_t align_rows(void* dst, int64_t dst_ld, const void* src, int64_t src_ld, int64_t inner, int64_t rows, cudaStream_t stream);   // i8.cu
+
+// Device memory of a plan.
+struct Memory {
+  static constexpr int kMost = 12;
+  void* parts[kMost] = {};
+  int count = 0;
+  int64_t bytes = 0;
+  cudaError_t err = cudaSuccess;
+  void* take(int64_t n) {
+    void* p = nullptr;
+    if (err != cudaSuccess || n <= 0) return nullptr;
+    if (count == kMost) { err = cudaErrorMemoryAllocation; return nullptr; }
+    err = cudaMalloc(&p, (size_t)n);
+    if (err != cudaSuccess) return nullptr;
+    parts[count++] = p;
+    bytes += n;
+    return p;
+  }
+  void give_back() {
+    for (int i = 0; i < count; ++i) cudaFree(parts[i]);
+    count = 0;
+  }
+};
+
+unsigned take_gave_up_i8(cudaError_t* e);
+unsigned take_gave_up_ffn(cudaError_t* e);
+unsigned take_gave_up_ce(cudaError_t* e);
+// of this translation unit's kernels, on the current device
+static inline unsigned take_gave_up_here(cudaError_t* e) {
+  unsigned n = 0, zero = 0;
+  *e = cudaMemcpyFromSymbol(&n, fused_gave_up, sizeof n);
+  if (*e == cudaSuccess && n) *e = cudaMemcpyToSymbol(fused_gave_up, &zero, sizeof zero);
+  return n;
+}
+// exo_gemm_check of a plan's products
+inline exo_gemm_status_t check_products(std::initializer_list<exo_gemm_handle_t> plans, exo_gemm_status_t st) {
+  for (exo_gemm_handle_t g : plans)
+    if (g) {
+      const exo_gemm_status_t s = exo_gemm_check(g, nullptr);
+      if (st == EXO_GEMM_OK) st = s;
+    }
+  return st;
+}
+
+}  // namespace fused
+}  // namespace exo

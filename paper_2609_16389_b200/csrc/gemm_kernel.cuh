@@ -514,8 +514,8 @@ exo_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant_
     const uint32_t tempty0 = PAIR ? ptx::map_to_cta(tempty_bar(0), leader) : tempty_bar(0);
     const bool has_beta_arg = p.beta != 0.f;
     const bool has_acc = nkb > 0;
-    const bool scale = p.alpha != 1.f;
-    const float alpha = p.alpha, beta = p.beta;
+    const float alpha = p.alpha_dev ? p.alpha * ptx::ld_global_cg_f32(p.alpha_dev) : p.alpha, beta = p.beta;
+    const bool scale = alpha != 1.f;
     // where this thread's j-th 16-byte piece of a 128-byte row goes (swizzled); recomputed at every use:
     // eight precomputed addresses would be eight registers held across the whole role
     const uint32_t my_row = buf0 + lane * 128u, my_xor = (lane & 7u) << 4;

@@ -109,6 +109,7 @@ struct GemmParams {
   FastDiv by_tiles_per_batch;
   uint32_t a_z_mask, b_z_mask;  // all ones, or 0 for an operand that every matrix of the batch shares
   float alpha, beta;
+  const float* alpha_dev;   // NULL, or a factor of alpha that an earlier kernel leaves on the device
   uint32_t idesc;           // tcgen05 instruction descriptor
   OperandStaging a, b;
   WorkPlan work;            // whole-K tiles round-robin, then the tail tiles cut along K

@@ -1,0 +1,302 @@
+// 8-bit integers with a scale per row, their products, and what the operators of exo_fused.h share: aligned copies, the state of device-side
+// waits.
+#include <new>
+
+#include "fused_host.h"
+
+namespace exo {
+namespace fused {
+namespace {
+
+// ---------------------------------------------------------------- quantisation
+// A CTA per row: the largest magnitude, then the codes; the second pass over the row finds it in L1 or L2.  Bound by memory for many rows
+// (2 + 1 bytes a value) and by two trips through it for one.
+struct QuantParams {
+  const void* x;
+  int64_t ldx;
+  int8_t* codes;
+  int64_t ld;
+  float* scales;
+  int32_t K;
+};
+constexpr int kQuantThreads = 256;
+
+template <class T> struct Element { using type = uint16_t; };
+template <> struct Element<float> { using type = float; };
+
+// V values from k on as fp32; those from K on are 0
+template <class T, int V>
+__device__ __forceinline__ void load_values(const typename Element<T>::type* x, int k, int K, float (&v)[V]) {
+  if constexpr (std::is_same<T, float>::value) {
+    if (V == 4) {
+      const float4 w = *reinterpret_cast<const float4*>(x + k);
+      v[0] = w.x; v[1] = w.y; v[2] = w.z; v[3] = w.w;
+    } else {
+      v[0] = x[k];
+    }
+  } else if constexpr (V == 8) {
+    const uint4 w = *reinterpret_cast<const uint4*>(x + k);
+    const float2 a = T::unpack(w.x), b = T::unpack(w.y), c = T::unpack(w.z), d = T::unpack(w.w);
+    v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y; v[4] = c.x; v[5] = c.y; v[6] = d.x; v[7] = d.y;
+  } else {
+    v[0] = T::unpack(x[k]).x;
+  }
+}
+
+// code of x: the quotient is rounded as IEEE division rounds it, and then to the nearest integer, ties to even
+__device__ __forceinline__ int code_of(float x, float scale) { return (int)fminf(fmaxf(rintf(__fdiv_rn(x, scale)), -127.f), 127.f); }
+
+// V: values per load, 16 bytes of them where the rows allow that, else one
+template <class T, int V>
+__global__ void __launch_bounds__(kQuantThreads) exo_i8_quantize_kernel(const QuantParams p) {
+  __shared__ float tops[kQuantThreads / 32];
+  ptx::grid_launch_dependents();
+  ptx::grid_dependency_wait();
+  const typename Element<T>::type* x = (const typename Element<T>::type*)p.x + (int64_t)blockIdx.x * p.ldx;
+  int8_t* codes = p.codes + (int64_t)blockIdx.x * p.ld;
+  const int whole = p.K / V * V;   // the values of whole loads; the others one by one
+  float top = 0.f;
+#pragma unroll 4
+  for (int k = threadIdx.x * V; k < whole; k += kQuantThreads * V) {
+    float v[V];
+    load_values<T, V>(x, k, p.K, v);
+#pragma unroll
+    for (int j = 0; j < V; ++j) top = fmaxf(top, fabsf(v[j]));
+  }
+  for (int k = whole + threadIdx.x; k < p.K; k += kQuantThreads) {
+    float v[1];
+    load_values<T, 1>(x, k, p.K, v);
+    top = fmaxf(top, fabsf(v[0]));
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  if ((threadIdx.x & 31) == 0) tops[threadIdx.x >> 5] = top;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kQuantThreads / 32; ++w) top = fmaxf(top, tops[w]);
+  const float scale = __fdiv_rn(top, 127.f);
+  if (threadIdx.x == 0) p.scales[blockIdx.x] = scale;
+  const bool zero = !(scale > 0.f);
+  for (int k = threadIdx.x * V; k < whole; k += kQuantThreads * V) {
+    float v[V];
+    load_values<T, V>(x, k, p.K, v);
+    uint32_t w[(V + 3) / 4] = {};
+#pragma unroll
+    for (int j = 0; j < V; ++j) w[j / 4] |= (uint32_t)((zero ? 0 : code_of(v[j], scale)) & 255) << (8 * (j & 3));
+    if constexpr (V == 8) *reinterpret_cast<uint2*>(codes + k) = make_uint2(w[0], w[1]);
+    else if constexpr (V == 4) *reinterpret_cast<uint32_t*>(codes + k) = w[0];
+    else codes[k] = (int8_t)w[0];
+  }
+  for (int k = whole + threadIdx.x; k < p.K; k += kQuantThreads) {
+    float v[1];
+    load_values<T, 1>(x, k, p.K, v);
+    codes[k] = (int8_t)(zero ? 0 : code_of(v[0], scale));
+  }
+}
+
+// ---------------------------------------------------------------- products
+// Integer sums are exact; a token's scale, its channels' scales and alpha are multiplied on in fp32.
+struct I8Op {
+  static constexpr bool kInt8 = true, kGated = false, kTwice = false;
+  static constexpr int kUnit = 32;   // columns at a time, by pairs
+  struct Params {
+    const float *xs, *ws;
+    void* y;
+    int64_t ldy;
+    int32_t y_dtype, align;   // align: what divides the address of every unit
+    float alpha, beta;
+  };
+  struct State {
+    float xs;
+  };
+  static __device__ __forceinline__ void begin(const Params& o, State& s, int row, bool row_ok) { s.xs = row_ok ? __ldcg(o.xs + row) : 0.f; }
+  template <int U>
+  static __device__ __forceinline__ void unit(const Params& o, State& s, uint32_t (&v)[U], uint32_t (&)[1], int row, bool row_ok, int col, int n) {
+    float y[U];
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      const float w = k < n ? __ldcg(o.ws + col + k) : 0.f;   // one address for the whole warp
+      y[k] = (float)(int32_t)v[k] * s.xs * w * o.alpha;
+    }
+    if (!row_ok) return;
+    const int64_t at = (int64_t)row * o.ldy + col;
+    if (o.y_dtype == EXO_GEMM_FP32) {
+      float* const c = (float*)o.y + at;
+      if (o.beta != 0.f) {
+#pragma unroll
+        for (int k = 0; k < U; ++k)
+          if (k < n) y[k] = fmaf(o.beta, c[k], y[k]);
+      }
+      store32<U>(c, y, n, o.align);
+      return;
+    }
+    uint16_t* const c = (uint16_t*)o.y + at;
+    if (o.beta != 0.f) {
+#pragma unroll
+      for (int k = 0; k < U; ++k)
+        if (k < n) y[k] = fmaf(o.beta, o.y_dtype == EXO_GEMM_BF16 ? Bf16::unpack(c[k]).x : Fp16::unpack(c[k]).x, y[k]);
+    }
+    if (o.y_dtype == EXO_GEMM_BF16) store16<Bf16, U>(c, y, n, o.align);
+    else store16<Fp16, U>(c, y, n, o.align);
+  }
+  static __device__ __forceinline__ void end(const Params&, State&, int, bool, int) {}
+};
+
+// Y = beta * Y, where there are no products
+struct ScaleYParams {
+  void* y;
+  int64_t ldy, rows, cols;
+  int32_t y_dtype;
+  float beta;
+};
+constexpr int kScaleYThreads = 256;
+__global__ void __launch_bounds__(kScaleYThreads) exo_i8_scale_kernel(const ScaleYParams p) {
+  ptx::grid_launch_dependents();
+  ptx::grid_dependency_wait();
+  for (int64_t i = (int64_t)blockIdx.x * kScaleYThreads + threadIdx.x; i < p.rows * p.cols; i += (int64_t)gridDim.x * kScaleYThreads) {
+    const int64_t at = i / p.cols * p.ldy + i % p.cols;
+    if (p.y_dtype == EXO_GEMM_FP32) {
+      float* c = (float*)p.y + at;
+      *c = p.beta != 0.f ? p.beta * *c : 0.f;
+    } else if (p.y_dtype == EXO_GEMM_BF16) {
+      uint16_t* c = (uint16_t*)p.y + at;
+      *c = (uint16_t)Bf16::pack(p.beta != 0.f ? p.beta * Bf16::unpack(*c).x : 0.f, 0.f);
+    } else {
+      uint16_t* c = (uint16_t*)p.y + at;
+      *c = (uint16_t)Fp16::pack(p.beta != 0.f ? p.beta * Fp16::unpack(*c).x : 0.f, 0.f);
+    }
+  }
+}
+
+// ---------------------------------------------------------------- aligned copies
+constexpr int kAlignThreads = 256;
+struct AlignParams {
+  uint16_t* dst;
+  const uint16_t* src;
+  int64_t dst_ld, src_ld, inner, rows, chunks;   // chunks: of eight values, per row
+  int32_t word;                                  // bytes that divide the address of every source row: 2, 4 or 8
+};
+// A thread moves eight values: 16 bytes out, in as wide pieces as the source's rows allow.
+__global__ void __launch_bounds__(kAlignThreads) exo_fused_align_kernel(const AlignParams p) {
+  ptx::grid_launch_dependents();
+  ptx::grid_dependency_wait();
+  const int64_t i = (int64_t)blockIdx.x * kAlignThreads + threadIdx.x;
+  const int64_t row = i / p.chunks, k = (i - row * p.chunks) * 8;
+  if (row >= p.rows) return;
+  const uint16_t* s = p.src + row * p.src_ld + k;
+  uint32_t w[4] = {};
+  if (k + 8 <= p.inner && p.word >= 8) {
+    const uint2 a = *reinterpret_cast<const uint2*>(s), b = *reinterpret_cast<const uint2*>(s + 4);
+    w[0] = a.x; w[1] = a.y; w[2] = b.x; w[3] = b.y;
+  } else if (k + 8 <= p.inner && p.word >= 4) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] = reinterpret_cast<const uint32_t*>(s)[j];
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (k + j < p.inner) w[j / 2] |= (uint32_t)s[j] << (16 * (j & 1));
+  }
+  ptx::st_global_v4(p.dst + row * p.dst_ld + k, w[0], w[1], w[2], w[3]);
+}
+
+std::atomic<int64_t> wait_hook{0};   // milliseconds * 2 + skip
+
+exo_gemm_status_t check_i8(const exo_i8_t* q) {
+  if (!q) return EXO_GEMM_ERR_NULL;
+  if (q->rows < 0 || q->K < 0 || q->rows > (1LL << 30) || q->K > (1LL << 30) || q->ld < q->K || q->ld > (1LL << 31)) return EXO_GEMM_ERR_INVALID_ARG;
+  return EXO_GEMM_OK;
+}
+exo_gemm_status_t check_i8_memory(const exo_i8_t* q) {
+  if (!q->codes || !q->scales) return EXO_GEMM_ERR_NULL;
+  return aligned16(q->codes) && q->ld % 16 == 0 && ((uintptr_t)q->scales & 3u) == 0 ? EXO_GEMM_OK : EXO_GEMM_ERR_ALIGNMENT;
+}
+
+template <class T, int V> void* quant_fn(bool wide) { return wide ? (void*)exo_i8_quantize_kernel<T, V> : (void*)exo_i8_quantize_kernel<T, 1>; }
+
+}  // namespace
+
+WaitHook take_wait_hook() {
+  const int64_t v = wait_hook.load(std::memory_order_relaxed) ? wait_hook.exchange(0) : 0;
+  return WaitHook{(uint64_t)(v / 2 > 0 ? v / 2 : 4000) * 2000000ull, (int)(v % 2)};   // SM clocks at 2 GHz, an upper bound of theirs
+}
+unsigned take_gave_up_i8(cudaError_t* e) { return take_gave_up_here(e); }
+
+exo_gemm_status_t align_rows(void* dst, int64_t dst_ld, const void* src, int64_t src_ld, int64_t inner, int64_t rows, cudaStream_t stream) {
+  AlignParams p{(uint16_t*)dst, (const uint16_t*)src, dst_ld, src_ld, inner, rows, (inner + 7) / 8, align_of(src, src_ld * 2)};
+  const int64_t ctas = (rows * p.chunks + kAlignThreads - 1) / kAlignThreads;
+  if (ctas >= (1LL << 31)) return EXO_GEMM_ERR_UNSUPPORTED;
+  if (ctas == 0) return EXO_GEMM_OK;
+  void* args[1] = {&p};
+  return launch_args((void*)exo_fused_align_kernel, dim3((unsigned)ctas), kAlignThreads, 0, 1, stream, args);
+}
+
+}  // namespace fused
+}  // namespace exo
+
+using namespace exo;
+using namespace exo::fused;
+
+extern "C" {
+
+exo_gemm_status_t exo_fused_check(void) {
+  cudaError_t e = cudaDeviceSynchronize();
+  unsigned n = 0;
+  if (e == cudaSuccess) n |= take_gave_up_i8(&e);
+  if (e == cudaSuccess) n |= take_gave_up_ffn(&e);
+  if (e == cudaSuccess) n |= take_gave_up_ce(&e);
+  if (e != cudaSuccess) return cuda_failed(e);
+  return n ? EXO_GEMM_ERR_DEVICE_TIMEOUT : EXO_GEMM_OK;
+}
+
+exo_gemm_status_t exo_fused_debug_set(int32_t timeout_ms, int32_t skip_copies) {
+  if (timeout_ms < 0 || timeout_ms > 10000 || skip_copies < 0 || skip_copies > 1) return EXO_GEMM_ERR_INVALID_ARG;
+  exo::fused::wait_hook.store((int64_t)timeout_ms * 2 + skip_copies);
+  return EXO_GEMM_OK;
+}
+
+exo_gemm_status_t exo_i8_quantize(const exo_i8_t* q, const void* X, int64_t ldx, int32_t x_dtype, void* cuda_stream) {
+  exo_gemm_status_t st = check_i8(q);
+  if (st != EXO_GEMM_OK) return st;
+  if (ldx < (q->K > 1 ? q->K : 1) || x_dtype < EXO_GEMM_BF16 || x_dtype > EXO_GEMM_FP32) return EXO_GEMM_ERR_INVALID_ARG;
+  if (q->rows == 0) return EXO_GEMM_OK;
+  if (!X && q->K > 0) return EXO_GEMM_ERR_NULL;
+  if ((st = check_i8_memory(q)) != EXO_GEMM_OK) return st;
+  const int bytes = x_dtype == EXO_GEMM_FP32 ? 4 : 2;
+  if ((uintptr_t)X & (unsigned)(bytes - 1)) return EXO_GEMM_ERR_ALIGNMENT;
+  int sms = 0;
+  if ((st = device_check(&sms)) != EXO_GEMM_OK) return st;
+  QuantParams p{X, ldx, q->codes, q->ld, q->scales, (int32_t)q->K};
+  const bool wide = align_of(X, ldx * bytes) >= 16;
+  void* fn = x_dtype == EXO_GEMM_FP32 ? quant_fn<float, 4>(wide) : x_dtype == EXO_GEMM_BF16 ? quant_fn<Bf16, 8>(wide) : quant_fn<Fp16, 8>(wide);
+  void* args[1] = {&p};
+  return launch_args(fn, dim3((unsigned)q->rows), kQuantThreads, 0, 1, (cudaStream_t)cuda_stream, args);
+}
+
+exo_gemm_status_t exo_gemm_i8_run(const exo_i8_t* X, const exo_i8_t* W, void* Y, int64_t ldy, int32_t y_dtype, float alpha, float beta, void* cuda_stream) {
+  exo_gemm_status_t st;
+  if ((st = check_i8(X)) != EXO_GEMM_OK || (st = check_i8(W)) != EXO_GEMM_OK) return st;
+  if (X->K != W->K || ldy < (W->rows > 1 ? W->rows : 1) || y_dtype < EXO_GEMM_BF16 || y_dtype > EXO_GEMM_FP32) return EXO_GEMM_ERR_INVALID_ARG;
+  if (X->K > 131071) return EXO_GEMM_ERR_UNSUPPORTED;   // 2^17 products of -128 * -128 are more than a 32-bit integer holds
+  if (X->rows == 0 || W->rows == 0) return EXO_GEMM_OK;
+  const bool read = alpha != 0.f && X->K > 0;
+  if (!Y) return EXO_GEMM_ERR_NULL;
+  if (read && ((st = check_i8_memory(X)) != EXO_GEMM_OK || (st = check_i8_memory(W)) != EXO_GEMM_OK)) return st;
+  const int bytes = y_dtype == EXO_GEMM_FP32 ? 4 : 2;
+  if ((uintptr_t)Y & (unsigned)(bytes - 1)) return EXO_GEMM_ERR_ALIGNMENT;
+  int sms = 0;
+  if ((st = device_check(&sms)) != EXO_GEMM_OK) return st;
+  cudaStream_t stream = (cudaStream_t)cuda_stream;
+  const int64_t M = X->rows, N = W->rows, K = X->K;
+  if (!read) {
+    ScaleYParams p{Y, ldy, M, N, y_dtype, beta};
+    const int64_t ctas = (M * N + kScaleYThreads - 1) / kScaleYThreads;
+    void* args[1] = {&p};
+    return launch_args((void*)exo_i8_scale_kernel, dim3((unsigned)(ctas < 16 * sms ? ctas : 16 * sms)), kScaleYThreads, 0, 1, stream, args);
+  }
+  I8Op::Params o{X->scales, W->scales, Y, ldy, y_dtype, align_of(Y, ldy * bytes), alpha, beta};
+  const Operand A{X->codes, M, K, X->ld}, B{W->codes, N, K, W->ld};
+  if (M <= kThinRows) return launch_thin<I8Op, 16>(thin_width(N, 16, 256, sms), A, B, N, K, 0, false, o, stream);
+  return launch_pair<I8Op, false>(pair_bn(M, N, false, sms), A, B, N, K, 0, false, sms, o, stream);
+}
+
+}  // extern "C"

@@ -255,8 +255,9 @@ exo_gemm_lean_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_cons
       mine = nch < 0 ? 0 : (nch > CPW ? CPW : nch);
     }
     const uint32_t buf0 = epi0 + (quad * NCHUNK + (uint32_t)first_chunk) * kEpiBufBytes;
-    const bool has_beta = p.beta != 0.f, has_acc = nkb > 0, scale = p.alpha != 1.f;
-    const float alpha = p.alpha, beta = p.beta;
+    const bool has_beta = p.beta != 0.f, has_acc = nkb > 0;
+    const float alpha = p.alpha_dev ? p.alpha * ptx::ld_global_cg_f32(p.alpha_dev) : p.alpha, beta = p.beta;
+    const bool scale = alpha != 1.f;
     const uint32_t owner = quad / QPC;               // the rank that finishes this warp's rows
     const bool finish = owner == rank;
     EXO_TRACE_W(0);

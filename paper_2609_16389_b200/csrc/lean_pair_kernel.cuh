@@ -212,8 +212,9 @@ exo_gemm_lean_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid
     }
     // a staging buffer per chunk and quadrant in the operand ring, which is idle once the accumulator is complete
     const uint32_t buf0 = stage0 + (quad * NCHUNK + (uint32_t)first_chunk) * kEpiBufBytes;
-    const bool has_beta = p.beta != 0.f, has_acc = nkb > 0, scale = p.alpha != 1.f;
-    const float alpha = p.alpha, beta = p.beta;
+    const bool has_beta = p.beta != 0.f, has_acc = nkb > 0;
+    const float alpha = p.alpha_dev ? p.alpha * ptx::ld_global_cg_f32(p.alpha_dev) : p.alpha, beta = p.beta;
+    const bool scale = alpha != 1.f;
     if (has_acc) {
       ok = wait_barrier<true>(tfull_bar, 0u, p, WaitSite{kRoleEpilogue, 200, blockIdx.x, 0});
       ok = __all_sync(0xffffffffu, ok);

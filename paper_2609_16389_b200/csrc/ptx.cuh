@@ -386,6 +386,12 @@ __device__ __forceinline__ void ld_global_cg_v4(const void* addr, uint32_t& a, u
                : "memory");
 }
 
+__device__ __forceinline__ float ld_global_cg_f32(const float* addr) {
+  float v;
+  asm volatile("ld.global.cg.f32 %0, [%1];" : "=f"(v) : "l"(addr) : "memory");
+  return v;
+}
+
 __device__ __forceinline__ uint32_t ld_acquire_gpu(const uint32_t* addr) {
   uint32_t v;
   asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(addr) : "memory");
