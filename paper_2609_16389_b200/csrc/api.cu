@@ -253,6 +253,37 @@ bool encode_operand_map(CUtensorMap* map, int elem_bytes, bool bf16, const void*
   return r == CUDA_SUCCESS;
 }
 
+// The whole 128-byte k-blocks of a tensor-core operand's rows (fused_host.h) as (value of a block, row, part, block), `parts` matrices
+// `part_bytes` apart: a copy lands block by block, each of `box_rows` rows of every part.  And what follows the last whole block, as (value,
+// row, part).
+bool encode_blocks_map(CUtensorMap* whole, CUtensorMap* rest, int elem_bytes, bool bf16, const void* base, uint64_t inner, uint64_t rows,
+                       uint64_t row_bytes, uint64_t parts, uint64_t part_bytes, uint32_t box_rows, uint32_t box_blocks) {
+  EncodeTiledFn fn = get_encode_fn();
+  const CUtensorMapDataType dt = elem_bytes == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                                                                                       : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+  const uint32_t per = 128u / (uint32_t)elem_bytes;
+  const uint64_t blocks = inner / per;
+  cuuint32_t estr[4] = {1, 1, 1, 1};
+  CUresult r = fn ? CUDA_SUCCESS : CUDA_ERROR_NOT_FOUND;
+  if (r == CUDA_SUCCESS && blocks > 0) {
+    cuuint64_t dims[4] = {per, rows, parts, blocks};
+    cuuint64_t strides[3] = {row_bytes, parts > 1 ? part_bytes : row_bytes, 128};
+    cuuint32_t box[4] = {per, box_rows, (cuuint32_t)parts, box_blocks};
+    r = fn(whole, dt, 4, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+           CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  }
+  if (r == CUDA_SUCCESS) {
+    cuuint64_t dims[3] = {inner, rows, parts};
+    cuuint64_t strides[2] = {row_bytes, parts > 1 ? part_bytes : row_bytes};
+    cuuint32_t box[3] = {per, box_rows, (cuuint32_t)parts};
+    r = fn(rest, dt, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+           CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  }
+  if (blocks == 0) *whole = *rest;   // never read: keeps its prefetch valid
+  if (r != CUDA_SUCCESS) g_last_cuda_error = (int)r;
+  return r == CUDA_SUCCESS;
+}
+
 }  // namespace exo
 
 struct exo_gemm_plan {

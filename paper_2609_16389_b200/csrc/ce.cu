@@ -48,22 +48,40 @@ struct StatsOp {
   }
   template <int U>
   static __device__ __forceinline__ void look(const Params&, State& s, uint32_t (&v)[U], int n) {
+    float top[4] = {s.top, s.top, s.top, s.top};
+    if (n >= U) {
 #pragma unroll
-    for (int k = 0; k < U; ++k)
-      if (k < n) s.top = fmaxf(s.top, __uint_as_float(v[k]));
+      for (int k = 0; k < U; ++k) top[k & 3] = fmaxf(top[k & 3], __uint_as_float(v[k]));
+    } else {
+#pragma unroll
+      for (int k = 0; k < U; ++k)
+        if (k < n) top[k & 3] = fmaxf(top[k & 3], __uint_as_float(v[k]));
+    }
+    s.top = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
   }
   static __device__ __forceinline__ void looked(State&) {}
   template <int U>
   static __device__ __forceinline__ void unit(const Params& o, State& s, uint32_t (&v)[U], uint32_t (&)[1], int row, bool row_ok, int col, int n) {
     const float top = s.top == -INFINITY ? 0.f : s.top;   // a part without a finite logit: exponentials of -inf, or NaN, as they are
     float e[U];
+    if (n >= U) {
 #pragma unroll
-    for (int k = 0; k < U; ++k) {
-      const float l = __uint_as_float(v[k]);
-      e[k] = k < n ? __expf(l - top) : 0.f;
-      s.sum += e[k];
-      if (o.all && k < n) s.all += l;
+      for (int k = 0; k < U; ++k) e[k] = __expf(__uint_as_float(v[k]) - top);
+      if (o.all) {
+#pragma unroll
+        for (int k = 0; k < U; ++k) s.all += __uint_as_float(v[k]);
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < U; ++k) {
+        e[k] = k < n ? __expf(__uint_as_float(v[k]) - top) : 0.f;
+        if (o.all && k < n) s.all += __uint_as_float(v[k]);
+      }
     }
+    float sum[4] = {};
+#pragma unroll
+    for (int k = 0; k < U; ++k) sum[k & 3] += e[k];
+    s.sum += (sum[0] + sum[1]) + (sum[2] + sum[3]);
     const int32_t t = s.target - col;
     if (t >= 0 && t < n) {
       float l = 0.f;
@@ -141,13 +159,23 @@ __global__ void __launch_bounds__(kJoinThreads) exo_ce_join_kernel(const JoinPar
   const int64_t row = (int64_t)blockIdx.x * 32 + lane;
   float top = -INFINITY, sum = 0.f, all = 0.f;
   if (row < p.rows) {
-    // the largest first: the sums are then of independent loads
-#pragma unroll 8
-    for (int i = warp; i < p.parts; i += 32) top = fmaxf(top, __ldcg(p.top + (int64_t)i * p.rows + row));
-    const float base = top == -INFINITY ? 0.f : top;
-#pragma unroll 4
-    for (int i = warp; i < p.parts; i += 32)
-      sum += weighted(__ldcg(p.sum + (int64_t)i * p.rows + row), __ldcg(p.top + (int64_t)i * p.rows + row), base);
+    // eight parts at a time: their loads are independent
+    for (int i0 = warp; i0 < p.parts; i0 += 8 * 32) {
+      float t[8], s[8], m = top;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int i = i0 + 32 * j;
+        t[j] = i < p.parts ? __ldcg(p.top + (int64_t)i * p.rows + row) : -INFINITY;
+        s[j] = i < p.parts ? __ldcg(p.sum + (int64_t)i * p.rows + row) : 0.f;
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) m = fmaxf(m, t[j]);
+      const float base = m == -INFINITY ? 0.f : m;
+      sum = weighted(sum, top, base);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sum += weighted(s[j], t[j], base);
+      top = m;
+    }
     if (p.all) {
 #pragma unroll 4
       for (int i = warp; i < p.parts; i += 32) all += __ldcg(p.all + (int64_t)i * p.rows + row);

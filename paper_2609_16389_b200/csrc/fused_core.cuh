@@ -46,8 +46,10 @@ struct CoreParams {
   int32_t nkb;         // k-blocks: 128 bytes of a row of A and of B
   int32_t stages;
   int32_t width;       // result columns of a tile
-  int32_t b_split;     // pair: how many rows of B lie between what CTA 0 and what CTA 1 stage; thin: between gate and up
+  int32_t b_split;     // pair: how many rows of B lie between what CTA 0 and what CTA 1 stage
   int32_t a_rows;      // thin: rows of A staged, M rounded up to 8
+  int32_t per_stage;   // thin: k-blocks of a stage
+  int32_t whole;       // thin: k-blocks that are whole; the last one may not be
   uint32_t idesc;
   OperandStaging a, b;
   Raster raster;
@@ -68,8 +70,8 @@ EXO_CX int pair_stages(int bn) {
 EXO_CX int pair_smem(int bn) { return pair_stages(bn) * pair_stage_bytes(bn) + kPairBarrierBytes + 1024; }
 // The MMAs read 128 rows of A whatever a stage holds of it: what follows the rows staged becomes accumulator rows that nobody reads, and
 // behind the last stage it is room that the ring keeps.
-EXO_CX int thin_smem(int stages, int b_rows, int a_rows) {
-  return 1024 + kThinBarrierBytes + 512 + stages * (b_rows + a_rows) * 128 + (128 - a_rows) * 128;
+EXO_CX int thin_smem(int stages, int per_stage, int b_rows, int a_rows) {
+  return 1024 + kThinBarrierBytes + 512 + stages * per_stage * (b_rows + a_rows) * 128 + (128 - a_rows) * 128;
 }
 
 // ---------------------------------------------------------------- bounded waits
@@ -118,6 +120,11 @@ template <class Op, int CTA_GROUP>
 __device__ __forceinline__ void umma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
   if constexpr (Op::kInt8) umma_i8<CTA_GROUP>(d, a, b, idesc, accumulate);
   else ptx::umma_f16<CTA_GROUP>(d, a, b, idesc, accumulate);
+}
+
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, int32_t x, int32_t y, int32_t z, int32_t w, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+               ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar) : "memory");
 }
 
 __device__ __forceinline__ void tmem_ld(uint32_t taddr, uint32_t (&r)[32]) { ptx::tmem_ld_32x32(taddr, r); }
@@ -371,11 +378,12 @@ exo_fused_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
 }
 
 // ---------------------------------------------------------------- a few rows: one tile per CTA
-// A stage is the tile's rows of B (gate's and up's for a gated product) and the a_rows rows of A.  U: columns of an epilogue unit.
+// A stage is `per_stage` k-blocks of the tile's rows of B (gate's and up's for a gated product) and of the a_rows rows of A, a copy each:
+// issuing a copy takes a few hundred clocks, in which an SM's share of memory bandwidth is some 8 KB.  U: columns of an epilogue unit.
 template <class Op, int U>
 __global__ void __launch_bounds__(kThinThreads, 2)
-exo_fused_thin_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b, const __grid_constant__ CoreParams p,
-                      const __grid_constant__ typename Op::Params o) {
+exo_fused_thin_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_a_rest, const __grid_constant__ CUtensorMap tm_b,
+                      const __grid_constant__ CUtensorMap tm_b_rest, const __grid_constant__ CoreParams p, const __grid_constant__ typename Op::Params o) {
   constexpr int SUB_K = Op::kInt8 ? 128 : 64;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t stage0 = (ptx::smem_u32(smem_raw) + kThinBarrierBytes + 1023u) & ~1023u, bar0 = stage0 - kThinBarrierBytes;
@@ -384,10 +392,11 @@ exo_fused_thin_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
   const uint32_t tfull_bar = bar0 + 8u * (2 * kThinMaxStages), tmem_slot = tfull_bar + 8u;
   const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
   const uint32_t width = (uint32_t)p.width, bn = Op::kGated ? 2u * width : width;
-  const uint32_t b_bytes = bn * 128u, stage_bytes = b_bytes + (uint32_t)p.a_rows * 128u, stages = (uint32_t)p.stages;
+  const uint32_t b_bytes = bn * 128u, a_bytes = (uint32_t)p.a_rows * 128u, stages = (uint32_t)p.stages;   // b_bytes, a_bytes: of a k-block
+  const uint32_t stage_bytes = (b_bytes + a_bytes) * (uint32_t)p.per_stage, a_at = b_bytes * (uint32_t)p.per_stage;
   uint32_t tmem_cols = 32;
   while (tmem_cols < bn) tmem_cols *= 2;
-  const int32_t nkb = p.nkb, col0 = (int32_t)(blockIdx.x * width);
+  const int32_t nkb = p.nkb, whole = p.whole, per = p.per_stage, col0 = (int32_t)(blockIdx.x * width);
 
   if (warp == 0) {
     if (lane == 0) {
@@ -413,16 +422,23 @@ exo_fused_thin_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
     ptx::grid_dependency_wait();
     uint32_t s = 0, ph = 0;
     bool skip = p.skip_copies != 0 && blockIdx.x == 0;
-    for (int32_t kb = 0; kb < nkb; ++kb) {
+    for (int32_t kb = 0; kb < nkb; kb += kb < whole ? (kb + per > whole ? whole - kb : per) : 1) {
       ok = wait_warp(empty_bar(s), ph ^ 1u, p.wait_clocks);
       if (!ok) break;
       if (ptx::elect_one()) {
-        const uint32_t dst = stage0 + s * stage_bytes;
-        ptx::mbar_arrive_expect_tx(full_bar(s), stage_bytes);
-        if (!skip) {
-          ptx::tma_load_2d(dst, &tm_b, kb * SUB_K, col0, full_bar(s));
-          if constexpr (Op::kGated) ptx::tma_load_2d(dst + width * 128u, &tm_b, kb * SUB_K, col0 + p.b_split, full_bar(s));
-          ptx::tma_load_2d(dst + b_bytes, &tm_a, kb * SUB_K, 0, full_bar(s));
+        const uint32_t dst = stage0 + s * stage_bytes, bar = full_bar(s);
+        if (kb < whole) {   // (blocks beyond the last whole one arrive as zeros)
+          ptx::mbar_arrive_expect_tx(bar, stage_bytes);
+          if (!skip) {
+            tma_load_4d(dst, &tm_b, 0, col0, 0, kb, bar);
+            tma_load_4d(dst + a_at, &tm_a, 0, 0, 0, kb, bar);
+          }
+        } else {
+          ptx::mbar_arrive_expect_tx(bar, b_bytes + a_bytes);
+          if (!skip) {
+            ptx::tma_load_3d(dst, &tm_b_rest, kb * SUB_K, col0, 0, bar);
+            ptx::tma_load_3d(dst + a_at, &tm_a_rest, kb * SUB_K, 0, 0, bar);
+          }
         }
       }
       skip = false;
@@ -432,17 +448,22 @@ exo_fused_thin_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
     ptx::grid_dependency_wait();
     uint32_t s = 0, ph = 0;
     const uint32_t a_step = p.a.k_step_enc, b_step = p.b.k_step_enc, idesc = p.idesc;
-    for (int32_t kb = 0; kb < nkb; ++kb) {
+    for (int32_t kb = 0; kb < nkb;) {
+      const int32_t blocks = kb < whole ? (kb + per > whole ? whole - kb : per) : 1;
       ok = wait_warp(full_bar(s), ph, p.wait_clocks);
       if (!ok) break;
       ptx::tc_fence_after_sync();
-      const uint64_t b_desc = smem_desc(stage0 + s * stage_bytes, p.b), a_desc = smem_desc(stage0 + s * stage_bytes + b_bytes, p.a);
+      const uint64_t b_desc = smem_desc(stage0 + s * stage_bytes, p.b), a_desc = smem_desc(stage0 + s * stage_bytes + a_at, p.a);
       if (ptx::elect_one()) {
+        for (int32_t j = 0; j < blocks; ++j) {
+          const uint64_t a_j = a_desc + (uint32_t)j * (a_bytes >> 4), b_j = b_desc + (uint32_t)j * (b_bytes >> 4);
 #pragma unroll
-        for (uint32_t k = 0; k < 4; ++k) umma<Op, 1>(tmem_base, a_desc + k * a_step, b_desc + k * b_step, idesc, (kb > 0 || k > 0) ? 1u : 0u);
+          for (uint32_t k = 0; k < 4; ++k) umma<Op, 1>(tmem_base, a_j + k * a_step, b_j + k * b_step, idesc, (kb > 0 || j > 0 || k > 0) ? 1u : 0u);
+        }
         ptx::umma_commit<1>(empty_bar(s), 1);
-        if (kb == nkb - 1) ptx::umma_commit<1>(tfull_bar, 1);
+        if (kb + blocks == nkb) ptx::umma_commit<1>(tfull_bar, 1);
       }
+      kb += blocks;
       if (++s == stages) { s = 0; ph ^= 1u; }
     }
   } else {

@@ -15,6 +15,8 @@
 namespace exo {
 bool encode_operand_map(CUtensorMap* map, int elem_bytes, bool bf16, const void* base, uint64_t inner, uint64_t rows, uint64_t row_bytes,
                         uint32_t box_rows);   // api.cu
+bool encode_blocks_map(CUtensorMap* whole, CUtensorMap* rest, int elem_bytes, bool bf16, const void* base, uint64_t inner, uint64_t rows,
+                       uint64_t row_bytes, uint64_t parts, uint64_t part_bytes, uint32_t box_rows, uint32_t box_blocks);   // api.cu
 exo_gemm_status_t gemm_create_exact(exo_gemm_handle_t* out, const exo_gemm_desc_t* desc);   // api.cu
 exo_gemm_status_t gemm_run_scaled(exo_gemm_plan* plan, const void* A, const void* B, void* C, float alpha, const float* alpha_dev, float beta,
                                   void* cuda_stream);   // api.cu
@@ -92,36 +94,33 @@ inline exo_gemm_status_t launch_args(void* fn, dim3 grid, unsigned threads, size
   return e == cudaSuccess ? EXO_GEMM_OK : cuda_failed(e);
 }
 
-// How a product runs: thin (a few rows) or by pairs of CTAs, and how many result columns a tile has.
-struct Shape {
-  bool thin;
-  int width;      // result columns of a tile
-  int stages;     // thin
-  int b_rows;     // thin: rows of B per stage
-};
-
 constexpr int kThinRows = 128;   // what one tile's accumulator has
 
-// Thin tiles: the widest that spreads the columns evenly over the SMs.  quantum: what a width is a multiple of; most: the widest.
+// Thin tiles: a width that spreads the columns evenly over the SMs, with a charge per tile for its start and end.  quantum: what a width is a
+// multiple of; most: the widest.
 inline int thin_width(int64_t N, int quantum, int most, int sms) {
   int best = quantum;
   int64_t cost = -1;
   for (int w = quantum; w <= most; w += quantum) {
-    const int64_t tiles = (N + w - 1) / w, waves = (tiles + sms - 1) / sms, c = waves * w;
+    const int64_t tiles = (N + w - 1) / w, waves = (tiles + sms - 1) / sms, c = waves * (w + 8);
     if (cost < 0 || c <= cost) { cost = c; best = w; }
   }
   return best;
 }
-// Stages of a thin tile: 100 KB of ring, so that two CTAs share an SM and one's start and end hide behind the other's copies, but four stages
-// at least.
-inline int thin_stages(int b_rows, int a_rows, int64_t nkb) {
-  const int stage = (b_rows + a_rows) * 128;
-  int n = 100 * 1024 / stage;
+// Stages of some 20 KB, and 100 KB of them in all, so that two CTAs share an SM and one's start and end hide behind the other's copies; four
+// stages at least.
+inline void thin_ring(int b_rows, int a_rows, int64_t whole, int* per_stage, int* stages) {
+  const int block = (b_rows + a_rows) * 128;
+  int per = 20 * 1024 / block;
+  if (per > 16) per = 16;
+  if (per > whole) per = (int)whole;
+  if (per < 1) per = 1;
+  int n = 100 * 1024 / (per * block);
   if (n < 4) n = 4;
-  while (n > 2 && thin_smem(n, b_rows, a_rows) > kSmemLimit) --n;
   if (n > kThinMaxStages) n = kThinMaxStages;
-  if (n > nkb) n = (int)nkb;
-  return n < 1 ? 1 : n;
+  while (n > 1 && thin_smem(n, per, b_rows, a_rows) > kSmemLimit) --n;
+  *per_stage = per;
+  *stages = n;
 }
 
 // Columns of a pair's tile: 256 accumulator columns, or 128 where that fills the waves better by more than it costs (a tile of 128 moves a half
@@ -185,24 +184,26 @@ exo_gemm_status_t launch_thin(int width, const Operand& A, const Operand& B, int
   p.N = (int32_t)N;
   p.nkb = (int32_t)((K + SUB_K - 1) / SUB_K);
   p.width = width;
-  p.b_split = (int32_t)b_split;
   p.a_rows = a_rows;
-  p.stages = thin_stages(bn, a_rows, p.nkb);
+  p.whole = (int32_t)(K / SUB_K);
+  thin_ring(bn, a_rows, p.whole, &p.per_stage, &p.stages);
   p.idesc = Op::kInt8 ? (2u << 4 | 1u << 7 | 1u << 10 | (uint32_t)(bn >> 3) << 17 | 8u << 24)
                       : make_idesc(bf16 ? EXO_GEMM_BF16 : EXO_GEMM_FP16, 0, 0, 128, bn);
   p.a = make_staging(0, kBlockM, 1, 2);
   p.b = make_staging(0, bn, 1, 2);
-  CUtensorMap ma, mb;
-  if (!encode_operand_map(&ma, ES, bf16, A.base, (uint64_t)A.inner, (uint64_t)A.rows, (uint64_t)(A.ld * ES), (uint32_t)a_rows) ||
-      !encode_operand_map(&mb, ES, bf16, B.base, (uint64_t)B.inner, (uint64_t)B.rows, (uint64_t)(B.ld * ES), (uint32_t)width))
+  CUtensorMap ma, ma_rest, mb, mb_rest;
+  const uint64_t parts = Op::kGated ? 2 : 1, part_bytes = (uint64_t)b_split * (uint64_t)(B.ld * ES);
+  if (!encode_blocks_map(&ma, &ma_rest, ES, bf16, A.base, (uint64_t)A.inner, (uint64_t)A.rows, (uint64_t)(A.ld * ES), 1, 0, (uint32_t)a_rows, (uint32_t)p.per_stage) ||
+      !encode_blocks_map(&mb, &mb_rest, ES, bf16, B.base, (uint64_t)B.inner, (uint64_t)N, (uint64_t)(B.ld * ES), parts, part_bytes, (uint32_t)width,
+                         (uint32_t)p.per_stage))
     return EXO_GEMM_ERR_CUDA;
   const WaitHook hook = take_wait_hook();
   p.wait_clocks = hook.clocks;
   p.skip_copies = hook.skip;
   typename Op::Params o = op;
-  void* args[4] = {&ma, &mb, &p, &o};
+  void* args[6] = {&ma, &ma_rest, &mb, &mb_rest, &p, &o};
   return launch_args((void*)exo_fused_thin_kernel<Op, U>, dim3((unsigned)((N + width - 1) / width)), kThinThreads,
-                     (size_t)thin_smem(p.stages, bn, a_rows), 1, stream, args);
+                     (size_t)thin_smem(p.stages, p.per_stage, bn, a_rows), 1, stream, args);
 }
 
 // dst = src, `rows` rows of `inner` 16-bit values; dst's rows start on 16 bytes and have room for a multiple of 8 values.

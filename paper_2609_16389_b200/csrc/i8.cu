@@ -9,8 +9,8 @@ namespace fused {
 namespace {
 
 // ---------------------------------------------------------------- quantisation
-// A CTA per row: the largest magnitude, then the codes; the second pass over the row finds it in L1 or L2.  Bound by memory for many rows
-// (2 + 1 bytes a value) and by two trips through it for one.
+// A CTA per row: the largest magnitude, then the codes, from registers.  Bound by memory for many rows (2 + 1 bytes a value) and by the
+// latency of a load, a reduction and a store for few.
 struct QuantParams {
   const void* x;
   int64_t ldx;
@@ -19,14 +19,12 @@ struct QuantParams {
   float* scales;
   int32_t K;
 };
-constexpr int kQuantThreads = 256;
-
 template <class T> struct Element { using type = uint16_t; };
 template <> struct Element<float> { using type = float; };
 
-// V values from k on as fp32; those from K on are 0
+// V values from k on as fp32
 template <class T, int V>
-__device__ __forceinline__ void load_values(const typename Element<T>::type* x, int k, int K, float (&v)[V]) {
+__device__ __forceinline__ void load_values(const typename Element<T>::type* x, int k, float (&v)[V]) {
   if constexpr (std::is_same<T, float>::value) {
     if (V == 4) {
       const float4 w = *reinterpret_cast<const float4*>(x + k);
@@ -43,29 +41,58 @@ __device__ __forceinline__ void load_values(const typename Element<T>::type* x, 
   }
 }
 
-// code of x: the quotient is rounded as IEEE division rounds it, and then to the nearest integer, ties to even
-__device__ __forceinline__ int code_of(float x, float scale) { return (int)fminf(fmaxf(rintf(__fdiv_rn(x, scale)), -127.f), 127.f); }
+// Codes: the quotient rounded as IEEE division rounds it, then to the nearest integer, ties to even.  The product with the rounded
+// reciprocal is within 2^-22 of the quotient, relative, so both round to the same integer unless the product is within 127 * 2^-22 of a tie; there,
+// and for scales whose reciprocal is not a normal number, the division is made.
+struct Divider {
+  float scale, inverse;
+  bool safe;
+  __device__ __forceinline__ explicit Divider(float s) : scale(s), inverse(1.f / s), safe(s > 0x1p-120f && s < 0x1p120f) {}
+  __device__ __forceinline__ int code(float x) const {
+    float q = x * inverse, r = rintf(q);
+    if (!safe || fabsf(fabsf(q - r) - 0.5f) < 0x1p-14f) r = rintf(__fdiv_rn(x, scale));
+    return (int)fminf(fmaxf(r, -127.f), 127.f);
+  }
+};
 
-// V: values per load, 16 bytes of them where the rows allow that, else one
-template <class T, int V>
-__global__ void __launch_bounds__(kQuantThreads) exo_i8_quantize_kernel(const QuantParams p) {
-  __shared__ float tops[kQuantThreads / 32];
+// V: values per load, 16 bytes of them where the rows allow that, else one.  THREADS per row; a thread keeps its first kHeld loads in
+// registers, further ones are read again.
+constexpr int kHeld = 8;
+template <class T, int V, int THREADS>
+__global__ void __launch_bounds__(THREADS) exo_i8_quantize_kernel(const QuantParams p) {
+  __shared__ float tops[THREADS / 32];
+  using E = typename Element<T>::type;
   ptx::grid_launch_dependents();
   ptx::grid_dependency_wait();
-  const typename Element<T>::type* x = (const typename Element<T>::type*)p.x + (int64_t)blockIdx.x * p.ldx;
+  const E* x = (const E*)p.x + (int64_t)blockIdx.x * p.ldx;
   int8_t* codes = p.codes + (int64_t)blockIdx.x * p.ld;
   const int whole = p.K / V * V;   // the values of whole loads; the others one by one
-  float top = 0.f;
+  const int first = threadIdx.x * V;
+  constexpr int STEP = THREADS * V;
+  float top = 0.f, held[kHeld][V];
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) {
+    if (first + i * STEP < whole) {
+      load_values<T, V>(x, first + i * STEP, held[i]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < V; ++j) held[i][j] = 0.f;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i)
+#pragma unroll
+    for (int j = 0; j < V; ++j) top = fmaxf(top, fabsf(held[i][j]));
 #pragma unroll 4
-  for (int k = threadIdx.x * V; k < whole; k += kQuantThreads * V) {
+  for (int k = first + kHeld * STEP; k < whole; k += STEP) {
     float v[V];
-    load_values<T, V>(x, k, p.K, v);
+    load_values<T, V>(x, k, v);
 #pragma unroll
     for (int j = 0; j < V; ++j) top = fmaxf(top, fabsf(v[j]));
   }
-  for (int k = whole + threadIdx.x; k < p.K; k += kQuantThreads) {
+  for (int k = whole + threadIdx.x; k < p.K; k += THREADS) {
     float v[1];
-    load_values<T, 1>(x, k, p.K, v);
+    load_values<T, 1>(x, k, v);
     top = fmaxf(top, fabsf(v[0]));
   }
 #pragma unroll
@@ -73,24 +100,31 @@ __global__ void __launch_bounds__(kQuantThreads) exo_i8_quantize_kernel(const Qu
   if ((threadIdx.x & 31) == 0) tops[threadIdx.x >> 5] = top;
   __syncthreads();
 #pragma unroll
-  for (int w = 0; w < kQuantThreads / 32; ++w) top = fmaxf(top, tops[w]);
+  for (int w = 0; w < THREADS / 32; ++w) top = fmaxf(top, tops[w]);
   const float scale = __fdiv_rn(top, 127.f);
   if (threadIdx.x == 0) p.scales[blockIdx.x] = scale;
   const bool zero = !(scale > 0.f);
-  for (int k = threadIdx.x * V; k < whole; k += kQuantThreads * V) {
-    float v[V];
-    load_values<T, V>(x, k, p.K, v);
+  const Divider by(zero ? 1.f : scale);
+  auto store = [&](int k, const float (&v)[V]) {
     uint32_t w[(V + 3) / 4] = {};
 #pragma unroll
-    for (int j = 0; j < V; ++j) w[j / 4] |= (uint32_t)((zero ? 0 : code_of(v[j], scale)) & 255) << (8 * (j & 3));
+    for (int j = 0; j < V; ++j) w[j / 4] |= (uint32_t)((zero ? 0 : by.code(v[j])) & 255) << (8 * (j & 3));
     if constexpr (V == 8) *reinterpret_cast<uint2*>(codes + k) = make_uint2(w[0], w[1]);
     else if constexpr (V == 4) *reinterpret_cast<uint32_t*>(codes + k) = w[0];
     else codes[k] = (int8_t)w[0];
+  };
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i)
+    if (first + i * STEP < whole) store(first + i * STEP, held[i]);
+  for (int k = first + kHeld * STEP; k < whole; k += STEP) {
+    float v[V];
+    load_values<T, V>(x, k, v);
+    store(k, v);
   }
-  for (int k = whole + threadIdx.x; k < p.K; k += kQuantThreads) {
+  for (int k = whole + threadIdx.x; k < p.K; k += THREADS) {
     float v[1];
-    load_values<T, 1>(x, k, p.K, v);
-    codes[k] = (int8_t)(zero ? 0 : code_of(v[0], scale));
+    load_values<T, 1>(x, k, v);
+    codes[k] = (int8_t)(zero ? 0 : by.code(v[0]));
   }
 }
 
@@ -211,7 +245,10 @@ exo_gemm_status_t check_i8_memory(const exo_i8_t* q) {
   return aligned16(q->codes) && q->ld % 16 == 0 && ((uintptr_t)q->scales & 3u) == 0 ? EXO_GEMM_OK : EXO_GEMM_ERR_ALIGNMENT;
 }
 
-template <class T, int V> void* quant_fn(bool wide) { return wide ? (void*)exo_i8_quantize_kernel<T, V> : (void*)exo_i8_quantize_kernel<T, 1>; }
+template <class T, int V> void* quant_fn(bool wide, int threads) {
+  if (wide) return threads == 128 ? (void*)exo_i8_quantize_kernel<T, V, 128> : (void*)exo_i8_quantize_kernel<T, V, 512>;
+  return threads == 128 ? (void*)exo_i8_quantize_kernel<T, 1, 128> : (void*)exo_i8_quantize_kernel<T, 1, 512>;
+}
 
 }  // namespace
 
@@ -267,9 +304,13 @@ exo_gemm_status_t exo_i8_quantize(const exo_i8_t* q, const void* X, int64_t ldx,
   if ((st = device_check(&sms)) != EXO_GEMM_OK) return st;
   QuantParams p{X, ldx, q->codes, q->ld, q->scales, (int32_t)q->K};
   const bool wide = align_of(X, ldx * bytes) >= 16;
-  void* fn = x_dtype == EXO_GEMM_FP32 ? quant_fn<float, 4>(wide) : x_dtype == EXO_GEMM_BF16 ? quant_fn<Bf16, 8>(wide) : quant_fn<Fp16, 8>(wide);
+  // few rows: more threads each, since nothing else hides a row's loads; many: more rows at once
+  const int threads = q->rows <= 2 * sms ? 512 : 128;
+  void* fn = x_dtype == EXO_GEMM_FP32   ? quant_fn<float, 4>(wide, threads)
+             : x_dtype == EXO_GEMM_BF16 ? quant_fn<Bf16, 8>(wide, threads)
+                                        : quant_fn<Fp16, 8>(wide, threads);
   void* args[1] = {&p};
-  return launch_args(fn, dim3((unsigned)q->rows), kQuantThreads, 0, 1, (cudaStream_t)cuda_stream, args);
+  return launch_args(fn, dim3((unsigned)q->rows), (unsigned)threads, 0, 1, (cudaStream_t)cuda_stream, args);
 }
 
 exo_gemm_status_t exo_gemm_i8_run(const exo_i8_t* X, const exo_i8_t* W, void* Y, int64_t ldy, int32_t y_dtype, float alpha, float beta, void* cuda_stream) {
