@@ -272,14 +272,15 @@ bool encode_blocks_map(CUtensorMap* whole, CUtensorMap* rest, int elem_bytes, bo
     r = fn(whole, dt, 4, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   }
-  if (r == CUDA_SUCCESS) {
+  if (r == CUDA_SUCCESS && inner % per) {
     cuuint64_t dims[3] = {inner, rows, parts};
     cuuint64_t strides[2] = {row_bytes, parts > 1 ? part_bytes : row_bytes};
     cuuint32_t box[3] = {per, box_rows, (cuuint32_t)parts};
     r = fn(rest, dt, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   }
-  if (blocks == 0) *whole = *rest;   // never read: keeps its prefetch valid
+  if (blocks == 0) *whole = *rest;   // one of the two may never be read: it is a valid map all the same
+  if (inner % per == 0) *rest = *whole;
   if (r != CUDA_SUCCESS) g_last_cuda_error = (int)r;
   return r == CUDA_SUCCESS;
 }

@@ -387,7 +387,7 @@ exo_gemm_status_t forward(exo_ce_plan* p, const void* x, const void* W, const in
   o.vocab = (int32_t)d.vocab;
   const Operand X{x, d.tokens, d.hidden, p->ldx}, Wo{W, d.vocab, d.hidden, p->ldw};
   const bool bf16 = d.dtype == EXO_GEMM_BF16;
-  return p->thin ? launch_thin<StatsOp<T>, 16>(p->width, X, Wo, d.vocab, d.hidden, 0, bf16, o, stream)
+  return p->thin ? launch_thin<StatsOp<T>, 16>(p->width, X, Wo, d.vocab, d.hidden, 0, bf16, p->sms, o, stream)
                  : launch_pair<StatsOp<T>, false>(p->width, X, Wo, d.vocab, d.hidden, 0, bf16, p->sms, o, stream);
 }
 
@@ -451,7 +451,7 @@ exo_gemm_status_t exo_ce_create(exo_ce_handle_t* out, const exo_ce_desc_t* desc)
   p->sms = sms;
   const int64_t T = d.tokens, H = d.hidden, V = d.vocab;
   p->thin = T <= kThinRows;
-  p->width = p->thin ? thin_width(V, 32, 256, sms) : pair_bn(T, V, false, sms);
+  p->width = p->thin ? thin_width(V, 32, 256, 1, T, sms) : pair_bn(T, V, false, sms);
   p->parts = (int)((V + p->width - 1) / p->width) * 2;
   p->ldx = d.ldx % 8 ? round_up(H, 64) : d.ldx;
   p->ldw = d.ldw % 8 ? round_up(H, 64) : d.ldw;

@@ -238,11 +238,11 @@ exo_gemm_status_t forward(exo_ffn_plan* p, const void* x, const void* gate_up, c
     st = launch_pair<GatedOp<T>, false>(p->bn_gated, X, GU, d.inner, d.hidden, d.inner, bf16, p->sms, gp, stream);
     return st != EXO_GEMM_OK ? st : gemm_run_scaled(p->down, p->h, down, y, 1.f, nullptr, 0.f, stream);
   }
-  st = launch_thin<GatedOp<T>, 8>(p->width_gated, X, GU, d.inner, d.hidden, d.inner, bf16, gp, stream);
+  st = launch_thin<GatedOp<T>, 8>(p->width_gated, X, GU, d.inner, d.hidden, d.inner, bf16, p->sms, gp, stream);
   if (st != EXO_GEMM_OK) return st;
   typename PlainOp<T>::Params yp{(uint16_t*)y, d.ldy, align_of(y, d.ldy * 2)};
   return launch_thin<PlainOp<T>, 16>(p->width_down, Operand{p->h, d.tokens, d.inner, p->ldh}, Operand{down, d.hidden, d.inner, p->ld_down}, d.hidden, d.inner,
-                                     0, bf16, yp, stream);
+                                     0, bf16, p->sms, yp, stream);
 }
 
 template <class T>
@@ -283,8 +283,8 @@ exo_gemm_status_t exo_ffn_create(exo_ffn_handle_t* out, const exo_ffn_desc_t* de
   p->sms = sms;
   const int64_t T = d.tokens, H = d.hidden, F = d.inner;
   p->thin = T <= kThinRows;
-  p->width_gated = thin_width(F, 8, 128, sms);
-  p->width_down = thin_width(H, 16, 256, sms);
+  p->width_gated = thin_width(F, 8, 128, 2, T, sms);
+  p->width_down = thin_width(H, 16, 256, 1, T, sms);
   p->bn_gated = pair_bn(T, F, true, sms);
   p->bn_back = pair_bn(T, F, false, sms);
   p->ldh = round_up(F, 64);

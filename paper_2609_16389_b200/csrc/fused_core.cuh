@@ -48,6 +48,7 @@ struct CoreParams {
   int32_t width;       // result columns of a tile
   int32_t b_split;     // pair: how many rows of B lie between what CTA 0 and what CTA 1 stage
   int32_t a_rows;      // thin: rows of A staged, M rounded up to 8
+  int32_t quad_rows;   // thin: rows in a lane quadrant of the accumulator: 16 where the MMAs have 64 rows, 32 where they have 128
   int32_t per_stage;   // thin: k-blocks of a stage
   int32_t whole;       // thin: k-blocks that are whole; the last one may not be
   uint32_t idesc;
@@ -68,10 +69,11 @@ EXO_CX int pair_stages(int bn) {
   return n > kMaxStages ? kMaxStages : n;
 }
 EXO_CX int pair_smem(int bn) { return pair_stages(bn) * pair_stage_bytes(bn) + kPairBarrierBytes + 1024; }
-// The MMAs read 128 rows of A whatever a stage holds of it: what follows the rows staged becomes accumulator rows that nobody reads, and
+// The MMAs read 64 or 128 rows of A whatever a stage holds of it: what follows the rows staged becomes accumulator rows that nobody reads, and
 // behind the last stage it is room that the ring keeps.
+EXO_CX int thin_mma_rows(int a_rows) { return a_rows <= 64 ? 64 : 128; }
 EXO_CX int thin_smem(int stages, int per_stage, int b_rows, int a_rows) {
-  return 1024 + kThinBarrierBytes + 512 + stages * per_stage * (b_rows + a_rows) * 128 + (128 - a_rows) * 128;
+  return 1024 + kThinBarrierBytes + 512 + stages * per_stage * (b_rows + a_rows) * 128 + (thin_mma_rows(a_rows) - a_rows) * 128;
 }
 
 // ---------------------------------------------------------------- bounded waits
@@ -379,7 +381,9 @@ exo_fused_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
 
 // ---------------------------------------------------------------- a few rows: one tile per CTA
 // A stage is `per_stage` k-blocks of the tile's rows of B (gate's and up's for a gated product) and of the a_rows rows of A, a copy each:
-// issuing a copy takes a few hundred clocks, in which an SM's share of memory bandwidth is some 8 KB.  U: columns of an epilogue unit.
+// issuing a copy takes a few hundred clocks, in which an SM's share of memory bandwidth is some 8 KB.  Up to 64 rows the MMAs have 64: what
+// such an MMA takes is the reading of its operands from shared memory, mostly A's.  There a lane quadrant of the accumulator holds 16 rows.
+// U: columns of an epilogue unit.
 template <class Op, int U>
 __global__ void __launch_bounds__(kThinThreads, 2)
 exo_fused_thin_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_a_rest, const __grid_constant__ CUtensorMap tm_b,
@@ -466,16 +470,19 @@ exo_fused_thin_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
       kb += blocks;
       if (++s == stages) { s = 0; ph ^= 1u; }
     }
-  } else {
+    ok = ok && wait_warp(tfull_bar, 0u, p.wait_clocks);
+  }
+  // The epilogue's warps wait here, where they take no issue slots: polling for the accumulator they would slow the loops above down by half.
+  const bool all_ok = __syncthreads_and(ok) != 0;
+  if (warp >= 2 && all_ok) {
     ptx::grid_dependency_wait();
     const uint32_t quad = warp & 3u;
-    const int32_t half = (int32_t)((warp - 2u) >> 2), row0 = (int32_t)quad * 32, row = row0 + (int32_t)lane;
-    ok = wait_warp(tfull_bar, 0u, p.wait_clocks);
-    if (ok && row0 < p.M) {
+    const int32_t half = (int32_t)((warp - 2u) >> 2), row0 = (int32_t)quad * p.quad_rows, row = row0 + (int32_t)lane;
+    if (row0 < p.M) {
       ptx::tc_fence_after_sync();
       const int32_t units = (int32_t)width / U, first = half ? (units + 1) / 2 : 0, mine = half ? units / 2 : (units + 1) / 2;
       const uint32_t tacc = tmem_base + ((quad * 32u) << 16) + (uint32_t)(first * U);
-      run_units<Op, U>(o, tacc, width, row, row < p.M, col0 + first * U, mine, p.N, (int)blockIdx.x * 2 + half, [] {});
+      run_units<Op, U>(o, tacc, width, row, (int32_t)lane < p.quad_rows && row < p.M, col0 + first * U, mine, p.N, (int)blockIdx.x * 2 + half, [] {});
     }
   }
   if (!ok)

@@ -96,27 +96,32 @@ inline exo_gemm_status_t launch_args(void* fn, dim3 grid, unsigned threads, size
 
 constexpr int kThinRows = 128;   // what one tile's accumulator has
 
+// Rows of B and A in a stage's k-block with which three stages leave an SM room for a second CTA.
+constexpr int kSharedRows = 288;
 // Thin tiles: a width that spreads the columns evenly over the SMs, with a charge per tile for its start and end.  quantum: what a width is a
-// multiple of; most: the widest.
-inline int thin_width(int64_t N, int quantum, int most, int sms) {
+// multiple of; most: the widest; parts: 2 for a gated product.  More tiles than SMs run two to an SM, which has to have the room.
+inline int thin_width(int64_t N, int quantum, int most, int parts, int64_t rows, int sms) {
+  const int a_rows = (int)round_up(rows, 8);
   int best = quantum;
   int64_t cost = -1;
   for (int w = quantum; w <= most; w += quantum) {
-    const int64_t tiles = (N + w - 1) / w, waves = (tiles + sms - 1) / sms, c = waves * (w + 8);
+    const int64_t tiles = (N + w - 1) / w, waves = (tiles + sms - 1) / sms, c = waves * (w + 64);
+    if (waves > 1 && w > quantum && parts * w + a_rows > kSharedRows) break;
     if (cost < 0 || c <= cost) { cost = c; best = w; }
   }
   return best;
 }
-// Stages of some 20 KB, and 100 KB of them in all, so that two CTAs share an SM and one's start and end hide behind the other's copies; four
-// stages at least.
-inline void thin_ring(int b_rows, int a_rows, int64_t whole, int* per_stage, int* stages) {
+// The ring of a thin tile: three large stages.  A stage costs the issuing warps some 500 clocks whatever it holds, which smaller ones do not
+// hide (16 tokens through a block of 4096 x 10240, us in all, with stages of 20, 32, 48 and 66 KB: 56.8, 52.7, 49.5, 48.3).  One CTA per SM takes
+// 200 KB; where there are more tiles than SMs two CTAs take 100 KB each, so that one's start and end hide behind the other's copies.
+inline void thin_ring(int b_rows, int a_rows, int64_t whole, bool alone, int* per_stage, int* stages) {
   const int block = (b_rows + a_rows) * 128;
-  int per = 20 * 1024 / block;
+  int per = (alone ? 66 : 33) * 1024 / block;
   if (per > 16) per = 16;
   if (per > whole) per = (int)whole;
   if (per < 1) per = 1;
-  int n = 100 * 1024 / (per * block);
-  if (n < 4) n = 4;
+  int n = (alone ? 200 : 100) * 1024 / (per * block);
+  if (n < 3) n = 3;
   if (n > kThinMaxStages) n = kThinMaxStages;
   while (n > 1 && thin_smem(n, per, b_rows, a_rows) > kSmemLimit) --n;
   *per_stage = per;
@@ -176,7 +181,7 @@ exo_gemm_status_t launch_pair(int bn, const Operand& A, const Operand& B, int64_
 
 template <class Op, int U>
 exo_gemm_status_t launch_thin(int width, const Operand& A, const Operand& B, int64_t N, int64_t K, int64_t b_split, bool bf16,
-                              const typename Op::Params& op, cudaStream_t stream) {
+                              int sms, const typename Op::Params& op, cudaStream_t stream) {
   constexpr int ES = Op::kInt8 ? 1 : 2, SUB_K = 128 / ES;
   const int bn = Op::kGated ? 2 * width : width, a_rows = (int)round_up(A.rows, 8);
   CoreParams p{};
@@ -185,10 +190,13 @@ exo_gemm_status_t launch_thin(int width, const Operand& A, const Operand& B, int
   p.nkb = (int32_t)((K + SUB_K - 1) / SUB_K);
   p.width = width;
   p.a_rows = a_rows;
+  const int mma_rows = thin_mma_rows(a_rows);
+  p.quad_rows = mma_rows / 4;
   p.whole = (int32_t)(K / SUB_K);
-  thin_ring(bn, a_rows, p.whole, &p.per_stage, &p.stages);
-  p.idesc = Op::kInt8 ? (2u << 4 | 1u << 7 | 1u << 10 | (uint32_t)(bn >> 3) << 17 | 8u << 24)
-                      : make_idesc(bf16 ? EXO_GEMM_BF16 : EXO_GEMM_FP16, 0, 0, 128, bn);
+  const int64_t tiles = (N + width - 1) / width;
+  thin_ring(bn, a_rows, p.whole, tiles <= sms, &p.per_stage, &p.stages);
+  p.idesc = Op::kInt8 ? (2u << 4 | 1u << 7 | 1u << 10 | (uint32_t)(bn >> 3) << 17 | (uint32_t)(mma_rows >> 4) << 24)
+                      : make_idesc(bf16 ? EXO_GEMM_BF16 : EXO_GEMM_FP16, 0, 0, mma_rows, bn);
   p.a = make_staging(0, kBlockM, 1, 2);
   p.b = make_staging(0, bn, 1, 2);
   CUtensorMap ma, ma_rest, mb, mb_rest;
@@ -202,7 +210,7 @@ exo_gemm_status_t launch_thin(int width, const Operand& A, const Operand& B, int
   p.skip_copies = hook.skip;
   typename Op::Params o = op;
   void* args[6] = {&ma, &ma_rest, &mb, &mb_rest, &p, &o};
-  return launch_args((void*)exo_fused_thin_kernel<Op, U>, dim3((unsigned)((N + width - 1) / width)), kThinThreads,
+  return launch_args((void*)exo_fused_thin_kernel<Op, U>, dim3((unsigned)tiles), kThinThreads,
                      (size_t)thin_smem(p.stages, p.per_stage, bn, a_rows), 1, stream, args);
 }
 
