@@ -451,7 +451,7 @@ exo_gemm_status_t exo_ce_create(exo_ce_handle_t* out, const exo_ce_desc_t* desc)
   p->sms = sms;
   const int64_t T = d.tokens, H = d.hidden, V = d.vocab;
   p->thin = T <= kThinRows;
-  p->width = p->thin ? thin_width(V, 32, 256, 1, T, sms) : pair_bn(T, V, false, sms);
+  p->width = p->thin ? thin_width(V, 32, 256, 1, T, sms) : pair_bn(T, V, false, 64, sms);
   p->parts = (int)((V + p->width - 1) / p->width) * 2;
   p->ldx = d.ldx % 8 ? round_up(H, 64) : d.ldx;
   p->ldw = d.ldw % 8 ? round_up(H, 64) : d.ldw;
@@ -468,7 +468,7 @@ exo_gemm_status_t exo_ce_create(exo_ce_handle_t* out, const exo_ce_desc_t* desc)
       if (p->piece < 256 && !d.piece) p->piece = 256;
       if (p->piece > V - p->keep) p->piece = V - p->keep;
       p->ldd = round_up(p->piece, 64);
-      p->bn_piece = pair_bn(T, p->piece, false, sms);
+      p->bn_piece = pair_bn(T, p->piece, false, 64, sms);
     }
   }
   const int64_t rest = p->piece ? (V - p->keep) % p->piece : 0;

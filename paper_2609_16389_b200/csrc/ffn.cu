@@ -285,8 +285,8 @@ exo_gemm_status_t exo_ffn_create(exo_ffn_handle_t* out, const exo_ffn_desc_t* de
   p->thin = T <= kThinRows;
   p->width_gated = thin_width(F, 8, 128, 2, T, sms);
   p->width_down = thin_width(H, 16, 256, 1, T, sms);
-  p->bn_gated = pair_bn(T, F, true, sms);
-  p->bn_back = pair_bn(T, F, false, sms);
+  p->bn_gated = pair_bn(T, F, true, 64, sms);
+  p->bn_back = pair_bn(T, F, false, 128, sms);
   p->ldh = round_up(F, 64);
   p->ld2 = round_up(2 * F, 64);
   auto packed = [](int64_t ld, int64_t inner) { return ld % 8 ? round_up(inner, 64) : ld; };

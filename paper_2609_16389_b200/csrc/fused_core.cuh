@@ -1,7 +1,7 @@
 // Products whose epilogue is an operator: the two kernels behind exo_fused.h.
 //
-// exo_fused_pair_kernel   persistent, a pair of CTAs (tcgen05 cta_group::2) per tile of 256 rows x BN accumulator columns, two accumulators
-//                         in tensor memory, so that a tile's epilogue runs beside the next tile's main loop
+// exo_fused_pair_kernel   persistent, a pair of CTAs (tcgen05 cta_group::2) per tile of 256 rows x up to 256 accumulator columns, two
+//                         accumulators in tensor memory, so that a tile's epilogue runs beside the next tile's main loop
 // exo_fused_thin_kernel   up to 128 rows (a few tokens): one tile per CTA, two CTAs per SM; what counts is the stream of B's rows
 //
 // The operator is a class `Op`: its epilogue takes a row's accumulator columns in units of U, and for a gated product (Op::kGated) two units
@@ -59,6 +59,7 @@ struct CoreParams {
 };
 
 constexpr int kPairBarrierBytes = 512;
+constexpr int kPairMaxStages = 10;
 constexpr int kThinThreads = 320;    // producer, MMA issuer, eight epilogue warps
 constexpr int kThinMaxStages = 16;
 constexpr int kThinBarrierBytes = 512;
@@ -66,7 +67,7 @@ constexpr int kThinBarrierBytes = 512;
 EXO_CX int pair_stage_bytes(int bn) { return kATileBytes + bn / 2 * 128; }
 EXO_CX int pair_stages(int bn) {
   const int n = (kSmemLimit - 1024 - kPairBarrierBytes) / pair_stage_bytes(bn);
-  return n > kMaxStages ? kMaxStages : n;
+  return n > kPairMaxStages ? kPairMaxStages : n;
 }
 EXO_CX int pair_smem(int bn) { return pair_stages(bn) * pair_stage_bytes(bn) + kPairBarrierBytes + 1024; }
 // The MMAs read 64 or 128 rows of A whatever a stage holds of it: what follows the rows staged becomes accumulator rows that nobody reads, and
@@ -107,6 +108,9 @@ __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, uint64_
 __device__ __forceinline__ uint64_t smem_desc(uint32_t addr, const OperandStaging& op) {
   return ((uint64_t)op.desc_hi << 32) | (((addr & 0x3FFFFu) >> 4) | (op.lbo_enc << 16));
 }
+
+// A barrier that orders nothing: a release would wait for the results' stores, some 0.9 us at a kernel's end.
+__device__ __forceinline__ void cluster_arrive_relaxed() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
 
 // ---------------------------------------------------------------- tensor-core instructions of exo_fused.h only
 template <int CTA_GROUP>
@@ -236,21 +240,21 @@ __device__ __forceinline__ void run_units(const typename Op::Params& o, uint32_t
 // ---------------------------------------------------------------- pairs of CTAs, persistent
 // Roles as in the library's plain product: warps 0 and 10 copy A and B, warp 1 issues the MMAs (CTA 0) and owns tensor memory, warps 2 to 9
 // are the epilogue, two per lane quadrant, each of them half of the tile's columns.
-template <class Op, int BN, bool B_MN>
+template <class Op, int U, bool B_MN>
 __global__ void __launch_bounds__(kNumThreads, 1)
 exo_fused_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b, const __grid_constant__ CoreParams p,
                       const __grid_constant__ typename Op::Params o) {
-  constexpr int B_ROWS = BN / 2, STAGE = pair_stage_bytes(BN), STAGES = pair_stages(BN);
-  constexpr int WIDTH = Op::kGated ? BN / 2 : BN;      // result columns of a tile
   constexpr int SUB_K = Op::kInt8 ? 128 : 64;          // elements of a k-block
-  constexpr uint32_t TMEM_COLS = 2 * BN;
+  constexpr uint32_t TMEM_COLS = 512, ACC = 256;       // columns of both accumulators, and between them
+  const int32_t width = p.width;                       // result columns of a tile
+  const uint32_t b_rows = (uint32_t)(Op::kGated ? width : width / 2), stage_bytes = (uint32_t)kATileBytes + b_rows * 128u, stages = (uint32_t)p.stages;
   extern __shared__ uint8_t smem_raw[];
-  const uint32_t stage0 = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u, bar0 = stage0 + STAGES * STAGE;
+  const uint32_t stage0 = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u, bar0 = stage0 + stages * stage_bytes;
   auto full_bar = [&](uint32_t s) { return bar0 + 8u * s; };
-  auto empty_bar = [&](uint32_t s) { return bar0 + 8u * (kMaxStages + s); };
-  auto tfull_bar = [&](uint32_t a) { return bar0 + 8u * (2 * kMaxStages + a); };
-  auto tempty_bar = [&](uint32_t a) { return bar0 + 8u * (2 * kMaxStages + 2 + a); };
-  const uint32_t tmem_slot = bar0 + 8u * (2 * kMaxStages + 4);
+  auto empty_bar = [&](uint32_t s) { return bar0 + 8u * (kPairMaxStages + s); };
+  auto tfull_bar = [&](uint32_t a) { return bar0 + 8u * (2 * kPairMaxStages + a); };
+  auto tempty_bar = [&](uint32_t a) { return bar0 + 8u * (2 * kPairMaxStages + 2 + a); };
+  const uint32_t tmem_slot = bar0 + 8u * (2 * kPairMaxStages + 4);
   const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
   const uint32_t rank = ptx::cluster_ctarank();
   const int64_t worker = blockIdx.x / 2, workers = gridDim.x / 2, tiles = raster_total(p.raster);
@@ -261,7 +265,7 @@ exo_fused_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
       ptx::prefetch_tensormap(&tm_a);
       ptx::prefetch_tensormap(&tm_b);
     }
-    for (uint32_t i = lane; i < 2u * kMaxStages + 4u; i += 32u) ptx::mbar_init(bar0 + 8u * i, i >= 2u * kMaxStages + 2u ? kEpiWarps * 2 : 1);
+    for (uint32_t i = lane; i < 2u * kPairMaxStages + 4u; i += 32u) ptx::mbar_init(bar0 + 8u * i, i >= 2u * kPairMaxStages + 2u ? kEpiWarps * 2 : 1);
     ptx::fence_mbar_init();
   }
   if (warp == 1) {
@@ -285,30 +289,29 @@ exo_fused_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
     bool skip = p.skip_copies != 0 && blockIdx.x == 0;
     for (int64_t t = worker; t < tiles && ok; t += workers) {
       const TileCoord tc = raster_decode(p.raster, t);
-      const int32_t a0 = tc.m * 256 + (int32_t)rank * 128, b0 = tc.n * WIDTH + (int32_t)rank * p.b_split;
+      const int32_t a0 = tc.m * 256 + (int32_t)rank * 128, b0 = tc.n * width + (int32_t)rank * p.b_split;
       for (int32_t kb = 0; kb < nkb; ++kb) {
         ok = wait_warp(empty_bar(s), ph ^ 1u, p.wait_clocks);
         if (!ok) break;
         if (ptx::elect_one()) {
-          if (rank == 0 && do_a) ptx::mbar_arrive_expect_tx(full_bar(s), STAGE * 2);
-          const uint32_t a_dst = stage0 + s * STAGE, b_dst = a_dst + kATileBytes, bar = full0 + 8u * s;
+          if (rank == 0 && do_a) ptx::mbar_arrive_expect_tx(full_bar(s), stage_bytes * 2);
+          const uint32_t a_dst = stage0 + s * stage_bytes, b_dst = a_dst + kATileBytes, bar = full0 + 8u * s;
           if (skip) {
           } else if (do_a) {
             ptx::tma_load_2d_pair(a_dst, &tm_a, kb * SUB_K, a0, bar);
           } else if constexpr (!B_MN) {
             ptx::tma_load_2d_pair(b_dst, &tm_b, kb * SUB_K, b0, bar);
           } else {
-#pragma unroll
-            for (int b = 0; b < B_ROWS / 64; ++b) ptx::tma_load_2d_pair(b_dst + b * 8192u, &tm_b, b0 + 64 * b, kb * SUB_K, bar);
+            for (uint32_t b = 0; b < b_rows / 64; ++b) ptx::tma_load_2d_pair(b_dst + b * 8192u, &tm_b, b0 + 64 * (int32_t)b, kb * SUB_K, bar);
           }
         }
         skip = false;
-        if (++s == STAGES) { s = 0; ph ^= 1u; }
+        if (++s == stages) { s = 0; ph ^= 1u; }
       }
     }
-    for (uint32_t i = 0; i < STAGES && ok; ++i) {   // no stage release may still be on its way to this CTA
+    for (uint32_t i = 0; i < stages && ok; ++i) {   // no stage release may still be on its way to this CTA
       ok = wait_warp(empty_bar(s), ph ^ 1u, p.wait_clocks);
-      if (++s == STAGES) { s = 0; ph ^= 1u; }
+      if (++s == stages) { s = 0; ph ^= 1u; }
     }
   } else if (warp == 1) {
     if (rank == 0) {
@@ -319,12 +322,12 @@ exo_fused_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
         ok = wait_warp(tempty_bar(acc), acc_ph ^ 1u, p.wait_clocks);   // both CTAs' epilogues have read it
         if (!ok) break;
         ptx::tc_fence_after_sync();
-        const uint32_t d = tmem_base + acc * BN;
+        const uint32_t d = tmem_base + acc * ACC;
         for (int32_t kb = 0; kb < nkb; ++kb) {
           ok = wait_warp(full_bar(s), ph, p.wait_clocks);
           if (!ok) break;
           ptx::tc_fence_after_sync();
-          const uint64_t a_desc = smem_desc(stage0 + s * STAGE, p.a), b_desc = smem_desc(stage0 + s * STAGE + kATileBytes, p.b);
+          const uint64_t a_desc = smem_desc(stage0 + s * stage_bytes, p.a), b_desc = smem_desc(stage0 + s * stage_bytes + kATileBytes, p.b);
           if (ptx::elect_one()) {
 #pragma unroll
             for (uint32_t k = 0; k < 4; ++k)   // 32 bytes of K each
@@ -332,7 +335,7 @@ exo_fused_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
             ptx::umma_commit<2>(empty_bar(s), 3);
             if (kb == nkb - 1) ptx::umma_commit<2>(tfull_bar(acc), 3);
           }
-          if (++s == STAGES) { s = 0; ph ^= 1u; }
+          if (++s == stages) { s = 0; ph ^= 1u; }
         }
         if ((acc ^= 1u) == 0u) acc_ph ^= 1u;
       }
@@ -343,8 +346,7 @@ exo_fused_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
     const uint32_t quad = warp & 3u;
     const int32_t half = (int32_t)((warp - 2u) >> 2);
     const uint32_t tempty0 = ptx::map_to_cta(tempty_bar(0), 0u);
-    constexpr int U = Op::kUnit, UNITS = WIDTH / 2 / U;
-    static_assert(UNITS * U * 2 == WIDTH, "whole units per warp");
+    const int32_t units = width / 2 / U;   // of this warp
     uint32_t acc = 0, acc_ph = 0;
     for (int64_t t = worker; t < tiles; t += workers) {
       const TileCoord tc = raster_decode(p.raster, t);
@@ -352,7 +354,10 @@ exo_fused_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
       ok = wait_warp(tfull_bar(acc), acc_ph, p.wait_clocks);
       if (!ok) break;
       ptx::tc_fence_after_sync();
+      // (Handed back only for a tile to come: an arrival that nobody waits for could reach a CTA that has gone.)
+      const bool wanted = t + 2 * workers < tiles;
       auto release = [&]() {
+        if (!wanted) return;
         ptx::tc_fence_before_sync();
         __syncwarp();
         if (ptx::elect_one()) ptx::mbar_arrive_cluster(tempty0 + 8u * acc);
@@ -360,8 +365,8 @@ exo_fused_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
       if (row0 >= p.M) {
         release();
       } else {
-        const uint32_t tacc = tmem_base + ((quad * 32u) << 16) + acc * BN + (uint32_t)(half * (WIDTH / 2));
-        run_units<Op, U>(o, tacc, (uint32_t)WIDTH, row, row < p.M, tc.n * WIDTH + half * (WIDTH / 2), UNITS, p.N, tc.n * 2 + half, release);
+        const uint32_t tacc = tmem_base + ((quad * 32u) << 16) + acc * ACC + (uint32_t)(half * (width / 2));
+        run_units<Op, U>(o, tacc, (uint32_t)width, row, row < p.M, tc.n * width + half * (width / 2), units, p.N, tc.n * 2 + half, release);
       }
       if ((acc ^= 1u) == 0u) acc_ph ^= 1u;
     }
@@ -371,7 +376,8 @@ exo_fused_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
     for (int i = 0; i < 200; ++i) __nanosleep(1000);   // a wait was abandoned: copies and MMAs in flight land first
   ptx::tc_fence_before_sync();
   __syncthreads();
-  ptx::cluster_arrive();   // the peer's shared and tensor memory stay valid until both CTAs are done
+  // The peer's shared and tensor memory stay valid until both CTAs are done; every arrival and copy that reaches over has been waited for.
+  cluster_arrive_relaxed();
   ptx::cluster_wait();
   if (warp == 1) {
     ptx::tc_fence_after_sync();

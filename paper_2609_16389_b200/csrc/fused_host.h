@@ -128,15 +128,19 @@ inline void thin_ring(int b_rows, int a_rows, int64_t whole, bool alone, int* pe
   *stages = n;
 }
 
-// Columns of a pair's tile: 256 accumulator columns, or 128 where that fills the waves better by more than it costs (a tile of 128 moves a half
-// more operand bytes per product).
-inline int pair_bn(int64_t M, int64_t N, bool gated, int sms) {
+// Accumulator columns of a pair's tile: what fills the waves best, multiples of 64 (128 for a B that lies K x N).  A narrow tile moves more
+// operand bytes per product: 2048 x 12288 x 4096, gated, took 1, 0.79, 0.64 and 0.59 of the time per tile with 256, 192, 128 and 64 columns; 30
+// stands for a tile's start and end.
+inline int pair_bn(int64_t M, int64_t N, bool gated, int multiple, int sms) {
   const int pairs = sms / 2;
-  auto cost = [&](int bn, double each) {
-    const int64_t w = gated ? bn / 2 : bn, tiles = ((M + 255) / 256) * ((N + w - 1) / w);
-    return (double)((tiles + pairs - 1) / pairs) * bn * each;
-  };
-  return cost(128, 1.15) < cost(256, 1.0) ? 128 : 256;
+  int best = 256;
+  int64_t cost = -1;
+  for (int bn = 256; bn >= multiple; bn -= multiple) {
+    const int64_t w = gated ? bn / 2 : bn, tiles = ((M + 255) / 256) * ((N + w - 1) / w), waves = (tiles + pairs - 1) / pairs;
+    const int64_t c = waves * (30 + (bn == 256 ? 256 : bn == 192 ? 203 : bn == 128 ? 165 : 152));
+    if (cost < 0 || c < cost) { cost = c; best = bn; }
+  }
+  return best;
 }
 
 struct Operand {
@@ -155,6 +159,7 @@ exo_gemm_status_t launch_pair(int bn, const Operand& A, const Operand& B, int64_
   p.N = (int32_t)N;
   p.nkb = (int32_t)((K + SUB_K - 1) / SUB_K);
   p.width = width;
+  p.stages = pair_stages(bn);
   p.b_split = (int32_t)(Op::kGated ? b_split : bn / 2);
   p.idesc = Op::kInt8 ? (2u << 4 | 1u << 7 | 1u << 10 | (uint32_t)(bn >> 3) << 17 | 16u << 24)   // signed bytes, 32-bit integer sums
                       : make_idesc(bf16 ? EXO_GEMM_BF16 : EXO_GEMM_FP16, 0, B_MN ? 1 : 0, 256, bn);
@@ -175,7 +180,8 @@ exo_gemm_status_t launch_pair(int bn, const Operand& A, const Operand& B, int64_
   const int64_t pairs = tiles < sms / 2 ? tiles : sms / 2;
   typename Op::Params o = op;
   void* args[4] = {&ma, &mb, &p, &o};
-  void* fn = bn == 256 ? (void*)exo_fused_pair_kernel<Op, 256, B_MN> : (void*)exo_fused_pair_kernel<Op, 128, B_MN>;
+  // units of the operator's own size where a warp's half of the tile is whole ones, else of 16 columns
+  void* fn = width / 2 % Op::kUnit == 0 ? (void*)exo_fused_pair_kernel<Op, Op::kUnit, B_MN> : (void*)exo_fused_pair_kernel<Op, 16, B_MN>;
   return launch_args(fn, dim3((unsigned)(2 * pairs)), kNumThreads, (size_t)pair_smem(bn), 2, stream, args);
 }
 

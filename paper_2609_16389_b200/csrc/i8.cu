@@ -337,7 +337,7 @@ exo_gemm_status_t exo_gemm_i8_run(const exo_i8_t* X, const exo_i8_t* W, void* Y,
   I8Op::Params o{X->scales, W->scales, Y, ldy, y_dtype, align_of(Y, ldy * bytes), alpha, beta};
   const Operand A{X->codes, M, K, X->ld}, B{W->codes, N, K, W->ld};
   if (M <= kThinRows) return launch_thin<I8Op, 16>(thin_width(N, 16, 256, 1, M, sms), A, B, N, K, 0, false, sms, o, stream);
-  return launch_pair<I8Op, false>(pair_bn(M, N, false, sms), A, B, N, K, 0, false, sms, o, stream);
+  return launch_pair<I8Op, false>(pair_bn(M, N, false, 64, sms), A, B, N, K, 0, false, sms, o, stream);
 }
 
 }  // extern "C"
