@@ -33,11 +33,13 @@ struct StatsOp {
     int32_t keep;             // columns kept
     int32_t rows, vocab;
   };
+  template <int U>
   struct State {
     float top, sum, all;
     int32_t target;
   };
-  static __device__ __forceinline__ void begin(const Params& o, State& s, int row, bool row_ok) {
+  template <int U>
+  static __device__ __forceinline__ void begin(const Params& o, State<U>& s, int row, bool row_ok, int, int) {
     s.top = -INFINITY;
     s.sum = s.all = 0.f;
     s.target = -1;
@@ -47,7 +49,7 @@ struct StatsOp {
     }
   }
   template <int U>
-  static __device__ __forceinline__ void look(const Params&, State& s, uint32_t (&v)[U], int n) {
+  static __device__ __forceinline__ void look(const Params&, State<U>& s, uint32_t (&v)[U], int n) {
     float top[4] = {s.top, s.top, s.top, s.top};
     if (n >= U) {
 #pragma unroll
@@ -59,9 +61,8 @@ struct StatsOp {
     }
     s.top = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
   }
-  static __device__ __forceinline__ void looked(State&) {}
   template <int U>
-  static __device__ __forceinline__ void unit(const Params& o, State& s, uint32_t (&v)[U], uint32_t (&)[1], int row, bool row_ok, int col, int n) {
+  static __device__ __forceinline__ void unit(const Params& o, State<U>& s, uint32_t (&v)[U], uint32_t (&)[1], int row, bool row_ok, int col, int n, bool) {
     const float top = s.top == -INFINITY ? 0.f : s.top;   // a part without a finite logit: exponentials of -inf, or NaN, as they are
     float e[U];
     if (n >= U) {
@@ -92,7 +93,8 @@ struct StatsOp {
     }
     if (o.e && col < o.keep && row_ok) store16<T, U>(o.e + (int64_t)row * o.lde + col, e, U, U >= 32 ? 32 : 16);
   }
-  static __device__ __forceinline__ void end(const Params& o, State& s, int row, bool row_ok, int part) {
+  template <int U>
+  static __device__ __forceinline__ void end(const Params& o, State<U>& s, int row, bool row_ok, int part) {
     if (!row_ok) return;
     const int64_t at = (int64_t)part * o.rows + row;
     o.top[at] = s.top;
@@ -114,17 +116,19 @@ struct GradOp {
     int64_t first;            // the piece's first column of the vocabulary
     float hot, rest;          // what the target's column loses, and every column: 1 - s and s / vocab
   };
+  template <int U>
   struct State {
     float lse, q;
     int64_t target;
   };
-  static __device__ __forceinline__ void begin(const Params& o, State& s, int row, bool row_ok) {
+  template <int U>
+  static __device__ __forceinline__ void begin(const Params& o, State<U>& s, int row, bool row_ok, int, int) {
     s.lse = row_ok ? o.lse[row] : 0.f;
     s.q = row_ok ? o.q[row] : 0.f;
     s.target = row_ok ? o.target[row] - o.first : -1;
   }
   template <int U>
-  static __device__ __forceinline__ void unit(const Params& o, State& s, uint32_t (&v)[U], uint32_t (&)[1], int row, bool row_ok, int col, int) {
+  static __device__ __forceinline__ void unit(const Params& o, State<U>& s, uint32_t (&v)[U], uint32_t (&)[1], int row, bool row_ok, int col, int, bool) {
     if (!row_ok) return;
     float d[U];
     const int64_t t = s.target - col;
@@ -135,7 +139,8 @@ struct GradOp {
     }
     store16<T, U>(o.d + (int64_t)row * o.ldd + col, d, U, 32);
   }
-  static __device__ __forceinline__ void end(const Params&, State&, int, bool, int) {}
+  template <int U>
+  static __device__ __forceinline__ void end(const Params&, State<U>&, int, bool, int) {}
 };
 
 // ---------------------------------------------------------------- rows from their parts

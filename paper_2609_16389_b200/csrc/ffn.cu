@@ -54,8 +54,10 @@ struct GatedOp {
     int64_t ld;
     int32_t act;
   };
+  template <int U>
   struct State {};
-  static __device__ __forceinline__ void begin(const Params&, State&, int, bool) {}
+  template <int U>
+  static __device__ __forceinline__ void begin(const Params&, State<U>&, int, bool, int, int) {}
   template <int ACT, int U>
   static __device__ __forceinline__ void product(const float (&g)[U], const float (&u)[U], float (&h)[U]) {
 #pragma unroll
@@ -66,7 +68,7 @@ struct GatedOp {
     }
   }
   template <int U>
-  static __device__ __forceinline__ void unit(const Params& o, State&, uint32_t (&v)[U], uint32_t (&v2)[U], int row, bool row_ok, int col, int) {
+  static __device__ __forceinline__ void unit(const Params& o, State<U>&, uint32_t (&v)[U], uint32_t (&v2)[U], int row, bool row_ok, int col, int, bool) {
     if (!row_ok) return;
     float g[U], u[U], h[U];
 #pragma unroll
@@ -82,7 +84,8 @@ struct GatedOp {
       store16<T, U>(o.u + at, u, U, align);
     }
   }
-  static __device__ __forceinline__ void end(const Params&, State&, int, bool, int) {}
+  template <int U>
+  static __device__ __forceinline__ void end(const Params&, State<U>&, int, bool, int) {}
 };
 
 // ---------------------------------------------------------------- dg, du and h from dh, g and u
@@ -99,8 +102,22 @@ struct GatedBackOp {
     int32_t inner, act;
     int32_t du_align;    // what divides the address of du's units
   };
-  struct State {};
-  static __device__ __forceinline__ void begin(const Params&, State&, int, bool) {}
+  template <int U>
+  struct State {
+    uint32_t g[U / 2], u[U / 2];   // of the next unit, fetched a unit's time ahead
+  };
+  template <int U>
+  static __device__ __forceinline__ void fetch(const Params& o, State<U>& s, int64_t at) {
+#pragma unroll
+    for (int j = 0; j < U / 8; ++j) {
+      ptx::ld_global_cg_v4(o.g + at + 8 * j, s.g[4 * j], s.g[4 * j + 1], s.g[4 * j + 2], s.g[4 * j + 3]);
+      ptx::ld_global_cg_v4(o.u + at + 8 * j, s.u[4 * j], s.u[4 * j + 1], s.u[4 * j + 2], s.u[4 * j + 3]);
+    }
+  }
+  template <int U>
+  static __device__ __forceinline__ void begin(const Params& o, State<U>& s, int row, bool row_ok, int col, int N) {
+    if (row_ok && col < N) fetch<U>(o, s, (int64_t)row * o.ld + col);
+  }
   template <int ACT, int U>
   static __device__ __forceinline__ void chain(const uint32_t (&v)[U], const uint32_t (&g)[U / 2], const uint32_t (&u)[U / 2], float (&dg)[U], float (&du)[U],
                                                float (&h)[U]) {
@@ -119,15 +136,13 @@ struct GatedBackOp {
     }
   }
   template <int U>
-  static __device__ __forceinline__ void unit(const Params& o, State&, uint32_t (&v)[U], uint32_t (&)[1], int row, bool row_ok, int col, int n) {
+  static __device__ __forceinline__ void unit(const Params& o, State<U>& s, uint32_t (&v)[U], uint32_t (&)[1], int row, bool row_ok, int col, int n, bool more) {
     if (!row_ok) return;
     const int64_t at = (int64_t)row * o.ld + col;
     uint32_t g[U / 2], u[U / 2];
 #pragma unroll
-    for (int j = 0; j < U / 8; ++j) {
-      ptx::ld_global_cg_v4(o.g + at + 8 * j, g[4 * j], g[4 * j + 1], g[4 * j + 2], g[4 * j + 3]);
-      ptx::ld_global_cg_v4(o.u + at + 8 * j, u[4 * j], u[4 * j + 1], u[4 * j + 2], u[4 * j + 3]);
-    }
+    for (int j = 0; j < U / 2; ++j) { g[j] = s.g[j]; u[j] = s.u[j]; }
+    if (more) fetch<U>(o, s, at + U);
     float dg[U], du[U], h[U];
     if (o.act == EXO_ACT_SILU) chain<EXO_ACT_SILU, U>(v, g, u, dg, du, h);
     else if (o.act == EXO_ACT_GELU) chain<EXO_ACT_GELU, U>(v, g, u, dg, du, h);
@@ -137,7 +152,8 @@ struct GatedBackOp {
     store16<T, U>(d, dg, n, 32);               // (not beyond `inner`: du begins there)
     store16<T, U>(d + o.inner, du, n, o.du_align);
   }
-  static __device__ __forceinline__ void end(const Params&, State&, int, bool, int) {}
+  template <int U>
+  static __device__ __forceinline__ void end(const Params&, State<U>&, int, bool, int) {}
 };
 
 // ---------------------------------------------------------------- y, for a few rows
@@ -149,17 +165,20 @@ struct PlainOp {
     int64_t ld;
     int32_t align;
   };
-  struct State {};
-  static __device__ __forceinline__ void begin(const Params&, State&, int, bool) {}
   template <int U>
-  static __device__ __forceinline__ void unit(const Params& o, State&, uint32_t (&v)[U], uint32_t (&)[1], int row, bool row_ok, int col, int n) {
+  struct State {};
+  template <int U>
+  static __device__ __forceinline__ void begin(const Params&, State<U>&, int, bool, int, int) {}
+  template <int U>
+  static __device__ __forceinline__ void unit(const Params& o, State<U>&, uint32_t (&v)[U], uint32_t (&)[1], int row, bool row_ok, int col, int n, bool) {
     if (!row_ok) return;
     float y[U];
 #pragma unroll
     for (int k = 0; k < U; ++k) y[k] = __uint_as_float(v[k]);
     store16<T, U>(o.y + (int64_t)row * o.ld + col, y, n, o.align);
   }
-  static __device__ __forceinline__ void end(const Params&, State&, int, bool, int) {}
+  template <int U>
+  static __device__ __forceinline__ void end(const Params&, State<U>&, int, bool, int) {}
 };
 
 }  // namespace

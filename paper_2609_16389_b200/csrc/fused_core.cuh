@@ -206,13 +206,12 @@ __device__ __forceinline__ void store32(void* at, const float (&v)[U], int n, in
 
 // ---------------------------------------------------------------- the epilogue of one warp: 32 rows, `units` units of U columns
 // tacc: the warp's lanes of the accumulator, at its first unit's column; release() hands the accumulator back after the last read.
+// s: what Op::begin has fetched for the row and the first unit, before the accumulator was complete; a unit fetches for the next one.
 template <class Op, int U, class Release>
-__device__ __forceinline__ void run_units(const typename Op::Params& o, uint32_t tacc, uint32_t gap, int row, bool row_ok, int col, int units, int N,
-                                          int part, const Release& release) {
+__device__ __forceinline__ void run_units(const typename Op::Params& o, typename Op::template State<U>& s, uint32_t tacc, uint32_t gap, int row, bool row_ok, int col,
+                                          int units, int N, int part, const Release& release) {
   const int left = N > col ? (N - col + U - 1) / U : 0;
   if (units > left) units = left;
-  typename Op::State s;
-  Op::begin(o, s, row, row_ok);
   if constexpr (Op::kTwice) {   // a first look at the columns
 #pragma unroll 1
     for (int i = 0; i < units; ++i) {
@@ -221,7 +220,6 @@ __device__ __forceinline__ void run_units(const typename Op::Params& o, uint32_t
       ptx::tmem_ld_wait();
       Op::template look<U>(o, s, v, N - col - i * U);
     }
-    Op::looked(s);
   }
   if (units == 0) release();
 #pragma unroll 1
@@ -232,7 +230,7 @@ __device__ __forceinline__ void run_units(const typename Op::Params& o, uint32_t
     ptx::tmem_ld_wait();
     if (i + 1 == units) release();
     const int n = N - col - i * U;
-    Op::template unit<U>(o, s, v, v2, row, row_ok, col + i * U, n < U ? n : U);
+    Op::template unit<U>(o, s, v, v2, row, row_ok, col + i * U, n < U ? n : U, i + 1 < units);
   }
   Op::end(o, s, row, row_ok, part);
 }
@@ -351,6 +349,9 @@ exo_fused_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
     for (int64_t t = worker; t < tiles; t += workers) {
       const TileCoord tc = raster_decode(p.raster, t);
       const int32_t row0 = tc.m * 256 + (int32_t)rank * 128 + (int32_t)quad * 32, row = row0 + (int32_t)lane;
+      const int32_t col = tc.n * width + half * (width / 2);
+      typename Op::template State<U> state;
+      Op::template begin<U>(o, state, row, row < p.M, col, p.N);
       ok = wait_warp(tfull_bar(acc), acc_ph, p.wait_clocks);
       if (!ok) break;
       ptx::tc_fence_after_sync();
@@ -366,7 +367,7 @@ exo_fused_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
         release();
       } else {
         const uint32_t tacc = tmem_base + ((quad * 32u) << 16) + acc * ACC + (uint32_t)(half * (width / 2));
-        run_units<Op, U>(o, tacc, (uint32_t)width, row, row < p.M, tc.n * width + half * (width / 2), units, p.N, tc.n * 2 + half, release);
+        run_units<Op, U>(o, state, tacc, (uint32_t)width, row, row < p.M, col, units, p.N, tc.n * 2 + half, release);
       }
       if ((acc ^= 1u) == 0u) acc_ph ^= 1u;
     }
@@ -478,18 +479,19 @@ exo_fused_thin_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
     }
     ok = ok && wait_warp(tfull_bar, 0u, p.wait_clocks);
   }
-  // The epilogue's warps wait here, where they take no issue slots: polling for the accumulator they would slow the loops above down by half.
-  const bool all_ok = __syncthreads_and(ok) != 0;
-  if (warp >= 2 && all_ok) {
+  const uint32_t quad = warp & 3u;
+  const int32_t half = (int32_t)((warp - 2u) >> 2), row0 = (int32_t)quad * p.quad_rows, row = row0 + (int32_t)lane;
+  const int32_t all = (int32_t)width / U, skipped = half ? (all + 1) / 2 : 0, mine = half ? all / 2 : (all + 1) / 2, col = col0 + skipped * U;
+  const bool row_ok = (int32_t)lane < p.quad_rows && row < p.M;
+  typename Op::template State<U> state;
+  if (warp >= 2) {
     ptx::grid_dependency_wait();
-    const uint32_t quad = warp & 3u;
-    const int32_t half = (int32_t)((warp - 2u) >> 2), row0 = (int32_t)quad * p.quad_rows, row = row0 + (int32_t)lane;
-    if (row0 < p.M) {
-      ptx::tc_fence_after_sync();
-      const int32_t units = (int32_t)width / U, first = half ? (units + 1) / 2 : 0, mine = half ? units / 2 : (units + 1) / 2;
-      const uint32_t tacc = tmem_base + ((quad * 32u) << 16) + (uint32_t)(first * U);
-      run_units<Op, U>(o, tacc, width, row, (int32_t)lane < p.quad_rows && row < p.M, col0 + first * U, mine, p.N, (int)blockIdx.x * 2 + half, [] {});
-    }
+    Op::template begin<U>(o, state, row, row_ok, col, p.N);
+  }
+  const bool all_ok = __syncthreads_and(ok) != 0;   // the epilogue's warps wait here for the accumulator, taking no issue slots
+  if (warp >= 2 && all_ok && row0 < p.M) {
+    ptx::tc_fence_after_sync();
+    run_units<Op, U>(o, state, tmem_base + ((quad * 32u) << 16) + (uint32_t)(skipped * U), width, row, row_ok, col, mine, p.N, (int)blockIdx.x * 2 + half, [] {});
   }
   if (!ok)
     for (int i = 0; i < 200; ++i) __nanosleep(1000);

@@ -137,21 +137,30 @@ struct I8Op {
     const float *xs, *ws;
     void* y;
     int64_t ldy;
-    int32_t y_dtype, align;   // align: what divides the address of every unit
+    int32_t cols, y_dtype, align;   // align: what divides the address of every unit
     float alpha, beta;
   };
-  struct State {
-    float xs;
-  };
-  static __device__ __forceinline__ void begin(const Params& o, State& s, int row, bool row_ok) { s.xs = row_ok ? __ldcg(o.xs + row) : 0.f; }
   template <int U>
-  static __device__ __forceinline__ void unit(const Params& o, State& s, uint32_t (&v)[U], uint32_t (&)[1], int row, bool row_ok, int col, int n) {
+  struct State {
+    float xs, ws;   // of the row; of column `lane` of the next unit
+  };
+  template <int U>
+  static __device__ __forceinline__ float scale_of(const Params& o, int col, int N) {
+    const int k = (int)ptx::lane_id();
+    return k < U && col + k < N ? __ldcg(o.ws + col + k) : 0.f;
+  }
+  template <int U>
+  static __device__ __forceinline__ void begin(const Params& o, State<U>& s, int row, bool row_ok, int col, int N) {
+    s.xs = row_ok ? __ldcg(o.xs + row) : 0.f;
+    s.ws = scale_of<U>(o, col, N);
+  }
+  template <int U>
+  static __device__ __forceinline__ void unit(const Params& o, State<U>& s, uint32_t (&v)[U], uint32_t (&)[1], int row, bool row_ok, int col, int n, bool more) {
     float y[U];
+    const float ws = s.ws;
+    if (more) s.ws = scale_of<U>(o, col + U, o.cols);
 #pragma unroll
-    for (int k = 0; k < U; ++k) {
-      const float w = k < n ? __ldcg(o.ws + col + k) : 0.f;   // one address for the whole warp
-      y[k] = (float)(int32_t)v[k] * s.xs * w * o.alpha;
-    }
+    for (int k = 0; k < U; ++k) y[k] = (float)(int32_t)v[k] * s.xs * __shfl_sync(0xffffffffu, ws, k) * o.alpha;
     if (!row_ok) return;
     const int64_t at = (int64_t)row * o.ldy + col;
     if (o.y_dtype == EXO_GEMM_FP32) {
@@ -173,7 +182,8 @@ struct I8Op {
     if (o.y_dtype == EXO_GEMM_BF16) store16<Bf16, U>(c, y, n, o.align);
     else store16<Fp16, U>(c, y, n, o.align);
   }
-  static __device__ __forceinline__ void end(const Params&, State&, int, bool, int) {}
+  template <int U>
+  static __device__ __forceinline__ void end(const Params&, State<U>&, int, bool, int) {}
 };
 
 // Y = beta * Y, where there are no products
@@ -334,7 +344,7 @@ exo_gemm_status_t exo_gemm_i8_run(const exo_i8_t* X, const exo_i8_t* W, void* Y,
     void* args[1] = {&p};
     return launch_args((void*)exo_i8_scale_kernel, dim3((unsigned)(ctas < 16 * sms ? ctas : 16 * sms)), kScaleYThreads, 0, 1, stream, args);
   }
-  I8Op::Params o{X->scales, W->scales, Y, ldy, y_dtype, align_of(Y, ldy * bytes), alpha, beta};
+  I8Op::Params o{X->scales, W->scales, Y, ldy, (int32_t)N, y_dtype, align_of(Y, ldy * bytes), alpha, beta};
   const Operand A{X->codes, M, K, X->ld}, B{W->codes, N, K, W->ld};
   if (M <= kThinRows) return launch_thin<I8Op, 16>(thin_width(N, 16, 256, 1, M, sms), A, B, N, K, 0, false, sms, o, stream);
   return launch_pair<I8Op, false>(pair_bn(M, N, false, 64, sms), A, B, N, K, 0, false, sms, o, stream);
