@@ -253,6 +253,20 @@ bool encode_operand_map(CUtensorMap* map, int elem_bytes, bool bf16, const void*
   return r == CUDA_SUCCESS;
 }
 
+// A result of 16-bit values that is stored in boxes of 32 x 32, their rows of 64 bytes swizzled (fused_host.h).
+bool encode_result_map(CUtensorMap* map, void* base, uint64_t cols, uint64_t rows, uint64_t row_bytes) {
+  EncodeTiledFn fn = get_encode_fn();
+  cuuint64_t dims[2] = {cols, rows};
+  cuuint64_t strides[1] = {row_bytes};
+  cuuint32_t box[2] = {32, 32};
+  cuuint32_t estr[2] = {1, 1};
+  const CUresult r = !fn ? CUDA_ERROR_NOT_FOUND
+                         : fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 2, base, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                              CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) g_last_cuda_error = (int)r;
+  return r == CUDA_SUCCESS;
+}
+
 // The whole 128-byte k-blocks of a tensor-core operand's rows (fused_host.h) as (value of a block, row, part, block), `parts` matrices
 // `part_bytes` apart: a copy lands block by block, each of `box_rows` rows of every part.  And what follows the last whole block, as (value,
 // row, part).

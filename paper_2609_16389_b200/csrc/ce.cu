@@ -23,7 +23,7 @@ constexpr float kTop = 16384.f;   // what the largest |dloss| becomes in q: |d| 
 template <class T>
 struct StatsOp {
   static constexpr bool kInt8 = false, kGated = false, kTwice = true;
-  static constexpr int kUnit = 32;   // columns at a time, by pairs
+  static constexpr int kUnit = 32, kBuffers = 2;   // by pairs
   struct Params {
     float *top, *sum, *all;   // [part][row]: largest logit, sum of exponentials, sum of logits (NULL: not wanted)
     float* hit;               // [row]: the target's logit
@@ -61,8 +61,8 @@ struct StatsOp {
     }
     s.top = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
   }
-  template <int U>
-  static __device__ __forceinline__ void unit(const Params& o, State<U>& s, uint32_t (&v)[U], uint32_t (&)[1], int row, bool row_ok, int col, int n, bool) {
+  template <int U, class OutT>
+  static __device__ __forceinline__ void unit(const Params& o, State<U>& s, OutT& out, uint32_t (&v)[U], uint32_t (&)[1], int row, bool row_ok, int col, int n, bool) {
     const float top = s.top == -INFINITY ? 0.f : s.top;   // a part without a finite logit: exponentials of -inf, or NaN, as they are
     float e[U];
     if (n >= U) {
@@ -91,7 +91,15 @@ struct StatsOp {
         if (k == t) l = __uint_as_float(v[k]);
       o.hit[row] = l;   // one thread in all has this column
     }
-    if (o.e && col < o.keep && row_ok) store16<T, U>(o.e + (int64_t)row * o.lde + col, e, U, U >= 32 ? 32 : 16);
+    if (o.e && col < o.keep) {
+      if constexpr (U == 32) {
+        uint32_t w[16];
+        pack<T, U>(e, w);
+        out.put(0, col, w);
+      } else if (row_ok) {
+        store16<T, U>(o.e + (int64_t)row * o.lde + col, e, U, 16);
+      }
+    }
   }
   template <int U>
   static __device__ __forceinline__ void end(const Params& o, State<U>& s, int row, bool row_ok, int part) {
@@ -107,12 +115,10 @@ struct StatsOp {
 template <class T>
 struct GradOp {
   static constexpr bool kInt8 = false, kGated = false, kTwice = false;
-  static constexpr int kUnit = 32;   // columns at a time, by pairs
+  static constexpr int kUnit = 32, kBuffers = 2;   // by pairs
   struct Params {
     const float *lse, *q;     // [row]; q: dloss scaled, 0 for an ignored row
     const int64_t* target;
-    uint16_t* d;              // rows of ldd values, ldd a multiple of 64: whole units can be written
-    int64_t ldd;
     int64_t first;            // the piece's first column of the vocabulary
     float hot, rest;          // what the target's column loses, and every column: 1 - s and s / vocab
   };
@@ -127,9 +133,8 @@ struct GradOp {
     s.q = row_ok ? o.q[row] : 0.f;
     s.target = row_ok ? o.target[row] - o.first : -1;
   }
-  template <int U>
-  static __device__ __forceinline__ void unit(const Params& o, State<U>& s, uint32_t (&v)[U], uint32_t (&)[1], int row, bool row_ok, int col, int, bool) {
-    if (!row_ok) return;
+  template <int U, class OutT>
+  static __device__ __forceinline__ void unit(const Params& o, State<U>& s, OutT& out, uint32_t (&v)[U], uint32_t (&)[1], int row, bool row_ok, int col, int, bool) {
     float d[U];
     const int64_t t = s.target - col;
 #pragma unroll
@@ -137,7 +142,9 @@ struct GradOp {
       const float p = __expf(__uint_as_float(v[k]) - s.lse) - o.rest - (t == k ? o.hot : 0.f);
       d[k] = s.q == 0.f ? 0.f : s.q * p;   // (an ignored row's logits may be anything)
     }
-    store16<T, U>(o.d + (int64_t)row * o.ldd + col, d, U, 32);
+    uint32_t w[U / 2];
+    pack<T, U>(d, w);
+    out.put(0, col, w);
   }
   template <int U>
   static __device__ __forceinline__ void end(const Params&, State<U>&, int, bool, int) {}
@@ -392,8 +399,9 @@ exo_gemm_status_t forward(exo_ce_plan* p, const void* x, const void* W, const in
   o.vocab = (int32_t)d.vocab;
   const Operand X{x, d.tokens, d.hidden, p->ldx}, Wo{W, d.vocab, d.hidden, p->ldw};
   const bool bf16 = d.dtype == EXO_GEMM_BF16;
-  return p->thin ? launch_thin<StatsOp<T>, 16>(p->width, X, Wo, d.vocab, d.hidden, 0, bf16, p->sms, o, stream)
-                 : launch_pair<StatsOp<T>, false>(p->width, X, Wo, d.vocab, d.hidden, 0, bf16, p->sms, o, stream);
+  if (p->thin) return launch_thin<StatsOp<T>, 16>(p->width, X, Wo, d.vocab, d.hidden, 0, bf16, p->sms, o, stream);
+  return saved ? launch_pair<StatsOp<T>, false>(p->width, X, Wo, d.vocab, d.hidden, 0, bf16, p->sms, o, {Result{saved, p->lde, p->lde}}, stream)
+               : launch_pair<StatsOp<T>, false>(p->width, X, Wo, d.vocab, d.hidden, 0, bf16, p->sms, o, {}, stream);
 }
 
 template <class T>
@@ -401,11 +409,12 @@ exo_gemm_status_t recompute(exo_ce_plan* p, const void* x, const void* W, const 
                             cudaStream_t stream) {
   const exo_ce_desc_t& d = p->d;
   typename GradOp<T>::Params o{};
-  o.lse = lse; o.q = p->q; o.target = target; o.d = p->pieces; o.ldd = p->ldd; o.first = first;
+  o.lse = lse; o.q = p->q; o.target = target; o.first = first;
   o.hot = 1.f - d.label_smoothing;
   o.rest = d.label_smoothing / (float)d.vocab;
   const Operand Wo{(const uint16_t*)W + first * p->ldw, columns, d.hidden, p->ldw};
-  return launch_pair<GradOp<T>, false>(p->bn_piece, Operand{x, d.tokens, d.hidden, p->ldx}, Wo, columns, d.hidden, 0, d.dtype == EXO_GEMM_BF16, p->sms, o, stream);
+  return launch_pair<GradOp<T>, false>(p->bn_piece, Operand{x, d.tokens, d.hidden, p->ldx}, Wo, columns, d.hidden, 0, d.dtype == EXO_GEMM_BF16, p->sms, o,
+                                       {Result{p->pieces, p->ldd, p->ldd}}, stream);
 }
 
 exo_gemm_status_t products(exo_ce_plan* p, int which, int64_t columns, int64_t ldd, bool several) {

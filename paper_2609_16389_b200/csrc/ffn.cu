@@ -27,8 +27,19 @@ __device__ __forceinline__ void activate(float g, float& a, float& slope) {
     a = g * s;
     if constexpr (GRAD) slope = s * fmaf(g, 1.f - s, 1.f);
   } else if constexpr (ACT == EXO_ACT_GELU) {
-    // Phi by erfc: 1 + erf would lose the digits of the left tail
-    const float phi = 0.5f * erfcf(-0.70710678118654752f * g);
+    // Phi by erfc: 1 + erf would lose the digits of the left tail.  erfc is the Chebyshev fit of Press et al., Numerical Recipes in C, section 6.2,
+    // good to 1.2e-7 of the value everywhere: a third of the instructions of erfcf, which bound the backward pass's epilogue.
+    const float z = 0.70710678118654752f * fabsf(g), t = __fdividef(1.f, fmaf(0.5f, z, 1.f));
+    float e = fmaf(t, 0.17087277f, -0.82215223f);
+    e = fmaf(t, e, 1.48851587f);
+    e = fmaf(t, e, -1.13520398f);
+    e = fmaf(t, e, 0.27886807f);
+    e = fmaf(t, e, -0.18628806f);
+    e = fmaf(t, e, 0.09678418f);
+    e = fmaf(t, e, 0.37409196f);
+    e = fmaf(t, e, 1.00002368f);
+    e = fmaf(t, e, -1.26551223f);
+    const float tail = 0.5f * t * __expf(fmaf(-z, z, e)), phi = g < 0.f ? tail : 1.f - tail;
     a = g * phi;
     if constexpr (GRAD) slope = fmaf(g * 0.39894228040143268f, __expf(-0.5f * g * g), phi);
   } else {
@@ -48,7 +59,7 @@ __device__ __forceinline__ void activate(float g, float& a, float& slope) {
 template <class T>
 struct GatedOp {
   static constexpr bool kInt8 = false, kGated = true, kTwice = false;
-  static constexpr int kUnit = 32;   // columns at a time, by pairs
+  static constexpr int kUnit = 32, kBuffers = 2;   // by pairs
   struct Params {
     uint16_t *h, *g, *u;   // rows of ld values, ld a multiple of 64: whole units can be written; g and u may be NULL
     int64_t ld;
@@ -67,21 +78,32 @@ struct GatedOp {
       h[k] = a * u[k];
     }
   }
-  template <int U>
-  static __device__ __forceinline__ void unit(const Params& o, State<U>&, uint32_t (&v)[U], uint32_t (&v2)[U], int row, bool row_ok, int col, int, bool) {
-    if (!row_ok) return;
+  template <int U, class OutT>
+  static __device__ __forceinline__ void unit(const Params& o, State<U>&, OutT& out, uint32_t (&v)[U], uint32_t (&v2)[U], int row, bool row_ok, int col, int, bool) {
+    if (U < 32 && !row_ok) return;   // (a TMA store takes the whole warp, and leaves out the rows that do not exist)
     float g[U], u[U], h[U];
 #pragma unroll
     for (int k = 0; k < U; ++k) { g[k] = __uint_as_float(v[k]); u[k] = __uint_as_float(v2[k]); }
     if (o.act == EXO_ACT_SILU) product<EXO_ACT_SILU, U>(g, u, h);
     else if (o.act == EXO_ACT_GELU) product<EXO_ACT_GELU, U>(g, u, h);
     else product<EXO_ACT_GELU_TANH, U>(g, u, h);
-    const int64_t at = (int64_t)row * o.ld + col;
-    constexpr int align = U >= 16 ? 32 : 16;
-    store16<T, U>(o.h + at, h, U, align);
-    if (o.g) {
-      store16<T, U>(o.g + at, g, U, align);
-      store16<T, U>(o.u + at, u, U, align);
+    if constexpr (U == 32) {
+      uint32_t w[16];
+      pack<T, U>(h, w);
+      out.put(0, col, w);
+      if (o.g) {
+        pack<T, U>(g, w);
+        out.put(1, col, w);
+        pack<T, U>(u, w);
+        out.put(2, col, w);
+      }
+    } else {
+      const int64_t at = (int64_t)row * o.ld + col;
+      store16<T, U>(o.h + at, h, U, 16);
+      if (o.g) {
+        store16<T, U>(o.g + at, g, U, 16);
+        store16<T, U>(o.u + at, u, U, 16);
+      }
     }
   }
   template <int U>
@@ -92,7 +114,7 @@ struct GatedOp {
 template <class T>
 struct GatedBackOp {
   static constexpr bool kInt8 = false, kGated = false, kTwice = false;
-  static constexpr int kUnit = 16;   // columns at a time, by pairs: dh, g, u and three results of 32 do not fit the registers
+  static constexpr int kUnit = 16, kBuffers = 3;   // by pairs; 32 columns at a time are more code than a small product's one tile hides the fetching of
   struct Params {
     const uint16_t *g, *u;
     uint16_t* h;
@@ -100,6 +122,7 @@ struct GatedBackOp {
     uint16_t* dgu;       // rows of ld2 values: dg, then du from value `inner` on
     int64_t ld2;
     int32_t inner, act;
+    int32_t aligned;     // dg and du are stored by TMA
     int32_t du_align;    // what divides the address of du's units
   };
   template <int U>
@@ -119,38 +142,43 @@ struct GatedBackOp {
     if (row_ok && col < N) fetch<U>(o, s, (int64_t)row * o.ld + col);
   }
   template <int ACT, int U>
-  static __device__ __forceinline__ void chain(const uint32_t (&v)[U], const uint32_t (&g)[U / 2], const uint32_t (&u)[U / 2], float (&dg)[U], float (&du)[U],
-                                               float (&h)[U]) {
+  static __device__ __forceinline__ void chain(const uint32_t (&v)[U], const uint32_t (&g)[U / 2], const uint32_t (&u)[U / 2], uint32_t (&dg)[U / 2],
+                                               uint32_t (&du)[U / 2], uint32_t (&h)[U / 2]) {
 #pragma unroll
     for (int k = 0; k < U; k += 2) {
-      const float2 gg = T::unpack(g[k / 2]), uu = T::unpack(u[k / 2]);
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const float dh = __uint_as_float(v[k + j]), x = j ? gg.y : gg.x, y = j ? uu.y : uu.x;
-        float a, slope;
-        activate<ACT, true>(x, a, slope);
-        dg[k + j] = dh * y * slope;
-        du[k + j] = dh * a;
-        h[k + j] = a * y;
-      }
+      const float2 x = T::unpack(g[k / 2]), y = T::unpack(u[k / 2]);
+      const float dh0 = __uint_as_float(v[k]), dh1 = __uint_as_float(v[k + 1]);
+      float a0, a1, slope0, slope1;
+      activate<ACT, true>(x.x, a0, slope0);
+      activate<ACT, true>(x.y, a1, slope1);
+      dg[k / 2] = T::pack(dh0 * y.x * slope0, dh1 * y.y * slope1);
+      du[k / 2] = T::pack(dh0 * a0, dh1 * a1);
+      h[k / 2] = T::pack(a0 * y.x, a1 * y.y);
     }
   }
-  template <int U>
-  static __device__ __forceinline__ void unit(const Params& o, State<U>& s, uint32_t (&v)[U], uint32_t (&)[1], int row, bool row_ok, int col, int n, bool more) {
-    if (!row_ok) return;
-    const int64_t at = (int64_t)row * o.ld + col;
-    uint32_t g[U / 2], u[U / 2];
+  template <int U, class OutT>
+  static __device__ __forceinline__ void unit(const Params& o, State<U>& s, OutT& out, uint32_t (&v)[U], uint32_t (&)[1], int row, bool row_ok, int col, int n,
+                                              bool more) {
+    uint32_t g[U / 2], u[U / 2], dg[U / 2], du[U / 2], h[U / 2];
 #pragma unroll
     for (int j = 0; j < U / 2; ++j) { g[j] = s.g[j]; u[j] = s.u[j]; }
-    if (more) fetch<U>(o, s, at + U);
-    float dg[U], du[U], h[U];
+    if (more && row_ok) fetch<U>(o, s, (int64_t)row * o.ld + col + U);
     if (o.act == EXO_ACT_SILU) chain<EXO_ACT_SILU, U>(v, g, u, dg, du, h);
     else if (o.act == EXO_ACT_GELU) chain<EXO_ACT_GELU, U>(v, g, u, dg, du, h);
     else chain<EXO_ACT_GELU_TANH, U>(v, g, u, dg, du, h);
-    store16<T, U>(o.h + at, h, U, 32);
-    uint16_t* const d = o.dgu + (int64_t)row * o.ld2 + col;
-    store16<T, U>(d, dg, n, 32);               // (not beyond `inner`: du begins there)
-    store16<T, U>(d + o.inner, du, n, o.du_align);
+    const bool second = (col & 16) != 0;
+    if (!second) out.open();
+    out.write16(0, col, h);
+    if (o.aligned) {
+      out.write16(1, col, dg);
+      out.write16(2, col, du);
+    }
+    if (second || !more) out.close(o.aligned ? 3 : 1, col);   // (columns beyond the last are the rows' padding, or not stored)
+    if (!o.aligned && row_ok) {   // `inner` is not a multiple of 8: du begins inside a 16-byte piece, and dg must not be written beyond its end
+      uint16_t* const d = o.dgu + (int64_t)row * o.ld2 + col;
+      store_words<U>(d, dg, n, 32);
+      store_words<U>(d + o.inner, du, n, o.du_align);
+    }
   }
   template <int U>
   static __device__ __forceinline__ void end(const Params&, State<U>&, int, bool, int) {}
@@ -169,8 +197,8 @@ struct PlainOp {
   struct State {};
   template <int U>
   static __device__ __forceinline__ void begin(const Params&, State<U>&, int, bool, int, int) {}
-  template <int U>
-  static __device__ __forceinline__ void unit(const Params& o, State<U>&, uint32_t (&v)[U], uint32_t (&)[1], int row, bool row_ok, int col, int n, bool) {
+  template <int U, class OutT>
+  static __device__ __forceinline__ void unit(const Params& o, State<U>&, OutT& out, uint32_t (&v)[U], uint32_t (&)[1], int row, bool row_ok, int col, int n, bool) {
     if (!row_ok) return;
     float y[U];
 #pragma unroll
@@ -254,7 +282,9 @@ exo_gemm_status_t forward(exo_ffn_plan* p, const void* x, const void* gate_up, c
   const Operand X{x, d.tokens, d.hidden, p->ldx}, GU{gate_up, 2 * d.inner, d.hidden, p->ld_gate_up};
   exo_gemm_status_t st;
   if (!p->thin) {
-    st = launch_pair<GatedOp<T>, false>(p->bn_gated, X, GU, d.inner, d.hidden, d.inner, bf16, p->sms, gp, stream);
+    const Result H{p->h, p->ldh, p->ldh}, G{gp.g, p->ldh, p->ldh}, U{gp.u, p->ldh, p->ldh};
+    st = saved ? launch_pair<GatedOp<T>, false>(p->bn_gated, X, GU, d.inner, d.hidden, d.inner, bf16, p->sms, gp, {H, G, U}, stream)
+               : launch_pair<GatedOp<T>, false>(p->bn_gated, X, GU, d.inner, d.hidden, d.inner, bf16, p->sms, gp, {H}, stream);
     return st != EXO_GEMM_OK ? st : gemm_run_scaled(p->down, p->h, down, y, 1.f, nullptr, 0.f, stream);
   }
   st = launch_thin<GatedOp<T>, 8>(p->width_gated, X, GU, d.inner, d.hidden, d.inner, bf16, p->sms, gp, stream);
@@ -268,9 +298,12 @@ template <class T>
 exo_gemm_status_t back(exo_ffn_plan* p, const void* down, const uint16_t* saved, const void* dy, cudaStream_t stream) {
   const exo_ffn_desc_t& d = p->d;
   typename GatedBackOp<T>::Params bp{saved, saved + d.tokens * p->ldh, p->h, p->ldh, p->dgu, p->ld2, (int32_t)d.inner, d.activation,
-                                     align_of(p->dgu, 2 * d.inner)};
-  return launch_pair<GatedBackOp<T>, true>(p->bn_back, Operand{dy, d.tokens, d.hidden, p->ldy}, Operand{down, d.hidden, d.inner, p->ld_down}, d.inner, d.hidden, 0,
-                                           d.dtype == EXO_GEMM_BF16, p->sms, bp, stream);
+                                     d.inner % 8 == 0, align_of(p->dgu, 2 * d.inner)};
+  const Operand dY{dy, d.tokens, d.hidden, p->ldy}, Wd{down, d.hidden, d.inner, p->ld_down};
+  const Result H{p->h, p->ldh, p->ldh}, G{p->dgu, d.inner, p->ld2}, U{p->dgu + d.inner, d.inner, p->ld2};
+  const bool bf16 = d.dtype == EXO_GEMM_BF16;
+  return bp.aligned ? launch_pair<GatedBackOp<T>, true>(p->bn_back, dY, Wd, d.inner, d.hidden, 0, bf16, p->sms, bp, {H, G, U}, stream)
+                    : launch_pair<GatedBackOp<T>, true>(p->bn_back, dY, Wd, d.inner, d.hidden, 0, bf16, p->sms, bp, {H}, stream);
 }
 
 }  // namespace

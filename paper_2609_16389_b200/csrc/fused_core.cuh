@@ -8,8 +8,9 @@
 // at once, the second from `gap` columns further on.  There the rows of B that a tile stages are `gap` rows of gate and `gap` rows of up:
 // CTA 0 of a pair stages the ones and CTA 1 the others, which is how a pair splits B anyway, so both projections are one product.
 //
-// Results go from registers to memory, a row per lane.  The main loops are long (K of a model's width), so that the 32 KB of staging are
-// better spent on a seventh stage of operands, as in the library's plain product.
+// A row of the accumulator is a lane's, and a warp's access to 32 rows takes 32 cycles of the load/store unit however few bytes it moves of
+// each.  Three results of 16 bits and two operands took 14 k cycles a tile of 256 x 256 that way, as long as a main loop over K = 1700; so 16-bit
+// results go through shared memory and TMA stores where their rows allow that (the pair kernel's Out).
 //
 // Every wait is bounded: one that gives up records that, all roles leave their loops, tensor memory is freed and the kernel returns.
 #pragma once
@@ -60,16 +61,19 @@ struct CoreParams {
 
 constexpr int kPairBarrierBytes = 512;
 constexpr int kPairMaxStages = 10;
+constexpr int kOutBytes = 2048;      // a buffer for results of an epilogue warp: 32 rows x 32 values of 16 bits; Op::kBuffers of them each
 constexpr int kThinThreads = 320;    // producer, MMA issuer, eight epilogue warps
 constexpr int kThinMaxStages = 16;
 constexpr int kThinBarrierBytes = 512;
 
 EXO_CX int pair_stage_bytes(int bn) { return kATileBytes + bn / 2 * 128; }
-EXO_CX int pair_stages(int bn) {
-  const int n = (kSmemLimit - 1024 - kPairBarrierBytes) / pair_stage_bytes(bn);
+EXO_CX int pair_stages(int bn, int buffers) {
+  const int n = (kSmemLimit - 1024 - kPairBarrierBytes - kEpiWarps * buffers * kOutBytes) / pair_stage_bytes(bn);
   return n > kPairMaxStages ? kPairMaxStages : n;
 }
-EXO_CX int pair_smem(int bn) { return pair_stages(bn) * pair_stage_bytes(bn) + kPairBarrierBytes + 1024; }
+EXO_CX int pair_smem(int bn, int buffers) {
+  return pair_stages(bn, buffers) * pair_stage_bytes(bn) + kEpiWarps * buffers * kOutBytes + kPairBarrierBytes + 1024;
+}
 // The MMAs read 64 or 128 rows of A whatever a stage holds of it: what follows the rows staged becomes accumulator rows that nobody reads, and
 // behind the last stage it is room that the ring keeps.
 EXO_CX int thin_mma_rows(int a_rows) { return a_rows <= 64 ? 64 : 128; }
@@ -146,13 +150,16 @@ __device__ __forceinline__ void tmem_ld(uint32_t taddr, uint32_t (&r)[8]) {
                : "r"(taddr) : "memory");
 }
 
-// ---------------------------------------------------------------- a row's U values to memory
-// `align`: a power of two up to 32 that divides the address of every unit.  n <= U values exist; the others are not written.
 template <class T, int U>
-__device__ __forceinline__ void store16(void* at, const float (&v)[U], int n, int align) {
-  uint32_t w[U / 2];
+__device__ __forceinline__ void pack(const float (&v)[U], uint32_t (&w)[U / 2]) {
 #pragma unroll
   for (int k = 0; k < U / 2; ++k) w[k] = T::pack(v[2 * k], v[2 * k + 1]);
+}
+
+// ---------------------------------------------------------------- a row's U values to memory
+// `align`: a power of two up to 32 that divides the address of every unit.  n <= U values exist; the others are not written.
+template <int U>
+__device__ __forceinline__ void store_words(void* at, const uint32_t (&w)[U / 2], int n, int align) {
   char* const c = static_cast<char*>(at);
   if (n >= U && align >= 16) {
     if (U >= 16 && align >= 32) {
@@ -183,6 +190,12 @@ __device__ __forceinline__ void store16(void* at, const float (&v)[U], int n, in
       }
   }
 }
+template <class T, int U>
+__device__ __forceinline__ void store16(void* at, const float (&v)[U], int n, int align) {
+  uint32_t w[U / 2];
+  pack<T, U>(v, w);
+  store_words<U>(at, w, n, align);
+}
 template <int U>
 __device__ __forceinline__ void store32(void* at, const float (&v)[U], int n, int align) {
   char* const c = static_cast<char*>(at);
@@ -204,11 +217,60 @@ __device__ __forceinline__ void store32(void* at, const float (&v)[U], int n, in
   }
 }
 
+// Where a warp of the pair kernel puts its results, 32 columns of 16 bits at a time: into a buffer, from there by a TMA store.  The buffers'
+// rows of 64 bytes are swizzled as the tensor maps say: 16-byte piece j of row r lies at j ^ (r / 2 % 4).
+struct OutMaps {
+  CUtensorMap m[3];
+};
+struct Out {
+  const OutMaps* maps;
+  uint32_t buffers, turn;
+  int32_t row0;           // the warp's first row
+  // N pieces of the lane's row, from piece `first` on
+  template <int N>
+  __device__ __forceinline__ void write(uint32_t at, uint32_t first, const uint32_t (&w)[4 * N]) {
+    const uint32_t lane = ptx::lane_id(), row = at + lane * 64u, x = (lane >> 1) & 3u;
+#pragma unroll
+    for (uint32_t j = 0; j < (uint32_t)N; ++j) ptx::st_shared_v4(row + (((first + j) ^ x) << 4), w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
+  }
+  // one result at a time, two buffers in turn
+  __device__ __forceinline__ void put(int map, int col, const uint32_t (&w)[16]) {
+    const uint32_t at = buffers + turn * kOutBytes;
+    if (ptx::elect_one()) ptx::bulk_wait_read<1>();   // the store before the last has read this buffer
+    __syncwarp();
+    write<4>(at, 0, w);
+    ptx::fence_proxy_async_smem();
+    __syncwarp();
+    if (ptx::elect_one()) {
+      ptx::tma_store_2d(&maps->m[map], col, row0, at);
+      ptx::bulk_commit();
+    }
+    turn ^= 1u;
+  }
+  // three results together, 16 columns at a time: open, write16 each, and close behind the second 16 or the last
+  __device__ __forceinline__ void open() {
+    if (ptx::elect_one()) ptx::bulk_wait_read<0>();
+    __syncwarp();
+  }
+  __device__ __forceinline__ void write16(int buffer, int col, const uint32_t (&w)[8]) {
+    write<2>(buffers + (uint32_t)buffer * kOutBytes, (uint32_t)(col >> 3) & 2u, w);
+  }
+  __device__ __forceinline__ void close(int results, int col) {
+    ptx::fence_proxy_async_smem();
+    __syncwarp();
+    if (ptx::elect_one()) {
+      for (int i = 0; i < results; ++i) ptx::tma_store_2d(&maps->m[i], col & ~31, row0, buffers + (uint32_t)i * kOutBytes);
+      ptx::bulk_commit();
+    }
+  }
+};
+struct NoOut {};
+
 // ---------------------------------------------------------------- the epilogue of one warp: 32 rows, `units` units of U columns
 // tacc: the warp's lanes of the accumulator, at its first unit's column; release() hands the accumulator back after the last read.
 // s: what Op::begin has fetched for the row and the first unit, before the accumulator was complete; a unit fetches for the next one.
-template <class Op, int U, class Release>
-__device__ __forceinline__ void run_units(const typename Op::Params& o, typename Op::template State<U>& s, uint32_t tacc, uint32_t gap, int row, bool row_ok, int col,
+template <class Op, int U, class OutT, class Release>
+__device__ __forceinline__ void run_units(const typename Op::Params& o, typename Op::template State<U>& s, OutT& out, uint32_t tacc, uint32_t gap, int row, bool row_ok, int col,
                                           int units, int N, int part, const Release& release) {
   const int left = N > col ? (N - col + U - 1) / U : 0;
   if (units > left) units = left;
@@ -230,7 +292,7 @@ __device__ __forceinline__ void run_units(const typename Op::Params& o, typename
     ptx::tmem_ld_wait();
     if (i + 1 == units) release();
     const int n = N - col - i * U;
-    Op::template unit<U>(o, s, v, v2, row, row_ok, col + i * U, n < U ? n : U, i + 1 < units);
+    Op::template unit<U>(o, s, out, v, v2, row, row_ok, col + i * U, n < U ? n : U, i + 1 < units);
   }
   Op::end(o, s, row, row_ok, part);
 }
@@ -238,16 +300,16 @@ __device__ __forceinline__ void run_units(const typename Op::Params& o, typename
 // ---------------------------------------------------------------- pairs of CTAs, persistent
 // Roles as in the library's plain product: warps 0 and 10 copy A and B, warp 1 issues the MMAs (CTA 0) and owns tensor memory, warps 2 to 9
 // are the epilogue, two per lane quadrant, each of them half of the tile's columns.
-template <class Op, int U, bool B_MN>
+template <class Op, bool B_MN>
 __global__ void __launch_bounds__(kNumThreads, 1)
-exo_fused_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b, const __grid_constant__ CoreParams p,
-                      const __grid_constant__ typename Op::Params o) {
+exo_fused_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b, const __grid_constant__ OutMaps tm_out,
+                      const __grid_constant__ CoreParams p, const __grid_constant__ typename Op::Params o) {
   constexpr int SUB_K = Op::kInt8 ? 128 : 64;          // elements of a k-block
   constexpr uint32_t TMEM_COLS = 512, ACC = 256;       // columns of both accumulators, and between them
   const int32_t width = p.width;                       // result columns of a tile
   const uint32_t b_rows = (uint32_t)(Op::kGated ? width : width / 2), stage_bytes = (uint32_t)kATileBytes + b_rows * 128u, stages = (uint32_t)p.stages;
   extern __shared__ uint8_t smem_raw[];
-  const uint32_t stage0 = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u, bar0 = stage0 + stages * stage_bytes;
+  const uint32_t stage0 = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u, out0 = stage0 + stages * stage_bytes, bar0 = out0 + kEpiWarps * Op::kBuffers * kOutBytes;
   auto full_bar = [&](uint32_t s) { return bar0 + 8u * s; };
   auto empty_bar = [&](uint32_t s) { return bar0 + 8u * (kPairMaxStages + s); };
   auto tfull_bar = [&](uint32_t a) { return bar0 + 8u * (2 * kPairMaxStages + a); };
@@ -344,12 +406,16 @@ exo_fused_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
     const uint32_t quad = warp & 3u;
     const int32_t half = (int32_t)((warp - 2u) >> 2);
     const uint32_t tempty0 = ptx::map_to_cta(tempty_bar(0), 0u);
-    const int32_t units = width / 2 / U;   // of this warp
+    // the tile's columns, 32 at a time: the first half of them, rounded up, is the first warp's of a lane quadrant
+    constexpr int U = Op::kUnit, PER = 32 / U;
+    const int32_t all = width / 32, skipped = (half ? (all + 1) / 2 : 0) * PER, units = (half ? all / 2 : (all + 1) / 2) * PER;
+    Out out{&tm_out, out0 + (warp - 2u) * (Op::kBuffers * kOutBytes), 0u, 0};
     uint32_t acc = 0, acc_ph = 0;
     for (int64_t t = worker; t < tiles; t += workers) {
       const TileCoord tc = raster_decode(p.raster, t);
       const int32_t row0 = tc.m * 256 + (int32_t)rank * 128 + (int32_t)quad * 32, row = row0 + (int32_t)lane;
-      const int32_t col = tc.n * width + half * (width / 2);
+      const int32_t col = tc.n * width + skipped * U;
+      out.row0 = row0;
       typename Op::template State<U> state;
       Op::template begin<U>(o, state, row, row < p.M, col, p.N);
       ok = wait_warp(tfull_bar(acc), acc_ph, p.wait_clocks);
@@ -366,11 +432,14 @@ exo_fused_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
       if (row0 >= p.M) {
         release();
       } else {
-        const uint32_t tacc = tmem_base + ((quad * 32u) << 16) + acc * ACC + (uint32_t)(half * (width / 2));
-        run_units<Op, U>(o, state, tacc, (uint32_t)width, row, row < p.M, col, units, p.N, tc.n * 2 + half, release);
+        const uint32_t tacc = tmem_base + ((quad * 32u) << 16) + acc * ACC + (uint32_t)(skipped * U);
+        run_units<Op, U>(o, state, out, tacc, (uint32_t)width, row, row < p.M, col, units, p.N, tc.n * 2 + half, release);
       }
       if ((acc ^= 1u) == 0u) acc_ph ^= 1u;
     }
+    __syncwarp();
+    if (ptx::elect_one()) ptx::bulk_wait_read<0>();   // the stores have read this CTA's shared memory
+    __syncwarp();
   }
 
   if (!ok)
@@ -491,7 +560,8 @@ exo_fused_thin_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
   const bool all_ok = __syncthreads_and(ok) != 0;   // the epilogue's warps wait here for the accumulator, taking no issue slots
   if (warp >= 2 && all_ok && row0 < p.M) {
     ptx::tc_fence_after_sync();
-    run_units<Op, U>(o, state, tmem_base + ((quad * 32u) << 16) + (uint32_t)(skipped * U), width, row, row_ok, col, mine, p.N, (int)blockIdx.x * 2 + half, [] {});
+    NoOut out;
+    run_units<Op, U>(o, state, out, tmem_base + ((quad * 32u) << 16) + (uint32_t)(skipped * U), width, row, row_ok, col, mine, p.N, (int)blockIdx.x * 2 + half, [] {});
   }
   if (!ok)
     for (int i = 0; i < 200; ++i) __nanosleep(1000);

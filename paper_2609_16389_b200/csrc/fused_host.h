@@ -3,6 +3,7 @@
 #include <cuda.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
+#include <string.h>
 
 #include <atomic>
 #include <initializer_list>
@@ -17,6 +18,7 @@ bool encode_operand_map(CUtensorMap* map, int elem_bytes, bool bf16, const void*
                         uint32_t box_rows);   // api.cu
 bool encode_blocks_map(CUtensorMap* whole, CUtensorMap* rest, int elem_bytes, bool bf16, const void* base, uint64_t inner, uint64_t rows,
                        uint64_t row_bytes, uint64_t parts, uint64_t part_bytes, uint32_t box_rows, uint32_t box_blocks);   // api.cu
+bool encode_result_map(CUtensorMap* map, void* base, uint64_t cols, uint64_t rows, uint64_t row_bytes);   // api.cu
 exo_gemm_status_t gemm_create_exact(exo_gemm_handle_t* out, const exo_gemm_desc_t* desc);   // api.cu
 exo_gemm_status_t gemm_run_scaled(exo_gemm_plan* plan, const void* A, const void* B, void* C, float alpha, const float* alpha_dev, float beta,
                                   void* cuda_stream);   // api.cu
@@ -148,10 +150,17 @@ struct Operand {
   int64_t rows, inner, ld;   // elements; ld * element size is a multiple of 16
 };
 
+// A 16-bit result that the pair kernel stores by TMA: its address a multiple of 16 bytes, ld of 8 values.  Where `cols` is not, a store
+// writes up to 7 values beyond them.
+struct Result {
+  void* at;
+  int64_t cols, ld;
+};
+
 // A product of A (M rows) and B with operator Op.  b_mn: B lies K x N (N contiguous) instead of N x K.
 template <class Op, bool B_MN>
 exo_gemm_status_t launch_pair(int bn, const Operand& A, const Operand& B, int64_t N, int64_t K, int64_t b_split, bool bf16, int sms,
-                              const typename Op::Params& op, cudaStream_t stream) {
+                              const typename Op::Params& op, std::initializer_list<Result> results, cudaStream_t stream) {
   constexpr int ES = Op::kInt8 ? 1 : 2, SUB_K = 128 / ES;
   const int width = Op::kGated ? bn / 2 : bn;
   CoreParams p{};
@@ -159,7 +168,7 @@ exo_gemm_status_t launch_pair(int bn, const Operand& A, const Operand& B, int64_
   p.N = (int32_t)N;
   p.nkb = (int32_t)((K + SUB_K - 1) / SUB_K);
   p.width = width;
-  p.stages = pair_stages(bn);
+  p.stages = pair_stages(bn, Op::kBuffers);
   p.b_split = (int32_t)(Op::kGated ? b_split : bn / 2);
   p.idesc = Op::kInt8 ? (2u << 4 | 1u << 7 | 1u << 10 | (uint32_t)(bn >> 3) << 17 | 16u << 24)   // signed bytes, 32-bit integer sums
                       : make_idesc(bf16 ? EXO_GEMM_BF16 : EXO_GEMM_FP16, 0, B_MN ? 1 : 0, 256, bn);
@@ -177,12 +186,15 @@ exo_gemm_status_t launch_pair(int bn, const Operand& A, const Operand& B, int64_
   const WaitHook hook = take_wait_hook();
   p.wait_clocks = hook.clocks;
   p.skip_copies = hook.skip;
+  OutMaps mo;
+  memset(&mo, 0, sizeof mo);
+  int n = 0;
+  for (const Result& r : results)
+    if (!encode_result_map(&mo.m[n++], r.at, (uint64_t)r.cols, (uint64_t)A.rows, (uint64_t)r.ld * 2)) return EXO_GEMM_ERR_CUDA;
   const int64_t pairs = tiles < sms / 2 ? tiles : sms / 2;
   typename Op::Params o = op;
-  void* args[4] = {&ma, &mb, &p, &o};
-  // units of the operator's own size where a warp's half of the tile is whole ones, else of 16 columns
-  void* fn = width / 2 % Op::kUnit == 0 ? (void*)exo_fused_pair_kernel<Op, Op::kUnit, B_MN> : (void*)exo_fused_pair_kernel<Op, 16, B_MN>;
-  return launch_args(fn, dim3((unsigned)(2 * pairs)), kNumThreads, (size_t)pair_smem(bn), 2, stream, args);
+  void* args[5] = {&ma, &mb, &mo, &p, &o};
+  return launch_args((void*)exo_fused_pair_kernel<Op, B_MN>, dim3((unsigned)(2 * pairs)), kNumThreads, (size_t)pair_smem(bn, Op::kBuffers), 2, stream, args);
 }
 
 template <class Op, int U>

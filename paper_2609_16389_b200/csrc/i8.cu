@@ -132,12 +132,13 @@ __global__ void __launch_bounds__(THREADS) exo_i8_quantize_kernel(const QuantPar
 // Integer sums are exact; a token's scale, its channels' scales and alpha are multiplied on in fp32.
 struct I8Op {
   static constexpr bool kInt8 = true, kGated = false, kTwice = false;
-  static constexpr int kUnit = 32;   // columns at a time, by pairs
+  static constexpr int kUnit = 32, kBuffers = 2;   // by pairs
   struct Params {
     const float *xs, *ws;
     void* y;
     int64_t ldy;
     int32_t cols, y_dtype, align;   // align: what divides the address of every unit
+    int32_t tma;                    // 16-bit results that are stored by TMA
     float alpha, beta;
   };
   template <int U>
@@ -154,13 +155,22 @@ struct I8Op {
     s.xs = row_ok ? __ldcg(o.xs + row) : 0.f;
     s.ws = scale_of<U>(o, col, N);
   }
-  template <int U>
-  static __device__ __forceinline__ void unit(const Params& o, State<U>& s, uint32_t (&v)[U], uint32_t (&)[1], int row, bool row_ok, int col, int n, bool more) {
+  template <int U, class OutT>
+  static __device__ __forceinline__ void unit(const Params& o, State<U>& s, OutT& out, uint32_t (&v)[U], uint32_t (&)[1], int row, bool row_ok, int col, int n, bool more) {
     float y[U];
     const float ws = s.ws;
     if (more) s.ws = scale_of<U>(o, col + U, o.cols);
 #pragma unroll
     for (int k = 0; k < U; ++k) y[k] = (float)(int32_t)v[k] * s.xs * __shfl_sync(0xffffffffu, ws, k) * o.alpha;
+    if constexpr (U == 32) {
+      if (o.tma) {
+        uint32_t w[16];
+        if (o.y_dtype == EXO_GEMM_BF16) pack<Bf16, U>(y, w);
+        else pack<Fp16, U>(y, w);
+        out.put(0, col, w);
+        return;
+      }
+    }
     if (!row_ok) return;
     const int64_t at = (int64_t)row * o.ldy + col;
     if (o.y_dtype == EXO_GEMM_FP32) {
@@ -344,10 +354,13 @@ exo_gemm_status_t exo_gemm_i8_run(const exo_i8_t* X, const exo_i8_t* W, void* Y,
     void* args[1] = {&p};
     return launch_args((void*)exo_i8_scale_kernel, dim3((unsigned)(ctas < 16 * sms ? ctas : 16 * sms)), kScaleYThreads, 0, 1, stream, args);
   }
-  I8Op::Params o{X->scales, W->scales, Y, ldy, (int32_t)N, y_dtype, align_of(Y, ldy * bytes), alpha, beta};
+  I8Op::Params o{X->scales, W->scales, Y, ldy, (int32_t)N, y_dtype, align_of(Y, ldy * bytes), 0, alpha, beta};
   const Operand A{X->codes, M, K, X->ld}, B{W->codes, N, K, W->ld};
   if (M <= kThinRows) return launch_thin<I8Op, 16>(thin_width(N, 16, 256, 1, M, sms), A, B, N, K, 0, false, sms, o, stream);
-  return launch_pair<I8Op, false>(pair_bn(M, N, false, 64, sms), A, B, N, K, 0, false, sms, o, stream);
+  const int bn = pair_bn(M, N, false, 64, sms);
+  o.tma = bytes == 2 && beta == 0.f && o.align >= 16 && N % 8 == 0;   // (nothing is written beyond a row's end)
+  return o.tma ? launch_pair<I8Op, false>(bn, A, B, N, K, 0, false, sms, o, {Result{Y, N, ldy}}, stream)
+               : launch_pair<I8Op, false>(bn, A, B, N, K, 0, false, sms, o, {}, stream);
 }
 
 }  // extern "C"
