@@ -535,6 +535,58 @@ def test_plans_side_by_side():
         f.check_backward(f.want(True))
 
 
+def test_example():
+    """It runs, and its gradients are those of automatic differentiation up to five roundings to bf16 (2^-8 each at most)."""
+    from examples import train_step
+    step = train_step.Step(140, 136, 200, 515)
+    loss, grads = step.by_autograd()
+    got = step.forward()
+    step.backward()
+    step.block.check()
+    step.loss_head.check()
+    assert abs(got.item() - loss.item()) <= 2.0 ** -8 * loss.item()
+    for a, b in zip((step.dx, step.d_gate_up, step.d_down, step.d_head), grads):
+        assert train_step.off(a, b) <= 5 * 2.0 ** -8
+    step.update(0.1)
+    logits, want = step.scores_in_8_bits()
+    assert logits.shape == want.shape and torch.isfinite(logits).all()
+
+
+def test_refusals_on_plans():
+    f = Ffn(20, 64, 48, "bf16", "silu", True, lds=(0, 0, 0, 51), seed=1)
+    x, gu, d, y, s, dy = (t.data_ptr() for t in (f.x0, f.gu0, f.d0, f.y0, f.saved, f.dy0))
+    dx, dgu, dd = f.dx0.data_ptr(), f.dgu0.data_ptr(), f.dd0.data_ptr()
+    h = f.plan.handle
+    for args, status in (((0, gu, d, y, s), 1), ((x, 0, d, y, s), 1), ((x, gu, 0, y, s), 1), ((x, gu, d, 0, s), 1), ((x + 2, gu, d, y, s), 4),
+                         ((x, gu + 8, d, y, s), 4), ((x, gu, d + 1, y, s), 4), ((x, gu, d, y + 4, s), 4), ((x, gu, d, y, s + 8), 4)):
+        assert E.exo_ffn_forward(h, *args, stream()) == status
+    for args, status in (((x, gu, 0, s, dy, dx, dgu, dd), 1), ((x, gu, d, 0, dy, dx, dgu, dd), 1), ((x, gu, d, s, 0, dx, dgu, dd), 1),
+                         ((0, gu, d, s, dy, dx, dgu, dd), 1), ((x, 0, d, s, dy, dx, dgu, dd), 1), ((x, gu, d, s + 2, dy, dx, dgu, dd), 4),
+                         ((x, gu, d, s, dy + 2, dx, dgu, dd), 4), ((x, gu, d, s, dy, dx + 8, dgu, dd), 4), ((x, gu, d, s, dy, dx, dgu + 4, dd), 4),
+                         ((x, gu, d, s, dy, dx, dgu, dd + 1), 4)):
+        assert E.exo_ffn_backward(h, *args, 0, stream()) == status
+    assert E.exo_ffn_backward(h, 0, 0, 0, 0, 0, 0, 0, 0, 0, stream()) == 0           # nothing wanted
+    c = Ce(20, 64, 48, "bf16", True, lds=(0, 67), seed=1)
+    x, w, t, lo, ls, s, dl = (v.data_ptr() for v in (c.x0, c.w0, c.target, c.loss, c.lse, c.saved, c.dloss))
+    dx, dw = c.dx0.data_ptr(), c.dw0.data_ptr()
+    h = c.plan.handle
+    for args, status in (((0, w, t, lo, ls, s), 1), ((x, 0, t, lo, ls, s), 1), ((x, w, 0, lo, ls, s), 1), ((x + 2, w, t, lo, ls, s), 4),
+                         ((x, w + 1, t, lo, ls, s), 4), ((x, w, t + 4, lo, ls, s), 4), ((x, w, t, lo + 2, ls, s), 4), ((x, w, t, lo, ls + 2, s), 4),
+                         ((x, w, t, lo, ls, s + 4), 4)):
+        assert E.exo_ce_forward(h, *args, stream()) == status
+    for args, status in (((0, w, t, ls, dl, s, dx, dw), 1), ((x, 0, t, ls, dl, s, dx, dw), 1), ((x, w, 0, ls, dl, s, dx, dw), 1),
+                         ((x, w, t, 0, dl, s, dx, dw), 1), ((x, w, t, ls, 0, s, dx, dw), 1), ((x, w, t, ls, dl, 0, dx, dw), 1),
+                         ((x, w, t, ls, dl, s + 8, dx, dw), 4), ((x, w, t, ls, dl, s, dx + 2, dw), 4), ((x, w, t, ls, dl, s, dx, dw + 1), 4)):
+        assert E.exo_ce_backward(h, *args, 0, stream()) == status
+    for kind, plan in (("ffn", Ffn(20, 64, 48, "bf16", "silu", False).plan), ("ce", Ce(20, 64, 48, "bf16", False).plan)):
+        assert plan.saved_bytes() == 0
+    g = Ffn(20, 64, 48, "bf16", "silu", False)
+    p = g.x0.data_ptr()
+    assert E.exo_ffn_forward(g.plan.handle, p, p, p, p, p, stream()) == 2            # a plan that does not train keeps nothing
+    assert E.exo_ffn_backward(g.plan.handle, p, p, p, p, p, p, p, p, 0, stream()) == 2
+    assert E.exo_fused_check() == 0
+
+
 @pytest.mark.parametrize("T", [4, 200])
 def test_a_wait_that_runs_out_is_reported(T):
     f = Ffn(T, 264, 136, "bf16", "silu", False, seed=1)
