@@ -285,10 +285,15 @@ exo_gemm_status_t forward(exo_ffn_plan* p, const void* x, const void* gate_up, c
     const Result H{p->h, p->ldh, p->ldh}, G{gp.g, p->ldh, p->ldh}, U{gp.u, p->ldh, p->ldh};
     st = saved ? launch_pair<GatedOp<T>, false>(p->bn_gated, X, GU, d.inner, d.hidden, d.inner, bf16, p->sms, gp, {H, G, U}, stream)
                : launch_pair<GatedOp<T>, false>(p->bn_gated, X, GU, d.inner, d.hidden, d.inner, bf16, p->sms, gp, {H}, stream);
-    return st != EXO_GEMM_OK ? st : gemm_run_scaled(p->down, p->h, down, y, 1.f, nullptr, 0.f, stream);
+  } else {
+    st = launch_thin<GatedOp<T>, 8>(p->width_gated, X, GU, d.inner, d.hidden, d.inner, bf16, p->sms, gp, stream);
   }
-  st = launch_thin<GatedOp<T>, 8>(p->width_gated, X, GU, d.inner, d.hidden, d.inner, bf16, p->sms, gp, stream);
   if (st != EXO_GEMM_OK) return st;
+  if (p->pack_down) {   // the copy of down goes on beside the first product
+    if ((st = align_rows(p->pack_down, p->ld_down, down, d.ld_down, d.inner, d.hidden, stream, true)) != EXO_GEMM_OK) return st;
+    down = p->pack_down;
+  }
+  if (!p->thin) return gemm_run_scaled(p->down, p->h, down, y, 1.f, nullptr, 0.f, stream);
   typename PlainOp<T>::Params yp{(uint16_t*)y, d.ldy, align_of(y, d.ldy * 2)};
   return launch_thin<PlainOp<T>, 16>(p->width_down, Operand{p->h, d.tokens, d.inner, p->ldh}, Operand{down, d.hidden, d.inner, p->ld_down}, d.hidden, d.inner,
                                      0, bf16, p->sms, yp, stream);
@@ -390,10 +395,8 @@ exo_gemm_status_t exo_ffn_forward(exo_ffn_handle_t p, const void* x, const void*
   exo_gemm_status_t st = EXO_GEMM_OK;
   if (p->pack_x && (st = align_rows(p->pack_x, p->ldx, x, d.ldx, d.hidden, d.tokens, s)) != EXO_GEMM_OK) return st;
   if (p->pack_gate_up && (st = align_rows(p->pack_gate_up, p->ld_gate_up, gate_up, d.ld_gate_up, d.hidden, 2 * d.inner, s)) != EXO_GEMM_OK) return st;
-  if (p->pack_down && (st = align_rows(p->pack_down, p->ld_down, down, d.ld_down, d.inner, d.hidden, s)) != EXO_GEMM_OK) return st;
   if (p->pack_x) x = p->pack_x;
   if (p->pack_gate_up) gate_up = p->pack_gate_up;
-  if (p->pack_down) down = p->pack_down;
   return d.dtype == EXO_GEMM_BF16 ? forward<Bf16>(p, x, gate_up, down, y, (uint16_t*)saved, s)
                                   : forward<Fp16>(p, x, gate_up, down, y, (uint16_t*)saved, s);
 }

@@ -401,8 +401,8 @@ exo_fused_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
       }
     }
   } else {
-    if (warp == 2) ptx::grid_launch_dependents();
     ptx::grid_dependency_wait();
+    if (warp == 2) ptx::grid_launch_dependents();   // (behind the wait: a kernel that starts now comes after all that this one waited for)
     const uint32_t quad = warp & 3u;
     const int32_t half = (int32_t)((warp - 2u) >> 2);
     const uint32_t tempty0 = ptx::map_to_cta(tempty_bar(0), 0u);
@@ -498,8 +498,8 @@ exo_fused_thin_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
   bool ok = true;
 
   if (warp == 0) {
-    ptx::grid_launch_dependents();
     ptx::grid_dependency_wait();
+    ptx::grid_launch_dependents();   // (behind the wait: a kernel that starts now comes after all that this one waited for)
     uint32_t s = 0, ph = 0;
     bool skip = p.skip_copies != 0 && blockIdx.x == 0;
     for (int32_t kb = 0; kb < nkb; kb += kb < whole ? (kb + per > whole ? whole - kb : per) : 1) {

@@ -233,7 +233,10 @@ exo_gemm_status_t launch_thin(int width, const Operand& A, const Operand& B, int
 }
 
 // dst = src, `rows` rows of `inner` 16-bit values; dst's rows start on 16 bytes and have room for a multiple of 8 values.
-exo_gemm_status_t align_rows(void* dst, int64_t dst_ld, const void* src, int64_t src_ld, int64_t inner, int64_t rows, cudaStream_t stream);   // i8.cu
+// beside: behind a kernel of this header whose results it does not touch, and beside it: that kernel has waited for all before it when this
+// one starts, and this one ends after it.
+exo_gemm_status_t align_rows(void* dst, int64_t dst_ld, const void* src, int64_t src_ld, int64_t inner, int64_t rows, cudaStream_t stream,
+                             bool beside = false);   // i8.cu
 
 // Device memory of a plan.
 struct Memory {

@@ -223,34 +223,49 @@ __global__ void __launch_bounds__(kScaleYThreads) exo_i8_scale_kernel(const Scal
 }
 
 // ---------------------------------------------------------------- aligned copies
-constexpr int kAlignThreads = 256;
+constexpr int kAlignThreads = 128;   // (with 40 registers at most, so that they fit an SM beside a CTA of a pair)
 struct AlignParams {
   uint16_t* dst;
   const uint16_t* src;
   int64_t dst_ld, src_ld, inner, rows, chunks;   // chunks: of eight values, per row
   int32_t word;                                  // bytes that divide the address of every source row: 2, 4 or 8
+  int32_t beside;
 };
-// A thread moves eight values: 16 bytes out, in as wide pieces as the source's rows allow.
+// A thread moves eight values at a time: 16 bytes out, in as wide pieces as the source's rows allow; four of them are on their way together.
 __global__ void __launch_bounds__(kAlignThreads) exo_fused_align_kernel(const AlignParams p) {
+  if (!p.beside) ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();
-  ptx::grid_dependency_wait();
-  const int64_t i = (int64_t)blockIdx.x * kAlignThreads + threadIdx.x;
-  const int64_t row = i / p.chunks, k = (i - row * p.chunks) * 8;
-  if (row >= p.rows) return;
-  const uint16_t* s = p.src + row * p.src_ld + k;
-  uint32_t w[4] = {};
-  if (k + 8 <= p.inner && p.word >= 8) {
-    const uint2 a = *reinterpret_cast<const uint2*>(s), b = *reinterpret_cast<const uint2*>(s + 4);
-    w[0] = a.x; w[1] = a.y; w[2] = b.x; w[3] = b.y;
-  } else if (k + 8 <= p.inner && p.word >= 4) {
+  const int64_t all = p.rows * p.chunks, step = (int64_t)gridDim.x * kAlignThreads;
+  for (int64_t i0 = (int64_t)blockIdx.x * kAlignThreads + threadIdx.x; i0 < all; i0 += 4 * step) {
+    uint32_t w[4][4];
+    int64_t to[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) w[j] = reinterpret_cast<const uint32_t*>(s)[j];
-  } else {
+    for (int q = 0; q < 4; ++q) {
+      const int64_t i = i0 + q * step;
+      to[q] = -1;
+      if (i >= all) continue;
+      const int64_t row = i / p.chunks, k = (i - row * p.chunks) * 8;
+      const uint16_t* s = p.src + row * p.src_ld + k;
+      to[q] = row * p.dst_ld + k;
+      if (k + 8 <= p.inner && p.word >= 8) {
+        const uint2 a = *reinterpret_cast<const uint2*>(s), b = *reinterpret_cast<const uint2*>(s + 4);
+        w[q][0] = a.x; w[q][1] = a.y; w[q][2] = b.x; w[q][3] = b.y;
+      } else if (k + 8 <= p.inner && p.word >= 4) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (k + j < p.inner) w[j / 2] |= (uint32_t)s[j] << (16 * (j & 1));
+        for (int j = 0; j < 4; ++j) w[q][j] = reinterpret_cast<const uint32_t*>(s)[j];
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[q][j] = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (k + j < p.inner) w[q][j / 2] |= (uint32_t)s[j] << (16 * (j & 1));
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (to[q] >= 0) ptx::st_global_v4(p.dst + to[q], w[q][0], w[q][1], w[q][2], w[q][3]);
   }
-  ptx::st_global_v4(p.dst + row * p.dst_ld + k, w[0], w[1], w[2], w[3]);
+  if (p.beside) ptx::grid_dependency_wait();   // what comes after this kernel comes after the one beside it, too
 }
 
 std::atomic<int64_t> wait_hook{0};   // milliseconds * 2 + skip
@@ -278,10 +293,13 @@ WaitHook take_wait_hook() {
 }
 unsigned take_gave_up_i8(cudaError_t* e) { return take_gave_up_here(e); }
 
-exo_gemm_status_t align_rows(void* dst, int64_t dst_ld, const void* src, int64_t src_ld, int64_t inner, int64_t rows, cudaStream_t stream) {
-  AlignParams p{(uint16_t*)dst, (const uint16_t*)src, dst_ld, src_ld, inner, rows, (inner + 7) / 8, align_of(src, src_ld * 2)};
-  const int64_t ctas = (rows * p.chunks + kAlignThreads - 1) / kAlignThreads;
-  if (ctas >= (1LL << 31)) return EXO_GEMM_ERR_UNSUPPORTED;
+exo_gemm_status_t align_rows(void* dst, int64_t dst_ld, const void* src, int64_t src_ld, int64_t inner, int64_t rows, cudaStream_t stream, bool beside) {
+  AlignParams p{(uint16_t*)dst, (const uint16_t*)src, dst_ld, src_ld, inner, rows, (inner + 7) / 8, align_of(src, src_ld * 2), beside ? 1 : 0};
+  // Beside another kernel the CTAs stay until that one ends, so there are as many as find room there.
+  int sms = 0;
+  const exo_gemm_status_t st = device_check(&sms);
+  if (st != EXO_GEMM_OK) return st;
+  const int64_t most = (beside ? 4 : 16) * sms, full = (rows * p.chunks + 4 * kAlignThreads - 1) / (4 * kAlignThreads), ctas = full < most ? full : most;
   if (ctas == 0) return EXO_GEMM_OK;
   void* args[1] = {&p};
   return launch_args((void*)exo_fused_align_kernel, dim3((unsigned)ctas), kAlignThreads, 0, 1, stream, args);
