@@ -61,8 +61,8 @@ struct StatsOp {
     }
     s.top = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
   }
-  template <int U, class OutT>
-  static __device__ __forceinline__ void unit(const Params& o, State<U>& s, OutT& out, uint32_t (&v)[U], uint32_t (&)[1], int row, bool row_ok, int col, int n, bool) {
+  template <int U>
+  static __device__ __forceinline__ void unit(const Params& o, State<U>& s, Out& out, uint32_t (&v)[U], uint32_t (&)[1], int row, bool row_ok, int col, int n, bool) {
     const float top = s.top == -INFINITY ? 0.f : s.top;   // a part without a finite logit: exponentials of -inf, or NaN, as they are
     float e[U];
     if (n >= U) {
@@ -133,8 +133,8 @@ struct GradOp {
     s.q = row_ok ? o.q[row] : 0.f;
     s.target = row_ok ? o.target[row] - o.first : -1;
   }
-  template <int U, class OutT>
-  static __device__ __forceinline__ void unit(const Params& o, State<U>& s, OutT& out, uint32_t (&v)[U], uint32_t (&)[1], int row, bool row_ok, int col, int, bool) {
+  template <int U>
+  static __device__ __forceinline__ void unit(const Params& o, State<U>& s, Out& out, uint32_t (&v)[U], uint32_t (&)[1], int row, bool row_ok, int col, int, bool) {
     float d[U];
     const int64_t t = s.target - col;
 #pragma unroll

@@ -78,8 +78,8 @@ struct GatedOp {
       h[k] = a * u[k];
     }
   }
-  template <int U, class OutT>
-  static __device__ __forceinline__ void unit(const Params& o, State<U>&, OutT& out, uint32_t (&v)[U], uint32_t (&v2)[U], int row, bool row_ok, int col, int, bool) {
+  template <int U>
+  static __device__ __forceinline__ void unit(const Params& o, State<U>&, Out& out, uint32_t (&v)[U], uint32_t (&v2)[U], int row, bool row_ok, int col, int, bool) {
     if (U < 32 && !row_ok) return;   // (a TMA store takes the whole warp, and leaves out the rows that do not exist)
     float g[U], u[U], h[U];
 #pragma unroll
@@ -156,8 +156,8 @@ struct GatedBackOp {
       h[k / 2] = T::pack(a0 * y.x, a1 * y.y);
     }
   }
-  template <int U, class OutT>
-  static __device__ __forceinline__ void unit(const Params& o, State<U>& s, OutT& out, uint32_t (&v)[U], uint32_t (&)[1], int row, bool row_ok, int col, int n,
+  template <int U>
+  static __device__ __forceinline__ void unit(const Params& o, State<U>& s, Out& out, uint32_t (&v)[U], uint32_t (&)[1], int row, bool row_ok, int col, int n,
                                               bool more) {
     uint32_t g[U / 2], u[U / 2], dg[U / 2], du[U / 2], h[U / 2];
 #pragma unroll
@@ -169,15 +169,16 @@ struct GatedBackOp {
     const bool second = (col & 16) != 0;
     if (!second) out.open();
     out.write16(0, col, h);
-    if (o.aligned) {
-      out.write16(1, col, dg);
-      out.write16(2, col, du);
-    }
-    if (second || !more) out.close(o.aligned ? 3 : 1, col);   // (columns beyond the last are the rows' padding, or not stored)
-    if (!o.aligned && row_ok) {   // `inner` is not a multiple of 8: du begins inside a 16-byte piece, and dg must not be written beyond its end
-      uint16_t* const d = o.dgu + (int64_t)row * o.ld2 + col;
-      store_words<U>(d, dg, n, 32);
-      store_words<U>(d + o.inner, du, n, o.du_align);
+    out.write16(1, col, dg);
+    out.write16(2, col, du);
+    if (second || !more) {
+      out.close(o.aligned ? 3 : 1, col);   // (columns beyond the last are the rows' padding, or not stored)
+      if (!o.aligned) {   // `inner` is not a multiple of 8: du begins inside a 16-byte piece, and dg must not be written beyond its end
+        uint16_t* const d = o.dgu + (int64_t)out.row0 * o.ld2 + (col & ~31);
+        const int there = n + (second ? 16 : 0);
+        out.store_rows<2>(1, d, 2 * o.ld2, there, 8);
+        out.store_rows<2>(2, d + o.inner, 2 * o.ld2, there, o.du_align);
+      }
     }
   }
   template <int U>
@@ -197,13 +198,19 @@ struct PlainOp {
   struct State {};
   template <int U>
   static __device__ __forceinline__ void begin(const Params&, State<U>&, int, bool, int, int) {}
-  template <int U, class OutT>
-  static __device__ __forceinline__ void unit(const Params& o, State<U>&, OutT& out, uint32_t (&v)[U], uint32_t (&)[1], int row, bool row_ok, int col, int n, bool) {
-    if (!row_ok) return;
+  template <int U>
+  static __device__ __forceinline__ void unit(const Params& o, State<U>&, Out& out, uint32_t (&v)[U], uint32_t (&)[1], int row, bool row_ok, int col, int n, bool) {
     float y[U];
 #pragma unroll
     for (int k = 0; k < U; ++k) y[k] = __uint_as_float(v[k]);
-    store16<T, U>(o.y + (int64_t)row * o.ld + col, y, n, o.align);
+    uint32_t w[U / 2];
+    pack<T, U>(y, w);
+    if (o.align >= 16 && n == U) {
+      if (row_ok) store_words<U>(o.y + (int64_t)row * o.ld + col, w, n, o.align);
+    } else {
+      out.write<U / 8>(out.buffers, 0, w);
+      out.store_rows<2>(0, o.y + (int64_t)out.row0 * o.ld + col, 2 * o.ld, n, o.align);
+    }
   }
   template <int U>
   static __device__ __forceinline__ void end(const Params&, State<U>&, int, bool, int) {}

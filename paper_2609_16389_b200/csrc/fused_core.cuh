@@ -78,7 +78,8 @@ EXO_CX int pair_smem(int bn, int buffers) {
 // behind the last stage it is room that the ring keeps.
 EXO_CX int thin_mma_rows(int a_rows) { return a_rows <= 64 ? 64 : 128; }
 EXO_CX int thin_smem(int stages, int per_stage, int b_rows, int a_rows) {
-  return 1024 + kThinBarrierBytes + 512 + stages * per_stage * (b_rows + a_rows) * 128 + (thin_mma_rows(a_rows) - a_rows) * 128;
+  const int ring = stages * per_stage * (b_rows + a_rows) * 128 + (thin_mma_rows(a_rows) - a_rows) * 128;
+  return 1024 + kThinBarrierBytes + 512 + (ring > kEpiWarps * 2 * kOutBytes ? ring : kEpiWarps * 2 * kOutBytes);   // (the epilogue's buffers lie in it)
 }
 
 // ---------------------------------------------------------------- bounded waits
@@ -169,25 +170,10 @@ __device__ __forceinline__ void store_words(void* at, const uint32_t (&w)[U / 2]
 #pragma unroll
       for (int j = 0; j < U / 8; ++j) ptx::st_global_v4(c + 16 * j, w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
     }
-  } else if (align >= 8) {
-#pragma unroll
-    for (int j = 0; j < U / 4; ++j)
-      if (4 * j + 4 <= n) {
-        *reinterpret_cast<uint2*>(c + 8 * j) = make_uint2(w[2 * j], w[2 * j + 1]);
-      } else {
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          if (4 * j + k < n) *reinterpret_cast<uint16_t*>(c + 8 * j + 2 * k) = (uint16_t)(w[2 * j + k / 2] >> (16 * (k & 1)));
-      }
   } else {
 #pragma unroll
-    for (int k = 0; k < U / 2; ++k)
-      if (align >= 4 && 2 * k + 2 <= n) {
-        *reinterpret_cast<uint32_t*>(c + 4 * k) = w[k];
-      } else {
-        if (2 * k < n) *reinterpret_cast<uint16_t*>(c + 4 * k) = (uint16_t)w[k];
-        if (2 * k + 1 < n) *reinterpret_cast<uint16_t*>(c + 4 * k + 2) = (uint16_t)(w[k] >> 16);
-      }
+    for (int k = 0; k < U; ++k)
+      if (k < n) reinterpret_cast<uint16_t*>(c)[k] = (uint16_t)(w[k / 2] >> (16 * (k & 1)));
   }
 }
 template <class T, int U>
@@ -197,23 +183,17 @@ __device__ __forceinline__ void store16(void* at, const float (&v)[U], int n, in
   store_words<U>(at, w, n, align);
 }
 template <int U>
-__device__ __forceinline__ void store32(void* at, const float (&v)[U], int n, int align) {
+__device__ __forceinline__ void store32(void* at, const float (&v)[U], int align) {   // align: 16 at least
   char* const c = static_cast<char*>(at);
-  if (n >= U && align >= 16) {
-    uint32_t w[U];
+  uint32_t w[U];
 #pragma unroll
-    for (int k = 0; k < U; ++k) w[k] = __float_as_uint(v[k]);
-    if (align >= 32) {
+  for (int k = 0; k < U; ++k) w[k] = __float_as_uint(v[k]);
+  if (align >= 32) {
 #pragma unroll
-      for (int j = 0; j < U / 8; ++j) ptx::st_global_v8(c + 32 * j, &w[8 * j]);
-    } else {
-#pragma unroll
-      for (int j = 0; j < U / 4; ++j) ptx::st_global_v4(c + 16 * j, w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
-    }
+    for (int j = 0; j < U / 8; ++j) ptx::st_global_v8(c + 32 * j, &w[8 * j]);
   } else {
 #pragma unroll
-    for (int k = 0; k < U; ++k)
-      if (k < n) reinterpret_cast<float*>(c)[k] = v[k];
+    for (int j = 0; j < U / 4; ++j) ptx::st_global_v4(c + 16 * j, w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
   }
 }
 
@@ -223,9 +203,9 @@ struct OutMaps {
   CUtensorMap m[3];
 };
 struct Out {
-  const OutMaps* maps;
+  const OutMaps* maps;    // NULL in the thin kernel, which stores rows only
   uint32_t buffers, turn;
-  int32_t row0;           // the warp's first row
+  int32_t row0, rows;     // the warp's first row, and how many of its rows exist
   // N pieces of the lane's row, from piece `first` on
   template <int N>
   __device__ __forceinline__ void write(uint32_t at, uint32_t first, const uint32_t (&w)[4 * N]) {
@@ -247,6 +227,55 @@ struct Out {
     }
     turn ^= 1u;
   }
+  // Results whose rows start anywhere: a row's `n` elements of ES bytes (64 bytes of it are in the buffer) are stored by neighbouring lanes, in
+  // pieces of what divides every row's address.  A row per lane would take 32 lines of memory for every instruction instead.
+  template <int ES, int W>
+  __device__ __forceinline__ void pieces(uint32_t at, char* dst, int64_t row_bytes, int n) {
+    constexpr int PER = W / ES, LANES = 64 / W;   // elements of a piece, pieces of a row
+    const int lane = (int)ptx::lane_id(), e = lane % LANES * PER;
+    const uint32_t byte = (uint32_t)(e * ES);
+    for (int r = lane / LANES; r < rows; r += 32 / LANES) {
+      const uint32_t from = at + (uint32_t)r * 64u + ((((byte >> 4) ^ ((uint32_t)r >> 1)) & 3u) << 4) + (byte & 15u);
+      char* const to = dst + (int64_t)r * row_bytes + byte;
+      if (e + PER <= n) {
+        if constexpr (W == 2) {
+          uint16_t v;
+          asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(from) : "memory");
+          *reinterpret_cast<uint16_t*>(to) = v;
+        } else if constexpr (W == 4) {
+          uint32_t v;
+          asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(from) : "memory");
+          *reinterpret_cast<uint32_t*>(to) = v;
+        } else {
+          uint2 v;
+          asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(from) : "memory");
+          *reinterpret_cast<uint2*>(to) = v;
+        }
+      } else {
+        for (int k = 0; k < n - e; ++k) {   // the end of a row inside a piece
+          if constexpr (ES == 2) {
+            uint16_t v;
+            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(from + 2u * (uint32_t)k) : "memory");
+            reinterpret_cast<uint16_t*>(to)[k] = v;
+          } else {
+            uint32_t v;
+            asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(from + 4u * (uint32_t)k) : "memory");
+            reinterpret_cast<uint32_t*>(to)[k] = v;
+          }
+        }
+      }
+    }
+  }
+  // dst: the first row's first element
+  template <int ES>
+  __device__ __forceinline__ void store_rows(int buffer, void* dst, int64_t row_bytes, int n, int align) {
+    const uint32_t at = buffers + (uint32_t)buffer * kOutBytes;
+    __syncwarp();
+    if (align >= 8) pieces<ES, 8>(at, static_cast<char*>(dst), row_bytes, n);
+    else if (ES == 4 || align >= 4) pieces<ES, 4>(at, static_cast<char*>(dst), row_bytes, n);
+    else if constexpr (ES == 2) pieces<ES, 2>(at, static_cast<char*>(dst), row_bytes, n);
+    __syncwarp();
+  }
   // three results together, 16 columns at a time: open, write16 each, and close behind the second 16 or the last
   __device__ __forceinline__ void open() {
     if (ptx::elect_one()) ptx::bulk_wait_read<0>();
@@ -264,13 +293,11 @@ struct Out {
     }
   }
 };
-struct NoOut {};
-
 // ---------------------------------------------------------------- the epilogue of one warp: 32 rows, `units` units of U columns
 // tacc: the warp's lanes of the accumulator, at its first unit's column; release() hands the accumulator back after the last read.
 // s: what Op::begin has fetched for the row and the first unit, before the accumulator was complete; a unit fetches for the next one.
-template <class Op, int U, class OutT, class Release>
-__device__ __forceinline__ void run_units(const typename Op::Params& o, typename Op::template State<U>& s, OutT& out, uint32_t tacc, uint32_t gap, int row, bool row_ok, int col,
+template <class Op, int U, class Release>
+__device__ __forceinline__ void run_units(const typename Op::Params& o, typename Op::template State<U>& s, Out& out, uint32_t tacc, uint32_t gap, int row, bool row_ok, int col,
                                           int units, int N, int part, const Release& release) {
   const int left = N > col ? (N - col + U - 1) / U : 0;
   if (units > left) units = left;
@@ -409,13 +436,14 @@ exo_fused_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
     // the tile's columns, 32 at a time: the first half of them, rounded up, is the first warp's of a lane quadrant
     constexpr int U = Op::kUnit, PER = 32 / U;
     const int32_t all = width / 32, skipped = (half ? (all + 1) / 2 : 0) * PER, units = (half ? all / 2 : (all + 1) / 2) * PER;
-    Out out{&tm_out, out0 + (warp - 2u) * (Op::kBuffers * kOutBytes), 0u, 0};
+    Out out{&tm_out, out0 + (warp - 2u) * (Op::kBuffers * kOutBytes), 0u, 0, 0};
     uint32_t acc = 0, acc_ph = 0;
     for (int64_t t = worker; t < tiles; t += workers) {
       const TileCoord tc = raster_decode(p.raster, t);
       const int32_t row0 = tc.m * 256 + (int32_t)rank * 128 + (int32_t)quad * 32, row = row0 + (int32_t)lane;
       const int32_t col = tc.n * width + skipped * U;
       out.row0 = row0;
+      out.rows = p.M - row0 < 32 ? p.M - row0 : 32;
       typename Op::template State<U> state;
       Op::template begin<U>(o, state, row, row < p.M, col, p.N);
       ok = wait_warp(tfull_bar(acc), acc_ph, p.wait_clocks);
@@ -560,7 +588,8 @@ exo_fused_thin_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
   const bool all_ok = __syncthreads_and(ok) != 0;   // the epilogue's warps wait here for the accumulator, taking no issue slots
   if (warp >= 2 && all_ok && row0 < p.M) {
     ptx::tc_fence_after_sync();
-    NoOut out;
+    const int32_t there = p.M - row0 < p.quad_rows ? p.M - row0 : p.quad_rows;
+    Out out{nullptr, stage0 + (warp - 2u) * (2 * kOutBytes), 0u, row0, there};   // (the ring is idle: every MMA has read its stage)
     run_units<Op, U>(o, state, out, tmem_base + ((quad * 32u) << 16) + (uint32_t)(skipped * U), width, row, row_ok, col, mine, p.N, (int)blockIdx.x * 2 + half, [] {});
   }
   if (!ok)

@@ -155,8 +155,8 @@ struct I8Op {
     s.xs = row_ok ? __ldcg(o.xs + row) : 0.f;
     s.ws = scale_of<U>(o, col, N);
   }
-  template <int U, class OutT>
-  static __device__ __forceinline__ void unit(const Params& o, State<U>& s, OutT& out, uint32_t (&v)[U], uint32_t (&)[1], int row, bool row_ok, int col, int n, bool more) {
+  template <int U>
+  static __device__ __forceinline__ void unit(const Params& o, State<U>& s, Out& out, uint32_t (&v)[U], uint32_t (&)[1], int row, bool row_ok, int col, int n, bool more) {
     float y[U];
     const float ws = s.ws;
     if (more) s.ws = scale_of<U>(o, col + U, o.cols);
@@ -171,26 +171,44 @@ struct I8Op {
         return;
       }
     }
-    if (!row_ok) return;
     const int64_t at = (int64_t)row * o.ldy + col;
+    const bool whole = n == U && o.align >= 16;
     if (o.y_dtype == EXO_GEMM_FP32) {
       float* const c = (float*)o.y + at;
-      if (o.beta != 0.f) {
+      if (o.beta != 0.f && row_ok) {
 #pragma unroll
         for (int k = 0; k < U; ++k)
           if (k < n) y[k] = fmaf(o.beta, c[k], y[k]);
       }
-      store32<U>(c, y, n, o.align);
+      if (whole) {
+        if (row_ok) store32<U>(c, y, o.align);
+        return;
+      }
+#pragma unroll
+      for (int h = 0; h < U / 16; ++h) {
+        uint32_t w[16];
+#pragma unroll
+        for (int k = 0; k < 16; ++k) w[k] = __float_as_uint(y[16 * h + k]);
+        out.write<4>(out.buffers + h * kOutBytes, 0, w);
+        out.store_rows<4>(h, (float*)o.y + (int64_t)out.row0 * o.ldy + col + 16 * h, 4 * o.ldy, n - 16 * h < 16 ? n - 16 * h : 16, o.align);
+      }
       return;
     }
     uint16_t* const c = (uint16_t*)o.y + at;
-    if (o.beta != 0.f) {
+    if (o.beta != 0.f && row_ok) {
 #pragma unroll
       for (int k = 0; k < U; ++k)
         if (k < n) y[k] = fmaf(o.beta, o.y_dtype == EXO_GEMM_BF16 ? Bf16::unpack(c[k]).x : Fp16::unpack(c[k]).x, y[k]);
     }
-    if (o.y_dtype == EXO_GEMM_BF16) store16<Bf16, U>(c, y, n, o.align);
-    else store16<Fp16, U>(c, y, n, o.align);
+    uint32_t w[U / 2];
+    if (o.y_dtype == EXO_GEMM_BF16) pack<Bf16, U>(y, w);
+    else pack<Fp16, U>(y, w);
+    if (whole) {
+      if (row_ok) store_words<U>(c, w, n, o.align);
+    } else {
+      out.write<U / 8>(out.buffers, 0, w);
+      out.store_rows<2>(0, (uint16_t*)o.y + (int64_t)out.row0 * o.ldy + col, 2 * o.ldy, n, o.align);
+    }
   }
   template <int U>
   static __device__ __forceinline__ void end(const Params&, State<U>&, int, bool, int) {}

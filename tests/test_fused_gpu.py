@@ -73,7 +73,7 @@ class Ffn:
             assert (whole[:, view.shape[1]:] == 7.0).all()
 
 
-FFN_SIZES = [(1, 64, 64), (1, 264, 8), (2, 8, 1), (5, 72, 35), (33, 136, 200), (64, 520, 1100), (128, 264, 2400), (129, 264, 136), (200, 136, 72),
+FFN_SIZES = [(1, 64, 64), (1, 264, 8), (2, 8, 1), (2, 1, 3), (140, 1, 1), (70, 37, 44), (5, 72, 35), (33, 136, 200), (64, 520, 1100), (128, 264, 2400), (129, 264, 136), (200, 136, 72),
              (300, 1032, 516), (513, 72, 1025)]
 
 
@@ -89,7 +89,7 @@ def test_ffn_forward(T, H, F, dtype):
 @pytest.mark.parametrize("T,H,F,dtype,act,grad", [
     (1, 64, 64, "bf16", "silu", "same"), (3, 72, 40, "fp16", "gelu", "fp32"), (128, 264, 200, "bf16", "gelu_tanh", "fp32"),
     (129, 264, 136, "fp16", "silu", "same"), (257, 520, 516, "bf16", "gelu", "same"), (300, 136, 1030, "fp16", "gelu_tanh", "same"),
-    (511, 1032, 257, "bf16", "silu", "fp32"), (1000, 256, 2304, "bf16", "silu", "same"), (2, 8, 1, "bf16", "gelu", "same")])
+    (511, 1032, 257, "bf16", "silu", "fp32"), (140, 72, 260, "bf16", "gelu", "same"), (140, 72, 262, "bf16", "silu", "same"), (7, 1, 1, "fp16", "silu", "same"), (1000, 256, 2304, "bf16", "silu", "same"), (2, 8, 1, "bf16", "gelu", "same")])
 def test_ffn_training(T, H, F, dtype, act, grad):
     f = Ffn(T, H, F, dtype, act, True, grad, seed=T)
     f.forward()
@@ -232,7 +232,7 @@ class Ce:
             R.check(self.dw, R.rounded(want["dw"], self.dw.dtype), "dw")
 
 
-CE_SIZES = [(1, 64, 64), (1, 8, 1), (2, 72, 7), (31, 136, 1000), (33, 264, 5001), (128, 520, 20011), (129, 264, 1003), (300, 72, 513), (513, 1032, 4099)]
+CE_SIZES = [(1, 64, 64), (1, 8, 1), (3, 1, 5), (140, 1, 2), (2, 72, 7), (31, 136, 1000), (33, 264, 5001), (128, 520, 20011), (129, 264, 1003), (300, 72, 513), (513, 1032, 4099)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
@@ -425,7 +425,7 @@ def test_i8_quantize_ties_and_tiny():
 
 @pytest.mark.parametrize("out", [torch.bfloat16, torch.float16, torch.float32])
 @pytest.mark.parametrize("M,N,K", [(1, 1, 1), (1, 300, 64), (3, 5001, 33), (16, 257, 1040), (37, 640, 4100), (128, 2403, 129), (129, 257, 40),
-                                   (300, 520, 1000), (1000, 130, 272)])
+                                   (300, 520, 1000), (300, 523, 1000), (257, 132, 64), (1000, 130, 272), (64, 35, 64), (65, 37, 272)])
 def test_i8_gemm(M, N, K, out):
     g = gen(M + N)
     (xc, xs, X), (wc, ws, W) = codes_of(M, K, g), codes_of(N, K, g)
@@ -493,15 +493,17 @@ def training_step(f, c):
     f.backward()
 
 
-def test_a_training_step_and_its_graph():
-    f = Ffn(200, 136, 264, "bf16", "silu", True, seed=21)
-    c = Ce(200, 136, 1003, "bf16", True, keep=300000, piece=256, seed=22)
+@pytest.mark.parametrize("T,F,lds,keep", [(200, 264, (0, 0, 0, 0), 300000), (200, 261, (0, 0, 0, 0), 300000), (40, 261, (0, 0, 0, 0), -1),
+                                          (40, 264, (0, 0, 139, 0), 0)])
+def test_a_training_step_and_its_graph(T, F, lds, keep):
+    f = Ffn(T, 136, F, "bf16", "silu", True, lds=lds, seed=21)
+    c = Ce(T, 136, 1003, "bf16", True, keep=keep, piece=256, seed=22)
     training_step(f, c)
     torch.cuda.synchronize()
     outs = lambda: (f.y, f.dy, f.dx, f.dgate_up, f.ddown, c.loss, c.dw)  # noqa: E731
     first = [t.clone() for t in outs()]
     # each operator on what the one before it left
-    want = R.ce(f.y, c.w, c.target, dloss=c.dloss)
+    want = R.ce(f.y, c.w, c.target, dloss=c.dloss, kept=keep != 0)
     R.check(c.loss, want["loss"])
     R.check(f.dy, want["dx"])
     f.check_backward(f.want(True))
