@@ -1,6 +1,7 @@
 // 8-bit integers with a scale per row, their products, and what the operators of exo_fused.h share: aligned copies, the state of device-side
 // waits.
 #include <new>
+#include <type_traits>
 
 #include "fused_host.h"
 
@@ -9,122 +10,166 @@ namespace fused {
 namespace {
 
 // ---------------------------------------------------------------- quantisation
-// A CTA per row: the largest magnitude, then the codes, from registers.  Bound by memory for many rows (2 + 1 bytes a value) and by the
-// latency of a load, a reduction and a store for few.
+// A row's largest magnitude, then its codes, from registers.  For many rows a warp takes a row and memory bounds the kernel (2 + 1 bytes a
+// value), if a value costs no more than about ten instructions; for few rows a CTA takes one, and the latencies of a load, a reduction and a
+// store are what is left.
 struct QuantParams {
   const void* x;
   int64_t ldx;
   int8_t* codes;
   int64_t ld;
   float* scales;
+  int64_t rows;
   int32_t K;
 };
 template <class T> struct Element { using type = uint16_t; };
 template <> struct Element<float> { using type = float; };
 
-// V values from k on as fp32
-template <class T, int V>
-__device__ __forceinline__ void load_values(const typename Element<T>::type* x, int k, float (&v)[V]) {
-  if constexpr (std::is_same<T, float>::value) {
-    if (V == 4) {
-      const float4 w = *reinterpret_cast<const float4*>(x + k);
-      v[0] = w.x; v[1] = w.y; v[2] = w.z; v[3] = w.w;
-    } else {
-      v[0] = x[k];
-    }
-  } else if constexpr (V == 8) {
-    const uint4 w = *reinterpret_cast<const uint4*>(x + k);
-    const float2 a = T::unpack(w.x), b = T::unpack(w.y), c = T::unpack(w.z), d = T::unpack(w.w);
-    v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y; v[4] = c.x; v[5] = c.y; v[6] = d.x; v[7] = d.y;
-  } else {
-    v[0] = T::unpack(x[k]).x;
-  }
-}
+template <int BYTES> struct Word;
+template <> struct Word<16> { using type = uint4; };
+template <> struct Word<8> { using type = uint2; };
+template <> struct Word<4> { using type = uint32_t; };
+template <> struct Word<2> { using type = uint16_t; };
+__device__ __forceinline__ uint32_t word_of(const uint4& w, int i) { return i == 0 ? w.x : i == 1 ? w.y : i == 2 ? w.z : w.w; }
+__device__ __forceinline__ uint32_t word_of(const uint2& w, int i) { return i == 0 ? w.x : w.y; }
+__device__ __forceinline__ uint32_t word_of(uint32_t w, int) { return w; }
+__device__ __forceinline__ uint32_t word_of(uint16_t w, int) { return w; }
 
-// Codes: the quotient rounded as IEEE division rounds it, then to the nearest integer, ties to even.  The product with the rounded
-// reciprocal is within 2^-22 of the quotient, relative, so both round to the same integer unless the product is within 127 * 2^-22 of a tie; there,
-// and for scales whose reciprocal is not a normal number, the division is made.
-struct Divider {
-  float scale, inverse;
-  bool safe;
-  __device__ __forceinline__ explicit Divider(float s) : scale(s), inverse(1.f / s), safe(s > 0x1p-120f && s < 0x1p120f) {}
-  __device__ __forceinline__ int code(float x) const {
-    float q = x * inverse, r = rintf(q);
-    if (!safe || fabsf(fabsf(q - r) - 0.5f) < 0x1p-14f) r = rintf(__fdiv_rn(x, scale));
-    return (int)fminf(fmaxf(r, -127.f), 127.f);
+// V consecutive values as they lie in memory, and as fp32
+template <class T, int V> struct Held {
+  using E = typename Element<T>::type;
+  typename Word<V * (int)sizeof(E)>::type w;
+  __device__ __forceinline__ void load(const E* x) { w = *reinterpret_cast<const decltype(w)*>(x); }
+  __device__ __forceinline__ void values(float (&v)[V]) const {
+    if constexpr (std::is_same<T, float>::value) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) v[j] = __uint_as_float(word_of(w, j));
+    } else {
+#pragma unroll
+      for (int j = 0; j < (V + 1) / 2; ++j) {
+        const float2 f = T::unpack(word_of(w, j));
+        v[2 * j] = f.x;
+        if (2 * j + 1 < V) v[2 * j + 1] = f.y;
+      }
+    }
+  }
+  __device__ __forceinline__ float largest() const {
+    float v[V], top = 0.f;
+    values(v);
+#pragma unroll
+    for (int j = 0; j < V; ++j) top = fmaxf(top, fabsf(v[j]));
+    return top;
   }
 };
 
-// V: values per load, 16 bytes of them where the rows allow that, else one.  THREADS per row; a thread keeps its first kHeld loads in
-// registers, further ones are read again.
-constexpr int kHeld = 8;
-template <class T, int V, int THREADS>
-__global__ void __launch_bounds__(THREADS) exo_i8_quantize_kernel(const QuantParams p) {
+// Codes: the quotient rounded as IEEE division rounds it, then to the nearest integer, ties to even.  The product with the rounded
+// reciprocal is within 2^-22 of the quotient, relative, so both round to the same integer unless the product is within 127 * 2^-22 of a tie; there,
+// and for scales whose reciprocal is not a normal number, the division is made.  Adding 1.5 * 2^23 rounds to an integer, whose last byte is the
+// code's.
+struct Divider {
+  float scale, inverse, limit;   // limit: how far from an integer the product may be
+  __device__ __forceinline__ explicit Divider(float s) : scale(s) {
+    const bool safe = s > 0x1p-120f && s < 0x1p120f;
+    inverse = safe ? 1.f / s : 0.f;
+    limit = safe ? 0.5f - 0x1p-14f : -1.f;
+  }
+  __device__ __noinline__ uint32_t divided(float x) const {
+    return scale > 0.f ? __float_as_uint(fminf(fmaxf(rintf(__fdiv_rn(x, scale)), -127.f), 127.f) + 12582912.f) : 0u;
+  }
+  template <int V>
+  __device__ __forceinline__ void codes(const float (&v)[V], uint32_t (&w)[(V + 3) / 4]) const {
+    constexpr float kRound = 12582912.f;
+    uint32_t c[V];
+    // A branch for every value: those of 16 bits meet ties often (half of a row's largest is one), a warp's 32 rarely all at one of them.
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const float q = v[j] * inverse, t = q + kRound;
+      c[j] = __float_as_uint(t);
+      if (fabsf(q - (t - kRound)) > limit) c[j] = divided(v[j]);   // (NaN and infinities give codes of no meaning)
+    }
+#pragma unroll
+    for (int j = 0; j < (V + 3) / 4; ++j) {
+      const uint32_t a = c[4 * j], b = 4 * j + 1 < V ? c[(4 * j + 1) % V] : 0u, d = 4 * j + 2 < V ? c[(4 * j + 2) % V] : 0u,
+                     e = 4 * j + 3 < V ? c[(4 * j + 3) % V] : 0u;
+      w[j] = __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(d, e, 0x0040), 0x5410);
+    }
+  }
+};
+
+// V: values per load, as many as 16 bytes hold where the rows' addresses allow that.  THREADS per row: a warp, or a CTA.  A thread keeps its
+// first HELD loads in registers, further ones are read again, from L1 or L2.  (A warp that keeps a row is so much code that fetching it takes
+// longer than reading twice: 4096 x 4096 bf16, 16 loads kept 35 us.)
+constexpr int kQuantWarps = 8;   // rows of a CTA, a warp each
+template <class T, int V, int THREADS, int HELD>
+__global__ void __launch_bounds__(THREADS == 32 ? 32 * kQuantWarps : THREADS) exo_i8_quantize_kernel(const QuantParams p) {
   __shared__ float tops[THREADS / 32];
   using E = typename Element<T>::type;
   ptx::grid_launch_dependents();
   ptx::grid_dependency_wait();
-  const E* x = (const E*)p.x + (int64_t)blockIdx.x * p.ldx;
-  int8_t* codes = p.codes + (int64_t)blockIdx.x * p.ld;
-  const int whole = p.K / V * V;   // the values of whole loads; the others one by one
-  const int first = threadIdx.x * V;
+  const int64_t row = THREADS == 32 ? (int64_t)blockIdx.x * kQuantWarps + (threadIdx.x >> 5) : blockIdx.x;
+  const int t = THREADS == 32 ? (int)(threadIdx.x & 31u) : (int)threadIdx.x;
+  if (row >= p.rows) return;   // (whole warps, where they have a row each)
+  const E* x = (const E*)p.x + row * p.ldx;
+  int8_t* codes = p.codes + row * p.ld;
   constexpr int STEP = THREADS * V;
-  float top = 0.f, held[kHeld][V];
+  const int whole = p.K / V * V, first = t * V;   // the values of whole loads; the others one by one
+  float top = 0.f;
+  Held<T, V> held[HELD > 0 ? HELD : 1];
 #pragma unroll
-  for (int i = 0; i < kHeld; ++i) {
-    if (first + i * STEP < whole) {
-      load_values<T, V>(x, first + i * STEP, held[i]);
-    } else {
+  for (int i = 0; i < HELD; ++i)
+    if (first + i * STEP < whole) held[i].load(x + first + i * STEP);
 #pragma unroll
-      for (int j = 0; j < V; ++j) held[i][j] = 0.f;
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < kHeld; ++i)
-#pragma unroll
-    for (int j = 0; j < V; ++j) top = fmaxf(top, fabsf(held[i][j]));
+  for (int i = 0; i < HELD; ++i)
+    if (first + i * STEP < whole) top = fmaxf(top, held[i].largest());
 #pragma unroll 4
-  for (int k = first + kHeld * STEP; k < whole; k += STEP) {
-    float v[V];
-    load_values<T, V>(x, k, v);
-#pragma unroll
-    for (int j = 0; j < V; ++j) top = fmaxf(top, fabsf(v[j]));
+  for (int k = first + HELD * STEP; k < whole; k += STEP) {
+    Held<T, V> h;
+    h.load(x + k);
+    top = fmaxf(top, h.largest());
   }
-  for (int k = whole + threadIdx.x; k < p.K; k += THREADS) {
-    float v[1];
-    load_values<T, 1>(x, k, v);
-    top = fmaxf(top, fabsf(v[0]));
+  for (int k = whole + t; k < p.K; k += THREADS) {
+    Held<T, 1> h;
+    h.load(x + k);
+    top = fmaxf(top, h.largest());
   }
 #pragma unroll
   for (int o = 16; o > 0; o /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-  if ((threadIdx.x & 31) == 0) tops[threadIdx.x >> 5] = top;
-  __syncthreads();
+  if constexpr (THREADS > 32) {
+    if ((t & 31) == 0) tops[t >> 5] = top;
+    __syncthreads();
 #pragma unroll
-  for (int w = 0; w < THREADS / 32; ++w) top = fmaxf(top, tops[w]);
+    for (int w = 0; w < THREADS / 32; ++w) top = fmaxf(top, tops[w]);
+  }
   const float scale = __fdiv_rn(top, 127.f);
-  if (threadIdx.x == 0) p.scales[blockIdx.x] = scale;
-  const bool zero = !(scale > 0.f);
-  const Divider by(zero ? 1.f : scale);
-  auto store = [&](int k, const float (&v)[V]) {
-    uint32_t w[(V + 3) / 4] = {};
-#pragma unroll
-    for (int j = 0; j < V; ++j) w[j / 4] |= (uint32_t)((zero ? 0 : by.code(v[j])) & 255) << (8 * (j & 3));
+  if (t == 0) p.scales[row] = scale;
+  const Divider by(scale);
+  auto store = [&](int k, const Held<T, V>& h) {
+    float v[V];
+    uint32_t w[(V + 3) / 4];
+    h.values(v);
+    by.codes<V>(v, w);
     if constexpr (V == 8) *reinterpret_cast<uint2*>(codes + k) = make_uint2(w[0], w[1]);
     else if constexpr (V == 4) *reinterpret_cast<uint32_t*>(codes + k) = w[0];
+    else if constexpr (V == 2) *reinterpret_cast<uint16_t*>(codes + k) = (uint16_t)w[0];
     else codes[k] = (int8_t)w[0];
   };
 #pragma unroll
-  for (int i = 0; i < kHeld; ++i)
+  for (int i = 0; i < HELD; ++i)
     if (first + i * STEP < whole) store(first + i * STEP, held[i]);
-  for (int k = first + kHeld * STEP; k < whole; k += STEP) {
-    float v[V];
-    load_values<T, V>(x, k, v);
-    store(k, v);
+#pragma unroll 2
+  for (int k = first + HELD * STEP; k < whole; k += STEP) {
+    Held<T, V> h;
+    h.load(x + k);
+    store(k, h);
   }
-  for (int k = whole + threadIdx.x; k < p.K; k += THREADS) {
+  for (int k = whole + t; k < p.K; k += THREADS) {
+    Held<T, 1> h;
     float v[1];
-    load_values<T, 1>(x, k, v);
-    codes[k] = (int8_t)(zero ? 0 : by.code(v[0]));
+    uint32_t w[1];
+    h.load(x + k);
+    h.values(v);
+    by.codes<1>(v, w);
+    codes[k] = (int8_t)w[0];
   }
 }
 
@@ -298,9 +343,17 @@ exo_gemm_status_t check_i8_memory(const exo_i8_t* q) {
   return aligned16(q->codes) && q->ld % 16 == 0 && ((uintptr_t)q->scales & 3u) == 0 ? EXO_GEMM_OK : EXO_GEMM_ERR_ALIGNMENT;
 }
 
-template <class T, int V> void* quant_fn(bool wide, int threads) {
-  if (wide) return threads == 128 ? (void*)exo_i8_quantize_kernel<T, V, 128> : (void*)exo_i8_quantize_kernel<T, V, 512>;
-  return threads == 128 ? (void*)exo_i8_quantize_kernel<T, 1, 128> : (void*)exo_i8_quantize_kernel<T, 1, 512>;
+template <class T, int V> void* quant_threads(int threads) {
+  return threads == 512 ? (void*)exo_i8_quantize_kernel<T, V, 512, 4> : threads == 128 ? (void*)exo_i8_quantize_kernel<T, V, 128, 4>
+                                                                                      : (void*)exo_i8_quantize_kernel<T, V, 32, 0>;
+}
+// bytes: what divides every row's address
+template <class T> void* quant_fn(int bytes, int threads) {
+  constexpr int ES = (int)sizeof(typename Element<T>::type);
+  if (bytes >= 16) return quant_threads<T, 16 / ES>(threads);
+  if (bytes >= 8) return quant_threads<T, 8 / ES>(threads);
+  if constexpr (ES == 2) return bytes >= 4 ? quant_threads<T, 2>(threads) : quant_threads<T, 1>(threads);
+  else return quant_threads<T, 1>(threads);
 }
 
 }  // namespace
@@ -358,15 +411,15 @@ exo_gemm_status_t exo_i8_quantize(const exo_i8_t* q, const void* X, int64_t ldx,
   if ((uintptr_t)X & (unsigned)(bytes - 1)) return EXO_GEMM_ERR_ALIGNMENT;
   int sms = 0;
   if ((st = device_check(&sms)) != EXO_GEMM_OK) return st;
-  QuantParams p{X, ldx, q->codes, q->ld, q->scales, (int32_t)q->K};
-  const bool wide = align_of(X, ldx * bytes) >= 16;
-  // few rows: more threads each, since nothing else hides a row's loads; many: more rows at once
-  const int threads = q->rows <= 2 * sms ? 512 : 128;
-  void* fn = x_dtype == EXO_GEMM_FP32   ? quant_fn<float, 4>(wide, threads)
-             : x_dtype == EXO_GEMM_BF16 ? quant_fn<Bf16, 8>(wide, threads)
-                                        : quant_fn<Fp16, 8>(wide, threads);
+  QuantParams p{X, ldx, q->codes, q->ld, q->scales, q->rows, (int32_t)q->K};
+  const int at = align_of(X, ldx * bytes);
+  const int threads = q->rows <= 4 * sms ? 512 : q->K > 1024 ? 128 : 32;
+  void* fn = x_dtype == EXO_GEMM_FP32   ? quant_fn<float>(at, threads)
+             : x_dtype == EXO_GEMM_BF16 ? quant_fn<Bf16>(at, threads)
+                                        : quant_fn<Fp16>(at, threads);
   void* args[1] = {&p};
-  return launch_args(fn, dim3((unsigned)q->rows), (unsigned)threads, 0, 1, (cudaStream_t)cuda_stream, args);
+  const int64_t ctas = threads > 32 ? q->rows : (q->rows + kQuantWarps - 1) / kQuantWarps;
+  return launch_args(fn, dim3((unsigned)ctas), threads > 32 ? (unsigned)threads : 32u * kQuantWarps, 0, 1, (cudaStream_t)cuda_stream, args);
 }
 
 exo_gemm_status_t exo_gemm_i8_run(const exo_i8_t* X, const exo_i8_t* W, void* Y, int64_t ldy, int32_t y_dtype, float alpha, float beta, void* cuda_stream) {
