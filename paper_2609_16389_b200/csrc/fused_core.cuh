@@ -52,6 +52,7 @@ struct CoreParams {
   int32_t quad_rows;   // thin: rows in a lane quadrant of the accumulator: 16 where the MMAs have 64 rows, 32 where they have 128
   int32_t per_stage;   // thin: k-blocks of a stage
   int32_t whole;       // thin: k-blocks that are whole; the last one may not be
+  int32_t split;       // thin: CTAs (a cluster of 1, 2, 4 or 8) that share a tile's K
   uint32_t idesc;
   OperandStaging a, b;
   Raster raster;
@@ -77,9 +78,12 @@ EXO_CX int pair_smem(int bn, int buffers) {
 // The MMAs read 64 or 128 rows of A whatever a stage holds of it: what follows the rows staged becomes accumulator rows that nobody reads, and
 // behind the last stage it is room that the ring keeps.
 EXO_CX int thin_mma_rows(int a_rows) { return a_rows <= 64 ? 64 : 128; }
-EXO_CX int thin_smem(int stages, int per_stage, int b_rows, int a_rows) {
+// What the epilogue keeps in the ring, when that is idle: buffers for results, and the partial sums of the other CTAs of a cluster, warp_bytes of
+// each warp.
+EXO_CX int thin_after(int warp_bytes, int split) { return kEpiWarps * (2 * kOutBytes + (split - 1) * warp_bytes); }
+EXO_CX int thin_smem(int stages, int per_stage, int b_rows, int a_rows, int after) {
   const int ring = stages * per_stage * (b_rows + a_rows) * 128 + (thin_mma_rows(a_rows) - a_rows) * 128;
-  return 1024 + kThinBarrierBytes + 512 + (ring > kEpiWarps * 2 * kOutBytes ? ring : kEpiWarps * 2 * kOutBytes);   // (the epilogue's buffers lie in it)
+  return 1024 + kThinBarrierBytes + 512 + (ring > after ? ring : after);
 }
 
 // ---------------------------------------------------------------- bounded waits
@@ -293,12 +297,38 @@ struct Out {
     }
   }
 };
+// The partial sums of a tile that the other CTAs of a cluster have left in this one's shared memory: per CTA and unit U columns (twice, for a
+// gated product) of a word per lane.
+struct Peers {
+  uint32_t count, at, step;   // step: bytes between two CTAs' sums
+};
+template <bool INT, int U>
+__device__ __forceinline__ void add_peers(const Peers& p, uint32_t offset, uint32_t (&v)[U]) {
+  const uint32_t lane = ptx::lane_id();
+  for (uint32_t i = 0; i < p.count; ++i) {   // in the order of K
+    const uint32_t from = p.at + i * p.step + offset + lane * 4u;
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      uint32_t w;
+      asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w) : "r"(from + 128u * (uint32_t)k) : "memory");
+      v[k] = INT ? v[k] + w : __float_as_uint(__uint_as_float(v[k]) + __uint_as_float(w));
+    }
+  }
+}
+template <int U>
+__device__ __forceinline__ void give_to_peer(uint32_t cluster_at, const uint32_t (&v)[U]) {
+  const uint32_t to = cluster_at + ptx::lane_id() * 4u;
+#pragma unroll
+  for (int k = 0; k < U; ++k) asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(to + 128u * (uint32_t)k), "r"(v[k]) : "memory");
+}
+
 // ---------------------------------------------------------------- the epilogue of one warp: 32 rows, `units` units of U columns
 // tacc: the warp's lanes of the accumulator, at its first unit's column; release() hands the accumulator back after the last read.
 // s: what Op::begin has fetched for the row and the first unit, before the accumulator was complete; a unit fetches for the next one.
-template <class Op, int U, class Release>
+template <class Op, int U, bool PEERS, class Release>
 __device__ __forceinline__ void run_units(const typename Op::Params& o, typename Op::template State<U>& s, Out& out, uint32_t tacc, uint32_t gap, int row, bool row_ok, int col,
-                                          int units, int N, int part, const Release& release) {
+                                          int units, int N, int part, const Peers& peers, const Release& release) {
+  constexpr uint32_t kUnitBytes = (Op::kGated ? 2 : 1) * U * 128;
   const int left = N > col ? (N - col + U - 1) / U : 0;
   if (units > left) units = left;
   if constexpr (Op::kTwice) {   // a first look at the columns
@@ -307,6 +337,7 @@ __device__ __forceinline__ void run_units(const typename Op::Params& o, typename
       uint32_t v[U];
       tmem_ld(tacc + (uint32_t)(i * U), v);
       ptx::tmem_ld_wait();
+      if constexpr (PEERS) add_peers<Op::kInt8, U>(peers, (uint32_t)i * kUnitBytes, v);
       Op::template look<U>(o, s, v, N - col - i * U);
     }
   }
@@ -318,6 +349,10 @@ __device__ __forceinline__ void run_units(const typename Op::Params& o, typename
     if constexpr (Op::kGated) tmem_ld(tacc + gap + (uint32_t)(i * U), v2);
     ptx::tmem_ld_wait();
     if (i + 1 == units) release();
+    if constexpr (PEERS) {
+      add_peers<Op::kInt8, U>(peers, (uint32_t)i * kUnitBytes, v);
+      if constexpr (Op::kGated) add_peers<Op::kInt8, U>(peers, (uint32_t)i * kUnitBytes + U * 128, v2);
+    }
     const int n = N - col - i * U;
     Op::template unit<U>(o, s, out, v, v2, row, row_ok, col + i * U, n < U ? n : U, i + 1 < units);
   }
@@ -461,7 +496,7 @@ exo_fused_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
         release();
       } else {
         const uint32_t tacc = tmem_base + ((quad * 32u) << 16) + acc * ACC + (uint32_t)(skipped * U);
-        run_units<Op, U>(o, state, out, tacc, (uint32_t)width, row, row < p.M, col, units, p.N, tc.n * 2 + half, release);
+        run_units<Op, U, false>(o, state, out, tacc, (uint32_t)width, row, row < p.M, col, units, p.N, tc.n * 2 + half, Peers{}, release);
       }
       if ((acc ^= 1u) == 0u) acc_ph ^= 1u;
     }
@@ -504,7 +539,9 @@ exo_fused_thin_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
   const uint32_t stage_bytes = (b_bytes + a_bytes) * (uint32_t)p.per_stage, a_at = b_bytes * (uint32_t)p.per_stage;
   uint32_t tmem_cols = 32;
   while (tmem_cols < bn) tmem_cols *= 2;
-  const int32_t nkb = p.nkb, whole = p.whole, per = p.per_stage, col0 = (int32_t)(blockIdx.x * width);
+  const uint32_t split = (uint32_t)p.split, rank = split > 1 ? ptx::cluster_ctarank() : 0u, tile = blockIdx.x / split;
+  const int32_t kb_first = (int32_t)((int64_t)p.nkb * rank / split), nkb = (int32_t)((int64_t)p.nkb * (rank + 1) / split);   // this CTA's k-blocks
+  const int32_t whole = p.whole < nkb ? p.whole : nkb, per = p.per_stage, col0 = (int32_t)(tile * width);
 
   if (warp == 0) {
     if (lane == 0) {
@@ -530,12 +567,12 @@ exo_fused_thin_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
     ptx::grid_launch_dependents();   // (behind the wait: a kernel that starts now comes after all that this one waited for)
     uint32_t s = 0, ph = 0;
     bool skip = p.skip_copies != 0 && blockIdx.x == 0;
-    for (int32_t kb = 0; kb < nkb; kb += kb < whole ? (kb + per > whole ? whole - kb : per) : 1) {
+    for (int32_t kb = kb_first; kb < nkb; kb += kb < whole ? (kb + per > whole ? whole - kb : per) : 1) {
       ok = wait_warp(empty_bar(s), ph ^ 1u, p.wait_clocks);
       if (!ok) break;
       if (ptx::elect_one()) {
         const uint32_t dst = stage0 + s * stage_bytes, bar = full_bar(s);
-        if (kb < whole) {   // (blocks beyond the last whole one arrive as zeros)
+        if (kb < whole) {   // (blocks beyond the last whole one arrive as zeros, another CTA's are not used)
           ptx::mbar_arrive_expect_tx(bar, stage_bytes);
           if (!skip) {
             tma_load_4d(dst, &tm_b, 0, col0, 0, kb, bar);
@@ -556,7 +593,7 @@ exo_fused_thin_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
     ptx::grid_dependency_wait();
     uint32_t s = 0, ph = 0;
     const uint32_t a_step = p.a.k_step_enc, b_step = p.b.k_step_enc, idesc = p.idesc;
-    for (int32_t kb = 0; kb < nkb;) {
+    for (int32_t kb = kb_first; kb < nkb;) {
       const int32_t blocks = kb < whole ? (kb + per > whole ? whole - kb : per) : 1;
       ok = wait_warp(full_bar(s), ph, p.wait_clocks);
       if (!ok) break;
@@ -566,7 +603,7 @@ exo_fused_thin_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
         for (int32_t j = 0; j < blocks; ++j) {
           const uint64_t a_j = a_desc + (uint32_t)j * (a_bytes >> 4), b_j = b_desc + (uint32_t)j * (b_bytes >> 4);
 #pragma unroll
-          for (uint32_t k = 0; k < 4; ++k) umma<Op, 1>(tmem_base, a_j + k * a_step, b_j + k * b_step, idesc, (kb > 0 || j > 0 || k > 0) ? 1u : 0u);
+          for (uint32_t k = 0; k < 4; ++k) umma<Op, 1>(tmem_base, a_j + k * a_step, b_j + k * b_step, idesc, (kb > kb_first || j > 0 || k > 0) ? 1u : 0u);
         }
         ptx::umma_commit<1>(empty_bar(s), 1);
         if (kb + blocks == nkb) ptx::umma_commit<1>(tfull_bar, 1);
@@ -586,11 +623,38 @@ exo_fused_thin_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
     Op::template begin<U>(o, state, row, row_ok, col, p.N);
   }
   const bool all_ok = __syncthreads_and(ok) != 0;   // the epilogue's warps wait here for the accumulator, taking no issue slots
-  if (warp >= 2 && all_ok && row0 < p.M) {
+  const uint32_t tacc = tmem_base + ((quad * 32u) << 16) + (uint32_t)(skipped * U);
+  // a warp's place for its sums in the first CTA of the cluster: [CTA][warp][unit]
+  constexpr uint32_t kUnitBytes = (Op::kGated ? 2 : 1) * U * 128;
+  const uint32_t most = (uint32_t)(all + 1) / 2u, peer_step = kEpiWarps * most * kUnitBytes;
+  const uint32_t peer_at = stage0 + kEpiWarps * 2 * kOutBytes + (warp - 2u) * most * kUnitBytes;
+  if (split > 1) {
+    ptx::cluster_arrive();
+    ptx::cluster_wait();   // the first CTA's ring is idle
+    if (rank > 0 && warp >= 2 && all_ok && row0 < p.M) {
+      ptx::tc_fence_after_sync();
+      const uint32_t to = ptx::map_to_cta(peer_at + (rank - 1u) * peer_step, 0u);
+      for (int32_t i = 0; i < mine; ++i) {
+        uint32_t v[U];
+        tmem_ld(tacc + (uint32_t)(i * U), v);
+        ptx::tmem_ld_wait();
+        give_to_peer<U>(to + (uint32_t)i * kUnitBytes, v);
+        if constexpr (Op::kGated) {
+          tmem_ld(tacc + width + (uint32_t)(i * U), v);
+          ptx::tmem_ld_wait();
+          give_to_peer<U>(to + (uint32_t)i * kUnitBytes + U * 128, v);
+        }
+      }
+    }
+    ptx::cluster_arrive();
+    ptx::cluster_wait();   // the sums are there
+  }
+  if (rank == 0 && warp >= 2 && all_ok && row0 < p.M) {
     ptx::tc_fence_after_sync();
     const int32_t there = p.M - row0 < p.quad_rows ? p.M - row0 : p.quad_rows;
     Out out{nullptr, stage0 + (warp - 2u) * (2 * kOutBytes), 0u, row0, there};   // (the ring is idle: every MMA has read its stage)
-    run_units<Op, U>(o, state, out, tmem_base + ((quad * 32u) << 16) + (uint32_t)(skipped * U), width, row, row_ok, col, mine, p.N, (int)blockIdx.x * 2 + half, [] {});
+    const Peers peers{split - 1u, peer_at, peer_step};
+    run_units<Op, U, true>(o, state, out, tacc, width, row, row_ok, col, mine, p.N, (int)tile * 2 + half, peers, [] {});
   }
   if (!ok)
     for (int i = 0; i < 200; ++i) __nanosleep(1000);

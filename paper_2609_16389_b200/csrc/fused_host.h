@@ -116,7 +116,7 @@ inline int thin_width(int64_t N, int quantum, int most, int parts, int64_t rows,
 // The ring of a thin tile: three large stages.  A stage costs the issuing warps some 500 clocks whatever it holds, which smaller ones do not
 // hide (16 tokens through a block of 4096 x 10240, us in all, with stages of 20, 32, 48 and 66 KB: 56.8, 52.7, 49.5, 48.3).  One CTA per SM takes
 // 200 KB; where there are more tiles than SMs two CTAs take 100 KB each, so that one's start and end hide behind the other's copies.
-inline void thin_ring(int b_rows, int a_rows, int64_t whole, bool alone, int* per_stage, int* stages) {
+inline void thin_ring(int b_rows, int a_rows, int64_t whole, bool alone, int after, int* per_stage, int* stages) {
   const int block = (b_rows + a_rows) * 128;
   int per = (alone ? 66 : 33) * 1024 / block;
   if (per > 16) per = 16;
@@ -125,7 +125,7 @@ inline void thin_ring(int b_rows, int a_rows, int64_t whole, bool alone, int* pe
   int n = (alone ? 200 : 100) * 1024 / (per * block);
   if (n < 3) n = 3;
   if (n > kThinMaxStages) n = kThinMaxStages;
-  while (n > 1 && thin_smem(n, per, b_rows, a_rows) > kSmemLimit) --n;
+  while (n > 1 && thin_smem(n, per, b_rows, a_rows, after) > kSmemLimit) --n;
   *per_stage = per;
   *stages = n;
 }
@@ -143,6 +143,15 @@ inline int pair_bn(int64_t M, int64_t N, bool gated, int multiple, int sms) {
     if (cost < 0 || c < cost) { cost = c; best = bn; }
   }
   return best;
+}
+
+// CTAs that share a thin tile's K where the tiles leave SMs idle: as many as the device holds clusters of (15 of 8 CTAs, 33 of 4), with
+// twelve k-blocks each, and room for the partial sums.  Whole and shared, us: 2 tokens through 7808 x 512 15.9, 13.8; 8 through 512 x 8192 17.8,
+// 13.1; 8 bits, 100 tokens by 256 x 16384 24.2, 12.9, 1 by 1024 x 8192 9.4, 8.5; with eight blocks each, 4 by 1024 x 2048, 5.4, 5.8.
+inline int thin_split(int64_t tiles, int warp_bytes, int64_t nkb, int sms) {
+  for (int s = 8; s > 1; s /= 2)
+    if (tiles * s <= (s == 8 ? sms * 4 / 5 : s == 4 ? sms * 8 / 9 : sms) && nkb >= 12 * s && thin_after(warp_bytes, s) <= 180 * 1024) return s;
+  return 1;
 }
 
 struct Operand {
@@ -212,7 +221,10 @@ exo_gemm_status_t launch_thin(int width, const Operand& A, const Operand& B, int
   p.quad_rows = mma_rows / 4;
   p.whole = (int32_t)(K / SUB_K);
   const int64_t tiles = (N + width - 1) / width;
-  thin_ring(bn, a_rows, p.whole, tiles <= sms, &p.per_stage, &p.stages);
+  const int warp_bytes = (width / U + 1) / 2 * (Op::kGated ? 2 : 1) * U * 128;   // of partial sums
+  p.split = thin_split(tiles, warp_bytes, p.nkb, sms);
+  const int after = thin_after(warp_bytes, p.split);
+  thin_ring(bn, a_rows, p.whole / p.split, tiles <= sms, after, &p.per_stage, &p.stages);
   p.idesc = Op::kInt8 ? (2u << 4 | 1u << 7 | 1u << 10 | (uint32_t)(bn >> 3) << 17 | (uint32_t)(mma_rows >> 4) << 24)
                       : make_idesc(bf16 ? EXO_GEMM_BF16 : EXO_GEMM_FP16, 0, 0, mma_rows, bn);
   p.a = make_staging(0, kBlockM, 1, 2);
@@ -228,8 +240,8 @@ exo_gemm_status_t launch_thin(int width, const Operand& A, const Operand& B, int
   p.skip_copies = hook.skip;
   typename Op::Params o = op;
   void* args[6] = {&ma, &ma_rest, &mb, &mb_rest, &p, &o};
-  return launch_args((void*)exo_fused_thin_kernel<Op, U>, dim3((unsigned)tiles), kThinThreads,
-                     (size_t)thin_smem(p.stages, p.per_stage, bn, a_rows), 1, stream, args);
+  return launch_args((void*)exo_fused_thin_kernel<Op, U>, dim3((unsigned)(tiles * p.split)), kThinThreads,
+                     (size_t)thin_smem(p.stages, p.per_stage, bn, a_rows, after), (unsigned)p.split, stream, args);
 }
 
 // dst = src, `rows` rows of `inner` 16-bit values; dst's rows start on 16 bytes and have room for a multiple of 8 values.

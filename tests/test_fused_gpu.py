@@ -73,7 +73,7 @@ class Ffn:
             assert (whole[:, view.shape[1]:] == 7.0).all()
 
 
-FFN_SIZES = [(1, 64, 64), (1, 264, 8), (2, 8, 1), (2, 1, 3), (140, 1, 1), (70, 37, 44), (5, 72, 35), (33, 136, 200), (64, 520, 1100), (128, 264, 2400), (129, 264, 136), (200, 136, 72),
+FFN_SIZES = [(1, 64, 64), (1, 264, 8), (2, 8, 1), (2, 1, 3), (140, 1, 1), (70, 37, 44), (3, 4104, 40), (70, 2064, 200), (1, 72, 4100), (5, 72, 35), (33, 136, 200), (64, 520, 1100), (128, 264, 2400), (129, 264, 136), (200, 136, 72),
              (300, 1032, 516), (513, 72, 1025)]
 
 
@@ -232,7 +232,7 @@ class Ce:
             R.check(self.dw, R.rounded(want["dw"], self.dw.dtype), "dw")
 
 
-CE_SIZES = [(1, 64, 64), (1, 8, 1), (3, 1, 5), (140, 1, 2), (2, 72, 7), (31, 136, 1000), (33, 264, 5001), (128, 520, 20011), (129, 264, 1003), (300, 72, 513), (513, 1032, 4099)]
+CE_SIZES = [(1, 64, 64), (1, 8, 1), (3, 1, 5), (140, 1, 2), (20, 2120, 900), (100, 1096, 70), (2, 72, 7), (31, 136, 1000), (33, 264, 5001), (128, 520, 20011), (129, 264, 1003), (300, 72, 513), (513, 1032, 4099)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
@@ -425,7 +425,7 @@ def test_i8_quantize_ties_and_tiny():
 
 @pytest.mark.parametrize("out", [torch.bfloat16, torch.float16, torch.float32])
 @pytest.mark.parametrize("M,N,K", [(1, 1, 1), (1, 300, 64), (3, 5001, 33), (16, 257, 1040), (37, 640, 4100), (128, 2403, 129), (129, 257, 40),
-                                   (300, 520, 1000), (300, 523, 1000), (257, 132, 64), (1000, 130, 272), (64, 35, 64), (65, 37, 272)])
+                                   (2, 64, 8192), (50, 272, 3100), (100, 1030, 4128), (300, 520, 1000), (300, 523, 1000), (257, 132, 64), (1000, 130, 272), (64, 35, 64), (65, 37, 272)])
 def test_i8_gemm(M, N, K, out):
     g = gen(M + N)
     (xc, xs, X), (wc, ws, W) = codes_of(M, K, g), codes_of(N, K, g)
