@@ -66,7 +66,7 @@ exo_gemm_status_t exo_ffn_create(exo_ffn_handle_t* out, const exo_ffn_desc_t* de
 int64_t exo_ffn_saved_bytes(exo_ffn_handle_t plan);
 
 /*
- * y = the block of x.  saved: NULL, or (training plans) exo_ffn_saved_bytes bytes, 16-byte aligned, that the backward call of these
+ * y = the block of x.  saved: NULL, or (training plans) exo_ffn_saved_bytes bytes, 32-byte aligned, that the backward call of these
  * tokens reads; the plan may be used for other tokens in between.  Both products are summed in fp32, act(g) * u is computed in fp32 and
  * rounded to dtype once, as the operand of the last product (a value beyond the largest finite one of fp16 becomes infinite); g and u
  * are rounded to dtype in `saved` only.  x and the weights must not overlap y or saved.
@@ -104,7 +104,8 @@ typedef struct exo_ce_plan* exo_ce_handle_t; /* opaque; owned by the library */
  *   lse_i = log sum_v exp(l_iv)
  *   loss_i = lse_i - (1 - s) * l_{i t_i} - s * mean_v l_iv
  *
- * A target that is ignore_index, or outside 0 .. vocab - 1, is ignored: loss_i = 0 and no gradient comes from its row.
+ * A target that is ignore_index, or outside 0 .. vocab - 1, is ignored: loss_i = 0, dx_i = 0 and nothing of the row is added to W's gradient
+ * (its x has to be finite all the same: 0 times an infinity or NaN is added).
  */
 typedef struct {
   int64_t tokens, hidden, vocab; /* tokens >= 0; hidden, vocab >= 1; each at most 2^24                                   */

@@ -23,7 +23,9 @@ constexpr float kTop = 16384.f;   // what the largest |dloss| becomes in q: |d| 
 template <class T>
 struct StatsOp {
   static constexpr bool kInt8 = false, kGated = false, kTwice = true;
-  static constexpr int kUnit = 32, kBuffers = 2;   // by pairs
+  static constexpr int kUnit = 32;         // columns at a time, by pairs
+  static constexpr bool kTogether = false;   // results go out together, a buffer each
+  static constexpr int kMore = 0;
   struct Params {
     float *top, *sum, *all;   // [part][row]: largest logit, sum of exponentials, sum of logits (NULL: not wanted)
     float* hit;               // [row]: the target's logit
@@ -115,7 +117,9 @@ struct StatsOp {
 template <class T>
 struct GradOp {
   static constexpr bool kInt8 = false, kGated = false, kTwice = false;
-  static constexpr int kUnit = 32, kBuffers = 2;   // by pairs
+  static constexpr int kUnit = 32;         // columns at a time, by pairs
+  static constexpr bool kTogether = false;   // results go out together, a buffer each
+  static constexpr int kMore = 0;
   struct Params {
     const float *lse, *q;     // [row]; q: dloss scaled, 0 for an ignored row
     const int64_t* target;

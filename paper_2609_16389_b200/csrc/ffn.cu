@@ -59,7 +59,9 @@ __device__ __forceinline__ void activate(float g, float& a, float& slope) {
 template <class T>
 struct GatedOp {
   static constexpr bool kInt8 = false, kGated = true, kTwice = false;
-  static constexpr int kUnit = 32, kBuffers = 2;   // by pairs
+  static constexpr int kUnit = 8;         // columns at a time, by pairs
+  static constexpr bool kTogether = true;   // results go out together, a buffer each
+  static constexpr int kMore = 0;
   struct Params {
     uint16_t *h, *g, *u;   // rows of ld values, ld a multiple of 64: whole units can be written; g and u may be NULL
     int64_t ld;
@@ -79,25 +81,26 @@ struct GatedOp {
     }
   }
   template <int U>
-  static __device__ __forceinline__ void unit(const Params& o, State<U>&, Out& out, uint32_t (&v)[U], uint32_t (&v2)[U], int row, bool row_ok, int col, int, bool) {
-    if (U < 32 && !row_ok) return;   // (a TMA store takes the whole warp, and leaves out the rows that do not exist)
+  static __device__ __forceinline__ void unit(const Params& o, State<U>&, Out& out, uint32_t (&v)[U], uint32_t (&v2)[U], int row, bool row_ok, int col, int, bool more) {
     float g[U], u[U], h[U];
 #pragma unroll
     for (int k = 0; k < U; ++k) { g[k] = __uint_as_float(v[k]); u[k] = __uint_as_float(v2[k]); }
     if (o.act == EXO_ACT_SILU) product<EXO_ACT_SILU, U>(g, u, h);
     else if (o.act == EXO_ACT_GELU) product<EXO_ACT_GELU, U>(g, u, h);
     else product<EXO_ACT_GELU_TANH, U>(g, u, h);
-    if constexpr (U == 32) {
-      uint32_t w[16];
+    uint32_t w[U / 2];
+    if (out.maps) {   // by pairs: 32 columns of up to three results, then a TMA store of each, which leaves out the rows that do not exist
+      if ((col & 31) == 0) out.open();
       pack<T, U>(h, w);
-      out.put(0, col, w);
+      out.piece<U / 8>(0, col, w);
       if (o.g) {
         pack<T, U>(g, w);
-        out.put(1, col, w);
+        out.piece<U / 8>(1, col, w);
         pack<T, U>(u, w);
-        out.put(2, col, w);
+        out.piece<U / 8>(2, col, w);
       }
-    } else {
+      if (((col + U) & 31) == 0 || !more) out.close(o.g ? 3 : 1, col);   // (columns beyond the last are the rows' padding)
+    } else if (row_ok) {
       const int64_t at = (int64_t)row * o.ld + col;
       store16<T, U>(o.h + at, h, U, 16);
       if (o.g) {
@@ -114,7 +117,9 @@ struct GatedOp {
 template <class T>
 struct GatedBackOp {
   static constexpr bool kInt8 = false, kGated = false, kTwice = false;
-  static constexpr int kUnit = 16, kBuffers = 3;   // by pairs; 32 columns at a time are more code than a small product's one tile hides the fetching of
+  static constexpr int kUnit = 16;         // columns at a time, by pairs
+  static constexpr bool kTogether = true;   // results go out together, a buffer each
+  static constexpr int kMore = 2;   // dg and du, also where they are not stored by TMA
   struct Params {
     const uint16_t *g, *u;
     uint16_t* h;
@@ -131,11 +136,9 @@ struct GatedBackOp {
   };
   template <int U>
   static __device__ __forceinline__ void fetch(const Params& o, State<U>& s, int64_t at) {
-#pragma unroll
-    for (int j = 0; j < U / 8; ++j) {
-      ptx::ld_global_cg_v4(o.g + at + 8 * j, s.g[4 * j], s.g[4 * j + 1], s.g[4 * j + 2], s.g[4 * j + 3]);
-      ptx::ld_global_cg_v4(o.u + at + 8 * j, s.u[4 * j], s.u[4 * j + 1], s.u[4 * j + 2], s.u[4 * j + 3]);
-    }
+    static_assert(U == 16, "a sector of each");
+    ld_global_cg_v8(o.g + at, s.g);
+    ld_global_cg_v8(o.u + at, s.u);
   }
   template <int U>
   static __device__ __forceinline__ void begin(const Params& o, State<U>& s, int row, bool row_ok, int col, int N) {
@@ -166,16 +169,15 @@ struct GatedBackOp {
     if (o.act == EXO_ACT_SILU) chain<EXO_ACT_SILU, U>(v, g, u, dg, du, h);
     else if (o.act == EXO_ACT_GELU) chain<EXO_ACT_GELU, U>(v, g, u, dg, du, h);
     else chain<EXO_ACT_GELU_TANH, U>(v, g, u, dg, du, h);
-    const bool second = (col & 16) != 0;
-    if (!second) out.open();
-    out.write16(0, col, h);
-    out.write16(1, col, dg);
-    out.write16(2, col, du);
-    if (second || !more) {
+    if ((col & 31) == 0) out.open();
+    out.piece<U / 8>(0, col, h);
+    out.piece<U / 8>(1, col, dg);
+    out.piece<U / 8>(2, col, du);
+    if (((col + U) & 31) == 0 || !more) {
       out.close(o.aligned ? 3 : 1, col);   // (columns beyond the last are the rows' padding, or not stored)
       if (!o.aligned) {   // `inner` is not a multiple of 8: du begins inside a 16-byte piece, and dg must not be written beyond its end
         uint16_t* const d = o.dgu + (int64_t)out.row0 * o.ld2 + (col & ~31);
-        const int there = n + (second ? 16 : 0);
+        const int there = (col & 31) + n;
         out.store_rows<2>(1, d, 2 * o.ld2, there, 8);
         out.store_rows<2>(2, d + o.inner, 2 * o.ld2, there, o.du_align);
       }
@@ -277,6 +279,9 @@ exo_gemm_status_t product(exo_gemm_handle_t* out, const exo_ffn_plan* p, int64_t
   g.device = p->device;
   return gemm_create_exact(out, &g);
 }
+
+// the saved g and u are read 32 bytes at a time
+bool aligned32(const void* p) { return ((uintptr_t)p & 31u) == 0; }
 
 // A 16-bit matrix of the caller's: 16-byte aligned where it is used in place, else aligned to its element.
 bool placed(const void* m, int64_t ld) { return ((uintptr_t)m & (ld % 8 ? 1u : 15u)) == 0; }
@@ -395,7 +400,7 @@ exo_gemm_status_t exo_ffn_forward(exo_ffn_handle_t p, const void* x, const void*
   if (saved && !d.training) return EXO_GEMM_ERR_INVALID_ARG;
   if (d.tokens == 0) return EXO_GEMM_OK;
   if (!x || !gate_up || !down || !y) return EXO_GEMM_ERR_NULL;
-  if (!placed(x, d.ldx) || !placed(gate_up, d.ld_gate_up) || !placed(down, d.ld_down) || !placed(y, d.ldy) || !aligned16(saved)) return EXO_GEMM_ERR_ALIGNMENT;
+  if (!placed(x, d.ldx) || !placed(gate_up, d.ld_gate_up) || !placed(down, d.ld_down) || !placed(y, d.ldy) || !aligned32(saved)) return EXO_GEMM_ERR_ALIGNMENT;
   OnDevice on(p->device);
   if (on.err != cudaSuccess) return cuda_failed(on.err);
   cudaStream_t s = (cudaStream_t)cuda_stream;
@@ -416,7 +421,7 @@ exo_gemm_status_t exo_ffn_backward(exo_ffn_handle_t p, const void* x, const void
   if (!dx && !d_gate_up && !d_down) return EXO_GEMM_OK;
   const bool any = d.tokens > 0;
   if (any && (!down || !saved || !dy || (d_gate_up && !x) || (dx && !gate_up))) return EXO_GEMM_ERR_NULL;
-  if (any && (!placed(down, d.ld_down) || !placed(dy, d.ldy) || !aligned16(saved) || (d_gate_up && !placed(x, d.ldx)) ||
+  if (any && (!placed(down, d.ld_down) || !placed(dy, d.ldy) || !aligned32(saved) || (d_gate_up && !placed(x, d.ldx)) ||
               (dx && (!placed(gate_up, d.ld_gate_up) || !placed(dx, d.ldx)))))
     return EXO_GEMM_ERR_ALIGNMENT;
   const int gb = d.grad_dtype == EXO_GEMM_FP32 ? 4 : 2;

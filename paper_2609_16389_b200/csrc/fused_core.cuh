@@ -8,9 +8,10 @@
 // at once, the second from `gap` columns further on.  There the rows of B that a tile stages are `gap` rows of gate and `gap` rows of up:
 // CTA 0 of a pair stages the ones and CTA 1 the others, which is how a pair splits B anyway, so both projections are one product.
 //
-// A row of the accumulator is a lane's, and a warp's access to 32 rows takes 32 cycles of the load/store unit however few bytes it moves of
-// each.  Three results of 16 bits and two operands took 14 k cycles a tile of 256 x 256 that way, as long as a main loop over K = 1700; so 16-bit
-// results go through shared memory and TMA stores where their rows allow that (the pair kernel's Out).
+// A row of the accumulator is a lane's, so a warp's access to memory is to 32 rows.  Operands of an epilogue are asked for a unit ahead, in whole
+// 32-byte sectors (a training step's backward kernel, 1024 tokens of 1024 x 2816: 3.3 us less than with 16 bytes); 16-bit results go through
+// shared memory and TMA stores where their rows allow that (the pair kernel's Out; 8192 x 32000 x 4096 with the exponentials kept: 1432 us with
+// stores from registers, 1404), and rows that start anywhere are stored by neighbouring lanes (8 bits, 320 x 1865 x 3648: 34.5 us a row per lane, 18.1).
 //
 // Every wait is bounded: one that gives up records that, all roles leave their loops, tensor memory is freed and the kernel returns.
 #pragma once
@@ -52,6 +53,7 @@ struct CoreParams {
   int32_t quad_rows;   // thin: rows in a lane quadrant of the accumulator: 16 where the MMAs have 64 rows, 32 where they have 128
   int32_t per_stage;   // thin: k-blocks of a stage
   int32_t whole;       // thin: k-blocks that are whole; the last one may not be
+  int32_t buffers;     // pair: of an epilogue warp, for results
   int32_t split;       // thin: CTAs (a cluster of 1, 2, 4 or 8) that share a tile's K
   uint32_t idesc;
   OperandStaging a, b;
@@ -62,7 +64,7 @@ struct CoreParams {
 
 constexpr int kPairBarrierBytes = 512;
 constexpr int kPairMaxStages = 10;
-constexpr int kOutBytes = 2048;      // a buffer for results of an epilogue warp: 32 rows x 32 values of 16 bits; Op::kBuffers of them each
+constexpr int kOutBytes = 2048;      // a buffer for results of an epilogue warp: 32 rows x 32 values of 16 bits
 constexpr int kThinThreads = 320;    // producer, MMA issuer, eight epilogue warps
 constexpr int kThinMaxStages = 16;
 constexpr int kThinBarrierBytes = 512;
@@ -135,6 +137,12 @@ template <class Op, int CTA_GROUP>
 __device__ __forceinline__ void umma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
   if constexpr (Op::kInt8) umma_i8<CTA_GROUP>(d, a, b, idesc, accumulate);
   else ptx::umma_f16<CTA_GROUP>(d, a, b, idesc, accumulate);
+}
+
+// 32 bytes of a lane, a whole sector: what a warp's rows cost is the sectors they ask for.
+__device__ __forceinline__ void ld_global_cg_v8(const void* at, uint32_t (&r)[8]) {
+  asm volatile("ld.global.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "l"(at) : "memory");
 }
 
 __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, int32_t x, int32_t y, int32_t z, int32_t w, uint32_t bar) {
@@ -280,13 +288,14 @@ struct Out {
     else if constexpr (ES == 2) pieces<ES, 2>(at, static_cast<char*>(dst), row_bytes, n);
     __syncwarp();
   }
-  // three results together, 16 columns at a time: open, write16 each, and close behind the second 16 or the last
+  // several results together, N * 8 columns at a time: open, piece each, and close behind the 32nd column or the last
   __device__ __forceinline__ void open() {
     if (ptx::elect_one()) ptx::bulk_wait_read<0>();
     __syncwarp();
   }
-  __device__ __forceinline__ void write16(int buffer, int col, const uint32_t (&w)[8]) {
-    write<2>(buffers + (uint32_t)buffer * kOutBytes, (uint32_t)(col >> 3) & 2u, w);
+  template <int N>
+  __device__ __forceinline__ void piece(int buffer, int col, const uint32_t (&w)[4 * N]) {
+    write<N>(buffers + (uint32_t)buffer * kOutBytes, (uint32_t)(col >> 3) & 3u, w);
   }
   __device__ __forceinline__ void close(int results, int col) {
     ptx::fence_proxy_async_smem();
@@ -371,7 +380,7 @@ exo_fused_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
   const int32_t width = p.width;                       // result columns of a tile
   const uint32_t b_rows = (uint32_t)(Op::kGated ? width : width / 2), stage_bytes = (uint32_t)kATileBytes + b_rows * 128u, stages = (uint32_t)p.stages;
   extern __shared__ uint8_t smem_raw[];
-  const uint32_t stage0 = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u, out0 = stage0 + stages * stage_bytes, bar0 = out0 + kEpiWarps * Op::kBuffers * kOutBytes;
+  const uint32_t stage0 = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u, out0 = stage0 + stages * stage_bytes, bar0 = out0 + kEpiWarps * (uint32_t)p.buffers * kOutBytes;
   auto full_bar = [&](uint32_t s) { return bar0 + 8u * s; };
   auto empty_bar = [&](uint32_t s) { return bar0 + 8u * (kPairMaxStages + s); };
   auto tfull_bar = [&](uint32_t a) { return bar0 + 8u * (2 * kPairMaxStages + a); };
@@ -471,7 +480,7 @@ exo_fused_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
     // the tile's columns, 32 at a time: the first half of them, rounded up, is the first warp's of a lane quadrant
     constexpr int U = Op::kUnit, PER = 32 / U;
     const int32_t all = width / 32, skipped = (half ? (all + 1) / 2 : 0) * PER, units = (half ? all / 2 : (all + 1) / 2) * PER;
-    Out out{&tm_out, out0 + (warp - 2u) * (Op::kBuffers * kOutBytes), 0u, 0, 0};
+    Out out{&tm_out, out0 + (warp - 2u) * ((uint32_t)p.buffers * kOutBytes), 0u, 0, 0};
     uint32_t acc = 0, acc_ph = 0;
     for (int64_t t = worker; t < tiles; t += workers) {
       const TileCoord tc = raster_decode(p.raster, t);

@@ -177,7 +177,8 @@ exo_gemm_status_t launch_pair(int bn, const Operand& A, const Operand& B, int64_
   p.N = (int32_t)N;
   p.nkb = (int32_t)((K + SUB_K - 1) / SUB_K);
   p.width = width;
-  p.stages = pair_stages(bn, Op::kBuffers);
+  p.buffers = Op::kTogether && results.size() + Op::kMore > 2 ? 3 : 2;
+  p.stages = pair_stages(bn, p.buffers);
   p.b_split = (int32_t)(Op::kGated ? b_split : bn / 2);
   p.idesc = Op::kInt8 ? (2u << 4 | 1u << 7 | 1u << 10 | (uint32_t)(bn >> 3) << 17 | 16u << 24)   // signed bytes, 32-bit integer sums
                       : make_idesc(bf16 ? EXO_GEMM_BF16 : EXO_GEMM_FP16, 0, B_MN ? 1 : 0, 256, bn);
@@ -203,7 +204,7 @@ exo_gemm_status_t launch_pair(int bn, const Operand& A, const Operand& B, int64_
   const int64_t pairs = tiles < sms / 2 ? tiles : sms / 2;
   typename Op::Params o = op;
   void* args[5] = {&ma, &mb, &mo, &p, &o};
-  return launch_args((void*)exo_fused_pair_kernel<Op, B_MN>, dim3((unsigned)(2 * pairs)), kNumThreads, (size_t)pair_smem(bn, Op::kBuffers), 2, stream, args);
+  return launch_args((void*)exo_fused_pair_kernel<Op, B_MN>, dim3((unsigned)(2 * pairs)), kNumThreads, (size_t)pair_smem(bn, p.buffers), 2, stream, args);
 }
 
 template <class Op, int U>

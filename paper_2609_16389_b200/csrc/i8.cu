@@ -177,7 +177,9 @@ __global__ void __launch_bounds__(THREADS == 32 ? 32 * kQuantWarps : THREADS) ex
 // Integer sums are exact; a token's scale, its channels' scales and alpha are multiplied on in fp32.
 struct I8Op {
   static constexpr bool kInt8 = true, kGated = false, kTwice = false;
-  static constexpr int kUnit = 32, kBuffers = 2;   // by pairs
+  static constexpr int kUnit = 32;         // columns at a time, by pairs
+  static constexpr bool kTogether = false;   // results go out together, a buffer each
+  static constexpr int kMore = 0;
   struct Params {
     const float *xs, *ws;
     void* y;

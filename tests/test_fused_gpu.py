@@ -560,10 +560,10 @@ def test_refusals_on_plans():
     dx, dgu, dd = f.dx0.data_ptr(), f.dgu0.data_ptr(), f.dd0.data_ptr()
     h = f.plan.handle
     for args, status in (((0, gu, d, y, s), 1), ((x, 0, d, y, s), 1), ((x, gu, 0, y, s), 1), ((x, gu, d, 0, s), 1), ((x + 2, gu, d, y, s), 4),
-                         ((x, gu + 8, d, y, s), 4), ((x, gu, d + 1, y, s), 4), ((x, gu, d, y + 4, s), 4), ((x, gu, d, y, s + 8), 4)):
+                         ((x, gu + 8, d, y, s), 4), ((x, gu, d + 1, y, s), 4), ((x, gu, d, y + 4, s), 4), ((x, gu, d, y, s + 16), 4)):
         assert E.exo_ffn_forward(h, *args, stream()) == status
     for args, status in (((x, gu, 0, s, dy, dx, dgu, dd), 1), ((x, gu, d, 0, dy, dx, dgu, dd), 1), ((x, gu, d, s, 0, dx, dgu, dd), 1),
-                         ((0, gu, d, s, dy, dx, dgu, dd), 1), ((x, 0, d, s, dy, dx, dgu, dd), 1), ((x, gu, d, s + 2, dy, dx, dgu, dd), 4),
+                         ((0, gu, d, s, dy, dx, dgu, dd), 1), ((x, 0, d, s, dy, dx, dgu, dd), 1), ((x, gu, d, s + 16, dy, dx, dgu, dd), 4),
                          ((x, gu, d, s, dy + 2, dx, dgu, dd), 4), ((x, gu, d, s, dy, dx + 8, dgu, dd), 4), ((x, gu, d, s, dy, dx, dgu + 4, dd), 4),
                          ((x, gu, d, s, dy, dx, dgu, dd + 1), 4)):
         assert E.exo_ffn_backward(h, *args, 0, stream()) == status
