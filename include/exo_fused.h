@@ -135,7 +135,8 @@ int64_t exo_ce_saved_bytes(exo_ce_handle_t plan);
 
 /*
  * loss and lse (fp32, `tokens` values each; either may be NULL) from x, W and target (int64, 8-byte aligned).  saved: NULL, or (training
- * plans) exo_ce_saved_bytes bytes, 16-byte aligned.  Logits, their exponentials' sums and the mean are held in fp32.
+ * plans) exo_ce_saved_bytes bytes, 16-byte aligned.  Logits, their exponentials' sums and the mean are held in fp32.  (The tensor core truncates
+ * as it adds: products of depth 4096 come out 3e-6 of their deviation nearer to zero, and lse 1.6e-5 low where the logits' deviation is 2.)
  */
 exo_gemm_status_t exo_ce_forward(exo_ce_handle_t plan, const void* x, const void* W, const int64_t* target, float* loss, float* lse,
                                  void* saved, void* cuda_stream);
