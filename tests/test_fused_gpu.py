@@ -524,6 +524,34 @@ def test_a_training_step_and_its_graph(T, F, lds, keep):
     f.check_backward(f.want(True))
 
 
+def test_first_calls_may_be_captured():
+    """In a process of its own: nothing has been launched before the capture, so kernels are loaded under it."""
+    import os
+    import subprocess
+    import sys
+    code = """
+import torch, test_fused_gpu as T
+from paper_2609_16389_b200 import fused as E
+f, c = T.Ffn(70, 136, 261, "bf16", "silu", True, seed=21), T.Ce(70, 136, 1003, "bf16", True, keep=100000, piece=256, seed=22)
+(_, _, W), x = T.codes_of(136, 136, T.gen(1)), torch.randn(70, 136, device="cuda").bfloat16()
+codes, scales, y = torch.empty(70, 144, device="cuda", dtype=torch.int8), torch.empty(70, device="cuda"), torch.empty(70, 136, device="cuda")
+X = E.I8(70, 136, 144, codes.data_ptr(), scales.data_ptr())
+torch.cuda.synchronize()
+graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+with torch.cuda.stream(side), torch.cuda.graph(graph, stream=side):
+    T.training_step(f, c)
+    X.quantize(x.data_ptr(), 136, E.BF16, T.stream())
+    W.gemm(X, y.data_ptr(), 136, E.FP32, stream=T.stream())
+graph.replay()
+torch.cuda.synchronize()
+f.check_backward(f.want(True))
+assert torch.isfinite(y).all() and y.abs().max() > 0
+"""
+    tests = os.path.dirname(os.path.abspath(__file__))
+    env = dict(os.environ, PYTHONPATH=os.pathsep.join((os.path.dirname(tests), tests)))
+    assert subprocess.run([sys.executable, "-c", code], env=env, timeout=300).returncode == 0
+
+
 def test_plans_side_by_side():
     """Two plans at once on two streams: they share nothing."""
     pairs = [(Ffn(150, 136, 264, "bf16", "silu", True, seed=s), Ce(150, 136, 515, "bf16", True, seed=s + 1), torch.cuda.Stream()) for s in (30, 40)]
