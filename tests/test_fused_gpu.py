@@ -16,10 +16,10 @@ def gen(seed):
 
 
 def strided(rows, cols, dtype, g, ld=0, scale=1.0, fill=None):
-    """A rows x cols view of a matrix with leading dimension ld, whose gap holds NaN (or `fill`)."""
+    """A rows x cols view of a matrix with leading dimension ld, whose gap holds NaN (or `fill`), and so do two rows behind it."""
     ld = ld or cols
-    whole = torch.full((rows, ld), float("nan") if fill is None else fill, device="cuda", dtype=dtype)
-    view = whole[:, :cols]
+    whole = torch.full((rows + 2, ld), float("nan") if fill is None else fill, device="cuda", dtype=dtype)
+    view = whole[:rows, :cols]
     if g is not None:
         view.copy_(torch.randn(rows, cols, device="cuda", generator=g) * scale)
     return whole, view
@@ -45,7 +45,7 @@ class Ffn:
         self.dd0, self.ddown = strided(H, F, gt, None, ldd, fill=7.0)
         self.act = act
         self.plan = E.FfnPlan(E.FfnDesc(T, H, F, code, ACT[act], int(train), gcode, ldx, ldy, ldg, ldd))
-        self.saved = torch.full((max(1, self.plan.saved_bytes()),), 255, device="cuda", dtype=torch.uint8)   # NaN, if it were read
+        self.saved = torch.full((self.plan.saved_bytes() + 256,), 255, device="cuda", dtype=torch.uint8)   # NaN, if it were read
 
     def forward(self, saved=True):
         self.plan.forward(self.x0.data_ptr(), self.gu0.data_ptr(), self.d0.data_ptr(), self.y0.data_ptr(), self.saved.data_ptr() if saved else 0,
@@ -61,16 +61,19 @@ class Ffn:
     def check_forward(self, want):
         self.plan.check()
         R.check(self.y, want["y"], "y")
+        assert (self.saved[self.plan.saved_bytes():] == 255).all() and (self.y0[self.y.shape[0]:] == 7.0).all()
 
     def check_backward(self, want):
         self.plan.check()
         R.check(self.dx, want["dx"], "dx")
         for name, got in (("dgate_up", self.dgate_up), ("ddown", self.ddown)):
             R.check(got, R.rounded(want[name], got.dtype), name)
+        for whole, view in ((self.dx0, self.dx), (self.dgu0, self.dgate_up), (self.dd0, self.ddown)):
+            assert (whole[view.shape[0]:] == 7.0).all()
 
     def gaps_untouched(self, train):
         for whole, view in ((self.y0, self.y),) + (((self.dx0, self.dx), (self.dgu0, self.dgate_up), (self.dd0, self.ddown)) if train else ()):
-            assert (whole[:, view.shape[1]:] == 7.0).all()
+            assert (whole[:, view.shape[1]:] == 7.0).all() and (whole[view.shape[0]:] == 7.0).all()
 
 
 FFN_SIZES = [(1, 64, 64), (1, 264, 8), (2, 8, 1), (2, 1, 3), (140, 1, 1), (70, 37, 44), (3, 4104, 40), (70, 2064, 200), (1, 72, 4100), (5, 72, 35), (33, 136, 200), (64, 520, 1100), (128, 264, 2400), (129, 264, 136), (200, 136, 72),
@@ -210,7 +213,7 @@ class Ce:
         self.dw0, self.dw = strided(V, H, gt, None, lds[1], fill=7.0)
         self.smoothing, self.ignore, self.kept = smoothing, ignore, keep != 0
         self.plan = E.CePlan(E.CeDesc(T, H, V, code, int(train), gcode, smoothing, ignore, lds[0], lds[1], keep, piece))
-        self.saved = torch.full((max(1, self.plan.saved_bytes()),), 255, device="cuda", dtype=torch.uint8)
+        self.saved = torch.full((self.plan.saved_bytes() + 256,), 255, device="cuda", dtype=torch.uint8)
 
     def forward(self, saved=True):
         self.plan.forward(self.x0.data_ptr(), self.w0.data_ptr(), self.target.data_ptr(), self.loss.data_ptr(), self.lse.data_ptr(),
@@ -230,6 +233,8 @@ class Ce:
         if "dx" in want:
             R.check(self.dx, want["dx"], "dx")
             R.check(self.dw, R.rounded(want["dw"], self.dw.dtype), "dw")
+            assert (self.dx0[self.dx.shape[0]:] == 7.0).all() and (self.dw0[self.dw.shape[0]:] == 7.0).all()
+        assert (self.saved[self.plan.saved_bytes():] == 255).all()
 
 
 CE_SIZES = [(1, 64, 64), (1, 8, 1), (3, 1, 5), (140, 1, 2), (20, 2120, 900), (100, 1096, 70), (2, 72, 7), (31, 136, 1000), (33, 264, 5001), (128, 520, 20011), (129, 264, 1003), (300, 72, 513), (513, 1032, 4099)]
@@ -441,7 +446,7 @@ def test_i8_gemm(M, N, K, out):
         # the sum's conversion and three products are rounded to 24 bits, the result to its type
         bound = 4 * 2.0 ** -24 * (alpha * real).abs()
         R.check(y, R.rounded((alpha * real, bound), out))
-        assert (y0[:, N:] == 7.0).all()
+        assert (y0[:, N:] == 7.0).all() and (y0[M:] == 7.0).all()
     _, y1 = strided(M, N, out, g, 0)
     before = y1.double()
     W.gemm(X, y1.data_ptr(), N, code, alpha, 0.5, stream())
