@@ -28,7 +28,7 @@ __device__ __forceinline__ void activate(float g, float& a, float& slope) {
     if constexpr (GRAD) slope = s * fmaf(g, 1.f - s, 1.f);
   } else if constexpr (ACT == EXO_ACT_GELU) {
     // Phi by erfc: 1 + erf would lose the digits of the left tail.  erfc is the Chebyshev fit of Press et al., Numerical Recipes in C, section 6.2,
-    // good to 1.2e-7 of the value everywhere: a third of the instructions of erfcf, which bound the backward pass's epilogue.
+    // good to 1.2e-7 of the value everywhere, with fewer instructions than erfcf: the backward pass's epilogue is exposed in products of one wave.
     const float z = 0.70710678118654752f * fabsf(g), t = __fdividef(1.f, fmaf(0.5f, z, 1.f));
     float e = fmaf(t, 0.17087277f, -0.82215223f);
     e = fmaf(t, e, 1.48851587f);
