@@ -248,6 +248,9 @@ exo_gemm_status_t exo_gemm_create_batched(exo_gemm_handle_t* out, const exo_gemm
  *             A and B are not read and C = beta*C.
  *   M == 0 or N == 0: returns OK without launching.
  *
+ * Nothing but the M x N values of C is written: neither the gaps between its rows (ldc beyond
+ * the extent) nor what follows the last row's last value.
+ *
  * The result is alpha*acc + beta*C_in evaluated in fp32, where acc is the fp32
  * tensor-core accumulation over k, then rounded to nearest-even into c_dtype.
  * For a fixed plan the result is bitwise reproducible from run to run.

@@ -20,48 +20,35 @@
 
 namespace exo {
 
-using KernelFn = void (*)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const GemmParams);
+using KernelFn = void (*)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap, const GemmParams);
 
-template <int G, int BN, int KSUB>
+// (ENDS: rows of C may end inside a 16-byte piece)
+template <int G, int BN, int KSUB, class Share, int MREP, bool ENDS>
 static KernelFn pick_out(int out) {
   switch (out) {
-    case EXO_GEMM_BF16: return exo_gemm_kernel<G, BN, kOutBf16, KSUB>;
-    case EXO_GEMM_FP16: return exo_gemm_kernel<G, BN, kOutFp16, KSUB>;
-    default:            return exo_gemm_kernel<G, BN, kOutFp32, KSUB>;
+    case EXO_GEMM_BF16: return exo_gemm_kernel<G, BN, kOutBf16, KSUB, Share, MREP, false, ENDS>;
+    case EXO_GEMM_FP16: return exo_gemm_kernel<G, BN, kOutFp16, KSUB, Share, MREP, false, ENDS>;
+    default:            return exo_gemm_kernel<G, BN, kOutFp32, KSUB, Share, MREP, false, ENDS>;
   }
 }
 
-template <int KSUB>
+template <int KSUB, bool ENDS>
 static KernelFn pick_shape(int cta_group, int bn, int out) {
-  if (cta_group == 2) return bn == 256 ? pick_out<2, 256, KSUB>(out) : pick_out<2, 128, KSUB>(out);
-  if (bn == 256) return pick_out<1, 256, KSUB>(out);
-  if (bn == 128) return pick_out<1, 128, KSUB>(out);
-  return pick_out<1, 64, KSUB>(out);
+  if (cta_group == 2) return bn == 256 ? pick_out<2, 256, KSUB, NoShare, 1, ENDS>(out) : pick_out<2, 128, KSUB, NoShare, 1, ENDS>(out);
+  if (bn == 256) return pick_out<1, 256, KSUB, NoShare, 1, ENDS>(out);
+  if (bn == 128) return pick_out<1, 128, KSUB, NoShare, 1, ENDS>(out);
+  return pick_out<1, 64, KSUB, NoShare, 1, ENDS>(out);
 }
 
 #ifdef EXO_GEMM_SHARE_PAIRS
 constexpr bool kHaveSharePairs = true;
-template <int KSUB>
-static KernelFn pick_shared(int out) {
-  switch (out) {
-    case EXO_GEMM_BF16: return exo_gemm_kernel<2, 256, kOutBf16, KSUB, SharePairs>;
-    case EXO_GEMM_FP16: return exo_gemm_kernel<2, 256, kOutFp16, KSUB, SharePairs>;
-    default:            return exo_gemm_kernel<2, 256, kOutFp32, KSUB, SharePairs>;
-  }
-}
+template <int KSUB, bool ENDS>
+static KernelFn pick_shared(int out) { return pick_out<2, 256, KSUB, SharePairs, 1, ENDS>(out); }
 #else
 constexpr bool kHaveSharePairs = false;
-template <int KSUB>
+template <int KSUB, bool ENDS>
 static KernelFn pick_shared(int) { return nullptr; }
 #endif
-
-static KernelFn pick_tall(int out) {
-  switch (out) {
-    case EXO_GEMM_BF16: return exo_gemm_kernel<2, 256, kOutBf16, 1, NoShare, 2>;
-    case EXO_GEMM_FP16: return exo_gemm_kernel<2, 256, kOutFp16, 1, NoShare, 2>;
-    default:            return exo_gemm_kernel<2, 256, kOutFp32, 1, NoShare, 2>;
-  }
-}
 
 // the instantiations that can add the parts of a cut tile onto C (fp32 C, plain tiles)
 template <int KSUB>
@@ -73,11 +60,16 @@ static KernelFn pick_reduce(int cta_group, int bn) {
   return exo_gemm_kernel<1, 64, kOutFp32, KSUB, NoShare, 1, true>;
 }
 
-static KernelFn pick_kernel(int cta_group, int bn, int ksub, int out, int pairs = 1, int mrep = 1, bool reduce = false) {
+template <bool ENDS>
+static KernelFn pick_ends(int cta_group, int bn, int ksub, int out, int pairs, int mrep) {
+  if (mrep == 2) return pick_out<2, 256, 1, NoShare, 2, ENDS>(out);
+  if (pairs == 2) return ksub == 2 ? pick_shared<2, ENDS>(out) : pick_shared<1, ENDS>(out);
+  return ksub == 2 ? pick_shape<2, ENDS>(cta_group, bn, out) : pick_shape<1, ENDS>(cta_group, bn, out);
+}
+
+static KernelFn pick_kernel(int cta_group, int bn, int ksub, int out, int pairs = 1, int mrep = 1, bool reduce = false, bool ends = false) {
   if (reduce) return ksub == 2 ? pick_reduce<2>(cta_group, bn) : pick_reduce<1>(cta_group, bn);
-  if (mrep == 2) return pick_tall(out);
-  if (pairs == 2) return ksub == 2 ? pick_shared<2>(out) : pick_shared<1>(out);
-  return ksub == 2 ? pick_shape<2>(cta_group, bn, out) : pick_shape<1>(cta_group, bn, out);
+  return ends ? pick_ends<true>(cta_group, bn, ksub, out, pairs, mrep) : pick_ends<false>(cta_group, bn, ksub, out, pairs, mrep);
 }
 
 // the one-tile-per-CTA kernel: 128 x 64 or 128 x 128 tiles
@@ -108,11 +100,15 @@ static KernelFn pick_lean_pair(int bn, int ksub, int out) {
   return ksub == 2 ? pick_lean_pair_out<128, 2>(out) : pick_lean_pair_out<128, 1>(out);
 }
 
+// Whether the rows of a plan's C end inside a 16-byte piece that the caller owns the rest of.  (An aligned copy of C is the plan's own, gaps
+// included: its rows are stored in whole pieces.)
+static bool row_ends(const Canonical& c, int repack) { return !(repack & 4) && c.N * c.c_bytes % 16 != 0; }
+
 // kernel and dynamic shared memory of a plan's configuration
-static KernelFn kernel_of(const TileConfig& cfg, int c_dtype, bool reduce) {
+static KernelFn kernel_of(const TileConfig& cfg, int c_dtype, bool reduce, bool ends) {
   if (cfg.lean && cfg.cta_group == 2) return pick_lean_pair(cfg.tile_n, cfg.ksub, c_dtype);
   if (cfg.lean) return pick_lean(cfg.tile_n, cfg.ksub, c_dtype);
-  return pick_kernel(cfg.cta_group, cfg.tile_n, cfg.ksub, c_dtype, cfg.pairs, cfg.mrep, reduce);
+  return pick_kernel(cfg.cta_group, cfg.tile_n, cfg.ksub, c_dtype, cfg.pairs, cfg.mrep, reduce, ends);
 }
 static int smem_of(const TileConfig& cfg, int c_dtype) {
   if (cfg.lean && cfg.cta_group == 2) return lean_pair_smem_bytes(cfg.tile_n, cfg.ksub, cfg.stages, c_dtype == EXO_GEMM_FP32 ? 4 : 2);
@@ -556,11 +552,8 @@ exo_gemm_status_t exo_gemm_create(exo_gemm_handle_t* out, const exo_gemm_desc_t*
   return exo_gemm_create_batched(out, desc, 1, 0, 0, 0);
 }
 
-}  // extern "C"
-
-// repack_more: matrices (4 = C) that go through an aligned copy although TMA could address them.
-static exo_gemm_status_t create_plan(exo_gemm_handle_t* out, const exo_gemm_desc_t* desc, int64_t batch_count, int64_t stride_a, int64_t stride_b,
-                                     int64_t stride_c, int repack_more) {
+exo_gemm_status_t exo_gemm_create_batched(exo_gemm_handle_t* out, const exo_gemm_desc_t* desc, int64_t batch_count,
+                                          int64_t stride_a, int64_t stride_b, int64_t stride_c) {
   if (!out) return EXO_GEMM_ERR_NULL;
   exo_gemm_status_t st = validate_batch(desc, batch_count, stride_a, stride_b, stride_c);
   if (st != EXO_GEMM_OK) return st;
@@ -584,7 +577,7 @@ static exo_gemm_status_t create_plan(exo_gemm_handle_t* out, const exo_gemm_desc
   exo_gemm_plan* p = new (std::nothrow) exo_gemm_plan{};
   if (!p) return EXO_GEMM_ERR_CUDA;
   p->user_desc = *desc;
-  p->repack = repack_mask(*desc) | repack_more;
+  p->repack = repack_mask(*desc);
   p->desc = aligned_desc(*desc, p->repack);
   p->canon = canonicalize(p->desc, batch_count, stride_a, stride_b, stride_c);
   p->device = device;
@@ -601,7 +594,7 @@ static exo_gemm_status_t create_plan(exo_gemm_handle_t* out, const exo_gemm_desc
 
   p->cfg = choose_config(p->canon, ov, sms, max_pairs, max_quads);
   p->cfg.workspace_bytes = ov.reduce_add ? 0 : split_workspace_bytes(p->cfg, desc->c_dtype);
-  p->kernel = kernel_of(p->cfg, desc->c_dtype, ov.reduce_add);
+  p->kernel = kernel_of(p->cfg, desc->c_dtype, ov.reduce_add, row_ends(p->canon, p->repack));
   p->smem_bytes = smem_of(p->cfg, desc->c_dtype);
   e = allow_full_smem(p->kernel);
   if (e != cudaSuccess) { delete p; return cuda_fail(e); }
@@ -648,22 +641,6 @@ static exo_gemm_status_t create_plan(exo_gemm_handle_t* out, const exo_gemm_desc
   }
   *out = p;
   return EXO_GEMM_OK;
-}
-
-namespace exo {
-// A plan that writes nothing but the M x N values of a row-major C: a TMA store moves 16 bytes at a time, so where a row ends inside such
-// a piece the rest of it, which belongs to the caller's gap between rows, is written as well unless C goes through a copy (fused_host.h).
-exo_gemm_status_t gemm_create_exact(exo_gemm_handle_t* out, const exo_gemm_desc_t* desc) {
-  const bool gap = desc->M > 0 && desc->N > 0 && desc->ldc > desc->N && desc->N * elem_bytes(desc->c_dtype) % 16 != 0;
-  return create_plan(out, desc, 1, 0, 0, 0, gap ? 4 : 0);
-}
-}  // namespace exo
-
-extern "C" {
-
-exo_gemm_status_t exo_gemm_create_batched(exo_gemm_handle_t* out, const exo_gemm_desc_t* desc, int64_t batch_count,
-                                          int64_t stride_a, int64_t stride_b, int64_t stride_c) {
-  return create_plan(out, desc, batch_count, stride_a, stride_b, stride_c, 0);
 }
 
 exo_gemm_status_t exo_gemm_get_info(exo_gemm_handle_t plan, exo_gemm_info_t* info) {
@@ -763,6 +740,10 @@ exo_gemm_status_t launch_plan(exo_gemm_plan* plan, const void* A, const void* B,
   prm.c_ptr = C;
   prm.ldc_bytes = cn.ldc * cn.c_bytes;
   prm.c_batch_bytes = cn.stride_c * cn.c_bytes;
+  const int64_t piece = 16 / cn.c_bytes, chunk = 128 / cn.c_bytes;
+  const bool row_end = row_ends(cn, plan->repack);
+  prm.n_whole = (int32_t)(row_end ? cn.N / piece * piece : cn.N);
+  prm.end_from = row_end ? (int32_t)(cn.N / chunk * chunk) : INT32_MAX;
   // the tail tiles are cut along K only when there is a K loop to cut and scratch to reduce through
   const bool split_now = cfg.tail_workers > 0 && read_ab && plan->d_tail_table != nullptr;   // (the table exists for every cutting plan)
   const bool reduce_add = split_now && (d.flags & (1u << 11)) != 0;
@@ -791,13 +772,14 @@ exo_gemm_status_t launch_plan(exo_gemm_plan* plan, const void* A, const void* B,
   prm.timeout_cycles = (uint64_t)(dbg_ms > 0 ? dbg_ms : 4000) * 2000000ull;
   prm.debug_skip_k_block = plan->dbg_skip_k_block.exchange(-1);
 
-  CUtensorMap tm_a, tm_b, tm_c;
+  CUtensorMap tm_a, tm_b, tm_c, tm_cin;   // tm_c: for the stores; tm_cin: for reading C
   memset(&tm_a, 0, sizeof tm_a);
   memset(&tm_b, 0, sizeof tm_b);
   CUresult r;
   const int b_rows = cfg.tile_n / cfg.cta_group;
   const int a_rows = kBlockM * cfg.mrep / cfg.pairs;  // pairs that share A fetch half of a CTA's rows each
   const uint32_t c_box = d.c_dtype == EXO_GEMM_FP32 ? 32 : 64;
+  const uint64_t stored = prm.n_whole > 0 ? (uint64_t)prm.n_whole : (uint64_t)piece;   // (a map is not empty; rows shorter than a piece use none)
   const bool atom32 = d.ab_dtype == EXO_GEMM_FP32;   // only read for M/N-contiguous operands
   if (cn.batch <= 1) {
     if (read_ab) {
@@ -808,7 +790,8 @@ exo_gemm_status_t launch_plan(exo_gemm_plan* plan, const void* A, const void* B,
                         : encode_2d(&tm_b, d.ab_dtype, opB, cn.K, cn.N, cn.ldb, sub_k, b_rows, true);
       if (r != CUDA_SUCCESS) { g_last_cuda_error = (int)r; return EXO_GEMM_ERR_CUDA; }
     }
-    r = encode_2d(&tm_c, d.c_dtype, C, cn.N, cn.M, cn.ldc, c_box, 32, false);
+    r = encode_2d(&tm_cin, d.c_dtype, C, cn.N, cn.M, cn.ldc, c_box, 32, false);
+    if (r == CUDA_SUCCESS && row_end) r = encode_2d(&tm_c, d.c_dtype, C, stored, cn.M, cn.ldc, c_box, 32, false);
     if (r != CUDA_SUCCESS) { g_last_cuda_error = (int)r; return EXO_GEMM_ERR_CUDA; }
   } else {  // strided batch: the matrix index is the third tensor-map coordinate
     if (read_ab) {
@@ -821,9 +804,11 @@ exo_gemm_status_t launch_plan(exo_gemm_plan* plan, const void* A, const void* B,
               : encode_3d(&tm_b, d.ab_dtype, opB, cn.K, cn.N, cn.ldb, cn.batch, cn.stride_b, sub_k, b_rows, true);
       if (r != CUDA_SUCCESS) { g_last_cuda_error = (int)r; return EXO_GEMM_ERR_CUDA; }
     }
-    r = encode_3d(&tm_c, d.c_dtype, C, cn.N, cn.M, cn.ldc, cn.batch, cn.stride_c, c_box, 32, false);
+    r = encode_3d(&tm_cin, d.c_dtype, C, cn.N, cn.M, cn.ldc, cn.batch, cn.stride_c, c_box, 32, false);
+    if (r == CUDA_SUCCESS && row_end) r = encode_3d(&tm_c, d.c_dtype, C, stored, cn.M, cn.ldc, cn.batch, cn.stride_c, c_box, 32, false);
     if (r != CUDA_SUCCESS) { g_last_cuda_error = (int)r; return EXO_GEMM_ERR_CUDA; }
   }
+  if (!row_end) tm_c = tm_cin;
   if (!read_ab) { tm_a = tm_c; tm_b = tm_c; }  // never dereferenced for data; keeps the prefetch valid
 
   DeviceGuard guard(plan->device);
@@ -865,7 +850,7 @@ exo_gemm_status_t launch_plan(exo_gemm_plan* plan, const void* A, const void* B,
   }
   // (The arrival counters of a K-slicing plan need nothing from the host per run: which run this is follows
   // from a second counter on the device, so the same parameters can be replayed from a CUDA graph.)
-  e = cudaLaunchKernelEx(&lc, plan->kernel, tm_a, tm_b, tm_c, prm);
+  e = cudaLaunchKernelEx(&lc, plan->kernel, tm_a, tm_b, tm_c, tm_cin, prm);
   if (e != cudaSuccess) return cuda_fail(e);
   return EXO_GEMM_OK;
 }
@@ -1011,7 +996,7 @@ exo_gemm_status_t exo_gemm_run_static(const exo_gemm_desc_t* desc, const void* A
   if (e != cudaSuccess) return cuda_fail(e);
   if (ov.share >= 2 && max_quads < 1) return EXO_GEMM_ERR_UNSUPPORTED;
   plan.cfg = choose_config(plan.canon, ov, sms, max_pairs, max_quads);
-  plan.kernel = kernel_of(plan.cfg, desc->c_dtype, false);
+  plan.kernel = kernel_of(plan.cfg, desc->c_dtype, false, row_ends(plan.canon, 0));
   plan.smem_bytes = smem_of(plan.cfg, desc->c_dtype);
   e = allow_full_smem(plan.kernel);
   if (e != cudaSuccess) return cuda_fail(e);

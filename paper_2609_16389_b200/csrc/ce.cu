@@ -431,13 +431,13 @@ exo_gemm_status_t products(exo_ce_plan* p, int which, int64_t columns, int64_t l
   g.c_dtype = several ? EXO_GEMM_FP32 : d.dtype;
   g.a_layout = g.b_layout = EXO_GEMM_ROW_MAJOR;
   g.lda = ldd; g.ldb = p->ldw; g.ldc = several ? round_up(d.hidden, 64) : d.ldx;
-  exo_gemm_status_t st = gemm_create_exact(&p->dx[which], &g);
+  exo_gemm_status_t st = exo_gemm_create(&p->dx[which], &g);
   if (st != EXO_GEMM_OK) return st;
   g.M = columns; g.N = d.hidden; g.K = d.tokens;          // dW = d^T x
   g.c_dtype = d.grad_dtype;
   g.a_layout = EXO_GEMM_COL_MAJOR;
   g.lda = ldd; g.ldb = p->ldx; g.ldc = d.ldw;
-  return gemm_create_exact(&p->dw[which], &g);
+  return exo_gemm_create(&p->dw[which], &g);
 }
 
 }  // namespace

@@ -277,7 +277,7 @@ exo_gemm_status_t product(exo_gemm_handle_t* out, const exo_ffn_plan* p, int64_t
   g.a_layout = a_layout; g.b_layout = b_layout; g.c_layout = EXO_GEMM_ROW_MAJOR;
   g.lda = lda; g.ldb = ldb; g.ldc = ldc;
   g.device = p->device;
-  return gemm_create_exact(out, &g);
+  return exo_gemm_create(out, &g);
 }
 
 // the saved g and u are read 32 bytes at a time

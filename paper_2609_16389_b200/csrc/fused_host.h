@@ -19,7 +19,6 @@ bool encode_operand_map(CUtensorMap* map, int elem_bytes, bool bf16, const void*
 bool encode_blocks_map(CUtensorMap* whole, CUtensorMap* rest, int elem_bytes, bool bf16, const void* base, uint64_t inner, uint64_t rows,
                        uint64_t row_bytes, uint64_t parts, uint64_t part_bytes, uint32_t box_rows, uint32_t box_blocks);   // api.cu
 bool encode_result_map(CUtensorMap* map, void* base, uint64_t cols, uint64_t rows, uint64_t row_bytes);   // api.cu
-exo_gemm_status_t gemm_create_exact(exo_gemm_handle_t* out, const exo_gemm_desc_t* desc);   // api.cu
 exo_gemm_status_t gemm_run_scaled(exo_gemm_plan* plan, const void* A, const void* B, void* C, float alpha, const float* alpha_dev, float beta,
                                   void* cuda_stream);   // api.cu
 

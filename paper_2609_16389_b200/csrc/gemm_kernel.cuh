@@ -131,6 +131,45 @@ __device__ __forceinline__ float2 unpack2(uint32_t w) {
   }
 }
 
+// The values of a lane's row behind its last whole 16 bytes (GemmParams::n_whole), from where the lane has staged the chunk at column `col`:
+// its 128 bytes at my_row, pieces swizzled by my_xor.  ADD: onto what is there.  Both the row's end in C and its place in the staged row
+// start on 16 bytes, so halves, quarters and eighths of a piece are aligned.
+template <int OUT, bool ADD = false>
+__device__ __forceinline__ void store_row_end(const GemmParams& p, uint32_t my_row, uint32_t my_xor, int32_t col, int32_t row, uint32_t bz) {
+  constexpr uint32_t ES = OUT == kOutFp32 ? 4 : 2;
+  if (row >= p.M) return;
+  uint32_t from = my_row + (((uint32_t)(p.n_whole - col) * ES) ^ my_xor);
+  char* to = static_cast<char*>(p.c_ptr) + (int64_t)bz * p.c_batch_bytes + (int64_t)row * p.ldc_bytes + (int64_t)p.n_whole * (int)ES;
+  const uint32_t bytes = (uint32_t)(p.N - p.n_whole) * ES;
+  if (bytes & 8u) {
+    uint32_t a, b;
+    asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(a), "=r"(b) : "r"(from) : "memory");
+    if constexpr (ADD) {
+      atomicAdd(reinterpret_cast<float*>(to), __uint_as_float(a));
+      atomicAdd(reinterpret_cast<float*>(to) + 1, __uint_as_float(b));
+    } else {
+      *reinterpret_cast<uint2*>(to) = make_uint2(a, b);
+    }
+    from += 8u;
+    to += 8;
+  }
+  if (bytes & 4u) {
+    uint32_t a;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(a) : "r"(from) : "memory");
+    if constexpr (ADD) atomicAdd(reinterpret_cast<float*>(to), __uint_as_float(a));
+    else *reinterpret_cast<uint32_t*>(to) = a;
+    from += 4u;
+    to += 4;
+  }
+  if constexpr (ES == 2) {
+    if (bytes & 2u) {
+      uint16_t a;
+      asm volatile("ld.shared.u16 %0, [%1];" : "=h"(a) : "r"(from) : "memory");
+      *reinterpret_cast<uint16_t*>(to) = a;
+    }
+  }
+}
+
 // Default policy: a CTA group loads all of its own operands.  The alternative (a cluster of two
 // CTA pairs that split the loads of the A rows they have in common) supplies kPairs == 2 and the
 // load functions for the shared half-blocks; it lives in a translation unit of its own.
@@ -145,10 +184,11 @@ struct NoShare {
 // REDUCE: the kernel can add the parts of a cut tile onto C (p.reduce_add); compiled only into the few
 // instantiations that plans with that flag use -- the extra paths cost the others 1-2 % where the epilogue
 // bounds a tile.
-template <int CTA_GROUP, int BN, int OUT, int KSUB, class Share = NoShare, int MREP = 1, bool REDUCE = false>
+// ENDS: rows of C may end inside a 16-byte piece (see GemmParams::n_whole); likewise an instantiation of its own (fp32 C, K = 512: 2 %).
+template <int CTA_GROUP, int BN, int OUT, int KSUB, class Share = NoShare, int MREP = 1, bool REDUCE = false, bool ENDS = REDUCE>
 __global__ void __launch_bounds__(kNumThreads, 1)
 exo_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b,
-                const __grid_constant__ CUtensorMap tm_c, const GemmParams p) {
+                const __grid_constant__ CUtensorMap tm_c, const __grid_constant__ CUtensorMap tm_cin, const GemmParams p) {
   const int32_t STAGE_K = (int32_t)p.sub_k * KSUB;   // k-elements per stage (64 or 32 per sub-block)
   constexpr int B_ROWS = BN / CTA_GROUP;             // rows of the B tile this CTA stages
   constexpr int STAGE_BYTES = stage_bytes(CTA_GROUP, BN, KSUB, MREP);
@@ -735,8 +775,8 @@ exo_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant_
       auto issue_cin = [&](uint32_t gg, int32_t i) {  // elected lane only: C_in of this warp's i-th chunk
         const uint32_t b = two_bufs ? (gg & 1u) : 0u;
         ptx::mbar_arrive_expect_tx(cin_bar(ew, b), kEpiBufBytes);
-        if (batched) ptx::tma_load_3d(buf0 + b * kEpiBufBytes, &tm_c, col0 + chunk_of(i) * CW, row0, (int32_t)bz, cin_bar(ew, b));
-        else ptx::tma_load_2d(buf0 + b * kEpiBufBytes, &tm_c, col0 + chunk_of(i) * CW, row0, cin_bar(ew, b));
+        if (batched) ptx::tma_load_3d(buf0 + b * kEpiBufBytes, ENDS ? &tm_cin : &tm_c, col0 + chunk_of(i) * CW, row0, (int32_t)bz, cin_bar(ew, b));
+        else ptx::tma_load_2d(buf0 + b * kEpiBufBytes, ENDS ? &tm_cin : &tm_c, col0 + chunk_of(i) * CW, row0, cin_bar(ew, b));
       };
       if (mine > 0 && has_beta && two_bufs && !direct) {
         if (ptx::elect_one()) {
@@ -893,7 +933,8 @@ exo_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant_
             ptx::fence_proxy_async_smem();  // generic-proxy writes -> visible to the TMA store
             __syncwarp();
             if (ptx::elect_one()) {
-              if (tile_reduce) {
+              if (ENDS && col >= p.n_whole) {   // nothing but the row's end
+              } else if (tile_reduce) {
                 if (batched) ptx::tma_reduce_add_3d(&tm_c, col, row0, (int32_t)bz, buf0 + boff);
                 else ptx::tma_reduce_add_2d(&tm_c, col, row0, buf0 + boff);
               } else if (p.c_evict_first) {
@@ -914,6 +955,16 @@ exo_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant_
         }
       }
       if (!ok) break;
+      if constexpr (ENDS) {
+        const int32_t last = col0 + chunk_of(mine - 1) * CW;
+        if (last >= p.end_from && mine > 0) {   // the rows end inside a piece of this warp's last chunk, which is still staged
+          const uint32_t boff = two_bufs ? ((g - 1u) & 1u) * kEpiBufBytes : 0u;
+          if (REDUCE && tile_reduce) store_row_end<OUT, REDUCE>(p, my_row + boff, my_xor, last, row0 + (int32_t)lane, bz);
+          else store_row_end<OUT>(p, my_row + boff, my_xor, last, row0 + (int32_t)lane, bz);
+          ptx::fence_proxy_async_smem();   // read before a copy may be issued into this buffer
+          __syncwarp();
+        }
+      }
       }  // accumulators of the tile
       if (!ok) break;
       if (wi.slices > 1 && wi.slice == 0 && !preloaded && !(REDUCE && p.reduce_add)) partials_consumed(wi.tail_index);

@@ -118,8 +118,12 @@ struct GemmParams {
   uint32_t c_evict_first;   // 1: the stores of C carry the L2 evict-first priority
   uint32_t reduce_add;      // 1: the parts of a cut tile add onto C (TMA reduce) instead of meeting in the workspace
   uint32_t split_arrivals;  // arrivals per contributing part of a tile and run: its epilogue warps (x accumulators)
-  void* c_ptr;              // C of matrix 0 and its strides in bytes (read by the direct stores only)
+  void* c_ptr;              // C of matrix 0 and its strides in bytes (for stores other than by TMA)
   int64_t ldc_bytes, c_batch_bytes;
+  // A TMA store writes whole 16-byte pieces.  Where a row of C ends inside one, what follows is the caller's: the map of the stores then has
+  // n_whole columns, and the rest of a row is stored by its lane (store_row_end).
+  int32_t n_whole;          // N, or N rounded down to whole pieces
+  int32_t end_from;         // the column from which a chunk holds such a row end (INT32_MAX: there is none)
   uint32_t* status;         // device: 8 words {code, role, barrier, tile, k_block, cta, -, -}
   uint64_t timeout_cycles;  // bound of every device-side wait, in SM clocks
   int64_t debug_skip_k_block;  // -1, or the producer k-block of CTA 0 whose loads are skipped

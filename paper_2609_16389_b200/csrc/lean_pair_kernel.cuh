@@ -25,7 +25,7 @@ namespace exo {
 template <int BN, int OUT, int KSUB>
 __global__ void __launch_bounds__(kLeanPairThreads, 1)
 exo_gemm_lean_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b,
-                          const __grid_constant__ CUtensorMap tm_c, const GemmParams p) {
+                          const __grid_constant__ CUtensorMap tm_c, const __grid_constant__ CUtensorMap tm_cin, const GemmParams p) {
   static_assert(BN == 128 || BN == 256, "tile N");
   constexpr int C_BYTES = OUT == kOutFp32 ? 4 : 2;
   constexpr int CW = 128 / C_BYTES;                  // columns per chunk = 128 bytes of C
@@ -224,7 +224,7 @@ exo_gemm_lean_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid
     if (ok && has_beta && mine > 0 && ptx::elect_one()) {   // C_in of all of this warp's chunks at once
       ptx::mbar_arrive_expect_tx(cin_bar(ew), (uint32_t)mine * kEpiBufBytes);
       for (int32_t i = 0; i < mine; ++i)
-        ptx::tma_load_2d(buf0 + (uint32_t)i * kEpiBufBytes, &tm_c, col0 + (first_chunk + i) * CW, row0, cin_bar(ew));
+        ptx::tma_load_2d(buf0 + (uint32_t)i * kEpiBufBytes, &tm_cin, col0 + (first_chunk + i) * CW, row0, cin_bar(ew));
     }
     __syncwarp();
     const uint32_t tacc = tmem_base + ((quad * 32u) << 16);
@@ -301,15 +301,19 @@ exo_gemm_lean_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid
         }
       }
       EXO_TRACE_CHUNK(i, 2);
+      const int32_t col = col0 + (first_chunk + i) * CW;
       ptx::fence_proxy_async_smem();   // generic-proxy writes -> visible to the TMA store
       __syncwarp();
       if (ptx::elect_one()) {
-        ptx::tma_store_2d(&tm_c, col0 + (first_chunk + i) * CW, row0, buf0 + (uint32_t)i * kEpiBufBytes);
+        if (col < p.n_whole) ptx::tma_store_2d(&tm_c, col, row0, buf0 + (uint32_t)i * kEpiBufBytes);
         ptx::bulk_commit();
       }
       EXO_TRACE_CHUNK(i, 3);
     }
     if (ok) {
+      const int32_t last = col0 + (first_chunk + mine - 1) * CW;
+      if (last >= p.end_from && mine > 0)   // the rows end inside a piece of this warp's last chunk
+        store_row_end<OUT>(p, buf0 + (uint32_t)(mine - 1) * kEpiBufBytes + lane * 128u, my_xor, last, row0 + (int32_t)lane, 0);
       // the stores must have read this warp's buffers before the CTA leaves
       if (warp == 2 && lane == 0) EXO_TRACE(2, 0, 1, 4096);
       if (ptx::elect_one()) ptx::bulk_wait_read<0>();
