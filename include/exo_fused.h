@@ -127,8 +127,9 @@ exo_gemm_status_t exo_ce_validate(const exo_ce_desc_t* desc);
 exo_gemm_status_t exo_ce_create(exo_ce_handle_t* out, const exo_ce_desc_t* desc);
 
 /*
- * Bytes of the buffer in which a forward call leaves exponentials exp(l_iv - largest of the row's columns computed together), in dtype,
- * for the backward call: for as many columns of the vocabulary as keep_bytes has room for.  The backward call recomputes the logits of
+ * Bytes of the buffer in which a forward call leaves exponentials exp(l_iv - largest of the row's columns computed together), in dtype
+ * (fp16: times 2^15, so that they are kept to 2^-29 of that largest with all bits), for the backward call: for as many columns of the
+ * vocabulary as keep_bytes has room for.  The backward call recomputes the logits of
  * the other columns, a piece at a time: a third more arithmetic for the part that is not kept.
  */
 int64_t exo_ce_saved_bytes(exo_ce_handle_t plan);

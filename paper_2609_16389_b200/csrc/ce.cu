@@ -17,6 +17,10 @@ namespace exo {
 namespace fused {
 namespace {
 
+// What a kept exponential is multiplied by.  They are at most 1, and fp16 has no normal numbers below 2^-14: from 2^15 on they reach down to 2^-29 of
+// their part's largest with all of their bits, and to 2^-39 with one.  bf16 has fp32's range.
+template <class T> constexpr float kKeptScale = 1.f;
+template <> constexpr float kKeptScale<Fp16> = 32768.f;
 constexpr float kTop = 16384.f;   // what the largest |dloss| becomes in q: |d| <= 2^14 in fp16, and 2^-24 / 2^14 is its smallest step
 
 // ---------------------------------------------------------------- parts of the rows
@@ -94,6 +98,10 @@ struct StatsOp {
       o.hit[row] = l;   // one thread in all has this column
     }
     if (o.e && col < o.keep) {
+      if constexpr (kKeptScale<T> != 1.f) {
+#pragma unroll
+        for (int k = 0; k < U; ++k) e[k] *= kKeptScale<T>;
+      }
       if constexpr (U == 32) {
         uint32_t w[16];
         pack<T, U>(e, w);
@@ -292,7 +300,7 @@ __global__ void __launch_bounds__(kRescaleThreads) exo_ce_rescale_kernel(const R
   for (int r = 0; r < kRescaleRows; ++r) {
     const int64_t row = row0 + r;
     if (row >= p.rows) break;
-    const float q = p.q[row], f = __expf(p.top[(int64_t)part * p.top_rows + row] - p.lse[row]);
+    const float q = p.q[row], f = __expf(p.top[(int64_t)part * p.top_rows + row] - p.lse[row]) * (1.f / kKeptScale<T>);
     const int64_t t = p.target[row] - col;
     float d[8];
 #pragma unroll

@@ -636,3 +636,18 @@ def test_a_wait_that_runs_out_is_reported(T):
     g.forward(saved=False)
     g.plan.check()
     assert torch.equal(g.y, good)
+
+
+def test_ce_keeps_rare_columns_in_fp16():
+    """Peaked rows: most columns' probabilities lie far below fp16's smallest part of the row's largest, and the kept exponentials still hold them."""
+    c = Ce(140, 72, 1000, "fp16", True, grad="fp32", seed=15, spread=6.0)
+    c.forward()
+    c.backward()
+    bare = R.ce(c.x, c.w, c.target, dloss=c.dloss, kept=False)
+    # what keeping may add: half a step of the exponential, relative, and half of fp16's smallest step where the row's largest is 2^15
+    l = c.x.double() @ c.w.double().t()
+    p = torch.softmax(l, 1)
+    kept = c.dloss.double()[:, None] * (p * 2.0 ** -11 + 2.0 ** -40 * p.amax(1, keepdim=True)) * (1 + 2.0 ** -10)
+    assert (p < 1e-7 * p.amax(1, keepdim=True)).double().mean() > 0.3
+    c.check({"loss": bare["loss"], "lse": bare["lse"], "dx": (bare["dx"][0], bare["dx"][1] + (1 + 2.0 ** -10) * (kept @ c.w.double().abs())),
+             "dw": (bare["dw"][0], bare["dw"][1] + kept.t() @ c.x.double().abs())})
