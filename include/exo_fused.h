@@ -87,7 +87,11 @@ exo_gemm_status_t exo_ffn_forward(exo_ffn_handle_t plan, const void* x, const vo
 exo_gemm_status_t exo_ffn_backward(exo_ffn_handle_t plan, const void* x, const void* gate_up, const void* down, const void* saved,
                                    const void* dy, void* dx, void* d_gate_up, void* d_down, int32_t accumulate, void* cuda_stream);
 
-/* As exo_fused_check, and for the plan's own products too. */
+/*
+ * Waits for the plan's device and returns EXO_GEMM_ERR_DEVICE_TIMEOUT if a bounded device-side wait of one of this plan's kernels, its own
+ * products' included, has given up since the last such call for this plan, else EXO_GEMM_OK.  What that call computed, and what the plan
+ * computed from then on, is then wrong; other plans are not concerned.
+ */
 exo_gemm_status_t exo_ffn_check(exo_ffn_handle_t plan);
 /* Device memory the plan owns, in bytes. */
 int64_t exo_ffn_workspace_bytes(exo_ffn_handle_t plan);
@@ -155,7 +159,7 @@ exo_gemm_status_t exo_ce_forward(exo_ce_handle_t plan, const void* x, const void
 exo_gemm_status_t exo_ce_backward(exo_ce_handle_t plan, const void* x, const void* W, const int64_t* target, const float* lse,
                                   const float* dloss, void* saved, void* dx, void* dW, int32_t accumulate, void* cuda_stream);
 
-/* As exo_fused_check, and for the plan's own products too. */
+/* As exo_ffn_check. */
 exo_gemm_status_t exo_ce_check(exo_ce_handle_t plan);
 /* Device memory the plan owns, in bytes. */
 int64_t exo_ce_workspace_bytes(exo_ce_handle_t plan);
@@ -192,7 +196,9 @@ exo_gemm_status_t exo_gemm_i8_run(const exo_i8_t* X, const exo_i8_t* W, void* Y,
 /* ---------------------------------------------------------------- device-side waits */
 /*
  * Waits for the current device and returns EXO_GEMM_ERR_DEVICE_TIMEOUT if a bounded device-side wait of a kernel of this header has
- * given up since the last call (what that launch computed, and what was launched after it, is then wrong), else EXO_GEMM_OK.
+ * given up there since the last call of this function, else EXO_GEMM_OK.  Whose wait it was a plan's own check tells, and this call takes
+ * nothing away from that.  The 8-bit products have no plan and share one report on a device, this one: from a wait that gave up until
+ * this call, what any of them computes may be wrong.
  */
 exo_gemm_status_t exo_fused_check(void);
 

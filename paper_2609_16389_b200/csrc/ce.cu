@@ -355,6 +355,7 @@ struct exo_ce_plan {
   int bn_piece;
   int64_t ldx, ldw;      // as the kernels see them
   Memory mem;
+  uint32_t* gave_up;
   float *top, *sum, *all, *hit, *q, *factor, *dx_sum;
   uint16_t *pieces, *pack_x, *pack_w;
   exo_gemm_handle_t dx[3], dw[3];   // the products of the kept columns, of a whole piece and of the last one
@@ -411,9 +412,9 @@ exo_gemm_status_t forward(exo_ce_plan* p, const void* x, const void* W, const in
   o.vocab = (int32_t)d.vocab;
   const Operand X{x, d.tokens, d.hidden, p->ldx}, Wo{W, d.vocab, d.hidden, p->ldw};
   const bool bf16 = d.dtype == EXO_GEMM_BF16;
-  if (p->thin) return launch_thin<StatsOp<T>, 16>(p->width, X, Wo, d.vocab, d.hidden, 0, bf16, p->sms, o, stream);
-  return saved ? launch_pair<StatsOp<T>, false>(p->width, X, Wo, d.vocab, d.hidden, 0, bf16, p->sms, o, {Result{saved, p->lde, p->lde}}, stream)
-               : launch_pair<StatsOp<T>, false>(p->width, X, Wo, d.vocab, d.hidden, 0, bf16, p->sms, o, {}, stream);
+  if (p->thin) return launch_thin<StatsOp<T>, 16>(p->width, X, Wo, d.vocab, d.hidden, 0, bf16, p->sms, o, p->gave_up, stream);
+  return saved ? launch_pair<StatsOp<T>, false>(p->width, X, Wo, d.vocab, d.hidden, 0, bf16, p->sms, o, {Result{saved, p->lde, p->lde}}, p->gave_up, stream)
+               : launch_pair<StatsOp<T>, false>(p->width, X, Wo, d.vocab, d.hidden, 0, bf16, p->sms, o, {}, p->gave_up, stream);
 }
 
 template <class T>
@@ -426,7 +427,7 @@ exo_gemm_status_t recompute(exo_ce_plan* p, const void* x, const void* W, const 
   o.rest = d.label_smoothing / (float)d.vocab;
   const Operand Wo{(const uint16_t*)W + first * p->ldw, columns, d.hidden, p->ldw};
   return launch_pair<GradOp<T>, false>(p->bn_piece, Operand{x, d.tokens, d.hidden, p->ldx}, Wo, columns, d.hidden, 0, d.dtype == EXO_GEMM_BF16, p->sms, o,
-                                       {Result{p->pieces, p->ldd, p->ldd}}, stream);
+                                       {Result{p->pieces, p->ldd, p->ldd}}, p->gave_up, stream);
 }
 
 exo_gemm_status_t products(exo_ce_plan* p, int which, int64_t columns, int64_t ldd, bool several) {
@@ -500,6 +501,7 @@ exo_gemm_status_t exo_ce_create(exo_ce_handle_t* out, const exo_ce_desc_t* desc)
   const int64_t rest = p->piece ? (V - p->keep) % p->piece : 0;
   const bool several = p->piece > 0 && (p->keep > 0 || p->piece < V);   // dx is a sum of more than one product
   if (T > 0) {
+    p->gave_up = p->mem.take_word();
     p->top = (float*)p->mem.take(4 * T * p->parts);
     p->sum = (float*)p->mem.take(4 * T * p->parts);
     if (d.label_smoothing > 0.f) p->all = (float*)p->mem.take(4 * T * p->parts);
@@ -655,7 +657,7 @@ exo_gemm_status_t exo_ce_check(exo_ce_handle_t p) {
   if (!p) return EXO_GEMM_ERR_NULL;
   OnDevice on(p->device);
   if (on.err != cudaSuccess) return cuda_failed(on.err);
-  return check_products({p->dx[0], p->dx[1], p->dx[2], p->dw[0], p->dw[1], p->dw[2]}, exo_fused_check());
+  return check_plan(p->gave_up, {p->dx[0], p->dx[1], p->dx[2], p->dw[0], p->dw[1], p->dw[2]});
 }
 
 int64_t exo_ce_workspace_bytes(exo_ce_handle_t p) {

@@ -234,6 +234,7 @@ struct exo_ffn_plan {
   int64_t ldh, ld2;                    // of h (and g, u) and of dg | du
   int64_t ldx, ldy, ld_gate_up, ld_down;   // as the kernels see them: of the aligned copies where there are some
   Memory mem;
+  uint32_t* gave_up;
   uint16_t *h, *dgu;
   uint16_t *pack_x, *pack_dy, *pack_gate_up, *pack_down;
   exo_gemm_handle_t down, dx, d_gate_up, d_down;
@@ -295,10 +296,10 @@ exo_gemm_status_t forward(exo_ffn_plan* p, const void* x, const void* gate_up, c
   exo_gemm_status_t st;
   if (!p->thin) {
     const Result H{p->h, p->ldh, p->ldh}, G{gp.g, p->ldh, p->ldh}, U{gp.u, p->ldh, p->ldh};
-    st = saved ? launch_pair<GatedOp<T>, false>(p->bn_gated, X, GU, d.inner, d.hidden, d.inner, bf16, p->sms, gp, {H, G, U}, stream)
-               : launch_pair<GatedOp<T>, false>(p->bn_gated, X, GU, d.inner, d.hidden, d.inner, bf16, p->sms, gp, {H}, stream);
+    st = saved ? launch_pair<GatedOp<T>, false>(p->bn_gated, X, GU, d.inner, d.hidden, d.inner, bf16, p->sms, gp, {H, G, U}, p->gave_up, stream)
+               : launch_pair<GatedOp<T>, false>(p->bn_gated, X, GU, d.inner, d.hidden, d.inner, bf16, p->sms, gp, {H}, p->gave_up, stream);
   } else {
-    st = launch_thin<GatedOp<T>, 8>(p->width_gated, X, GU, d.inner, d.hidden, d.inner, bf16, p->sms, gp, stream);
+    st = launch_thin<GatedOp<T>, 8>(p->width_gated, X, GU, d.inner, d.hidden, d.inner, bf16, p->sms, gp, p->gave_up, stream);
   }
   if (st != EXO_GEMM_OK) return st;
   if (p->pack_down) {   // the copy of down goes on beside the first product
@@ -308,7 +309,7 @@ exo_gemm_status_t forward(exo_ffn_plan* p, const void* x, const void* gate_up, c
   if (!p->thin) return gemm_run_scaled(p->down, p->h, down, y, 1.f, nullptr, 0.f, stream);
   typename PlainOp<T>::Params yp{(uint16_t*)y, d.ldy, align_of(y, d.ldy * 2)};
   return launch_thin<PlainOp<T>, 16>(p->width_down, Operand{p->h, d.tokens, d.inner, p->ldh}, Operand{down, d.hidden, d.inner, p->ld_down}, d.hidden, d.inner,
-                                     0, bf16, p->sms, yp, stream);
+                                     0, bf16, p->sms, yp, p->gave_up, stream);
 }
 
 template <class T>
@@ -319,8 +320,8 @@ exo_gemm_status_t back(exo_ffn_plan* p, const void* down, const uint16_t* saved,
   const Operand dY{dy, d.tokens, d.hidden, p->ldy}, Wd{down, d.hidden, d.inner, p->ld_down};
   const Result H{p->h, p->ldh, p->ldh}, G{p->dgu, d.inner, p->ld2}, U{p->dgu + d.inner, d.inner, p->ld2};
   const bool bf16 = d.dtype == EXO_GEMM_BF16;
-  return bp.aligned ? launch_pair<GatedBackOp<T>, true>(p->bn_back, dY, Wd, d.inner, d.hidden, 0, bf16, p->sms, bp, {H, G, U}, stream)
-                    : launch_pair<GatedBackOp<T>, true>(p->bn_back, dY, Wd, d.inner, d.hidden, 0, bf16, p->sms, bp, {H}, stream);
+  return bp.aligned ? launch_pair<GatedBackOp<T>, true>(p->bn_back, dY, Wd, d.inner, d.hidden, 0, bf16, p->sms, bp, {H, G, U}, p->gave_up, stream)
+                    : launch_pair<GatedBackOp<T>, true>(p->bn_back, dY, Wd, d.inner, d.hidden, 0, bf16, p->sms, bp, {H}, p->gave_up, stream);
 }
 
 }  // namespace
@@ -365,6 +366,7 @@ exo_gemm_status_t exo_ffn_create(exo_ffn_handle_t* out, const exo_ffn_desc_t* de
   p->ld_down = packed(d.ld_down, F);
   if (T > 0) {
     auto take = [&](int64_t values) { return (uint16_t*)p->mem.take(2 * values); };
+    p->gave_up = p->mem.take_word();
     p->h = take(T * p->ldh);
     if (d.training) p->dgu = take(T * p->ld2);
     if (d.ldx % 8) p->pack_x = take(T * p->ldx);
@@ -454,7 +456,7 @@ exo_gemm_status_t exo_ffn_check(exo_ffn_handle_t p) {
   if (!p) return EXO_GEMM_ERR_NULL;
   OnDevice on(p->device);
   if (on.err != cudaSuccess) return cuda_failed(on.err);
-  return check_products({p->down, p->dx, p->d_gate_up, p->d_down}, exo_fused_check());
+  return check_plan(p->gave_up, {p->down, p->dx, p->d_gate_up, p->d_down});
 }
 
 int64_t exo_ffn_workspace_bytes(exo_ffn_handle_t p) {

@@ -13,7 +13,7 @@
 // shared memory and TMA stores where their rows allow that (the pair kernel's Out; 8192 x 32000 x 4096 with the exponentials kept: 1432 us with
 // stores from registers, 1404), and rows that start anywhere are stored by neighbouring lanes (8 bits, 320 x 1865 x 3648: 34.5 us a row per lane, 18.1).
 //
-// Every wait is bounded: one that gives up records that, all roles leave their loops, tensor memory is freed and the kernel returns.
+// Every wait is bounded: one that gives up records that with its plan, all roles leave their loops, tensor memory is freed and the kernel returns.
 #pragma once
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -43,6 +43,11 @@ struct Fp16 {
   static __device__ __forceinline__ float2 unpack(uint32_t w) { return __half22float2(*reinterpret_cast<__half2*>(&w)); }
 };
 
+struct Waits {
+  uint64_t clocks;     // bound of every wait, in SM clocks
+  uint32_t* gave_up;   // the plan's count of waits that gave up; NULL for operators without a plan, which share their file's
+};
+
 struct CoreParams {
   int32_t M, N;        // rows of A, and columns of the result (columns of gate, for a gated product)
   int32_t nkb;         // k-blocks: 128 bytes of a row of A and of B
@@ -58,7 +63,7 @@ struct CoreParams {
   uint32_t idesc;
   OperandStaging a, b;
   Raster raster;
-  uint64_t wait_clocks;   // bound of every wait, in SM clocks
+  Waits waits;
   int32_t skip_copies;    // test hook: CTA 0 leaves out the copies of its first k-block
 };
 
@@ -89,31 +94,34 @@ EXO_CX int thin_smem(int stages, int per_stage, int b_rows, int a_rows, int afte
 }
 
 // ---------------------------------------------------------------- bounded waits
-static __device__ uint32_t fused_gave_up;   // one per translation unit: the number of waits that gave up
+// Waits that gave up in this translation unit's kernels on this device, whoever's they were (exo_fused_check).
+static __device__ uint32_t fused_gave_up;
 
-static __device__ __noinline__ bool wait_slow(uint32_t bar, uint32_t parity, uint64_t clocks) {
+static __device__ __noinline__ bool wait_slow(uint32_t bar, uint32_t parity, uint64_t clocks, uint32_t* gave_up) {
   const long long t0 = clock64();
+  uint32_t* const word = gave_up ? gave_up : &fused_gave_up;
   uint32_t n = 0;
   for (;;) {
     if (ptx::mbar_try_wait(bar, parity)) return true;
     if ((++n & 63u) == 0u) {
-      if (*(volatile uint32_t*)&fused_gave_up != 0u) return false;   // another role, or an earlier launch that nobody has asked about
+      if (*(volatile uint32_t*)word != 0u) return false;   // another role, or an earlier launch that nobody has asked about
       if ((uint64_t)(clock64() - t0) > clocks) {
-        atomicAdd(&fused_gave_up, 1u);
+        atomicAdd(word, 1u);
+        if (gave_up) atomicAdd(&fused_gave_up, 1u);
         return false;
       }
     }
   }
 }
-__device__ __forceinline__ bool wait_on(uint32_t bar, uint32_t parity, uint64_t clocks) {
+__device__ __forceinline__ bool wait_on(uint32_t bar, uint32_t parity, const Waits& w) {
 #pragma unroll 1
   for (int i = 0; i < 8; ++i)
     if (ptx::mbar_try_wait(bar, parity)) return true;
-  return wait_slow(bar, parity, clocks);
+  return wait_slow(bar, parity, w.clocks, w.gave_up);
 }
 // the same for a whole warp: true if no lane gave up
-__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, uint64_t clocks) {
-  return __all_sync(0xffffffffu, wait_on(bar, parity, clocks)) != 0;
+__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, const Waits& w) {
+  return __all_sync(0xffffffffu, wait_on(bar, parity, w)) != 0;
 }
 
 __device__ __forceinline__ uint64_t smem_desc(uint32_t addr, const OperandStaging& op) {
@@ -422,7 +430,7 @@ exo_fused_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
       const TileCoord tc = raster_decode(p.raster, t);
       const int32_t a0 = tc.m * 256 + (int32_t)rank * 128, b0 = tc.n * width + (int32_t)rank * p.b_split;
       for (int32_t kb = 0; kb < nkb; ++kb) {
-        ok = wait_warp(empty_bar(s), ph ^ 1u, p.wait_clocks);
+        ok = wait_warp(empty_bar(s), ph ^ 1u, p.waits);
         if (!ok) break;
         if (ptx::elect_one()) {
           if (rank == 0 && do_a) ptx::mbar_arrive_expect_tx(full_bar(s), stage_bytes * 2);
@@ -441,7 +449,7 @@ exo_fused_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
       }
     }
     for (uint32_t i = 0; i < stages && ok; ++i) {   // no stage release may still be on its way to this CTA
-      ok = wait_warp(empty_bar(s), ph ^ 1u, p.wait_clocks);
+      ok = wait_warp(empty_bar(s), ph ^ 1u, p.waits);
       if (++s == stages) { s = 0; ph ^= 1u; }
     }
   } else if (warp == 1) {
@@ -450,12 +458,12 @@ exo_fused_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
       uint32_t s = 0, ph = 0, acc = 0, acc_ph = 0;
       const uint32_t a_step = p.a.k_step_enc, b_step = p.b.k_step_enc, idesc = p.idesc;
       for (int64_t t = worker; t < tiles && ok; t += workers) {
-        ok = wait_warp(tempty_bar(acc), acc_ph ^ 1u, p.wait_clocks);   // both CTAs' epilogues have read it
+        ok = wait_warp(tempty_bar(acc), acc_ph ^ 1u, p.waits);   // both CTAs' epilogues have read it
         if (!ok) break;
         ptx::tc_fence_after_sync();
         const uint32_t d = tmem_base + acc * ACC;
         for (int32_t kb = 0; kb < nkb; ++kb) {
-          ok = wait_warp(full_bar(s), ph, p.wait_clocks);
+          ok = wait_warp(full_bar(s), ph, p.waits);
           if (!ok) break;
           ptx::tc_fence_after_sync();
           const uint64_t a_desc = smem_desc(stage0 + s * stage_bytes, p.a), b_desc = smem_desc(stage0 + s * stage_bytes + kATileBytes, p.b);
@@ -490,7 +498,7 @@ exo_fused_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
       out.rows = p.M - row0 < 32 ? p.M - row0 : 32;
       typename Op::template State<U> state;
       Op::template begin<U>(o, state, row, row < p.M, col, p.N);
-      ok = wait_warp(tfull_bar(acc), acc_ph, p.wait_clocks);
+      ok = wait_warp(tfull_bar(acc), acc_ph, p.waits);
       if (!ok) break;
       ptx::tc_fence_after_sync();
       // (Handed back only for a tile to come: an arrival that nobody waits for could reach a CTA that has gone.)
@@ -577,7 +585,7 @@ exo_fused_thin_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
     uint32_t s = 0, ph = 0;
     bool skip = p.skip_copies != 0 && blockIdx.x == 0;
     for (int32_t kb = kb_first; kb < nkb; kb += kb < whole ? (kb + per > whole ? whole - kb : per) : 1) {
-      ok = wait_warp(empty_bar(s), ph ^ 1u, p.wait_clocks);
+      ok = wait_warp(empty_bar(s), ph ^ 1u, p.waits);
       if (!ok) break;
       if (ptx::elect_one()) {
         const uint32_t dst = stage0 + s * stage_bytes, bar = full_bar(s);
@@ -604,7 +612,7 @@ exo_fused_thin_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
     const uint32_t a_step = p.a.k_step_enc, b_step = p.b.k_step_enc, idesc = p.idesc;
     for (int32_t kb = kb_first; kb < nkb;) {
       const int32_t blocks = kb < whole ? (kb + per > whole ? whole - kb : per) : 1;
-      ok = wait_warp(full_bar(s), ph, p.wait_clocks);
+      ok = wait_warp(full_bar(s), ph, p.waits);
       if (!ok) break;
       ptx::tc_fence_after_sync();
       const uint64_t b_desc = smem_desc(stage0 + s * stage_bytes, p.b), a_desc = smem_desc(stage0 + s * stage_bytes + a_at, p.a);
@@ -620,7 +628,7 @@ exo_fused_thin_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
       kb += blocks;
       if (++s == stages) { s = 0; ph ^= 1u; }
     }
-    ok = ok && wait_warp(tfull_bar, 0u, p.wait_clocks);
+    ok = ok && wait_warp(tfull_bar, 0u, p.waits);
   }
   const uint32_t quad = warp & 3u;
   const int32_t half = (int32_t)((warp - 2u) >> 2), row0 = (int32_t)quad * p.quad_rows, row = row0 + (int32_t)lane;

@@ -165,10 +165,10 @@ struct Result {
   int64_t cols, ld;
 };
 
-// A product of A (M rows) and B with operator Op.  b_mn: B lies K x N (N contiguous) instead of N x K.
+// A product of A (M rows) and B with operator Op.  b_mn: B lies K x N (N contiguous) instead of N x K.  gave_up: the plan's word, or NULL.
 template <class Op, bool B_MN>
 exo_gemm_status_t launch_pair(int bn, const Operand& A, const Operand& B, int64_t N, int64_t K, int64_t b_split, bool bf16, int sms,
-                              const typename Op::Params& op, std::initializer_list<Result> results, cudaStream_t stream) {
+                              const typename Op::Params& op, std::initializer_list<Result> results, uint32_t* gave_up, cudaStream_t stream) {
   constexpr int ES = Op::kInt8 ? 1 : 2, SUB_K = 128 / ES;
   const int width = Op::kGated ? bn / 2 : bn;
   CoreParams p{};
@@ -193,7 +193,7 @@ exo_gemm_status_t launch_pair(int bn, const Operand& A, const Operand& B, int64_
       !encode_operand_map(&mb, ES, bf16, B.base, (uint64_t)B.inner, (uint64_t)B.rows, (uint64_t)(B.ld * ES), B_MN ? 64u : (uint32_t)bn / 2))
     return EXO_GEMM_ERR_CUDA;
   const WaitHook hook = take_wait_hook();
-  p.wait_clocks = hook.clocks;
+  p.waits = Waits{hook.clocks, gave_up};
   p.skip_copies = hook.skip;
   OutMaps mo;
   memset(&mo, 0, sizeof mo);
@@ -208,7 +208,7 @@ exo_gemm_status_t launch_pair(int bn, const Operand& A, const Operand& B, int64_
 
 template <class Op, int U>
 exo_gemm_status_t launch_thin(int width, const Operand& A, const Operand& B, int64_t N, int64_t K, int64_t b_split, bool bf16,
-                              int sms, const typename Op::Params& op, cudaStream_t stream) {
+                              int sms, const typename Op::Params& op, uint32_t* gave_up, cudaStream_t stream) {
   constexpr int ES = Op::kInt8 ? 1 : 2, SUB_K = 128 / ES;
   constexpr int PARTS = Op::kGated ? 2 : 1;
   const int a_rows = (int)round_up(A.rows, 8);
@@ -247,7 +247,7 @@ exo_gemm_status_t launch_thin(int width, const Operand& A, const Operand& B, int
                          (uint32_t)p.per_stage))
     return EXO_GEMM_ERR_CUDA;
   const WaitHook hook = take_wait_hook();
-  p.wait_clocks = hook.clocks;
+  p.waits = Waits{hook.clocks, gave_up};
   p.skip_copies = hook.skip;
   typename Op::Params o = op;
   void* args[6] = {&ma, &ma_rest, &mb, &mb_rest, &p, &o};
@@ -278,6 +278,12 @@ struct Memory {
     bytes += n;
     return p;
   }
+  // a word of a plan's waits, clear when it returns
+  uint32_t* take_word() {
+    uint32_t* const p = (uint32_t*)take(sizeof(uint32_t));
+    if (p) err = clear_now(p, sizeof(uint32_t));
+    return p;
+  }
   void give_back() {
     for (int i = 0; i < count; ++i) cudaFree(parts[i]);
     count = 0;
@@ -294,8 +300,14 @@ static inline unsigned take_gave_up_here(cudaError_t* e) {
   if (*e == cudaSuccess && n) *e = cudaMemcpyToSymbol(fused_gave_up, &zero, sizeof zero);
   return n;
 }
-// exo_gemm_check of a plan's products
-inline exo_gemm_status_t check_products(std::initializer_list<exo_gemm_handle_t> plans, exo_gemm_status_t st) {
+// What exo_ffn_check and exo_ce_check do: the plan's own word, and exo_gemm_check of its products.  On the plan's device.
+inline exo_gemm_status_t check_plan(uint32_t* gave_up, std::initializer_list<exo_gemm_handle_t> plans) {
+  cudaError_t e = cudaDeviceSynchronize();
+  uint32_t n = 0;
+  if (e == cudaSuccess && gave_up) e = cudaMemcpy(&n, gave_up, sizeof n, cudaMemcpyDeviceToHost);
+  if (e == cudaSuccess && n) e = clear_now(gave_up, sizeof n);
+  if (e != cudaSuccess) return cuda_failed(e);
+  exo_gemm_status_t st = n ? EXO_GEMM_ERR_DEVICE_TIMEOUT : EXO_GEMM_OK;
   for (exo_gemm_handle_t g : plans)
     if (g) {
       const exo_gemm_status_t s = exo_gemm_check(g, nullptr);

@@ -447,11 +447,11 @@ exo_gemm_status_t exo_gemm_i8_run(const exo_i8_t* X, const exo_i8_t* W, void* Y,
   }
   I8Op::Params o{X->scales, W->scales, Y, ldy, (int32_t)N, y_dtype, align_of(Y, ldy * bytes), 0, alpha, beta};
   const Operand A{X->codes, M, K, X->ld}, B{W->codes, N, K, W->ld};
-  if (M <= kThinRows) return launch_thin<I8Op, 16>(thin_width(N, 16, 256, 1, M, sms), A, B, N, K, 0, false, sms, o, stream);
+  if (M <= kThinRows) return launch_thin<I8Op, 16>(thin_width(N, 16, 256, 1, M, sms), A, B, N, K, 0, false, sms, o, nullptr, stream);
   const int bn = pair_bn(M, N, false, 64, sms);
   o.tma = bytes == 2 && beta == 0.f && o.align >= 16 && N % 8 == 0;   // (nothing is written beyond a row's end)
-  return o.tma ? launch_pair<I8Op, false>(bn, A, B, N, K, 0, false, sms, o, {Result{Y, N, ldy}}, stream)
-               : launch_pair<I8Op, false>(bn, A, B, N, K, 0, false, sms, o, {}, stream);
+  return o.tma ? launch_pair<I8Op, false>(bn, A, B, N, K, 0, false, sms, o, {Result{Y, N, ldy}}, nullptr, stream)
+               : launch_pair<I8Op, false>(bn, A, B, N, K, 0, false, sms, o, {}, nullptr, stream);
 }
 
 }  // extern "C"

@@ -651,3 +651,40 @@ def test_ce_keeps_rare_columns_in_fp16():
     assert (p < 1e-7 * p.amax(1, keepdim=True)).double().mean() > 0.3
     c.check({"loss": bare["loss"], "lse": bare["lse"], "dx": (bare["dx"][0], bare["dx"][1] + (1 + 2.0 ** -10) * (kept @ c.w.double().abs())),
              "dw": (bare["dw"][0], bare["dw"][1] + kept.t() @ c.x.double().abs())})
+
+
+@pytest.mark.parametrize("T", [4, 200])
+def test_a_wait_that_runs_out_is_its_own_plans(T):
+    """Of two plans, the one whose wait ran out reports that, whoever is asked first; the other's results are right and it reports nothing."""
+    for first in (0, 1):
+        pair = [Ffn(T, 264, 136, "bf16", "silu", True, seed=s) for s in (1, 2)]
+        heads = [Ce(T, 264, 515, "bf16", True, seed=s) for s in (1, 2)]
+        for broken, well, want in (pair + [lambda o: R.check(o.y, o.want(False)["y"])], heads + [lambda o: R.check(o.lse, o.want(False)["lse"])]):
+            well.forward()
+            torch.cuda.synchronize()
+            assert E.exo_fused_debug_set(20, 1) == E.OK
+            broken.forward()
+            well.forward()
+            for o in ((broken, well), (well, broken))[first]:
+                if o is broken:
+                    with pytest.raises(E.ExoGemmError) as e:
+                        o.plan.check()
+                    assert e.value.status == 7
+                else:
+                    o.plan.check()
+                    want(o)
+            broken.forward()          # it has been asked: the next call is as good as any
+            broken.plan.check()
+            want(broken)
+        assert E.exo_fused_check() == 7 and E.exo_fused_check() == E.OK   # of the device, since it was asked last
+
+
+def test_a_wait_of_an_8_bit_product_is_no_plans():
+    f = Ffn(40, 264, 136, "bf16", "silu", False, seed=1)
+    (_, _, X), (_, _, W) = codes_of(5, 640, gen(1)), codes_of(33, 640, gen(2))
+    y = torch.zeros(5, 33, device="cuda")
+    assert E.exo_fused_debug_set(20, 1) == E.OK
+    W.gemm(X, y.data_ptr(), 33, E.FP32, stream=stream())
+    f.forward(saved=False)
+    f.check_forward(f.want(False))
+    assert E.exo_fused_check() == 7 and E.exo_fused_check() == E.OK
