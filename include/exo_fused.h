@@ -151,8 +151,8 @@ exo_gemm_status_t exo_ce_forward(exo_ce_handle_t plan, const void* x, const void
  *
  *   d_iv = dloss_i * (exp(l_iv - lse_i) - (1 - s) * [v == t_i] - s / vocab),    dx_i = sum_v d_iv w_v,    dW_v = sum_i d_iv x_i
  *
- * saved: what the forward call of the same x and W left (it is overwritten: one backward call per forward call); not read if
- * exo_ce_saved_bytes is 0.  dx or dW may be NULL: not wanted.  accumulate != 0 adds dW onto what is there.  d_iv is scaled to the range of dtype by the
+ * saved: what the forward call of the same x and W left (it is overwritten: one backward call per forward call; a second one, or one
+ * without its forward call, finds that and gives NaN); not read if exo_ce_saved_bytes is 0.  dx or dW may be NULL: not wanted.  accumulate != 0 adds dW onto what is there.  d_iv is scaled to the range of dtype by the
  * largest finite |dloss_i|, rounded to dtype as the operand of both products (a kept exponential is rounded before that too), and the
  * scale is taken back in fp32; dx is summed in fp32 over all pieces.  Outputs must not overlap inputs or each other.
  */

@@ -162,11 +162,15 @@ struct GradOp {
   static __device__ __forceinline__ void end(const Params&, State<U>&, int, bool, int) {}
 };
 
+// What a forward call leaves at the end of `saved`, and the backward call that uses `saved` up takes away.
+constexpr uint32_t kMark = 0x6B657074u;
+
 // ---------------------------------------------------------------- rows from their parts
 struct JoinParams {
   const float *top, *sum, *all, *hit;
   const int64_t* target;
   float *loss, *lse;
+  uint32_t* mark;           // of `saved`, or NULL
   int64_t rows, vocab, ignore;
   int32_t parts;
   float smoothing;
@@ -181,6 +185,7 @@ __global__ void __launch_bounds__(kJoinThreads) exo_ce_join_kernel(const JoinPar
   ptx::grid_dependency_wait();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int64_t row = (int64_t)blockIdx.x * 32 + lane;
+  if (p.mark && blockIdx.x == 0 && threadIdx.x == 0) *p.mark = kMark;
   float top = -INFINITY, sum = 0.f, all = 0.f;
   if (row < p.rows) {
     // eight parts at a time: their loads are independent
@@ -240,6 +245,7 @@ struct ScaleParams {
   const float* dloss;
   const int64_t* target;
   float *q, *factor;
+  uint32_t* mark;           // of `saved`, or NULL
   int64_t rows, vocab, ignore;
 };
 constexpr int kScaleThreads = 1024;
@@ -251,6 +257,7 @@ __global__ void __launch_bounds__(kScaleThreads) exo_ce_scale_kernel(const Scale
     const int64_t t = p.target[i];
     return t >= 0 && t < p.vocab && t != p.ignore ? p.dloss[i] : 0.f;
   };
+  const bool stale = p.mark && *p.mark != kMark;   // `saved` holds no exponentials (any more): nothing that looks like a gradient comes of it
   float top = 0.f;
   for (int64_t i = threadIdx.x; i < p.rows; i += kScaleThreads) {
     const float d = fabsf(of(i));
@@ -268,8 +275,11 @@ __global__ void __launch_bounds__(kScaleThreads) exo_ce_scale_kernel(const Scale
   if (top > 0.f) frexpf(top, &e);   // 2^(e - 1) <= top < 2^e
   e = e < -100 ? -100 : e;          // e <= 128: both factors are normal numbers, between 2^-114 and 2^114
   const float up = ldexpf(kTop, -e), down = ldexpf(1.f / kTop, e);
-  if (threadIdx.x == 0) *p.factor = down;
-  for (int64_t i = threadIdx.x; i < p.rows; i += kScaleThreads) p.q[i] = of(i) * up;
+  if (threadIdx.x == 0) {
+    *p.factor = down;
+    if (p.mark) *p.mark = 0u;   // (every thread has read it)
+  }
+  for (int64_t i = threadIdx.x; i < p.rows; i += kScaleThreads) p.q[i] = stale ? NAN : of(i) * up;
 }
 
 // ---------------------------------------------------------------- d of the kept part, in place
@@ -393,8 +403,10 @@ void release(exo_ce_plan* p) {
 
 bool placed(const void* m, int64_t ld) { return ((uintptr_t)m & (ld % 8 ? 1u : 15u)) == 0; }
 
-// bytes of the kept exponentials; the parts' largest logits follow them
+// bytes of the kept exponentials; the parts' largest logits follow them, and the mark
 int64_t kept_bytes(const exo_ce_plan* p) { return round_up(p->d.tokens * p->lde * 2, 256); }
+constexpr int64_t kMarkBytes = 16;
+uint32_t* mark_of(const exo_ce_plan* p, void* saved) { return (uint32_t*)((char*)saved + kept_bytes(p) + 4 * p->d.tokens * p->parts); }
 
 template <class T>
 exo_gemm_status_t forward(exo_ce_plan* p, const void* x, const void* W, const int64_t* target, void* saved, cudaStream_t stream) {
@@ -484,7 +496,7 @@ exo_gemm_status_t exo_ce_create(exo_ce_handle_t* out, const exo_ce_desc_t* desc)
   p->ldw = d.ldw % 8 ? round_up(H, 64) : d.ldw;
   p->lde = p->ldd = 64;
   if (d.training && T > 0) {
-    const int64_t most = (d.keep_bytes < 0 ? kKeepBytes : d.keep_bytes) - 4 * T * p->parts - 256;
+    const int64_t most = (d.keep_bytes < 0 ? kKeepBytes : d.keep_bytes) - 4 * T * p->parts - kMarkBytes - 256;
     p->keep = most <= 0 ? 0 : most / (2 * T) / 64 * 64;   // (rows of a multiple of 64)
     if (p->keep >= round_up(V, 64)) p->keep = V;
     else p->keep = p->keep / p->width * p->width;   // whole tiles of the forward product, less than V of them
@@ -534,7 +546,7 @@ exo_gemm_status_t exo_ce_create(exo_ce_handle_t* out, const exo_ce_desc_t* desc)
   return EXO_GEMM_OK;
 }
 
-int64_t exo_ce_saved_bytes(exo_ce_handle_t p) { return p && p->keep > 0 ? kept_bytes(p) + 4 * p->d.tokens * p->parts : 0; }
+int64_t exo_ce_saved_bytes(exo_ce_handle_t p) { return p && p->keep > 0 ? kept_bytes(p) + 4 * p->d.tokens * p->parts + kMarkBytes : 0; }
 
 exo_gemm_status_t exo_ce_forward(exo_ce_handle_t p, const void* x, const void* W, const int64_t* target, float* loss, float* lse, void* saved,
                                  void* cuda_stream) {
@@ -559,6 +571,7 @@ exo_gemm_status_t exo_ce_forward(exo_ce_handle_t p, const void* x, const void* W
   JoinParams j{};
   j.top = saved ? (const float*)((const char*)saved + kept_bytes(p)) : p->top;
   j.sum = p->sum; j.all = p->all; j.hit = p->hit; j.target = target; j.loss = loss; j.lse = lse;
+  j.mark = saved ? mark_of(p, saved) : nullptr;
   j.rows = d.tokens; j.vocab = d.vocab; j.ignore = d.ignore_index; j.parts = p->parts; j.smoothing = d.label_smoothing;
   void* args[1] = {&j};
   return launch_args((void*)exo_ce_join_kernel, dim3((unsigned)((d.tokens + 31) / 32)), kJoinThreads, 0, 1, s, args);
@@ -588,7 +601,7 @@ exo_gemm_status_t exo_ce_backward(exo_ce_handle_t p, const void* x, const void* 
   if (p->pack_x) x = p->pack_x;
   if (p->pack_w) W = p->pack_w;
 
-  ScaleParams sp{dloss, target, p->q, p->factor, d.tokens, d.vocab, d.ignore_index};
+  ScaleParams sp{dloss, target, p->q, p->factor, p->keep > 0 ? mark_of(p, saved) : nullptr, d.tokens, d.vocab, d.ignore_index};
   void* scale_args[1] = {&sp};
   if ((st = launch_args((void*)exo_ce_scale_kernel, dim3(1), kScaleThreads, 0, 1, s, scale_args)) != EXO_GEMM_OK) return st;
 

@@ -688,3 +688,22 @@ def test_a_wait_of_an_8_bit_product_is_no_plans():
     f.forward(saved=False)
     f.check_forward(f.want(False))
     assert E.exo_fused_check() == 7 and E.exo_fused_check() == E.OK
+
+
+@pytest.mark.parametrize("T,keep", [(40, -1), (200, 300000)])
+def test_ce_second_backward_is_not_taken_for_a_gradient(T, keep):
+    """The kept exponentials serve one backward call: a second one, or one without its forward call, gives NaN and no numbers."""
+    c = Ce(T, 72, 1003, "bf16", True, keep=keep, piece=256, seed=16)
+    assert 0 < c.plan.saved_bytes() and (keep < 0 or c.plan.saved_bytes() <= keep)
+    c.forward(saved=False)
+    c.backward()                       # nothing has been left in `saved`
+    assert c.dx.isnan().all() and c.dw.isnan().all()
+    c.forward()
+    c.backward()
+    c.check(c.want(True))
+    dx, dw = c.dx.clone(), c.dw.clone()
+    c.backward()
+    assert c.dx.isnan().all() and c.dw.isnan().all()
+    c.forward()
+    c.backward()
+    assert torch.equal(c.dx, dx) and torch.equal(c.dw, dw)
