@@ -16,10 +16,10 @@ SHARE_DIR = os.path.join(CSRC, "cluster4")
 SHARE_LIB = os.path.join(HERE, "libexo_gemm_cluster4.so")
 SHARE_DEPS = [os.path.join("cluster4", "share_pairs.cuh")]
 SOURCES = ["api.cu", "gemv.cu", "q4.cu", "moe.cu", "ffn.cu", "ce.cu", "i8.cu"]
-DEPS = ["api.cu", "gemv.cu", "gemm_kernel.cuh", "gemm_params.h", "plan.h", "ptx.cuh", "tile_scheduler.h",
-        "q4.cu", "moe.cu", "decode_core.cuh", "decode_host.h", "ffn.cu", "ce.cu", "i8.cu", "fused_core.cuh", "fused_host.h",
-        os.path.join("..", "..", "include", "exo_gemm.h"), os.path.join("..", "..", "include", "exo_decode.h"),
-        os.path.join("..", "..", "include", "exo_fused.h")]
+INCLUDE = os.path.join(os.path.dirname(HERE), "include")
+# what a library is older than when it has to be built again: every source and header (paths from CSRC)
+DEPS = sorted([f for f in os.listdir(CSRC) if f.endswith((".cu", ".cuh", ".h"))] +
+              [os.path.join("..", "..", "include", f) for f in os.listdir(INCLUDE) if f.endswith(".h")])
 
 
 def nvcc_path() -> str:

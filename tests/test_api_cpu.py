@@ -487,3 +487,27 @@ def test_smoke_cases_are_in_the_supported_set():
         d = harness.desc_of(p)
         assert B.exo_gemm_validate(d) == B.OK, p.name
         assert B.exo_gemm_plan_preview(d, 148)[0] == B.OK, p.name
+
+
+def test_a_change_of_any_included_file_makes_the_library_stale(tmp_path, monkeypatch):
+    from paper_2609_16389_b200 import build as cuda_build
+    known = {os.path.realpath(os.path.join(cuda_build.CSRC, d)) for d in cuda_build.DEPS}
+    extra = {os.path.realpath(os.path.join(cuda_build.CSRC, d)) for d in cuda_build.SHARE_DEPS}
+    files, seen = [os.path.join(cuda_build.CSRC, s) for s in cuda_build.SOURCES], set()
+    while files:      # every file that a source includes by name, and what those include
+        at = os.path.realpath(files.pop())
+        if at in seen:
+            continue
+        seen.add(at)
+        files += [os.path.join(os.path.dirname(at), name) for name in re.findall(r'^\s*#include "([^"]+)"', open(at).read(), flags=re.M)]
+    assert len(seen) > 20 and seen <= known | extra, sorted(seen - known - extra)
+    # each of them, and nothing else, decides
+    lib = tmp_path / "lib.so"
+    lib.write_bytes(b"")
+    for d in cuda_build.DEPS:
+        path = os.path.realpath(os.path.join(cuda_build.CSRC, d))
+        times = {p: 100.0 for p in known} | {os.path.realpath(lib): 200.0}
+        monkeypatch.setattr(os.path, "getmtime", lambda p, t=times: t[os.path.realpath(p)])
+        assert not cuda_build.is_stale(str(lib))
+        times[path] = 300.0
+        assert cuda_build.is_stale(str(lib)), d
