@@ -707,3 +707,61 @@ def test_ce_second_backward_is_not_taken_for_a_gradient(T, keep):
     c.forward()
     c.backward()
     assert torch.equal(c.dx, dx) and torch.equal(c.dw, dw)
+
+
+# ---------------------------------------------------------------- values where functions saturate
+@pytest.mark.parametrize("T", [20, 130])
+@pytest.mark.parametrize("act", ACT)
+def test_ffn_values_in_the_gates_tails(act, T):
+    """Gates far in both tails, exact since a token has a single value, 1: there act is g or 0 and its slope 1 or 0, also where exponentials, and
+    the cube of a gate, overflow."""
+    H, F = 64, 72
+    f = Ffn(T, H, F, "bf16", act, True, "fp32", seed=2)
+    at = torch.arange(T, device="cuda")
+    f.x.zero_()
+    f.x[at, at % H] = 1
+    g0 = gen(3)
+    f.gate_up[:F] = torch.sign(torch.randn(F, H, device="cuda", generator=g0)) * 2.0 ** torch.randint(7, 10, (F, H), device="cuda", generator=g0)
+    if act == "gelu_tanh":
+        f.gate_up[:F] *= 2.0 ** 50
+    f.forward()
+    f.backward()
+    f.plan.check()
+    dt = f.x.dtype
+    g, u = (w[:, at % H].t().double() for w in (f.gate_up[:F], f.gate_up[F:]))
+    up = (g > 0).double()
+    # a sigmoid next to 1 may be a step of fp32 off, which its factor g multiplies in the slope
+    a, slope = (g * up, R.FUNCTION * g * up), (up, R.FUNCTION * (1 + g.abs().clamp(max=1024.0) * up))
+    X, Wg, Wu, Wd, dY, U = R.exactly(f.x), R.exactly(f.gate_up[:F]), R.exactly(f.gate_up[F:]), R.exactly(f.down), R.exactly(f.dy), R.exactly(u)
+    h = R.rounded(R.product(a, U), dt)
+    R.check(f.y, R.rounded(R.matmul(h, R.turned(Wd)), dt), "y")
+    dh = R.matmul(dY, Wd)
+    dg, du = R.rounded(R.product(R.product(dh, U), slope), dt), R.rounded(R.product(dh, a), dt)
+    dx = R.plus(R.matmul(dg, Wg), R.matmul(du, Wu))
+    m = (dg[0].abs() + dg[1]) @ Wg[0].abs() + (du[0].abs() + du[1]) @ Wu[0].abs()
+    R.check(f.dx, R.rounded((dx[0], dx[1] + 2 * F * 2.0 ** -23 * m), dt), "dx")   # one sum of 2 F products
+    dgu = [R.matmul(R.turned(t), X) for t in (dg, du)]
+    R.check(f.dgate_up, (torch.cat([t[0] for t in dgu]), torch.cat([t[1] for t in dgu])), "dgate_up")
+    R.check(f.ddown, R.matmul(R.turned(dY), h), "ddown")
+    assert (f.dgate_up[:F][(f.gate_up[:F] < 0) & (torch.arange(H, device="cuda") < T)] == 0).all()   # nothing flows through a closed gate
+
+
+@pytest.mark.parametrize("T,keep", [(100, -1), (140, -1), (140, 0)])
+def test_ce_gradients_of_large_logits(T, keep):
+    """Logits of some thousands: a row's gradient is at its target and its largest column, and nowhere where these are one."""
+    c = Ce(T, 64, 1000, "bf16", True, spread=400.0, grad="fp32", keep=keep, piece=256, seed=7)
+    at = torch.arange(T, device="cuda")
+    c.x.zero_()
+    c.x[at, at % 64] = 32
+    l = c.x.double() @ c.w.double().t()
+    c.target[::2] = l.argmax(1)[::2]
+    c.forward()
+    c.backward()
+    want = c.want(True)
+    # an exponential below fp32's smallest normal number, 2^-126, may be lost: that much of every column, times the row's |dloss|
+    lost = (c.dloss.double()[:, None] * 2.0 ** -126).expand(T, 1000)
+    want["dx"] = want["dx"][0], want["dx"][1] + lost @ c.w.double().abs()
+    want["dw"] = want["dw"][0], want["dw"][1] + lost.t() @ c.x.double().abs()
+    c.check(want)
+    d = torch.softmax(l, 1) - torch.nn.functional.one_hot(c.target, 1000)
+    assert l.abs().max() > 4000 and (d.abs().sum(1) > 1.9).any() and (d.abs().sum(1) < 1e-6).any()
