@@ -765,3 +765,53 @@ def test_ce_gradients_of_large_logits(T, keep):
     c.check(want)
     d = torch.softmax(l, 1) - torch.nn.functional.one_hot(c.target, 1000)
     assert l.abs().max() > 4000 and (d.abs().sum(1) > 1.9).any() and (d.abs().sum(1) < 1e-6).any()
+
+
+# ---------------------------------------------------------------- several tiles to a pair of CTAs
+# On 148 SMs (74 pairs) these take tiles of 64 to 256 columns, up to thirteen to a pair: both accumulators and their hand-over, rings that run on
+# from tile to tile, bands of several tile columns, results whose buffers are used again.
+@pytest.mark.parametrize("T,H,F,dtype,act,grad", [
+    (600, 264, 3104, "bf16", "silu", "same"),        # 147 tiles of 128 gated columns
+    (900, 136, 9541, "fp16", "gelu", "fp32"),        # 400 of 192, rows of odd length; 152 of 256 in the backward pass
+    (1100, 200, 11456, "bf16", "gelu_tanh", "fp32"),  # 450 of 256
+    (1300, 136, 6254, "fp16", "silu", "same"),       # 294 of 128 in the backward pass
+    (2600, 72, 774, "bf16", "silu", "fp32")])        # many rows, few columns
+def test_ffn_many_tiles(T, H, F, dtype, act, grad):
+    f = Ffn(T, H, F, dtype, act, True, grad, seed=F)
+    f.forward()
+    f.backward()
+    want = f.want(True)
+    f.check_forward(want)
+    f.check_backward(want)
+
+
+@pytest.mark.parametrize("T,H,V,dtype,smoothing,keep,piece", [
+    (600, 136, 6254, "bf16", 0.1, -1, 0),            # 147 tiles of 128
+    (900, 72, 9541, "fp16", 0.0, -1, 0),             # 200 of 192
+    (1100, 136, 40003, "bf16", 0.0, -1, 0),          # 785 of 256
+    (1100, 136, 40003, "fp16", 0.1, 0, 20000),       # pieces of several tiles to a pair
+    (900, 264, 23000, "bf16", 0.0, 12000000, 9541)])  # a part kept, the rest recomputed
+def test_ce_many_tiles(T, H, V, dtype, smoothing, keep, piece):
+    c = Ce(T, H, V, dtype, True, smoothing, grad="fp32", keep=keep, piece=piece, seed=V)
+    c.target[::5] = -100
+    c.forward()
+    c.backward()
+    c.check(c.want(True))
+
+
+@pytest.mark.parametrize("M,N,K", [(600, 6254, 200), (900, 9544, 130), (1100, 11460, 1040), (2600, 1030, 272)])
+def test_i8_many_tiles(M, N, K):
+    g = gen(N)
+    (xc, xs, X), (wc, ws, W) = codes_of(M, K, g), codes_of(N, K, g)
+    real = (xc[:, :K].double() @ wc[:, :K].double().t()) * xs.double()[:, None] * ws.double()[None]
+    bound = 4 * 2.0 ** -24 * real.abs()   # the sum's conversion and three products
+    for out, code in ((torch.bfloat16, E.BF16), (torch.float32, E.FP32)):
+        for ldy in (N, (N + 31) // 32 * 32 + 32):     # rows that start anywhere, and on 16 bytes
+            y0, y = strided(M, N, out, None, ldy, fill=7.0)
+            W.gemm(X, y0.data_ptr(), ldy, code, 1.0, 0.0, stream())
+            R.check(y, R.rounded((real, bound), out))
+            assert (y0[:, N:] == 7.0).all() and (y0[M:] == 7.0).all()
+            W.gemm(X, y0.data_ptr(), ldy, code, 1.0, 0.5, stream())
+            twice = 1.5 * real, 6 * 2.0 ** -24 * 1.5 * real.abs() + (0.5 * R.half_step(out) * 1.01 * real.abs())   # beta times the rounded result
+            R.check(y, R.rounded(twice, out))
+    assert E.exo_fused_check() == E.OK
