@@ -10,9 +10,9 @@ namespace fused {
 namespace {
 
 // ---------------------------------------------------------------- quantisation
-// A row's largest magnitude, then its codes, from registers.  For many rows a warp takes a row and memory bounds the kernel (2 + 1 bytes a
-// value), if a value costs no more than about ten instructions; for few rows a CTA takes one, and the latencies of a load, a reduction and a
-// store are what is left.
+// A row's largest magnitude, then its codes, from registers.  For many rows what bounds the kernel is the instructions per value (4096 x 4096 bf16,
+// 128 threads a row: 14.7 us, issue slots 61 % busy, where 2 + 1 bytes a value would take 7.7); for few rows a CTA of 512 takes one, and the
+// latencies of a load, a reduction and a store are what is left.
 struct QuantParams {
   const void* x;
   int64_t ldx;
@@ -96,7 +96,8 @@ struct Divider {
   }
 };
 
-// V: values per load, as many as 16 bytes hold where the rows' addresses allow that.  THREADS per row: a warp, or a CTA.  A thread keeps its
+// V: values per load, as many as 16 bytes hold where the rows' addresses allow that.  THREADS per row: a CTA of 512 for few rows, of 128 for many,
+// a warp where a row has 1024 values at most.  A thread keeps its
 // first HELD loads in registers, further ones are read again, from L1 or L2.  (A warp that keeps a row is so much code that fetching it takes
 // longer than reading twice: 4096 x 4096 bf16, 16 loads kept 35 us.)
 constexpr int kQuantWarps = 8;   // rows of a CTA, a warp each
